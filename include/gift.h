@@ -55,6 +55,8 @@ extern "C" {
 #define GIFT_ST_NO_KEY          8u   /* the owner has no key in the ctx */
 #define GIFT_ST_BAD_DESC       16u   /* descriptor misaligned, out of range, or reserved flags set */
 #define GIFT_ST_OVERLAP        32u   /* shares bytes with another segment of the call (only with GIFT_CTX_CHECK_OVERLAP) */
+#define GIFT_ST_NO_BLOCKS      64u   /* block tables: the free pages do not reach to this request */
+#define GIFT_ST_BAD_TABLE     128u   /* the call as a whole was refused: free pages, tables or row count malformed */
 
 #define GIFT_OWNER_PARAM     (-1)
 #define GIFT_OWNER_NONE      (-2)
@@ -466,6 +468,138 @@ int gift_import_from_host(gift_ctx* ctx, const void* h_src, const uint8_t* h_tag
                           const gift_seg* segs, uint32_t nseg, const gift_chunk* chunks, uint32_t n_chunks,
                           const gift_pages* pages, gift_labels* labels, uint8_t* d_tags, uint32_t* d_status,
                           uint32_t* h_status, void* stream);
+
+/* ------------------------------------------------------------------------------------------
+ * The paged cache between the boundary calls: from the lengths of a step's requests to block
+ * tables, slots, written pages, attention over them, and the segment table that exports them
+ * (paper sec. 4.2 and 4.5 on KV blocks and their index tables; sec. 4.3, rule step 5, for the
+ * reading side).  Nothing here waits for the device or copies to the host, so a step can be
+ * captured in a graph; no array but those named is kept by a call.
+ *
+ * gift_batch: the requests of one step (host structure, device arrays).  Request r has owner[r]
+ * in [0, 2^20), have[r] tokens cached before the step and want[r] after it; its block table is
+ * table[r*max_blocks ..]: entry j is the physical page of its tokens [j*page_tokens,
+ * (j+1)*page_tokens).  The step's rows are the want - have tokens of every request that grows,
+ * request by request.  A request with a negative length, an owner out of range, or a length
+ * that max_blocks blocks do not hold is malformed: it has no rows and no blocks.
+ * n_req <= GIFT_MAX_REQS, page_tokens <= GIFT_MAX_PAGE_TOKENS, n_pages * page_tokens < 2^31. */
+#define GIFT_MAX_REQS         8192u
+#define GIFT_MAX_PAGE_TOKENS 65536u
+#define GIFT_MAX_LAYERS       1024u
+#define GIFT_MAX_HEADS        1024u
+typedef struct {
+    uint32_t n_req, max_blocks, page_tokens, n_pages;
+    const int32_t* owner;
+    const int32_t* have;
+    const int32_t* want;
+    int32_t* table;
+} gift_batch;
+
+/* Block tables from request lengths.  free_pages[0 .. *n_free-1] (device; room for free_cap) is
+ * a stack of free pages; owner_map[l*n_pages + p] the label of page p in layer l, for `layers`
+ * layers that share the page numbers.  A request whose want needs more blocks than its have
+ * takes pages from the top of the stack, in request order; the pages become its owner's in
+ * every layer and are entered in its table.  It is served when the pages that it and all
+ * requests before it need are there, else its table stays as it was and status[r] is
+ * GIFT_ST_NO_BLOCKS.  A request whose want needs fewer blocks gives the others back: their
+ * entries become -1, their labels GIFT_OWNER_NONE, and they go on the stack behind what was
+ * taken.  Malformed requests: GIFT_ST_BAD_DESC.  The stack and the tables may come from the
+ * untrusted framework: if a page that would change hands is out of range, is named twice,
+ * is taken while a layer's label is not NONE, or given back while it is another user's or a
+ * parameter's, or if *n_free is out of range or the stack has no room, the call as a whole is
+ * refused: status is GIFT_ST_BAD_TABLE for every request and nothing else changes.  Labels must be
+ * user ids or the special labels.  status: one word per request. */
+int gift_block_tables(gift_ctx* ctx, const gift_batch* batch, int32_t* free_pages, uint32_t free_cap, int32_t* n_free,
+                      int32_t* owner_map, uint32_t layers, uint32_t* status, void* stream);
+
+/* Where the step's rows go: for row t = (request r, its i-th new token), slots[t] = page *
+ * page_tokens + offset of position have[r] + i, and, where the pointers are not NULL,
+ * row_req[t] = r, row_pos[t] = the position, row_owner[t] = owner[r] (the row labels that the
+ * flow rules take), row_ptr[r] = first row of r (n_req + 1 entries, the rows' CSR pointer) and
+ * total[0] = number of rows.  With rel (n_rows entries, or NULL) row t goes to position have[r]
+ * + rel[t] instead of + i: the rows of a drafted tree that were accepted, moved up behind the
+ * cached tokens; rel[t] outside [0, want - have) means not at all.  slots[t] and row_pos[t] are -1
+ * for such a row; slots[t] is -1 where the table has no page in range.  Rows from the last one
+ * to n_rows are padding: -1 everywhere, row_owner GIFT_OWNER_NONE.  If the step has more than
+ * n_rows rows, all rows are padding and row_ptr is all 0. */
+int gift_slot_map(gift_ctx* ctx, const gift_batch* batch, const int32_t* rel, uint32_t n_rows, int64_t* slots,
+                  int32_t* row_req, int32_t* row_pos, int32_t* row_owner, int32_t* row_ptr, int64_t* total, void* stream);
+
+/* The segment table that hands the requests' blocks to gift_seg_encrypt: one paged segment per
+ * (layer, request, block), layers outermost, each its block's filled bytes (token_bytes per
+ * token), so that what a page held before is never exported under a new owner's key.  Segment e
+ * has owner[r], nonce LE32(serial[r]) || LE32(layer) || LE32(block), page0 = e, and page_table[e]
+ * = layer * n_pages + page (-1, which the segment calls refuse, where the table has no page in
+ * range).  serial[r] must be new for every export of a key: the library does not check nonces.
+ * flags:
+ *   GIFT_KV_WHOLE_PAGES  len is the whole page even where the last block is part full
+ *   GIFT_KV_NEW_BLOCKS   only the blocks that hold tokens from have on (default: all of want)
+ * segs and page_table have cap entries; those behind the last segment carry a reserved flag, so
+ * that the segment calls refuse them.  total[0] (or NULL) receives the number of segments; if
+ * it exceeds cap, no segment is written (every entry is such a refused one). */
+#define GIFT_KV_WHOLE_PAGES 1u
+#define GIFT_KV_NEW_BLOCKS  2u
+int gift_kv_segments(gift_ctx* ctx, const gift_batch* batch, const uint32_t* serial, uint32_t layers, uint64_t token_bytes,
+                     uint32_t flags, gift_seg* segs, int32_t* page_table, uint32_t cap, int64_t* total, void* stream);
+
+/* One layer's pages: pages[n_pages][page_tokens][2][n_heads][head_dim], K before V, 16-byte
+ * aligned; head_dim a multiple of 8.  owner_map: one label per page, or NULL to skip label
+ * handling.  Host structure. */
+#define GIFT_BF16 0u
+#define GIFT_FP16 1u
+typedef struct {
+    void* pages;
+    uint32_t n_pages, page_tokens, n_heads, head_dim, dtype;
+    const int32_t* owner_map;
+} gift_kv_pool;
+
+/* Write K and V rows into pages.  Row t, head h of k starts at k + t*k_row_stride +
+ * h*k_head_stride elements (multiples of 8, 16-byte aligned); head_dim elements are contiguous.
+ * The row is written to slots[t] if the page's label is row_owner[t].  status[t]: 0,
+ * GIFT_ST_OWNER_MISMATCH (another user's or a parameter's page), GIFT_ST_UNOWNED (NONE or CONFLICT),
+ * GIFT_ST_BAD_DESC (slot out of range); then nothing is written.  Slot -1 is a row that goes nowhere
+ * (status 0).  The slots of a call must be distinct; if two rows name one slot, it receives
+ * bytes of either. */
+int gift_kv_append(gift_ctx* ctx, const gift_kv_pool* pool, const void* k, uint64_t k_row_stride, uint64_t k_head_stride,
+                   const void* v, uint64_t v_row_stride, uint64_t v_head_stride, uint32_t n_rows, const int64_t* slots,
+                   const int32_t* row_owner, uint32_t* status, void* stream);
+
+/* Attention of the step's rows over the paged cache, the step's own tokens (already appended)
+ * included.  Row i of request r sees the cached tokens at positions < have[r] and of the step's
+ * tokens those whose bit is set in tree_mask (mask_words words of 32 bits per row; bit j is token
+ * have[r] + j, the row's own bit like any other), or, with tree_mask NULL, tokens 0 .. i.  One
+ * row per request is the decode form.  For query head h (n_heads, a multiple of the pool's; head
+ * h reads K/V head h / (n_heads / pool heads)):
+ *   out = sum_t p_t v_t / sum_t p_t,  p_t = exp(scale * q . k_t - max),  lse = max + log sum p_t
+ * over the visible tokens; scores, sums and the running maximum are 32-bit, p is rounded to the
+ * pool's type for the product with v.  A row that sees nothing (or only scores of minus
+ * infinity) is zero with lse minus infinity.  What a hidden token holds, infinities and NaN
+ * included, does not reach a row.
+ * The rule of this launch (sec. 4.3 step 5) is checked on the block table that is read: every page
+ * that holds a token of the request must be its owner's or a parameter's (a shared prefix).
+ * Else the request is refused: its rows are zero, lse minus infinity, row_owner
+ * GIFT_OWNER_CONFLICT, and status[r] has GIFT_ST_OWNER_MISMATCH and / or GIFT_ST_UNOWNED, or GIFT_ST_BAD_DESC
+ * alone (a page out of range, a malformed request, more step tokens than mask bits).  row_owner
+ * and lse may be NULL.  If the step has more than n_rows rows, status is GIFT_ST_BAD_TABLE for every
+ * request and nothing else is written.  Rows behind the last one are left as they were.
+ * q, out: like k in gift_kv_append, in the pool's type; out must overlap no input.  head_dim is
+ * 64 or 128.  lse: n_rows x n_heads floats.  The first call on a ctx allocates a fixed scratch
+ * (about 80 MB); make it before any stream capture begins.  Graphs that were captured from one
+ * ctx must not run at the same time. */
+typedef struct {
+    const void* q;
+    uint64_t q_row_stride, q_head_stride;
+    void* out;
+    uint64_t out_row_stride, out_head_stride;
+    uint32_t n_rows, n_heads;
+    float scale;
+    const uint32_t* tree_mask;
+    uint32_t mask_words;
+    float* lse;
+    int32_t* row_owner;
+} gift_attn;
+int gift_kv_attention(gift_ctx* ctx, const gift_batch* batch, const gift_kv_pool* pool, const gift_attn* attn,
+                      uint32_t* status, void* stream);
 
 #ifdef __cplusplus
 }

@@ -17,10 +17,13 @@ LIB_PATH = os.environ.get("GIFT_LIB", os.path.join(_HERE, "libgift.so"))
 
 OK, E_INVAL, E_NOMEM, E_CUDA, E_RANGE, E_ALIGN = 0, -1, -2, -3, -4, -5
 ST_TAG_MISMATCH, ST_OWNER_MISMATCH, ST_UNOWNED, ST_NO_KEY, ST_BAD_DESC, ST_OVERLAP = 1, 2, 4, 8, 16, 32
+ST_NO_BLOCKS, ST_BAD_TABLE = 64, 128
 CTX_TWO_TABLES, CTX_CHECK_OVERLAP, CTX_SPLIT_LAUNCH = 1, 2, 4
 OWNER_PARAM, OWNER_NONE, OWNER_CONFLICT = -1, -2, -3
 RULE_IDENTITY, RULE_ROWWISE, RULE_SEGREDUCE, RULE_BROADCAST = 0, 1, 2, 3
 STATIC_MAX_SEGS = 65536
+KV_WHOLE_PAGES, KV_NEW_BLOCKS = 1, 2
+MAX_REQS = 8192
 
 EXPORTS = [
     "gift_ctx_create", "gift_ctx_destroy", "gift_ctx_reserve", "gift_set_keys", "gift_clear_keys",
@@ -29,6 +32,7 @@ EXPORTS = [
     "gift_resolve_args", "gift_slice_runs", "gift_expand_owners", "gift_labels_swap_out", "gift_labels_swap_in",
     "gift_strerror", "gift_version", "gift_launch_count", "gift_timing_enable", "gift_timing_read",
     "gift_export_to_host", "gift_import_from_host", "gift_last_error_detail",
+    "gift_block_tables", "gift_slot_map", "gift_kv_segments", "gift_kv_append", "gift_kv_attention",
 ]
 
 
@@ -65,6 +69,23 @@ class _Trace(C.Structure):
     _fields_ = [("n_events", C.c_uint32), ("n_streams", C.c_uint32), ("n_segments", C.c_uint32),
                 ("kind", C.c_void_p), ("stream", C.c_void_p), ("seg_ptr", C.c_void_p),
                 ("seg_event", C.c_void_p), ("seg_write", C.c_void_p)]
+
+
+class _Batch(C.Structure):
+    _fields_ = [("n_req", C.c_uint32), ("max_blocks", C.c_uint32), ("page_tokens", C.c_uint32), ("n_pages", C.c_uint32),
+                ("owner", C.c_void_p), ("have", C.c_void_p), ("want", C.c_void_p), ("table", C.c_void_p)]
+
+
+class _KvPool(C.Structure):
+    _fields_ = [("pages", C.c_void_p), ("n_pages", C.c_uint32), ("page_tokens", C.c_uint32), ("n_heads", C.c_uint32),
+                ("head_dim", C.c_uint32), ("dtype", C.c_uint32), ("owner_map", C.c_void_p)]
+
+
+class _Attn(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("q_row_stride", C.c_uint64), ("q_head_stride", C.c_uint64),
+                ("out", C.c_void_p), ("out_row_stride", C.c_uint64), ("out_head_stride", C.c_uint64),
+                ("n_rows", C.c_uint32), ("n_heads", C.c_uint32), ("scale", C.c_float), ("tree_mask", C.c_void_p),
+                ("mask_words", C.c_uint32), ("lse", C.c_void_p), ("row_owner", C.c_void_p)]
 
 
 RACE_RAW, RACE_WAR, RACE_WAW = 1, 2, 4
@@ -172,6 +193,12 @@ def lib():
         l.gift_import_from_host.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_uint64, C.c_void_p,
                                             C.c_uint32, C.c_void_p, C.c_uint32, C.POINTER(_Pages), C.POINTER(_Labels),
                                             C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]
+        vp, u32, u64 = C.c_void_p, C.c_uint32, C.c_uint64
+        l.gift_block_tables.argtypes = [vp, C.POINTER(_Batch), vp, u32, vp, vp, u32, vp, vp]
+        l.gift_slot_map.argtypes = [vp, C.POINTER(_Batch), vp, u32, vp, vp, vp, vp, vp, vp, vp]
+        l.gift_kv_segments.argtypes = [vp, C.POINTER(_Batch), vp, u32, u64, u32, vp, vp, u32, vp, vp]
+        l.gift_kv_append.argtypes = [vp, C.POINTER(_KvPool), vp, u64, u64, vp, u64, u64, u32, vp, vp, vp, vp]
+        l.gift_kv_attention.argtypes = [vp, C.POINTER(_Batch), C.POINTER(_KvPool), C.POINTER(_Attn), vp, vp]
         _lib = l
     return _lib
 
@@ -204,6 +231,63 @@ def _dev(t):
     if not (t.is_cuda or t.is_pinned()) or not t.is_contiguous():
         raise ValueError("expected a contiguous CUDA tensor or a pinned host tensor")
     return C.c_void_p(t.data_ptr())
+
+
+def _arr(t, device, what, dtype="int32", n=None, optional=False):
+    """Pointer of a contiguous tensor of the named type on cuda:device with at least n elements."""
+    if t is None:
+        if optional:
+            return None
+        raise ValueError("%s is missing" % what)
+    if t.get_device() != device or device < 0 or not t.is_contiguous():
+        raise ValueError("%s: expected a contiguous tensor on %s" % (what, "a GPU" if device < 0 else "cuda:%d" % device))
+    if t.dtype not in _dtypes()[dtype]:
+        raise ValueError("%s: expected %s, got %s" % (what, dtype, t.dtype))
+    if n is not None and t.numel() < n:
+        raise ValueError("%s: %d elements, %d are needed" % (what, t.numel(), n))
+    return t.data_ptr()
+
+
+_dtype_table = {}
+
+
+def _dtypes():
+    """The torch types that an array of the named type may have (int32 arrays hold 32-bit words)."""
+    if not _dtype_table:
+        import torch
+        _dtype_table.update(int32=(torch.int32, torch.uint32), int64=(torch.int64,), float32=(torch.float32,))
+    return _dtype_table
+
+
+def _rows3(t, device, what, heads, dim, dtype, rows=None):
+    """(pointer, row stride, head stride) of a [rows, heads, dim] tensor whose last dimension is contiguous."""
+    shape = t.shape
+    if len(shape) != 3 or shape[1] != heads or shape[2] != dim or (rows is not None and shape[0] != rows):
+        raise ValueError("%s: expected shape [rows, %d, %d], got %s" % (what, heads, dim, tuple(shape)))
+    if t.get_device() != device or t.dtype != dtype:
+        raise ValueError("%s: expected %s on cuda:%d" % (what, dtype, device))
+    row, head, one = t.stride()
+    if one != 1:
+        raise ValueError("%s: a head's elements must be contiguous" % what)
+    # the stride of a dimension of one entry is never used
+    return t.data_ptr(), row if shape[0] > 1 else 0, head if heads > 1 else 0
+
+
+class Batch:
+    """gift_batch: the requests of one step.  owner, have, want: int32 [n_req]; table: int32
+    [n_req, max_blocks], physical page of every block; page_tokens: tokens of a page; n_pages:
+    pages of one layer.  The tensors are used by the calls that the batch is given to."""
+
+    def __init__(self, owner, have, want, table, page_tokens, n_pages):
+        n, dev = owner.numel(), owner.get_device()
+        if table.dim() != 2 or table.shape[0] != n:
+            raise ValueError("table: expected shape [%d, max_blocks], got %s" % (n, tuple(table.shape)))
+        if page_tokens <= 0 or n_pages < 0:
+            raise ValueError("page_tokens must be positive and n_pages not negative")
+        self.n_req, self.page_tokens, self.n_pages, self.device = n, page_tokens, n_pages, dev
+        self.tensors = (owner, have, want, table)
+        self.c = _Batch(n, table.shape[1], page_tokens, n_pages, _arr(owner, dev, "owner"), _arr(have, dev, "have", n=n),
+                        _arr(want, dev, "want", n=n), _arr(table, dev, "table"))
 
 
 class Ctx:
@@ -389,6 +473,97 @@ class Ctx:
         _check(f(self._h, _dev(owner_map), owner_map.numel(), _dev(units), units.numel(), _dev(saved), _dev(viol),
                  _stream_ptr(stream)), "gift_labels_swap_in")
 
+    def _stream(self, stream):
+        import torch
+        return C.c_void_p(torch.cuda.current_stream(self.device).cuda_stream if stream is None else int(stream))
+
+    def _batch(self, batch):
+        if batch.device != self.device:
+            raise ValueError("the batch lies on cuda:%s, the context on cuda:%d" % (batch.device, self.device))
+        return C.byref(batch.c)
+
+    def block_tables(self, batch, free_pages, n_free, owner_map, status, layers=1, stream=None):
+        """gift_block_tables: free_pages int32 [cap], n_free int32 [1], owner_map int32 [layers, n_pages],
+        status int32 [n_req]; batch's table, the stack and the labels are updated in place."""
+        d, n = self.device, batch.n_req
+        _check(lib().gift_block_tables(self._h, self._batch(batch), _arr(free_pages, d, "free_pages"), free_pages.numel(),
+                                       _arr(n_free, d, "n_free", n=1), _arr(owner_map, d, "owner_map", n=layers * batch.n_pages),
+                                       layers, _arr(status, d, "status", n=n), self._stream(stream)), "gift_block_tables")
+
+    def slot_map(self, batch, slots, row_req=None, row_pos=None, row_owner=None, row_ptr=None, total=None, rel=None,
+                 stream=None):
+        """gift_slot_map: slots int64 [n_rows]; row_req, row_pos, row_owner int32 [n_rows], row_ptr int32
+        [n_req + 1], total int64 [1] or None; rel int32 [n_rows] or None."""
+        d, n = self.device, slots.numel()
+        _check(lib().gift_slot_map(self._h, self._batch(batch), _arr(rel, d, "rel", n=n, optional=True), n,
+                                   _arr(slots, d, "slots", "int64"), _arr(row_req, d, "row_req", n=n, optional=True),
+                                   _arr(row_pos, d, "row_pos", n=n, optional=True),
+                                   _arr(row_owner, d, "row_owner", n=n, optional=True),
+                                   _arr(row_ptr, d, "row_ptr", n=batch.n_req + 1, optional=True),
+                                   _arr(total, d, "total", "int64", n=1, optional=True), self._stream(stream)), "gift_slot_map")
+
+    def kv_segments(self, batch, serial, segs, page_table, layers, token_bytes, whole_pages=False, new_blocks=False,
+                    total=None, stream=None):
+        """gift_kv_segments: serial int32 [n_req]; segs a contiguous tensor of 40 bytes per entry of
+        page_table (int32 [cap]); total int64 [1] or None."""
+        d, cap = self.device, page_table.numel()
+        if segs.get_device() != d or not segs.is_contiguous():
+            raise ValueError("segs: expected a contiguous tensor on cuda:%d" % d)
+        if segs.numel() * segs.element_size() < 40 * cap:
+            raise ValueError("segs holds fewer entries than page_table")
+        flags = (KV_WHOLE_PAGES if whole_pages else 0) | (KV_NEW_BLOCKS if new_blocks else 0)
+        _check(lib().gift_kv_segments(self._h, self._batch(batch), _arr(serial, d, "serial", n=batch.n_req), layers,
+                                      token_bytes, flags, segs.data_ptr(), _arr(page_table, d, "page_table"), cap,
+                                      _arr(total, d, "total", "int64", n=1, optional=True), self._stream(stream)),
+               "gift_kv_segments")
+
+    def _pool(self, pages, owner_map):
+        if pages.dim() != 5 or pages.shape[2] != 2:
+            raise ValueError("pages: expected shape [n_pages, page_tokens, 2, n_heads, head_dim], got %s" % (tuple(pages.shape),))
+        dtype = {"torch.bfloat16": 0, "torch.float16": 1}.get(str(pages.dtype))
+        if dtype is None:
+            raise ValueError("pages: expected bfloat16 or float16, got %s" % pages.dtype)
+        n, pt, _, heads, dim = pages.shape
+        d = self.device
+        if pages.get_device() != d or not pages.is_contiguous():
+            raise ValueError("pages: expected a contiguous tensor on cuda:%d" % d)
+        return _KvPool(pages.data_ptr(), n, pt, heads, dim, dtype, _arr(owner_map, d, "owner_map", n=n, optional=True))
+
+    def kv_append(self, pages, k, v, slots, row_owner, status, owner_map=None, stream=None):
+        """gift_kv_append: pages [n_pages, page_tokens, 2, n_heads, head_dim] of one layer; k, v [rows, n_heads,
+        head_dim] of the same type, with any strides that keep a head contiguous; slots int64, row_owner and
+        status int32 [rows]; owner_map int32 [n_pages] or None (no label handling; row_owner may be None)."""
+        d, n = self.device, k.shape[0]
+        pool = self._pool(pages, owner_map)
+        kp, kr, kh = _rows3(k, d, "k", pages.shape[3], pages.shape[4], pages.dtype)
+        vp, vr, vh = _rows3(v, d, "v", pages.shape[3], pages.shape[4], pages.dtype, n)
+        _check(lib().gift_kv_append(self._h, C.byref(pool), kp, kr, kh, vp, vr, vh, n, _arr(slots, d, "slots", "int64", n=n),
+                                    _arr(row_owner, d, "row_owner", n=n, optional=owner_map is None),
+                                    _arr(status, d, "status", n=n), self._stream(stream)), "gift_kv_append")
+
+    def kv_attention(self, batch, pages, q, out, status, tree_mask=None, lse=None, row_owner=None, owner_map=None,
+                     scale=None, stream=None):
+        """gift_kv_attention: q, out [rows, heads, head_dim] in the type of pages (see kv_append); tree_mask int32
+        [rows, mask_words] or None (every row sees the step's rows up to its own); lse float32 [rows, heads],
+        row_owner int32 [rows] or None; scale: 1 / sqrt(head_dim) unless given."""
+        if q.dim() != 3:
+            raise ValueError("q: expected shape [rows, heads, head_dim], got %s" % (tuple(q.shape),))
+        d, n, heads, dim = self.device, q.shape[0], q.shape[1], pages.shape[-1]
+        pool = self._pool(pages, owner_map)
+        qp, qr, qh = _rows3(q, d, "q", heads, dim, pages.dtype)
+        op, orow, oh = _rows3(out, d, "out", heads, dim, pages.dtype, n)
+        words = 0
+        if tree_mask is not None:
+            if tree_mask.dim() != 2 or tree_mask.shape[0] != n:
+                raise ValueError("tree_mask: expected shape [%d, mask_words], got %s" % (n, tuple(tree_mask.shape)))
+            words = tree_mask.shape[1]
+        a = _Attn(qp, qr, qh, op, orow, oh, n, heads, dim ** -0.5 if scale is None else scale,
+                  _arr(tree_mask, d, "tree_mask", optional=True), words,
+                  _arr(lse, d, "lse", "float32", n=n * heads, optional=True),
+                  _arr(row_owner, d, "row_owner", n=n, optional=True))
+        _check(lib().gift_kv_attention(self._h, self._batch(batch), C.byref(pool), C.byref(a),
+                                       _arr(status, d, "status", n=batch.n_req), self._stream(stream)), "gift_kv_attention")
+
     @staticmethod
     def chunk_array(chunks):
         """HOST array of gift_chunk from (byte_lo, byte_hi, seg_lo, seg_hi) tuples or Chunk objects."""
@@ -551,6 +726,26 @@ def gift_export_to_host(ctx: Ctx, *args, **kw):
 
 def gift_import_from_host(ctx: Ctx, *args, **kw):
     ctx.import_from_host(*args, **kw)
+
+
+def gift_block_tables(ctx: Ctx, *args, **kw):
+    ctx.block_tables(*args, **kw)
+
+
+def gift_slot_map(ctx: Ctx, *args, **kw):
+    ctx.slot_map(*args, **kw)
+
+
+def gift_kv_segments(ctx: Ctx, *args, **kw):
+    ctx.kv_segments(*args, **kw)
+
+
+def gift_kv_append(ctx: Ctx, *args, **kw):
+    ctx.kv_append(*args, **kw)
+
+
+def gift_kv_attention(ctx: Ctx, *args, **kw):
+    ctx.kv_attention(*args, **kw)
 
 
 def gift_last_error_detail() -> str:

@@ -1,0 +1,547 @@
+// Attention of a step's rows over the labelled paged cache (the subject of the SEGREDUCE rule,
+// with the rule checked on the very block table that is read).
+#include <cuda_runtime.h>
+#include <math.h>
+#include <stdint.h>
+#include <string.h>
+
+#include <type_traits>
+
+#include "gift_attn.cuh"
+#include "gift_internal.cuh"
+#include "gift_kv.cuh"
+
+using namespace gift;
+
+namespace {
+
+// ---------------------------------------------------------------------------
+// few query rows per K/V head: warp-level products
+// ---------------------------------------------------------------------------
+//
+// With R query rows per K/V head the kernel does R operations per K/V byte, so up to some 32 rows
+// HBM bandwidth bounds it and the matrix instructions need only keep out of the way.  Every
+// warp works on its own 16 tokens of a 64-token tile, with a ring of 3 stages of K and V rows in
+// shared memory that only it fills and reads: no barrier inside a piece.  2 CTAs of 4 warps per
+// SM keep 128 to 192 KiB in flight.  The warps' maxima, sums and rows are joined at a piece's end.
+
+constexpr int FEW_WARPS = 4;
+constexpr int FEW_THREADS = FEW_WARPS * 32;
+constexpr int FEW_TILE = FEW_WARPS * 16;
+constexpr int FEW_STAGES = 3;
+
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, uint32_t bytes)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+__device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t addr)
+{
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void ldsm4t(uint32_t (&r)[4], uint32_t addr)
+{
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+
+template <class T>
+__device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
+{
+    if constexpr (std::is_same<T, __half>::value)
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                     : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+    else
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                     : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+// Address of 16-byte chunk `chunk` of row `row` in a tile of rows of D elements: chunks are
+// permuted within a row by the row number, so that 8 rows' equal chunks lie in different banks.
+template <int D> __device__ __forceinline__ uint32_t tile_at(uint32_t base, uint32_t row, uint32_t chunk)
+{
+    return base + row * (D * 2) + ((chunk ^ (row & 7u)) << 4);
+}
+
+template <int D, int MT> struct FewSmem {
+    static constexpr int ring = FEW_WARPS * FEW_STAGES * 16 * D * 2 * 2;
+    static constexpr int join = FEW_WARPS * MT * 16 * D * 4;
+    static constexpr int bytes = ring > join ? ring : join;
+};
+
+template <class T, int D, int MT>
+__global__ void __launch_bounds__(FEW_THREADS, 2) attn_few_kernel(const __grid_constant__ AttnArgs a)
+{
+    constexpr int ROWS = 16 * MT;
+    constexpr int CH = D / 8;                      // 16-byte chunks of a K or V row
+    constexpr int KS = D / 16;                     // k steps of the score product
+    constexpr uint32_t HALF = 16 * D * 2;          // bytes of 16 K (or V) rows
+    extern __shared__ __align__(128) char smem[];
+    __shared__ PlaceShared place;
+    __shared__ float2 s_ml[FEW_WARPS][ROWS];
+    __shared__ uint32_t s_bits;
+
+    uint64_t total, slice;
+    if (!place_unit<FEW_THREADS>(a, blockIdx.x, ROWS, FEW_TILE, blockIdx.x == 0, &place, &total, &slice)) return;
+    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t ring = (uint32_t)__cvta_generic_to_shared(smem) + warp * (FEW_STAGES * 2 * HALF);
+
+    uint32_t r = place.at.r, row0 = place.at.row0;
+    uint64_t off = place.at.off, left = slice < total - slice * blockIdx.x ? slice : total - slice * blockIdx.x;
+    ReqShape s = load_shape(a.b, r);
+    ItemShape it = item_shape(a, s, ROWS, FEW_TILE);
+    while (left > 0) {
+        while (off >= it.units) {
+            off -= it.units;
+            row0 += it.rows_m;
+            r++;
+            s = load_shape(a.b, r);
+            it = item_shape(a, s, ROWS, FEW_TILE);
+        }
+        const uint32_t item = (uint32_t)(off / it.tiles), tb = (uint32_t)(off - (uint64_t)item * it.tiles);
+        const uint32_t n_tiles = (uint64_t)(it.tiles - tb) < left ? it.tiles - tb : (uint32_t)left;
+        const uint32_t h = item / it.nqt, qt = item - h * it.nqt;
+        const uint32_t all_q = it.rows_m * a.group;                // query rows of the K/V head
+        const uint32_t q0 = qt * ROWS;
+        const int32_t owner = a.b.owner[r];
+        const int32_t* table = a.b.table + (uint64_t)r * a.b.max_blocks;
+        uint32_t bits = a.mask && it.rows_m > a.mask_words * 32u ? GIFT_ST_BAD_DESC : 0u;
+
+        // this lane's query rows g and g + 8 of every 16-row tile
+        const uint32_t g = lane >> 2, c2 = (lane & 3) * 2;
+        uint32_t qf[MT][KS][4];
+        uint32_t row_i[MT][2];
+        const uint32_t* words[MT][2];
+#pragma unroll
+        for (int mt = 0; mt < MT; mt++) {
+#pragma unroll
+            for (int half = 0; half < 2; half++) {
+                const uint32_t rho = q0 + mt * 16 + half * 8 + g;
+                const bool there = rho < all_q;
+                const uint32_t i = there ? rho / a.group : 0u, hq = h * a.group + (there ? rho - i * a.group : 0u);
+                row_i[mt][half] = i;
+                words[mt][half] = a.mask + (uint64_t)(row0 + i) * a.mask_words;
+                const char* q = a.q + (uint64_t)(row0 + i) * a.q_row + (uint64_t)hq * a.q_head;
+#pragma unroll
+                for (int ks = 0; ks < KS; ks++)
+#pragma unroll
+                    for (int hi = 0; hi < 2; hi++)
+                        qf[mt][ks][hi * 2 + half] =
+                            there ? *reinterpret_cast<const uint32_t*>(q + (ks * 16 + hi * 8 + c2) * 2) : 0u;
+            }
+        }
+        float o[MT][D / 8][4];
+        float m[MT][2], l[MT][2];
+#pragma unroll
+        for (int mt = 0; mt < MT; mt++) {
+            m[mt][0] = m[mt][1] = NEG_INF;
+            l[mt][0] = l[mt][1] = 0.f;
+#pragma unroll
+            for (int n = 0; n < D / 8; n++)
+#pragma unroll
+                for (int e = 0; e < 4; e++) o[mt][n][e] = 0.f;
+        }
+
+        // Lane l looks after token l % 16 of the warp's 16: its table entry is fetched one step
+        // ahead of the copies that need it, its label is looked at one step after.
+        const uint32_t my = lane & 15u;
+        auto entry = [&](uint32_t step) -> int32_t {
+            const uint32_t t = (tb + step) * FEW_TILE + warp * 16 + my;
+            return step < n_tiles && t < s.want ? table[t / a.b.page_tokens] : -1;
+        };
+        int32_t next = entry(0);
+        uint32_t label_bits = 0;
+        auto issue = [&](uint32_t step) {
+            if (step < n_tiles) {
+                const uint32_t t = (tb + step) * FEW_TILE + warp * 16 + my;
+                const int32_t page = next;
+                next = entry(step + 1);
+                bits |= label_bits;
+                label_bits = 0;
+                const bool valid = t < s.want, ok = valid && page >= 0 && (uint32_t)page < a.b.n_pages;
+                uint64_t src = 0;
+                if (ok) {
+                    src = ((uint64_t)(uint32_t)page * a.b.page_tokens + t % a.b.page_tokens) * a.token_bytes + (uint64_t)h * (D * 2);
+                    if (a.owner_map) label_bits = label_read_status(a.owner_map[page], owner);
+                } else if (valid) {
+                    bits |= GIFT_ST_BAD_DESC;
+                }
+                const uint32_t base = ring + (step % FEW_STAGES) * (2 * HALF);
+#pragma unroll
+                for (int i = 0; i < CH / 2; i++) {
+                    const uint32_t row = i * (32 / CH) + lane / CH, chunk = lane % CH;
+                    const uint64_t from = __shfl_sync(0xFFFFFFFFu, src, row);
+                    const uint32_t size = __shfl_sync(0xFFFFFFFFu, ok ? 16u : 0u, row);
+                    const char* p = a.pages + from + chunk * 16;
+                    // rows past the context are filled with zeros: what memory holds there does not matter
+                    cp_async16(tile_at<D>(base, row, chunk), p, size);
+                    cp_async16(tile_at<D>(base + HALF, row, chunk), size ? p + (uint64_t)a.kv_heads * (D * 2) : p, size);
+                }
+            }
+            cp_commit();
+        };
+#pragma unroll
+        for (int st = 0; st < FEW_STAGES - 1; st++) issue(st);
+
+        for (uint32_t step = 0; step < n_tiles; step++) {
+            issue(step + FEW_STAGES - 1);
+            cp_wait<FEW_STAGES - 1>();
+            __syncwarp();
+            const uint32_t kb = ring + (step % FEW_STAGES) * (2 * HALF), vb = kb + HALF;
+            const uint32_t t0 = (tb + step) * FEW_TILE + warp * 16;
+            float sc[MT][2][4];
+#pragma unroll
+            for (int mt = 0; mt < MT; mt++)
+#pragma unroll
+                for (int n = 0; n < 2; n++)
+#pragma unroll
+                    for (int e = 0; e < 4; e++) sc[mt][n][e] = 0.f;
+#pragma unroll
+            for (int ks = 0; ks < KS; ks++) {
+                uint32_t kf[4];
+                ldsm4(kf, tile_at<D>(kb, (lane >> 4) * 8 + (lane & 7), ks * 2 + ((lane >> 3) & 1)));
+#pragma unroll
+                for (int mt = 0; mt < MT; mt++) {
+                    mma16816<T>(sc[mt][0], qf[mt][ks], kf[0], kf[1]);
+                    mma16816<T>(sc[mt][1], qf[mt][ks], kf[2], kf[3]);
+                }
+            }
+            const bool mixed = t0 + 16 > s.have;       // some rows may not see some of these tokens
+            uint32_t pf[MT][4];
+#pragma unroll
+            for (int mt = 0; mt < MT; mt++) {
+#pragma unroll
+                for (int n = 0; n < 2; n++)
+#pragma unroll
+                    for (int e = 0; e < 4; e++) sc[mt][n][e] *= a.scale_log2;
+                if (mixed) {
+#pragma unroll
+                    for (int n = 0; n < 2; n++)
+#pragma unroll
+                        for (int e = 0; e < 4; e++)
+                            if (bits & GIFT_ST_BAD_DESC || !row_sees(a, s, row_i[mt][e >> 1], words[mt][e >> 1], t0 + n * 8 + c2 + (e & 1)))
+                                sc[mt][n][e] = NEG_INF;
+                }
+                float alpha[2];
+#pragma unroll
+                for (int half = 0; half < 2; half++) {
+                    float top = fmaxf(fmaxf(sc[mt][0][half * 2], sc[mt][0][half * 2 + 1]), fmaxf(sc[mt][1][half * 2], sc[mt][1][half * 2 + 1]));
+                    top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
+                    top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
+                    const float now = fmaxf(m[mt][half], top);
+                    const float use = now == NEG_INF ? 0.f : now;      // nothing seen yet: exp2(-inf - 0) = 0
+                    alpha[half] = fast_exp2(m[mt][half] - use);
+                    m[mt][half] = now;
+                    float sum = 0.f;
+#pragma unroll
+                    for (int n = 0; n < 2; n++)
+#pragma unroll
+                        for (int e = 0; e < 2; e++) {
+                            const float p = fast_exp2(sc[mt][n][half * 2 + e] - use);
+                            sc[mt][n][half * 2 + e] = p;
+                            sum += p;
+                        }
+                    l[mt][half] = l[mt][half] * alpha[half] + sum;
+                }
+                if (__any_sync(0xFFFFFFFFu, alpha[0] != 1.f || alpha[1] != 1.f)) {
+#pragma unroll
+                    for (int n = 0; n < D / 8; n++) {
+                        o[mt][n][0] *= alpha[0]; o[mt][n][1] *= alpha[0];
+                        o[mt][n][2] *= alpha[1]; o[mt][n][3] *= alpha[1];
+                    }
+                }
+                // p is rounded to the pool's type: the operands of one product have one type, and the
+                // rounding (2^-9 relative at most for bf16) is of the size of v's own
+                pf[mt][0] = pack2<T>(sc[mt][0][0], sc[mt][0][1]);
+                pf[mt][1] = pack2<T>(sc[mt][0][2], sc[mt][0][3]);
+                pf[mt][2] = pack2<T>(sc[mt][1][0], sc[mt][1][1]);
+                pf[mt][3] = pack2<T>(sc[mt][1][2], sc[mt][1][3]);
+            }
+            // 0 * inf is NaN: where a row may not see a token whose v is not finite, the product is
+            // taken token by token, over what the row sees
+            bool plain = true;
+            if (mixed) {
+                bool odd = false;
+#pragma unroll
+                for (int i = 0; i < CH / 2; i++) {
+                    uint4 x;
+                    const uint32_t at = vb + (i * 32 + lane) * 16;
+                    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w) : "r"(at) : "memory");
+                    odd |= pair_not_finite<T>(x.x) || pair_not_finite<T>(x.y) || pair_not_finite<T>(x.z) || pair_not_finite<T>(x.w);
+                }
+                plain = !__any_sync(0xFFFFFFFFu, odd);
+            }
+            if (plain) {
+#pragma unroll
+                for (int np = 0; np < D / 16; np++) {
+                    uint32_t vf[4];
+                    ldsm4t(vf, tile_at<D>(vb, ((lane >> 3) & 1) * 8 + (lane & 7), np * 2 + (lane >> 4)));
+#pragma unroll
+                    for (int mt = 0; mt < MT; mt++) {
+                        mma16816<T>(o[mt][np * 2], pf[mt], vf[0], vf[1]);
+                        mma16816<T>(o[mt][np * 2 + 1], pf[mt], vf[2], vf[3]);
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int mt = 0; mt < MT; mt++)
+                    for (int t = 0; t < 16; t++) {
+#pragma unroll
+                        for (int half = 0; half < 2; half++) {
+                            // token t's p of this lane's row: held by lane (t % 8) / 2 of the row's four
+                            const int from = (lane & ~3) | ((t & 7) >> 1);
+                            const float p0 = __shfl_sync(0xFFFFFFFFu, t < 8 ? sc[mt][0][half * 2] : sc[mt][1][half * 2], from);
+                            const float p1 = __shfl_sync(0xFFFFFFFFu, t < 8 ? sc[mt][0][half * 2 + 1] : sc[mt][1][half * 2 + 1], from);
+                            const float p = t & 1 ? p1 : p0;
+                            const bool sees = !(bits & GIFT_ST_BAD_DESC) && row_sees(a, s, row_i[mt][half], words[mt][half], t0 + t);
+                            if (!sees) continue;
+#pragma unroll
+                            for (int n = 0; n < D / 8; n++) {
+                                uint32_t x;
+                                asm volatile("ld.shared.u32 %0, [%1];" : "=r"(x) : "r"(tile_at<D>(vb, t, n) + c2 * 2) : "memory");
+                                const T* v = reinterpret_cast<const T*>(&x);
+                                o[mt][n][half * 2] += p * to_float<T>(v[0]);
+                                o[mt][n][half * 2 + 1] += p * to_float<T>(v[1]);
+                            }
+                        }
+                    }
+            }
+            __syncwarp();                              // the stage may be filled again
+        }
+        bits |= label_bits;
+        cp_wait<0>();
+
+        // Join the four warps' parts.
+#pragma unroll
+        for (int mt = 0; mt < MT; mt++)
+#pragma unroll
+            for (int half = 0; half < 2; half++) {
+                l[mt][half] += __shfl_xor_sync(0xFFFFFFFFu, l[mt][half], 1);
+                l[mt][half] += __shfl_xor_sync(0xFFFFFFFFu, l[mt][half], 2);
+                if ((lane & 3) == 0) s_ml[warp][mt * 16 + half * 8 + g] = make_float2(m[mt][half], l[mt][half]);
+            }
+        bits = __reduce_or_sync(0xFFFFFFFFu, bits);
+        if (threadIdx.x == 0) s_bits = 0u;
+        __syncthreads();                               // the ring is idle; s_ml is complete
+        if (lane == 0 && bits) atomicOr(&s_bits, bits);
+        float* join = reinterpret_cast<float*>(smem) + (uint32_t)warp * (ROWS * D);
+#pragma unroll
+        for (int mt = 0; mt < MT; mt++)
+#pragma unroll
+            for (int n = 0; n < D / 8; n++)
+#pragma unroll
+                for (int half = 0; half < 2; half++)
+                    *reinterpret_cast<float2*>(join + (mt * 16 + half * 8 + g) * D + n * 8 + c2) =
+                        make_float2(o[mt][n][half * 2], o[mt][n][half * 2 + 1]);
+        __syncthreads();
+        bits = s_bits;
+        const bool whole = tb == 0 && n_tiles == it.tiles;
+        const uint32_t slot = blockIdx.x * 2u + (tb == 0 ? 1u : 0u);
+        const uint32_t nr = all_q - q0 < (uint32_t)ROWS ? all_q - q0 : (uint32_t)ROWS;
+        for (uint32_t c = threadIdx.x; c < nr * (uint32_t)CH; c += FEW_THREADS) {
+            const uint32_t row = c / CH, ch = c % CH;
+            float top = NEG_INF;
+#pragma unroll
+            for (int w = 0; w < FEW_WARPS; w++) top = fmaxf(top, s_ml[w][row].x);
+            const float use = top == NEG_INF ? 0.f : top;
+            float sum = 0.f, acc[8];
+#pragma unroll
+            for (int e = 0; e < 8; e++) acc[e] = 0.f;
+#pragma unroll
+            for (int w = 0; w < FEW_WARPS; w++) {
+                const float f = fast_exp2(s_ml[w][row].x - use);
+                sum += s_ml[w][row].y * f;
+                const float4* from = reinterpret_cast<const float4*>(reinterpret_cast<const float*>(smem) + (w * ROWS + row) * D + ch * 8);
+                const float4 x = from[0], y = from[1];
+                // a warp that saw nothing holds zeros, and f is 0
+                acc[0] += f * x.x; acc[1] += f * x.y; acc[2] += f * x.z; acc[3] += f * x.w;
+                acc[4] += f * y.x; acc[5] += f * y.y; acc[6] += f * y.z; acc[7] += f * y.w;
+            }
+            if (whole) {
+                const uint32_t rho = q0 + row, i = rho / a.group, hq = h * a.group + (rho - i * a.group);
+                const bool none = bits != 0u || sum == 0.f;
+                const float inv = none ? 0.f : 1.f / sum;
+                uint4 v = make_uint4(0u, 0u, 0u, 0u);
+                if (!none) {
+                    v.x = pack2<T>(acc[0] * inv, acc[1] * inv); v.y = pack2<T>(acc[2] * inv, acc[3] * inv);
+                    v.z = pack2<T>(acc[4] * inv, acc[5] * inv); v.w = pack2<T>(acc[6] * inv, acc[7] * inv);
+                }
+                *reinterpret_cast<uint4*>(a.out + (uint64_t)(row0 + i) * a.out_row + (uint64_t)hq * a.out_head + ch * 16) = v;
+                if (a.lse && ch == 0)
+                    a.lse[(uint64_t)(row0 + i) * a.heads + hq] = none ? NEG_INF : (top + log2f(sum)) * 0.6931471805599453f;
+            } else {
+                float4* to = reinterpret_cast<float4*>(a.part_o + ((uint64_t)slot * ROWS + row) * D + ch * 8);
+                to[0] = make_float4(acc[0], acc[1], acc[2], acc[3]);
+                to[1] = make_float4(acc[4], acc[5], acc[6], acc[7]);
+                if (ch == 0) a.part_ml[(uint64_t)slot * ROWS + row] = make_float2(top, sum);
+            }
+        }
+        if (whole) {
+            if (h == 0 && qt == 0) write_request<FEW_THREADS>(a, r, row0, it.rows_m, bits);
+        } else if (threadIdx.x == 0) {
+            a.part_bits[slot] = bits;
+        }
+        __syncthreads();                               // smem is free for the next piece
+        off += n_tiles;
+        left -= n_tiles;
+    }
+}
+
+// Joins the pieces of the items that a slice boundary cuts.  CTA w looks after the item that
+// boundary w cuts, if no earlier boundary cuts it too.
+constexpr int JOIN_THREADS = 128;
+
+template <class T, int D, int ROWS, int TILE>
+__global__ void __launch_bounds__(JOIN_THREADS) attn_join_kernel(const __grid_constant__ AttnArgs a)
+{
+    constexpr int CH = D / 8;
+    __shared__ PlaceShared place;
+    __shared__ float2 s_top[ROWS];
+    __shared__ uint32_t s_bits;
+    const uint32_t w = blockIdx.x + 1;
+    uint64_t total, slice;
+    if (!place_unit<JOIN_THREADS>(a, w, ROWS, TILE, false, &place, &total, &slice)) return;
+    const uint32_t r = place.at.r, row0 = place.at.row0;
+    const ReqShape s = load_shape(a.b, r);
+    const ItemShape it = item_shape(a, s, ROWS, TILE);
+    const uint32_t item = (uint32_t)(place.at.off / it.tiles), tb = (uint32_t)(place.at.off - (uint64_t)item * it.tiles);
+    if (tb == 0 || tb > slice) return;                 // not cut here, or cut by an earlier boundary as well
+    const uint64_t end = slice * w - tb + it.tiles;    // one past the item's last unit
+    const uint32_t w_last = (uint32_t)((end - 1) / slice), pieces = w_last - w + 2;
+    const uint32_t h = item / it.nqt, qt = item - h * it.nqt, q0 = qt * ROWS;
+    const uint32_t all_q = it.rows_m * a.group;
+    const uint32_t nr = all_q - q0 < (uint32_t)ROWS ? all_q - q0 : (uint32_t)ROWS;
+    // the item starts in CTA w - 1 (its last piece) and goes on as the first piece of w, w + 1, ...
+    auto slot_of = [&](uint32_t p) -> uint64_t { return p == 0 ? 2ull * (w - 1) + 1 : 2ull * (w + p - 1); };
+    if (threadIdx.x == 0) s_bits = 0u;
+    __syncthreads();
+    for (uint32_t p = threadIdx.x; p < pieces; p += JOIN_THREADS)
+        if (a.part_bits[slot_of(p)]) atomicOr(&s_bits, a.part_bits[slot_of(p)]);
+    for (uint32_t row = threadIdx.x; row < nr; row += JOIN_THREADS) {
+        float top = NEG_INF, sum = 0.f;
+        for (uint32_t p = 0; p < pieces; p++) top = fmaxf(top, a.part_ml[slot_of(p) * ROWS + row].x);
+        const float use = top == NEG_INF ? 0.f : top;
+        for (uint32_t p = 0; p < pieces; p++) {
+            const float2 ml = a.part_ml[slot_of(p) * ROWS + row];
+            sum += ml.y * fast_exp2(ml.x - use);
+        }
+        s_top[row] = make_float2(top, sum);
+    }
+    __syncthreads();
+    const uint32_t bits = s_bits;
+    for (uint32_t c = threadIdx.x; c < nr * (uint32_t)CH; c += JOIN_THREADS) {
+        const uint32_t row = c / CH, ch = c % CH;
+        const float top = s_top[row].x, sum = s_top[row].y, use = top == NEG_INF ? 0.f : top;
+        float acc[8];
+#pragma unroll
+        for (int e = 0; e < 8; e++) acc[e] = 0.f;
+        for (uint32_t p = 0; p < pieces; p++) {
+            const uint64_t at = slot_of(p) * ROWS + row;
+            const float f = fast_exp2(a.part_ml[at].x - use);
+            const float4* from = reinterpret_cast<const float4*>(a.part_o + at * D + ch * 8);
+            const float4 x = from[0], y = from[1];
+            acc[0] += f * x.x; acc[1] += f * x.y; acc[2] += f * x.z; acc[3] += f * x.w;
+            acc[4] += f * y.x; acc[5] += f * y.y; acc[6] += f * y.z; acc[7] += f * y.w;
+        }
+        const uint32_t rho = q0 + row, i = rho / a.group, hq = h * a.group + (rho - i * a.group);
+        const bool none = bits != 0u || sum == 0.f;
+        const float inv = none ? 0.f : 1.f / sum;
+        uint4 v = make_uint4(0u, 0u, 0u, 0u);
+        if (!none) {
+            v.x = pack2<T>(acc[0] * inv, acc[1] * inv); v.y = pack2<T>(acc[2] * inv, acc[3] * inv);
+            v.z = pack2<T>(acc[4] * inv, acc[5] * inv); v.w = pack2<T>(acc[6] * inv, acc[7] * inv);
+        }
+        *reinterpret_cast<uint4*>(a.out + (uint64_t)(row0 + i) * a.out_row + (uint64_t)hq * a.out_head + ch * 16) = v;
+        if (a.lse && ch == 0) a.lse[(uint64_t)(row0 + i) * a.heads + hq] = none ? NEG_INF : (top + log2f(sum)) * 0.6931471805599453f;
+    }
+    if (h == 0 && qt == 0) write_request<JOIN_THREADS>(a, r, row0, it.rows_m, bits);
+}
+
+template <class T, int D, int MT>
+int launch_few(gift_ctx* c, AttnArgs& a, cudaStream_t st)
+{
+    constexpr int smem = FewSmem<D, MT>::bytes;
+    CU_TRY(cudaFuncSetAttribute(attn_few_kernel<T, D, MT>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+    a.n_cta = 2u * c->num_sms;
+    a.least = 1;
+    attn_few_kernel<T, D, MT><<<a.n_cta, FEW_THREADS, smem, st>>>(a);
+    c->launches++;
+    attn_join_kernel<T, D, 16 * MT, FEW_TILE><<<a.n_cta - 1, JOIN_THREADS, 0, st>>>(a);
+    c->launches++;
+    CU_TRY(cudaGetLastError());
+    return GIFT_OK;
+}
+
+template <class T, int D>
+int launch_attn(gift_ctx* c, AttnArgs& a, cudaStream_t st)
+{
+    // rows of an average request's K/V head
+    const uint64_t rows = ((uint64_t)a.n_rows + a.b.n_req - 1) / a.b.n_req * a.group;
+    return rows <= 16 ? launch_few<T, D, 1>(c, a, st) : launch_few<T, D, 2>(c, a, st);
+}
+
+constexpr uint32_t PART_ROWS = 32;       // most rows of a tile of query rows
+constexpr uint32_t PART_D = 128;
+
+// The scratch is allocated once, at a size that no call exceeds, and stays where it is until the
+// ctx is destroyed: a captured graph that names it stays valid.
+int scratch_ensure(gift_ctx* c)
+{
+    if (c->d_attn) return GIFT_OK;
+    const size_t parts = 4ull * c->num_sms;
+    CU_TRY(cudaMalloc(&c->d_attn, parts * (PART_ROWS * (PART_D * 4 + 8) + 4)));
+    return GIFT_OK;
+}
+
+}  // namespace
+
+extern "C" int gift_kv_attention(gift_ctx* c, const gift_batch* batch, const gift_kv_pool* pool, const gift_attn* t,
+                                 uint32_t* status, void* stream)
+{
+    if (!c) return GIFT_E_INVAL;
+    int rc = batch_args_ok(batch);
+    if (rc != GIFT_OK) return rc;
+    if ((rc = pool_args_ok(pool)) != GIFT_OK) return rc;
+    if (!t) return GIFT_E_INVAL;
+    if (batch->n_req == 0) return GIFT_OK;
+    if (!status || pool->n_pages != batch->n_pages || pool->page_tokens != batch->page_tokens) return GIFT_E_INVAL;
+    if (pool->head_dim != 64 && pool->head_dim != 128) return GIFT_E_RANGE;
+    if (t->n_heads == 0 || t->n_heads % pool->n_heads != 0) return GIFT_E_INVAL;
+    if (t->n_heads > GIFT_MAX_HEADS || t->mask_words > 0x00FFFFFFu || (uint64_t)t->n_rows * t->n_heads > 0x7FFFFFFFu) return GIFT_E_RANGE;
+    if (t->tree_mask && t->mask_words == 0) return GIFT_E_INVAL;
+    if (t->n_rows) {
+        if ((rc = rows_args_ok(t->q, t->q_row_stride, t->q_head_stride)) != GIFT_OK) return rc;
+        if ((rc = rows_args_ok(t->out, t->out_row_stride, t->out_head_stride)) != GIFT_OK) return rc;
+        // rows that share memory cannot all be written
+        if ((t->n_rows > 1 && t->out_row_stride == 0) || (t->n_heads > 1 && t->out_head_stride == 0)) return GIFT_E_INVAL;
+    }
+    DeviceGuard g(c->device);
+    if (!g.ok) return GIFT_E_CUDA;
+    if ((rc = scratch_ensure(c)) != GIFT_OK) return rc;
+    AttnArgs a;
+    memset(&a, 0, sizeof(a));
+    a.b = batch_args(batch);
+    a.pages = static_cast<const char*>(pool->pages);
+    a.token_bytes = (uint64_t)pool->n_heads * pool->head_dim * 4;
+    a.kv_heads = pool->n_heads; a.heads = t->n_heads; a.group = t->n_heads / pool->n_heads;
+    a.q = static_cast<const char*>(t->q); a.q_row = t->q_row_stride * 2; a.q_head = t->q_head_stride * 2;
+    a.out = static_cast<char*>(t->out); a.out_row = t->out_row_stride * 2; a.out_head = t->out_head_stride * 2;
+    a.n_rows = t->n_rows;
+    a.scale_log2 = t->scale * 1.4426950408889634f;
+    a.mask = t->tree_mask; a.mask_words = t->mask_words;
+    a.lse = t->lse; a.row_owner = t->row_owner; a.owner_map = pool->owner_map; a.status = status;
+    const size_t parts = 4ull * c->num_sms;
+    char* p = static_cast<char*>(c->d_attn);
+    a.part_o = reinterpret_cast<float*>(p);
+    a.part_ml = reinterpret_cast<float2*>(p + parts * PART_ROWS * PART_D * 4);
+    a.part_bits = reinterpret_cast<uint32_t*>(p + parts * PART_ROWS * (PART_D * 4 + 8));
+    cudaStream_t st = (cudaStream_t)stream;
+    if (pool->dtype == GIFT_BF16)
+        return pool->head_dim == 128 ? launch_attn<__nv_bfloat16, 128>(c, a, st) : launch_attn<__nv_bfloat16, 64>(c, a, st);
+    return pool->head_dim == 128 ? launch_attn<__half, 128>(c, a, st) : launch_attn<__half, 64>(c, a, st);
+}

@@ -1,0 +1,179 @@
+// Attention of a step's rows over the labelled paged cache: how the work is cut, and the pieces
+// that the kernels share.
+//
+// An ITEM is one (request, K/V head, tile of query rows); the query rows of a K/V head are the
+// request's tokens times the group of query heads that share the head.  An item's cost is the
+// number of token tiles of its context.  Contexts differ by orders of magnitude, so the items'
+// tiles are laid end to end and cut into equal slices, one per resident CTA (the split the
+// cipher kernel uses).  A CTA walks its slice; an item that lies inside it is finished there, an
+// item that a slice boundary cuts leaves its pieces' maxima, sums and unnormalised rows in
+// scratch, and a second kernel joins them.  A slice has at most two such pieces (it enters one
+// item in the middle and leaves one in the middle), so the scratch does not depend on the call.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "gift_batch.cuh"
+
+namespace gift {
+
+struct AttnArgs {
+    BatchArgs b;
+    const char* pages;
+    uint64_t token_bytes;            // K and V of one token
+    uint32_t kv_heads, heads, group;
+    const char* q;
+    uint64_t q_row, q_head;          // strides in bytes
+    char* out;
+    uint64_t out_row, out_head;
+    uint32_t n_rows;
+    float scale_log2;                // scale * log2(e): scores are kept in base 2
+    const uint32_t* mask;
+    uint32_t mask_words;
+    float* lse;
+    int32_t* row_owner;
+    const int32_t* owner_map;
+    uint32_t* status;
+    uint32_t least;                  // smallest slice, in tiles
+    uint32_t n_cta;                  // CTAs of the attention kernel
+    float* part_o;                   // [2 n_cta][rows][D]
+    float2* part_ml;                 // [2 n_cta][rows] running maximum, sum
+    uint32_t* part_bits;             // [2 n_cta] status bits of the piece's pages
+};
+
+constexpr float NEG_INF = -__builtin_huge_valf();
+
+// Shape of a request's items.
+struct ItemShape {
+    uint32_t rows_m;                 // step tokens
+    uint32_t nqt;                    // tiles of query rows
+    uint32_t tiles;                  // token tiles of the context
+    uint64_t units;                  // tiles of all its items
+};
+
+__device__ __forceinline__ ItemShape item_shape(const AttnArgs& a, const ReqShape& s, uint32_t tile_rows, uint32_t tile_tokens)
+{
+    ItemShape i;
+    i.rows_m = s.rows;
+    i.nqt = (uint32_t)(((uint64_t)s.rows * a.group + tile_rows - 1) / tile_rows);
+    i.tiles = (s.want + tile_tokens - 1) / tile_tokens;      // >= 1 when rows > 0
+    i.units = (uint64_t)i.nqt * i.tiles * a.kv_heads;
+    return i;
+}
+
+// Where a unit lies.
+struct Place {
+    uint32_t r;                      // request
+    uint32_t row0;                   // its first row
+    uint64_t off;                    // the unit's index within the request
+};
+
+struct PlaceShared {
+    uint64_t sums[32];
+    Place at;
+};
+
+// Block-wide: the total of the requests' units and the place of unit w * slice.  Returns false
+// (for every thread) when that unit does not exist, or the step has more rows than the caller
+// gave; `first` marks the CTA that writes the status of requests without items.
+template <int THREADS>
+__device__ bool place_unit(const AttnArgs& a, uint32_t w, uint32_t tile_rows, uint32_t tile_tokens, bool first,
+                           PlaceShared* sh, uint64_t* total_out, uint64_t* slice_out)
+{
+    const uint32_t n = a.b.n_req, per = (n + THREADS - 1) / THREADS;
+    const uint32_t r0 = threadIdx.x * per, r1 = r0 + per < n ? r0 + per : n;
+    uint64_t rows = 0, units = 0;
+    for (uint32_t r = r0; r < r1; r++) {
+        const ReqShape s = load_shape(a.b, r);
+        rows += s.rows;
+        units += item_shape(a, s, tile_rows, tile_tokens).units;
+        if (first && s.rows == 0) a.status[r] = s.ok ? 0u : GIFT_ST_BAD_DESC;
+    }
+    uint64_t all_rows, total;
+    const uint64_t incl_rows = block_scan<THREADS>(rows, sh->sums, &all_rows);
+    const uint64_t incl = block_scan<THREADS>(units, sh->sums, &total);
+    if (all_rows > a.n_rows) {
+        if (first)
+            for (uint32_t r = threadIdx.x; r < n; r += THREADS) a.status[r] = GIFT_ST_BAD_TABLE;
+        return false;
+    }
+    const uint64_t slice = slice_units(total, a.n_cta, a.least);
+    const uint64_t u = slice * w;
+    *total_out = total;
+    *slice_out = slice;
+    if (u >= total) return false;
+    uint64_t before = incl - units, row = incl_rows - rows;
+    if (u >= before && u < incl) {
+        for (uint32_t r = r0; r < r1; r++) {
+            const ReqShape s = load_shape(a.b, r);
+            const uint64_t n_u = item_shape(a, s, tile_rows, tile_tokens).units;
+            if (u < before + n_u) {
+                sh->at.r = r;
+                sh->at.row0 = (uint32_t)row;
+                sh->at.off = u - before;
+                break;
+            }
+            before += n_u;
+            row += s.rows;
+        }
+    }
+    __syncthreads();
+    return true;
+}
+
+__device__ __forceinline__ float fast_exp2(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// Whether row i of the step (its mask words at `words`) sees token t.
+__device__ __forceinline__ bool row_sees(const AttnArgs& a, const ReqShape& s, uint32_t i, const uint32_t* words, uint32_t t)
+{
+    if (t < s.have) return true;
+    if (t >= s.want) return false;
+    const uint32_t j = t - s.have;
+    return a.mask ? (words[j >> 5] >> (j & 31)) & 1u : j <= i;
+}
+
+template <class T> __device__ __forceinline__ uint32_t pack2(float lo, float hi);
+template <> __device__ __forceinline__ uint32_t pack2<__nv_bfloat16>(float lo, float hi)
+{
+    const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&v);
+}
+template <> __device__ __forceinline__ uint32_t pack2<__half>(float lo, float hi)
+{
+    const __half2 v = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&v);
+}
+
+template <class T> __device__ __forceinline__ float to_float(T v);
+template <> __device__ __forceinline__ float to_float<__nv_bfloat16>(__nv_bfloat16 v) { return __bfloat162float(v); }
+template <> __device__ __forceinline__ float to_float<__half>(__half v) { return __half2float(v); }
+
+// Whether either half of a pair is infinite or NaN.
+template <class T> __device__ __forceinline__ bool pair_not_finite(uint32_t x)
+{
+    const uint32_t e = std::is_same<T, __half>::value ? 0x7C00u : 0x7F80u;
+    return (x & e) == e || ((x >> 16) & e) == e;
+}
+
+// BAD_DESC stands alone (no other bit is evaluated for a bad descriptor).
+__device__ __forceinline__ uint32_t final_status(uint32_t bits) { return bits & GIFT_ST_BAD_DESC ? GIFT_ST_BAD_DESC : bits; }
+
+// What one item's end writes besides its rows: by the first item of a request.
+template <int THREADS>
+__device__ __forceinline__ void write_request(const AttnArgs& a, uint32_t r, uint32_t row0, uint32_t rows_m, uint32_t bits)
+{
+    if (threadIdx.x == 0) a.status[r] = final_status(bits);
+    if (a.row_owner) {
+        const int32_t o = bits ? GIFT_OWNER_CONFLICT : a.b.owner[r];
+        for (uint32_t t = threadIdx.x; t < rows_m; t += THREADS) a.row_owner[row0 + t] = o;
+    }
+}
+
+}  // namespace gift

@@ -12,7 +12,7 @@
 
 using namespace gift;
 
-#define GIFT_VERSION 200u   // 0.2.0
+#define GIFT_VERSION 300u   // 0.3.0
 
 #include "gift_internal.cuh"
 #include "gift_seg.cuh"
@@ -355,6 +355,7 @@ int gift_ctx_destroy(gift_ctx* c)
         CU_NOTE(cudaFree(c->d_stage_keys));
         CU_NOTE(cudaFree(c->d_snapshot));
         CU_NOTE(cudaFree(c->d_next_sync));
+        CU_NOTE(cudaFree(c->d_attn));
         if (c->h_stage) {
             memset(c->h_stage, 0, (size_t)c->stage_cap * 20);
             CU_NOTE(cudaFreeHost(c->h_stage));

@@ -13,6 +13,7 @@
 
 #include "gift_core.cuh"
 #include "gift_csr.cuh"
+#include "gift_batch.cuh"
 
 using namespace gift;
 
@@ -114,6 +115,20 @@ void hc_slice_piece(uint64_t g0, uint64_t g1, uint64_t p0, uint64_t p1, uint64_t
     const SlicePiece r = slice_piece(g0, g1, p0, p1, nblk, slice);
     out[0] = r.first; out[1] = r.end; out[2] = r.reporters;
 }
+
+// The length arithmetic of the paged-cache calls.
+void hc_req_shape(int32_t owner, int32_t have, int32_t want, uint32_t pt, uint32_t width, uint32_t* out)
+{
+    const ReqShape r = req_shape(owner, have, want, pt, width);
+    out[0] = r.ok ? 1u : 0u; out[1] = r.have; out[2] = r.want; out[3] = r.bh; out[4] = r.bw; out[5] = r.rows;
+}
+
+uint32_t hc_req_of(const uint32_t* first, uint32_t n, uint32_t k) { return req_of(first, n, k); }
+int32_t hc_label_flip(int32_t l) { return label_flip(l); }
+int hc_label_claimed(int32_t l) { return label_claimed(l) ? 1 : 0; }
+uint32_t hc_label_read_status(int32_t l, int32_t owner) { return label_read_status(l, owner); }
+uint32_t hc_label_write_status(int32_t l, int32_t owner) { return label_write_status(l, owner); }
+uint64_t hc_slice_units(uint64_t total, uint32_t n_cta, uint32_t least) { return slice_units(total, n_cta, least); }
 
 }  // extern "C"
 

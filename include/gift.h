@@ -56,6 +56,7 @@ extern "C" {
 #define GIFT_ST_BAD_DESC       16u   /* descriptor misaligned, out of range, or reserved flags set */
 #define GIFT_ST_OVERLAP        32u   /* shares bytes with another segment of the call (only with GIFT_CTX_CHECK_OVERLAP) */
 #define GIFT_ST_NO_BLOCKS      64u   /* block tables: the free pages do not reach to this request */
+#define GIFT_ST_STALLED       256u   /* attention: a wait inside the kernel ran out; the request's rows are zero */
 #define GIFT_ST_BAD_TABLE     128u   /* the call as a whole was refused: free pages, tables or row count malformed */
 
 #define GIFT_OWNER_PARAM     (-1)
@@ -584,7 +585,7 @@ int gift_kv_append(gift_ctx* ctx, const gift_kv_pool* pool, const void* k, uint6
  * request and nothing else is written.  Rows behind the last one are left as they were.
  * q, out: like k in gift_kv_append, in the pool's type; out must overlap no input.  head_dim is
  * 64 or 128.  lse: n_rows x n_heads floats.  The first call on a ctx allocates a fixed scratch
- * (about 80 MB); make it before any stream capture begins.  Graphs that were captured from one
+ * (about 40 MB); make it before any stream capture begins.  Graphs that were captured from one
  * ctx must not run at the same time. */
 typedef struct {
     const void* q;

@@ -17,7 +17,7 @@ LIB_PATH = os.environ.get("GIFT_LIB", os.path.join(_HERE, "libgift.so"))
 
 OK, E_INVAL, E_NOMEM, E_CUDA, E_RANGE, E_ALIGN = 0, -1, -2, -3, -4, -5
 ST_TAG_MISMATCH, ST_OWNER_MISMATCH, ST_UNOWNED, ST_NO_KEY, ST_BAD_DESC, ST_OVERLAP = 1, 2, 4, 8, 16, 32
-ST_NO_BLOCKS, ST_BAD_TABLE = 64, 128
+ST_NO_BLOCKS, ST_BAD_TABLE, ST_STALLED = 64, 128, 256
 CTX_TWO_TABLES, CTX_CHECK_OVERLAP, CTX_SPLIT_LAUNCH = 1, 2, 4
 OWNER_PARAM, OWNER_NONE, OWNER_CONFLICT = -1, -2, -3
 RULE_IDENTITY, RULE_ROWWISE, RULE_SEGREDUCE, RULE_BROADCAST = 0, 1, 2, 3

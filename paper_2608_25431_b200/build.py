@@ -10,7 +10,7 @@ PROBE = os.path.join(HERE, "libgift_probe.so")
 SOURCES = ["gift_lib.cu", "gift_rules.cu", "gift_hostio.cu", "gift_tokens.cu", "gift_order.cu", "gift_index.cu",
            "gift_chain.cu", "gift_blocks.cu", "gift_kv.cu", "gift_attn.cu"]
 HEADERS = ["gf128.cuh", "aes_tt.cuh", "gift_core.cuh", "gift_internal.cuh", "gift_rules.cuh", "gift_csr.cuh", "gift_seg.cuh",
-           "gift_batch.cuh", "gift_kv.cuh", "gift_attn.cuh",
+           "gift_batch.cuh", "gift_kv.cuh", "gift_attn.cuh", "gift_attn_tc.cuh",
            os.path.join("..", "..", "include", "gift.h")]
 
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",

@@ -8,6 +8,7 @@
 #include <type_traits>
 
 #include "gift_attn.cuh"
+#include "gift_attn_tc.cuh"
 #include "gift_internal.cuh"
 #include "gift_kv.cuh"
 
@@ -392,18 +393,19 @@ __global__ void __launch_bounds__(FEW_THREADS, 2) attn_few_kernel(const __grid_c
     }
 }
 
-// Joins the pieces of the items that a slice boundary cuts.  CTA w looks after the item that
-// boundary w cuts, if no earlier boundary cuts it too.
+// Joins the pieces of the items that a slice boundary cuts, 16 rows per CTA.  CTAs (w, *) look after
+// the item that boundary w + 1 cuts, if no earlier boundary cuts it too.
 constexpr int JOIN_THREADS = 128;
+constexpr int JOIN_ROWS = 16;
 
 template <class T, int D, int ROWS, int TILE>
 __global__ void __launch_bounds__(JOIN_THREADS) attn_join_kernel(const __grid_constant__ AttnArgs a)
 {
     constexpr int CH = D / 8;
     __shared__ PlaceShared place;
-    __shared__ float2 s_top[ROWS];
+    __shared__ float2 s_top[JOIN_ROWS];
     __shared__ uint32_t s_bits;
-    const uint32_t w = blockIdx.x + 1;
+    const uint32_t w = blockIdx.x + 1, row_lo = blockIdx.y * JOIN_ROWS;
     uint64_t total, slice;
     if (!place_unit<JOIN_THREADS>(a, w, ROWS, TILE, false, &place, &total, &slice)) return;
     const uint32_t r = place.at.r, row0 = place.at.row0;
@@ -413,24 +415,35 @@ __global__ void __launch_bounds__(JOIN_THREADS) attn_join_kernel(const __grid_co
     if (tb == 0 || tb > slice) return;                 // not cut here, or cut by an earlier boundary as well
     const uint64_t end = slice * w - tb + it.tiles;    // one past the item's last unit
     const uint32_t w_last = (uint32_t)((end - 1) / slice), pieces = w_last - w + 2;
-    const uint32_t h = item / it.nqt, qt = item - h * it.nqt, q0 = qt * ROWS;
+    const uint32_t h = item / it.nqt, qt = item - h * it.nqt, q0 = qt * ROWS + row_lo;
     const uint32_t all_q = it.rows_m * a.group;
-    const uint32_t nr = all_q - q0 < (uint32_t)ROWS ? all_q - q0 : (uint32_t)ROWS;
+    if (q0 >= all_q) return;
+    const uint32_t nr = all_q - q0 < (uint32_t)JOIN_ROWS ? all_q - q0 : (uint32_t)JOIN_ROWS;
     // the item starts in CTA w - 1 (its last piece) and goes on as the first piece of w, w + 1, ...
     auto slot_of = [&](uint32_t p) -> uint64_t { return p == 0 ? 2ull * (w - 1) + 1 : 2ull * (w + p - 1); };
     if (threadIdx.x == 0) s_bits = 0u;
     __syncthreads();
     for (uint32_t p = threadIdx.x; p < pieces; p += JOIN_THREADS)
         if (a.part_bits[slot_of(p)]) atomicOr(&s_bits, a.part_bits[slot_of(p)]);
-    for (uint32_t row = threadIdx.x; row < nr; row += JOIN_THREADS) {
+    // maxima and sums: 8 threads per row, pieces dealt among them
+    {
+        const uint32_t row = threadIdx.x >> 3, sub = threadIdx.x & 7u;
         float top = NEG_INF, sum = 0.f;
-        for (uint32_t p = 0; p < pieces; p++) top = fmaxf(top, a.part_ml[slot_of(p) * ROWS + row].x);
-        const float use = top == NEG_INF ? 0.f : top;
-        for (uint32_t p = 0; p < pieces; p++) {
-            const float2 ml = a.part_ml[slot_of(p) * ROWS + row];
-            sum += ml.y * fast_exp2(ml.x - use);
+        if (row < nr)
+            for (uint32_t p = sub; p < pieces; p += 8) {
+                const float2 ml = a.part_ml[slot_of(p) * ROWS + row_lo + row];
+                const float now = fmaxf(top, ml.x), use = now == NEG_INF ? 0.f : now;
+                sum = sum * fast_exp2(top - use) + ml.y * fast_exp2(ml.x - use);
+                top = now;
+            }
+#pragma unroll
+        for (int d = 1; d < 8; d <<= 1) {
+            const float other_top = __shfl_xor_sync(0xFFFFFFFFu, top, d), other_sum = __shfl_xor_sync(0xFFFFFFFFu, sum, d);
+            const float now = fmaxf(top, other_top), use = now == NEG_INF ? 0.f : now;
+            sum = sum * fast_exp2(top - use) + other_sum * fast_exp2(other_top - use);
+            top = now;
         }
-        s_top[row] = make_float2(top, sum);
+        if (row < nr && sub == 0) s_top[row] = make_float2(top, sum);
     }
     __syncthreads();
     const uint32_t bits = s_bits;
@@ -440,8 +453,9 @@ __global__ void __launch_bounds__(JOIN_THREADS) attn_join_kernel(const __grid_co
         float acc[8];
 #pragma unroll
         for (int e = 0; e < 8; e++) acc[e] = 0.f;
+#pragma unroll 4
         for (uint32_t p = 0; p < pieces; p++) {
-            const uint64_t at = slot_of(p) * ROWS + row;
+            const uint64_t at = slot_of(p) * ROWS + row_lo + row;
             const float f = fast_exp2(a.part_ml[at].x - use);
             const float4* from = reinterpret_cast<const float4*>(a.part_o + at * D + ch * 8);
             const float4 x = from[0], y = from[1];
@@ -459,7 +473,7 @@ __global__ void __launch_bounds__(JOIN_THREADS) attn_join_kernel(const __grid_co
         *reinterpret_cast<uint4*>(a.out + (uint64_t)(row0 + i) * a.out_row + (uint64_t)hq * a.out_head + ch * 16) = v;
         if (a.lse && ch == 0) a.lse[(uint64_t)(row0 + i) * a.heads + hq] = none ? NEG_INF : (top + log2f(sum)) * 0.6931471805599453f;
     }
-    if (h == 0 && qt == 0) write_request<JOIN_THREADS>(a, r, row0, it.rows_m, bits);
+    if (h == 0 && q0 == 0) write_request<JOIN_THREADS>(a, r, row0, it.rows_m, bits);
 }
 
 template <class T, int D, int MT>
@@ -471,7 +485,63 @@ int launch_few(gift_ctx* c, AttnArgs& a, cudaStream_t st)
     a.least = 1;
     attn_few_kernel<T, D, MT><<<a.n_cta, FEW_THREADS, smem, st>>>(a);
     c->launches++;
-    attn_join_kernel<T, D, 16 * MT, FEW_TILE><<<a.n_cta - 1, JOIN_THREADS, 0, st>>>(a);
+    attn_join_kernel<T, D, 16 * MT, FEW_TILE><<<dim3(a.n_cta - 1, MT), JOIN_THREADS, 0, st>>>(a);
+    c->launches++;
+    CU_TRY(cudaGetLastError());
+    return GIFT_OK;
+}
+
+// cuTensorMapEncodeTiled of the driver, looked up once: the library does not link against it.
+typedef CUresult (*EncodeTiled)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+int encode_tiled(EncodeTiled* out)
+{
+    static EncodeTiled fn = nullptr;
+    if (!fn) {
+        void* p = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        CU_TRY(cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &q));
+        if (q != cudaDriverEntryPointSuccess || !p) return GIFT_E_CUDA;
+        fn = reinterpret_cast<EncodeTiled>(p);
+    }
+    *out = fn;
+    return GIFT_OK;
+}
+
+// The pool as rows of one token: row = slot, 64 columns at a time, rows gathered one by one.
+int slot_map_of_pool(const AttnArgs& a, bool half, uint32_t head_dim, CUtensorMap* map)
+{
+    EncodeTiled encode;
+    const int rc = encode_tiled(&encode);
+    if (rc != GIFT_OK) return rc;
+    const cuuint64_t dims[2] = {(cuuint64_t)2 * a.kv_heads * head_dim, a.b.n_pages ? (cuuint64_t)a.b.n_pages * a.b.page_tokens : 1};
+    const cuuint64_t strides[1] = {a.token_bytes};
+    const cuuint32_t box[2] = {64, 1}, steps[2] = {1, 1};
+    if (encode(map, half ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<char*>(a.pages), dims,
+               strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+        return GIFT_E_CUDA;
+    return GIFT_OK;
+}
+
+template <class T, int D>
+int launch_many(gift_ctx* c, AttnArgs& a, cudaStream_t st)
+{
+    CUtensorMap map;
+    const int rc = slot_map_of_pool(a, std::is_same<T, __half>::value, D, &map);
+    if (rc != GIFT_OK) return rc;
+    constexpr int smem = TcSmem<D>::bytes;
+    CU_TRY(cudaFuncSetAttribute(attn_tc_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+    a.n_cta = 2u * c->num_sms;
+    a.least = 4;
+    // the kernel takes the maximum before it scales: the scale must be positive (0 becomes a factor that
+    // makes every finite score 0 in effect, and keeps a hidden token's minus infinity what it is)
+    a.negate = a.scale_log2 < 0.f ? 1u : 0u;
+    a.scale_log2 = fmaxf(fabsf(a.scale_log2), 1e-30f);
+    attn_tc_kernel<T, D><<<a.n_cta, TC_THREADS, smem, st>>>(a, map);
+    c->launches++;
+    attn_join_kernel<T, D, TC_ROWS, TC_TILE><<<dim3(a.n_cta - 1, TC_ROWS / JOIN_ROWS), JOIN_THREADS, 0, st>>>(a);
     c->launches++;
     CU_TRY(cudaGetLastError());
     return GIFT_OK;
@@ -482,10 +552,10 @@ int launch_attn(gift_ctx* c, AttnArgs& a, cudaStream_t st)
 {
     // rows of an average request's K/V head
     const uint64_t rows = ((uint64_t)a.n_rows + a.b.n_req - 1) / a.b.n_req * a.group;
-    return rows <= 16 ? launch_few<T, D, 1>(c, a, st) : launch_few<T, D, 2>(c, a, st);
+    return rows <= 16 ? launch_few<T, D, 1>(c, a, st) : rows <= 32 ? launch_few<T, D, 2>(c, a, st) : launch_many<T, D>(c, a, st);
 }
 
-constexpr uint32_t PART_ROWS = 32;       // most rows of a tile of query rows
+constexpr uint32_t PART_ROWS = TC_ROWS;  // most rows of a tile of query rows
 constexpr uint32_t PART_D = 128;
 
 // The scratch is allocated once, at a size that no call exceeds, and stays where it is until the

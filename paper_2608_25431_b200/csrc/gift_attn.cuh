@@ -30,6 +30,7 @@ struct AttnArgs {
     uint64_t out_row, out_head;
     uint32_t n_rows;
     float scale_log2;                // scale * log2(e): scores are kept in base 2
+    uint32_t negate;                 // tcgen05 kernel: scale_log2 is the positive one, q is negated
     const uint32_t* mask;
     uint32_t mask_words;
     float* lse;

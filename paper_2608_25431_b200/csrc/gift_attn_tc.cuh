@@ -1,0 +1,641 @@
+// Attention over the labelled paged cache, many query rows per K/V head: tcgen05 products.
+//
+// A tile of 128 query rows meets tiles of 64 tokens.  S = Q K^T (128 x 64, 32-bit) lands in tensor
+// memory, one row per thread of four softmax warps; P, rounded to the pool's type, goes back
+// into the tensor-memory columns of its S and is the A operand of O += P V, whose accumulator
+// (128 x D) stays in tensor memory for the whole piece.  Roles, which meet on mbarriers alone:
+//   warps 0-3  softmax: thread = query row; running maximum and sum in registers
+//   warp 4     brings Q and the K tiles into swizzled shared memory, warp 5 the V tiles.  A page holds
+//              any number of tokens, so a tile is gathered row by row: one TMA gather per 4 tokens
+//              and 64 elements, whose row numbers are slots.  Rows past the context are given a
+//              slot out of range, which reads as zeros, so that what memory holds there does not
+//              matter.  Warp 4 also looks at the pages' labels.
+//   warp 6     one thread issues the products: Q K^T of tile j + 1 runs while the softmax of tile
+//              j does; P V of tile j follows.
+// O is rescaled only when a row's maximum has grown by more than 2^8 over the one in use: p is then at
+// most 2^8, which neither 16-bit type minds, and nearly all tiles leave O alone.
+// 2 CTAs per SM share its tensor memory (256 of 512 columns each) and hide each other's waits.
+//
+// Every wait is bounded; a CTA whose wait runs out flags the rest of its slice (GIFT_ST_STALLED).
+#pragma once
+#include <cuda.h>
+
+#include "gift_attn.cuh"
+
+namespace gift {
+
+constexpr int TC_ROWS = 128;
+constexpr int TC_TILE = 64;
+constexpr int TC_THREADS = 224;
+constexpr int TC_STAGES = 2;
+constexpr int TC_BITS_RING = 4;      // the copies finish at most two pieces ahead of the softmax (see below)
+constexpr uint32_t TC_SPINS = 1u << 20;
+
+template <int D> struct TcSmem {
+    static constexpr uint32_t half_rows(uint32_t rows) { return rows * 128u; }        // 64 elements of each row
+    static constexpr uint32_t q = 0;                                                  // [D/64][128][64]
+    static constexpr uint32_t k = TC_ROWS * D * 2;                                    // [stage][D/64][64][64]
+    static constexpr uint32_t v = k + TC_STAGES * TC_TILE * D * 2;
+    static constexpr uint32_t bytes = v + TC_STAGES * TC_TILE * D * 2;
+};
+
+struct TcShared {
+    uint64_t k_full[TC_STAGES], k_empty[TC_STAGES], v_full[TC_STAGES], v_empty[TC_STAGES];
+    uint64_t s_full[2], p_full[2], o_done[2], q_full, q_empty, last;
+    uint32_t tmem;
+    uint32_t bits[TC_BITS_RING];
+    int odd[2];                      // P V of this S buffer's tile is done by the softmax warps
+    int dead;
+    PlaceShared place;
+};
+
+__device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+
+__device__ __forceinline__ void bar_init(uint64_t* b, uint32_t count)
+{
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(b)), "r"(count) : "memory");
+}
+__device__ __forceinline__ void bar_arrive(uint64_t* b)
+{
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(b)) : "memory");
+}
+// Arrives and announces how many bytes the copies will bring in this phase.
+__device__ __forceinline__ void bar_expect(uint64_t* b, uint32_t bytes)
+{
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(smem_u32(b)), "r"(bytes) : "memory");
+}
+// 64 elements from column x of four rows of the map; the rows land behind one another, 128 bytes each.
+__device__ __forceinline__ void gather4(uint32_t dst, const CUtensorMap* map, int32_t x, const int32_t (&row)[4], uint64_t* b)
+{
+    asm volatile(
+        "cp.async.bulk.tensor.2d.shared::cta.global.tile::gather4.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];"
+        ::"r"(dst), "l"(map), "r"(x), "r"(row[0]), "r"(row[1]), "r"(row[2]), "r"(row[3]), "r"(smem_u32(b)) : "memory");
+}
+__device__ __forceinline__ bool bar_try(uint64_t* b, uint32_t parity)
+{
+    uint32_t done;
+    asm volatile(
+        "{\n .reg .pred p;\n"
+        " mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n"
+        " selp.u32 %0, 1, 0, p;\n}"
+        : "=r"(done) : "r"(smem_u32(b)), "r"(parity) : "memory");
+    return done != 0u;
+}
+// Waits until the barrier's phase with this parity is complete; false when that takes too long, or
+// another role of the CTA has given up.
+__device__ __forceinline__ bool bar_wait(uint64_t* b, uint32_t parity, volatile int* dead)
+{
+    for (uint32_t i = 0; i < TC_SPINS; i++) {
+        if (bar_try(b, parity)) return true;
+        if ((i & 255u) == 255u && *dead) return false;
+    }
+    *dead = 1;
+    return false;
+}
+// The same for a whole warp, with one answer for all its lanes.
+__device__ __forceinline__ bool warp_wait(uint64_t* b, uint32_t parity, volatile int* dead)
+{
+    return __all_sync(0xFFFFFFFFu, bar_wait(b, parity, dead));
+}
+
+__device__ __forceinline__ void cp_row16(uint32_t dst, const void* src, uint32_t bytes)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+
+// Shared-memory operand descriptor, 128-byte swizzle: start, stride between 64-element column blocks
+// (operands with the column dimension contiguous), stride between groups of 8 rows.
+__device__ __forceinline__ uint64_t smem_desc(uint32_t addr, uint32_t block_stride, uint32_t group_stride)
+{
+    return (uint64_t)((addr >> 4) & 0x3FFFu) | ((uint64_t)((block_stride >> 4) & 0x3FFFu) << 16) |
+           ((uint64_t)((group_stride >> 4) & 0x3FFFu) << 32) | (1ull << 46) | (2ull << 61);
+}
+
+// Instruction descriptor of kind::f16: 32-bit accumulator, both operands of type T, M x N, B either
+// with k contiguous (0) or with n contiguous (1).
+template <class T> __host__ __device__ constexpr uint32_t instr_desc(uint32_t m, uint32_t n, uint32_t b_n_major)
+{
+    const uint32_t t = std::is_same<T, __half>::value ? 0u : 1u;
+    return (1u << 4) | (t << 7) | (t << 10) | (b_n_major << 16) | ((n >> 3) << 17) | ((m >> 4) << 24);
+}
+
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add)
+{
+    asm volatile(
+        "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
+        " tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}"
+        ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add) : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool add)
+{
+    asm volatile(
+        "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
+        " tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}"
+        ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)add) : "memory");
+}
+// The barrier is told when all products issued so far are complete.
+__device__ __forceinline__ void mma_commit(uint64_t* b)
+{
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(b)) : "memory");
+}
+__device__ __forceinline__ void tc_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// 32 columns of this thread's tensor-memory row.  The wait names the registers, so that nothing that
+// uses them is moved before it.
+__device__ __forceinline__ void tc_ld32(uint32_t (&r)[32], uint32_t addr)
+{
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+        "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+          "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]),
+          "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]),
+          "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void tc_pin32(uint32_t (&r)[32])
+{
+    asm volatile("" : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]),
+                 "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]));
+    asm volatile("" : "+r"(r[16]), "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]), "+r"(r[23]),
+                 "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31]));
+}
+__device__ __forceinline__ void tc_st32(uint32_t addr, const uint32_t (&r)[32])
+{
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+        "{%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};"
+        ::"r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+          "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]),
+          "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]),
+          "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+        : "memory");
+}
+
+__device__ __forceinline__ void tc_ld8(uint32_t (&r)[8], uint32_t addr)
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void tc_pin8(uint32_t (&r)[8])
+{
+    asm volatile("" : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]));
+}
+// One column, waited for.
+__device__ __forceinline__ uint32_t tc_ld1(uint32_t addr)
+{
+    uint32_t r;
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];\n tcgen05.wait::ld.sync.aligned;" : "=r"(r) : "r"(addr) : "memory");
+    return r;
+}
+__device__ __forceinline__ void tc_st8(uint32_t addr, const uint32_t (&r)[8])
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
+                 ::"r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
+}
+
+// The pieces of a CTA's slice, in order; every role walks them for itself.
+struct Walk {
+    ReqShape s;
+    ItemShape it;
+    uint32_t r, row0;
+    uint64_t off, left;
+    // the current piece
+    uint32_t tb, n_tiles, h, qt, all_q;
+
+    __device__ void start(const AttnArgs& a, const Place& p, uint64_t units)
+    {
+        r = p.r; row0 = p.row0; off = p.off; left = units;
+        s = load_shape(a.b, r);
+        it = item_shape(a, s, TC_ROWS, TC_TILE);
+        n_tiles = 0;
+    }
+    __device__ bool next(const AttnArgs& a)
+    {
+        off += n_tiles;
+        left -= n_tiles;
+        if (left == 0) return false;
+        while (off >= it.units) {
+            off -= it.units;
+            row0 += it.rows_m;
+            r++;
+            s = load_shape(a.b, r);
+            it = item_shape(a, s, TC_ROWS, TC_TILE);
+        }
+        const uint32_t item = (uint32_t)(off / it.tiles);
+        tb = (uint32_t)(off - (uint64_t)item * it.tiles);
+        n_tiles = (uint64_t)(it.tiles - tb) < left ? it.tiles - tb : (uint32_t)left;
+        h = item / it.nqt;
+        qt = item - h * it.nqt;
+        all_q = it.rows_m * a.group;
+        return true;
+    }
+    // more step tokens than the mask has bits: the request is refused without looking at the mask
+    __device__ bool masked_short(const AttnArgs& a) const { return a.mask && it.rows_m > a.mask_words * 32u; }
+};
+
+// Which of the 64 tokens from t0 on row i of the step sees, as bits.
+__device__ __forceinline__ uint64_t row_sees64(const AttnArgs& a, const Walk& w, uint32_t i, uint32_t t0)
+{
+    const uint32_t j0 = t0 > w.s.have ? t0 - w.s.have : 0u;            // first step token at or after t0
+    const uint32_t cached = t0 < w.s.have ? w.s.have - t0 : 0u;
+    if (cached >= 64u) return ~0ull;
+    uint64_t own;                                                      // bit b: step token j0 + b
+    if (a.mask) {
+        const uint32_t* words = a.mask + (uint64_t)(w.row0 + i) * a.mask_words;
+        const uint32_t k = j0 >> 5, sh = j0 & 31u;
+        const uint64_t lo = k < a.mask_words ? words[k] : 0u, mid = k + 1 < a.mask_words ? words[k + 1] : 0u;
+        const uint64_t hi = k + 2 < a.mask_words ? words[k + 2] : 0u;
+        own = ((lo | (mid << 32)) >> sh) | (sh ? hi << (64u - sh) : 0ull);
+    } else {
+        const uint32_t n = i >= j0 ? i - j0 + 1u : 0u;
+        own = n >= 64u ? ~0ull : (1ull << n) - 1ull;
+    }
+    uint64_t sees = (own << cached) | ((1ull << cached) - 1ull);
+    const uint32_t there = w.s.want - t0;                              // tokens from t0 to the end, > 0
+    if (there < 64u) sees &= (1ull << there) - 1ull;
+    return sees;
+}
+
+template <class T, int D>
+__global__ void __launch_bounds__(TC_THREADS, 2) attn_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensorMap map)
+{
+    constexpr uint32_t CH = D / 8;                         // 16-byte chunks of a row
+    constexpr uint32_t TMEM_COLS = 256;                    // 2 S, O; a power of two, half of what an SM has
+    constexpr uint32_t S_COL = 0, O_COL = 2 * TC_TILE;
+    extern __shared__ __align__(1024) char smem[];
+    __shared__ TcShared sh;
+    using L = TcSmem<D>;
+
+    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < TC_STAGES; i++) {
+            bar_init(&sh.k_full[i], 1); bar_init(&sh.k_empty[i], 1);
+            bar_init(&sh.v_full[i], 1); bar_init(&sh.v_empty[i], 1);
+        }
+        for (int i = 0; i < 2; i++) { bar_init(&sh.s_full[i], 1); bar_init(&sh.p_full[i], 4); bar_init(&sh.o_done[i], 1); sh.odd[i] = 0; }
+        bar_init(&sh.q_full, 1); bar_init(&sh.q_empty, 1); bar_init(&sh.last, 1);
+        for (int i = 0; i < TC_BITS_RING; i++) sh.bits[i] = 0u;
+        sh.dead = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    uint64_t total, slice;
+    // ends with a barrier for every thread, taken or not
+    const bool some = place_unit<TC_THREADS>(a, blockIdx.x, TC_ROWS, TC_TILE, blockIdx.x == 0, &sh.place, &total, &slice);
+    if (!some) return;
+    if (warp == 6) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sh.tmem)), "r"(TMEM_COLS) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc_before();
+    __syncthreads();
+    tc_after();
+    const uint32_t tmem = sh.tmem;
+    volatile int* dead = &sh.dead;
+    const uint64_t units = slice < total - slice * blockIdx.x ? slice : total - slice * blockIdx.x;
+    const uint32_t sm = smem_u32(smem);
+    Walk w;
+    w.start(a, sh.place.at, units);
+
+    if (warp == 4 || warp == 5) {
+        // ------------------------------------------------------------------ copies
+        // Lane l gathers tokens 4 (l % 16) .. + 3 of a tile, elements 64 (l / 16) .. + 63 of their rows.
+        const uint32_t kv = warp - 4, quad = (lane & 15u) * 4, col = D == 128 ? lane >> 4 : 0u;
+        const bool mine = D == 128 || lane < 16;
+        uint64_t* full = kv ? sh.v_full : sh.k_full;
+        uint64_t* empty = kv ? sh.v_empty : sh.k_empty;
+        uint32_t n = 0, piece = 0;                         // tiles and pieces so far
+        bool ok = true;
+        while (ok && w.next(a)) {
+            const int32_t owner = a.b.owner[w.r];
+            const int32_t* table = a.b.table + (uint64_t)w.r * a.b.max_blocks;
+            const int32_t x = (int32_t)((kv * a.kv_heads + w.h) * D + col * 64);
+            uint32_t bits = w.masked_short(a) ? GIFT_ST_BAD_DESC : 0u;
+            if (kv == 0) {
+                // Q, once the products of the piece before have read the old rows
+                ok = piece == 0 || warp_wait(&sh.q_empty, (piece - 1) & 1u, dead);
+                if (!ok) break;
+                const uint32_t chunk = lane % CH, sub = lane / CH;
+#pragma unroll 4
+                for (uint32_t row = sub; row < (uint32_t)TC_ROWS; row += 32 / CH) {
+                    const uint32_t rho = w.qt * TC_ROWS + row;
+                    const bool there = rho < w.all_q;
+                    const uint32_t i = there ? rho / a.group : 0u, hq = w.h * a.group + (there ? rho - i * a.group : 0u);
+                    const char* src = a.q + (uint64_t)(w.row0 + i) * a.q_row + (uint64_t)hq * a.q_head + chunk * 16;
+                    cp_row16(sm + L::q + (chunk >> 3) * (TC_ROWS * 128) + row * 128 + (((chunk & 7u) ^ (row & 7u)) << 4), src, there ? 16u : 0u);
+                }
+                asm volatile("cp.async.commit_group;" ::: "memory");
+            }
+            int32_t next[4];                               // table entries, fetched a tile ahead
+            auto entries = [&](uint32_t j) {
+#pragma unroll
+                for (int e = 0; e < 4; e++) {
+                    const uint32_t t = (w.tb + j) * TC_TILE + quad + e;
+                    next[e] = j < w.n_tiles && t < w.s.want ? table[t / a.b.page_tokens] : -1;
+                }
+            };
+            entries(0);
+            int32_t label[4] = {GIFT_OWNER_PARAM, GIFT_OWNER_PARAM, GIFT_OWNER_PARAM, GIFT_OWNER_PARAM};   // judged a tile later
+            for (uint32_t j = 0; j < w.n_tiles; j++, n++) {
+                const uint32_t stage = n % TC_STAGES, round = n / TC_STAGES;
+                int32_t slot[4], page[4];
+#pragma unroll
+                for (int e = 0; e < 4; e++) bits |= label_read_status(label[e], owner);
+#pragma unroll
+                for (int e = 0; e < 4; e++) {
+                    const uint32_t t = (w.tb + j) * TC_TILE + quad + e;
+                    const bool fine = next[e] >= 0 && (uint32_t)next[e] < a.b.n_pages;
+                    page[e] = fine ? next[e] : -1;
+                    slot[e] = fine ? (int32_t)((uint32_t)next[e] * a.b.page_tokens + t % a.b.page_tokens) : -1;
+                    if (t < w.s.want && !fine) bits |= GIFT_ST_BAD_DESC;
+                }
+                entries(j + 1);
+                if (kv == 0 && a.owner_map) {
+#pragma unroll
+                    for (int e = 0; e < 4; e++) label[e] = page[e] >= 0 ? a.owner_map[page[e]] : GIFT_OWNER_PARAM;
+                }
+                ok = round == 0 || warp_wait(&empty[stage], (round - 1) & 1u, dead);
+                if (!ok) break;
+                if (mine) gather4(sm + (kv ? L::v : L::k) + stage * (TC_TILE * D * 2) + col * (TC_TILE * 128) + quad * 128, &map, x, slot, &full[stage]);
+                if (kv == 0 && j + 1 == w.n_tiles) {
+                    // the piece's verdict, before the last tile is announced
+#pragma unroll
+                    for (int e = 0; e < 4; e++) bits |= label_read_status(label[e], owner);
+                    bits = __reduce_or_sync(0xFFFFFFFFu, bits);
+                    if (lane == 0 && bits) atomicOr(&sh.bits[piece % TC_BITS_RING], bits);
+                }
+                __syncwarp();
+                if (lane == 0) bar_expect(&full[stage], TC_TILE * D * 2);
+                if (kv == 0 && j == 0) {
+                    asm volatile("cp.async.wait_group 0;" ::: "memory");
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0) bar_arrive(&sh.q_full);
+                }
+            }
+            piece++;
+        }
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        if (*dead) {
+            // nobody may be left to wait for the copies under way: they end before the CTA does
+            for (uint32_t k = n > TC_STAGES ? n - TC_STAGES : 0; k < n; k++)
+                for (uint32_t i = 0; i < TC_SPINS && !bar_try(&full[k % TC_STAGES], (k / TC_STAGES) & 1u); i++) {}
+        }
+    } else if (warp == 6) {
+        // ------------------------------------------------------------------ products
+        if (lane == 0) {
+            // a negative scale: the products negate q, so that the scale used on the scores is positive
+            const uint32_t id_s = instr_desc<T>(TC_ROWS, TC_TILE, 0) | (a.negate << 13);
+            constexpr uint32_t id_o = instr_desc<T>(TC_ROWS, D, 1);
+            uint32_t n = 0, piece = 0;
+            bool ok = true;
+            auto scores = [&](uint32_t j) {                // S of the slice's j-th tile
+                const uint32_t stage = j % TC_STAGES;
+                if (!bar_wait(&sh.k_full[stage], (j / TC_STAGES) & 1u, dead)) return false;
+                tc_after();
+                const uint32_t kb = sm + L::k + stage * (TC_TILE * D * 2);
+#pragma unroll
+                for (uint32_t ks = 0; ks < D / 16; ks++) {
+                    const uint64_t da = smem_desc(sm + L::q + (ks >> 2) * (TC_ROWS * 128) + (ks & 3u) * 32, 16, 1024);
+                    const uint64_t db = smem_desc(kb + (ks >> 2) * (TC_TILE * 128) + (ks & 3u) * 32, 16, 1024);
+                    mma_ss(tmem + S_COL + (j & 1u) * TC_TILE, da, db, id_s, ks > 0);
+                }
+                mma_commit(&sh.k_empty[stage]);
+                mma_commit(&sh.s_full[j & 1u]);
+                return true;
+            };
+            while (ok && w.next(a)) {
+                ok = bar_wait(&sh.q_full, piece & 1u, dead) && (n < 2 || bar_wait(&sh.o_done[n & 1u], ((n - 2) >> 1) & 1u, dead)) && scores(n);
+                if (ok && w.n_tiles == 1) mma_commit(&sh.q_empty);
+                for (uint32_t j = 0; ok && j < w.n_tiles; j++, n++) {
+                    if (j + 1 < w.n_tiles) {
+                        // S of tile n + 1 takes the columns that held P of tile n - 1
+                        ok = (n == 0 || bar_wait(&sh.o_done[(n - 1) & 1u], ((n - 1) >> 1) & 1u, dead)) && scores(n + 1);
+                        if (ok && j + 2 == w.n_tiles) mma_commit(&sh.q_empty);
+                    }
+                    const uint32_t stage = n % TC_STAGES;
+                    ok = ok && bar_wait(&sh.v_full[stage], (n / TC_STAGES) & 1u, dead) && bar_wait(&sh.p_full[n & 1u], (n >> 1) & 1u, dead);
+                    if (!ok) break;
+                    tc_after();
+                    if (!*(volatile int*)&sh.odd[n & 1u]) {
+                        const uint32_t vb = sm + L::v + stage * (TC_TILE * D * 2);
+#pragma unroll
+                        for (uint32_t ks = 0; ks < TC_TILE / 16; ks++)
+                            mma_ts(tmem + O_COL, tmem + S_COL + (n & 1u) * TC_TILE + ks * 8, smem_desc(vb + ks * 2048, TC_TILE * 128, 1024),
+                                   id_o, j > 0 || ks > 0);
+                    }
+                    mma_commit(&sh.v_empty[stage]);
+                    mma_commit(&sh.o_done[n & 1u]);
+                }
+                piece++;
+            }
+            // nothing may be in flight when the tensor memory is given back
+            mma_commit(&sh.last);
+            for (uint32_t i = 0; i < TC_SPINS && !bar_try(&sh.last, 0); i++) {}
+        }
+        __syncwarp();
+    } else {
+        // ------------------------------------------------------------------ softmax
+        const uint32_t row = threadIdx.x, lane_base = (warp * 32u) << 16;
+        uint32_t n = 0, piece = 0;
+        bool alive = true;
+        while (w.next(a)) {
+            const uint32_t rho = w.qt * TC_ROWS + row;
+            const bool there = rho < w.all_q;
+            const bool warp_there = w.qt * TC_ROWS + warp * 32 < w.all_q;
+            const uint32_t i = there ? rho / a.group : 0u, hq = w.h * a.group + (there ? rho - i * a.group : 0u);
+            const bool masked_short = w.masked_short(a);
+            float m = NEG_INF, l = 0.f;                    // the maximum in use, the sum relative to it
+            for (uint32_t j = 0; alive && j < w.n_tiles; j++, n++) {
+                const uint32_t s_at = tmem + lane_base + S_COL + (n & 1u) * TC_TILE;
+                const uint32_t t0 = (w.tb + j) * TC_TILE;
+                const bool mixed = t0 + TC_TILE > w.s.have;
+                if (!warp_wait(&sh.s_full[n & 1u], (n >> 1) & 1u, dead)) { alive = false; break; }
+                // every tile's P V is waited for in turn, two tiles on, when it has long been done: a barrier
+                // that was not looked at for two phases cannot be told from one that is a phase behind
+                if (n >= 2 && !warp_wait(&sh.o_done[n & 1u], ((n - 2) >> 1) & 1u, dead)) { alive = false; break; }
+                bool odd = false;
+                if (mixed) {
+                    // 0 * inf is NaN: if a v of a tile whose tokens some rows may not see is not finite, the
+                    // tile's product is taken token by token, over what each row sees
+                    const uint32_t stage = n % TC_STAGES;
+                    if (!warp_wait(&sh.v_full[stage], (n / TC_STAGES) & 1u, dead)) { alive = false; break; }
+                    const uint4* v = reinterpret_cast<const uint4*>(smem + L::v + stage * (TC_TILE * D * 2));
+#pragma unroll 8
+                    for (uint32_t x = lane; x < TC_TILE * CH; x += 32) {
+                        const uint4 q = v[x];
+                        odd |= pair_not_finite<T>(q.x) || pair_not_finite<T>(q.y) || pair_not_finite<T>(q.z) || pair_not_finite<T>(q.w);
+                    }
+                    odd = __any_sync(0xFFFFFFFFu, odd);    // every warp has seen the whole tile: one answer for all
+                }
+                // after s_full: the product of tile n - 2, which used this flag, has been issued
+                if (row == 0) *(volatile int*)&sh.odd[n & 1u] = odd ? 1 : 0;
+                if (!warp_there) {                         // rows that do not exist: whatever P holds stays in them
+                    __syncwarp();
+                    if (lane == 0) bar_arrive(&sh.p_full[n & 1u]);
+                    continue;
+                }
+                tc_after();
+                uint32_t sc[2][32];
+                tc_ld32(sc[0], s_at);
+                tc_ld32(sc[1], s_at + 32);
+                tc_wait_ld();
+                tc_pin32(sc[0]);
+                tc_pin32(sc[1]);
+                uint64_t sees = ~0ull;
+                if (mixed) {
+                    sees = there && !masked_short ? row_sees64(a, w, i, t0) : 0ull;
+#pragma unroll
+                    for (int x = 0; x < 2; x++)
+#pragma unroll
+                        for (int c = 0; c < 32; c++)
+                            if (!((uint32_t)(sees >> (32 * x)) >> c & 1u)) sc[x][c] = 0xFF800000u;      // minus infinity
+                }
+                float tops[4] = {NEG_INF, NEG_INF, NEG_INF, NEG_INF};
+#pragma unroll
+                for (int x = 0; x < 2; x++)
+#pragma unroll
+                    for (int c = 0; c < 32; c++) tops[c & 3] = fmaxf(tops[c & 3], __uint_as_float(sc[x][c]));
+                // the scale is positive here (q's sign carries it), so the largest score stays the largest
+                const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])) * a.scale_log2;
+                const bool grow = top > m + 8.f;           // also when nothing has been seen yet
+                float alpha = 1.f;
+                if (grow) {
+                    alpha = fast_exp2(m - top);            // 0 from minus infinity
+                    m = top;
+                }
+                const float minus = m == NEG_INF ? 0.f : -m;
+                float sums[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int x = 0; x < 2; x++)
+#pragma unroll
+                    for (int c = 0; c < 32; c++) {
+                        const float p = fast_exp2(fmaf(__uint_as_float(sc[x][c]), a.scale_log2, minus));
+                        sc[x][c] = __float_as_uint(p);
+                        sums[c & 3] += p;
+                    }
+                l = l * alpha + ((sums[0] + sums[1]) + (sums[2] + sums[3]));
+                if (!odd) {
+                    // P into the first 32 columns of its S
+                    uint32_t pk[32];
+#pragma unroll
+                    for (int x = 0; x < 2; x++)
+#pragma unroll
+                        for (int c = 0; c < 16; c++)
+                            pk[x * 16 + c] = pack2<T>(__uint_as_float(sc[x][2 * c]), __uint_as_float(sc[x][2 * c + 1]));
+                    tc_st32(s_at, pk);
+                }
+                const bool rescale = j > 0 && __any_sync(0xFFFFFFFFu, grow && there);
+                if ((rescale || odd) && n > 0) {
+                    // every product so far is in O (the one of tile n is not issued before p_full)
+                    if (!warp_wait(&sh.o_done[(n - 1) & 1u], ((n - 1) >> 1) & 1u, dead)) { alive = false; break; }
+                    tc_after();
+                }
+                if (odd) {
+                    // p, in 32 bits, into the columns of its S; then column by column (rare: registers matter more)
+                    tc_st32(s_at, sc[0]);
+                    tc_st32(s_at + 32, sc[1]);
+                    tc_wait_st();
+#pragma unroll 1
+                    for (uint32_t ch = 0; ch < CH; ch++) {
+                        uint32_t o[8];
+                        tc_ld8(o, tmem + lane_base + O_COL + ch * 8);
+                        tc_wait_ld();
+                        tc_pin8(o);
+#pragma unroll
+                        for (int e = 0; e < 8; e++) o[e] = j > 0 ? __float_as_uint(__uint_as_float(o[e]) * alpha) : 0u;
+                        const char* v = smem + L::v + (n % TC_STAGES) * (TC_TILE * D * 2) + (ch >> 3) * (TC_TILE * 128);
+#pragma unroll 1
+                        for (uint32_t t = 0; t < 64; t++) {
+                            const uint4 q = *reinterpret_cast<const uint4*>(v + t * 128 + (((ch & 7u) ^ (t & 7u)) << 4));
+                            const uint32_t pair[4] = {q.x, q.y, q.z, q.w};
+                            const float p = __uint_as_float(tc_ld1(s_at + t));
+                            const bool seen = sees >> t & 1ull;
+#pragma unroll
+                            for (int y = 0; y < 8; y++) {
+                                const T* e = reinterpret_cast<const T*>(&pair[y >> 1]);
+                                if (seen) o[y] = __float_as_uint(__uint_as_float(o[y]) + p * to_float<T>(e[y & 1]));
+                            }
+                            __syncwarp();
+                        }
+                        tc_st8(tmem + lane_base + O_COL + ch * 8, o);
+                    }
+                } else if (rescale) {
+                    for (uint32_t c0 = 0; c0 < (uint32_t)D; c0 += 32) {
+                        uint32_t o[32];
+                        tc_ld32(o, tmem + lane_base + O_COL + c0);
+                        tc_wait_ld();
+                        tc_pin32(o);
+#pragma unroll
+                        for (int c = 0; c < 32; c++) o[c] = __float_as_uint(__uint_as_float(o[c]) * alpha);
+                        tc_st32(tmem + lane_base + O_COL + c0, o);
+                    }
+                }
+                tc_wait_st();
+                tc_before();
+                __syncwarp();
+                if (lane == 0) bar_arrive(&sh.p_full[n & 1u]);
+            }
+            // ---------------------------------------------------------- the piece's end
+            if (alive && n >= 2) alive = warp_wait(&sh.o_done[n & 1u], ((n - 2) >> 1) & 1u, dead);
+            if (alive) alive = warp_wait(&sh.o_done[(n - 1) & 1u], ((n - 1) >> 1) & 1u, dead);
+            tc_after();
+            uint32_t bits = alive ? *(volatile uint32_t*)&sh.bits[piece % TC_BITS_RING] : GIFT_ST_STALLED;
+            const bool whole = w.tb == 0 && w.n_tiles == w.it.tiles;
+            const uint32_t slot = blockIdx.x * 2u + (w.tb == 0 ? 1u : 0u);
+            const bool none = bits != 0u || l == 0.f;
+            const float inv = none ? 0.f : 1.f / l;
+            if (warp_there) {
+                for (uint32_t c0 = 0; c0 < (uint32_t)D; c0 += 32) {
+                    uint32_t o[32];
+                    tc_ld32(o, tmem + lane_base + O_COL + c0);
+                    tc_wait_ld();
+                    tc_pin32(o);
+                    if (there && whole) {
+                        uint4* to = reinterpret_cast<uint4*>(a.out + (uint64_t)(w.row0 + i) * a.out_row + (uint64_t)hq * a.out_head + c0 * 2);
+#pragma unroll
+                        for (int x = 0; x < 4; x++) {
+                            uint4 v = make_uint4(0u, 0u, 0u, 0u);
+                            if (!none) {
+                                v.x = pack2<T>(__uint_as_float(o[8 * x]) * inv, __uint_as_float(o[8 * x + 1]) * inv);
+                                v.y = pack2<T>(__uint_as_float(o[8 * x + 2]) * inv, __uint_as_float(o[8 * x + 3]) * inv);
+                                v.z = pack2<T>(__uint_as_float(o[8 * x + 4]) * inv, __uint_as_float(o[8 * x + 5]) * inv);
+                                v.w = pack2<T>(__uint_as_float(o[8 * x + 6]) * inv, __uint_as_float(o[8 * x + 7]) * inv);
+                            }
+                            to[x] = v;
+                        }
+                    } else if (there) {
+                        uint4* to = reinterpret_cast<uint4*>(a.part_o + ((uint64_t)slot * TC_ROWS + row) * D + c0);
+#pragma unroll
+                        for (int x = 0; x < 8; x++) to[x] = make_uint4(o[4 * x], o[4 * x + 1], o[4 * x + 2], o[4 * x + 3]);
+                    }
+                    __syncwarp();
+                }
+                if (there) {
+                    if (!whole) a.part_ml[(uint64_t)slot * TC_ROWS + row] = make_float2(m, l);
+                    else if (a.lse) a.lse[(uint64_t)(w.row0 + i) * a.heads + hq] = none ? NEG_INF : (m + log2f(l)) * 0.6931471805599453f;
+                }
+            }
+            if (whole) {
+                if (w.h == 0 && w.qt == 0) write_request<128>(a, w.r, w.row0, w.it.rows_m, bits);
+            } else if (row == 0) {
+                a.part_bits[slot] = bits;
+            }
+            // the ring's entry is used again four pieces on: clear it once all four warps have read it
+            asm volatile("barrier.cta.sync 1, 128;" ::: "memory");
+            if (row == 0) *(volatile uint32_t*)&sh.bits[piece % TC_BITS_RING] = 0u;
+            tc_before();
+            piece++;
+        }
+    }
+    __syncthreads();
+    if (warp == 6) {
+        tc_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(TMEM_COLS) : "memory");
+    }
+}
+
+}  // namespace gift

@@ -88,30 +88,21 @@ __global__ void __launch_bounds__(FEW_THREADS, 2) attn_few_kernel(const __grid_c
     __shared__ uint32_t s_bits;
 
     uint64_t total, slice;
-    if (!place_unit<FEW_THREADS>(a, blockIdx.x, ROWS, FEW_TILE, blockIdx.x == 0, &place, &total, &slice)) return;
+    if (!place_unit<FEW_THREADS>(a, blockIdx.x, FEW_TILE, blockIdx.x == 0, &place, &total, &slice)) return;
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t ring = (uint32_t)__cvta_generic_to_shared(smem) + warp * (FEW_STAGES * 2 * HALF);
 
-    uint32_t r = place.at.r, row0 = place.at.row0;
-    uint64_t off = place.at.off, left = slice < total - slice * blockIdx.x ? slice : total - slice * blockIdx.x;
-    ReqShape s = load_shape(a.b, r);
-    ItemShape it = item_shape(a, s, ROWS, FEW_TILE);
-    while (left > 0) {
-        while (off >= it.units) {
-            off -= it.units;
-            row0 += it.rows_m;
-            r++;
-            s = load_shape(a.b, r);
-            it = item_shape(a, s, ROWS, FEW_TILE);
-        }
-        const uint32_t item = (uint32_t)(off / it.tiles), tb = (uint32_t)(off - (uint64_t)item * it.tiles);
-        const uint32_t n_tiles = (uint64_t)(it.tiles - tb) < left ? it.tiles - tb : (uint32_t)left;
-        const uint32_t h = item / it.nqt, qt = item - h * it.nqt;
+    Walk<FEW_TILE> w;
+    w.start(a, place.at, slice < total - slice * blockIdx.x ? slice : total - slice * blockIdx.x);
+    while (w.next(a)) {
+        const ReqShape& s = w.s;
+        const ItemShape& it = w.it;
+        const uint32_t r = w.r, row0 = w.row0, tb = w.tb, n_tiles = w.n_tiles, h = w.h, qt = w.qt;
         const uint32_t all_q = it.rows_m * a.group;                // query rows of the K/V head
         const uint32_t q0 = qt * ROWS;
         const int32_t owner = a.b.owner[r];
         const int32_t* table = a.b.table + (uint64_t)r * a.b.max_blocks;
-        uint32_t bits = a.mask && it.rows_m > a.mask_words * 32u ? GIFT_ST_BAD_DESC : 0u;
+        uint32_t bits = w.masked_short(a) ? GIFT_ST_BAD_DESC : 0u;
 
         // this lane's query rows g and g + 8 of every 16-row tile
         const uint32_t g = lane >> 2, c2 = (lane & 3) * 2;
@@ -124,7 +115,7 @@ __global__ void __launch_bounds__(FEW_THREADS, 2) attn_few_kernel(const __grid_c
             for (int half = 0; half < 2; half++) {
                 const uint32_t rho = q0 + mt * 16 + half * 8 + g;
                 const bool there = rho < all_q;
-                const uint32_t i = there ? rho / a.group : 0u, hq = h * a.group + (there ? rho - i * a.group : 0u);
+                const uint32_t i = there ? a.by_group.quot(rho) : 0u, hq = h * a.group + (there ? rho - i * a.group : 0u);
                 row_i[mt][half] = i;
                 words[mt][half] = a.mask + (uint64_t)(row0 + i) * a.mask_words;
                 const char* q = a.q + (uint64_t)(row0 + i) * a.q_row + (uint64_t)hq * a.q_head;
@@ -153,7 +144,7 @@ __global__ void __launch_bounds__(FEW_THREADS, 2) attn_few_kernel(const __grid_c
         const uint32_t my = lane & 15u;
         auto entry = [&](uint32_t step) -> int32_t {
             const uint32_t t = (tb + step) * FEW_TILE + warp * 16 + my;
-            return step < n_tiles && t < s.want ? table[t / a.b.page_tokens] : -1;
+            return step < n_tiles && t < s.want ? table[a.b.page.quot(t)] : -1;
         };
         int32_t next = entry(0);
         uint32_t label_bits = 0;
@@ -167,7 +158,7 @@ __global__ void __launch_bounds__(FEW_THREADS, 2) attn_few_kernel(const __grid_c
                 const bool valid = t < s.want, ok = valid && page >= 0 && (uint32_t)page < a.b.n_pages;
                 uint64_t src = 0;
                 if (ok) {
-                    src = ((uint64_t)(uint32_t)page * a.b.page_tokens + t % a.b.page_tokens) * a.token_bytes + (uint64_t)h * (D * 2);
+                    src = ((uint64_t)(uint32_t)page * a.b.page_tokens + (t - a.b.page.quot(t) * a.b.page_tokens)) * a.token_bytes + (uint64_t)h * (D * 2);
                     if (a.owner_map) label_bits = label_read_status(a.owner_map[page], owner);
                 } else if (valid) {
                     bits |= GIFT_ST_BAD_DESC;
@@ -364,7 +355,7 @@ __global__ void __launch_bounds__(FEW_THREADS, 2) attn_few_kernel(const __grid_c
                 acc[4] += f * y.x; acc[5] += f * y.y; acc[6] += f * y.z; acc[7] += f * y.w;
             }
             if (whole) {
-                const uint32_t rho = q0 + row, i = rho / a.group, hq = h * a.group + (rho - i * a.group);
+                const uint32_t rho = q0 + row, i = a.by_group.quot(rho), hq = h * a.group + (rho - i * a.group);
                 const bool none = bits != 0u || sum == 0.f;
                 const float inv = none ? 0.f : 1.f / sum;
                 uint4 v = make_uint4(0u, 0u, 0u, 0u);
@@ -388,8 +379,6 @@ __global__ void __launch_bounds__(FEW_THREADS, 2) attn_few_kernel(const __grid_c
             a.part_bits[slot] = bits;
         }
         __syncthreads();                               // smem is free for the next piece
-        off += n_tiles;
-        left -= n_tiles;
     }
 }
 
@@ -407,18 +396,20 @@ __global__ void __launch_bounds__(JOIN_THREADS) attn_join_kernel(const __grid_co
     __shared__ uint32_t s_bits;
     const uint32_t w = blockIdx.x + 1, row_lo = blockIdx.y * JOIN_ROWS;
     uint64_t total, slice;
-    if (!place_unit<JOIN_THREADS>(a, w, ROWS, TILE, false, &place, &total, &slice)) return;
+    if (!place_unit<JOIN_THREADS>(a, w, TILE, false, &place, &total, &slice)) return;
     const uint32_t r = place.at.r, row0 = place.at.row0;
     const ReqShape s = load_shape(a.b, r);
-    const ItemShape it = item_shape(a, s, ROWS, TILE);
-    const uint32_t item = (uint32_t)(place.at.off / it.tiles), tb = (uint32_t)(place.at.off - (uint64_t)item * it.tiles);
-    if (tb == 0 || tb > slice) return;                 // not cut here, or cut by an earlier boundary as well
-    const uint64_t end = slice * w - tb + it.tiles;    // one past the item's last unit
+    const ItemShape it = item_shape(a, s, TILE);
+    const uint32_t item = place.at.item, u = place.at.u;
+    // not cut here (the boundary lies before the item's first tile or behind it), or cut by an earlier boundary as well
+    if (u <= a.extra || (uint64_t)u > slice + a.extra) return;
+    const uint64_t end = slice * w - u + it.cost;      // one past the item's last unit
     const uint32_t w_last = (uint32_t)((end - 1) / slice), pieces = w_last - w + 2;
-    const uint32_t h = item / it.nqt, qt = item - h * it.nqt, q0 = qt * ROWS + row_lo;
+    const uint32_t h = item / it.nqt, qt = item - h * it.nqt, q0 = qt * a.tile_rows + row_lo;
     const uint32_t all_q = it.rows_m * a.group;
-    if (q0 >= all_q) return;
-    const uint32_t nr = all_q - q0 < (uint32_t)JOIN_ROWS ? all_q - q0 : (uint32_t)JOIN_ROWS;
+    const uint32_t in_tile = all_q - qt * a.tile_rows < a.tile_rows ? all_q - qt * a.tile_rows : a.tile_rows;
+    if (row_lo >= in_tile) return;
+    const uint32_t nr = in_tile - row_lo < (uint32_t)JOIN_ROWS ? in_tile - row_lo : (uint32_t)JOIN_ROWS;
     // the item starts in CTA w - 1 (its last piece) and goes on as the first piece of w, w + 1, ...
     auto slot_of = [&](uint32_t p) -> uint64_t { return p == 0 ? 2ull * (w - 1) + 1 : 2ull * (w + p - 1); };
     if (threadIdx.x == 0) s_bits = 0u;
@@ -462,7 +453,7 @@ __global__ void __launch_bounds__(JOIN_THREADS) attn_join_kernel(const __grid_co
             acc[0] += f * x.x; acc[1] += f * x.y; acc[2] += f * x.z; acc[3] += f * x.w;
             acc[4] += f * y.x; acc[5] += f * y.y; acc[6] += f * y.z; acc[7] += f * y.w;
         }
-        const uint32_t rho = q0 + row, i = rho / a.group, hq = h * a.group + (rho - i * a.group);
+        const uint32_t rho = q0 + row, i = a.by_group.quot(rho), hq = h * a.group + (rho - i * a.group);
         const bool none = bits != 0u || sum == 0.f;
         const float inv = none ? 0.f : 1.f / sum;
         uint4 v = make_uint4(0u, 0u, 0u, 0u);
@@ -482,7 +473,10 @@ int launch_few(gift_ctx* c, AttnArgs& a, cudaStream_t st)
     constexpr int smem = FewSmem<D, MT>::bytes;
     CU_TRY(cudaFuncSetAttribute(attn_few_kernel<T, D, MT>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
     a.n_cta = 2u * c->num_sms;
+    a.tile_rows = 16 * MT;
+    a.by_tile_rows = fixed_div(a.tile_rows);
     a.least = 1;
+    a.extra = 1;
     attn_few_kernel<T, D, MT><<<a.n_cta, FEW_THREADS, smem, st>>>(a);
     c->launches++;
     attn_join_kernel<T, D, 16 * MT, FEW_TILE><<<dim3(a.n_cta - 1, MT), JOIN_THREADS, 0, st>>>(a);
@@ -509,7 +503,7 @@ int encode_tiled(EncodeTiled* out)
     return GIFT_OK;
 }
 
-// The pool as rows of one token: row = slot, 64 columns at a time, rows gathered one by one.
+// The pool as rows of one token (row = slot), taken a run of rows by 64 columns at a time.
 int slot_map_of_pool(const AttnArgs& a, bool half, uint32_t head_dim, CUtensorMap* map)
 {
     EncodeTiled encode;
@@ -517,9 +511,26 @@ int slot_map_of_pool(const AttnArgs& a, bool half, uint32_t head_dim, CUtensorMa
     if (rc != GIFT_OK) return rc;
     const cuuint64_t dims[2] = {(cuuint64_t)2 * a.kv_heads * head_dim, a.b.n_pages ? (cuuint64_t)a.b.n_pages * a.b.page_tokens : 1};
     const cuuint64_t strides[1] = {a.token_bytes};
-    const cuuint32_t box[2] = {64, 1}, steps[2] = {1, 1};
+    const cuuint32_t box[2] = {64, a.run < 8 ? 1 : a.run}, steps[2] = {1, 1};     // gathers take boxes of one row
     if (encode(map, half ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<char*>(a.pages), dims,
                strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+        return GIFT_E_CUDA;
+    return GIFT_OK;
+}
+
+// Q as (columns, heads, rows): a box holds the group's heads of as many tokens as a tile of rows takes.
+int map_of_q(const AttnArgs& a, bool half, uint32_t head_dim, CUtensorMap* map)
+{
+    EncodeTiled encode;
+    const int rc = encode_tiled(&encode);
+    if (rc != GIFT_OK) return rc;
+    const cuuint64_t dims[3] = {head_dim, a.heads, a.n_rows};
+    // the stride of a dimension of one entry is never used, but may not be 0
+    const cuuint64_t strides[2] = {a.heads > 1 ? a.q_head : head_dim * 2, a.n_rows > 1 ? a.q_row : (cuuint64_t)a.heads * head_dim * 2};
+    const cuuint32_t box[3] = {64, a.group, (cuuint32_t)(TC_ROWS / a.group)}, steps[3] = {1, 1, 1};
+    if (encode(map, half ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<char*>(a.q), dims, strides,
+               box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
         return GIFT_E_CUDA;
     return GIFT_OK;
@@ -528,18 +539,24 @@ int slot_map_of_pool(const AttnArgs& a, bool half, uint32_t head_dim, CUtensorMa
 template <class T, int D>
 int launch_many(gift_ctx* c, AttnArgs& a, cudaStream_t st)
 {
-    CUtensorMap map;
-    const int rc = slot_map_of_pool(a, std::is_same<T, __half>::value, D, &map);
+    a.run = a.b.page_tokens & (0u - a.b.page_tokens);
+    if (a.run > (uint32_t)TC_TILE) a.run = TC_TILE;
+    CUtensorMap map, q_map;
+    int rc = slot_map_of_pool(a, std::is_same<T, __half>::value, D, &map);
+    if (rc == GIFT_OK) rc = map_of_q(a, std::is_same<T, __half>::value, D, &q_map);
     if (rc != GIFT_OK) return rc;
     constexpr int smem = TcSmem<D>::bytes;
     CU_TRY(cudaFuncSetAttribute(attn_tc_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
     a.n_cta = 2u * c->num_sms;
+    a.tile_rows = TC_ROWS / a.group * a.group;             // whole tokens
+    a.by_tile_rows = fixed_div(a.tile_rows);
     a.least = 4;
+    a.extra = 8;
     // the kernel takes the maximum before it scales: the scale must be positive (0 becomes a factor that
     // makes every finite score 0 in effect, and keeps a hidden token's minus infinity what it is)
     a.negate = a.scale_log2 < 0.f ? 1u : 0u;
     a.scale_log2 = fmaxf(fabsf(a.scale_log2), 1e-30f);
-    attn_tc_kernel<T, D><<<a.n_cta, TC_THREADS, smem, st>>>(a, map);
+    attn_tc_kernel<T, D><<<a.n_cta, TC_THREADS, smem, st>>>(a, map, q_map);
     c->launches++;
     attn_join_kernel<T, D, TC_ROWS, TC_TILE><<<dim3(a.n_cta - 1, TC_ROWS / JOIN_ROWS), JOIN_THREADS, 0, st>>>(a);
     c->launches++;
@@ -550,9 +567,12 @@ int launch_many(gift_ctx* c, AttnArgs& a, cudaStream_t st)
 template <class T, int D>
 int launch_attn(gift_ctx* c, AttnArgs& a, cudaStream_t st)
 {
+    // what the tensor maps of the tcgen05 kernel do not describe: groups of more heads than a tile has
+    // rows, a q whose rows or heads share memory
+    const bool plain_q = a.group <= (uint32_t)TC_ROWS && (a.n_rows == 1 || a.q_row > 0) && (a.heads == 1 || a.q_head > 0);
     // rows of an average request's K/V head
     const uint64_t rows = ((uint64_t)a.n_rows + a.b.n_req - 1) / a.b.n_req * a.group;
-    return rows <= 16 ? launch_few<T, D, 1>(c, a, st) : rows <= 32 ? launch_few<T, D, 2>(c, a, st) : launch_many<T, D>(c, a, st);
+    return rows <= 16 ? launch_few<T, D, 1>(c, a, st) : rows <= 32 || !plain_q ? launch_few<T, D, 2>(c, a, st) : launch_many<T, D>(c, a, st);
 }
 
 constexpr uint32_t PART_ROWS = TC_ROWS;  // most rows of a tile of query rows
@@ -599,6 +619,7 @@ extern "C" int gift_kv_attention(gift_ctx* c, const gift_batch* batch, const gif
     a.pages = static_cast<const char*>(pool->pages);
     a.token_bytes = (uint64_t)pool->n_heads * pool->head_dim * 4;
     a.kv_heads = pool->n_heads; a.heads = t->n_heads; a.group = t->n_heads / pool->n_heads;
+    a.by_group = fixed_div(a.group);
     a.q = static_cast<const char*>(t->q); a.q_row = t->q_row_stride * 2; a.q_head = t->q_head_stride * 2;
     a.out = static_cast<char*>(t->out); a.out_row = t->out_row_stride * 2; a.out_head = t->out_head_stride * 2;
     a.n_rows = t->n_rows;

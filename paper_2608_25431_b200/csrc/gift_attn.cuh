@@ -2,8 +2,10 @@
 // that the kernels share.
 //
 // An ITEM is one (request, K/V head, tile of query rows); the query rows of a K/V head are the
-// request's tokens times the group of query heads that share the head.  An item's cost is the
-// number of token tiles of its context.  Contexts differ by orders of magnitude, so the items'
+// request's tokens times the group of query heads that share the head.  An item costs the
+// token tiles of its context and, before the first of them, some tiles' time for its start and end
+// (`extra`): a batch whose shortest contexts are a few tiles would otherwise give one CTA
+// many more items than the others.  Contexts differ by orders of magnitude, so the items'
 // tiles are laid end to end and cut into equal slices, one per resident CTA (the split the
 // cipher kernel uses).  A CTA walks its slice; an item that lies inside it is finished there, an
 // item that a slice boundary cuts leaves its pieces' maxima, sums and unnormalised rows in
@@ -24,12 +26,14 @@ struct AttnArgs {
     const char* pages;
     uint64_t token_bytes;            // K and V of one token
     uint32_t kv_heads, heads, group;
+    FixedDiv by_group, by_tile_rows;
     const char* q;
     uint64_t q_row, q_head;          // strides in bytes
     char* out;
     uint64_t out_row, out_head;
     uint32_t n_rows;
     float scale_log2;                // scale * log2(e): scores are kept in base 2
+    uint32_t run;                    // tcgen05 kernel: tokens that are one copy (see there); below 8: gathered
     uint32_t negate;                 // tcgen05 kernel: scale_log2 is the positive one, q is negated
     const uint32_t* mask;
     uint32_t mask_words;
@@ -37,7 +41,9 @@ struct AttnArgs {
     int32_t* row_owner;
     const int32_t* owner_map;
     uint32_t* status;
+    uint32_t tile_rows;              // query rows of an item, at most
     uint32_t least;                  // smallest slice, in tiles
+    uint32_t extra;                  // tiles that an item costs beyond its own
     uint32_t n_cta;                  // CTAs of the attention kernel
     float* part_o;                   // [2 n_cta][rows][D]
     float2* part_ml;                 // [2 n_cta][rows] running maximum, sum
@@ -51,16 +57,19 @@ struct ItemShape {
     uint32_t rows_m;                 // step tokens
     uint32_t nqt;                    // tiles of query rows
     uint32_t tiles;                  // token tiles of the context
-    uint64_t units;                  // tiles of all its items
+    uint32_t cost;                   // units of one item: extra, then its tiles
+    uint64_t units;                  // units of all its items
 };
 
-__device__ __forceinline__ ItemShape item_shape(const AttnArgs& a, const ReqShape& s, uint32_t tile_rows, uint32_t tile_tokens)
+__device__ __forceinline__ ItemShape item_shape(const AttnArgs& a, const ReqShape& s, uint32_t tile_tokens)
 {
     ItemShape i;
     i.rows_m = s.rows;
-    i.nqt = (uint32_t)(((uint64_t)s.rows * a.group + tile_rows - 1) / tile_rows);
+    // rows * group fits 31 bits unless the step has more rows than the call, which is refused on the rows alone
+    i.nqt = a.by_tile_rows.cover(s.rows * a.group & 0x7FFFFFFFu);
     i.tiles = (s.want + tile_tokens - 1) / tile_tokens;      // >= 1 when rows > 0
-    i.units = (uint64_t)i.nqt * i.tiles * a.kv_heads;
+    i.cost = i.tiles + a.extra;
+    i.units = (uint64_t)i.nqt * i.cost * a.kv_heads;
     return i;
 }
 
@@ -68,7 +77,7 @@ __device__ __forceinline__ ItemShape item_shape(const AttnArgs& a, const ReqShap
 struct Place {
     uint32_t r;                      // request
     uint32_t row0;                   // its first row
-    uint64_t off;                    // the unit's index within the request
+    uint32_t item, u;                // the request's item, the unit's index within it
 };
 
 struct PlaceShared {
@@ -80,16 +89,17 @@ struct PlaceShared {
 // (for every thread) when that unit does not exist, or the step has more rows than the caller
 // gave; `first` marks the CTA that writes the status of requests without items.
 template <int THREADS>
-__device__ bool place_unit(const AttnArgs& a, uint32_t w, uint32_t tile_rows, uint32_t tile_tokens, bool first,
+__device__ bool place_unit(const AttnArgs& a, uint32_t w, uint32_t tile_tokens, bool first,
                            PlaceShared* sh, uint64_t* total_out, uint64_t* slice_out)
 {
     const uint32_t n = a.b.n_req, per = (n + THREADS - 1) / THREADS;
     const uint32_t r0 = threadIdx.x * per, r1 = r0 + per < n ? r0 + per : n;
     uint64_t rows = 0, units = 0;
+#pragma unroll 1
     for (uint32_t r = r0; r < r1; r++) {
         const ReqShape s = load_shape(a.b, r);
         rows += s.rows;
-        units += item_shape(a, s, tile_rows, tile_tokens).units;
+        units += item_shape(a, s, tile_tokens).units;
         if (first && s.rows == 0) a.status[r] = s.ok ? 0u : GIFT_ST_BAD_DESC;
     }
     uint64_t all_rows, total;
@@ -107,22 +117,85 @@ __device__ bool place_unit(const AttnArgs& a, uint32_t w, uint32_t tile_rows, ui
     if (u >= total) return false;
     uint64_t before = incl - units, row = incl_rows - rows;
     if (u >= before && u < incl) {
+#pragma unroll 1
         for (uint32_t r = r0; r < r1; r++) {
             const ReqShape s = load_shape(a.b, r);
-            const uint64_t n_u = item_shape(a, s, tile_rows, tile_tokens).units;
-            if (u < before + n_u) {
+            const ItemShape it = item_shape(a, s, tile_tokens);
+            if (u < before + it.units) {
                 sh->at.r = r;
                 sh->at.row0 = (uint32_t)row;
-                sh->at.off = u - before;
+                sh->at.item = (uint32_t)((u - before) / it.cost);
+                sh->at.u = (uint32_t)((u - before) - (uint64_t)sh->at.item * it.cost);
                 break;
             }
-            before += n_u;
+            before += it.units;
             row += s.rows;
         }
     }
     __syncthreads();
     return true;
 }
+
+// The pieces of a CTA's slice, in order.
+template <uint32_t TILE> struct Walk {
+    ReqShape s;
+    ItemShape it;
+    uint32_t r, row0;
+    uint32_t u;                      // units of the current item that are done
+    uint64_t left;                   // units to go
+    int32_t next_owner, next_have, next_want;       // of request r + 1, fetched ahead
+    // the current piece: K/V head, tile of query rows, token tiles
+    uint32_t h, qt, tb, n_tiles, all_q;
+
+    __device__ __forceinline__ void fetch(const AttnArgs& a)
+    {
+        const uint32_t k = r + 1 < a.b.n_req ? r + 1 : r;
+        next_owner = a.b.owner[k]; next_have = a.b.have[k]; next_want = a.b.want[k];
+    }
+    __device__ __forceinline__ void start(const AttnArgs& a, const Place& p, uint64_t units)
+    {
+        r = p.r; row0 = p.row0; left = units;
+        s = load_shape(a.b, r);
+        it = item_shape(a, s, TILE);
+        fetch(a);
+        u = (uint32_t)p.u;
+        h = p.item / it.nqt;
+        qt = p.item - h * it.nqt;
+        all_q = it.rows_m * a.group;
+    }
+    __device__ __forceinline__ bool next(const AttnArgs& a)
+    {
+        while (left > 0) {
+            if (u >= it.cost) {
+                u = 0;
+                if (++qt == it.nqt) {
+                    qt = 0;
+                    if (++h == a.kv_heads) {
+                        h = 0;
+                        do {
+                            row0 += it.rows_m;
+                            r++;
+                            s = req_shape(next_owner, next_have, next_want, a.b.page, a.b.max_blocks);
+                            it = item_shape(a, s, TILE);
+                            fetch(a);
+                        } while (it.nqt == 0);
+                        all_q = it.rows_m * a.group;
+                    }
+                }
+            }
+            const uint32_t used = (uint64_t)(it.cost - u) < left ? it.cost - u : (uint32_t)left;
+            const uint32_t end = u + used;
+            tb = u > a.extra ? u - a.extra : 0u;
+            n_tiles = (end > a.extra ? end - a.extra : 0u) - tb;       // none when the units end in the item's extra
+            u = end;
+            left -= used;
+            if (n_tiles) return true;
+        }
+        return false;
+    }
+    // more step tokens than the mask has bits: the request is refused without looking at the mask
+    __device__ __forceinline__ bool masked_short(const AttnArgs& a) const { return a.mask && it.rows_m > a.mask_words * 32u; }
+};
 
 __device__ __forceinline__ float fast_exp2(float x)
 {

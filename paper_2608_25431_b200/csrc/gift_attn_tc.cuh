@@ -1,17 +1,21 @@
 // Attention over the labelled paged cache, many query rows per K/V head: tcgen05 products.
 //
-// A tile of 128 query rows meets tiles of 64 tokens.  S = Q K^T (128 x 64, 32-bit) lands in tensor
+// A tile of 128 query rows (or what whole tokens fit) meets tiles of 64 tokens.  S = Q K^T (128 x 64, 32-bit) lands in tensor
 // memory, one row per thread of four softmax warps; P, rounded to the pool's type, goes back
 // into the tensor-memory columns of its S and is the A operand of O += P V, whose accumulator
 // (128 x D) stays in tensor memory for the whole piece.  Roles, which meet on mbarriers alone:
 //   warps 0-3  softmax: thread = query row; running maximum and sum in registers
-//   warp 4     brings Q and the K tiles into swizzled shared memory, warp 5 the V tiles.  A page holds
-//              any number of tokens, so a tile is gathered row by row: one TMA gather per 4 tokens
-//              and 64 elements, whose row numbers are slots.  Rows past the context are given a
-//              slot out of range, which reads as zeros, so that what memory holds there does not
-//              matter.  Warp 4 also looks at the pages' labels.
-//   warp 6     one thread issues the products: Q K^T of tile j + 1 runs while the softmax of tile
-//              j does; P V of tile j follows.
+//   warp 4     brings Q and the K tiles into swizzled shared memory, warp 5 the V tiles, by TMA.  What
+//              is contiguous in a page is a run of tokens: the largest power of two, up to a tile,
+//              that divides the page.  A run is one copy of 64 columns.  A TMA copy costs some 37
+//              clocks of the SM's one unit however little it brings, so pages whose runs are
+//              shorter than 8 tokens are gathered 4 tokens to a copy (measured: 875 us where runs
+//              of 16 take 547).  Rows outside the map read as zeros: that is where the runs past
+//              the context are sent.  Warp 4 also looks at the pages' labels.
+//   warp 6     one thread issues Q K^T: tile j + 1's runs while the softmax of tile j does.
+//   warp 7     looks over the V tiles that hold step tokens (below), and one thread issues P V.  Two
+//              issuers, because what one thread spends on a tile (waits, descriptors, commits) was
+//              the longest part of the cycle.
 // O is rescaled only when a row's maximum has grown by more than 2^8 over the one in use: p is then at
 // most 2^8, which neither 16-bit type minds, and nearly all tiles leave O alone.
 // 2 CTAs per SM share its tensor memory (256 of 512 columns each) and hide each other's waits.
@@ -26,25 +30,26 @@ namespace gift {
 
 constexpr int TC_ROWS = 128;
 constexpr int TC_TILE = 64;
-constexpr int TC_THREADS = 224;
+constexpr int TC_THREADS = 256;
 constexpr int TC_STAGES = 2;
 constexpr int TC_BITS_RING = 4;      // the copies finish at most two pieces ahead of the softmax (see below)
-constexpr uint32_t TC_SPINS = 1u << 20;
+constexpr uint32_t TC_SPINS = 1u << 16, TC_SUSPEND_NS = 1000;        // a wait gives up after some 70 ms
 
 template <int D> struct TcSmem {
     static constexpr uint32_t half_rows(uint32_t rows) { return rows * 128u; }        // 64 elements of each row
     static constexpr uint32_t q = 0;                                                  // [D/64][128][64]
     static constexpr uint32_t k = TC_ROWS * D * 2;                                    // [stage][D/64][64][64]
     static constexpr uint32_t v = k + TC_STAGES * TC_TILE * D * 2;
-    static constexpr uint32_t bytes = v + TC_STAGES * TC_TILE * D * 2;
+    static constexpr uint32_t o = v + TC_STAGES * TC_TILE * D * 2;                    // [4 warps][32 rows][64 bytes]
+    static constexpr uint32_t bytes = o + 4 * 32 * 64;
 };
 
 struct TcShared {
     uint64_t k_full[TC_STAGES], k_empty[TC_STAGES], v_full[TC_STAGES], v_empty[TC_STAGES];
-    uint64_t s_full[2], p_full[2], o_done[2], q_full, q_empty, last;
+    uint64_t s_full[2], p_full[2], o_done[2], checked[2], q_full, q_empty, last;
     uint32_t tmem;
     uint32_t bits[TC_BITS_RING];
-    int odd[2];                      // P V of this S buffer's tile is done by the softmax warps
+    int odd[2];                      // P V of the tile with step tokens in this stage is done by the softmax warps
     int dead;
     PlaceShared place;
 };
@@ -71,20 +76,33 @@ __device__ __forceinline__ void gather4(uint32_t dst, const CUtensorMap* map, in
         "cp.async.bulk.tensor.2d.shared::cta.global.tile::gather4.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];"
         ::"r"(dst), "l"(map), "r"(x), "r"(row[0]), "r"(row[1]), "r"(row[2]), "r"(row[3]), "r"(smem_u32(b)) : "memory");
 }
+// 64 columns from x of a box of heads and tokens of q.
+__device__ __forceinline__ void copy_q(uint32_t dst, const CUtensorMap* map, int32_t x, int32_t head, int32_t token, uint64_t* b)
+{
+    asm volatile("cp.async.bulk.tensor.3d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+                 ::"r"(dst), "l"(map), "r"(x), "r"(head), "r"(token), "r"(smem_u32(b)) : "memory");
+}
+// 64 columns from x of a run of rows from `row`.
+__device__ __forceinline__ void copy_run(uint32_t dst, const CUtensorMap* map, int32_t x, int32_t row, uint64_t* b)
+{
+    asm volatile("cp.async.bulk.tensor.2d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+                 ::"r"(dst), "l"(map), "r"(x), "r"(row), "r"(smem_u32(b)) : "memory");
+}
 __device__ __forceinline__ bool bar_try(uint64_t* b, uint32_t parity)
 {
     uint32_t done;
     asm volatile(
         "{\n .reg .pred p;\n"
-        " mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n"
+        " mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n"
         " selp.u32 %0, 1, 0, p;\n}"
-        : "=r"(done) : "r"(smem_u32(b)), "r"(parity) : "memory");
+        : "=r"(done) : "r"(smem_u32(b)), "r"(parity), "r"(TC_SUSPEND_NS) : "memory");
     return done != 0u;
 }
 // Waits until the barrier's phase with this parity is complete; false when that takes too long, or
 // another role of the CTA has given up.
-__device__ __forceinline__ bool bar_wait(uint64_t* b, uint32_t parity, volatile int* dead)
+__device__ __noinline__ bool bar_wait_long(uint64_t* b, uint32_t parity, volatile int* dead)
 {
+#pragma unroll 1
     for (uint32_t i = 0; i < TC_SPINS; i++) {
         if (bar_try(b, parity)) return true;
         if ((i & 255u) == 255u && *dead) return false;
@@ -92,15 +110,14 @@ __device__ __forceinline__ bool bar_wait(uint64_t* b, uint32_t parity, volatile 
     *dead = 1;
     return false;
 }
+__device__ __forceinline__ bool bar_wait(uint64_t* b, uint32_t parity, volatile int* dead)
+{
+    return bar_try(b, parity) || bar_wait_long(b, parity, dead);
+}
 // The same for a whole warp, with one answer for all its lanes.
 __device__ __forceinline__ bool warp_wait(uint64_t* b, uint32_t parity, volatile int* dead)
 {
     return __all_sync(0xFFFFFFFFu, bar_wait(b, parity, dead));
-}
-
-__device__ __forceinline__ void cp_row16(uint32_t dst, const void* src, uint32_t bytes)
-{
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
 
 // Shared-memory operand descriptor, 128-byte swizzle: start, stride between 64-element column blocks
@@ -184,6 +201,13 @@ __device__ __forceinline__ void tc_pin8(uint32_t (&r)[8])
 {
     asm volatile("" : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]));
 }
+__device__ __forceinline__ void tc_st16(uint32_t addr, const uint32_t (&r)[16])
+{
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
+        ::"r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+          "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
+}
 // One column, waited for.
 __device__ __forceinline__ uint32_t tc_ld1(uint32_t addr)
 {
@@ -197,48 +221,23 @@ __device__ __forceinline__ void tc_st8(uint32_t addr, const uint32_t (&r)[8])
                  ::"r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
 }
 
-// The pieces of a CTA's slice, in order; every role walks them for itself.
-struct Walk {
-    ReqShape s;
-    ItemShape it;
-    uint32_t r, row0;
-    uint64_t off, left;
-    // the current piece
-    uint32_t tb, n_tiles, h, qt, all_q;
+using TcWalk = Walk<TC_TILE>;
 
-    __device__ void start(const AttnArgs& a, const Place& p, uint64_t units)
-    {
-        r = p.r; row0 = p.row0; off = p.off; left = units;
-        s = load_shape(a.b, r);
-        it = item_shape(a, s, TC_ROWS, TC_TILE);
-        n_tiles = 0;
-    }
-    __device__ bool next(const AttnArgs& a)
-    {
-        off += n_tiles;
-        left -= n_tiles;
-        if (left == 0) return false;
-        while (off >= it.units) {
-            off -= it.units;
-            row0 += it.rows_m;
-            r++;
-            s = load_shape(a.b, r);
-            it = item_shape(a, s, TC_ROWS, TC_TILE);
-        }
-        const uint32_t item = (uint32_t)(off / it.tiles);
-        tb = (uint32_t)(off - (uint64_t)item * it.tiles);
-        n_tiles = (uint64_t)(it.tiles - tb) < left ? it.tiles - tb : (uint32_t)left;
-        h = item / it.nqt;
-        qt = item - h * it.nqt;
-        all_q = it.rows_m * a.group;
-        return true;
-    }
-    // more step tokens than the mask has bits: the request is refused without looking at the mask
-    __device__ bool masked_short(const AttnArgs& a) const { return a.mask && it.rows_m > a.mask_words * 32u; }
-};
+// A role's walk lies in shared memory: its two dozen words are used at a piece's ends, and the softmax
+// threads need every register in between (spills go through what little L1 the tiles leave, and made
+// an item's end several times as long).
+__device__ __noinline__ bool walk_next(TcWalk& w, const AttnArgs& a, uint32_t lane)
+{
+    TcWalk x = w;
+    const bool more = x.next(a);
+    __syncwarp();
+    if (lane == 0) w = x;
+    __syncwarp();
+    return more;
+}
 
 // Which of the 64 tokens from t0 on row i of the step sees, as bits.
-__device__ __forceinline__ uint64_t row_sees64(const AttnArgs& a, const Walk& w, uint32_t i, uint32_t t0)
+__device__ __noinline__ uint64_t row_sees64(const AttnArgs& a, const TcWalk& w, uint32_t i, uint32_t t0)
 {
     const uint32_t j0 = t0 > w.s.have ? t0 - w.s.have : 0u;            // first step token at or after t0
     const uint32_t cached = t0 < w.s.have ? w.s.have - t0 : 0u;
@@ -261,13 +260,14 @@ __device__ __forceinline__ uint64_t row_sees64(const AttnArgs& a, const Walk& w,
 }
 
 template <class T, int D>
-__global__ void __launch_bounds__(TC_THREADS, 2) attn_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensorMap map)
+__global__ void __launch_bounds__(TC_THREADS, 2) attn_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensorMap map, const __grid_constant__ CUtensorMap q_map)
 {
     constexpr uint32_t CH = D / 8;                         // 16-byte chunks of a row
     constexpr uint32_t TMEM_COLS = 256;                    // 2 S, O; a power of two, half of what an SM has
     constexpr uint32_t S_COL = 0, O_COL = 2 * TC_TILE;
     extern __shared__ __align__(1024) char smem[];
     __shared__ TcShared sh;
+    __shared__ TcWalk walks[TC_THREADS / 32];
     using L = TcSmem<D>;
 
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -276,15 +276,15 @@ __global__ void __launch_bounds__(TC_THREADS, 2) attn_tc_kernel(const __grid_con
             bar_init(&sh.k_full[i], 1); bar_init(&sh.k_empty[i], 1);
             bar_init(&sh.v_full[i], 1); bar_init(&sh.v_empty[i], 1);
         }
-        for (int i = 0; i < 2; i++) { bar_init(&sh.s_full[i], 1); bar_init(&sh.p_full[i], 4); bar_init(&sh.o_done[i], 1); sh.odd[i] = 0; }
-        bar_init(&sh.q_full, 1); bar_init(&sh.q_empty, 1); bar_init(&sh.last, 1);
+        for (int i = 0; i < 2; i++) { bar_init(&sh.s_full[i], 1); bar_init(&sh.p_full[i], 4); bar_init(&sh.o_done[i], 1); bar_init(&sh.checked[i], 1); sh.odd[i] = 0; }
+        bar_init(&sh.q_full, 1); bar_init(&sh.q_empty, 1); bar_init(&sh.last, 2);
         for (int i = 0; i < TC_BITS_RING; i++) sh.bits[i] = 0u;
         sh.dead = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     uint64_t total, slice;
     // ends with a barrier for every thread, taken or not
-    const bool some = place_unit<TC_THREADS>(a, blockIdx.x, TC_ROWS, TC_TILE, blockIdx.x == 0, &sh.place, &total, &slice);
+    const bool some = place_unit<TC_THREADS>(a, blockIdx.x, TC_TILE, blockIdx.x == 0, &sh.place, &total, &slice);
     if (!some) return;
     if (warp == 6) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sh.tmem)), "r"(TMEM_COLS) : "memory");
@@ -297,48 +297,53 @@ __global__ void __launch_bounds__(TC_THREADS, 2) attn_tc_kernel(const __grid_con
     volatile int* dead = &sh.dead;
     const uint64_t units = slice < total - slice * blockIdx.x ? slice : total - slice * blockIdx.x;
     const uint32_t sm = smem_u32(smem);
-    Walk w;
-    w.start(a, sh.place.at, units);
+    TcWalk& w = walks[warp];
+    {
+        TcWalk x;
+        x.start(a, sh.place.at, units);
+        if (lane == 0) w = x;
+        __syncwarp();
+    }
 
     if (warp == 4 || warp == 5) {
         // ------------------------------------------------------------------ copies
-        // Lane l gathers tokens 4 (l % 16) .. + 3 of a tile, elements 64 (l / 16) .. + 63 of their rows.
-        const uint32_t kv = warp - 4, quad = (lane & 15u) * 4, col = D == 128 ? lane >> 4 : 0u;
-        const bool mine = D == 128 || lane < 16;
+        // Lane l brings run l % runs of a tile (or gathers 4 tokens), columns 64 (l / runs) .. + 63.
+        const uint32_t kv = warp - 4, runs = TC_TILE / (a.run > 4 ? a.run : 4), col = lane / runs, first = (lane % runs) * (TC_TILE / runs);
+        const bool mine = col < D / 64, gather = a.run < 8;
         uint64_t* full = kv ? sh.v_full : sh.k_full;
         uint64_t* empty = kv ? sh.v_empty : sh.k_empty;
-        uint32_t n = 0, piece = 0;                         // tiles and pieces so far
+        uint32_t n = 0, piece = 0, q_loads = 0;            // tiles and pieces so far
         bool ok = true;
-        while (ok && w.next(a)) {
+        while (ok && walk_next(w, a, lane)) {
             const int32_t owner = a.b.owner[w.r];
             const int32_t* table = a.b.table + (uint64_t)w.r * a.b.max_blocks;
             const int32_t x = (int32_t)((kv * a.kv_heads + w.h) * D + col * 64);
             uint32_t bits = w.masked_short(a) ? GIFT_ST_BAD_DESC : 0u;
             if (kv == 0) {
-                // Q, once the products of the piece before have read the old rows
+                // Q, once the products of the piece before have read the old rows.  What the box holds past
+                // the request's rows is another request's: rows that nobody asks for.
                 ok = piece == 0 || warp_wait(&sh.q_empty, (piece - 1) & 1u, dead);
                 if (!ok) break;
-                const uint32_t chunk = lane % CH, sub = lane / CH;
-#pragma unroll 4
-                for (uint32_t row = sub; row < (uint32_t)TC_ROWS; row += 32 / CH) {
-                    const uint32_t rho = w.qt * TC_ROWS + row;
-                    const bool there = rho < w.all_q;
-                    const uint32_t i = there ? rho / a.group : 0u, hq = w.h * a.group + (there ? rho - i * a.group : 0u);
-                    const char* src = a.q + (uint64_t)(w.row0 + i) * a.q_row + (uint64_t)hq * a.q_head + chunk * 16;
-                    cp_row16(sm + L::q + (chunk >> 3) * (TC_ROWS * 128) + row * 128 + (((chunk & 7u) ^ (row & 7u)) << 4), src, there ? 16u : 0u);
+                q_loads++;
+                if (lane == 0) {
+                    bar_expect(&sh.q_full, a.tile_rows * D * 2);
+#pragma unroll
+                    for (int c = 0; c < D / 64; c++)
+                        copy_q(sm + L::q + c * (TC_ROWS * 128), &q_map, c * 64, (int32_t)(w.h * a.group),
+                               (int32_t)(w.row0 + a.by_group.quot(w.qt * a.tile_rows)), &sh.q_full);
                 }
-                asm volatile("cp.async.commit_group;" ::: "memory");
             }
             int32_t next[4];                               // table entries, fetched a tile ahead
             auto entries = [&](uint32_t j) {
 #pragma unroll
                 for (int e = 0; e < 4; e++) {
-                    const uint32_t t = (w.tb + j) * TC_TILE + quad + e;
-                    next[e] = j < w.n_tiles && t < w.s.want ? table[t / a.b.page_tokens] : -1;
+                    const uint32_t t = (w.tb + j) * TC_TILE + first + e;
+                    next[e] = (e == 0 || gather) && mine && j < w.n_tiles && t < w.s.want ? table[a.b.page.quot(t)] : -1;
                 }
             };
             entries(0);
             int32_t label[4] = {GIFT_OWNER_PARAM, GIFT_OWNER_PARAM, GIFT_OWNER_PARAM, GIFT_OWNER_PARAM};   // judged a tile later
+#pragma unroll 1
             for (uint32_t j = 0; j < w.n_tiles; j++, n++) {
                 const uint32_t stage = n % TC_STAGES, round = n / TC_STAGES;
                 int32_t slot[4], page[4];
@@ -346,11 +351,11 @@ __global__ void __launch_bounds__(TC_THREADS, 2) attn_tc_kernel(const __grid_con
                 for (int e = 0; e < 4; e++) bits |= label_read_status(label[e], owner);
 #pragma unroll
                 for (int e = 0; e < 4; e++) {
-                    const uint32_t t = (w.tb + j) * TC_TILE + quad + e;
+                    const uint32_t t = (w.tb + j) * TC_TILE + first + e;
                     const bool fine = next[e] >= 0 && (uint32_t)next[e] < a.b.n_pages;
                     page[e] = fine ? next[e] : -1;
-                    slot[e] = fine ? (int32_t)((uint32_t)next[e] * a.b.page_tokens + t % a.b.page_tokens) : -1;
-                    if (t < w.s.want && !fine) bits |= GIFT_ST_BAD_DESC;
+                    slot[e] = fine ? (int32_t)((uint32_t)next[e] * a.b.page_tokens + (t - a.b.page.quot(t) * a.b.page_tokens)) : -1;
+                    if ((e == 0 || gather) && mine && t < w.s.want && !fine) bits |= GIFT_ST_BAD_DESC;
                 }
                 entries(j + 1);
                 if (kv == 0 && a.owner_map) {
@@ -359,7 +364,11 @@ __global__ void __launch_bounds__(TC_THREADS, 2) attn_tc_kernel(const __grid_con
                 }
                 ok = round == 0 || warp_wait(&empty[stage], (round - 1) & 1u, dead);
                 if (!ok) break;
-                if (mine) gather4(sm + (kv ? L::v : L::k) + stage * (TC_TILE * D * 2) + col * (TC_TILE * 128) + quad * 128, &map, x, slot, &full[stage]);
+                const uint32_t dst = sm + (kv ? L::v : L::k) + stage * (TC_TILE * D * 2) + col * (TC_TILE * 128) + first * 128;
+                if (mine) {
+                    if (gather) gather4(dst, &map, x, slot, &full[stage]);
+                    else copy_run(dst, &map, x, slot[0] < 0 ? -(int32_t)TC_TILE : slot[0], &full[stage]);
+                }
                 if (kv == 0 && j + 1 == w.n_tiles) {
                     // the piece's verdict, before the last tile is announced
 #pragma unroll
@@ -369,70 +378,114 @@ __global__ void __launch_bounds__(TC_THREADS, 2) attn_tc_kernel(const __grid_con
                 }
                 __syncwarp();
                 if (lane == 0) bar_expect(&full[stage], TC_TILE * D * 2);
-                if (kv == 0 && j == 0) {
-                    asm volatile("cp.async.wait_group 0;" ::: "memory");
-                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                    __syncwarp();
-                    if (lane == 0) bar_arrive(&sh.q_full);
-                }
             }
             piece++;
         }
-        asm volatile("cp.async.wait_all;" ::: "memory");
         if (*dead) {
             // nobody may be left to wait for the copies under way: they end before the CTA does
             for (uint32_t k = n > TC_STAGES ? n - TC_STAGES : 0; k < n; k++)
                 for (uint32_t i = 0; i < TC_SPINS && !bar_try(&full[k % TC_STAGES], (k / TC_STAGES) & 1u); i++) {}
+            if (kv == 0 && q_loads > 0)
+                for (uint32_t i = 0; i < TC_SPINS && !bar_try(&sh.q_full, (q_loads - 1) & 1u); i++) {}
         }
     } else if (warp == 6) {
-        // ------------------------------------------------------------------ products
-        if (lane == 0) {
-            // a negative scale: the products negate q, so that the scale used on the scores is positive
-            const uint32_t id_s = instr_desc<T>(TC_ROWS, TC_TILE, 0) | (a.negate << 13);
-            constexpr uint32_t id_o = instr_desc<T>(TC_ROWS, D, 1);
-            uint32_t n = 0, piece = 0;
-            bool ok = true;
-            auto scores = [&](uint32_t j) {                // S of the slice's j-th tile
-                const uint32_t stage = j % TC_STAGES;
-                if (!bar_wait(&sh.k_full[stage], (j / TC_STAGES) & 1u, dead)) return false;
-                tc_after();
-                const uint32_t kb = sm + L::k + stage * (TC_TILE * D * 2);
-#pragma unroll
-                for (uint32_t ks = 0; ks < D / 16; ks++) {
-                    const uint64_t da = smem_desc(sm + L::q + (ks >> 2) * (TC_ROWS * 128) + (ks & 3u) * 32, 16, 1024);
-                    const uint64_t db = smem_desc(kb + (ks >> 2) * (TC_TILE * 128) + (ks & 3u) * 32, 16, 1024);
-                    mma_ss(tmem + S_COL + (j & 1u) * TC_TILE, da, db, id_s, ks > 0);
-                }
-                mma_commit(&sh.k_empty[stage]);
-                mma_commit(&sh.s_full[j & 1u]);
-                return true;
-            };
-            while (ok && w.next(a)) {
-                ok = bar_wait(&sh.q_full, piece & 1u, dead) && (n < 2 || bar_wait(&sh.o_done[n & 1u], ((n - 2) >> 1) & 1u, dead)) && scores(n);
-                if (ok && w.n_tiles == 1) mma_commit(&sh.q_empty);
-                for (uint32_t j = 0; ok && j < w.n_tiles; j++, n++) {
-                    if (j + 1 < w.n_tiles) {
-                        // S of tile n + 1 takes the columns that held P of tile n - 1
-                        ok = (n == 0 || bar_wait(&sh.o_done[(n - 1) & 1u], ((n - 1) >> 1) & 1u, dead)) && scores(n + 1);
-                        if (ok && j + 2 == w.n_tiles) mma_commit(&sh.q_empty);
-                    }
-                    const uint32_t stage = n % TC_STAGES;
-                    ok = ok && bar_wait(&sh.v_full[stage], (n / TC_STAGES) & 1u, dead) && bar_wait(&sh.p_full[n & 1u], (n >> 1) & 1u, dead);
+        // ------------------------------------------------------------------ Q K^T
+        // a negative scale: the products negate q, so that the scale used on the scores is positive
+        const uint32_t id_s = instr_desc<T>(TC_ROWS, TC_TILE, 0) | (a.negate << 13);
+        const uint64_t q_desc = smem_desc(sm + L::q, 16, 1024), k_desc = smem_desc(sm + L::k, 16, 1024);
+        uint32_t n = 0, piece = 0;
+        bool ok = true;
+        while (ok && walk_next(w, a, lane)) {
+            const uint32_t n_tiles = w.n_tiles;
+            if (lane == 0) {
+                ok = bar_wait(&sh.q_full, piece & 1u, dead);
+#pragma unroll 1
+                for (uint32_t j = 0; ok && j < n_tiles; j++) {
+                    const uint32_t t = n + j, stage = t % TC_STAGES;
+                    // S takes the columns that held P of tile t - 2
+                    ok = bar_wait(&sh.k_full[stage], (t / TC_STAGES) & 1u, dead) &&
+                         (t < 2 || bar_wait(&sh.o_done[t & 1u], ((t - 2) >> 1) & 1u, dead));
                     if (!ok) break;
                     tc_after();
-                    if (!*(volatile int*)&sh.odd[n & 1u]) {
-                        const uint32_t vb = sm + L::v + stage * (TC_TILE * D * 2);
+                    const uint64_t kb = k_desc + stage * (TC_TILE * D * 2 / 16);
+                    const uint32_t d = tmem + S_COL + (t & 1u) * TC_TILE;
 #pragma unroll
-                        for (uint32_t ks = 0; ks < TC_TILE / 16; ks++)
-                            mma_ts(tmem + O_COL, tmem + S_COL + (n & 1u) * TC_TILE + ks * 8, smem_desc(vb + ks * 2048, TC_TILE * 128, 1024),
-                                   id_o, j > 0 || ks > 0);
-                    }
-                    mma_commit(&sh.v_empty[stage]);
-                    mma_commit(&sh.o_done[n & 1u]);
+                    for (uint32_t ks = 0; ks < D / 16; ks++)       // 16 columns are 32 bytes; 64 columns a block
+                        mma_ss(d, q_desc + (ks >> 2) * (TC_ROWS * 128 / 16) + (ks & 3u) * 2,
+                               kb + (ks >> 2) * (TC_TILE * 128 / 16) + (ks & 3u) * 2, id_s, ks > 0);
+                    mma_commit(&sh.s_full[t & 1u]);
+                    mma_commit(&sh.k_empty[stage]);
+                    if (j + 1 == n_tiles) mma_commit(&sh.q_empty);
                 }
-                piece++;
             }
+            ok = __shfl_sync(0xFFFFFFFFu, ok, 0);
+            n += n_tiles;
+            piece++;
+        }
+        if (lane == 0) {
             // nothing may be in flight when the tensor memory is given back
+            mma_commit(&sh.last);
+            for (uint32_t i = 0; i < TC_SPINS && !bar_try(&sh.last, 0); i++) {}
+        }
+        __syncwarp();
+    } else if (warp == 7) {
+        // ------------------------------------------------------------------ P V
+        // What a hidden token's V holds must not reach a row, and 0 * inf is NaN: if a step token's V in a
+        // tile is not finite, the softmax warps take the tile's product token by token, over what each
+        // row sees.  Tokens of the cache are seen by every row.  The rows of a run that lie past the
+        // context hold what the page held: they become zeros here.
+        constexpr uint32_t id_o = instr_desc<T>(TC_ROWS, D, 1);
+        const uint64_t v_desc = smem_desc(sm + L::v, TC_TILE * 128, 1024);
+        uint32_t n = 0;
+        bool ok = true;
+        while (ok && walk_next(w, a, lane)) {
+#pragma unroll 1
+            for (uint32_t j = 0; j < w.n_tiles; j++, n++) {
+                const uint32_t stage = n % TC_STAGES, t0 = (w.tb + j) * TC_TILE;
+                ok = warp_wait(&sh.v_full[stage], (n / TC_STAGES) & 1u, dead);
+                if (!ok) break;
+                bool odd = false;
+                if (t0 + TC_TILE > w.s.have) {
+                    const uint32_t lo = w.s.have > t0 ? w.s.have - t0 : 0u;
+                    const uint32_t hi = w.s.want - t0 < (uint32_t)TC_TILE ? w.s.want - t0 : (uint32_t)TC_TILE;
+                    uint4* v = reinterpret_cast<uint4*>(smem + L::v + stage * (TC_TILE * D * 2));
+#pragma unroll
+                    for (uint32_t b = 0; b < (uint32_t)D / 64; b++) {
+#pragma unroll 2
+                        for (uint32_t x = lo * 8 + lane; x < hi * 8; x += 32) {
+                            const uint4 q = v[b * (TC_TILE * 8) + x];
+                            odd |= pair_not_finite<T>(q.x) || pair_not_finite<T>(q.y) || pair_not_finite<T>(q.z) || pair_not_finite<T>(q.w);
+                        }
+                        if (a.run >= 8)
+#pragma unroll 1
+                            for (uint32_t x = hi * 8 + lane; x < TC_TILE * 8; x += 32) v[b * (TC_TILE * 8) + x] = make_uint4(0u, 0u, 0u, 0u);
+                    }
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    odd = __any_sync(0xFFFFFFFFu, odd);
+                    if (lane == 0) {
+                        *(volatile int*)&sh.odd[stage] = odd ? 1 : 0;
+                        bar_arrive(&sh.checked[stage]);
+                    }
+                    __syncwarp();
+                }
+                ok = warp_wait(&sh.p_full[n & 1u], (n >> 1) & 1u, dead);
+                if (!ok) break;
+                if (lane == 0) {
+                    tc_after();
+                    if (!odd) {
+                        const uint64_t vb = v_desc + stage * (TC_TILE * D * 2 / 16);
+                        const uint32_t p = tmem + S_COL + (n & 1u) * TC_TILE;
+#pragma unroll
+                        for (uint32_t ks = 0; ks < TC_TILE / 16; ks++)      // 16 tokens are 8 columns of P, 2048 bytes of V
+                            mma_ts(tmem + O_COL, p + ks * 8, vb + ks * (2048 / 16), id_o, j > 0 || ks > 0);
+                    }
+                    mma_commit(&sh.o_done[n & 1u]);
+                    mma_commit(&sh.v_empty[stage]);
+                }
+                __syncwarp();
+            }
+        }
+        if (lane == 0) {
             mma_commit(&sh.last);
             for (uint32_t i = 0; i < TC_SPINS && !bar_try(&sh.last, 0); i++) {}
         }
@@ -441,38 +494,30 @@ __global__ void __launch_bounds__(TC_THREADS, 2) attn_tc_kernel(const __grid_con
         // ------------------------------------------------------------------ softmax
         const uint32_t row = threadIdx.x, lane_base = (warp * 32u) << 16;
         uint32_t n = 0, piece = 0;
+        uint32_t checks0 = 0, checks1 = 0;                 // tiles with step tokens so far, per stage
+        char* stage_o = smem + L::o + warp * (32 * 64);
         bool alive = true;
-        while (w.next(a)) {
-            const uint32_t rho = w.qt * TC_ROWS + row;
-            const bool there = rho < w.all_q;
-            const bool warp_there = w.qt * TC_ROWS + warp * 32 < w.all_q;
-            const uint32_t i = there ? rho / a.group : 0u, hq = w.h * a.group + (there ? rho - i * a.group : 0u);
+        while (walk_next(w, a, lane)) {
+            const uint32_t rho = w.qt * a.tile_rows + row;
+            const bool there = rho < w.all_q && row < a.tile_rows;
+            const bool warp_there = w.qt * a.tile_rows + warp * 32 < w.all_q && warp * 32 < a.tile_rows;
+            const uint32_t i = there ? a.by_group.quot(rho) : 0u, hq = w.h * a.group + (there ? rho - i * a.group : 0u);
             const bool masked_short = w.masked_short(a);
             float m = NEG_INF, l = 0.f;                    // the maximum in use, the sum relative to it
+#pragma unroll 1
             for (uint32_t j = 0; alive && j < w.n_tiles; j++, n++) {
                 const uint32_t s_at = tmem + lane_base + S_COL + (n & 1u) * TC_TILE;
                 const uint32_t t0 = (w.tb + j) * TC_TILE;
                 const bool mixed = t0 + TC_TILE > w.s.have;
+                uint64_t sees = ~0ull;
+                if (mixed) sees = there && !masked_short ? row_sees64(a, w, i, t0) : 0ull;
                 if (!warp_wait(&sh.s_full[n & 1u], (n >> 1) & 1u, dead)) { alive = false; break; }
-                // every tile's P V is waited for in turn, two tiles on, when it has long been done: a barrier
-                // that was not looked at for two phases cannot be told from one that is a phase behind
-                if (n >= 2 && !warp_wait(&sh.o_done[n & 1u], ((n - 2) >> 1) & 1u, dead)) { alive = false; break; }
                 bool odd = false;
                 if (mixed) {
-                    // 0 * inf is NaN: if a v of a tile whose tokens some rows may not see is not finite, the
-                    // tile's product is taken token by token, over what each row sees
-                    const uint32_t stage = n % TC_STAGES;
-                    if (!warp_wait(&sh.v_full[stage], (n / TC_STAGES) & 1u, dead)) { alive = false; break; }
-                    const uint4* v = reinterpret_cast<const uint4*>(smem + L::v + stage * (TC_TILE * D * 2));
-#pragma unroll 8
-                    for (uint32_t x = lane; x < TC_TILE * CH; x += 32) {
-                        const uint4 q = v[x];
-                        odd |= pair_not_finite<T>(q.x) || pair_not_finite<T>(q.y) || pair_not_finite<T>(q.z) || pair_not_finite<T>(q.w);
-                    }
-                    odd = __any_sync(0xFFFFFFFFu, odd);    // every warp has seen the whole tile: one answer for all
+                    const uint32_t round = n & 1u ? checks1++ : checks0++;
+                    if (!warp_wait(&sh.checked[n & 1u], round & 1u, dead)) { alive = false; break; }
+                    odd = *(volatile int*)&sh.odd[n & 1u] != 0;
                 }
-                // after s_full: the product of tile n - 2, which used this flag, has been issued
-                if (row == 0) *(volatile int*)&sh.odd[n & 1u] = odd ? 1 : 0;
                 if (!warp_there) {                         // rows that do not exist: whatever P holds stays in them
                     __syncwarp();
                     if (lane == 0) bar_arrive(&sh.p_full[n & 1u]);
@@ -485,9 +530,7 @@ __global__ void __launch_bounds__(TC_THREADS, 2) attn_tc_kernel(const __grid_con
                 tc_wait_ld();
                 tc_pin32(sc[0]);
                 tc_pin32(sc[1]);
-                uint64_t sees = ~0ull;
                 if (mixed) {
-                    sees = there && !masked_short ? row_sees64(a, w, i, t0) : 0ull;
 #pragma unroll
                     for (int x = 0; x < 2; x++)
 #pragma unroll
@@ -510,27 +553,27 @@ __global__ void __launch_bounds__(TC_THREADS, 2) attn_tc_kernel(const __grid_con
                 const float minus = m == NEG_INF ? 0.f : -m;
                 float sums[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int x = 0; x < 2; x++)
+                for (int x = 0; x < 2; x++) {
 #pragma unroll
                     for (int c = 0; c < 32; c++) {
                         const float p = fast_exp2(fmaf(__uint_as_float(sc[x][c]), a.scale_log2, minus));
                         sc[x][c] = __float_as_uint(p);
                         sums[c & 3] += p;
                     }
-                l = l * alpha + ((sums[0] + sums[1]) + (sums[2] + sums[3]));
-                if (!odd) {
-                    // P into the first 32 columns of its S
-                    uint32_t pk[32];
+                    if (!odd) {
+                        // P into the first 32 columns of its S
+                        uint32_t pk[16];
 #pragma unroll
-                    for (int x = 0; x < 2; x++)
-#pragma unroll
-                        for (int c = 0; c < 16; c++)
-                            pk[x * 16 + c] = pack2<T>(__uint_as_float(sc[x][2 * c]), __uint_as_float(sc[x][2 * c + 1]));
-                    tc_st32(s_at, pk);
+                        for (int c = 0; c < 16; c++) pk[c] = pack2<T>(__uint_as_float(sc[x][2 * c]), __uint_as_float(sc[x][2 * c + 1]));
+                        tc_st16(s_at + x * 16, pk);
+                    }
                 }
+                l = l * alpha + ((sums[0] + sums[1]) + (sums[2] + sums[3]));
                 const bool rescale = j > 0 && __any_sync(0xFFFFFFFFu, grow && there);
                 if ((rescale || odd) && n > 0) {
-                    // every product so far is in O (the one of tile n is not issued before p_full)
+                    // Every product so far is in O (the one of tile n is not issued before p_full).  That
+                    // the barrier is no more than one phase behind follows from S of tile n - 1, whose
+                    // product waited for tile n - 3's P V.
                     if (!warp_wait(&sh.o_done[(n - 1) & 1u], ((n - 1) >> 1) & 1u, dead)) { alive = false; break; }
                     tc_after();
                 }
@@ -564,6 +607,7 @@ __global__ void __launch_bounds__(TC_THREADS, 2) attn_tc_kernel(const __grid_con
                         tc_st8(tmem + lane_base + O_COL + ch * 8, o);
                     }
                 } else if (rescale) {
+#pragma unroll 1
                     for (uint32_t c0 = 0; c0 < (uint32_t)D; c0 += 32) {
                         uint32_t o[32];
                         tc_ld32(o, tmem + lane_base + O_COL + c0);
@@ -580,7 +624,6 @@ __global__ void __launch_bounds__(TC_THREADS, 2) attn_tc_kernel(const __grid_con
                 if (lane == 0) bar_arrive(&sh.p_full[n & 1u]);
             }
             // ---------------------------------------------------------- the piece's end
-            if (alive && n >= 2) alive = warp_wait(&sh.o_done[n & 1u], ((n - 2) >> 1) & 1u, dead);
             if (alive) alive = warp_wait(&sh.o_done[(n - 1) & 1u], ((n - 1) >> 1) & 1u, dead);
             tc_after();
             uint32_t bits = alive ? *(volatile uint32_t*)&sh.bits[piece % TC_BITS_RING] : GIFT_ST_STALLED;
@@ -589,30 +632,41 @@ __global__ void __launch_bounds__(TC_THREADS, 2) attn_tc_kernel(const __grid_con
             const bool none = bits != 0u || l == 0.f;
             const float inv = none ? 0.f : 1.f / l;
             if (warp_there) {
+                // Rows leave by way of shared memory, 64 bytes of 32 rows at a time, so that four lanes write
+                // a row's 64 bytes (a lane writing its own row: 5 000 clocks, most of an item's end).
+                char* mine = whole ? a.out + (uint64_t)(w.row0 + i) * a.out_row + (uint64_t)hq * a.out_head
+                                   : reinterpret_cast<char*>(a.part_o + ((uint64_t)slot * TC_ROWS + row) * D);
+                const uint32_t last = w.all_q - w.qt * a.tile_rows < a.tile_rows ? w.all_q - w.qt * a.tile_rows : a.tile_rows;
+                const uint32_t rows = last - warp * 32;                         // rows of this warp that exist, if below 32
+#pragma unroll 1
                 for (uint32_t c0 = 0; c0 < (uint32_t)D; c0 += 32) {
                     uint32_t o[32];
                     tc_ld32(o, tmem + lane_base + O_COL + c0);
                     tc_wait_ld();
                     tc_pin32(o);
-                    if (there && whole) {
-                        uint4* to = reinterpret_cast<uint4*>(a.out + (uint64_t)(w.row0 + i) * a.out_row + (uint64_t)hq * a.out_head + c0 * 2);
+                    if (whole) {
 #pragma unroll
-                        for (int x = 0; x < 4; x++) {
-                            uint4 v = make_uint4(0u, 0u, 0u, 0u);
-                            if (!none) {
-                                v.x = pack2<T>(__uint_as_float(o[8 * x]) * inv, __uint_as_float(o[8 * x + 1]) * inv);
-                                v.y = pack2<T>(__uint_as_float(o[8 * x + 2]) * inv, __uint_as_float(o[8 * x + 3]) * inv);
-                                v.z = pack2<T>(__uint_as_float(o[8 * x + 4]) * inv, __uint_as_float(o[8 * x + 5]) * inv);
-                                v.w = pack2<T>(__uint_as_float(o[8 * x + 6]) * inv, __uint_as_float(o[8 * x + 7]) * inv);
-                            }
-                            to[x] = v;
-                        }
-                    } else if (there) {
-                        uint4* to = reinterpret_cast<uint4*>(a.part_o + ((uint64_t)slot * TC_ROWS + row) * D + c0);
-#pragma unroll
-                        for (int x = 0; x < 8; x++) to[x] = make_uint4(o[4 * x], o[4 * x + 1], o[4 * x + 2], o[4 * x + 3]);
+                        for (int x = 0; x < 16; x++)
+                            o[x] = none ? 0u : pack2<T>(__uint_as_float(o[2 * x]) * inv, __uint_as_float(o[2 * x + 1]) * inv);
                     }
-                    __syncwarp();
+                    const uint32_t parts = whole ? 1 : 2;                       // 32 columns are 64 or 128 bytes
+#pragma unroll
+                    for (uint32_t part = 0; part < 2; part++) {
+                        if (part >= parts) break;
+#pragma unroll
+                        for (uint32_t x = 0; x < 4; x++)
+                            *reinterpret_cast<uint4*>(stage_o + lane * 64 + ((x ^ ((lane >> 1) & 3u)) << 4)) =
+                                make_uint4(o[part * 16 + 4 * x], o[part * 16 + 4 * x + 1], o[part * 16 + 4 * x + 2], o[part * 16 + 4 * x + 3]);
+                        __syncwarp();
+#pragma unroll
+                        for (uint32_t y = 0; y < 4; y++) {
+                            const uint32_t other = y * 8 + (lane >> 2), x = lane & 3u;
+                            char* to = reinterpret_cast<char*>(__shfl_sync(0xFFFFFFFFu, (unsigned long long)mine, other));
+                            const uint4 v = *reinterpret_cast<const uint4*>(stage_o + other * 64 + ((x ^ ((other >> 1) & 3u)) << 4));
+                            if (other < rows) *reinterpret_cast<uint4*>(to + (whole ? c0 * 2 : c0 * 4 + part * 64) + x * 16) = v;
+                        }
+                        __syncwarp();
+                    }
                 }
                 if (there) {
                     if (!whole) a.part_ml[(uint64_t)slot * TC_ROWS + row] = make_float2(m, l);

@@ -11,6 +11,27 @@ namespace gift {
 
 constexpr int32_t BATCH_MAX_OWNER = 1 << 20;    // user ids of a ctx are below this
 
+// Division by a number that is fixed for a call, for dividends below 2^31: with l = ceil(log2 d)
+// and m = ceil(2^(31+l) / d), which is below 2^32, t / d = t m >> (31 + l), since the excess t (m d -
+// 2^(31+l)) < 2^31 2^l.  (The compiler's own division of unknown numbers is some 20 instructions,
+// and the kernels divide several times per token.)
+struct FixedDiv {
+    uint32_t d, mul, shift;
+    GIFT_HD uint32_t quot(uint32_t t) const { return (uint32_t)((uint64_t)t * mul >> shift); }
+    // how many d cover t
+    GIFT_HD uint32_t cover(uint32_t t) const { return t ? quot(t - 1u) + 1u : 0u; }
+};
+inline FixedDiv fixed_div(uint32_t d)
+{
+    uint32_t l = 0;
+    while (l < 31 && (1u << l) < d) l++;
+    FixedDiv f;
+    f.d = d;
+    f.shift = 31 + l;
+    f.mul = d ? (uint32_t)((((uint64_t)1 << f.shift) + d - 1) / d) : 0u;
+    return f;
+}
+
 // What a request's lengths say.  A malformed request takes no part in any call: no rows, no blocks.
 struct ReqShape {
     bool ok;
@@ -19,15 +40,14 @@ struct ReqShape {
     uint32_t rows;           // tokens the step adds
 };
 
-GIFT_HD ReqShape req_shape(int32_t owner, int32_t have, int32_t want, uint32_t page_tokens, uint32_t max_blocks)
+GIFT_HD ReqShape req_shape(int32_t owner, int32_t have, int32_t want, const FixedDiv& page, uint32_t max_blocks)
 {
     ReqShape s;
     s.ok = owner >= 0 && owner < BATCH_MAX_OWNER && have >= 0 && want >= 0;
     s.have = s.ok ? (uint32_t)have : 0u;
     s.want = s.ok ? (uint32_t)want : 0u;
-    // 2^31 - 1 + 65535 fits 32 bits unsigned
-    s.bh = (s.have + page_tokens - 1u) / page_tokens;
-    s.bw = (s.want + page_tokens - 1u) / page_tokens;
+    s.bh = page.cover(s.have);
+    s.bw = page.cover(s.want);
     if (s.bh > max_blocks || s.bw > max_blocks) {
         s.ok = false;
         s.have = s.want = s.bh = s.bw = 0u;
@@ -106,6 +126,7 @@ inline int batch_args_ok(const gift_batch* b)
 
 struct BatchArgs {
     uint32_t n_req, max_blocks, page_tokens, n_pages;
+    FixedDiv page;                   // by page_tokens
     const int32_t* __restrict__ owner;
     const int32_t* __restrict__ have;
     const int32_t* __restrict__ want;
@@ -116,13 +137,14 @@ inline BatchArgs batch_args(const gift_batch* b)
 {
     BatchArgs a;
     a.n_req = b->n_req; a.max_blocks = b->max_blocks; a.page_tokens = b->page_tokens; a.n_pages = b->n_pages;
+    a.page = fixed_div(b->page_tokens);
     a.owner = b->owner; a.have = b->have; a.want = b->want; a.table = b->table;
     return a;
 }
 
 __device__ __forceinline__ ReqShape load_shape(const BatchArgs& b, uint32_t r)
 {
-    return req_shape(b.owner[r], b.have[r], b.want[r], b.page_tokens, b.max_blocks);
+    return req_shape(b.owner[r], b.have[r], b.want[r], b.page, b.max_blocks);
 }
 
 // Inclusive sum of v over the threads of the block, in thread order; *total is the block's sum.

@@ -224,7 +224,7 @@ __global__ void __launch_bounds__(MAP_THREADS) slot_map_kernel(const __grid_cons
             req = (int32_t)r;
             owner = a.b.owner[r];
             if (i >= 0 && (uint32_t)i < s.rows) {
-                const uint32_t p = s.have + (uint32_t)i, blk = p / a.b.page_tokens;
+                const uint32_t p = s.have + (uint32_t)i, blk = a.b.page.quot(p);
                 pos = (int32_t)p;
                 const int32_t page = a.b.table[(uint64_t)r * a.b.max_blocks + blk];
                 if (page >= 0 && (uint32_t)page < a.b.n_pages)
@@ -251,7 +251,7 @@ struct SegTabArgs {
 __device__ __forceinline__ uint32_t first_block(const SegTabArgs& a, const ReqShape& s)
 {
     if (!(a.flags & GIFT_KV_NEW_BLOCKS)) return 0u;
-    const uint32_t b0 = s.have / a.b.page_tokens;      // a block that was part full is exported again
+    const uint32_t b0 = a.b.page.quot(s.have);      // a block that was part full is exported again
     return b0 < s.bw ? b0 : s.bw;
 }
 

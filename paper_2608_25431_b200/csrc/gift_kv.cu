@@ -24,7 +24,8 @@ struct AppendArgs {
     const int32_t* row_owner;
     const int32_t* owner_map;
     uint32_t* status;
-    uint32_t n_rows, n_slots, page_tokens;
+    uint32_t n_rows, n_slots;
+    FixedDiv page, head;                     // by page_tokens, by head_chunks
     uint32_t head_chunks;                    // 16-byte chunks of one head
     uint32_t half_chunks;                    // chunks of K (or of V) of one token
     uint32_t lanes;                          // threads that share a row
@@ -35,7 +36,7 @@ __device__ __forceinline__ uint32_t row_status(const AppendArgs& a, int64_t slot
 {
     if (slot < 0 || slot >= (int64_t)a.n_slots) return GIFT_ST_BAD_DESC;
     if (!a.owner_map) return 0u;
-    return label_write_status(a.owner_map[(uint32_t)slot / a.page_tokens], a.row_owner[t]);
+    return label_write_status(a.owner_map[a.page.quot((uint32_t)slot)], a.row_owner[t]);
 }
 
 __global__ void __launch_bounds__(APPEND_THREADS) kv_append_kernel(const __grid_constant__ AppendArgs a)
@@ -54,7 +55,7 @@ __global__ void __launch_bounds__(APPEND_THREADS) kv_append_kernel(const __grid_
         // a token is K then V, each heads x head_dim: 2 * half_chunks contiguous chunks
         uint4* dst = a.pages + (uint64_t)slot * (2u * a.half_chunks);
         for (uint32_t c = lane; c < a.half_chunks; c += a.lanes) {
-            const uint32_t h = c / a.head_chunks, o = c - h * a.head_chunks;
+            const uint32_t h = a.head.quot(c), o = c - h * a.head_chunks;
             const uint4 kk = __ldcs(a.k + (uint64_t)t * a.k_row + (uint64_t)h * a.k_head + o);
             const uint4 vv = __ldcs(a.v + (uint64_t)t * a.v_row + (uint64_t)h * a.v_head + o);
             dst[c] = kk;
@@ -84,8 +85,9 @@ extern "C" int gift_kv_append(gift_ctx* c, const gift_kv_pool* pool, const void*
     a.k_row = k_row_stride / 8; a.k_head = k_head_stride / 8; a.v_row = v_row_stride / 8; a.v_head = v_head_stride / 8;
     a.pages = static_cast<uint4*>(pool->pages);
     a.slots = slots; a.row_owner = row_owner; a.owner_map = pool->owner_map; a.status = status;
-    a.n_rows = n_rows; a.n_slots = pool->n_pages * pool->page_tokens; a.page_tokens = pool->page_tokens;
+    a.n_rows = n_rows; a.n_slots = pool->n_pages * pool->page_tokens; a.page = fixed_div(pool->page_tokens);
     a.head_chunks = pool->head_dim / 8;
+    a.head = fixed_div(a.head_chunks);
     a.half_chunks = pool->n_heads * a.head_chunks;
     a.lanes = a.half_chunks < (uint32_t)APPEND_THREADS ? a.half_chunks : (uint32_t)APPEND_THREADS;
     a.rows_per_cta = APPEND_THREADS / a.lanes;

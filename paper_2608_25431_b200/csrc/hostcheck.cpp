@@ -119,10 +119,11 @@ void hc_slice_piece(uint64_t g0, uint64_t g1, uint64_t p0, uint64_t p1, uint64_t
 // The length arithmetic of the paged-cache calls.
 void hc_req_shape(int32_t owner, int32_t have, int32_t want, uint32_t pt, uint32_t width, uint32_t* out)
 {
-    const ReqShape r = req_shape(owner, have, want, pt, width);
+    const ReqShape r = req_shape(owner, have, want, fixed_div(pt), width);
     out[0] = r.ok ? 1u : 0u; out[1] = r.have; out[2] = r.want; out[3] = r.bh; out[4] = r.bw; out[5] = r.rows;
 }
 
+uint32_t hc_quot(uint32_t d, uint32_t t) { return fixed_div(d).quot(t); }
 uint32_t hc_req_of(const uint32_t* first, uint32_t n, uint32_t k) { return req_of(first, n, k); }
 int32_t hc_label_flip(int32_t l) { return label_flip(l); }
 int hc_label_claimed(int32_t l) { return label_claimed(l) ? 1 : 0; }

@@ -129,6 +129,16 @@ def test_request_shapes_of_the_kernels_match_the_oracle(hc):
         assert list(out) == [int(ok), h, w, bh, bw, max(0, w - h)]
 
 
+def test_fixed_division_of_the_kernels(hc):
+    rng = np.random.default_rng(7)
+    hc.hc_quot.restype = C.c_uint32
+    for d in [1, 2, 3, 5, 7, 16, 24, 125, 1023, 1024, 65535, 65536, 2 ** 30 + 1] + rng.integers(1, 65537, size=60).tolist():
+        edge = [0, 1, d - 1, d, d + 1, 2 ** 31 - 1, 2 ** 31 - 2, (2 ** 31 - 1) // d * d, (2 ** 31 - 1) // d * d - 1]
+        for t in edge + rng.integers(0, 2 ** 31, size=200).tolist():
+            if 0 <= t < 2 ** 31:
+                assert hc.hc_quot(d, t) == t // d, (d, t)
+
+
 def test_prefix_search_of_the_kernels(hc):
     rng = np.random.default_rng(6)
     for _ in range(200):

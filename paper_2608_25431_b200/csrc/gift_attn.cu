@@ -29,7 +29,7 @@ namespace {
 constexpr int FEW_WARPS = 4;
 constexpr int FEW_THREADS = FEW_WARPS * 32;
 constexpr int FEW_TILE = FEW_WARPS * 16;
-constexpr int FEW_STAGES = 3;
+constexpr int FEW_ROWS = 16;
 
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, uint32_t bytes)
 {
@@ -69,16 +69,17 @@ template <int D> __device__ __forceinline__ uint32_t tile_at(uint32_t base, uint
     return base + row * (D * 2) + ((chunk ^ (row & 7u)) << 4);
 }
 
-template <int D, int MT> struct FewSmem {
-    static constexpr int ring = FEW_WARPS * FEW_STAGES * 16 * D * 2 * 2;
-    static constexpr int join = FEW_WARPS * MT * 16 * D * 4;
+template <int D> struct FewSmem {
+    static constexpr int stages = 384 / D;                          // 96 KiB
+    static constexpr int ring = FEW_WARPS * stages * 16 * D * 2 * 2;
+    static constexpr int join = FEW_WARPS * FEW_ROWS * D * 4;
     static constexpr int bytes = ring > join ? ring : join;
 };
 
-template <class T, int D, int MT>
+template <class T, int D>
 __global__ void __launch_bounds__(FEW_THREADS, 2) attn_few_kernel(const __grid_constant__ AttnArgs a)
 {
-    constexpr int ROWS = 16 * MT;
+    constexpr int ROWS = FEW_ROWS, MT = 1, FEW_STAGES = FewSmem<D>::stages;
     constexpr int CH = D / 8;                      // 16-byte chunks of a K or V row
     constexpr int KS = D / 16;                     // k steps of the score product
     constexpr uint32_t HALF = 16 * D * 2;          // bytes of 16 K (or V) rows
@@ -93,7 +94,7 @@ __global__ void __launch_bounds__(FEW_THREADS, 2) attn_few_kernel(const __grid_c
     const uint32_t ring = (uint32_t)__cvta_generic_to_shared(smem) + warp * (FEW_STAGES * 2 * HALF);
 
     Walk<FEW_TILE> w;
-    w.start(a, place.at, slice < total - slice * blockIdx.x ? slice : total - slice * blockIdx.x);
+    w.start(a, place.at, 0, slice < total - slice * blockIdx.x ? slice : total - slice * blockIdx.x);
     while (w.next(a)) {
         const ReqShape& s = w.s;
         const ItemShape& it = w.it;
@@ -382,8 +383,8 @@ __global__ void __launch_bounds__(FEW_THREADS, 2) attn_few_kernel(const __grid_c
     }
 }
 
-// Joins the pieces of the items that a slice boundary cuts, 16 rows per CTA.  CTAs (w, *) look after
-// the item that boundary w + 1 cuts, if no earlier boundary cuts it too.
+// Joins the pieces of the items that a slice boundary cuts, 16 rows per CTA.  CTAs (w, *, way) look
+// after the item that boundary w + 1 cuts, if no earlier boundary cuts it too.
 constexpr int JOIN_THREADS = 128;
 constexpr int JOIN_ROWS = 16;
 
@@ -394,13 +395,14 @@ __global__ void __launch_bounds__(JOIN_THREADS) attn_join_kernel(const __grid_co
     __shared__ PlaceShared place;
     __shared__ float2 s_top[JOIN_ROWS];
     __shared__ uint32_t s_bits;
-    const uint32_t w = blockIdx.x + 1, row_lo = blockIdx.y * JOIN_ROWS;
+    const uint32_t w = blockIdx.x + 1, row_lo = blockIdx.y * JOIN_ROWS, way = blockIdx.z;
     uint64_t total, slice;
     if (!place_unit<JOIN_THREADS>(a, w, TILE, false, &place, &total, &slice)) return;
     const uint32_t r = place.at.r, row0 = place.at.row0;
     const ReqShape s = load_shape(a.b, r);
     const ItemShape it = item_shape(a, s, TILE);
-    const uint32_t item = place.at.item, u = place.at.u;
+    const uint32_t item = place.at.k * a.ways + way, u = place.at.u;
+    if (item >= it.items) return;
     // not cut here (the boundary lies before the item's first tile or behind it), or cut by an earlier boundary as well
     if (u <= a.extra || (uint64_t)u > slice + a.extra) return;
     const uint64_t end = slice * w - u + it.cost;      // one past the item's last unit
@@ -410,8 +412,8 @@ __global__ void __launch_bounds__(JOIN_THREADS) attn_join_kernel(const __grid_co
     const uint32_t in_tile = all_q - qt * a.tile_rows < a.tile_rows ? all_q - qt * a.tile_rows : a.tile_rows;
     if (row_lo >= in_tile) return;
     const uint32_t nr = in_tile - row_lo < (uint32_t)JOIN_ROWS ? in_tile - row_lo : (uint32_t)JOIN_ROWS;
-    // the item starts in CTA w - 1 (its last piece) and goes on as the first piece of w, w + 1, ...
-    auto slot_of = [&](uint32_t p) -> uint64_t { return p == 0 ? 2ull * (w - 1) + 1 : 2ull * (w + p - 1); };
+    // the item starts in slice w - 1 (its last piece) and goes on as the first piece of w, w + 1, ...
+    auto slot_of = [&](uint32_t p) -> uint64_t { return 2ull * ((w + p - 1) * a.ways + way) + (p == 0 ? 1 : 0); };
     if (threadIdx.x == 0) s_bits = 0u;
     __syncthreads();
     for (uint32_t p = threadIdx.x; p < pieces; p += JOIN_THREADS)
@@ -467,19 +469,20 @@ __global__ void __launch_bounds__(JOIN_THREADS) attn_join_kernel(const __grid_co
     if (h == 0 && q0 == 0) write_request<JOIN_THREADS>(a, r, row0, it.rows_m, bits);
 }
 
-template <class T, int D, int MT>
+template <class T, int D>
 int launch_few(gift_ctx* c, AttnArgs& a, cudaStream_t st)
 {
-    constexpr int smem = FewSmem<D, MT>::bytes;
-    CU_TRY(cudaFuncSetAttribute(attn_few_kernel<T, D, MT>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-    a.n_cta = 2u * c->num_sms;
-    a.tile_rows = 16 * MT;
+    constexpr int smem = FewSmem<D>::bytes;
+    CU_TRY(cudaFuncSetAttribute(attn_few_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+    a.n_slices = 2u * c->num_sms;
+    a.ways = 1;
+    a.tile_rows = FEW_ROWS;
     a.by_tile_rows = fixed_div(a.tile_rows);
     a.least = 1;
     a.extra = 1;
-    attn_few_kernel<T, D, MT><<<a.n_cta, FEW_THREADS, smem, st>>>(a);
+    attn_few_kernel<T, D><<<a.n_slices, FEW_THREADS, smem, st>>>(a);
     c->launches++;
-    attn_join_kernel<T, D, 16 * MT, FEW_TILE><<<dim3(a.n_cta - 1, MT), JOIN_THREADS, 0, st>>>(a);
+    attn_join_kernel<T, D, FEW_ROWS, FEW_TILE><<<a.n_slices - 1, JOIN_THREADS, 0, st>>>(a);
     c->launches++;
     CU_TRY(cudaGetLastError());
     return GIFT_OK;
@@ -537,7 +540,7 @@ int map_of_q(const AttnArgs& a, bool half, uint32_t head_dim, CUtensorMap* map)
 }
 
 template <class T, int D>
-int launch_many(gift_ctx* c, AttnArgs& a, cudaStream_t st)
+int launch_many(gift_ctx* c, AttnArgs& a, uint64_t rows, cudaStream_t st)
 {
     a.run = a.b.page_tokens & (0u - a.b.page_tokens);
     if (a.run > (uint32_t)TC_TILE) a.run = TC_TILE;
@@ -547,7 +550,9 @@ int launch_many(gift_ctx* c, AttnArgs& a, cudaStream_t st)
     if (rc != GIFT_OK) return rc;
     constexpr int smem = TcSmem<D>::bytes;
     CU_TRY(cudaFuncSetAttribute(attn_tc_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-    a.n_cta = 2u * c->num_sms;
+    // two CTAs to a slice when an average request's rows fill more than one tile
+    a.ways = rows > (uint64_t)TC_ROWS ? 2u : 1u;
+    a.n_slices = 2u * c->num_sms / a.ways;
     a.tile_rows = TC_ROWS / a.group * a.group;             // whole tokens
     a.by_tile_rows = fixed_div(a.tile_rows);
     a.least = 4;
@@ -556,9 +561,9 @@ int launch_many(gift_ctx* c, AttnArgs& a, cudaStream_t st)
     // makes every finite score 0 in effect, and keeps a hidden token's minus infinity what it is)
     a.negate = a.scale_log2 < 0.f ? 1u : 0u;
     a.scale_log2 = fmaxf(fabsf(a.scale_log2), 1e-30f);
-    attn_tc_kernel<T, D><<<a.n_cta, TC_THREADS, smem, st>>>(a, map, q_map);
+    attn_tc_kernel<T, D><<<a.n_slices * a.ways, TC_THREADS, smem, st>>>(a, map, q_map);
     c->launches++;
-    attn_join_kernel<T, D, TC_ROWS, TC_TILE><<<dim3(a.n_cta - 1, TC_ROWS / JOIN_ROWS), JOIN_THREADS, 0, st>>>(a);
+    attn_join_kernel<T, D, TC_ROWS, TC_TILE><<<dim3(a.n_slices - 1, TC_ROWS / JOIN_ROWS, a.ways), JOIN_THREADS, 0, st>>>(a);
     c->launches++;
     CU_TRY(cudaGetLastError());
     return GIFT_OK;
@@ -572,7 +577,7 @@ int launch_attn(gift_ctx* c, AttnArgs& a, cudaStream_t st)
     const bool plain_q = a.group <= (uint32_t)TC_ROWS && (a.n_rows == 1 || a.q_row > 0) && (a.heads == 1 || a.q_head > 0);
     // rows of an average request's K/V head
     const uint64_t rows = ((uint64_t)a.n_rows + a.b.n_req - 1) / a.b.n_req * a.group;
-    return rows <= 16 ? launch_few<T, D, 1>(c, a, st) : rows <= 32 || !plain_q ? launch_few<T, D, 2>(c, a, st) : launch_many<T, D>(c, a, st);
+    return rows <= (uint64_t)FEW_ROWS || !plain_q ? launch_few<T, D>(c, a, st) : launch_many<T, D>(c, a, rows, st);
 }
 
 constexpr uint32_t PART_ROWS = TC_ROWS;  // most rows of a tile of query rows

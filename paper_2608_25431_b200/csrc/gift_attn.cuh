@@ -11,6 +11,11 @@
 // item that a slice boundary cuts leaves its pieces' maxima, sums and unnormalised rows in
 // scratch, and a second kernel joins them.  A slice has at most two such pieces (it enters one
 // item in the middle and leaves one in the middle), so the scratch does not depend on the call.
+//
+// Where the rows of a K/V head fill several tiles, two CTAs walk one slice together (`ways` 2): its
+// units are then those of pairs of a request's items (2 k, 2 k + 1), and each CTA takes its own of
+// every pair.  Neighbouring items are tiles of query rows of one K/V head, so the second reader
+// of every token finds it in L2.
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -44,10 +49,10 @@ struct AttnArgs {
     uint32_t tile_rows;              // query rows of an item, at most
     uint32_t least;                  // smallest slice, in tiles
     uint32_t extra;                  // tiles that an item costs beyond its own
-    uint32_t n_cta;                  // CTAs of the attention kernel
-    float* part_o;                   // [2 n_cta][rows][D]
-    float2* part_ml;                 // [2 n_cta][rows] running maximum, sum
-    uint32_t* part_bits;             // [2 n_cta] status bits of the piece's pages
+    uint32_t n_slices, ways;         // slices, and CTAs that share one
+    float* part_o;                   // [2 CTAs][rows][D]
+    float2* part_ml;                 // [2 CTAs][rows] running maximum, sum
+    uint32_t* part_bits;             // [2 CTAs] status bits of the piece's pages
 };
 
 constexpr float NEG_INF = -__builtin_huge_valf();
@@ -57,7 +62,8 @@ struct ItemShape {
     uint32_t rows_m;                 // step tokens
     uint32_t nqt;                    // tiles of query rows
     uint32_t tiles;                  // token tiles of the context
-    uint32_t cost;                   // units of one item: extra, then its tiles
+    uint32_t items;                  // nqt for every K/V head
+    uint32_t cost;                   // units of one item (or pair of items): extra, then its tiles
     uint64_t units;                  // units of all its items
 };
 
@@ -69,7 +75,8 @@ __device__ __forceinline__ ItemShape item_shape(const AttnArgs& a, const ReqShap
     i.nqt = a.by_tile_rows.cover(s.rows * a.group & 0x7FFFFFFFu);
     i.tiles = (s.want + tile_tokens - 1) / tile_tokens;      // >= 1 when rows > 0
     i.cost = i.tiles + a.extra;
-    i.units = (uint64_t)i.nqt * i.cost * a.kv_heads;
+    i.items = i.nqt * a.kv_heads;
+    i.units = (uint64_t)((i.items + a.ways - 1) / a.ways) * i.cost;
     return i;
 }
 
@@ -77,7 +84,7 @@ __device__ __forceinline__ ItemShape item_shape(const AttnArgs& a, const ReqShap
 struct Place {
     uint32_t r;                      // request
     uint32_t row0;                   // its first row
-    uint32_t item, u;                // the request's item, the unit's index within it
+    uint32_t k, u;                   // the request's item (or pair), the unit's index within it
 };
 
 struct PlaceShared {
@@ -110,7 +117,7 @@ __device__ bool place_unit(const AttnArgs& a, uint32_t w, uint32_t tile_tokens, 
             for (uint32_t r = threadIdx.x; r < n; r += THREADS) a.status[r] = GIFT_ST_BAD_TABLE;
         return false;
     }
-    const uint64_t slice = slice_units(total, a.n_cta, a.least);
+    const uint64_t slice = slice_units(total, a.n_slices, a.least);
     const uint64_t u = slice * w;
     *total_out = total;
     *slice_out = slice;
@@ -124,8 +131,8 @@ __device__ bool place_unit(const AttnArgs& a, uint32_t w, uint32_t tile_tokens, 
             if (u < before + it.units) {
                 sh->at.r = r;
                 sh->at.row0 = (uint32_t)row;
-                sh->at.item = (uint32_t)((u - before) / it.cost);
-                sh->at.u = (uint32_t)((u - before) - (uint64_t)sh->at.item * it.cost);
+                sh->at.k = (uint32_t)((u - before) / it.cost);
+                sh->at.u = (uint32_t)((u - before) - (uint64_t)sh->at.k * it.cost);
                 break;
             }
             before += it.units;
@@ -141,7 +148,7 @@ template <uint32_t TILE> struct Walk {
     ReqShape s;
     ItemShape it;
     uint32_t r, row0;
-    uint32_t u;                      // units of the current item that are done
+    uint32_t way, k, u;              // which of the CTAs that share the slice; item (or pair); its units that are done
     uint64_t left;                   // units to go
     int32_t next_owner, next_have, next_want;       // of request r + 1, fetched ahead
     // the current piece: K/V head, tile of query rows, token tiles
@@ -152,15 +159,13 @@ template <uint32_t TILE> struct Walk {
         const uint32_t k = r + 1 < a.b.n_req ? r + 1 : r;
         next_owner = a.b.owner[k]; next_have = a.b.have[k]; next_want = a.b.want[k];
     }
-    __device__ __forceinline__ void start(const AttnArgs& a, const Place& p, uint64_t units)
+    __device__ __forceinline__ void start(const AttnArgs& a, const Place& p, uint32_t which, uint64_t units)
     {
+        way = which; k = p.k; u = p.u;
         r = p.r; row0 = p.row0; left = units;
         s = load_shape(a.b, r);
         it = item_shape(a, s, TILE);
         fetch(a);
-        u = (uint32_t)p.u;
-        h = p.item / it.nqt;
-        qt = p.item - h * it.nqt;
         all_q = it.rows_m * a.group;
     }
     __device__ __forceinline__ bool next(const AttnArgs& a)
@@ -168,19 +173,16 @@ template <uint32_t TILE> struct Walk {
         while (left > 0) {
             if (u >= it.cost) {
                 u = 0;
-                if (++qt == it.nqt) {
-                    qt = 0;
-                    if (++h == a.kv_heads) {
-                        h = 0;
-                        do {
-                            row0 += it.rows_m;
-                            r++;
-                            s = req_shape(next_owner, next_have, next_want, a.b.page, a.b.max_blocks);
-                            it = item_shape(a, s, TILE);
-                            fetch(a);
-                        } while (it.nqt == 0);
-                        all_q = it.rows_m * a.group;
-                    }
+                if (++k * a.ways >= it.items) {
+                    k = 0;
+                    do {
+                        row0 += it.rows_m;
+                        r++;
+                        s = req_shape(next_owner, next_have, next_want, a.b.page, a.b.max_blocks);
+                        it = item_shape(a, s, TILE);
+                        fetch(a);
+                    } while (it.nqt == 0);
+                    all_q = it.rows_m * a.group;
                 }
             }
             const uint32_t used = (uint64_t)(it.cost - u) < left ? it.cost - u : (uint32_t)left;
@@ -189,7 +191,11 @@ template <uint32_t TILE> struct Walk {
             n_tiles = (end > a.extra ? end - a.extra : 0u) - tb;       // none when the units end in the item's extra
             u = end;
             left -= used;
-            if (n_tiles) return true;
+            const uint32_t item = k * a.ways + way;
+            if (n_tiles == 0 || item >= it.items) continue;            // an odd last item has no partner
+            h = item / it.nqt;
+            qt = item - h * it.nqt;
+            return true;
         }
         return false;
     }

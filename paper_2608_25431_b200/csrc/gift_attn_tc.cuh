@@ -284,7 +284,7 @@ __global__ void __launch_bounds__(TC_THREADS, 2) attn_tc_kernel(const __grid_con
     }
     uint64_t total, slice;
     // ends with a barrier for every thread, taken or not
-    const bool some = place_unit<TC_THREADS>(a, blockIdx.x, TC_TILE, blockIdx.x == 0, &sh.place, &total, &slice);
+    const bool some = place_unit<TC_THREADS>(a, blockIdx.x / a.ways, TC_TILE, blockIdx.x == 0, &sh.place, &total, &slice);
     if (!some) return;
     if (warp == 6) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sh.tmem)), "r"(TMEM_COLS) : "memory");
@@ -295,12 +295,12 @@ __global__ void __launch_bounds__(TC_THREADS, 2) attn_tc_kernel(const __grid_con
     tc_after();
     const uint32_t tmem = sh.tmem;
     volatile int* dead = &sh.dead;
-    const uint64_t units = slice < total - slice * blockIdx.x ? slice : total - slice * blockIdx.x;
+    const uint64_t begin = slice * (blockIdx.x / a.ways), units = slice < total - begin ? slice : total - begin;
     const uint32_t sm = smem_u32(smem);
     TcWalk& w = walks[warp];
     {
         TcWalk x;
-        x.start(a, sh.place.at, units);
+        x.start(a, sh.place.at, blockIdx.x % a.ways, units);
         if (lane == 0) w = x;
         __syncwarp();
     }
@@ -308,8 +308,8 @@ __global__ void __launch_bounds__(TC_THREADS, 2) attn_tc_kernel(const __grid_con
     if (warp == 4 || warp == 5) {
         // ------------------------------------------------------------------ copies
         // Lane l brings run l % runs of a tile (or gathers 4 tokens), columns 64 (l / runs) .. + 63.
-        const uint32_t kv = warp - 4, runs = TC_TILE / (a.run > 4 ? a.run : 4), col = lane / runs, first = (lane % runs) * (TC_TILE / runs);
-        const bool mine = col < D / 64, gather = a.run < 8;
+        const uint32_t kv = warp - 4, runs = TC_TILE / (a.run > 4 ? a.run : 4), col = lane / runs, first = (lane & (runs - 1)) * (TC_TILE / runs);
+        const bool active = col < D / 64, gather = a.run < 8;
         uint64_t* full = kv ? sh.v_full : sh.k_full;
         uint64_t* empty = kv ? sh.v_empty : sh.k_empty;
         uint32_t n = 0, piece = 0, q_loads = 0;            // tiles and pieces so far
@@ -333,51 +333,53 @@ __global__ void __launch_bounds__(TC_THREADS, 2) attn_tc_kernel(const __grid_con
                                (int32_t)(w.row0 + a.by_group.quot(w.qt * a.tile_rows)), &sh.q_full);
                 }
             }
-            int32_t next[4];                               // table entries, fetched a tile ahead
-            auto entries = [&](uint32_t j) {
-#pragma unroll
-                for (int e = 0; e < 4; e++) {
-                    const uint32_t t = (w.tb + j) * TC_TILE + first + e;
-                    next[e] = (e == 0 || gather) && mine && j < w.n_tiles && t < w.s.want ? table[a.b.page.quot(t)] : -1;
-                }
-            };
-            entries(0);
-            int32_t label[4] = {GIFT_OWNER_PARAM, GIFT_OWNER_PARAM, GIFT_OWNER_PARAM, GIFT_OWNER_PARAM};   // judged a tile later
+            // Where runs are copied, lane l looks up its run's first token; where tokens are gathered, tokens
+            // l and l + 32.  Table entries are fetched a tile ahead, labels judged a tile later.
+            int32_t next[2] = {-1, -1}, label[2] = {GIFT_OWNER_PARAM, GIFT_OWNER_PARAM};
+            const uint32_t mine = gather ? lane : first;
 #pragma unroll 1
-            for (uint32_t j = 0; j < w.n_tiles; j++, n++) {
+            for (uint32_t j = 0; j <= w.n_tiles; j++) {
+                int32_t slot[2], page[2];
+#pragma unroll
+                for (int e = 0; e < 2; e++) {
+                    // the slots of tile j - 1, and the entries of tile j
+                    const uint32_t t_next = (w.tb + j) * TC_TILE + mine + e * 32, t = t_next - TC_TILE;
+                    const bool used = e == 0 || gather;
+                    bits |= label_read_status(label[e], owner);
+                    page[e] = -1;
+                    if (j > 0 && used && t < w.s.want) {
+                        page[e] = (uint32_t)next[e] < a.b.n_pages ? next[e] : -1;
+                        if (page[e] < 0) bits |= GIFT_ST_BAD_DESC;
+                    }
+                    slot[e] = page[e] >= 0 ? (int32_t)((uint32_t)page[e] * a.b.page_tokens + (t - a.b.page.quot(t) * a.b.page_tokens)) : -(int32_t)TC_TILE;
+                    next[e] = j < w.n_tiles && used && t_next < w.s.want ? table[a.b.page.quot(t_next)] : -1;
+                    label[e] = kv == 0 && a.owner_map && page[e] >= 0 ? a.owner_map[page[e]] : GIFT_OWNER_PARAM;
+                }
+                if (j == 0) continue;
                 const uint32_t stage = n % TC_STAGES, round = n / TC_STAGES;
-                int32_t slot[4], page[4];
-#pragma unroll
-                for (int e = 0; e < 4; e++) bits |= label_read_status(label[e], owner);
-#pragma unroll
-                for (int e = 0; e < 4; e++) {
-                    const uint32_t t = (w.tb + j) * TC_TILE + first + e;
-                    const bool fine = next[e] >= 0 && (uint32_t)next[e] < a.b.n_pages;
-                    page[e] = fine ? next[e] : -1;
-                    slot[e] = fine ? (int32_t)((uint32_t)next[e] * a.b.page_tokens + (t - a.b.page.quot(t) * a.b.page_tokens)) : -1;
-                    if ((e == 0 || gather) && mine && t < w.s.want && !fine) bits |= GIFT_ST_BAD_DESC;
-                }
-                entries(j + 1);
-                if (kv == 0 && a.owner_map) {
-#pragma unroll
-                    for (int e = 0; e < 4; e++) label[e] = page[e] >= 0 ? a.owner_map[page[e]] : GIFT_OWNER_PARAM;
-                }
                 ok = round == 0 || warp_wait(&empty[stage], (round - 1) & 1u, dead);
                 if (!ok) break;
                 const uint32_t dst = sm + (kv ? L::v : L::k) + stage * (TC_TILE * D * 2) + col * (TC_TILE * 128) + first * 128;
-                if (mine) {
-                    if (gather) gather4(dst, &map, x, slot, &full[stage]);
-                    else copy_run(dst, &map, x, slot[0] < 0 ? -(int32_t)TC_TILE : slot[0], &full[stage]);
-                }
-                if (kv == 0 && j + 1 == w.n_tiles) {
-                    // the piece's verdict, before the last tile is announced
+                if (gather) {
+                    int32_t four[4];
 #pragma unroll
-                    for (int e = 0; e < 4; e++) bits |= label_read_status(label[e], owner);
+                    for (int e = 0; e < 4; e++) {
+                        const int32_t lo = __shfl_sync(0xFFFFFFFFu, slot[0], (first + e) & 31u), hi = __shfl_sync(0xFFFFFFFFu, slot[1], (first + e) & 31u);
+                        four[e] = first < 32 ? lo : hi;
+                    }
+                    if (active) gather4(dst, &map, x, four, &full[stage]);
+                } else if (active) {
+                    copy_run(dst, &map, x, slot[0], &full[stage]);
+                }
+                if (kv == 0 && j == w.n_tiles) {
+                    // the piece's verdict, before the last tile is announced
+                    bits |= label_read_status(label[0], owner) | label_read_status(label[1], owner);
                     bits = __reduce_or_sync(0xFFFFFFFFu, bits);
                     if (lane == 0 && bits) atomicOr(&sh.bits[piece % TC_BITS_RING], bits);
                 }
                 __syncwarp();
                 if (lane == 0) bar_expect(&full[stage], TC_TILE * D * 2);
+                n++;
             }
             piece++;
         }

@@ -233,30 +233,34 @@ def _dev(t):
     return C.c_void_p(t.data_ptr())
 
 
-def _arr(t, device, what, dtype="int32", n=None, optional=False):
+def _arr(t, device, what, dtype="int32", n=0, optional=False):
     """Pointer of a contiguous tensor of the named type on cuda:device with at least n elements."""
     if t is None:
         if optional:
             return None
         raise ValueError("%s is missing" % what)
-    if t.get_device() != device or device < 0 or not t.is_contiguous():
-        raise ValueError("%s: expected a contiguous tensor on %s" % (what, "a GPU" if device < 0 else "cuda:%d" % device))
-    if t.dtype not in _dtypes()[dtype]:
-        raise ValueError("%s: expected %s, got %s" % (what, dtype, t.dtype))
-    if n is not None and t.numel() < n:
+    # one condition, looked into only when it fails: a call checks a dozen arrays
+    if t.get_device() != device or device < 0 or t.dtype not in _torch_types[dtype] or t.numel() < n or not t.is_contiguous():
+        if t.get_device() != device or device < 0 or not t.is_contiguous():
+            raise ValueError("%s: expected a contiguous tensor on %s" % (what, "a GPU" if device < 0 else "cuda:%d" % device))
+        if t.dtype not in _torch_types[dtype]:
+            raise ValueError("%s: expected %s, got %s" % (what, dtype, t.dtype))
         raise ValueError("%s: %d elements, %d are needed" % (what, t.numel(), n))
     return t.data_ptr()
 
 
-_dtype_table = {}
+class _TorchTypes(dict):
+    """The torch types that an array of the named type may have (int32 arrays hold 32-bit words); torch is
+    imported when the first of them is looked up."""
 
-
-def _dtypes():
-    """The torch types that an array of the named type may have (int32 arrays hold 32-bit words)."""
-    if not _dtype_table:
+    def __missing__(self, key):
         import torch
-        _dtype_table.update(int32=(torch.int32, torch.uint32), int64=(torch.int64,), float32=(torch.float32,))
-    return _dtype_table
+        self.update(int32=(torch.int32, torch.uint32), int64=(torch.int64,), float32=(torch.float32,),
+                    pool={torch.bfloat16: 0, torch.float16: 1})
+        return self[key]
+
+
+_torch_types = _TorchTypes()
 
 
 def _rows3(t, device, what, heads, dim, dtype, rows=None):
@@ -474,8 +478,17 @@ class Ctx:
                  _stream_ptr(stream)), "gift_labels_swap_in")
 
     def _stream(self, stream):
-        import torch
-        return C.c_void_p(torch.cuda.current_stream(self.device).cuda_stream if stream is None else int(stream))
+        """The given stream, or the context's device's current one, as a number."""
+        if stream is not None:
+            return int(stream)
+        if self._raw_stream is None:
+            import torch
+            # the number alone; torch.cuda.current_stream() makes a Stream object, ten times as slow
+            self._raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
+                (lambda d: torch.cuda.current_stream(d).cuda_stream)
+        return self._raw_stream(self.device)
+
+    _raw_stream = None
 
     def _batch(self, batch):
         if batch.device != self.device:
@@ -520,7 +533,7 @@ class Ctx:
     def _pool(self, pages, owner_map):
         if pages.dim() != 5 or pages.shape[2] != 2:
             raise ValueError("pages: expected shape [n_pages, page_tokens, 2, n_heads, head_dim], got %s" % (tuple(pages.shape),))
-        dtype = {"torch.bfloat16": 0, "torch.float16": 1}.get(str(pages.dtype))
+        dtype = _torch_types["pool"].get(pages.dtype)
         if dtype is None:
             raise ValueError("pages: expected bfloat16 or float16, got %s" % pages.dtype)
         n, pt, _, heads, dim = pages.shape

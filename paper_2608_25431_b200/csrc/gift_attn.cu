@@ -469,11 +469,22 @@ __global__ void __launch_bounds__(JOIN_THREADS) attn_join_kernel(const __grid_co
     if (h == 0 && q0 == 0) write_request<JOIN_THREADS>(a, r, row0, it.rows_m, bits);
 }
 
+// A kernel's shared-memory limit, raised once per device: the call costs as much as a launch's half.
+template <auto KERNEL> cudaError_t allow_smem(int device, int bytes)
+{
+    static bool done[64];
+    if (device < 0 || device >= 64) return cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (done[device]) return cudaSuccess;
+    const cudaError_t e = cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    done[device] = e == cudaSuccess;
+    return e;
+}
+
 template <class T, int D>
 int launch_few(gift_ctx* c, AttnArgs& a, cudaStream_t st)
 {
     constexpr int smem = FewSmem<D>::bytes;
-    CU_TRY(cudaFuncSetAttribute(attn_few_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+    CU_TRY((allow_smem<attn_few_kernel<T, D>>(c->device, smem)));
     a.n_slices = 2u * c->num_sms;
     a.ways = 1;
     a.tile_rows = FEW_ROWS;
@@ -549,7 +560,7 @@ int launch_many(gift_ctx* c, AttnArgs& a, uint64_t rows, cudaStream_t st)
     if (rc == GIFT_OK) rc = map_of_q(a, std::is_same<T, __half>::value, D, &q_map);
     if (rc != GIFT_OK) return rc;
     constexpr int smem = TcSmem<D>::bytes;
-    CU_TRY(cudaFuncSetAttribute(attn_tc_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+    CU_TRY((allow_smem<attn_tc_kernel<T, D>>(c->device, smem)));
     // two CTAs to a slice when an average request's rows fill more than one tile
     a.ways = rows > (uint64_t)TC_ROWS ? 2u : 1u;
     a.n_slices = 2u * c->num_sms / a.ways;

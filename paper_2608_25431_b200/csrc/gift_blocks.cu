@@ -20,12 +20,19 @@ namespace {
 // block tables
 // ---------------------------------------------------------------------------
 //
-// One cluster of 8 CTAs, so that the stages (check and claim, commit labels and taken entries,
-// push what is given back) can be separated by the cluster's hardware barrier; what they touch is
-// a few words per page that changes hands and layer.  Latency bound.
-
-constexpr int BT_CTAS = 8;
-constexpr int BT_THREADS = 512;
+// One cluster of 16 CTAs (8 where the device cannot co-schedule 16), so that the stages (check and
+// claim, commit labels and taken entries, push what is given back) can be separated by the
+// cluster's hardware barrier.  What they touch is a word per page that changes hands and layer,
+// scattered over the label map: latency bound when few pages change hands, bound by the 16 SMs'
+// scattered accesses when many do.  2 to 32 threads share a page when there are threads to spare;
+// a thread has 8 layers' labels under way at once, and what it needs of the page's request lies in
+// shared memory.
+// (measured: see below)
+constexpr int BT_CTAS_PORTABLE = 8;
+constexpr int BT_CTAS_LARGE = 16;
+constexpr int BT_THREADS = 1024;
+constexpr uint32_t BT_REQ_BYTES = 12;    // shared memory per request
+constexpr int BT_MAX_DEVICES = 64;
 
 struct BlockArgs {
     BatchArgs b;
@@ -37,51 +44,59 @@ struct BlockArgs {
     uint32_t* status;
 };
 
+// What every CTA knows of the requests after the prefix sums.
+struct BlockPlan {
+    uint32_t* take;          // [n_req] exclusive prefix of the pages taken
+    uint32_t* give;          // [n_req] exclusive prefix of the pages given back
+    uint32_t* from;          // [n_req] first block taken, or given back
+    uint32_t taken;
+    int32_t height;          // of the stack before the call
+};
+
 // One page that changes hands: item k < taken comes off the stack, the others go back to it.
 struct PageMove {
     uint32_t r;
-    uint32_t i;              // which of the request's taken / given pages
     uint64_t entry;          // its entry in the block tables
     int32_t page;
 };
 
-__device__ __forceinline__ PageMove page_move(const BlockArgs& a, const uint32_t* p_take, const uint32_t* p_give,
-                                              uint32_t taken, int32_t height, uint32_t k)
+__device__ __forceinline__ PageMove page_move(const BlockArgs& a, const BlockPlan& p, uint32_t k)
 {
     PageMove m;
-    const bool take = k < taken;
-    const uint32_t* first = take ? p_take : p_give;
-    const uint32_t at = take ? k : k - taken;
+    const bool take = k < p.taken;
+    const uint32_t* first = take ? p.take : p.give;
+    const uint32_t at = take ? k : k - p.taken;
     m.r = req_of(first, a.b.n_req, at);
-    m.i = at - first[m.r];
-    const ReqShape s = load_shape(a.b, m.r);
-    m.entry = (uint64_t)m.r * a.b.max_blocks + (take ? s.bh : s.bw) + m.i;
-    m.page = take ? __ldcg(a.free_pages + (height - 1 - (int32_t)k)) : __ldcg(a.b.table + m.entry);
+    m.entry = (uint64_t)m.r * a.b.max_blocks + p.from[m.r] + (at - first[m.r]);
+    m.page = take ? __ldcg(a.free_pages + (p.height - 1 - (int32_t)k)) : __ldcg(a.b.table + m.entry);
     return m;
 }
 
-__global__ void __cluster_dims__(BT_CTAS, 1, 1) __launch_bounds__(BT_THREADS)
+__global__ void __launch_bounds__(BT_THREADS, 1)
 block_tables_kernel(const __grid_constant__ BlockArgs a)
 {
     extern __shared__ uint32_t dyn[];
     __shared__ uint64_t warp_sums[BT_THREADS / 32];
     __shared__ uint32_t s_bad;                          // CTA 0's copy is the cluster's
     __shared__ unsigned long long s_taken;
-    uint32_t* p_take = dyn;                             // [n_req] exclusive prefix of the pages taken
-    uint32_t* p_give = dyn + a.b.n_req;                 // [n_req] exclusive prefix of the pages given back
     cg::cluster_group cl = cg::this_cluster();
     uint32_t* bad = cl.map_shared_rank(&s_bad, 0);
-    const uint32_t tid = blockIdx.x * BT_THREADS + threadIdx.x, nthr = BT_CTAS * BT_THREADS;
+    // neighbouring warps of work go to different CTAs: a few pages are spread over the SMs
+    const uint32_t n_cta = gridDim.x, tid = (threadIdx.x >> 5) * n_cta * 32 + blockIdx.x * 32 + (threadIdx.x & 31), nthr = n_cta * BT_THREADS;
     const uint32_t n = a.b.n_req;
-    const int32_t height = *a.n_free;
-    const bool stack_bad = height < 0 || (uint32_t)height > a.free_cap;
+    BlockPlan p;
+    p.take = dyn;
+    p.give = dyn + n;
+    p.from = dyn + 2 * n;
+    p.height = *a.n_free;
+    const bool stack_bad = p.height < 0 || (uint32_t)p.height > a.free_cap;
     if (threadIdx.x == 0) { s_bad = 0u; s_taken = 0ull; }
     __syncthreads();
 
     // Prefix sums.  Pages are handed out in request order; a request is served when its need and
     // all needs before it (refused ones included) fit the stack, so the served ones are a prefix
     // of those that need anything.
-    uint64_t take0 = 0, give0 = 0;
+    uint64_t take0 = 0, give0 = 0, most = 0;
     for (uint32_t r0 = 0; r0 < n; r0 += BT_THREADS) {
         const uint32_t r = r0 + threadIdx.x;
         uint64_t need = 0, give = 0;
@@ -89,42 +104,59 @@ block_tables_kernel(const __grid_constant__ BlockArgs a)
             const ReqShape s = load_shape(a.b, r);
             need = req_need(s);
             give = req_give(s);
+            p.from[r] = need ? s.bh : s.bw;
         }
         uint64_t tot_take, tot_give;
         const uint64_t incl_take = take0 + block_scan<BT_THREADS>(need, warp_sums, &tot_take);
         const uint64_t incl_give = give0 + block_scan<BT_THREADS>(give, warp_sums, &tot_give);
         if (r < n) {
-            p_take[r] = saturate32(incl_take - need);
-            p_give[r] = saturate32(incl_give - give);
-            if (need && !stack_bad && incl_take <= (uint64_t)height) atomicMax(&s_taken, (unsigned long long)incl_take);
+            p.take[r] = saturate32(incl_take - need);
+            p.give[r] = saturate32(incl_give - give);
+            if (need && !stack_bad && incl_take <= (uint64_t)p.height) most = incl_take;
         }
         take0 += tot_take;
         give0 += tot_give;
     }
+    if (most) atomicMax(&s_taken, (unsigned long long)most);
     __syncthreads();
-    const uint32_t taken = (uint32_t)s_taken;           // <= height
+    p.taken = (uint32_t)s_taken;                        // <= height
     // more given back than the stack has room for (or than there are pages): some page is named twice
-    const bool no_room = stack_bad || (uint64_t)(height - (int32_t)taken) + give0 > a.free_cap;
+    const bool no_room = stack_bad || (uint64_t)(p.height - (int32_t)p.taken) + give0 > a.free_cap;
     const uint32_t given = no_room ? 0u : (uint32_t)give0;
-    const uint32_t moves = no_room ? 0u : taken + given;
+    const uint32_t moves = no_room ? 0u : p.taken + given;
     cl.sync();                                          // every CTA's s_bad is initialised
+
+    // threads that share a page, and this one's number among them
+    uint32_t share = 32;
+    while (share > 1 && (uint64_t)moves * share > nthr) share >>= 1;
+    const uint32_t sub = tid & (share - 1), first = tid / share, step = nthr / share;
 
     // Check and claim.  A page may be taken only if nobody owns it in any layer, given back only
     // by its owner, and appear once in the call: the first mention claims its label.
-    const uint64_t n_work = (uint64_t)moves * a.layers;
-    for (uint64_t e = tid; e < n_work; e += nthr) {
-        const uint32_t k = (uint32_t)(e / a.layers), l = (uint32_t)(e % a.layers);
-        const PageMove m = page_move(a, p_take, p_give, taken, height, k);
+    bool wrong = no_room;
+    for (uint32_t k = first; k < moves; k += step) {
+        const PageMove m = page_move(a, p, k);
         bool ok = m.page >= 0 && (uint32_t)m.page < a.b.n_pages;
         if (ok) {
-            int32_t* lab = a.owner_map + (uint64_t)l * a.b.n_pages + m.page;
-            const int32_t v = __ldcg(lab);
-            ok = k < taken ? label_takable(v) : label_givable(v, a.b.owner[m.r]);
-            if (ok && l == 0) ok = atomicCAS(lab, v, label_flip(v)) == v;
+            const int32_t owner = a.b.owner[m.r];
+            int32_t* lab = a.owner_map + m.page;
+            if (sub == 0) {
+                const int32_t v = __ldcg(lab);
+                ok = k < p.taken ? label_takable(v) : label_givable(v, owner);
+                if (ok) ok = atomicCAS(lab, v, label_flip(v)) == v;
+            }
+            for (uint32_t l0 = sub == 0 ? share : sub; l0 < a.layers; l0 += 8 * share) {
+                int32_t w[8];
+#pragma unroll
+                for (int e = 0; e < 8; e++)
+                    w[e] = l0 + e * share < a.layers ? __ldcg(lab + (uint64_t)(l0 + e * share) * a.b.n_pages) : GIFT_OWNER_NONE;
+#pragma unroll
+                for (int e = 0; e < 8; e++) ok = ok && (k < p.taken ? label_takable(w[e]) : label_givable(w[e], owner));
+            }
         }
-        if (!ok) atomicOr(bad, 1u);
+        wrong = wrong || !ok;
     }
-    if (no_room && tid == 0) atomicOr(bad, 1u);
+    if (wrong) atomicOr(bad, 1u);
     cl.sync();
     const bool refused = *bad != 0u;
 
@@ -133,14 +165,14 @@ block_tables_kernel(const __grid_constant__ BlockArgs a)
         if (!refused) {
             const ReqShape s = load_shape(a.b, r);
             const uint32_t need = req_need(s);
-            st = !s.ok ? GIFT_ST_BAD_DESC : need && (uint64_t)p_take[r] + need > (uint64_t)height ? GIFT_ST_NO_BLOCKS : 0u;
+            st = !s.ok ? GIFT_ST_BAD_DESC : need && (uint64_t)p.take[r] + need > (uint64_t)p.height ? GIFT_ST_NO_BLOCKS : 0u;
         }
         a.status[r] = st;
     }
     if (refused) {
         // put the claimed labels back; a page mentioned twice is put back by whoever gets there first
         for (uint32_t k = tid; k < moves; k += nthr) {
-            const PageMove m = page_move(a, p_take, p_give, taken, height, k);
+            const PageMove m = page_move(a, p, k);
             if (m.page < 0 || (uint32_t)m.page >= a.b.n_pages) continue;
             const int32_t v = __ldcg(a.owner_map + m.page);
             if (label_claimed(v)) atomicCAS(a.owner_map + m.page, v, label_flip(v));
@@ -150,21 +182,24 @@ block_tables_kernel(const __grid_constant__ BlockArgs a)
     }
 
     // Commit the labels, and the taken pages' entries.
-    for (uint64_t e = tid; e < n_work; e += nthr) {
-        const uint32_t k = (uint32_t)(e / a.layers), l = (uint32_t)(e % a.layers);
-        const PageMove m = page_move(a, p_take, p_give, taken, height, k);
-        a.owner_map[(uint64_t)l * a.b.n_pages + m.page] = k < taken ? a.b.owner[m.r] : GIFT_OWNER_NONE;
-        if (l == 0 && k < taken) a.b.table[m.entry] = m.page;
+    for (uint32_t k = first; k < moves; k += step) {
+        const PageMove m = page_move(a, p, k);
+        const bool take = k < p.taken;
+        const int32_t label = take ? a.b.owner[m.r] : GIFT_OWNER_NONE;
+        int32_t* lab = a.owner_map + m.page;
+#pragma unroll 8
+        for (uint32_t l = sub; l < a.layers; l += share) lab[(uint64_t)l * a.b.n_pages] = label;
+        if (take && sub == 0) a.b.table[m.entry] = m.page;
     }
     cl.sync();                                          // taken entries of the stack have been read
 
     // Push what is given back where the taken pages were, and above.
-    for (uint32_t k = taken + tid; k < moves; k += nthr) {
-        const PageMove m = page_move(a, p_take, p_give, taken, height, k);
-        a.free_pages[(uint32_t)height - taken + (k - taken)] = m.page;
+    for (uint32_t k = p.taken + tid; k < moves; k += nthr) {
+        const PageMove m = page_move(a, p, k);
+        a.free_pages[(uint32_t)p.height - p.taken + (k - p.taken)] = m.page;
         a.b.table[m.entry] = -1;
     }
-    if (tid == 0) *a.n_free = height - (int32_t)taken + (int32_t)given;
+    if (tid == 0) *a.n_free = p.height - (int32_t)p.taken + (int32_t)given;
 }
 
 // ---------------------------------------------------------------------------
@@ -320,10 +355,38 @@ int gift_block_tables(gift_ctx* c, const gift_batch* batch, int32_t* free_pages,
     a.b = batch_args(batch);
     a.free_pages = free_pages; a.n_free = n_free; a.free_cap = free_cap;
     a.owner_map = owner_map; a.layers = layers; a.status = status;
-    const size_t smem = (size_t)batch->n_req * 8;
-    if (smem > 40 * 1024)
-        CU_TRY(cudaFuncSetAttribute(block_tables_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, GIFT_MAX_REQS * 8));
-    block_tables_kernel<<<BT_CTAS, BT_THREADS, smem, (cudaStream_t)stream>>>(a);
+    cudaLaunchConfig_t cfg;
+    memset(&cfg, 0, sizeof(cfg));
+    cfg.blockDim = dim3(BT_THREADS, 1, 1);
+    cfg.stream = (cudaStream_t)stream;
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.y = 1;
+    attr.val.clusterDim.z = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    // Once per device: shared memory for the most requests, and whether 16 such CTAs can be co-scheduled.
+    static int ctas_for_device[BT_MAX_DEVICES];
+    const int slot = c->device >= 0 && c->device < BT_MAX_DEVICES ? c->device : -1;
+    int ctas = slot >= 0 ? ctas_for_device[slot] : 0;
+    if (ctas == 0) {
+        CU_TRY(cudaFuncSetAttribute(block_tables_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, GIFT_MAX_REQS * BT_REQ_BYTES));
+        ctas = BT_CTAS_PORTABLE;
+        if (cudaFuncSetAttribute(block_tables_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess) {
+            int n_clusters = 0;
+            cfg.gridDim = dim3(BT_CTAS_LARGE, 1, 1);
+            cfg.dynamicSmemBytes = GIFT_MAX_REQS * BT_REQ_BYTES;
+            attr.val.clusterDim.x = BT_CTAS_LARGE;
+            if (cudaOccupancyMaxActiveClusters(&n_clusters, block_tables_kernel, &cfg) == cudaSuccess && n_clusters >= 1)
+                ctas = BT_CTAS_LARGE;
+        }
+        (void)cudaGetLastError();
+        if (slot >= 0) ctas_for_device[slot] = ctas;
+    }
+    cfg.gridDim = dim3(ctas, 1, 1);
+    cfg.dynamicSmemBytes = (size_t)batch->n_req * BT_REQ_BYTES;
+    attr.val.clusterDim.x = ctas;
+    CU_TRY(cudaLaunchKernelEx(&cfg, block_tables_kernel, a));
     c->launches++;
     CU_TRY(cudaGetLastError());
     return GIFT_OK;

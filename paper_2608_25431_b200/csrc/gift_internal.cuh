@@ -107,15 +107,16 @@ void gift_note_cuda_error(cudaError_t e, const char* file, int line);
 // Makes a device current for the duration of a call and restores the previous one.
 struct DeviceGuard {
     int prev;
-    bool ok;
-    explicit DeviceGuard(int dev) : prev(-1), ok(false)
+    bool ok, moved;
+    explicit DeviceGuard(int dev) : prev(-1), ok(false), moved(false)
     {
         if (cudaGetDevice(&prev) != cudaSuccess) return;
-        ok = prev == dev || cudaSetDevice(dev) == cudaSuccess;
+        moved = prev != dev;
+        ok = !moved || cudaSetDevice(dev) == cudaSuccess;
     }
     ~DeviceGuard()
     {
-        if (ok && prev >= 0) cudaSetDevice(prev);
+        if (ok && moved) cudaSetDevice(prev);
     }
 };
 

@@ -109,7 +109,6 @@ __global__ void __launch_bounds__(FEW_THREADS, 2) attn_few_kernel(const __grid_c
         const uint32_t g = lane >> 2, c2 = (lane & 3) * 2;
         uint32_t qf[MT][KS][4];
         uint32_t row_i[MT][2];
-        const uint32_t* words[MT][2];
 #pragma unroll
         for (int mt = 0; mt < MT; mt++) {
 #pragma unroll
@@ -118,7 +117,6 @@ __global__ void __launch_bounds__(FEW_THREADS, 2) attn_few_kernel(const __grid_c
                 const bool there = rho < all_q;
                 const uint32_t i = there ? a.by_group.quot(rho) : 0u, hq = h * a.group + (there ? rho - i * a.group : 0u);
                 row_i[mt][half] = i;
-                words[mt][half] = a.mask + (uint64_t)(row0 + i) * a.mask_words;
                 const char* q = a.q + (uint64_t)(row0 + i) * a.q_row + (uint64_t)hq * a.q_head;
 #pragma unroll
                 for (int ks = 0; ks < KS; ks++)
@@ -178,11 +176,12 @@ __global__ void __launch_bounds__(FEW_THREADS, 2) attn_few_kernel(const __grid_c
             }
             cp_commit();
         };
-#pragma unroll
-        for (int st = 0; st < FEW_STAGES - 1; st++) issue(st);
-
-        for (uint32_t step = 0; step < n_tiles; step++) {
-            issue(step + FEW_STAGES - 1);
+        // the first rounds only fill the ring (one copy of the code: it is large, and short items meet it cold)
+#pragma unroll 1
+        for (uint32_t round = 0; round < n_tiles + FEW_STAGES - 1; round++) {
+            issue(round);
+            if (round < (uint32_t)FEW_STAGES - 1) continue;
+            const uint32_t step = round - (FEW_STAGES - 1);
             cp_wait<FEW_STAGES - 1>();
             __syncwarp();
             const uint32_t kb = ring + (step % FEW_STAGES) * (2 * HALF), vb = kb + HALF;
@@ -205,7 +204,7 @@ __global__ void __launch_bounds__(FEW_THREADS, 2) attn_few_kernel(const __grid_c
                 }
             }
             const bool mixed = t0 + 16 > s.have;       // some rows may not see some of these tokens
-            uint32_t pf[MT][4];
+            uint32_t pf[MT][4], sees[MT][2];           // of the 16 tokens, by row
 #pragma unroll
             for (int mt = 0; mt < MT; mt++) {
 #pragma unroll
@@ -213,12 +212,15 @@ __global__ void __launch_bounds__(FEW_THREADS, 2) attn_few_kernel(const __grid_c
 #pragma unroll
                     for (int e = 0; e < 4; e++) sc[mt][n][e] *= a.scale_log2;
                 if (mixed) {
+                    const bool none = w.masked_short(a) || t0 >= s.want;
+#pragma unroll
+                    for (int half = 0; half < 2; half++)
+                        sees[mt][half] = none ? 0u : (uint32_t)row_sees64(a, s.have, s.want, row0 + row_i[mt][half], row_i[mt][half], t0);
 #pragma unroll
                     for (int n = 0; n < 2; n++)
 #pragma unroll
                         for (int e = 0; e < 4; e++)
-                            if (bits & GIFT_ST_BAD_DESC || !row_sees(a, s, row_i[mt][e >> 1], words[mt][e >> 1], t0 + n * 8 + c2 + (e & 1)))
-                                sc[mt][n][e] = NEG_INF;
+                            if (!(sees[mt][e >> 1] >> (n * 8 + c2 + (e & 1)) & 1u)) sc[mt][n][e] = NEG_INF;
                 }
                 float alpha[2];
 #pragma unroll
@@ -283,6 +285,7 @@ __global__ void __launch_bounds__(FEW_THREADS, 2) attn_few_kernel(const __grid_c
             } else {
 #pragma unroll
                 for (int mt = 0; mt < MT; mt++)
+#pragma unroll 1
                     for (int t = 0; t < 16; t++) {
 #pragma unroll
                         for (int half = 0; half < 2; half++) {
@@ -291,8 +294,7 @@ __global__ void __launch_bounds__(FEW_THREADS, 2) attn_few_kernel(const __grid_c
                             const float p0 = __shfl_sync(0xFFFFFFFFu, t < 8 ? sc[mt][0][half * 2] : sc[mt][1][half * 2], from);
                             const float p1 = __shfl_sync(0xFFFFFFFFu, t < 8 ? sc[mt][0][half * 2 + 1] : sc[mt][1][half * 2 + 1], from);
                             const float p = t & 1 ? p1 : p0;
-                            const bool sees = !(bits & GIFT_ST_BAD_DESC) && row_sees(a, s, row_i[mt][half], words[mt][half], t0 + t);
-                            if (!sees) continue;
+                            if (!(sees[mt][half] >> t & 1u)) continue;
 #pragma unroll
                             for (int n = 0; n < D / 8; n++) {
                                 uint32_t x;

@@ -210,13 +210,27 @@ __device__ __forceinline__ float fast_exp2(float x)
     return y;
 }
 
-// Whether row i of the step (its mask words at `words`) sees token t.
-__device__ __forceinline__ bool row_sees(const AttnArgs& a, const ReqShape& s, uint32_t i, const uint32_t* words, uint32_t t)
+// Which of the 64 tokens from t0 a request's i-th row (row `row` of the step) sees, as bits.
+static __device__ __noinline__ uint64_t row_sees64(const AttnArgs& a, uint32_t have, uint32_t want, uint32_t row, uint32_t i, uint32_t t0)
 {
-    if (t < s.have) return true;
-    if (t >= s.want) return false;
-    const uint32_t j = t - s.have;
-    return a.mask ? (words[j >> 5] >> (j & 31)) & 1u : j <= i;
+    const uint32_t j0 = t0 > have ? t0 - have : 0u;            // first step token at or after t0
+    const uint32_t cached = t0 < have ? have - t0 : 0u;
+    if (cached >= 64u) return ~0ull;
+    uint64_t own;                                                      // bit b: step token j0 + b
+    if (a.mask) {
+        const uint32_t* words = a.mask + (uint64_t)row * a.mask_words;
+        const uint32_t k = j0 >> 5, sh = j0 & 31u;
+        const uint64_t lo = k < a.mask_words ? words[k] : 0u, mid = k + 1 < a.mask_words ? words[k + 1] : 0u;
+        const uint64_t hi = k + 2 < a.mask_words ? words[k + 2] : 0u;
+        own = ((lo | (mid << 32)) >> sh) | (sh ? hi << (64u - sh) : 0ull);
+    } else {
+        const uint32_t n = i >= j0 ? i - j0 + 1u : 0u;
+        own = n >= 64u ? ~0ull : (1ull << n) - 1ull;
+    }
+    uint64_t sees = (own << cached) | ((1ull << cached) - 1ull);
+    const uint32_t there = want - t0;                              // tokens from t0 to the end, > 0
+    if (there < 64u) sees &= (1ull << there) - 1ull;
+    return sees;
 }
 
 template <class T> __device__ __forceinline__ uint32_t pack2(float lo, float hi);

@@ -236,29 +236,6 @@ __device__ __noinline__ bool walk_next(TcWalk& w, const AttnArgs& a, uint32_t la
     return more;
 }
 
-// Which of the 64 tokens from t0 on row i of the step sees, as bits.
-__device__ __noinline__ uint64_t row_sees64(const AttnArgs& a, const TcWalk& w, uint32_t i, uint32_t t0)
-{
-    const uint32_t j0 = t0 > w.s.have ? t0 - w.s.have : 0u;            // first step token at or after t0
-    const uint32_t cached = t0 < w.s.have ? w.s.have - t0 : 0u;
-    if (cached >= 64u) return ~0ull;
-    uint64_t own;                                                      // bit b: step token j0 + b
-    if (a.mask) {
-        const uint32_t* words = a.mask + (uint64_t)(w.row0 + i) * a.mask_words;
-        const uint32_t k = j0 >> 5, sh = j0 & 31u;
-        const uint64_t lo = k < a.mask_words ? words[k] : 0u, mid = k + 1 < a.mask_words ? words[k + 1] : 0u;
-        const uint64_t hi = k + 2 < a.mask_words ? words[k + 2] : 0u;
-        own = ((lo | (mid << 32)) >> sh) | (sh ? hi << (64u - sh) : 0ull);
-    } else {
-        const uint32_t n = i >= j0 ? i - j0 + 1u : 0u;
-        own = n >= 64u ? ~0ull : (1ull << n) - 1ull;
-    }
-    uint64_t sees = (own << cached) | ((1ull << cached) - 1ull);
-    const uint32_t there = w.s.want - t0;                              // tokens from t0 to the end, > 0
-    if (there < 64u) sees &= (1ull << there) - 1ull;
-    return sees;
-}
-
 template <class T, int D>
 __global__ void __launch_bounds__(TC_THREADS, 2) attn_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensorMap map, const __grid_constant__ CUtensorMap q_map)
 {
@@ -512,7 +489,7 @@ __global__ void __launch_bounds__(TC_THREADS, 2) attn_tc_kernel(const __grid_con
                 const uint32_t t0 = (w.tb + j) * TC_TILE;
                 const bool mixed = t0 + TC_TILE > w.s.have;
                 uint64_t sees = ~0ull;
-                if (mixed) sees = there && !masked_short ? row_sees64(a, w, i, t0) : 0ull;
+                if (mixed) sees = there && !masked_short ? row_sees64(a, w.s.have, w.s.want, w.row0 + i, i, t0) : 0ull;
                 if (!warp_wait(&sh.s_full[n & 1u], (n >> 1) & 1u, dead)) { alive = false; break; }
                 bool odd = false;
                 if (mixed) {

@@ -492,7 +492,7 @@ int launch_few(gift_ctx* c, AttnArgs& a, cudaStream_t st)
     a.tile_rows = FEW_ROWS;
     a.by_tile_rows = fixed_div(a.tile_rows);
     a.least = 1;
-    a.extra = 1;
+    a.extra = 4;
     attn_few_kernel<T, D><<<a.n_slices, FEW_THREADS, smem, st>>>(a);
     c->launches++;
     attn_join_kernel<T, D, FEW_ROWS, FEW_TILE><<<a.n_slices - 1, JOIN_THREADS, 0, st>>>(a);

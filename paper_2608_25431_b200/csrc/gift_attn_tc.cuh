@@ -208,6 +208,32 @@ __device__ __forceinline__ void tc_st16(uint32_t addr, const uint32_t (&r)[16])
         ::"r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
           "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
 }
+// Two 32-bit elements at a time.
+__device__ __forceinline__ uint64_t pair2(float lo, float hi)
+{
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ void split2(uint64_t v, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c)
+{
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b)
+{
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
 // One column, waited for.
 __device__ __forceinline__ uint32_t tc_ld1(uint32_t addr)
 {
@@ -516,13 +542,17 @@ __global__ void __launch_bounds__(TC_THREADS, 2) attn_tc_kernel(const __grid_con
                         for (int c = 0; c < 32; c++)
                             if (!((uint32_t)(sees >> (32 * x)) >> c & 1u)) sc[x][c] = 0xFF800000u;      // minus infinity
                 }
+                // Instruction issue bounds this part (two softmax warps and the other roles share a
+                // scheduler; half of the exponentials as polynomials on the FMA pipe: 402 -> 459 us): three
+                // inputs to a maximum, two elements to an FMA or a sum.
                 float tops[4] = {NEG_INF, NEG_INF, NEG_INF, NEG_INF};
 #pragma unroll
                 for (int x = 0; x < 2; x++)
 #pragma unroll
-                    for (int c = 0; c < 32; c++) tops[c & 3] = fmaxf(tops[c & 3], __uint_as_float(sc[x][c]));
+                    for (int c = 0; c < 32; c += 2)
+                        tops[(c >> 1) & 3] = max3(tops[(c >> 1) & 3], __uint_as_float(sc[x][c]), __uint_as_float(sc[x][c + 1]));
                 // the scale is positive here (q's sign carries it), so the largest score stays the largest
-                const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])) * a.scale_log2;
+                const float top = max3(tops[0], tops[1], fmaxf(tops[2], tops[3])) * a.scale_log2;
                 const bool grow = top > m + 8.f;           // also when nothing has been seen yet
                 float alpha = 1.f;
                 if (grow) {
@@ -530,14 +560,19 @@ __global__ void __launch_bounds__(TC_THREADS, 2) attn_tc_kernel(const __grid_con
                     m = top;
                 }
                 const float minus = m == NEG_INF ? 0.f : -m;
-                float sums[4] = {0.f, 0.f, 0.f, 0.f};
+                const uint64_t scale2 = pair2(a.scale_log2, a.scale_log2), minus2 = pair2(minus, minus);
+                uint64_t sums[2] = {0ull, 0ull};
 #pragma unroll
                 for (int x = 0; x < 2; x++) {
 #pragma unroll
-                    for (int c = 0; c < 32; c++) {
-                        const float p = fast_exp2(fmaf(__uint_as_float(sc[x][c]), a.scale_log2, minus));
-                        sc[x][c] = __float_as_uint(p);
-                        sums[c & 3] += p;
+                    for (int c = 0; c < 32; c += 2) {
+                        float lo, hi;
+                        split2(fma2(pair2(__uint_as_float(sc[x][c]), __uint_as_float(sc[x][c + 1])), scale2, minus2), lo, hi);
+                        lo = fast_exp2(lo);
+                        hi = fast_exp2(hi);
+                        sc[x][c] = __float_as_uint(lo);
+                        sc[x][c + 1] = __float_as_uint(hi);
+                        sums[(c >> 1) & 1] = add2(sums[(c >> 1) & 1], pair2(lo, hi));
                     }
                     if (!odd) {
                         // P into the first 32 columns of its S
@@ -547,7 +582,11 @@ __global__ void __launch_bounds__(TC_THREADS, 2) attn_tc_kernel(const __grid_con
                         tc_st16(s_at + x * 16, pk);
                     }
                 }
-                l = l * alpha + ((sums[0] + sums[1]) + (sums[2] + sums[3]));
+                {
+                    float lo, hi;
+                    split2(add2(sums[0], sums[1]), lo, hi);
+                    l = l * alpha + (lo + hi);
+                }
                 const bool rescale = j > 0 && __any_sync(0xFFFFFFFFu, grow && there);
                 if ((rescale || odd) && n > 0) {
                     // Every product so far is in O (the one of tile n is not issued before p_full).  That

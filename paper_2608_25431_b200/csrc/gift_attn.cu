@@ -89,6 +89,7 @@ __global__ void __launch_bounds__(FEW_THREADS, 2) attn_few_kernel(const __grid_c
     __shared__ uint32_t s_bits;
 
     uint64_t total, slice;
+    join_may_start();
     if (!place_unit<FEW_THREADS>(a, blockIdx.x, FEW_TILE, blockIdx.x == 0, &place, &total, &slice)) return;
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t ring = (uint32_t)__cvta_generic_to_shared(smem) + warp * (FEW_STAGES * 2 * HALF);
@@ -390,6 +391,11 @@ __global__ void __launch_bounds__(FEW_THREADS, 2) attn_few_kernel(const __grid_c
 constexpr int JOIN_THREADS = 128;
 constexpr int JOIN_ROWS = 16;
 
+static_assert(FEW_TILE == TC_TILE, "one joining kernel for both");
+
+// Until the kernel before this one is complete and what it wrote can be seen.
+__device__ __forceinline__ void join_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
 template <class T, int D, int ROWS, int TILE>
 __global__ void __launch_bounds__(JOIN_THREADS) attn_join_kernel(const __grid_constant__ AttnArgs a)
 {
@@ -399,7 +405,9 @@ __global__ void __launch_bounds__(JOIN_THREADS) attn_join_kernel(const __grid_co
     __shared__ uint32_t s_bits;
     const uint32_t w = blockIdx.x + 1, row_lo = blockIdx.y * JOIN_ROWS, way = blockIdx.z;
     uint64_t total, slice;
-    if (!place_unit<JOIN_THREADS>(a, w, TILE, false, &place, &total, &slice)) return;
+    const bool some = place_unit<JOIN_THREADS>(a, w, TILE, false, &place, &total, &slice);
+    join_wait();                                       // also without work: what follows this kernel follows both
+    if (!some) return;
     const uint32_t r = place.at.r, row0 = place.at.row0;
     const ReqShape s = load_shape(a.b, r);
     const ItemShape it = item_shape(a, s, TILE);
@@ -471,6 +479,24 @@ __global__ void __launch_bounds__(JOIN_THREADS) attn_join_kernel(const __grid_co
     if (h == 0 && q0 == 0) write_request<JOIN_THREADS>(a, r, row0, it.rows_m, bits);
 }
 
+// The joining kernel may start while the attention kernel runs: its launch and its search for the
+// cut items, some 4 us, are hidden behind it, and it waits for the pieces itself.
+template <class T, int D, int ROWS>
+cudaError_t launch_join(const AttnArgs& a, cudaStream_t st)
+{
+    cudaLaunchConfig_t cfg;
+    memset(&cfg, 0, sizeof(cfg));
+    cfg.gridDim = dim3(a.n_slices - 1, ROWS / JOIN_ROWS, a.ways);
+    cfg.blockDim = dim3(JOIN_THREADS, 1, 1);
+    cfg.stream = st;
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, attn_join_kernel<T, D, ROWS, FEW_TILE>, a);
+}
+
 // A kernel's shared-memory limit, raised once per device: the call costs as much as a launch's half.
 template <auto KERNEL> cudaError_t allow_smem(int device, int bytes)
 {
@@ -495,9 +521,9 @@ int launch_few(gift_ctx* c, AttnArgs& a, cudaStream_t st)
     a.extra = 4;
     attn_few_kernel<T, D><<<a.n_slices, FEW_THREADS, smem, st>>>(a);
     c->launches++;
-    attn_join_kernel<T, D, FEW_ROWS, FEW_TILE><<<a.n_slices - 1, JOIN_THREADS, 0, st>>>(a);
-    c->launches++;
     CU_TRY(cudaGetLastError());
+    CU_TRY((launch_join<T, D, FEW_ROWS>(a, st)));
+    c->launches++;
     return GIFT_OK;
 }
 
@@ -576,9 +602,9 @@ int launch_many(gift_ctx* c, AttnArgs& a, uint64_t rows, cudaStream_t st)
     a.scale_log2 = fmaxf(fabsf(a.scale_log2), 1e-30f);
     attn_tc_kernel<T, D><<<a.n_slices * a.ways, TC_THREADS, smem, st>>>(a, map, q_map);
     c->launches++;
-    attn_join_kernel<T, D, TC_ROWS, TC_TILE><<<dim3(a.n_slices - 1, TC_ROWS / JOIN_ROWS, a.ways), JOIN_THREADS, 0, st>>>(a);
-    c->launches++;
     CU_TRY(cudaGetLastError());
+    CU_TRY((launch_join<T, D, TC_ROWS>(a, st)));
+    c->launches++;
     return GIFT_OK;
 }
 

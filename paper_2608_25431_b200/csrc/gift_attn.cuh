@@ -203,6 +203,9 @@ template <uint32_t TILE> struct Walk {
     __device__ __forceinline__ bool masked_short(const AttnArgs& a) const { return a.mask && it.rows_m > a.mask_words * 32u; }
 };
 
+// The kernel that joins this one's pieces may be launched.
+__device__ __forceinline__ void join_may_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
 __device__ __forceinline__ float fast_exp2(float x)
 {
     float y;

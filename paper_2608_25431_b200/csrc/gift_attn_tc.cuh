@@ -273,6 +273,7 @@ __global__ void __launch_bounds__(TC_THREADS, 2) attn_tc_kernel(const __grid_con
     __shared__ TcWalk walks[TC_THREADS / 32];
     using L = TcSmem<D>;
 
+    join_may_start();
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         for (int i = 0; i < TC_STAGES; i++) {

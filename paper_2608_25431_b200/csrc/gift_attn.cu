@@ -20,16 +20,19 @@ namespace {
 // few query rows per K/V head: warp-level products
 // ---------------------------------------------------------------------------
 //
-// With R query rows per K/V head the kernel does R operations per K/V byte, so up to some 32 rows
-// HBM bandwidth bounds it and the matrix instructions need only keep out of the way.  Every
-// warp works on its own 16 tokens of a 64-token tile, with a ring of 3 stages of K and V rows in
-// shared memory that only it fills and reads: no barrier inside a piece.  2 CTAs of 4 warps per
-// SM keep 128 to 192 KiB in flight.  The warps' maxima, sums and rows are joined at a piece's end.
+// With R query rows per K/V head the kernel does R operations per K/V byte, so up to 16 rows HBM
+// bandwidth bounds it and the matrix instructions need only keep out of the way.  Every warp
+// works on its own tokens of a tile (16 of 64, or 32 of 128 when a head is 64 wide, so that a
+// step moves 8 KiB either way), with a ring of 3 stages of K and V rows in shared memory that
+// only it fills and reads: no barrier inside a piece.  2 CTAs of 4 warps per SM keep up to 192 KiB
+// in flight.  The warps' maxima, sums and rows are joined at a piece's end.
 
 constexpr int FEW_WARPS = 4;
 constexpr int FEW_THREADS = FEW_WARPS * 32;
-constexpr int FEW_TILE = FEW_WARPS * 16;
 constexpr int FEW_ROWS = 16;
+constexpr int FEW_STAGES = 3;
+template <int D> constexpr int FEW_BLOCKS = 128 / D;                     // 16-token blocks of a warp's step
+template <int D> constexpr int FEW_TILE = FEW_WARPS * 16 * FEW_BLOCKS<D>;
 
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, uint32_t bytes)
 {
@@ -70,8 +73,8 @@ template <int D> __device__ __forceinline__ uint32_t tile_at(uint32_t base, uint
 }
 
 template <int D> struct FewSmem {
-    static constexpr int stages = 384 / D;                          // 96 KiB
-    static constexpr int ring = FEW_WARPS * stages * 16 * D * 2 * 2;
+    static constexpr int half = 16 * FEW_BLOCKS<D> * D * 2;              // bytes of a step's K (or V) rows
+    static constexpr int ring = FEW_WARPS * FEW_STAGES * 2 * half;
     static constexpr int join = FEW_WARPS * FEW_ROWS * D * 4;
     static constexpr int bytes = ring > join ? ring : join;
 };
@@ -79,10 +82,10 @@ template <int D> struct FewSmem {
 template <class T, int D>
 __global__ void __launch_bounds__(FEW_THREADS, 2) attn_few_kernel(const __grid_constant__ AttnArgs a)
 {
-    constexpr int ROWS = FEW_ROWS, MT = 1, FEW_STAGES = FewSmem<D>::stages;
+    constexpr int ROWS = FEW_ROWS, NB = FEW_BLOCKS<D>, TOK = 16 * NB, TILE = FEW_TILE<D>;
     constexpr int CH = D / 8;                      // 16-byte chunks of a K or V row
     constexpr int KS = D / 16;                     // k steps of the score product
-    constexpr uint32_t HALF = 16 * D * 2;          // bytes of 16 K (or V) rows
+    constexpr uint32_t HALF = FewSmem<D>::half;
     extern __shared__ __align__(128) char smem[];
     __shared__ PlaceShared place;
     __shared__ float2 s_ml[FEW_WARPS][ROWS];
@@ -90,11 +93,11 @@ __global__ void __launch_bounds__(FEW_THREADS, 2) attn_few_kernel(const __grid_c
 
     uint64_t total, slice;
     join_may_start();
-    if (!place_unit<FEW_THREADS>(a, blockIdx.x, FEW_TILE, blockIdx.x == 0, &place, &total, &slice)) return;
+    if (!place_unit<FEW_THREADS>(a, blockIdx.x, TILE, blockIdx.x == 0, &place, &total, &slice)) return;
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t ring = (uint32_t)__cvta_generic_to_shared(smem) + warp * (FEW_STAGES * 2 * HALF);
 
-    Walk<FEW_TILE> w;
+    Walk<TILE> w;
     w.start(a, place.at, 0, slice < total - slice * blockIdx.x ? slice : total - slice * blockIdx.x);
     while (w.next(a)) {
         const ReqShape& s = w.s;
@@ -104,75 +107,69 @@ __global__ void __launch_bounds__(FEW_THREADS, 2) attn_few_kernel(const __grid_c
         const uint32_t q0 = qt * ROWS;
         const int32_t owner = a.b.owner[r];
         const int32_t* table = a.b.table + (uint64_t)r * a.b.max_blocks;
-        uint32_t bits = w.masked_short(a) ? GIFT_ST_BAD_DESC : 0u;
+        const bool masked_short = w.masked_short(a);
+        uint32_t bits = masked_short ? GIFT_ST_BAD_DESC : 0u;
 
-        // this lane's query rows g and g + 8 of every 16-row tile
+        // this lane's query rows g and g + 8
         const uint32_t g = lane >> 2, c2 = (lane & 3) * 2;
-        uint32_t qf[MT][KS][4];
-        uint32_t row_i[MT][2];
+        uint32_t qf[KS][4];
+        uint32_t row_i[2];
 #pragma unroll
-        for (int mt = 0; mt < MT; mt++) {
+        for (int half = 0; half < 2; half++) {
+            const uint32_t rho = q0 + half * 8 + g;
+            const bool there = rho < all_q;
+            const uint32_t i = there ? a.by_group.quot(rho) : 0u, hq = h * a.group + (there ? rho - i * a.group : 0u);
+            row_i[half] = i;
+            const char* q = a.q + (uint64_t)(row0 + i) * a.q_row + (uint64_t)hq * a.q_head;
 #pragma unroll
-            for (int half = 0; half < 2; half++) {
-                const uint32_t rho = q0 + mt * 16 + half * 8 + g;
-                const bool there = rho < all_q;
-                const uint32_t i = there ? a.by_group.quot(rho) : 0u, hq = h * a.group + (there ? rho - i * a.group : 0u);
-                row_i[mt][half] = i;
-                const char* q = a.q + (uint64_t)(row0 + i) * a.q_row + (uint64_t)hq * a.q_head;
+            for (int ks = 0; ks < KS; ks++)
 #pragma unroll
-                for (int ks = 0; ks < KS; ks++)
-#pragma unroll
-                    for (int hi = 0; hi < 2; hi++)
-                        qf[mt][ks][hi * 2 + half] =
-                            there ? *reinterpret_cast<const uint32_t*>(q + (ks * 16 + hi * 8 + c2) * 2) : 0u;
-            }
+                for (int hi = 0; hi < 2; hi++)
+                    qf[ks][hi * 2 + half] = there ? *reinterpret_cast<const uint32_t*>(q + (ks * 16 + hi * 8 + c2) * 2) : 0u;
         }
-        float o[MT][D / 8][4];
-        float m[MT][2], l[MT][2];
+        float o[D / 8][4];
+        float m[2] = {NEG_INF, NEG_INF}, l[2] = {0.f, 0.f};
 #pragma unroll
-        for (int mt = 0; mt < MT; mt++) {
-            m[mt][0] = m[mt][1] = NEG_INF;
-            l[mt][0] = l[mt][1] = 0.f;
+        for (int n = 0; n < D / 8; n++)
 #pragma unroll
-            for (int n = 0; n < D / 8; n++)
-#pragma unroll
-                for (int e = 0; e < 4; e++) o[mt][n][e] = 0.f;
-        }
+            for (int e = 0; e < 4; e++) o[n][e] = 0.f;
 
-        // Lane l looks after token l % 16 of the warp's 16: its table entry is fetched one step
-        // ahead of the copies that need it, its label is looked at one step after.
-        const uint32_t my = lane & 15u;
+        // Lane x looks after token x % TOK of the warp's: its table entry is fetched one step ahead of
+        // the copies that need it, its label is judged one step after it was asked for.
+        const uint32_t my = lane % TOK;
         auto entry = [&](uint32_t step) -> int32_t {
-            const uint32_t t = (tb + step) * FEW_TILE + warp * 16 + my;
+            const uint32_t t = (tb + step) * TILE + warp * TOK + my;
             return step < n_tiles && t < s.want ? table[a.b.page.quot(t)] : -1;
         };
-        int32_t next = entry(0);
-        uint32_t label_bits = 0;
+        int32_t next = entry(0), label = GIFT_OWNER_PARAM;
         auto issue = [&](uint32_t step) {
             if (step < n_tiles) {
-                const uint32_t t = (tb + step) * FEW_TILE + warp * 16 + my;
+                const uint32_t t = (tb + step) * TILE + warp * TOK + my;
                 const int32_t page = next;
                 next = entry(step + 1);
-                bits |= label_bits;
-                label_bits = 0;
-                const bool valid = t < s.want, ok = valid && page >= 0 && (uint32_t)page < a.b.n_pages;
-                uint64_t src = 0;
-                if (ok) {
-                    src = ((uint64_t)(uint32_t)page * a.b.page_tokens + (t - a.b.page.quot(t) * a.b.page_tokens)) * a.token_bytes + (uint64_t)h * (D * 2);
-                    if (a.owner_map) label_bits = label_read_status(a.owner_map[page], owner);
-                } else if (valid) {
-                    bits |= GIFT_ST_BAD_DESC;
+                bits |= label_read_status(label, owner);
+                label = GIFT_OWNER_PARAM;
+                // the token's slot; rows past the context are filled with zeros: what memory holds there does not matter
+                uint32_t slot = 0xFFFFFFFFu;
+                if (t < s.want) {
+                    if ((uint32_t)page < a.b.n_pages) {
+                        slot = (uint32_t)page * a.b.page_tokens + (t - a.b.page.quot(t) * a.b.page_tokens);
+                        if (a.owner_map) label = a.owner_map[page];
+                    } else {
+                        bits |= GIFT_ST_BAD_DESC;
+                    }
                 }
-                const uint32_t base = ring + (step % FEW_STAGES) * (2 * HALF);
+                const uint32_t base = ring + (step % FEW_STAGES) * (2 * HALF), chunk = lane % CH;
+                const char* head = a.pages + (uint64_t)h * (D * 2) + chunk * 16;
+                const uint64_t to_v = (uint64_t)a.kv_heads * (D * 2);
 #pragma unroll
-                for (int i = 0; i < CH / 2; i++) {
-                    const uint32_t row = i * (32 / CH) + lane / CH, chunk = lane % CH;
-                    const uint64_t from = __shfl_sync(0xFFFFFFFFu, src, row);
-                    const uint32_t size = __shfl_sync(0xFFFFFFFFu, ok ? 16u : 0u, row);
-                    const char* p = a.pages + from + chunk * 16;
-                    // rows past the context are filled with zeros: what memory holds there does not matter
-                    cp_async16(tile_at<D>(base, row, chunk), p, size);
-                    cp_async16(tile_at<D>(base + HALF, row, chunk), size ? p + (uint64_t)a.kv_heads * (D * 2) : p, size);
+                for (int i = 0; i < CH * TOK / 32; i++) {
+                    const uint32_t row = i * (32 / CH) + lane / CH;
+                    const uint32_t from = __shfl_sync(0xFFFFFFFFu, slot, row);
+                    const bool there = from != 0xFFFFFFFFu;
+                    const char* p = there ? head + (uint64_t)from * a.token_bytes : head;
+                    cp_async16(tile_at<D>(base, row, chunk), p, there ? 16u : 0u);
+                    cp_async16(tile_at<D>(base + HALF, row, chunk), p + to_v, there ? 16u : 0u);
                 }
             }
             cp_commit();
@@ -186,77 +183,67 @@ __global__ void __launch_bounds__(FEW_THREADS, 2) attn_few_kernel(const __grid_c
             cp_wait<FEW_STAGES - 1>();
             __syncwarp();
             const uint32_t kb = ring + (step % FEW_STAGES) * (2 * HALF), vb = kb + HALF;
-            const uint32_t t0 = (tb + step) * FEW_TILE + warp * 16;
-            float sc[MT][2][4];
+            const uint32_t t0 = (tb + step) * TILE + warp * TOK;
+            float sc[2 * NB][4];
 #pragma unroll
-            for (int mt = 0; mt < MT; mt++)
+            for (int n = 0; n < 2 * NB; n++)
 #pragma unroll
-                for (int n = 0; n < 2; n++)
+                for (int e = 0; e < 4; e++) sc[n][e] = 0.f;
 #pragma unroll
-                    for (int e = 0; e < 4; e++) sc[mt][n][e] = 0.f;
+            for (int ks = 0; ks < KS; ks++)
 #pragma unroll
-            for (int ks = 0; ks < KS; ks++) {
-                uint32_t kf[4];
-                ldsm4(kf, tile_at<D>(kb, (lane >> 4) * 8 + (lane & 7), ks * 2 + ((lane >> 3) & 1)));
-#pragma unroll
-                for (int mt = 0; mt < MT; mt++) {
-                    mma16816<T>(sc[mt][0], qf[mt][ks], kf[0], kf[1]);
-                    mma16816<T>(sc[mt][1], qf[mt][ks], kf[2], kf[3]);
+                for (int k = 0; k < NB; k++) {
+                    uint32_t kf[4];
+                    ldsm4(kf, tile_at<D>(kb, k * 16 + (lane >> 4) * 8 + (lane & 7), ks * 2 + ((lane >> 3) & 1)));
+                    mma16816<T>(sc[2 * k], qf[ks], kf[0], kf[1]);
+                    mma16816<T>(sc[2 * k + 1], qf[ks], kf[2], kf[3]);
                 }
+#pragma unroll
+            for (int n = 0; n < 2 * NB; n++)
+#pragma unroll
+                for (int e = 0; e < 4; e++) sc[n][e] *= a.scale_log2;
+            const bool mixed = t0 + TOK > s.have;      // some rows may not see some of these tokens
+            uint32_t sees[2];                          // of the step's tokens, by row
+            if (mixed) {
+                const bool none = masked_short || t0 >= s.want;
+#pragma unroll
+                for (int half = 0; half < 2; half++)
+                    sees[half] = none ? 0u : (uint32_t)row_sees64(a, s.have, s.want, row0 + row_i[half], row_i[half], t0);
+#pragma unroll
+                for (int n = 0; n < 2 * NB; n++)
+#pragma unroll
+                    for (int e = 0; e < 4; e++)
+                        if (!(sees[e >> 1] >> (n * 8 + c2 + (e & 1)) & 1u)) sc[n][e] = NEG_INF;
             }
-            const bool mixed = t0 + 16 > s.have;       // some rows may not see some of these tokens
-            uint32_t pf[MT][4], sees[MT][2];           // of the 16 tokens, by row
+            float alpha[2];
 #pragma unroll
-            for (int mt = 0; mt < MT; mt++) {
+            for (int half = 0; half < 2; half++) {
+                float top = fmaxf(sc[0][half * 2], sc[0][half * 2 + 1]);
 #pragma unroll
-                for (int n = 0; n < 2; n++)
+                for (int n = 1; n < 2 * NB; n++) top = fmaxf(top, fmaxf(sc[n][half * 2], sc[n][half * 2 + 1]));
+                top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
+                top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
+                const float now = fmaxf(m[half], top);
+                const float use = now == NEG_INF ? 0.f : now;          // nothing seen yet: exp2(-inf - 0) = 0
+                alpha[half] = fast_exp2(m[half] - use);
+                m[half] = now;
+                float sum = 0.f;
 #pragma unroll
-                    for (int e = 0; e < 4; e++) sc[mt][n][e] *= a.scale_log2;
-                if (mixed) {
-                    const bool none = w.masked_short(a) || t0 >= s.want;
+                for (int n = 0; n < 2 * NB; n++)
 #pragma unroll
-                    for (int half = 0; half < 2; half++)
-                        sees[mt][half] = none ? 0u : (uint32_t)row_sees64(a, s.have, s.want, row0 + row_i[mt][half], row_i[mt][half], t0);
-#pragma unroll
-                    for (int n = 0; n < 2; n++)
-#pragma unroll
-                        for (int e = 0; e < 4; e++)
-                            if (!(sees[mt][e >> 1] >> (n * 8 + c2 + (e & 1)) & 1u)) sc[mt][n][e] = NEG_INF;
-                }
-                float alpha[2];
-#pragma unroll
-                for (int half = 0; half < 2; half++) {
-                    float top = fmaxf(fmaxf(sc[mt][0][half * 2], sc[mt][0][half * 2 + 1]), fmaxf(sc[mt][1][half * 2], sc[mt][1][half * 2 + 1]));
-                    top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
-                    top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
-                    const float now = fmaxf(m[mt][half], top);
-                    const float use = now == NEG_INF ? 0.f : now;      // nothing seen yet: exp2(-inf - 0) = 0
-                    alpha[half] = fast_exp2(m[mt][half] - use);
-                    m[mt][half] = now;
-                    float sum = 0.f;
-#pragma unroll
-                    for (int n = 0; n < 2; n++)
-#pragma unroll
-                        for (int e = 0; e < 2; e++) {
-                            const float p = fast_exp2(sc[mt][n][half * 2 + e] - use);
-                            sc[mt][n][half * 2 + e] = p;
-                            sum += p;
-                        }
-                    l[mt][half] = l[mt][half] * alpha[half] + sum;
-                }
-                if (__any_sync(0xFFFFFFFFu, alpha[0] != 1.f || alpha[1] != 1.f)) {
-#pragma unroll
-                    for (int n = 0; n < D / 8; n++) {
-                        o[mt][n][0] *= alpha[0]; o[mt][n][1] *= alpha[0];
-                        o[mt][n][2] *= alpha[1]; o[mt][n][3] *= alpha[1];
+                    for (int e = 0; e < 2; e++) {
+                        const float p = fast_exp2(sc[n][half * 2 + e] - use);
+                        sc[n][half * 2 + e] = p;
+                        sum += p;
                     }
+                l[half] = l[half] * alpha[half] + sum;
+            }
+            if (__any_sync(0xFFFFFFFFu, alpha[0] != 1.f || alpha[1] != 1.f)) {
+#pragma unroll
+                for (int n = 0; n < D / 8; n++) {
+                    o[n][0] *= alpha[0]; o[n][1] *= alpha[0];
+                    o[n][2] *= alpha[1]; o[n][3] *= alpha[1];
                 }
-                // p is rounded to the pool's type: the operands of one product have one type, and the
-                // rounding (2^-9 relative at most for bf16) is of the size of v's own
-                pf[mt][0] = pack2<T>(sc[mt][0][0], sc[mt][0][1]);
-                pf[mt][1] = pack2<T>(sc[mt][0][2], sc[mt][0][3]);
-                pf[mt][2] = pack2<T>(sc[mt][1][0], sc[mt][1][1]);
-                pf[mt][3] = pack2<T>(sc[mt][1][2], sc[mt][1][3]);
             }
             // 0 * inf is NaN: where a row may not see a token whose v is not finite, the product is
             // taken token by token, over what the row sees
@@ -264,7 +251,7 @@ __global__ void __launch_bounds__(FEW_THREADS, 2) attn_few_kernel(const __grid_c
             if (mixed) {
                 bool odd = false;
 #pragma unroll
-                for (int i = 0; i < CH / 2; i++) {
+                for (int i = 0; i < CH * TOK / 32; i++) {
                     uint4 x;
                     const uint32_t at = vb + (i * 32 + lane) * 16;
                     asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w) : "r"(at) : "memory");
@@ -273,67 +260,73 @@ __global__ void __launch_bounds__(FEW_THREADS, 2) attn_few_kernel(const __grid_c
                 plain = !__any_sync(0xFFFFFFFFu, odd);
             }
             if (plain) {
+                // p is rounded to the pool's type: the operands of one product have one type, and the
+                // rounding (2^-9 relative at most for bf16) is of the size of v's own
+                uint32_t pf[NB][4];
 #pragma unroll
-                for (int np = 0; np < D / 16; np++) {
-                    uint32_t vf[4];
-                    ldsm4t(vf, tile_at<D>(vb, ((lane >> 3) & 1) * 8 + (lane & 7), np * 2 + (lane >> 4)));
-#pragma unroll
-                    for (int mt = 0; mt < MT; mt++) {
-                        mma16816<T>(o[mt][np * 2], pf[mt], vf[0], vf[1]);
-                        mma16816<T>(o[mt][np * 2 + 1], pf[mt], vf[2], vf[3]);
-                    }
+                for (int k = 0; k < NB; k++) {
+                    pf[k][0] = pack2<T>(sc[2 * k][0], sc[2 * k][1]);
+                    pf[k][1] = pack2<T>(sc[2 * k][2], sc[2 * k][3]);
+                    pf[k][2] = pack2<T>(sc[2 * k + 1][0], sc[2 * k + 1][1]);
+                    pf[k][3] = pack2<T>(sc[2 * k + 1][2], sc[2 * k + 1][3]);
                 }
+#pragma unroll
+                for (int np = 0; np < D / 16; np++)
+#pragma unroll
+                    for (int k = 0; k < NB; k++) {
+                        uint32_t vf[4];
+                        ldsm4t(vf, tile_at<D>(vb, k * 16 + ((lane >> 3) & 1) * 8 + (lane & 7), np * 2 + (lane >> 4)));
+                        mma16816<T>(o[np * 2], pf[k], vf[0], vf[1]);
+                        mma16816<T>(o[np * 2 + 1], pf[k], vf[2], vf[3]);
+                    }
             } else {
 #pragma unroll
-                for (int mt = 0; mt < MT; mt++)
+                for (int n0 = 0; n0 < 2 * NB; n0++)
 #pragma unroll 1
-                    for (int t = 0; t < 16; t++) {
+                    for (int t = n0 * 8; t < n0 * 8 + 8; t++) {
 #pragma unroll
                         for (int half = 0; half < 2; half++) {
                             // token t's p of this lane's row: held by lane (t % 8) / 2 of the row's four
                             const int from = (lane & ~3) | ((t & 7) >> 1);
-                            const float p0 = __shfl_sync(0xFFFFFFFFu, t < 8 ? sc[mt][0][half * 2] : sc[mt][1][half * 2], from);
-                            const float p1 = __shfl_sync(0xFFFFFFFFu, t < 8 ? sc[mt][0][half * 2 + 1] : sc[mt][1][half * 2 + 1], from);
+                            const float p0 = __shfl_sync(0xFFFFFFFFu, sc[n0][half * 2], from);
+                            const float p1 = __shfl_sync(0xFFFFFFFFu, sc[n0][half * 2 + 1], from);
                             const float p = t & 1 ? p1 : p0;
-                            if (!(sees[mt][half] >> t & 1u)) continue;
+                            if (sees[half] >> t & 1u) {
 #pragma unroll
-                            for (int n = 0; n < D / 8; n++) {
-                                uint32_t x;
-                                asm volatile("ld.shared.u32 %0, [%1];" : "=r"(x) : "r"(tile_at<D>(vb, t, n) + c2 * 2) : "memory");
-                                const T* v = reinterpret_cast<const T*>(&x);
-                                o[mt][n][half * 2] += p * to_float<T>(v[0]);
-                                o[mt][n][half * 2 + 1] += p * to_float<T>(v[1]);
+                                for (int n = 0; n < D / 8; n++) {
+                                    uint32_t x;
+                                    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(x) : "r"(tile_at<D>(vb, t, n) + c2 * 2) : "memory");
+                                    const T* v = reinterpret_cast<const T*>(&x);
+                                    o[n][half * 2] += p * to_float<T>(v[0]);
+                                    o[n][half * 2 + 1] += p * to_float<T>(v[1]);
+                                }
                             }
+                            __syncwarp();
                         }
                     }
             }
             __syncwarp();                              // the stage may be filled again
         }
-        bits |= label_bits;
+        bits |= label_read_status(label, owner);
         cp_wait<0>();
 
         // Join the four warps' parts.
 #pragma unroll
-        for (int mt = 0; mt < MT; mt++)
-#pragma unroll
-            for (int half = 0; half < 2; half++) {
-                l[mt][half] += __shfl_xor_sync(0xFFFFFFFFu, l[mt][half], 1);
-                l[mt][half] += __shfl_xor_sync(0xFFFFFFFFu, l[mt][half], 2);
-                if ((lane & 3) == 0) s_ml[warp][mt * 16 + half * 8 + g] = make_float2(m[mt][half], l[mt][half]);
-            }
+        for (int half = 0; half < 2; half++) {
+            l[half] += __shfl_xor_sync(0xFFFFFFFFu, l[half], 1);
+            l[half] += __shfl_xor_sync(0xFFFFFFFFu, l[half], 2);
+            if ((lane & 3) == 0) s_ml[warp][half * 8 + g] = make_float2(m[half], l[half]);
+        }
         bits = __reduce_or_sync(0xFFFFFFFFu, bits);
         if (threadIdx.x == 0) s_bits = 0u;
         __syncthreads();                               // the ring is idle; s_ml is complete
         if (lane == 0 && bits) atomicOr(&s_bits, bits);
         float* join = reinterpret_cast<float*>(smem) + (uint32_t)warp * (ROWS * D);
 #pragma unroll
-        for (int mt = 0; mt < MT; mt++)
+        for (int n = 0; n < D / 8; n++)
 #pragma unroll
-            for (int n = 0; n < D / 8; n++)
-#pragma unroll
-                for (int half = 0; half < 2; half++)
-                    *reinterpret_cast<float2*>(join + (mt * 16 + half * 8 + g) * D + n * 8 + c2) =
-                        make_float2(o[mt][n][half * 2], o[mt][n][half * 2 + 1]);
+            for (int half = 0; half < 2; half++)
+                *reinterpret_cast<float2*>(join + (half * 8 + g) * D + n * 8 + c2) = make_float2(o[n][half * 2], o[n][half * 2 + 1]);
         __syncthreads();
         bits = s_bits;
         const bool whole = tb == 0 && n_tiles == it.tiles;
@@ -390,8 +383,6 @@ __global__ void __launch_bounds__(FEW_THREADS, 2) attn_few_kernel(const __grid_c
 // after the item that boundary w + 1 cuts, if no earlier boundary cuts it too.
 constexpr int JOIN_THREADS = 128;
 constexpr int JOIN_ROWS = 16;
-
-static_assert(FEW_TILE == TC_TILE, "one joining kernel for both");
 
 // Until the kernel before this one is complete and what it wrote can be seen.
 __device__ __forceinline__ void join_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
@@ -481,7 +472,7 @@ __global__ void __launch_bounds__(JOIN_THREADS) attn_join_kernel(const __grid_co
 
 // The joining kernel may start while the attention kernel runs: its launch and its search for the
 // cut items, some 4 us, are hidden behind it, and it waits for the pieces itself.
-template <class T, int D, int ROWS>
+template <class T, int D, int ROWS, int TILE>
 cudaError_t launch_join(const AttnArgs& a, cudaStream_t st)
 {
     cudaLaunchConfig_t cfg;
@@ -494,7 +485,7 @@ cudaError_t launch_join(const AttnArgs& a, cudaStream_t st)
     attr.val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, attn_join_kernel<T, D, ROWS, FEW_TILE>, a);
+    return cudaLaunchKernelEx(&cfg, attn_join_kernel<T, D, ROWS, TILE>, a);
 }
 
 // A kernel's shared-memory limit, raised once per device: the call costs as much as a launch's half.
@@ -522,7 +513,7 @@ int launch_few(gift_ctx* c, AttnArgs& a, cudaStream_t st)
     attn_few_kernel<T, D><<<a.n_slices, FEW_THREADS, smem, st>>>(a);
     c->launches++;
     CU_TRY(cudaGetLastError());
-    CU_TRY((launch_join<T, D, FEW_ROWS>(a, st)));
+    CU_TRY((launch_join<T, D, FEW_ROWS, FEW_TILE<D>>(a, st)));
     c->launches++;
     return GIFT_OK;
 }
@@ -603,7 +594,7 @@ int launch_many(gift_ctx* c, AttnArgs& a, uint64_t rows, cudaStream_t st)
     attn_tc_kernel<T, D><<<a.n_slices * a.ways, TC_THREADS, smem, st>>>(a, map, q_map);
     c->launches++;
     CU_TRY(cudaGetLastError());
-    CU_TRY((launch_join<T, D, TC_ROWS>(a, st)));
+    CU_TRY((launch_join<T, D, TC_ROWS, TC_TILE>(a, st)));
     c->launches++;
     return GIFT_OK;
 }

@@ -93,6 +93,7 @@ __global__ void __launch_bounds__(FEW_THREADS, 2) attn_few_kernel(const __grid_c
 
     uint64_t total, slice;
     join_may_start();
+    if (threadIdx.x == 0) a.part_head[blockIdx.x * 2u + 1u].pieces = 0u;
     if (!place_unit<FEW_THREADS>(a, blockIdx.x, TILE, blockIdx.x == 0, &place, &total, &slice)) return;
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t ring = (uint32_t)__cvta_generic_to_shared(smem) + warp * (FEW_STAGES * 2 * HALF);
@@ -329,8 +330,8 @@ __global__ void __launch_bounds__(FEW_THREADS, 2) attn_few_kernel(const __grid_c
                 *reinterpret_cast<float2*>(join + (half * 8 + g) * D + n * 8 + c2) = make_float2(o[n][half * 2], o[n][half * 2 + 1]);
         __syncthreads();
         bits = s_bits;
-        const bool whole = tb == 0 && n_tiles == it.tiles;
-        const uint32_t slot = blockIdx.x * 2u + (tb == 0 ? 1u : 0u);
+        const bool whole = w.whole();
+        const uint32_t slot = w.slot();
         const uint32_t nr = all_q - q0 < (uint32_t)ROWS ? all_q - q0 : (uint32_t)ROWS;
         for (uint32_t c = threadIdx.x; c < nr * (uint32_t)CH; c += FEW_THREADS) {
             const uint32_t row = c / CH, ch = c % CH;
@@ -373,52 +374,36 @@ __global__ void __launch_bounds__(FEW_THREADS, 2) attn_few_kernel(const __grid_c
         if (whole) {
             if (h == 0 && qt == 0) write_request<FEW_THREADS>(a, r, row0, it.rows_m, bits);
         } else if (threadIdx.x == 0) {
-            a.part_bits[slot] = bits;
+            w.write_head(a, bits, slice);
         }
         __syncthreads();                               // smem is free for the next piece
     }
 }
 
 // Joins the pieces of the items that a slice boundary cuts, 16 rows per CTA.  CTAs (w, *, way) look
-// after the item that boundary w + 1 cuts, if no earlier boundary cuts it too.
+// after the item that slice w leaves unfinished, if it begins there.
 constexpr int JOIN_THREADS = 128;
 constexpr int JOIN_ROWS = 16;
 
-// Until the kernel before this one is complete and what it wrote can be seen.
-__device__ __forceinline__ void join_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
-
-template <class T, int D, int ROWS, int TILE>
+template <class T, int D, int ROWS>
 __global__ void __launch_bounds__(JOIN_THREADS) attn_join_kernel(const __grid_constant__ AttnArgs a)
 {
     constexpr int CH = D / 8;
-    __shared__ PlaceShared place;
     __shared__ float2 s_top[JOIN_ROWS];
     __shared__ uint32_t s_bits;
-    const uint32_t w = blockIdx.x + 1, row_lo = blockIdx.y * JOIN_ROWS, way = blockIdx.z;
-    uint64_t total, slice;
-    const bool some = place_unit<JOIN_THREADS>(a, w, TILE, false, &place, &total, &slice);
-    join_wait();                                       // also without work: what follows this kernel follows both
-    if (!some) return;
-    const uint32_t r = place.at.r, row0 = place.at.row0;
-    const ReqShape s = load_shape(a.b, r);
-    const ItemShape it = item_shape(a, s, TILE);
-    const uint32_t item = place.at.k * a.ways + way, u = place.at.u;
-    if (item >= it.items) return;
-    // not cut here (the boundary lies before the item's first tile or behind it), or cut by an earlier boundary as well
-    if (u <= a.extra || (uint64_t)u > slice + a.extra) return;
-    const uint64_t end = slice * w - u + it.cost;      // one past the item's last unit
-    const uint32_t w_last = (uint32_t)((end - 1) / slice), pieces = w_last - w + 2;
-    const uint32_t h = item / it.nqt, qt = item - h * it.nqt, q0 = qt * a.tile_rows + row_lo;
-    const uint32_t all_q = it.rows_m * a.group;
-    const uint32_t in_tile = all_q - qt * a.tile_rows < a.tile_rows ? all_q - qt * a.tile_rows : a.tile_rows;
-    if (row_lo >= in_tile) return;
-    const uint32_t nr = in_tile - row_lo < (uint32_t)JOIN_ROWS ? in_tile - row_lo : (uint32_t)JOIN_ROWS;
-    // the item starts in slice w - 1 (its last piece) and goes on as the first piece of w, w + 1, ...
-    auto slot_of = [&](uint32_t p) -> uint64_t { return 2ull * ((w + p - 1) * a.ways + way) + (p == 0 ? 1 : 0); };
+    const uint32_t w = blockIdx.x, row_lo = blockIdx.y * JOIN_ROWS, way = blockIdx.z;
+    // until the attention kernel is complete and what it wrote can be seen
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const PartHead head = a.part_head[2u * (w * a.ways + way) + 1u];
+    if (head.pieces == 0 || row_lo >= head.nr) return;
+    const uint32_t pieces = head.pieces, r = head.r, row0 = head.row0, h = head.h, q0 = head.q0 + row_lo;
+    const uint32_t nr = head.nr - row_lo < (uint32_t)JOIN_ROWS ? head.nr - row_lo : (uint32_t)JOIN_ROWS;
+    // the item starts as slice w's last piece and goes on as the first piece of w + 1, w + 2, ...
+    auto slot_of = [&](uint32_t p) -> uint64_t { return 2ull * ((w + p) * a.ways + way) + (p == 0 ? 1 : 0); };
     if (threadIdx.x == 0) s_bits = 0u;
     __syncthreads();
     for (uint32_t p = threadIdx.x; p < pieces; p += JOIN_THREADS)
-        if (a.part_bits[slot_of(p)]) atomicOr(&s_bits, a.part_bits[slot_of(p)]);
+        if (a.part_head[slot_of(p)].bits) atomicOr(&s_bits, a.part_head[slot_of(p)].bits);
     // maxima and sums: 8 threads per row, pieces dealt among them
     {
         const uint32_t row = threadIdx.x >> 3, sub = threadIdx.x & 7u;
@@ -467,12 +452,12 @@ __global__ void __launch_bounds__(JOIN_THREADS) attn_join_kernel(const __grid_co
         *reinterpret_cast<uint4*>(a.out + (uint64_t)(row0 + i) * a.out_row + (uint64_t)hq * a.out_head + ch * 16) = v;
         if (a.lse && ch == 0) a.lse[(uint64_t)(row0 + i) * a.heads + hq] = none ? NEG_INF : (top + log2f(sum)) * 0.6931471805599453f;
     }
-    if (h == 0 && q0 == 0) write_request<JOIN_THREADS>(a, r, row0, it.rows_m, bits);
+    if (h == 0 && q0 == 0) write_request<JOIN_THREADS>(a, r, row0, head.rows_m, bits);
 }
 
-// The joining kernel may start while the attention kernel runs: its launch and its search for the
-// cut items, some 4 us, are hidden behind it, and it waits for the pieces itself.
-template <class T, int D, int ROWS, int TILE>
+// The joining kernel may start while the attention kernel runs: its launch is hidden behind it, and it
+// waits for the pieces itself.
+template <class T, int D, int ROWS>
 cudaError_t launch_join(const AttnArgs& a, cudaStream_t st)
 {
     cudaLaunchConfig_t cfg;
@@ -485,7 +470,7 @@ cudaError_t launch_join(const AttnArgs& a, cudaStream_t st)
     attr.val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, attn_join_kernel<T, D, ROWS, TILE>, a);
+    return cudaLaunchKernelEx(&cfg, attn_join_kernel<T, D, ROWS>, a);
 }
 
 // A kernel's shared-memory limit, raised once per device: the call costs as much as a launch's half.
@@ -513,7 +498,7 @@ int launch_few(gift_ctx* c, AttnArgs& a, cudaStream_t st)
     attn_few_kernel<T, D><<<a.n_slices, FEW_THREADS, smem, st>>>(a);
     c->launches++;
     CU_TRY(cudaGetLastError());
-    CU_TRY((launch_join<T, D, FEW_ROWS, FEW_TILE<D>>(a, st)));
+    CU_TRY((launch_join<T, D, FEW_ROWS>(a, st)));
     c->launches++;
     return GIFT_OK;
 }
@@ -594,7 +579,7 @@ int launch_many(gift_ctx* c, AttnArgs& a, uint64_t rows, cudaStream_t st)
     attn_tc_kernel<T, D><<<a.n_slices * a.ways, TC_THREADS, smem, st>>>(a, map, q_map);
     c->launches++;
     CU_TRY(cudaGetLastError());
-    CU_TRY((launch_join<T, D, TC_ROWS, TC_TILE>(a, st)));
+    CU_TRY((launch_join<T, D, TC_ROWS>(a, st)));
     c->launches++;
     return GIFT_OK;
 }
@@ -619,7 +604,7 @@ int scratch_ensure(gift_ctx* c)
 {
     if (c->d_attn) return GIFT_OK;
     const size_t parts = 4ull * c->num_sms;
-    CU_TRY(cudaMalloc(&c->d_attn, parts * (PART_ROWS * (PART_D * 4 + 8) + 4)));
+    CU_TRY(cudaMalloc(&c->d_attn, parts * (PART_ROWS * (PART_D * 4 + 8) + sizeof(PartHead))));
     return GIFT_OK;
 }
 
@@ -665,7 +650,7 @@ extern "C" int gift_kv_attention(gift_ctx* c, const gift_batch* batch, const gif
     char* p = static_cast<char*>(c->d_attn);
     a.part_o = reinterpret_cast<float*>(p);
     a.part_ml = reinterpret_cast<float2*>(p + parts * PART_ROWS * PART_D * 4);
-    a.part_bits = reinterpret_cast<uint32_t*>(p + parts * PART_ROWS * (PART_D * 4 + 8));
+    a.part_head = reinterpret_cast<PartHead*>(p + parts * PART_ROWS * (PART_D * 4 + 8));
     cudaStream_t st = (cudaStream_t)stream;
     if (pool->dtype == GIFT_BF16)
         return pool->head_dim == 128 ? launch_attn<__nv_bfloat16, 128>(c, a, st) : launch_attn<__nv_bfloat16, 64>(c, a, st);

@@ -26,6 +26,14 @@
 
 namespace gift {
 
+// What the joining kernel has to know of a piece.  The first piece of a cut item describes the item.
+struct PartHead {
+    uint32_t pieces;                 // of the item, this one included; 0: this slot is not a first piece
+    uint32_t bits;                   // status bits of the piece's pages
+    uint32_t r, row0, rows_m;        // request, its first row, its rows
+    uint32_t h, q0, nr;              // K/V head, the item's first query row and number of query rows
+};
+
 struct AttnArgs {
     BatchArgs b;
     const char* pages;
@@ -52,7 +60,7 @@ struct AttnArgs {
     uint32_t n_slices, ways;         // slices, and CTAs that share one
     float* part_o;                   // [2 CTAs][rows][D]
     float2* part_ml;                 // [2 CTAs][rows] running maximum, sum
-    uint32_t* part_bits;             // [2 CTAs] status bits of the piece's pages
+    PartHead* part_head;             // [2 CTAs]
 };
 
 constexpr float NEG_INF = -__builtin_huge_valf();
@@ -198,6 +206,23 @@ template <uint32_t TILE> struct Walk {
             return true;
         }
         return false;
+    }
+    // Whether the piece is the whole item, and the scratch slot of one that is not: a slice's last piece, if
+    // it starts an item, or its first one.
+    __device__ __forceinline__ bool whole() const { return tb == 0 && n_tiles == it.tiles; }
+    __device__ __forceinline__ uint32_t slot() const { return blockIdx.x * 2u + (tb == 0 ? 1u : 0u); }
+    // One thread, after a piece that is not whole: what the joining kernel needs.  The item goes on in the
+    // slices behind this one.
+    __device__ __forceinline__ void write_head(const AttnArgs& a, uint32_t bits, uint64_t slice) const
+    {
+        PartHead p;
+        const uint32_t rest = it.cost - u;
+        p.pieces = tb == 0 ? 1u + (uint32_t)((rest + slice - 1) / slice) : 0u;
+        p.bits = bits;
+        p.r = r; p.row0 = row0; p.rows_m = it.rows_m;
+        p.h = h; p.q0 = qt * a.tile_rows;
+        p.nr = all_q - p.q0 < a.tile_rows ? all_q - p.q0 : a.tile_rows;
+        a.part_head[slot()] = p;
     }
     // more step tokens than the mask has bits: the request is refused without looking at the mask
     __device__ __forceinline__ bool masked_short(const AttnArgs& a) const { return a.mask && it.rows_m > a.mask_words * 32u; }

@@ -274,6 +274,7 @@ __global__ void __launch_bounds__(TC_THREADS, 2) attn_tc_kernel(const __grid_con
     using L = TcSmem<D>;
 
     join_may_start();
+    if (threadIdx.x == 0) a.part_head[blockIdx.x * 2u + 1u].pieces = 0u;
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         for (int i = 0; i < TC_STAGES; i++) {
@@ -646,8 +647,8 @@ __global__ void __launch_bounds__(TC_THREADS, 2) attn_tc_kernel(const __grid_con
             if (alive) alive = warp_wait(&sh.o_done[(n - 1) & 1u], ((n - 1) >> 1) & 1u, dead);
             tc_after();
             uint32_t bits = alive ? *(volatile uint32_t*)&sh.bits[piece % TC_BITS_RING] : GIFT_ST_STALLED;
-            const bool whole = w.tb == 0 && w.n_tiles == w.it.tiles;
-            const uint32_t slot = blockIdx.x * 2u + (w.tb == 0 ? 1u : 0u);
+            const bool whole = w.whole();
+            const uint32_t slot = w.slot();
             const bool none = bits != 0u || l == 0.f;
             const float inv = none ? 0.f : 1.f / l;
             if (warp_there) {
@@ -695,7 +696,7 @@ __global__ void __launch_bounds__(TC_THREADS, 2) attn_tc_kernel(const __grid_con
             if (whole) {
                 if (w.h == 0 && w.qt == 0) write_request<128>(a, w.r, w.row0, w.it.rows_m, bits);
             } else if (row == 0) {
-                a.part_bits[slot] = bits;
+                w.write_head(a, bits, slice);
             }
             // the ring's entry is used again four pieces on: clear it once all four warps have read it
             asm volatile("barrier.cta.sync 1, 128;" ::: "memory");

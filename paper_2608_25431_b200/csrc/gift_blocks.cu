@@ -301,12 +301,18 @@ __global__ void __launch_bounds__(MAP_THREADS) kv_segments_kernel(const __grid_c
 {
     extern __shared__ uint32_t first[];
     __shared__ uint64_t warp_sums[MAP_THREADS / 32];
+    __shared__ uint64_t words[MAP_THREADS / 32][32 * 5];
     const uint64_t blocks = prefix_requests(a.b.n_req, first, warp_sums, [&](uint32_t r) { return n_export(a, load_shape(a.b, r)); });
     const bool fits = blocks <= a.cap && blocks * a.layers <= a.cap;
     const uint32_t n = fits ? (uint32_t)(blocks * a.layers) : 0u;
     if (a.total && blockIdx.x == 0 && threadIdx.x == 0)
         *a.total = blocks > 0x7FFFFFFFFFFFFFFFull / a.layers ? 0x7FFFFFFFFFFFFFFFll : (int64_t)(blocks * a.layers);
-    for (uint32_t e = blockIdx.x * MAP_THREADS + threadIdx.x; e < a.cap; e += gridDim.x * MAP_THREADS) {
+    // A lane makes a segment's five words; the warp writes its 32 segments as one run (each lane
+    // writing its own 40 bytes: 10.3 us for 262 000 segments, this way 8.3).
+    const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const uint32_t warps = gridDim.x * (MAP_THREADS / 32);
+    for (uint32_t e0 = (blockIdx.x * (MAP_THREADS / 32) + warp) * 32; e0 < a.cap; e0 += warps * 32) {
+        const uint32_t e = e0 + lane;
         // an entry behind the last segment has a reserved flag set: the segment calls refuse it
         uint64_t w0 = (uint32_t)GIFT_OWNER_NONE | ((uint64_t)1 << 32), len = 0, w3 = 0, w4 = (uint64_t)e << 32;
         int32_t entry = -1;
@@ -324,9 +330,14 @@ __global__ void __launch_bounds__(MAP_THREADS) kv_segments_kernel(const __grid_c
             const int32_t page = a.b.table[(uint64_t)r * a.b.max_blocks + blk];
             if (page >= 0 && (uint32_t)page < a.b.n_pages) entry = (int32_t)(layer * a.b.n_pages + (uint32_t)page);
         }
-        uint64_t* o = a.segs + (uint64_t)e * 5;
-        o[0] = w0; o[1] = 0; o[2] = len; o[3] = w3; o[4] = w4;
-        a.page_table[e] = entry;
+        uint64_t* mine = words[warp] + lane * 5;
+        mine[0] = w0; mine[1] = 0; mine[2] = len; mine[3] = w3; mine[4] = w4;
+        if (e < a.cap) a.page_table[e] = entry;
+        __syncwarp();
+        const uint32_t n_words = (a.cap - e0 < 32u ? a.cap - e0 : 32u) * 5;
+        uint64_t* o = a.segs + (uint64_t)e0 * 5;
+        for (uint32_t k = lane; k < n_words; k += 32) o[k] = words[warp][k];
+        __syncwarp();
     }
 }
 

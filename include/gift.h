@@ -560,7 +560,7 @@ typedef struct {
  * GIFT_ST_OWNER_MISMATCH (another user's or a parameter's page), GIFT_ST_UNOWNED (NONE or CONFLICT),
  * GIFT_ST_BAD_DESC (slot out of range); then nothing is written.  Slot -1 is a row that goes nowhere
  * (status 0).  The slots of a call must be distinct; if two rows name one slot, it receives
- * bytes of either. */
+ * bytes of either.  k and v must not overlap the pages. */
 int gift_kv_append(gift_ctx* ctx, const gift_kv_pool* pool, const void* k, uint64_t k_row_stride, uint64_t k_head_stride,
                    const void* v, uint64_t v_row_stride, uint64_t v_head_stride, uint32_t n_rows, const int64_t* slots,
                    const int32_t* row_owner, uint32_t* status, void* stream);

@@ -570,6 +570,8 @@ class Ctx:
             if tree_mask.dim() != 2 or tree_mask.shape[0] != n:
                 raise ValueError("tree_mask: expected shape [%d, mask_words], got %s" % (n, tuple(tree_mask.shape)))
             words = tree_mask.shape[1]
+            if words == 0:
+                raise ValueError("tree_mask has no words")
         a = _Attn(qp, qr, qh, op, orow, oh, n, heads, dim ** -0.5 if scale is None else scale,
                   _arr(tree_mask, d, "tree_mask", optional=True), words,
                   _arr(lse, d, "lse", "float32", n=n * heads, optional=True),

@@ -32,7 +32,10 @@ constexpr int TC_ROWS = 128;
 constexpr int TC_TILE = 64;
 constexpr int TC_THREADS = 256;
 constexpr int TC_STAGES = 2;
-constexpr int TC_BITS_RING = 4;      // the copies finish at most two pieces ahead of the softmax (see below)
+// Pieces whose page verdicts are kept: warp 4 is at most three pieces ahead of the softmax (Q of the fourth
+// waits for S of the third, that for P V of the first, that for the softmax), and a verdict is
+// cleared one piece after it was read.
+constexpr int TC_BITS_RING = 8;
 constexpr uint32_t TC_SPINS = 1u << 16, TC_SUSPEND_NS = 1000;        // a wait gives up after some 70 ms
 
 template <int D> struct TcSmem {
@@ -646,7 +649,11 @@ __global__ void __launch_bounds__(TC_THREADS, 2) attn_tc_kernel(const __grid_con
             // ---------------------------------------------------------- the piece's end
             if (alive) alive = warp_wait(&sh.o_done[(n - 1) & 1u], ((n - 1) >> 1) & 1u, dead);
             tc_after();
-            uint32_t bits = alive ? *(volatile uint32_t*)&sh.bits[piece % TC_BITS_RING] : GIFT_ST_STALLED;
+            // The four warps agree on how the piece ended; the verdict of the piece before, which all have
+            // read by now, makes room.
+            asm volatile("barrier.cta.sync 1, 128;" ::: "memory");
+            const uint32_t bits = *dead ? (uint32_t)GIFT_ST_STALLED : *(volatile uint32_t*)&sh.bits[piece % TC_BITS_RING];
+            if (row == 0) *(volatile uint32_t*)&sh.bits[(piece + TC_BITS_RING - 1) % TC_BITS_RING] = 0u;
             const bool whole = w.whole();
             const uint32_t slot = w.slot();
             const bool none = bits != 0u || l == 0.f;
@@ -698,9 +705,6 @@ __global__ void __launch_bounds__(TC_THREADS, 2) attn_tc_kernel(const __grid_con
             } else if (row == 0) {
                 w.write_head(a, bits, slice);
             }
-            // the ring's entry is used again four pieces on: clear it once all four warps have read it
-            asm volatile("barrier.cta.sync 1, 128;" ::: "memory");
-            if (row == 0) *(volatile uint32_t*)&sh.bits[piece % TC_BITS_RING] = 0u;
             tc_before();
             piece++;
         }

@@ -23,7 +23,8 @@ inline int pool_args_ok(const gift_kv_pool* p)
 inline int rows_args_ok(const void* p, uint64_t row_stride, uint64_t head_stride)
 {
     if (!p) return GIFT_E_INVAL;
-    if (row_stride > ((uint64_t)1 << 40) || head_stride > ((uint64_t)1 << 40)) return GIFT_E_RANGE;
+    // tensor maps take strides below 2^40 bytes
+    if (row_stride >= ((uint64_t)1 << 38) || head_stride >= ((uint64_t)1 << 38)) return GIFT_E_RANGE;
     if (((uintptr_t)p & 15) || row_stride % 8 != 0 || head_stride % 8 != 0) return GIFT_E_ALIGN;
     return GIFT_OK;
 }

@@ -94,7 +94,6 @@ def check(ctx, x, scale=None, labels=True, extra=0):
     assert np.array_equal(who[:n].cpu().numpy(), ref["row_owner"]) and (who[n:] == 7).all()
     got, gl = out.double().cpu().numpy(), lse.double().cpu().numpy()
     assert (got[n:] == 7).all() and (gl[n:] == 7).all()
-    ab = dict(x)
     mags = P.attention(x["owner"], x["have"], x["want"], x["table"], np.concatenate([pool[:, :, :1], np.abs(pool[:, :, 1:])], 2), q,
                        float(np.float32(sc)), x["mask"], x["label"] if labels else None)["out"]
     e = torch.finfo(x["q"].dtype).eps / 2
@@ -112,7 +111,6 @@ def check(ctx, x, scale=None, labels=True, extra=0):
         lsame = (gl[:n] == ref["lse"]) | (np.isnan(gl[:n]) & np.isnan(ref["lse"]))
         ltol = s + 2.0 ** -20 + tokens * 2.0 ** -24 + np.abs(ref["lse"]) * 2.0 ** -22
         assert (lsame | (loff <= ltol)).all(), np.nanmax(loff / ltol)
-    del ab
     return out, lse
 
 
@@ -138,6 +136,81 @@ def test_pages_of_any_size(ctx, dtype, pt):
 @pytest.mark.parametrize("tree", [True, False])
 def test_drafted_tokens_of_every_tile_size(ctx, dtype, dim, new, tree):
     check(ctx, make(3, dtype, [0, 40, 129], [new, max(1, new // 2), new], 2, 2, dim, 16, tree))
+
+
+@pytest.mark.parametrize("dtype,dim", [(BF, 128), (HF, 64)])
+@pytest.mark.parametrize("pt", [1, 2, 3, 8, 24, 32, 64, 100, 256])
+def test_pages_of_any_size_under_many_rows(ctx, dtype, dim, pt):
+    # runs of 8 to 64 tokens in one copy, shorter ones gathered
+    check(ctx, make(21, dtype, [0, 70, 300, 63], [40, 24, 33, 65], 2, 2, dim, pt))
+
+
+@pytest.mark.parametrize("heads,group,new", [(1, 3, 40), (3, 5, 40), (2, 7, 20), (1, 16, 16), (1, 100, 3), (2, 128, 2), (1, 160, 2), (3, 8, 33)])
+@pytest.mark.parametrize("dtype", [BF, HF])
+def test_groups_of_any_size_under_many_rows(ctx, dtype, heads, group, new):
+    # tiles of whole tokens (125 rows for groups of 5), several tiles per head, groups wider than a tile
+    check(ctx, make(22, dtype, [0, 200, 61], [new, 1, new], heads, group, 128 if group < 10 else 64, 16))
+
+
+@pytest.mark.parametrize("heads", [1, 3, 4])
+def test_tiles_of_query_rows_that_share_a_slice(ctx, heads):
+    # two CTAs walk one slice; an odd number of items leaves one without a partner
+    check(ctx, make(23, BF, [3000, 10, 700, 0], [70, 64, 3, 100], heads, 4, 128, 16), extra=3)
+
+
+@pytest.mark.parametrize("new,tree", [(150, True), (300, False), (129, True)])
+def test_more_step_tokens_than_a_tile_has_rows(ctx, new, tree):
+    check(ctx, make(24, BF, [0, 100], [new, 5], 1, 1, 64, 16, tree))
+
+
+def test_rows_of_q_that_share_memory(ctx):
+    x = make(25, BF, [50, 0], [30, 30], 1, 2, 128, 16)
+    x["q"] = x["q"][:1].expand(60, 2, 128)
+    check(ctx, x)
+    x = make(25, BF, [50, 0], [30, 30], 1, 4, 64, 16)
+    x["q"] = x["q"][:, :1].expand(60, 4, 64)
+    check(ctx, x)
+    x = make(25, BF, [50, 0], [30, 30], 2, 2, 64, 16)
+    x["q"] = x["q"].transpose(0, 1).contiguous().transpose(0, 1)          # heads outermost
+    check(ctx, x)
+
+
+@pytest.mark.parametrize("dtype,dim,group,new", [(BF, 128, 4, 20), (HF, 64, 8, 40)])
+def test_refusals_under_many_rows(ctx, dtype, dim, group, new):
+    x = make(26, dtype, [1500, 30, 2000, 5, 700], [new] * 5, 2, group, dim, 16)
+    x["label"][x["table"][0, 60]] = x["owner"][0] + 1
+    x["label"][x["table"][1, 0]] = P.CONFLICT
+    x["label"][x["table"][2, 3]] = P.PARAM
+    x["table"][3, 0] = -7
+    x["label"][x["table"][4, 44]], x["label"][x["table"][4, 2]] = P.NONE, x["owner"][4] + 1
+    out, _ = check(ctx, x)
+    assert not out[:2 * new].any() and out[2 * new: 3 * new].any()
+    check(ctx, x, labels=False)
+
+
+@pytest.mark.parametrize("new", [1, 20])
+def test_many_short_items_of_which_some_are_refused(ctx, new):
+    # a handful of one-tile items per CTA: each must get its own verdict
+    n = 400
+    x = make(28, BF, [r % 23 for r in range(n)], [new] * n, 4, 1, 64, 8)
+    for r in range(0, n, 3):
+        x["label"][x["table"][r, 0]] = P.CONFLICT if r % 2 else x["owner"][r] + 1
+    _, _ = check(ctx, x)
+
+
+def test_what_pages_hold_past_the_context_does_not_matter(ctx):
+    for pt in (8, 16, 64):
+        x = make(27, HF, [37, 5, 64, 100], [20] * 4, 2, 2, 128, pt)
+        want = call(ctx, x)
+        for r in range(4):
+            end = int(x["want"][r])
+            page = x["pool"][int(x["table"][r, end // pt])] if end % pt else None
+            if page is not None:
+                page[end % pt:] = float("nan")
+        got = call(ctx, x)
+        for a, b in zip(want[:3], got[:3]):
+            assert torch.equal(a, b)
+        check(ctx, x)
 
 
 @pytest.mark.parametrize("dtype,dim,group", [(BF, 128, 1), (HF, 128, 8), (BF, 64, 4)])
@@ -302,6 +375,8 @@ def test_wrong_tensors_are_refused(ctx):
         call(ctx, dict(x, q=x["q"].half()))
     with pytest.raises(ValueError):
         call(ctx, dict(x, mask=np.zeros((3, 1), np.uint32)))
+    with pytest.raises(ValueError):
+        call(ctx, dict(x, mask=np.zeros((2, 0), np.uint32)))
     with pytest.raises(ValueError):
         call(ctx, dict(x, pool=x["pool"].float(), q=x["q"].float()))
     with pytest.raises(binding.GiftError):

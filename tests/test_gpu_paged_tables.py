@@ -265,3 +265,17 @@ def test_appends_past_four_gib(ctx):
     ctx.kv_append(pool, k, -k, slots, None, st)
     got = pool[-4:].view(rows, 2, heads, dim)
     assert torch.equal(got[:, 0], k) and torch.equal(got[:, 1], -k) and not pool[:1].any()
+
+
+def test_entries_behind_the_last_segment_are_refused_by_the_cipher(ctx):
+    ctx.set_keys(np.arange(4, dtype=np.int32), np.arange(64, dtype=np.uint8))
+    b = binding.Batch(dev([1, 2]), dev([0, 0]), dev([3, 2]), dev([[1, 0], [3, -1]]), 2, 4)
+    segs, table = torch.zeros((6, 40), dtype=torch.uint8, device="cuda"), torch.zeros(6, dtype=torch.int32, device="cuda")
+    ctx.kv_segments(b, dev([7, 8]), segs, table, 1, 64)
+    buf = torch.arange(512, device="cuda").to(torch.uint8)
+    out = torch.zeros_like(buf)
+    tags, st = torch.ones((6, 16), dtype=torch.uint8, device="cuda"), torch.zeros(6, dtype=torch.int32, device="cuda")
+    ctx.seg_encrypt(buf, out, segs, 6, tags, st, page_table=table, page_bytes=128, owner_map=dev([1, 1, P.NONE, 2]), unit_bytes=128)
+    assert st.tolist() == [0, 0, 0] + [binding.ST_BAD_DESC] * 3 and not tags[3:].any()
+    assert not out[64:128].any() and not out[256:384].any()            # the part of a page that holds no token, an unused page
+    assert out[:64].any() and out[128:256].any() and out[384:].any()

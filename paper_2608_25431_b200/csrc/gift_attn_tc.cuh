@@ -1,17 +1,18 @@
 // Attention over the labelled paged cache, many query rows per K/V head: tcgen05 products.
 //
-// A tile of 128 query rows (or what whole tokens fit) meets tiles of 64 tokens.  S = Q K^T (128 x 64, 32-bit) lands in tensor
-// memory, one row per thread of four softmax warps; P, rounded to the pool's type, goes back
+// A tile of 128 query rows (or what whole tokens fit) meets tiles of 64 tokens.  S = Q K^T (128 x 64,
+// 32-bit) lands in tensor memory, one row per thread of four softmax warps; P, rounded to the pool's type, goes back
 // into the tensor-memory columns of its S and is the A operand of O += P V, whose accumulator
 // (128 x D) stays in tensor memory for the whole piece.  Roles, which meet on mbarriers alone:
 //   warps 0-3  softmax: thread = query row; running maximum and sum in registers
 //   warp 4     brings Q and the K tiles into swizzled shared memory, warp 5 the V tiles, by TMA.  What
 //              is contiguous in a page is a run of tokens: the largest power of two, up to a tile,
-//              that divides the page.  A run is one copy of 64 columns.  A TMA copy costs some 37
-//              clocks of the SM's one unit however little it brings, so pages whose runs are
-//              shorter than 8 tokens are gathered 4 tokens to a copy (measured: 875 us where runs
-//              of 16 take 547).  Rows outside the map read as zeros: that is where the runs past
-//              the context are sent.  Warp 4 also looks at the pages' labels.
+//              that divides the page.  A run of 8 or more is one copy of 64 columns; shorter ones are
+//              gathered, 4 tokens to a copy, which costs some 37 clocks of the SM's one TMA unit
+//              however little it brings (32 requests of 8192 tokens, 8 K/V heads, 128 rows each: 201
+//              us with pages of 16, 279 us with pages of 4).  Rows outside the map read as zeros:
+//              that is where the runs past the context are sent.  Warp 4 also looks at the pages'
+//              labels.
 //   warp 6     one thread issues Q K^T: tile j + 1's runs while the softmax of tile j does.
 //   warp 7     looks over the V tiles that hold step tokens (below), and one thread issues P V.  Two
 //              issuers, because what one thread spends on a tile (waits, descriptors, commits) was
@@ -19,6 +20,15 @@
 // O is rescaled only when a row's maximum has grown by more than 2^8 over the one in use: p is then at
 // most 2^8, which neither 16-bit type minds, and nearly all tiles leave O alone.
 // 2 CTAs per SM share its tensor memory (256 of 512 columns each) and hide each other's waits.
+//
+// What bounds it: with one tile of query rows per K/V head, HBM (24 drafted tokens of 32 heads over
+// contexts of 256 to 8192, 64 requests: 714 us, 6.3 TB/s; 32 requests as above: 201 us, 5.4 TB/s and 685
+// TFLOP/s); with several, the chain of a tile through softmax and products, some 1 900 clocks per
+// CTA, and under a long load the power cap, which takes the clock from 1965 to some 1250 MHz.  The
+// whole kernel is written small: items of a few tiles meet its cold parts at every end, and
+// fetching those past the instruction cache cost as much as the tiles (code of 105 KB: 505 us
+// where 66 KB take 442, contexts of 64 to 1024 tokens 261 and 169 us).
+// Eight softmax warps, two to a row's columns, were no faster (406 against 388 us).
 //
 // Every wait is bounded; a CTA whose wait runs out flags the rest of its slice (GIFT_ST_STALLED).
 #pragma once
@@ -39,7 +49,6 @@ constexpr int TC_BITS_RING = 8;
 constexpr uint32_t TC_SPINS = 1u << 16, TC_SUSPEND_NS = 1000;        // a wait gives up after some 70 ms
 
 template <int D> struct TcSmem {
-    static constexpr uint32_t half_rows(uint32_t rows) { return rows * 128u; }        // 64 elements of each row
     static constexpr uint32_t q = 0;                                                  // [D/64][128][64]
     static constexpr uint32_t k = TC_ROWS * D * 2;                                    // [stage][D/64][64][64]
     static constexpr uint32_t v = k + TC_STAGES * TC_TILE * D * 2;
@@ -547,9 +556,8 @@ __global__ void __launch_bounds__(TC_THREADS, 2) attn_tc_kernel(const __grid_con
                         for (int c = 0; c < 32; c++)
                             if (!((uint32_t)(sees >> (32 * x)) >> c & 1u)) sc[x][c] = 0xFF800000u;      // minus infinity
                 }
-                // Instruction issue bounds this part (two softmax warps and the other roles share a
-                // scheduler; half of the exponentials as polynomials on the FMA pipe: 402 -> 459 us): three
-                // inputs to a maximum, two elements to an FMA or a sum.
+                // Three inputs to a maximum, two elements to an FMA or a sum (short contexts 170 -> 148 us; half of
+                // the exponentials as polynomials on the FMA pipe instead: 402 -> 459 us).
                 float tops[4] = {NEG_INF, NEG_INF, NEG_INF, NEG_INF};
 #pragma unroll
                 for (int x = 0; x < 2; x++)

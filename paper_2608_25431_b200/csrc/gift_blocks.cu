@@ -27,7 +27,8 @@ namespace {
 // scattered accesses when many do.  2 to 32 threads share a page when there are threads to spare;
 // a thread has 8 layers' labels under way at once, and what it needs of the page's request lies in
 // shared memory.
-// (measured: see below)
+// 256 requests that take 16 pages in 32 layers: 12 us; 512 that take 4 000 and give back 700: 25 us (one
+// thread per page and layer, the lengths read again for each, 8 CTAs: 107 us).
 constexpr int BT_CTAS_PORTABLE = 8;
 constexpr int BT_CTAS_LARGE = 16;
 constexpr int BT_THREADS = 1024;

@@ -578,7 +578,7 @@ int launch_many(gift_ctx* c, AttnArgs& a, uint64_t rows, cudaStream_t st)
     // the kernel takes the maximum before it scales: the scale must be positive (0 becomes a factor that
     // makes every finite score 0 in effect, and keeps a hidden token's minus infinity what it is)
     a.negate = a.scale_log2 < 0.f ? 1u : 0u;
-    a.scale_log2 = fmaxf(fabsf(a.scale_log2), 1e-30f);
+    a.scale_log2 = fmaxf(fabsf(a.scale_log2), 1e-44f);
     attn_tc_kernel<T, D><<<a.n_slices * a.ways, TC_THREADS, smem, st>>>(a, map, q_map);
     c->launches++;
     CU_TRY(cudaGetLastError());

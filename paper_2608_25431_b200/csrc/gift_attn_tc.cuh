@@ -46,7 +46,7 @@ constexpr int TC_STAGES = 2;
 // waits for S of the third, that for P V of the first, that for the softmax), and a verdict is
 // cleared one piece after it was read.
 constexpr int TC_BITS_RING = 8;
-constexpr uint32_t TC_SPINS = 1u << 16, TC_SUSPEND_NS = 1000;        // a wait gives up after some 70 ms
+constexpr uint32_t TC_SPINS = 1u << 20, TC_SUSPEND_NS = 1000;        // a wait gives up after 50 ms to a second
 
 template <int D> struct TcSmem {
     static constexpr uint32_t q = 0;                                                  // [D/64][128][64]

@@ -75,6 +75,7 @@ extern "C" int gift_kv_append(gift_ctx* c, const gift_kv_pool* pool, const void*
     int rc = pool_args_ok(pool);
     if (rc != GIFT_OK) return rc;
     if (n_rows == 0) return GIFT_OK;
+    if (n_rows > 0x7FFFFFFFu) return GIFT_E_RANGE;
     if (!slots || !status || (pool->owner_map && !row_owner)) return GIFT_E_INVAL;
     if ((rc = rows_args_ok(k, k_row_stride, k_head_stride)) != GIFT_OK) return rc;
     if ((rc = rows_args_ok(v, v_row_stride, v_head_stride)) != GIFT_OK) return rc;

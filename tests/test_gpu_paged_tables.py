@@ -267,6 +267,16 @@ def test_appends_past_four_gib(ctx):
     assert torch.equal(got[:, 0], k) and torch.equal(got[:, 1], -k) and not pool[:1].any()
 
 
+def test_block_tables_without_a_stack(ctx):
+    # nothing free and no room: what needs nothing is left alone, what needs a page is told so
+    label = torch.full((1, 4), 1, dtype=torch.int32, device="cuda")
+    t, st = dev([[0, 1], [2, -1]]), torch.full((2,), 9, dtype=torch.int32, device="cuda")
+    n_free = torch.zeros(1, dtype=torch.int32, device="cuda")
+    b = binding.Batch(dev([1, 1]), dev([8, 4]), dev([8, 5]), t, 4, 4)
+    ctx.block_tables(b, torch.zeros(0, dtype=torch.int32, device="cuda"), n_free, label, st)
+    assert st.tolist() == [0, P.NO_BLOCKS] and t.tolist() == [[0, 1], [2, -1]] and (label == 1).all()
+
+
 def test_entries_behind_the_last_segment_are_refused_by_the_cipher(ctx):
     ctx.set_keys(np.arange(4, dtype=np.int32), np.arange(64, dtype=np.uint8))
     b = binding.Batch(dev([1, 2]), dev([0, 0]), dev([3, 2]), dev([[1, 0], [3, -1]]), 2, 4)

@@ -117,7 +117,8 @@ def test_append(lib, ctx):
         assert append(lib, ctx, p, **kw) == binding.E_INVAL
     for kw in (dict(k=PTR + 2), dict(v=PTR + 8), dict(ks=(1028, 128)), dict(vs=(1024, 100))):
         assert append(lib, ctx, p, **kw) == binding.E_ALIGN
-    assert append(lib, ctx, p, ks=(2 ** 41, 128)) == binding.E_RANGE
+    assert append(lib, ctx, p, ks=(2 ** 41, 128)) == append(lib, ctx, p, vs=(1024, 2 ** 38)) == binding.E_RANGE
+    assert append(lib, ctx, p, n=2 ** 31) == binding.E_RANGE
     assert append(lib, ctx, p, n=0) == binding.OK
 
 

@@ -358,7 +358,7 @@ int gift_block_tables(gift_ctx* c, const gift_batch* batch, int32_t* free_pages,
     if (!c) return GIFT_E_INVAL;
     const int rc = batch_args_ok(batch);
     if (rc != GIFT_OK || batch->n_req == 0) return rc;
-    if ((free_cap && !free_pages) || !n_free || !owner_map || !status || layers == 0) return GIFT_E_INVAL;
+    if ((free_cap && !free_pages) || !n_free || (batch->n_pages && !owner_map) || !status || layers == 0) return GIFT_E_INVAL;
     if (layers > GIFT_MAX_LAYERS || free_cap > 0x7FFFFFFFu) return GIFT_E_RANGE;
     DeviceGuard g(c->device);
     if (!g.ok) return GIFT_E_CUDA;

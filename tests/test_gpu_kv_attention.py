@@ -328,6 +328,30 @@ def test_the_same_call_gives_the_same_bits_and_streams_are_kept_apart(ctx):
         assert torch.equal(a, b)
 
 
+def test_two_contexts_on_two_streams_at_once(ctx):
+    # kernels of two calls that share SMs, tensor memory and L2; each context has its own scratch
+    other = binding.Ctx(4)
+    xs = [make(30, BF, [3000, 500, 40], [30, 40, 50], 2, 4, 128, 16), make(31, HF, [2500, 900, 0], [33, 20, 60], 4, 2, 64, 8)]
+    want = [call(c, x) for c, x in zip((ctx, other), xs)]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    bufs = []
+    for x in xs:
+        heads, dim = x["q"].shape[1:]
+        bufs.append(dict(b=binding.Batch(dev(x["owner"]), dev(x["have"]), dev(x["want"]), dev(x["table"]), x["pt"], x["pool"].shape[0]),
+                         mask=torch.from_numpy(x["mask"].view(np.int32)).cuda(), label=dev(x["label"]),
+                         out=torch.zeros((x["rows"], heads, dim), dtype=x["q"].dtype, device="cuda"),
+                         lse=torch.zeros((x["rows"], heads), device="cuda"), st=torch.full((3,), 9, dtype=torch.int32, device="cuda")))
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for c, x, s, d in zip((ctx, other), xs, streams, bufs):
+            c.kv_attention(d["b"], x["pool"], x["q"], d["out"], d["st"], tree_mask=d["mask"], lse=d["lse"], owner_map=d["label"],
+                           stream=s.cuda_stream)
+    torch.cuda.synchronize()
+    for w, d in zip(want, bufs):
+        assert torch.equal(w[0], d["out"]) and torch.equal(w[1], d["lse"]) and not d["st"].any()
+    other.close()
+
+
 def test_a_captured_call_follows_its_inputs(ctx):
     x = make(15, BF, [400, 20, 64], [6, 3, 9], 2, 2, 128, 16)
     want = call(ctx, x)
@@ -356,17 +380,28 @@ def test_a_captured_call_follows_its_inputs(ctx):
     assert torch.equal(out[:10], want[0][:10]) and torch.equal(lse[:10], want[1][:10])
 
 
-def test_a_cache_past_four_gib(ctx):
+@pytest.mark.parametrize("new,pt", [(2, 16), (20, 16), (20, 4)])
+def test_a_cache_past_four_gib(ctx, new, pt):
     # the request's pages are the pool's last ones: past 32-bit byte offsets
-    pt, heads, dim, pages = 16, 32, 128, 20480
+    heads, dim, pages = 32, 128, 20480 * 16 // pt
     pool = torch.empty((pages, pt, 2, heads, dim), dtype=BF, device="cuda")
-    x = make(16, BF, [50], [2], heads, 1, dim, pt)
+    x = make(16, BF, [50], [new], heads, 1, dim, pt)
     want, _, _, _ = call(ctx, x)
     n = int(x["table"].size)
     pool[pages - n:] = x["pool"][torch.from_numpy(x["table"][0]).long().cuda()]
     y = dict(x, pool=pool, table=np.arange(pages - n, pages, dtype=np.int32)[None], label=np.full(pages, x["owner"][0], np.int32))
     got, _, _, st = call(ctx, y)
     assert not st.any() and torch.equal(got, want)
+
+
+@pytest.mark.parametrize("n,new", [(8192, 1), (900, 18)])
+def test_as_many_requests_as_a_batch_holds(ctx, n, new):
+    rng = np.random.default_rng(n)
+    check(ctx, make(29, BF, rng.integers(0, 12, size=n), np.where(rng.random(n) < 0.1, 0, new), 1, 1, 64, 4))
+    if n == 8192:
+        x = make(29, BF, [1] * (n + 1), [1] * (n + 1), 1, 1, 64, 4)
+        with pytest.raises(binding.GiftError):
+            call(ctx, x)
 
 
 def test_wrong_tensors_are_refused(ctx):

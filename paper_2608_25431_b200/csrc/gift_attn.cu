@@ -17,6 +17,94 @@ using namespace gift;
 namespace {
 
 // ---------------------------------------------------------------------------
+// joining the pieces of cut items
+// ---------------------------------------------------------------------------
+
+constexpr int JOIN_THREADS = 128;
+constexpr int JOIN_ROWS = 16;
+
+struct JoinShared {
+    float2 top[JOIN_ROWS];
+    uint32_t bits;
+};
+
+// 16 rows from row_lo of the item that begins in slice w: the item is that slice's last piece and goes on
+// as the first piece of w + 1, w + 2, ...  Called by 128 threads.  LIVE: the pieces may have been written
+// while this kernel runs, and are read past L1.
+template <bool LIVE, class V> __device__ __forceinline__ V load_part(const V* p) { return LIVE ? __ldcg(p) : *p; }
+
+template <class T, int D, int ROWS, bool LIVE>
+__device__ __forceinline__ void join_rows(const AttnArgs& a, const PartHead& head, uint32_t w, uint32_t way, uint32_t row_lo, JoinShared* sh)
+{
+    constexpr int CH = D / 8;
+    const uint32_t pieces = head.pieces, r = head.r, row0 = head.row0, h = head.h, q0 = head.q0 + row_lo;
+    const uint32_t nr = head.nr - row_lo < (uint32_t)JOIN_ROWS ? head.nr - row_lo : (uint32_t)JOIN_ROWS;
+    auto slot_of = [&](uint32_t p) -> uint64_t { return 2ull * ((w + p) * a.ways + way) + (p == 0 ? 1 : 0); };
+    if (threadIdx.x == 0) sh->bits = 0u;
+    __syncthreads();
+    for (uint32_t p = threadIdx.x; p < pieces; p += JOIN_THREADS) {
+        const uint32_t bits = load_part<LIVE>(&a.part_head[slot_of(p)].bits);
+        if (bits) atomicOr(&sh->bits, bits);
+    }
+    // maxima and sums: 8 threads per row, pieces dealt among them
+    {
+        const uint32_t row = threadIdx.x >> 3, sub = threadIdx.x & 7u;
+        float top = NEG_INF, sum = 0.f;
+        if (row < nr)
+            for (uint32_t p = sub; p < pieces; p += 8) {
+                const float2 ml = load_part<LIVE>(&a.part_ml[slot_of(p) * ROWS + row_lo + row]);
+                const float now = fmaxf(top, ml.x), use = now == NEG_INF ? 0.f : now;
+                sum = sum * fast_exp2(top - use) + ml.y * fast_exp2(ml.x - use);
+                top = now;
+            }
+#pragma unroll
+        for (int d = 1; d < 8; d <<= 1) {
+            const float other_top = __shfl_xor_sync(0xFFFFFFFFu, top, d), other_sum = __shfl_xor_sync(0xFFFFFFFFu, sum, d);
+            const float now = fmaxf(top, other_top), use = now == NEG_INF ? 0.f : now;
+            sum = sum * fast_exp2(top - use) + other_sum * fast_exp2(other_top - use);
+            top = now;
+        }
+        if (row < nr && sub == 0) sh->top[row] = make_float2(top, sum);
+    }
+    __syncthreads();
+    const uint32_t bits = sh->bits;
+    for (uint32_t c = threadIdx.x; c < nr * (uint32_t)CH; c += JOIN_THREADS) {
+        const uint32_t row = c / CH, ch = c % CH;
+        const float top = sh->top[row].x, sum = sh->top[row].y, use = top == NEG_INF ? 0.f : top;
+        float acc[8];
+#pragma unroll
+        for (int e = 0; e < 8; e++) acc[e] = 0.f;
+#pragma unroll 4
+        for (uint32_t p = 0; p < pieces; p++) {
+            const uint64_t at = slot_of(p) * ROWS + row_lo + row;
+            const float f = fast_exp2(load_part<LIVE>(&a.part_ml[at]).x - use);
+            const float4* from = reinterpret_cast<const float4*>(a.part_o + at * D + ch * 8);
+            const float4 x = load_part<LIVE>(from), y = load_part<LIVE>(from + 1);
+            acc[0] += f * x.x; acc[1] += f * x.y; acc[2] += f * x.z; acc[3] += f * x.w;
+            acc[4] += f * y.x; acc[5] += f * y.y; acc[6] += f * y.z; acc[7] += f * y.w;
+        }
+        const uint32_t rho = q0 + row, i = a.by_group.quot(rho), hq = h * a.group + (rho - i * a.group);
+        const bool none = bits != 0u || sum == 0.f;
+        const float inv = none ? 0.f : 1.f / sum;
+        uint4 v = make_uint4(0u, 0u, 0u, 0u);
+        if (!none) {
+            v.x = pack2<T>(acc[0] * inv, acc[1] * inv); v.y = pack2<T>(acc[2] * inv, acc[3] * inv);
+            v.z = pack2<T>(acc[4] * inv, acc[5] * inv); v.w = pack2<T>(acc[6] * inv, acc[7] * inv);
+        }
+        *reinterpret_cast<uint4*>(a.out + (uint64_t)(row0 + i) * a.out_row + (uint64_t)hq * a.out_head + ch * 16) = v;
+        if (a.lse && ch == 0) a.lse[(uint64_t)(row0 + i) * a.heads + hq] = none ? NEG_INF : (top + log2f(sum)) * 0.6931471805599453f;
+    }
+    if (h == 0 && q0 == 0) write_request<JOIN_THREADS>(a, r, row0, head.rows_m, bits);
+}
+
+// The same from within the attention kernel, kept out of its loops' code.
+template <class T, int D, int ROWS>
+__device__ __noinline__ void join_here(const AttnArgs& a, const PartHead& head, uint32_t w, JoinShared* sh)
+{
+    join_rows<T, D, ROWS, true>(a, head, w, 0, 0, sh);
+}
+
+// ---------------------------------------------------------------------------
 // few query rows per K/V head: warp-level products
 // ---------------------------------------------------------------------------
 //
@@ -25,7 +113,9 @@ namespace {
 // works on its own tokens of a tile (16 of 64, or 32 of 128 when a head is 64 wide, so that a
 // step moves 8 KiB either way), with a ring of 3 stages of K and V rows in shared memory that
 // only it fills and reads: no barrier inside a piece.  2 CTAs of 4 warps per SM keep up to 192 KiB
-// in flight.  The warps' maxima, sums and rows are joined at a piece's end.  64 requests of 256 to 8192
+// in flight.  The warps' maxima, sums and rows are joined at a piece's end, the pieces of a cut item by
+// the CTA whose piece is ready last (a second kernel for that: 29.6 us a call of one token from Python,
+// this way 27.0; the device's time is the same).  64 requests of 256 to 8192
 // tokens, 32 heads: 16 rows 687 us (6.5 TB/s), 8 rows 678 us; one row over 256 to 2048 tokens 195 us
 // (6.2 TB/s).
 
@@ -91,17 +181,18 @@ __global__ void __launch_bounds__(FEW_THREADS, 2) attn_few_kernel(const __grid_c
     extern __shared__ __align__(128) char smem[];
     __shared__ PlaceShared place;
     __shared__ float2 s_ml[FEW_WARPS][ROWS];
-    __shared__ uint32_t s_bits;
+    __shared__ uint32_t s_bits, s_last, s_first;
+    __shared__ JoinShared s_join;
+    __shared__ PartHead s_head;
 
     uint64_t total, slice;
-    join_may_start();
-    if (threadIdx.x == 0) a.part_head[blockIdx.x * 2u + 1u].pieces = 0u;
     if (!place_unit<FEW_THREADS>(a, blockIdx.x, TILE, blockIdx.x == 0, &place, &total, &slice)) return;
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t ring = (uint32_t)__cvta_generic_to_shared(smem) + warp * (FEW_STAGES * 2 * HALF);
 
     Walk<TILE> w;
-    w.start(a, place.at, 0, slice < total - slice * blockIdx.x ? slice : total - slice * blockIdx.x);
+    const uint64_t begin = slice * blockIdx.x, units = slice < total - begin ? slice : total - begin;
+    w.start(a, place.at, 0, units);
     while (w.next(a)) {
         const ReqShape& s = w.s;
         const ItemShape& it = w.it;
@@ -375,8 +466,28 @@ __global__ void __launch_bounds__(FEW_THREADS, 2) attn_few_kernel(const __grid_c
         }
         if (whole) {
             if (h == 0 && qt == 0) write_request<FEW_THREADS>(a, r, row0, it.rows_m, bits);
-        } else if (threadIdx.x == 0) {
-            w.write_head(a, bits, slice);
+            __syncthreads();                           // smem is free for the next piece
+            continue;
+        }
+        // The last of an item's pieces to be ready joins them: every piece is in memory before its CTA takes a
+        // ticket, and whoever takes the last one puts the ticket back to 0 for the next call.
+        if (threadIdx.x == 0) a.part_head[slot].bits = bits;
+        __threadfence();
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            const uint64_t item = begin + (units - w.left) - w.u;      // the item's first unit
+            const uint32_t w0 = (uint32_t)((item + a.extra) / slice);  // the slice with its first tile
+            s_head.pieces = (uint32_t)((item + it.cost - 1) / slice) - w0 + 1u;
+            s_head.r = r; s_head.row0 = row0; s_head.rows_m = it.rows_m;
+            s_head.h = h; s_head.q0 = q0; s_head.nr = nr;
+            s_first = w0;
+            s_last = atomicAdd(&a.tickets[w0], 1u) + 1u == s_head.pieces;
+            if (s_last) a.tickets[w0] = 0u;
+        }
+        __syncthreads();
+        if (s_last) {
+            __threadfence();
+            join_here<T, D, ROWS>(a, s_head, s_first, &s_join);
         }
         __syncthreads();                               // smem is free for the next piece
     }
@@ -384,77 +495,16 @@ __global__ void __launch_bounds__(FEW_THREADS, 2) attn_few_kernel(const __grid_c
 
 // Joins the pieces of the items that a slice boundary cuts, 16 rows per CTA.  CTAs (w, *, way) look
 // after the item that slice w leaves unfinished, if it begins there.
-constexpr int JOIN_THREADS = 128;
-constexpr int JOIN_ROWS = 16;
-
 template <class T, int D, int ROWS>
 __global__ void __launch_bounds__(JOIN_THREADS) attn_join_kernel(const __grid_constant__ AttnArgs a)
 {
-    constexpr int CH = D / 8;
-    __shared__ float2 s_top[JOIN_ROWS];
-    __shared__ uint32_t s_bits;
+    __shared__ JoinShared sh;
     const uint32_t w = blockIdx.x, row_lo = blockIdx.y * JOIN_ROWS, way = blockIdx.z;
     // until the attention kernel is complete and what it wrote can be seen
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const PartHead head = a.part_head[2u * (w * a.ways + way) + 1u];
     if (head.pieces == 0 || row_lo >= head.nr) return;
-    const uint32_t pieces = head.pieces, r = head.r, row0 = head.row0, h = head.h, q0 = head.q0 + row_lo;
-    const uint32_t nr = head.nr - row_lo < (uint32_t)JOIN_ROWS ? head.nr - row_lo : (uint32_t)JOIN_ROWS;
-    // the item starts as slice w's last piece and goes on as the first piece of w + 1, w + 2, ...
-    auto slot_of = [&](uint32_t p) -> uint64_t { return 2ull * ((w + p) * a.ways + way) + (p == 0 ? 1 : 0); };
-    if (threadIdx.x == 0) s_bits = 0u;
-    __syncthreads();
-    for (uint32_t p = threadIdx.x; p < pieces; p += JOIN_THREADS)
-        if (a.part_head[slot_of(p)].bits) atomicOr(&s_bits, a.part_head[slot_of(p)].bits);
-    // maxima and sums: 8 threads per row, pieces dealt among them
-    {
-        const uint32_t row = threadIdx.x >> 3, sub = threadIdx.x & 7u;
-        float top = NEG_INF, sum = 0.f;
-        if (row < nr)
-            for (uint32_t p = sub; p < pieces; p += 8) {
-                const float2 ml = a.part_ml[slot_of(p) * ROWS + row_lo + row];
-                const float now = fmaxf(top, ml.x), use = now == NEG_INF ? 0.f : now;
-                sum = sum * fast_exp2(top - use) + ml.y * fast_exp2(ml.x - use);
-                top = now;
-            }
-#pragma unroll
-        for (int d = 1; d < 8; d <<= 1) {
-            const float other_top = __shfl_xor_sync(0xFFFFFFFFu, top, d), other_sum = __shfl_xor_sync(0xFFFFFFFFu, sum, d);
-            const float now = fmaxf(top, other_top), use = now == NEG_INF ? 0.f : now;
-            sum = sum * fast_exp2(top - use) + other_sum * fast_exp2(other_top - use);
-            top = now;
-        }
-        if (row < nr && sub == 0) s_top[row] = make_float2(top, sum);
-    }
-    __syncthreads();
-    const uint32_t bits = s_bits;
-    for (uint32_t c = threadIdx.x; c < nr * (uint32_t)CH; c += JOIN_THREADS) {
-        const uint32_t row = c / CH, ch = c % CH;
-        const float top = s_top[row].x, sum = s_top[row].y, use = top == NEG_INF ? 0.f : top;
-        float acc[8];
-#pragma unroll
-        for (int e = 0; e < 8; e++) acc[e] = 0.f;
-#pragma unroll 4
-        for (uint32_t p = 0; p < pieces; p++) {
-            const uint64_t at = slot_of(p) * ROWS + row_lo + row;
-            const float f = fast_exp2(a.part_ml[at].x - use);
-            const float4* from = reinterpret_cast<const float4*>(a.part_o + at * D + ch * 8);
-            const float4 x = from[0], y = from[1];
-            acc[0] += f * x.x; acc[1] += f * x.y; acc[2] += f * x.z; acc[3] += f * x.w;
-            acc[4] += f * y.x; acc[5] += f * y.y; acc[6] += f * y.z; acc[7] += f * y.w;
-        }
-        const uint32_t rho = q0 + row, i = a.by_group.quot(rho), hq = h * a.group + (rho - i * a.group);
-        const bool none = bits != 0u || sum == 0.f;
-        const float inv = none ? 0.f : 1.f / sum;
-        uint4 v = make_uint4(0u, 0u, 0u, 0u);
-        if (!none) {
-            v.x = pack2<T>(acc[0] * inv, acc[1] * inv); v.y = pack2<T>(acc[2] * inv, acc[3] * inv);
-            v.z = pack2<T>(acc[4] * inv, acc[5] * inv); v.w = pack2<T>(acc[6] * inv, acc[7] * inv);
-        }
-        *reinterpret_cast<uint4*>(a.out + (uint64_t)(row0 + i) * a.out_row + (uint64_t)hq * a.out_head + ch * 16) = v;
-        if (a.lse && ch == 0) a.lse[(uint64_t)(row0 + i) * a.heads + hq] = none ? NEG_INF : (top + log2f(sum)) * 0.6931471805599453f;
-    }
-    if (h == 0 && q0 == 0) write_request<JOIN_THREADS>(a, r, row0, head.rows_m, bits);
+    join_rows<T, D, ROWS, false>(a, head, w, way, row_lo, &sh);
 }
 
 // The joining kernel may start while the attention kernel runs: its launch is hidden behind it, and it
@@ -500,8 +550,6 @@ int launch_few(gift_ctx* c, AttnArgs& a, cudaStream_t st)
     attn_few_kernel<T, D><<<a.n_slices, FEW_THREADS, smem, st>>>(a);
     c->launches++;
     CU_TRY(cudaGetLastError());
-    CU_TRY((launch_join<T, D, FEW_ROWS>(a, st)));
-    c->launches++;
     return GIFT_OK;
 }
 
@@ -604,11 +652,20 @@ constexpr uint32_t PART_D = 128;
 
 // The scratch is allocated once, at a size that no call exceeds, and stays where it is until the
 // ctx is destroyed: a captured graph that names it stays valid.
-int scratch_ensure(gift_ctx* c)
+int scratch_ensure(gift_ctx* c, cudaStream_t st)
 {
     if (c->d_attn) return GIFT_OK;
     const size_t parts = 4ull * c->num_sms;
-    CU_TRY(cudaMalloc(&c->d_attn, parts * (PART_ROWS * (PART_D * 4 + 8) + sizeof(PartHead))));
+    const size_t before = parts * (PART_ROWS * (PART_D * 4 + 8) + sizeof(PartHead)), tickets = 2ull * c->num_sms * 4;
+    void* p = nullptr;
+    CU_TRY(cudaMalloc(&p, before + tickets));
+    const cudaError_t e = cudaMemsetAsync(static_cast<char*>(p) + before, 0, tickets, st);     // tickets are 0 between calls
+    if (e != cudaSuccess) {
+        gift_note_cuda_error(e, __FILE__, __LINE__);
+        cudaFree(p);
+        return GIFT_E_CUDA;
+    }
+    c->d_attn = p;
     return GIFT_OK;
 }
 
@@ -636,7 +693,8 @@ extern "C" int gift_kv_attention(gift_ctx* c, const gift_batch* batch, const gif
     }
     DeviceGuard g(c->device);
     if (!g.ok) return GIFT_E_CUDA;
-    if ((rc = scratch_ensure(c)) != GIFT_OK) return rc;
+    cudaStream_t st = (cudaStream_t)stream;
+    if ((rc = scratch_ensure(c, st)) != GIFT_OK) return rc;
     AttnArgs a;
     memset(&a, 0, sizeof(a));
     a.b = batch_args(batch);
@@ -655,7 +713,7 @@ extern "C" int gift_kv_attention(gift_ctx* c, const gift_batch* batch, const gif
     a.part_o = reinterpret_cast<float*>(p);
     a.part_ml = reinterpret_cast<float2*>(p + parts * PART_ROWS * PART_D * 4);
     a.part_head = reinterpret_cast<PartHead*>(p + parts * PART_ROWS * (PART_D * 4 + 8));
-    cudaStream_t st = (cudaStream_t)stream;
+    a.tickets = reinterpret_cast<uint32_t*>(p + parts * (PART_ROWS * (PART_D * 4 + 8) + sizeof(PartHead)));
     if (pool->dtype == GIFT_BF16)
         return pool->head_dim == 128 ? launch_attn<__nv_bfloat16, 128>(c, a, st) : launch_attn<__nv_bfloat16, 64>(c, a, st);
     return pool->head_dim == 128 ? launch_attn<__half, 128>(c, a, st) : launch_attn<__half, 64>(c, a, st);

@@ -9,7 +9,8 @@
 // tiles are laid end to end and cut into equal slices, one per resident CTA (the split the
 // cipher kernel uses).  A CTA walks its slice; an item that lies inside it is finished there, an
 // item that a slice boundary cuts leaves its pieces' maxima, sums and unnormalised rows in
-// scratch, and a second kernel joins them.  A slice has at most two such pieces (it enters one
+// scratch, to be joined: where the rows are few by the CTA whose piece is ready last, where they are
+// many (128 rows are 64 KiB a piece) by a second kernel.  A slice has at most two such pieces (it enters one
 // item in the middle and leaves one in the middle), so the scratch does not depend on the call.
 //
 // Where the rows of a K/V head fill several tiles, two CTAs walk one slice together (`ways` 2): its
@@ -61,6 +62,7 @@ struct AttnArgs {
     float* part_o;                   // [2 CTAs][rows][D]
     float2* part_ml;                 // [2 CTAs][rows] running maximum, sum
     PartHead* part_head;             // [2 CTAs]
+    uint32_t* tickets;               // [CTAs] few rows: pieces of the item that begins in a slice which are ready
 };
 
 constexpr float NEG_INF = -__builtin_huge_valf();

@@ -603,6 +603,13 @@ typedef struct {
 int gift_kv_attention(gift_ctx* ctx, const gift_batch* batch, const gift_kv_pool* pool, const gift_attn* attn,
                       uint32_t* status, void* stream);
 
+/* How long a wait inside gift_kv_attention (for a copy, a product, another warp) lasts before it gives up
+ * and the call ends with GIFT_ST_STALLED: about ns nanoseconds, at most GIFT_MAX_WAIT_NS; 0 is the default,
+ * some 50 ms to a second.  For the ctx's calls from now on; a captured graph keeps the limit of its
+ * capture.  For a caller that would rather have no result than a late one, and for tests of that path. */
+#define GIFT_MAX_WAIT_NS 1000000000ull
+int gift_ctx_wait_limit(gift_ctx* ctx, uint64_t ns);
+
 #ifdef __cplusplus
 }
 #endif

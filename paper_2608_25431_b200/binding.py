@@ -32,7 +32,7 @@ EXPORTS = [
     "gift_resolve_args", "gift_slice_runs", "gift_expand_owners", "gift_labels_swap_out", "gift_labels_swap_in",
     "gift_strerror", "gift_version", "gift_launch_count", "gift_timing_enable", "gift_timing_read",
     "gift_export_to_host", "gift_import_from_host", "gift_last_error_detail",
-    "gift_block_tables", "gift_slot_map", "gift_kv_segments", "gift_kv_append", "gift_kv_attention",
+    "gift_block_tables", "gift_slot_map", "gift_kv_segments", "gift_kv_append", "gift_kv_attention", "gift_ctx_wait_limit",
 ]
 
 
@@ -198,6 +198,7 @@ def lib():
         l.gift_slot_map.argtypes = [vp, C.POINTER(_Batch), vp, u32, vp, vp, vp, vp, vp, vp, vp]
         l.gift_kv_segments.argtypes = [vp, C.POINTER(_Batch), vp, u32, u64, u32, vp, vp, u32, vp, vp]
         l.gift_kv_append.argtypes = [vp, C.POINTER(_KvPool), vp, u64, u64, vp, u64, u64, u32, vp, vp, vp, vp]
+        l.gift_ctx_wait_limit.argtypes = [vp, u64]
         l.gift_kv_attention.argtypes = [vp, C.POINTER(_Batch), C.POINTER(_KvPool), C.POINTER(_Attn), vp, vp]
         _lib = l
     return _lib
@@ -579,6 +580,12 @@ class Ctx:
         _check(lib().gift_kv_attention(self._h, self._batch(batch), C.byref(pool), C.byref(a),
                                        _arr(status, d, "status", n=batch.n_req), self._stream(stream)), "gift_kv_attention")
 
+    def wait_limit(self, ns=0):
+        """gift_ctx_wait_limit: how long a wait inside kv_attention lasts before the call gives up; 0: the default."""
+        if not 0 <= ns < 1 << 64:
+            raise ValueError("ns: expected a number of nanoseconds, got %r" % (ns,))
+        _check(lib().gift_ctx_wait_limit(self._h, ns), "gift_ctx_wait_limit")
+
     @staticmethod
     def chunk_array(chunks):
         """HOST array of gift_chunk from (byte_lo, byte_hi, seg_lo, seg_hi) tuples or Chunk objects."""
@@ -761,6 +768,10 @@ def gift_kv_append(ctx: Ctx, *args, **kw):
 
 def gift_kv_attention(ctx: Ctx, *args, **kw):
     ctx.kv_attention(*args, **kw)
+
+
+def gift_ctx_wait_limit(ctx: Ctx, ns=0):
+    ctx.wait_limit(ns)
 
 
 def gift_last_error_detail() -> str:

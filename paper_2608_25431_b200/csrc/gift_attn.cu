@@ -626,6 +626,8 @@ int launch_many(gift_ctx* c, AttnArgs& a, uint64_t rows, cudaStream_t st)
     // the kernel takes the maximum before it scales: the scale must be positive (0 becomes a factor that
     // makes every finite score 0 in effect, and keeps a hidden token's minus infinity what it is)
     a.negate = a.scale_log2 < 0.f ? 1u : 0u;
+    a.wait_tries = c->attn_wait_ns ? (uint32_t)(c->attn_wait_ns / TC_SUSPEND_NS) : TC_WAIT_TRIES;
+    a.wait_ns = c->attn_wait_ns && c->attn_wait_ns < TC_SUSPEND_NS ? (uint32_t)c->attn_wait_ns : TC_SUSPEND_NS;
     a.scale_log2 = fmaxf(fabsf(a.scale_log2), 1e-44f);
     attn_tc_kernel<T, D><<<a.n_slices * a.ways, TC_THREADS, smem, st>>>(a, map, q_map);
     c->launches++;
@@ -670,6 +672,14 @@ int scratch_ensure(gift_ctx* c, cudaStream_t st)
 }
 
 }  // namespace
+
+extern "C" int gift_ctx_wait_limit(gift_ctx* c, uint64_t ns)
+{
+    if (!c) return GIFT_E_INVAL;
+    if (ns > GIFT_MAX_WAIT_NS) return GIFT_E_RANGE;
+    c->attn_wait_ns = ns;
+    return GIFT_OK;
+}
 
 extern "C" int gift_kv_attention(gift_ctx* c, const gift_batch* batch, const gift_kv_pool* pool, const gift_attn* t,
                                  uint32_t* status, void* stream)

@@ -59,6 +59,7 @@ struct AttnArgs {
     uint32_t least;                  // smallest slice, in tiles
     uint32_t extra;                  // tiles that an item costs beyond its own
     uint32_t n_slices, ways;         // slices, and CTAs that share one
+    uint32_t wait_tries, wait_ns;    // tcgen05 kernel: further attempts of a wait, and the longest single one
     float* part_o;                   // [2 CTAs][rows][D]
     float2* part_ml;                 // [2 CTAs][rows] running maximum, sum
     PartHead* part_head;             // [2 CTAs]

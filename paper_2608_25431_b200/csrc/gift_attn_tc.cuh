@@ -30,7 +30,9 @@
 // where 66 KB take 442, contexts of 64 to 1024 tokens 261 and 169 us).
 // Eight softmax warps, two to a row's columns, were no faster (406 against 388 us).
 //
-// Every wait is bounded; a CTA whose wait runs out flags the rest of its slice (GIFT_ST_STALLED).
+// Every wait is bounded (gift_ctx_wait_limit); a CTA whose wait runs out flags the rest of its slice
+// (GIFT_ST_STALLED).  It ends only when its own copies and products have: the warps that started them wait
+// for the last of them, with a limit of their own.
 #pragma once
 #include <cuda.h>
 
@@ -46,7 +48,9 @@ constexpr int TC_STAGES = 2;
 // waits for S of the third, that for P V of the first, that for the softmax), and a verdict is
 // cleared one piece after it was read.
 constexpr int TC_BITS_RING = 8;
-constexpr uint32_t TC_SPINS = 1u << 20, TC_SUSPEND_NS = 1000;        // a wait gives up after 50 ms to a second
+constexpr uint32_t TC_SUSPEND_NS = 1000;                             // longest single attempt of a wait
+constexpr uint32_t TC_WAIT_TRIES = 1u << 20;                         // attempts unless the ctx says otherwise: 50 ms to a second
+constexpr uint32_t TC_DRAIN_TRIES = 1u << 20;                        // of the waits for a CTA's own copies and products at its end
 
 template <int D> struct TcSmem {
     static constexpr uint32_t q = 0;                                                  // [D/64][128][64]
@@ -100,36 +104,42 @@ __device__ __forceinline__ void copy_run(uint32_t dst, const CUtensorMap* map, i
     asm volatile("cp.async.bulk.tensor.2d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
                  ::"r"(dst), "l"(map), "r"(x), "r"(row), "r"(smem_u32(b)) : "memory");
 }
-__device__ __forceinline__ bool bar_try(uint64_t* b, uint32_t parity)
+__device__ __forceinline__ bool bar_try(uint64_t* b, uint32_t parity, uint32_t ns)
 {
     uint32_t done;
     asm volatile(
         "{\n .reg .pred p;\n"
         " mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n"
         " selp.u32 %0, 1, 0, p;\n}"
-        : "=r"(done) : "r"(smem_u32(b)), "r"(parity), "r"(TC_SUSPEND_NS) : "memory");
+        : "=r"(done) : "r"(smem_u32(b)), "r"(parity), "r"(ns) : "memory");
     return done != 0u;
 }
 // Waits until the barrier's phase with this parity is complete; false when that takes too long, or
 // another role of the CTA has given up.
-__device__ __noinline__ bool bar_wait_long(uint64_t* b, uint32_t parity, volatile int* dead)
+__device__ __noinline__ bool bar_wait_long(uint64_t* b, uint32_t parity, volatile int* dead, const AttnArgs& a)
 {
 #pragma unroll 1
-    for (uint32_t i = 0; i < TC_SPINS; i++) {
-        if (bar_try(b, parity)) return true;
+    for (uint32_t i = 0; i < a.wait_tries; i++) {
+        if (bar_try(b, parity, a.wait_ns)) return true;
         if ((i & 255u) == 255u && *dead) return false;
     }
     *dead = 1;
     return false;
 }
-__device__ __forceinline__ bool bar_wait(uint64_t* b, uint32_t parity, volatile int* dead)
+__device__ __forceinline__ bool bar_wait(uint64_t* b, uint32_t parity, volatile int* dead, const AttnArgs& a)
 {
-    return bar_try(b, parity) || bar_wait_long(b, parity, dead);
+    return bar_try(b, parity, a.wait_ns) || bar_wait_long(b, parity, dead, a);
 }
 // The same for a whole warp, with one answer for all its lanes.
-__device__ __forceinline__ bool warp_wait(uint64_t* b, uint32_t parity, volatile int* dead)
+__device__ __forceinline__ bool warp_wait(uint64_t* b, uint32_t parity, volatile int* dead, const AttnArgs& a)
 {
-    return __all_sync(0xFFFFFFFFu, bar_wait(b, parity, dead));
+    return __all_sync(0xFFFFFFFFu, bar_wait(b, parity, dead, a));
+}
+// Waits for this CTA's own copies or products, which always end, whatever became of the other roles.
+__device__ __forceinline__ void bar_drain(uint64_t* b, uint32_t parity)
+{
+#pragma unroll 1
+    for (uint32_t i = 0; i < TC_DRAIN_TRIES && !bar_try(b, parity, TC_SUSPEND_NS); i++) {}
 }
 
 // Shared-memory operand descriptor, 128-byte swizzle: start, stride between 64-element column blocks
@@ -339,7 +349,7 @@ __global__ void __launch_bounds__(TC_THREADS, 2) attn_tc_kernel(const __grid_con
             if (kv == 0) {
                 // Q, once the products of the piece before have read the old rows.  What the box holds past
                 // the request's rows is another request's: rows that nobody asks for.
-                ok = piece == 0 || warp_wait(&sh.q_empty, (piece - 1) & 1u, dead);
+                ok = piece == 0 || warp_wait(&sh.q_empty, (piece - 1) & 1u, dead, a);
                 if (!ok) break;
                 q_loads++;
                 if (lane == 0) {
@@ -374,7 +384,7 @@ __global__ void __launch_bounds__(TC_THREADS, 2) attn_tc_kernel(const __grid_con
                 }
                 if (j == 0) continue;
                 const uint32_t stage = n % TC_STAGES, round = n / TC_STAGES;
-                ok = round == 0 || warp_wait(&empty[stage], (round - 1) & 1u, dead);
+                ok = round == 0 || warp_wait(&empty[stage], (round - 1) & 1u, dead, a);
                 if (!ok) break;
                 const uint32_t dst = sm + (kv ? L::v : L::k) + stage * (TC_TILE * D * 2) + col * (TC_TILE * 128) + first * 128;
                 if (gather) {
@@ -400,13 +410,10 @@ __global__ void __launch_bounds__(TC_THREADS, 2) attn_tc_kernel(const __grid_con
             }
             piece++;
         }
-        if (*dead) {
-            // nobody may be left to wait for the copies under way: they end before the CTA does
-            for (uint32_t k = n > TC_STAGES ? n - TC_STAGES : 0; k < n; k++)
-                for (uint32_t i = 0; i < TC_SPINS && !bar_try(&full[k % TC_STAGES], (k / TC_STAGES) & 1u); i++) {}
-            if (kv == 0 && q_loads > 0)
-                for (uint32_t i = 0; i < TC_SPINS && !bar_try(&sh.q_full, (q_loads - 1) & 1u); i++) {}
-        }
+        // The copies under way end before the CTA does, whether or not anybody is left to wait for them: one of
+        // the others may still give up after this warp has issued its last.
+        for (uint32_t k = n > TC_STAGES ? n - TC_STAGES : 0; k < n; k++) bar_drain(&full[k % TC_STAGES], (k / TC_STAGES) & 1u);
+        if (kv == 0 && q_loads > 0) bar_drain(&sh.q_full, (q_loads - 1) & 1u);
     } else if (warp == 6) {
         // ------------------------------------------------------------------ Q K^T
         // a negative scale: the products negate q, so that the scale used on the scores is positive
@@ -417,13 +424,13 @@ __global__ void __launch_bounds__(TC_THREADS, 2) attn_tc_kernel(const __grid_con
         while (ok && walk_next(w, a, lane)) {
             const uint32_t n_tiles = w.n_tiles;
             if (lane == 0) {
-                ok = bar_wait(&sh.q_full, piece & 1u, dead);
+                ok = bar_wait(&sh.q_full, piece & 1u, dead, a);
 #pragma unroll 1
                 for (uint32_t j = 0; ok && j < n_tiles; j++) {
                     const uint32_t t = n + j, stage = t % TC_STAGES;
                     // S takes the columns that held P of tile t - 2
-                    ok = bar_wait(&sh.k_full[stage], (t / TC_STAGES) & 1u, dead) &&
-                         (t < 2 || bar_wait(&sh.o_done[t & 1u], ((t - 2) >> 1) & 1u, dead));
+                    ok = bar_wait(&sh.k_full[stage], (t / TC_STAGES) & 1u, dead, a) &&
+                         (t < 2 || bar_wait(&sh.o_done[t & 1u], ((t - 2) >> 1) & 1u, dead, a));
                     if (!ok) break;
                     tc_after();
                     const uint64_t kb = k_desc + stage * (TC_TILE * D * 2 / 16);
@@ -444,7 +451,7 @@ __global__ void __launch_bounds__(TC_THREADS, 2) attn_tc_kernel(const __grid_con
         if (lane == 0) {
             // nothing may be in flight when the tensor memory is given back
             mma_commit(&sh.last);
-            for (uint32_t i = 0; i < TC_SPINS && !bar_try(&sh.last, 0); i++) {}
+            bar_drain(&sh.last, 0);
         }
         __syncwarp();
     } else if (warp == 7) {
@@ -461,7 +468,7 @@ __global__ void __launch_bounds__(TC_THREADS, 2) attn_tc_kernel(const __grid_con
 #pragma unroll 1
             for (uint32_t j = 0; j < w.n_tiles; j++, n++) {
                 const uint32_t stage = n % TC_STAGES, t0 = (w.tb + j) * TC_TILE;
-                ok = warp_wait(&sh.v_full[stage], (n / TC_STAGES) & 1u, dead);
+                ok = warp_wait(&sh.v_full[stage], (n / TC_STAGES) & 1u, dead, a);
                 if (!ok) break;
                 bool odd = false;
                 if (t0 + TC_TILE > w.s.have) {
@@ -487,7 +494,7 @@ __global__ void __launch_bounds__(TC_THREADS, 2) attn_tc_kernel(const __grid_con
                     }
                     __syncwarp();
                 }
-                ok = warp_wait(&sh.p_full[n & 1u], (n >> 1) & 1u, dead);
+                ok = warp_wait(&sh.p_full[n & 1u], (n >> 1) & 1u, dead, a);
                 if (!ok) break;
                 if (lane == 0) {
                     tc_after();
@@ -506,7 +513,7 @@ __global__ void __launch_bounds__(TC_THREADS, 2) attn_tc_kernel(const __grid_con
         }
         if (lane == 0) {
             mma_commit(&sh.last);
-            for (uint32_t i = 0; i < TC_SPINS && !bar_try(&sh.last, 0); i++) {}
+            bar_drain(&sh.last, 0);
         }
         __syncwarp();
     } else {
@@ -530,11 +537,11 @@ __global__ void __launch_bounds__(TC_THREADS, 2) attn_tc_kernel(const __grid_con
                 const bool mixed = t0 + TC_TILE > w.s.have;
                 uint64_t sees = ~0ull;
                 if (mixed) sees = there && !masked_short ? row_sees64(a, w.s.have, w.s.want, w.row0 + i, i, t0) : 0ull;
-                if (!warp_wait(&sh.s_full[n & 1u], (n >> 1) & 1u, dead)) { alive = false; break; }
+                if (!warp_wait(&sh.s_full[n & 1u], (n >> 1) & 1u, dead, a)) { alive = false; break; }
                 bool odd = false;
                 if (mixed) {
                     const uint32_t round = n & 1u ? checks1++ : checks0++;
-                    if (!warp_wait(&sh.checked[n & 1u], round & 1u, dead)) { alive = false; break; }
+                    if (!warp_wait(&sh.checked[n & 1u], round & 1u, dead, a)) { alive = false; break; }
                     odd = *(volatile int*)&sh.odd[n & 1u] != 0;
                 }
                 if (!warp_there) {                         // rows that do not exist: whatever P holds stays in them
@@ -605,7 +612,7 @@ __global__ void __launch_bounds__(TC_THREADS, 2) attn_tc_kernel(const __grid_con
                     // Every product so far is in O (the one of tile n is not issued before p_full).  That
                     // the barrier is no more than one phase behind follows from S of tile n - 1, whose
                     // product waited for tile n - 3's P V.
-                    if (!warp_wait(&sh.o_done[(n - 1) & 1u], ((n - 1) >> 1) & 1u, dead)) { alive = false; break; }
+                    if (!warp_wait(&sh.o_done[(n - 1) & 1u], ((n - 1) >> 1) & 1u, dead, a)) { tc_wait_st(); alive = false; break; }
                     tc_after();
                 }
                 if (odd) {
@@ -655,7 +662,7 @@ __global__ void __launch_bounds__(TC_THREADS, 2) attn_tc_kernel(const __grid_con
                 if (lane == 0) bar_arrive(&sh.p_full[n & 1u]);
             }
             // ---------------------------------------------------------- the piece's end
-            if (alive) alive = warp_wait(&sh.o_done[(n - 1) & 1u], ((n - 1) >> 1) & 1u, dead);
+            if (alive) alive = warp_wait(&sh.o_done[(n - 1) & 1u], ((n - 1) >> 1) & 1u, dead, a);
             tc_after();
             // The four warps agree on how the piece ended; the verdict of the piece before, which all have
             // read by now, makes room.

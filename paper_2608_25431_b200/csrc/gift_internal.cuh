@@ -64,6 +64,7 @@ struct gift_ctx {
     const uint8_t* aad;                // per-segment additional authenticated data bound to the next calls, or nullptr
     uint32_t aad_n;                    // entries of the bound array
     void* d_attn;                      // pieces of cut items of gift_kv_attention (fixed size, from its first call on)
+    uint64_t attn_wait_ns;             // limit of the waits inside gift_kv_attention; 0: the default
     uint64_t launches;
     int timing;                        // record events around the cipher kernel
     uint32_t n_timed;

@@ -580,8 +580,9 @@ int gift_kv_append(gift_ctx* ctx, const gift_kv_pool* pool, const void* k, uint6
  * that holds a token of the request must be its owner's or a parameter's (a shared prefix).
  * Else the request is refused: its rows are zero, lse minus infinity, row_owner
  * GIFT_OWNER_CONFLICT, and status[r] has GIFT_ST_OWNER_MISMATCH and / or GIFT_ST_UNOWNED, or GIFT_ST_BAD_DESC
- * alone (a page out of range, a malformed request, more step tokens than mask bits).  GIFT_ST_STALLED: a
- * bounded wait inside the kernel ran out (not seen so far); the request's rows are zero.  row_owner
+ * alone (a page out of range, a malformed request, more step tokens than mask bits).  GIFT_ST_STALLED
+ * alone: a bounded wait inside the kernel ran out (gift_ctx_wait_limit; not seen so far under the default
+ * limit) before all of the request's rows were done; it is answered like a refused one.  row_owner
  * and lse may be NULL.  If the step has more than n_rows rows, status is GIFT_ST_BAD_TABLE for every
  * request and nothing else is written.  Rows behind the last one are left as they were.
  * q, out: like k in gift_kv_append, in the pool's type; out must overlap no input.  head_dim is

@@ -493,6 +493,30 @@ __global__ void __launch_bounds__(FEW_THREADS, 2) attn_few_kernel(const __grid_c
     }
 }
 
+// What a wait that ran out leaves: a CTA knows of its own pieces only, so the requests that it could not
+// finish become zero here, when all of the rows' writers are done, by all CTAs of the joining kernel.
+template <int D>
+__device__ __noinline__ void clear_stalled(const AttnArgs& a)
+{
+    constexpr uint32_t CH = D / 8;
+    const uint32_t n_cta = gridDim.x * gridDim.y * gridDim.z;
+    const uint32_t cta = blockIdx.x + gridDim.x * (blockIdx.y + gridDim.y * blockIdx.z);
+#pragma unroll 1
+    for (uint32_t k = 0; k < a.n_slices * a.ways; k++) {
+        const uint4 s = a.part_stall[k];
+        for (uint32_t r = s.x + cta * JOIN_THREADS + threadIdx.x; r < s.y; r += n_cta * JOIN_THREADS)
+            if (load_shape(a.b, r).rows) a.status[r] = GIFT_ST_STALLED;
+        for (uint32_t t = s.z + cta; t < s.w; t += n_cta) {
+            for (uint32_t c = threadIdx.x; c < a.heads * CH; c += JOIN_THREADS) {
+                const uint32_t hq = c / CH, ch = c % CH;
+                *reinterpret_cast<uint4*>(a.out + (uint64_t)t * a.out_row + (uint64_t)hq * a.out_head + ch * 16) = make_uint4(0u, 0u, 0u, 0u);
+                if (a.lse && ch == 0) a.lse[(uint64_t)t * a.heads + hq] = NEG_INF;
+            }
+            if (a.row_owner && threadIdx.x == 0) a.row_owner[t] = GIFT_OWNER_CONFLICT;
+        }
+    }
+}
+
 // Joins the pieces of the items that a slice boundary cuts, 16 rows per CTA.  CTAs (w, *, way) look
 // after the item that slice w leaves unfinished, if it begins there.
 template <class T, int D, int ROWS>
@@ -503,6 +527,16 @@ __global__ void __launch_bounds__(JOIN_THREADS) attn_join_kernel(const __grid_co
     // until the attention kernel is complete and what it wrote can be seen
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const PartHead head = a.part_head[2u * (w * a.ways + way) + 1u];
+    bool any = false, mine = false;
+    for (uint32_t k = threadIdx.x; k < a.n_slices * a.ways; k += JOIN_THREADS) {
+        const uint4 s = a.part_stall[k];
+        any = any || s.y != 0u;
+        mine = mine || (head.r >= s.x && head.r < s.y);
+    }
+    if (__syncthreads_or(any)) {
+        clear_stalled<D>(a);
+        if (__syncthreads_or(mine)) return;
+    }
     if (head.pieces == 0 || row_lo >= head.nr) return;
     join_rows<T, D, ROWS, false>(a, head, w, way, row_lo, &sh);
 }
@@ -658,7 +692,8 @@ int scratch_ensure(gift_ctx* c, cudaStream_t st)
 {
     if (c->d_attn) return GIFT_OK;
     const size_t parts = 4ull * c->num_sms;
-    const size_t before = parts * (PART_ROWS * (PART_D * 4 + 8) + sizeof(PartHead)), tickets = 2ull * c->num_sms * 4;
+    const size_t before = parts * (PART_ROWS * (PART_D * 4 + 8) + sizeof(PartHead)) + 2ull * c->num_sms * sizeof(uint4);
+    const size_t tickets = 2ull * c->num_sms * 4;
     void* p = nullptr;
     CU_TRY(cudaMalloc(&p, before + tickets));
     const cudaError_t e = cudaMemsetAsync(static_cast<char*>(p) + before, 0, tickets, st);     // tickets are 0 between calls
@@ -723,7 +758,8 @@ extern "C" int gift_kv_attention(gift_ctx* c, const gift_batch* batch, const gif
     a.part_o = reinterpret_cast<float*>(p);
     a.part_ml = reinterpret_cast<float2*>(p + parts * PART_ROWS * PART_D * 4);
     a.part_head = reinterpret_cast<PartHead*>(p + parts * PART_ROWS * (PART_D * 4 + 8));
-    a.tickets = reinterpret_cast<uint32_t*>(p + parts * (PART_ROWS * (PART_D * 4 + 8) + sizeof(PartHead)));
+    a.part_stall = reinterpret_cast<uint4*>(a.part_head + parts);
+    a.tickets = reinterpret_cast<uint32_t*>(a.part_stall + 2ull * c->num_sms);
     if (pool->dtype == GIFT_BF16)
         return pool->head_dim == 128 ? launch_attn<__nv_bfloat16, 128>(c, a, st) : launch_attn<__nv_bfloat16, 64>(c, a, st);
     return pool->head_dim == 128 ? launch_attn<__half, 128>(c, a, st) : launch_attn<__half, 64>(c, a, st);

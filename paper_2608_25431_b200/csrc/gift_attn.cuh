@@ -63,6 +63,7 @@ struct AttnArgs {
     float* part_o;                   // [2 CTAs][rows][D]
     float2* part_ml;                 // [2 CTAs][rows] running maximum, sum
     PartHead* part_head;             // [2 CTAs]
+    uint4* part_stall;               // [CTAs] many rows: requests x .. y - 1, which have rows z .. w - 1, were not all done
     uint32_t* tickets;               // [CTAs] few rows: pieces of the item that begins in a slice which are ready
 };
 
@@ -226,6 +227,15 @@ template <uint32_t TILE> struct Walk {
         p.h = h; p.q0 = qt * a.tile_rows;
         p.nr = all_q - p.q0 < a.tile_rows ? all_q - p.q0 : a.tile_rows;
         a.part_head[slot()] = p;
+    }
+    // One thread, after a piece that could not be done: nor will any behind it in the slice.
+    __device__ __forceinline__ void note_stall(const AttnArgs& a) const
+    {
+        uint4 s = a.part_stall[blockIdx.x];
+        if (s.y == 0u) { s.x = r; s.z = row0; }
+        s.y = r + 1u;
+        s.w = row0 + it.rows_m;
+        a.part_stall[blockIdx.x] = s;
     }
     // more step tokens than the mask has bits: the request is refused without looking at the mask
     __device__ __forceinline__ bool masked_short(const AttnArgs& a) const { return a.mask && it.rows_m > a.mask_words * 32u; }

@@ -30,8 +30,9 @@
 // where 66 KB take 442, contexts of 64 to 1024 tokens 261 and 169 us).
 // Eight softmax warps, two to a row's columns, were no faster (406 against 388 us).
 //
-// Every wait is bounded (gift_ctx_wait_limit); a CTA whose wait runs out flags the rest of its slice
-// (GIFT_ST_STALLED).  It ends only when its own copies and products have: the warps that started them wait
+// Every wait is bounded (gift_ctx_wait_limit).  A CTA whose wait runs out leaves the rest of its slice undone and
+// notes which requests that concerns (part_stall): the joining kernel makes all their rows zero, those of
+// other CTAs too, and their status GIFT_ST_STALLED.  It ends only when its own copies and products have: the warps that started them wait
 // for the last of them, with a limit of their own.
 #pragma once
 #include <cuda.h>
@@ -134,6 +135,14 @@ __device__ __forceinline__ bool bar_wait(uint64_t* b, uint32_t parity, volatile 
 __device__ __forceinline__ bool warp_wait(uint64_t* b, uint32_t parity, volatile int* dead, const AttnArgs& a)
 {
     return __all_sync(0xFFFFFFFFu, bar_wait(b, parity, dead, a));
+}
+// Whether any of the four softmax warps says so, for all of their threads alike.
+__device__ __forceinline__ bool any_softmax(bool x)
+{
+    uint32_t r;
+    asm volatile("{\n .reg .pred p, q;\n setp.ne.u32 p, %1, 0;\n barrier.cta.red.or.pred q, 1, 128, p;\n selp.u32 %0, 1, 0, q;\n}"
+                 : "=r"(r) : "r"((uint32_t)x) : "memory");
+    return r != 0u;
 }
 // Waits for this CTA's own copies or products, which always end, whatever became of the other roles.
 __device__ __forceinline__ void bar_drain(uint64_t* b, uint32_t parity)
@@ -296,7 +305,10 @@ __global__ void __launch_bounds__(TC_THREADS, 2) attn_tc_kernel(const __grid_con
     using L = TcSmem<D>;
 
     join_may_start();
-    if (threadIdx.x == 0) a.part_head[blockIdx.x * 2u + 1u].pieces = 0u;
+    if (threadIdx.x == 0) {
+        a.part_head[blockIdx.x * 2u + 1u].pieces = 0u;
+        a.part_stall[blockIdx.x] = make_uint4(0u, 0u, 0u, 0u);
+    }
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         for (int i = 0; i < TC_STAGES; i++) {
@@ -664,10 +676,12 @@ __global__ void __launch_bounds__(TC_THREADS, 2) attn_tc_kernel(const __grid_con
             // ---------------------------------------------------------- the piece's end
             if (alive) alive = warp_wait(&sh.o_done[(n - 1) & 1u], ((n - 1) >> 1) & 1u, dead, a);
             tc_after();
-            // The four warps agree on how the piece ended; the verdict of the piece before, which all have
-            // read by now, makes room.
-            asm volatile("barrier.cta.sync 1, 128;" ::: "memory");
-            const uint32_t bits = *dead ? (uint32_t)GIFT_ST_STALLED : *(volatile uint32_t*)&sh.bits[piece % TC_BITS_RING];
+            // The four warps agree on how the piece ended: it is complete when each of them saw its last
+            // product, whatever the other roles come to.  The verdict of the piece before, which all have read
+            // by now, makes room.
+            alive = !any_softmax(!alive);
+            const uint32_t bits = alive ? *(volatile uint32_t*)&sh.bits[piece % TC_BITS_RING] : (uint32_t)GIFT_ST_STALLED;
+            if (!alive && row == 0) w.note_stall(a);
             if (row == 0) *(volatile uint32_t*)&sh.bits[(piece + TC_BITS_RING - 1) % TC_BITS_RING] = 0u;
             const bool whole = w.whole();
             const uint32_t slot = w.slot();

@@ -53,3 +53,27 @@ def test_limits_out_of_range(ctx):
         ctx.wait_limit(-1)
     ctx.wait_limit(10 ** 9)
     ctx.wait_limit(0)
+
+
+@pytest.mark.parametrize("dtype,dim,group,new,pt", CASES)
+def test_a_stalled_request_says_so(ctx, dtype, dim, group, new, pt):
+    # a CTA that gives up may hold any head and any tile of rows of a request
+    x = batch(dtype, dim, group, new, pt)
+    rows = torch.tensor([max(0, int(w) - int(h)) for h, w in zip(x["have"], x["want"])])
+    of_row = torch.repeat_interleave(torch.arange(len(rows)), rows).cuda()
+    ctx.wait_limit(0)
+    want = base.call(ctx, x)
+    seen = set()
+    for ns in LIMITS:
+        for _ in range(4):
+            ctx.wait_limit(ns)
+            out, lse, who, st = base.call(ctx, x)
+            assert all(s in (0, binding.ST_STALLED) for s in st), (ns, st)
+            seen |= set(int(s) for s, m in zip(st, rows) if m)
+            assert not st[rows == 0].any()
+            stalled = torch.from_numpy(st.astype("int64")).cuda()[of_row] != 0
+            assert not out[stalled].any() and torch.isneginf(lse[stalled]).all() and (who[stalled] == binding.OWNER_CONFLICT).all(), ns
+            for a, b in zip((out, lse, who), want[:3]):
+                assert torch.equal(a[~stalled], b[~stalled]), ns
+    ctx.wait_limit(0)
+    assert seen == {0, binding.ST_STALLED}

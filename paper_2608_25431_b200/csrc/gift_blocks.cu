@@ -27,12 +27,19 @@ namespace {
 // scattered accesses when many do.  2 to 32 threads share a page when there are threads to spare;
 // a thread has 8 layers' labels under way at once, and what it needs of the page's request lies in
 // shared memory.
+//
+// Stack and tables may be the untrusted side's and may be rewritten while the call runs, so a page is
+// read once, by one of the threads that share it, and what was checked is what is committed: the threads keep
+// the pages of their first BT_KEEP rounds in shared memory (131 072 pages with 16 CTAs).  Behind those a page is
+// read again, and committed only if it is one that this call has claimed and not yet committed.
 // 256 requests that take 16 pages in 32 layers: 12 us; 512 that take 4 000 and give back 700: 25 us (one
 // thread per page and layer, the lengths read again for each, 8 CTAs: 107 us).
 constexpr int BT_CTAS_PORTABLE = 8;
 constexpr int BT_CTAS_LARGE = 16;
 constexpr int BT_THREADS = 1024;
-constexpr uint32_t BT_REQ_BYTES = 12;    // shared memory per request
+constexpr uint32_t BT_REQ_BYTES = 16;    // shared memory per request
+constexpr uint32_t BT_KEEP = 8;          // rounds whose pages are kept
+constexpr uint32_t BT_KEEP_BYTES = BT_KEEP * BT_THREADS * 4;
 constexpr int BT_MAX_DEVICES = 64;
 
 struct BlockArgs {
@@ -50,6 +57,7 @@ struct BlockPlan {
     uint32_t* take;          // [n_req] exclusive prefix of the pages taken
     uint32_t* give;          // [n_req] exclusive prefix of the pages given back
     uint32_t* from;          // [n_req] first block taken, or given back
+    int32_t* owner;          // [n_req]
     uint32_t taken;
     int32_t height;          // of the stack before the call
 };
@@ -58,7 +66,6 @@ struct BlockPlan {
 struct PageMove {
     uint32_t r;
     uint64_t entry;          // its entry in the block tables
-    int32_t page;
 };
 
 __device__ __forceinline__ PageMove page_move(const BlockArgs& a, const BlockPlan& p, uint32_t k)
@@ -69,8 +76,13 @@ __device__ __forceinline__ PageMove page_move(const BlockArgs& a, const BlockPla
     const uint32_t at = take ? k : k - p.taken;
     m.r = req_of(first, a.b.n_req, at);
     m.entry = (uint64_t)m.r * a.b.max_blocks + p.from[m.r] + (at - first[m.r]);
-    m.page = take ? __ldcg(a.free_pages + (p.height - 1 - (int32_t)k)) : __ldcg(a.b.table + m.entry);
     return m;
+}
+
+// The page as the stack or the table has it now.
+__device__ __forceinline__ int32_t page_named(const BlockArgs& a, const BlockPlan& p, uint32_t k, const PageMove& m)
+{
+    return k < p.taken ? __ldcg(a.free_pages + (p.height - 1 - (int32_t)k)) : __ldcg(a.b.table + m.entry);
 }
 
 __global__ void __launch_bounds__(BT_THREADS, 1)
@@ -89,6 +101,8 @@ block_tables_kernel(const __grid_constant__ BlockArgs a)
     p.take = dyn;
     p.give = dyn + n;
     p.from = dyn + 2 * n;
+    p.owner = reinterpret_cast<int32_t*>(dyn + 3 * n);
+    int32_t* kept = p.owner + n + threadIdx.x;          // this thread's pages, BT_THREADS apart
     p.height = *a.n_free;
     const bool stack_bad = p.height < 0 || (uint32_t)p.height > a.free_cap;
     if (threadIdx.x == 0) { s_bad = 0u; s_taken = 0ull; }
@@ -102,9 +116,11 @@ block_tables_kernel(const __grid_constant__ BlockArgs a)
         const uint32_t r = r0 + threadIdx.x;
         uint64_t need = 0, give = 0;
         if (r < n) {
-            const ReqShape s = load_shape(a.b, r);
+            const int32_t owner = a.b.owner[r];
+            const ReqShape s = req_shape(owner, a.b.have[r], a.b.want[r], a.b.page, a.b.max_blocks);
             need = req_need(s);
             give = req_give(s);
+            p.owner[r] = owner;
             p.from[r] = need ? s.bh : s.bw;
         }
         uint64_t tot_take, tot_give;
@@ -131,16 +147,25 @@ block_tables_kernel(const __grid_constant__ BlockArgs a)
     uint32_t share = 32;
     while (share > 1 && (uint64_t)moves * share > nthr) share >>= 1;
     const uint32_t sub = tid & (share - 1), first = tid / share, step = nthr / share;
+    const uint32_t rounds = (moves + step - 1) / step;  // one, where threads share
 
     // Check and claim.  A page may be taken only if nobody owns it in any layer, given back only
     // by its owner, and appear once in the call: the first mention claims its label.
     bool wrong = no_room;
-    for (uint32_t k = first; k < moves; k += step) {
-        const PageMove m = page_move(a, p, k);
-        bool ok = m.page >= 0 && (uint32_t)m.page < a.b.n_pages;
+    for (uint32_t i = 0; i < rounds; i++) {
+        const uint32_t k = first + i * step;
+        int32_t page = -1, owner = 0;
+        if (k < moves) {
+            const PageMove m = page_move(a, p, k);
+            owner = p.owner[m.r];
+            if (sub == 0) page = page_named(a, p, k, m);
+        }
+        page = __shfl_sync(0xFFFFFFFFu, page, threadIdx.x & (32u - share));
+        if (i < BT_KEEP) kept[i * BT_THREADS] = page;
+        if (k >= moves) continue;
+        bool ok = page >= 0 && (uint32_t)page < a.b.n_pages;
         if (ok) {
-            const int32_t owner = a.b.owner[m.r];
-            int32_t* lab = a.owner_map + m.page;
+            int32_t* lab = a.owner_map + page;
             if (sub == 0) {
                 const int32_t v = __ldcg(lab);
                 ok = k < p.taken ? label_takable(v) : label_givable(v, owner);
@@ -172,32 +197,44 @@ block_tables_kernel(const __grid_constant__ BlockArgs a)
     }
     if (refused) {
         // put the claimed labels back; a page mentioned twice is put back by whoever gets there first
-        for (uint32_t k = tid; k < moves; k += nthr) {
-            const PageMove m = page_move(a, p, k);
-            if (m.page < 0 || (uint32_t)m.page >= a.b.n_pages) continue;
-            const int32_t v = __ldcg(a.owner_map + m.page);
-            if (label_claimed(v)) atomicCAS(a.owner_map + m.page, v, label_flip(v));
+        for (uint32_t i = 0; i < rounds; i++) {
+            const uint32_t k = first + i * step;
+            if (k >= moves || sub != 0) continue;
+            const int32_t page = i < BT_KEEP ? kept[i * BT_THREADS] : page_named(a, p, k, page_move(a, p, k));
+            if (page < 0 || (uint32_t)page >= a.b.n_pages) continue;
+            const int32_t v = __ldcg(a.owner_map + page);
+            if (label_claimed(v)) atomicCAS(a.owner_map + page, v, label_flip(v));
         }
         cl.sync();                                      // CTA 0's s_bad stays until every CTA has read it
         return;
     }
 
     // Commit the labels, and the taken pages' entries.
-    for (uint32_t k = first; k < moves; k += step) {
+    for (uint32_t i = 0; i < rounds; i++) {
+        const uint32_t k = first + i * step;
+        if (k >= moves) continue;
         const PageMove m = page_move(a, p, k);
         const bool take = k < p.taken;
-        const int32_t label = take ? a.b.owner[m.r] : GIFT_OWNER_NONE;
-        int32_t* lab = a.owner_map + m.page;
+        const int32_t label = take ? p.owner[m.r] : GIFT_OWNER_NONE;
+        const int32_t page = i < BT_KEEP ? kept[i * BT_THREADS] : page_named(a, p, k, m);
+        if (i >= BT_KEEP) {
+            if (page < 0 || (uint32_t)page >= a.b.n_pages) continue;
+            const int32_t v = __ldcg(a.owner_map + page);
+            if (!label_claimed(v) || atomicCAS(a.owner_map + page, v, label) != v) continue;
+        }
+        int32_t* lab = a.owner_map + page;
 #pragma unroll 8
         for (uint32_t l = sub; l < a.layers; l += share) lab[(uint64_t)l * a.b.n_pages] = label;
-        if (take && sub == 0) a.b.table[m.entry] = m.page;
+        if (take && sub == 0) a.b.table[m.entry] = page;
     }
     cl.sync();                                          // taken entries of the stack have been read
 
     // Push what is given back where the taken pages were, and above.
-    for (uint32_t k = p.taken + tid; k < moves; k += nthr) {
+    for (uint32_t i = 0; i < rounds; i++) {
+        const uint32_t k = first + i * step;
+        if (k < p.taken || k >= moves || sub != 0) continue;
         const PageMove m = page_move(a, p, k);
-        a.free_pages[(uint32_t)p.height - p.taken + (k - p.taken)] = m.page;
+        a.free_pages[(uint32_t)p.height - p.taken + (k - p.taken)] = i < BT_KEEP ? kept[i * BT_THREADS] : page_named(a, p, k, m);
         a.b.table[m.entry] = -1;
     }
     if (tid == 0) *a.n_free = p.height - (int32_t)p.taken + (int32_t)given;
@@ -382,12 +419,12 @@ int gift_block_tables(gift_ctx* c, const gift_batch* batch, int32_t* free_pages,
     const int slot = c->device >= 0 && c->device < BT_MAX_DEVICES ? c->device : -1;
     int ctas = slot >= 0 ? ctas_for_device[slot] : 0;
     if (ctas == 0) {
-        CU_TRY(cudaFuncSetAttribute(block_tables_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, GIFT_MAX_REQS * BT_REQ_BYTES));
+        CU_TRY(cudaFuncSetAttribute(block_tables_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, GIFT_MAX_REQS * BT_REQ_BYTES + BT_KEEP_BYTES));
         ctas = BT_CTAS_PORTABLE;
         if (cudaFuncSetAttribute(block_tables_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess) {
             int n_clusters = 0;
             cfg.gridDim = dim3(BT_CTAS_LARGE, 1, 1);
-            cfg.dynamicSmemBytes = GIFT_MAX_REQS * BT_REQ_BYTES;
+            cfg.dynamicSmemBytes = GIFT_MAX_REQS * BT_REQ_BYTES + BT_KEEP_BYTES;
             attr.val.clusterDim.x = BT_CTAS_LARGE;
             if (cudaOccupancyMaxActiveClusters(&n_clusters, block_tables_kernel, &cfg) == cudaSuccess && n_clusters >= 1)
                 ctas = BT_CTAS_LARGE;
@@ -396,7 +433,7 @@ int gift_block_tables(gift_ctx* c, const gift_batch* batch, int32_t* free_pages,
         if (slot >= 0) ctas_for_device[slot] = ctas;
     }
     cfg.gridDim = dim3(ctas, 1, 1);
-    cfg.dynamicSmemBytes = (size_t)batch->n_req * BT_REQ_BYTES;
+    cfg.dynamicSmemBytes = (size_t)batch->n_req * BT_REQ_BYTES + BT_KEEP_BYTES;
     attr.val.clusterDim.x = ctas;
     CU_TRY(cudaLaunchKernelEx(&cfg, block_tables_kernel, a));
     c->launches++;

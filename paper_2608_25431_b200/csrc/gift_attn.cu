@@ -104,6 +104,22 @@ __device__ __noinline__ void join_here(const AttnArgs& a, const PartHead& head, 
     join_rows<T, D, ROWS, true>(a, head, w, 0, 0, sh);
 }
 
+// At the end of every CTA of the few-row kernel, when it takes no more tickets: the call's last CTA makes all
+// tickets 0 for the next call.  The CTAs are counted, a number that only the launch fixes, so nothing that a
+// call meets (lengths that change while it runs, a second call at the same time against the rule) is
+// left to a later one; a counter in step with the grid returns to 0 by itself.
+__device__ __forceinline__ void leave_tickets(const AttnArgs& a)
+{
+    if (threadIdx.x >= 32) return;
+    bool last = false;
+    if (threadIdx.x == 0) {
+        __threadfence();                               // this CTA's tickets are taken
+        last = atomicInc(a.tickets + a.n_slices, gridDim.x - 1u) == gridDim.x - 1u;
+    }
+    if (__shfl_sync(0xFFFFFFFFu, last, 0))
+        for (uint32_t k = threadIdx.x; k < a.n_slices; k += 32) a.tickets[k] = 0u;
+}
+
 // ---------------------------------------------------------------------------
 // few query rows per K/V head: warp-level products
 // ---------------------------------------------------------------------------
@@ -186,7 +202,10 @@ __global__ void __launch_bounds__(FEW_THREADS, 2) attn_few_kernel(const __grid_c
     __shared__ PartHead s_head;
 
     uint64_t total, slice;
-    if (!place_unit<FEW_THREADS>(a, blockIdx.x, TILE, blockIdx.x == 0, &place, &total, &slice)) return;
+    if (!place_unit<FEW_THREADS>(a, blockIdx.x, TILE, blockIdx.x == 0, &place, &total, &slice)) {
+        leave_tickets(a);
+        return;
+    }
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t ring = (uint32_t)__cvta_generic_to_shared(smem) + warp * (FEW_STAGES * 2 * HALF);
 
@@ -470,7 +489,7 @@ __global__ void __launch_bounds__(FEW_THREADS, 2) attn_few_kernel(const __grid_c
             continue;
         }
         // The last of an item's pieces to be ready joins them: every piece is in memory before its CTA takes a
-        // ticket, and whoever takes the last one puts the ticket back to 0 for the next call.
+        // ticket.
         if (threadIdx.x == 0) a.part_head[slot].bits = bits;
         __threadfence();
         __syncthreads();
@@ -482,7 +501,6 @@ __global__ void __launch_bounds__(FEW_THREADS, 2) attn_few_kernel(const __grid_c
             s_head.h = h; s_head.q0 = q0; s_head.nr = nr;
             s_first = w0;
             s_last = atomicAdd(&a.tickets[w0], 1u) + 1u == s_head.pieces;
-            if (s_last) a.tickets[w0] = 0u;
         }
         __syncthreads();
         if (s_last) {
@@ -491,6 +509,7 @@ __global__ void __launch_bounds__(FEW_THREADS, 2) attn_few_kernel(const __grid_c
         }
         __syncthreads();                               // smem is free for the next piece
     }
+    leave_tickets(a);
 }
 
 // What a wait that ran out leaves: a CTA knows of its own pieces only, so the requests that it could not
@@ -693,7 +712,7 @@ int scratch_ensure(gift_ctx* c, cudaStream_t st)
     if (c->d_attn) return GIFT_OK;
     const size_t parts = 4ull * c->num_sms;
     const size_t before = parts * (PART_ROWS * (PART_D * 4 + 8) + sizeof(PartHead)) + 2ull * c->num_sms * sizeof(uint4);
-    const size_t tickets = 2ull * c->num_sms * 4;
+    const size_t tickets = (2ull * c->num_sms + 1) * 4;
     void* p = nullptr;
     CU_TRY(cudaMalloc(&p, before + tickets));
     const cudaError_t e = cudaMemsetAsync(static_cast<char*>(p) + before, 0, tickets, st);     // tickets are 0 between calls

@@ -64,7 +64,7 @@ struct AttnArgs {
     float2* part_ml;                 // [2 CTAs][rows] running maximum, sum
     PartHead* part_head;             // [2 CTAs]
     uint4* part_stall;               // [CTAs] many rows: requests x .. y - 1, which have rows z .. w - 1, were not all done
-    uint32_t* tickets;               // [CTAs] few rows: pieces of the item that begins in a slice which are ready
+    uint32_t* tickets;               // few rows: [CTAs] pieces of the item that begins in a slice which are ready; [1] CTAs that are done
 };
 
 constexpr float NEG_INF = -__builtin_huge_valf();

@@ -706,10 +706,14 @@ constexpr uint32_t PART_ROWS = TC_ROWS;  // most rows of a tile of query rows
 constexpr uint32_t PART_D = 128;
 
 // The scratch is allocated once, at a size that no call exceeds, and stays where it is until the
-// ctx is destroyed: a captured graph that names it stays valid.
+// ctx is destroyed: a captured graph that names it stays valid.  Not under a capture: the tickets' first
+// zeros would then be the graph's to write, and calls before its first replay would find whatever was there.
 int scratch_ensure(gift_ctx* c, cudaStream_t st)
 {
     if (c->d_attn) return GIFT_OK;
+    cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
+    CU_TRY(cudaStreamIsCapturing(st, &capture));
+    if (capture != cudaStreamCaptureStatusNone) return GIFT_E_INVAL;
     const size_t parts = 4ull * c->num_sms;
     const size_t before = parts * (PART_ROWS * (PART_D * 4 + 8) + sizeof(PartHead)) + 2ull * c->num_sms * sizeof(uint4);
     const size_t tickets = (2ull * c->num_sms + 1) * 4;

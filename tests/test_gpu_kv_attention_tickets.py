@@ -62,3 +62,29 @@ def test_calls_of_every_kind_in_turn():
             got = base.call(ctx, x)
             assert all(torch.equal(a, b) for a, b in zip(w[:3], got[:3])) and not got[3].any()
     ctx.close()
+
+
+@pytest.mark.parametrize("new", [1, 40])
+@pytest.mark.parametrize("mode", ["global", "relaxed"])
+def test_the_first_call_of_a_context_is_refused_under_a_capture(new, mode):
+    x = base.make(63, torch.bfloat16, [5000, 9], [new, new], 1, 1, 128, 16, tree=False)
+    ctx = binding.Ctx(64)
+    b = binding.Batch(base.dev(x["owner"]), base.dev(x["have"]), base.dev(x["want"]), base.dev(x["table"]), x["pt"], x["pool"].shape[0])
+    q = x["q"].contiguous()
+    out, st = torch.zeros_like(q), torch.zeros(2, dtype=torch.int32, device="cuda")
+    refused = []
+    with torch.cuda.graph(torch.cuda.CUDAGraph(), capture_error_mode=mode):
+        out.zero_()
+        try:
+            ctx.kv_attention(b, x["pool"], q, out, st)
+        except binding.GiftError as e:
+            refused.append(e)
+    assert len(refused) == 1
+    base.check(ctx, x)                                 # outside it is served, and so is a capture from then on
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, capture_error_mode=mode):
+        ctx.kv_attention(b, x["pool"], q, out, st)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(out, base.call(ctx, x)[0]) and not st.any()
+    ctx.close()

@@ -588,7 +588,7 @@ int gift_kv_append(gift_ctx* ctx, const gift_kv_pool* pool, const void* k, uint6
  * and lse may be NULL.  If the step has more than n_rows rows, status is GIFT_ST_BAD_TABLE for every
  * request and nothing else is written.  Rows behind the last one are left as they were.
  * q, out: like k in gift_kv_append, in the pool's type; out must overlap no input.  head_dim is
- * 64 or 128.  lse: n_rows x n_heads floats.  The first call on a ctx allocates a fixed scratch
+ * 64 or 128.  scale is finite, of either sign, below 2.3e38.  lse: n_rows x n_heads floats.  The first call on a ctx allocates a fixed scratch
  * (about 40 MB); make it before any stream capture begins (under one it is refused: GIFT_E_INVAL).
  * Graphs that were captured from one ctx must not run at the same time. */
 typedef struct {

@@ -753,6 +753,8 @@ extern "C" int gift_kv_attention(gift_ctx* c, const gift_batch* batch, const gif
     if (t->n_heads == 0 || t->n_heads % pool->n_heads != 0) return GIFT_E_INVAL;
     if (t->n_heads > GIFT_MAX_HEADS || t->mask_words > 0x00FFFFFFu || (uint64_t)t->n_rows * t->n_heads > 0x7FFFFFFFu) return GIFT_E_RANGE;
     if (t->tree_mask && t->mask_words == 0) return GIFT_E_INVAL;
+    if (!isfinite(t->scale)) return GIFT_E_INVAL;
+    if (!isfinite(t->scale * 1.4426950408889634f)) return GIFT_E_RANGE;
     if (t->n_rows) {
         if ((rc = rows_args_ok(t->q, t->q_row_stride, t->q_head_stride)) != GIFT_OK) return rc;
         if ((rc = rows_args_ok(t->out, t->out_row_stride, t->out_head_stride)) != GIFT_OK) return rc;

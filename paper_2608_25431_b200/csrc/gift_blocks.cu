@@ -92,6 +92,7 @@ block_tables_kernel(const __grid_constant__ BlockArgs a)
     __shared__ uint64_t warp_sums[BT_THREADS / 32];
     __shared__ uint32_t s_bad;                          // CTA 0's copy is the cluster's
     __shared__ unsigned long long s_taken;
+    __shared__ int32_t s_height;
     cg::cluster_group cl = cg::this_cluster();
     uint32_t* bad = cl.map_shared_rank(&s_bad, 0);
     // neighbouring warps of work go to different CTAs: a few pages are spread over the SMs
@@ -103,10 +104,10 @@ block_tables_kernel(const __grid_constant__ BlockArgs a)
     p.from = dyn + 2 * n;
     p.owner = reinterpret_cast<int32_t*>(dyn + 3 * n);
     int32_t* kept = p.owner + n + threadIdx.x;          // this thread's pages, BT_THREADS apart
-    p.height = *a.n_free;
-    const bool stack_bad = p.height < 0 || (uint32_t)p.height > a.free_cap;
-    if (threadIdx.x == 0) { s_bad = 0u; s_taken = 0ull; }
+    if (threadIdx.x == 0) { s_bad = 0u; s_taken = 0ull; s_height = __ldcg(a.n_free); }
     __syncthreads();
+    p.height = s_height;                                // one reading, and so one number of rounds, for all threads
+    const bool stack_bad = p.height < 0 || (uint32_t)p.height > a.free_cap;
 
     // Prefix sums.  Pages are handed out in request order; a request is served when its need and
     // all needs before it (refused ones included) fit the stack, so the served ones are a prefix

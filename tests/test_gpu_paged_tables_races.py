@@ -80,3 +80,40 @@ def test_more_pages_than_are_kept(ctx, spoil):
     got, ref = run_tables(ctx, s, 1), P.block_tables(owner, have, want, table, 1, pages, free, n_free, label)
     assert bool((ref[4] == P.BAD_TABLE).all()) == spoil
     same_tables(got, ref)
+
+
+@pytest.mark.parametrize("heights", [(4, 1000), (1000, -3), (40, 30000)])
+def test_a_height_that_changes(ctx, heights):
+    # the number of free pages is read once by a CTA: whatever each of them saw, labels stay with their pages
+    pages, n = 20000, 64
+    label0 = torch.full((2, pages), P.NONE, dtype=torch.int32, device="cuda")
+    label0[:, 1000:] = 9                                  # user 9's, and not on the stack
+    free = torch.arange(pages, dtype=torch.int32, device="cuda")
+    table = torch.full((n, 4), -1, dtype=torch.int32, device="cuda")
+    n_free, label, st = dev([heights[0]]), label0.clone(), torch.zeros(n, dtype=torch.int32, device="cuda")
+    zero = torch.zeros(n, dtype=torch.int32, device="cuda")
+    b = binding.Batch(torch.arange(n, dtype=torch.int32, device="cuda") % 8, zero, zero + 60, table, 16, pages)
+    one, other = dev([heights[0]]), dev([heights[1]])
+    side, flips = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(flips):
+        for _ in range(1000):
+            n_free.copy_(other)
+            n_free.copy_(one)
+    for _ in range(15):
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            flips.replay()
+        seen = []
+        for _ in range(15):
+            label.copy_(label0)
+            ctx.block_tables(b, free, n_free, label, st, layers=2)
+            seen.append(label.clone())
+        torch.cuda.synchronize()
+        for lab in seen:
+            assert (lab[:, 1000:] == 9).all() and (lab[:, :1000] >= P.NONE).all() and (lab[:, :1000] < 8).all() and torch.equal(lab[0], lab[1])
+    label.copy_(label0)
+    n_free.fill_(1000)
+    ctx.block_tables(b, free, n_free, label, st, layers=2)
+    torch.cuda.synchronize()
+    assert not st.any() and int((label[0, :1000] >= 0).sum()) == n * 4 and torch.equal(label[0], label[1])

@@ -477,7 +477,8 @@ int gift_import_from_host(gift_ctx* ctx, const void* h_src, const uint8_t* h_tag
  * reading side).  Nothing here waits for the device or copies to the host, so a step can be
  * captured in a graph; no array but those named is kept by a call.  owner, have and want must not
  * change while a call that takes them runs.  The stack, the block tables and the slots may (they may be the
- * untrusted side's): labels are then judged, and given, by what the call read.
+ * untrusted side's): labels are then judged, and given, by what the call read, and a request may be
+ * refused in some of its heads and rows only.
  *
  * gift_batch: the requests of one step (host structure, device arrays).  Request r has owner[r]
  * in [0, 2^20), have[r] tokens cached before the step and want[r] after it; its block table is

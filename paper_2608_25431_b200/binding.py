@@ -250,6 +250,13 @@ def _arr(t, device, what, dtype="int32", n=0, optional=False):
     return t.data_ptr()
 
 
+def _whole(v, what, bits=32):
+    """v, if it fits the argument's bits: ctypes cuts what does not, and the call would see another number."""
+    if not 0 <= v < 1 << bits:
+        raise ValueError("%s: %r does not fit %d bits" % (what, v, bits))
+    return v
+
+
 class _TorchTypes(dict):
     """The torch types that an array of the named type may have (int32 arrays hold 32-bit words); torch is
     imported when the first of them is looked up."""
@@ -289,6 +296,7 @@ class Batch:
             raise ValueError("table: expected shape [%d, max_blocks], got %s" % (n, tuple(table.shape)))
         if page_tokens <= 0 or n_pages < 0:
             raise ValueError("page_tokens must be positive and n_pages not negative")
+        _whole(page_tokens, "page_tokens"), _whole(n_pages, "n_pages")
         self.n_req, self.page_tokens, self.n_pages, self.device = n, page_tokens, n_pages, dev
         self.tensors = (owner, have, want, table)
         self.c = _Batch(n, table.shape[1], page_tokens, n_pages, _arr(owner, dev, "owner"), _arr(have, dev, "have", n=n),
@@ -502,7 +510,7 @@ class Ctx:
         d, n = self.device, batch.n_req
         _check(lib().gift_block_tables(self._h, self._batch(batch), _arr(free_pages, d, "free_pages"), free_pages.numel(),
                                        _arr(n_free, d, "n_free", n=1), _arr(owner_map, d, "owner_map", n=layers * batch.n_pages),
-                                       layers, _arr(status, d, "status", n=n), self._stream(stream)), "gift_block_tables")
+                                       _whole(layers, "layers"), _arr(status, d, "status", n=n), self._stream(stream)), "gift_block_tables")
 
     def slot_map(self, batch, slots, row_req=None, row_pos=None, row_owner=None, row_ptr=None, total=None, rel=None,
                  stream=None):
@@ -526,8 +534,8 @@ class Ctx:
         if segs.numel() * segs.element_size() < 40 * cap:
             raise ValueError("segs holds fewer entries than page_table")
         flags = (KV_WHOLE_PAGES if whole_pages else 0) | (KV_NEW_BLOCKS if new_blocks else 0)
-        _check(lib().gift_kv_segments(self._h, self._batch(batch), _arr(serial, d, "serial", n=batch.n_req), layers,
-                                      token_bytes, flags, segs.data_ptr(), _arr(page_table, d, "page_table"), cap,
+        _check(lib().gift_kv_segments(self._h, self._batch(batch), _arr(serial, d, "serial", n=batch.n_req), _whole(layers, "layers"),
+                                      _whole(token_bytes, "token_bytes", 64), flags, segs.data_ptr(), _arr(page_table, d, "page_table"), cap,
                                       _arr(total, d, "total", "int64", n=1, optional=True), self._stream(stream)),
                "gift_kv_segments")
 
@@ -582,9 +590,7 @@ class Ctx:
 
     def wait_limit(self, ns=0):
         """gift_ctx_wait_limit: how long a wait inside kv_attention lasts before the call gives up; 0: the default."""
-        if not 0 <= ns < 1 << 64:
-            raise ValueError("ns: expected a number of nanoseconds, got %r" % (ns,))
-        _check(lib().gift_ctx_wait_limit(self._h, ns), "gift_ctx_wait_limit")
+        _check(lib().gift_ctx_wait_limit(self._h, _whole(ns, "ns", 64)), "gift_ctx_wait_limit")
 
     @staticmethod
     def chunk_array(chunks):

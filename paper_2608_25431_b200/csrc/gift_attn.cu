@@ -132,8 +132,8 @@ __device__ __forceinline__ void leave_tickets(const AttnArgs& a)
 // in flight.  The warps' maxima, sums and rows are joined at a piece's end, the pieces of a cut item by
 // the CTA whose piece is ready last (a second kernel for that: 29.6 us a call of one token from Python,
 // this way 27.0; the device's time is the same).  64 requests of 256 to 8192
-// tokens, 32 heads: 16 rows 687 us (6.5 TB/s), 8 rows 678 us; one row over 256 to 2048 tokens 195 us
-// (6.2 TB/s).
+// tokens, 32 heads: 16 rows 688 us (6.5 TB/s), 8 rows 678 us; one row over 256 to 2048 tokens 198 us
+// (6.1 TB/s); one request of 514 tokens and one row 14.4 us.
 
 constexpr int FEW_WARPS = 4;
 constexpr int FEW_THREADS = FEW_WARPS * 32;
@@ -374,7 +374,8 @@ __global__ void __launch_bounds__(FEW_THREADS, 2) attn_few_kernel(const __grid_c
             }
             if (plain) {
                 // p is rounded to the pool's type: the operands of one product have one type, and the
-                // rounding (2^-9 relative at most for bf16) is of the size of v's own
+                // rounding (half a step: 2^-8 relative at most for bf16, 2^-11 for fp16) is of the size of v's own;
+                // the sum of the weights takes them unrounded
                 uint32_t pf[NB][4];
 #pragma unroll
                 for (int k = 0; k < NB; k++) {

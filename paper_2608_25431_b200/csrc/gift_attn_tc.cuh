@@ -9,7 +9,7 @@
 //              is contiguous in a page is a run of tokens: the largest power of two, up to a tile,
 //              that divides the page.  A run of 8 or more is one copy of 64 columns; shorter ones are
 //              gathered, 4 tokens to a copy, which costs some 37 clocks of the SM's one TMA unit
-//              however little it brings (32 requests of 8192 tokens, 8 K/V heads, 128 rows each: 201
+//              however little it brings (32 requests of 8192 tokens, 8 K/V heads, 128 rows each: 204
 //              us with pages of 16, 279 us with pages of 4).  Rows outside the map read as zeros:
 //              that is where the runs past the context are sent.  Each of the two judges the
 //              labels of the pages that it copies from: both look a page up for themselves, and a table
@@ -23,9 +23,11 @@
 // 2 CTAs per SM share its tensor memory (256 of 512 columns each) and hide each other's waits.
 //
 // What bounds it: with one tile of query rows per K/V head, HBM (24 drafted tokens of 32 heads over
-// contexts of 256 to 8192, 64 requests: 714 us, 6.3 TB/s; 32 requests as above: 201 us, 5.4 TB/s and 685
-// TFLOP/s); with several, the chain of a tile through softmax and products, some 1 900 clocks per
-// CTA, and under a long load the power cap, which takes the clock from 1965 to some 1250 MHz.  The
+// contexts of 256 to 8192, 64 requests: 716 us, 6.3 TB/s; 32 requests as above: 204 us, 5.4 TB/s and 675
+// TFLOP/s).  With several (48 requests, trees of 1 to 64, up to 16384 tokens, 8 of 32 heads) it takes 389 us at
+// 1965 MHz, 3 000 clocks per tile and CTA, where the chain of a tile through softmax and products takes
+// 1 900 with K/V in L2: the rest, waits for K and V among it, is not accounted for.  Under a long load the
+// power cap takes the clock to 1390 MHz and the time to 464 us.  The
 // whole kernel is written small: items of a few tiles meet its cold parts at every end, and
 // fetching those past the instruction cache cost as much as the tiles (code of 105 KB: 505 us
 // where 66 KB take 442, contexts of 64 to 1024 tokens 261 and 169 us).

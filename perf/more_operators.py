@@ -395,7 +395,7 @@ def _own(s):
                      pos=s["pos"], freq=s["freq"], sections=s["sections"], paired=c["paired"], owner_map=s["label"])
         return [s["q_out"], s["pool"], s["status"]] if c["bits"] == 16 else [s["q_out"], *_parts(s["pool"], c["heads"], c["dim"]), s["status"]]
     b = binding.Batch(s["owner"], s["have"], s["want"], s["table"], c["pt"], s["pages"])
-    ctx.kv_attention8(b, s["pool"], c["heads"], q, s["out"], s["status"], tree_mask=s["mask"], lse=s["lse"], row_owner=s["row_owner"], owner_map=s["label"],
+    ctx.kv_attention_codes(b, s["pool"], c["heads"], q, s["out"], s["status"], tree_mask=s["mask"], lse=s["lse"], row_owner=s["row_owner"], owner_map=s["label"],
                       softcap=c["cap"], window=c["window"], slopes=s["slopes"])
     return [s["out"], s["lse"], s["row_owner"], s["status"]]
 

@@ -614,6 +614,88 @@ int gift_kv_attention(gift_ctx* ctx, const gift_batch* batch, const gift_kv_pool
 #define GIFT_MAX_WAIT_NS 1000000000ull
 int gift_ctx_wait_limit(gift_ctx* ctx, uint64_t ns);
 
+/* ------------------------------------------------------------------------------------------
+ * The cache in 8 bits: rows on their way into the pages, rows out of them, and attention over them.
+ * Half the bytes of a 16-bit cache for the attention to read and for a handoff to encrypt.
+ *
+ * A token of an 8-bit page (gift_kv_pool with dtype GIFT_E4M3): GIFT_KV8_TOKEN_BYTES(n_heads, head_dim)
+ * bytes, that is, e4m3 codes of K [n_heads][head_dim], codes of V [n_heads][head_dim], for each head two 32-bit
+ * scales, K's and V's, and zeros up to a multiple of 16 bytes.  An element's value is code * scale.  The
+ * scales lie with their token, so that what gift_kv_segments (token_bytes as above) hands to the cipher
+ * is all that the other side needs.  page p's tokens begin at pages + p * page_tokens * token bytes.  head_dim is a
+ * multiple of 16. */
+#define GIFT_E4M3 2u
+#define GIFT_KV8_TOKEN_BYTES(heads, dim) ((2ull * (heads) * ((dim) + 4ull) + 15ull) & ~15ull)
+
+/* A step's rows on their way from the projection to the cache, in one pass: norms of the heads of q
+ * and k, rotary positions, q to q_out, K and V into labelled pages of 16 or 8 bits.
+ *   norm      head x of q (q_norm not NULL) or of k (k_norm): x * w / sqrt(mean(x^2) + eps), with w the head_dim
+ *             weights, in dtype
+ *   rotation  (n_freq > 0) of the first 2 n_freq elements of every head of q and k: with angle = pos * freq[i],
+ *             freq 32-bit and the product taken in 64 bits, pair i becomes (a cos - b sin, b cos + a sin).  Pair i is elements (i, n_freq
+ *             + i), or with GIFT_ROTATE_PAIRS (2 i, 2 i + 1).  The first sections[0] pairs turn by row t's
+ *             position on axis 0, pos[t], the next sections[1] by that on axis 1, pos[pos_stride + t], and so on
+ *             (time, height, width of an image's or video's rows); the sections of the n_axes axes add up to n_freq.
+ *   8 bits    of K (normed and turned) and V: scale = max(max |x| / 448, 2^-126) over a head's elements, code = the
+ *             e4m3 number nearest to x / scale.  A head that holds an infinity or NaN reads back as NaN throughout:
+ *             scale NaN, codes 0.
+ * All in 32 bits, rounded once.  Row t, head h of k starts at k + t*k_row_stride + h*k_head_stride elements of dtype
+ * (strides multiples of 8, 16-byte aligned, a head's elements contiguous); likewise v, q and q_out.  q NULL: K and V alone.  dtype is that of
+ * all rows (GIFT_BF16 or GIFT_FP16), and of a 16-bit pool.  Labels, slots and status as in gift_kv_append: a
+ * row is written to slots[t] if the page's label is row_owner[t], else status[t] says why and nothing of the
+ * row is written, q_out neither; nor for slot -1 (status 0).  q_out may be q itself (same strides) and overlaps
+ * nothing else.  head_dim <= 256, n_freq a multiple of 4, 2 n_freq <= head_dim, n_axes <= GIFT_MAX_AXES, eps >= 0. */
+#define GIFT_MAX_AXES 4u
+#define GIFT_ROTATE_PAIRS 1u
+typedef struct {
+    const void* q;
+    uint64_t q_row_stride, q_head_stride;
+    void* q_out;
+    uint64_t q_out_row_stride, q_out_head_stride;
+    const void* k;
+    uint64_t k_row_stride, k_head_stride;
+    const void* v;
+    uint64_t v_row_stride, v_head_stride;
+    uint32_t n_rows, n_heads, dtype, flags;
+    const void* q_norm;
+    const void* k_norm;
+    float eps;
+    uint32_t n_freq, n_axes;
+    uint32_t sections[GIFT_MAX_AXES];
+    const float* freq;
+    const int32_t* pos;
+    uint64_t pos_stride;
+} gift_kv_rows;
+int gift_kv_write(gift_ctx* ctx, const gift_kv_pool* pool, const gift_kv_rows* rows, const int64_t* slots,
+                  const int32_t* row_owner, uint32_t* status, void* stream);
+
+/* The way back: row t of k and v (in dtype, GIFT_BF16 or GIFT_FP16, that of a 16-bit pool; strides as above) receives the values in
+ * slots[t], code * scale rounded once, if the page's label is row_owner[t] or GIFT_OWNER_PARAM (a shared
+ * prefix).  Else the row is zero and status[t] is GIFT_ST_OWNER_MISMATCH, GIFT_ST_UNOWNED or GIFT_ST_BAD_DESC (slot out of range).  Slot -1: the
+ * row is left as it was, status 0.  gift_slot_map gives the slots: with have 0 those of whole requests.  k and v
+ * overlap neither each other nor the pages. */
+int gift_kv_read(gift_ctx* ctx, const gift_kv_pool* pool, uint32_t dtype, uint32_t n_rows, const int64_t* slots, const int32_t* row_owner,
+                 void* k, uint64_t k_row_stride, uint64_t k_head_stride, void* v, uint64_t v_row_stride, uint64_t v_head_stride,
+                 uint32_t* status, void* stream);
+
+/* gift_kv_attention over 8-bit pages (pool->dtype GIFT_E4M3); q and out are of dtype.  All that is said there holds, and
+ * the score of query head h's row at position x with token t is
+ *   s = scale * q . k_t;  softcap > 0: s = softcap * tanh(s / softcap);  slopes: s += slopes[h] * (t - x)
+ * A row at position x (have + i) sees with window > 0 only tokens t > x - window; a page with no token that one of the
+ * request's rows may see is neither read nor judged.  slopes (n_heads floats, NULL: none) and window need distances, which
+ * drafted trees do not have here: with a tree_mask they are refused.  Scores, softmax and sums are 32-bit; the products
+ * take q, codes and the weights p * scale in 16 bits (fp16 of a row's own power of two).  Scratch as for
+ * gift_kv_attention, and shared with it. */
+typedef struct {
+    gift_attn attn;
+    uint32_t dtype;
+    float softcap;
+    uint32_t window;
+    const float* slopes;
+} gift_attn_codes;
+int gift_kv_attention_codes(gift_ctx* ctx, const gift_batch* batch, const gift_kv_pool* pool, const gift_attn_codes* attn,
+                       uint32_t* status, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -23,6 +23,7 @@ OWNER_PARAM, OWNER_NONE, OWNER_CONFLICT = -1, -2, -3
 RULE_IDENTITY, RULE_ROWWISE, RULE_SEGREDUCE, RULE_BROADCAST = 0, 1, 2, 3
 STATIC_MAX_SEGS = 65536
 KV_WHOLE_PAGES, KV_NEW_BLOCKS = 1, 2
+E4M3, ROTATE_PAIRS, MAX_AXES = 2, 1, 4
 MAX_REQS = 8192
 
 EXPORTS = [
@@ -33,6 +34,7 @@ EXPORTS = [
     "gift_strerror", "gift_version", "gift_launch_count", "gift_timing_enable", "gift_timing_read",
     "gift_export_to_host", "gift_import_from_host", "gift_last_error_detail",
     "gift_block_tables", "gift_slot_map", "gift_kv_segments", "gift_kv_append", "gift_kv_attention", "gift_ctx_wait_limit",
+    "gift_kv_write", "gift_kv_read", "gift_kv_attention_codes",
 ]
 
 
@@ -86,6 +88,20 @@ class _Attn(C.Structure):
                 ("out", C.c_void_p), ("out_row_stride", C.c_uint64), ("out_head_stride", C.c_uint64),
                 ("n_rows", C.c_uint32), ("n_heads", C.c_uint32), ("scale", C.c_float), ("tree_mask", C.c_void_p),
                 ("mask_words", C.c_uint32), ("lse", C.c_void_p), ("row_owner", C.c_void_p)]
+
+
+class _KvRows(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("q_row_stride", C.c_uint64), ("q_head_stride", C.c_uint64),
+                ("q_out", C.c_void_p), ("q_out_row_stride", C.c_uint64), ("q_out_head_stride", C.c_uint64),
+                ("k", C.c_void_p), ("k_row_stride", C.c_uint64), ("k_head_stride", C.c_uint64),
+                ("v", C.c_void_p), ("v_row_stride", C.c_uint64), ("v_head_stride", C.c_uint64),
+                ("n_rows", C.c_uint32), ("n_heads", C.c_uint32), ("dtype", C.c_uint32), ("flags", C.c_uint32),
+                ("q_norm", C.c_void_p), ("k_norm", C.c_void_p), ("eps", C.c_float), ("n_freq", C.c_uint32), ("n_axes", C.c_uint32),
+                ("sections", C.c_uint32 * MAX_AXES), ("freq", C.c_void_p), ("pos", C.c_void_p), ("pos_stride", C.c_uint64)]
+
+
+class _AttnCodes(C.Structure):
+    _fields_ = [("attn", _Attn), ("dtype", C.c_uint32), ("softcap", C.c_float), ("window", C.c_uint32), ("slopes", C.c_void_p)]
 
 
 RACE_RAW, RACE_WAR, RACE_WAW = 1, 2, 4
@@ -200,6 +216,9 @@ def lib():
         l.gift_kv_append.argtypes = [vp, C.POINTER(_KvPool), vp, u64, u64, vp, u64, u64, u32, vp, vp, vp, vp]
         l.gift_ctx_wait_limit.argtypes = [vp, u64]
         l.gift_kv_attention.argtypes = [vp, C.POINTER(_Batch), C.POINTER(_KvPool), C.POINTER(_Attn), vp, vp]
+        l.gift_kv_write.argtypes = [vp, C.POINTER(_KvPool), C.POINTER(_KvRows), vp, vp, vp, vp]
+        l.gift_kv_read.argtypes = [vp, C.POINTER(_KvPool), u32, u32, vp, vp, vp, u64, u64, vp, u64, u64, vp, vp]
+        l.gift_kv_attention_codes.argtypes = [vp, C.POINTER(_Batch), C.POINTER(_KvPool), C.POINTER(_AttnCodes), vp, vp]
         _lib = l
     return _lib
 
@@ -264,7 +283,7 @@ class _TorchTypes(dict):
     def __missing__(self, key):
         import torch
         self.update(int32=(torch.int32, torch.uint32), int64=(torch.int64,), float32=(torch.float32,),
-                    pool={torch.bfloat16: 0, torch.float16: 1})
+                    pool={torch.bfloat16: 0, torch.float16: 1}, codes=torch.uint8)
         return self[key]
 
 
@@ -283,6 +302,11 @@ def _rows3(t, device, what, heads, dim, dtype, rows=None):
         raise ValueError("%s: a head's elements must be contiguous" % what)
     # the stride of a dimension of one entry is never used
     return t.data_ptr(), row if shape[0] > 1 else 0, head if heads > 1 else 0
+
+
+def kv8_token_bytes(heads, dim):
+    """GIFT_KV8_TOKEN_BYTES: bytes of one token of an 8-bit page."""
+    return -(-2 * heads * (dim + 4) // 16) * 16
 
 
 class Batch:
@@ -588,6 +612,114 @@ class Ctx:
         _check(lib().gift_kv_attention(self._h, self._batch(batch), C.byref(pool), C.byref(a),
                                        _arr(status, d, "status", n=batch.n_req), self._stream(stream)), "gift_kv_attention")
 
+    def _pool8(self, pages, heads, dim, owner_map):
+        """An 8-bit pool: uint8 [n_pages, page_tokens, kv8_token_bytes(heads, dim)]."""
+        if pages.dim() != 3 or pages.shape[2] != kv8_token_bytes(heads, dim):
+            raise ValueError("pages: expected shape [n_pages, page_tokens, %d], got %s" % (kv8_token_bytes(heads, dim), tuple(pages.shape)))
+        d = self.device
+        if pages.get_device() != d or not pages.is_contiguous():
+            raise ValueError("pages: expected a contiguous tensor on cuda:%d" % d)
+        n, pt, _ = pages.shape
+        return _KvPool(pages.data_ptr(), n, pt, heads, dim, E4M3, _arr(owner_map, d, "owner_map", n=n, optional=True))
+
+    def _any_pool(self, pages, k, owner_map):
+        """(pool, dtype of rows) of 16-bit pages (see kv_append) or of 8-bit ones, uint8, for rows like k."""
+        if k.dim() != 3:
+            raise ValueError("k: expected shape [rows, n_heads, head_dim], got %s" % (tuple(k.shape),))
+        dtype = _torch_types["pool"].get(k.dtype)
+        if dtype is None:
+            raise ValueError("k: expected bfloat16 or float16, got %s" % k.dtype)
+        if pages.dtype is _torch_types["codes"]:
+            return self._pool8(pages, k.shape[1], k.shape[2], owner_map), dtype
+        if pages.dtype != k.dtype:
+            raise ValueError("pages: expected uint8 or %s, got %s" % (k.dtype, pages.dtype))
+        pool = self._pool(pages, owner_map)
+        if (pool.n_heads, pool.head_dim) != (k.shape[1], k.shape[2]):
+            raise ValueError("k: expected shape [rows, %d, %d], got %s" % (pool.n_heads, pool.head_dim, tuple(k.shape)))
+        return pool, dtype
+
+    def kv_write(self, pages, k, v, slots, row_owner, status, q=None, q_out=None, q_norm=None, k_norm=None, eps=1e-6, pos=None,
+                 freq=None, sections=None, paired=False, owner_map=None, stream=None):
+        """gift_kv_write: pages uint8 [n_pages, page_tokens, kv8_token_bytes(n_heads, head_dim)] (8 bits) or as for kv_append;
+        k, v [rows, n_heads, head_dim], q and q_out [rows, heads, head_dim] or None, all of one type; slots, row_owner, status,
+        owner_map as for kv_append; q_norm, k_norm [head_dim] in that type or None; freq float32 [n_freq] or None (no rotation), pos int32
+        [rows] or [axes, rows], sections: pairs that turn by each axis (None: one axis); paired: neighbours are pairs."""
+        d, n, dim, dtype = self.device, k.shape[0], k.shape[-1], k.dtype
+        pool, code = self._any_pool(pages, k, owner_map)
+        a = _KvRows()
+        a.k, a.k_row_stride, a.k_head_stride = _rows3(k, d, "k", pool.n_heads, dim, dtype)
+        a.v, a.v_row_stride, a.v_head_stride = _rows3(v, d, "v", pool.n_heads, dim, dtype, n)
+        a.n_rows, a.dtype, a.eps = n, code, eps
+        if q is not None:
+            if q.dim() != 3 or q_out is None:
+                raise ValueError("q: expected shape [rows, heads, head_dim], and a q_out")
+            a.n_heads = q.shape[1]
+            a.q, a.q_row_stride, a.q_head_stride = _rows3(q, d, "q", q.shape[1], dim, dtype, n)
+            a.q_out, a.q_out_row_stride, a.q_out_head_stride = _rows3(q_out, d, "q_out", q.shape[1], dim, dtype, n)
+        elif q_out is not None or q_norm is not None:
+            raise ValueError("q_out and q_norm go with q")
+        for w, what in ((q_norm, "q_norm"), (k_norm, "k_norm")):
+            if w is not None:
+                if w.dtype != dtype or w.shape != (dim,):
+                    raise ValueError("%s: expected %s [%d], got %s %s" % (what, dtype, dim, w.dtype, tuple(w.shape)))
+                if w.get_device() != d or not w.is_contiguous():
+                    raise ValueError("%s: expected a contiguous tensor on cuda:%d" % (what, d))
+                setattr(a, what, w.data_ptr())
+        if freq is not None:
+            a.freq, a.n_freq = _arr(freq, d, "freq", "float32"), freq.numel()
+            if pos is None or pos.dim() not in (1, 2) or pos.shape[-1] != n:
+                raise ValueError("pos: expected shape [%d] or [axes, %d]" % (n, n))
+            axes = 1 if pos.dim() == 1 else pos.shape[0]
+            sections = [a.n_freq] if sections is None and axes == 1 else sections
+            if sections is None or len(sections) != axes or axes > MAX_AXES:
+                raise ValueError("sections: one number of pairs for each of pos's axes (%d; at most %d)" % (axes, MAX_AXES))
+            for x, count in enumerate(sections):
+                a.sections[x] = _whole(count, "sections")
+            a.n_axes, a.pos, a.pos_stride, a.flags = axes, _arr(pos, d, "pos"), n, ROTATE_PAIRS if paired else 0
+        elif pos is not None or sections is not None:
+            raise ValueError("pos and sections go with freq")
+        _check(lib().gift_kv_write(self._h, C.byref(pool), C.byref(a), _arr(slots, d, "slots", "int64", n=n),
+                                   _arr(row_owner, d, "row_owner", n=n, optional=owner_map is None),
+                                   _arr(status, d, "status", n=n), self._stream(stream)), "gift_kv_write")
+
+    def kv_read(self, pages, k, v, slots, row_owner, status, owner_map=None, stream=None):
+        """gift_kv_read: the values in slots (int64 [rows]) of pages (8 or 16 bits, as for kv_write) into k, v [rows, n_heads,
+        head_dim]; row_owner and status int32 [rows]; owner_map int32 [n_pages] or None."""
+        d, n = self.device, k.shape[0]
+        pool, code = self._any_pool(pages, k, owner_map)
+        kp, kr, kh = _rows3(k, d, "k", pool.n_heads, pool.head_dim, k.dtype)
+        vp, vr, vh = _rows3(v, d, "v", pool.n_heads, pool.head_dim, k.dtype, n)
+        _check(lib().gift_kv_read(self._h, C.byref(pool), code, n, _arr(slots, d, "slots", "int64", n=n),
+                                  _arr(row_owner, d, "row_owner", n=n, optional=owner_map is None), kp, kr, kh, vp, vr, vh,
+                                  _arr(status, d, "status", n=n), self._stream(stream)), "gift_kv_read")
+
+    def kv_attention_codes(self, batch, pages, kv_heads, q, out, status, tree_mask=None, lse=None, row_owner=None, owner_map=None, scale=None,
+                      softcap=0.0, window=0, slopes=None, stream=None):
+        """gift_kv_attention_codes: as kv_attention, over 8-bit pages (uint8, see kv_write) of kv_heads heads; softcap: 0 for none;
+        window: tokens that a row sees, 0 for all; slopes float32 [heads] or None."""
+        if q.dim() != 3:
+            raise ValueError("q: expected shape [rows, heads, head_dim], got %s" % (tuple(q.shape),))
+        dtype = _torch_types["pool"].get(q.dtype)
+        if dtype is None or pages.dtype is not _torch_types["codes"]:
+            raise ValueError("expected q in bfloat16 or float16 and pages in uint8, got %s and %s" % (q.dtype, pages.dtype))
+        d, n, heads, dim = self.device, q.shape[0], q.shape[1], q.shape[2]
+        pool = self._pool8(pages, _whole(kv_heads, "kv_heads"), dim, owner_map)
+        qp, qr, qh = _rows3(q, d, "q", heads, dim, q.dtype)
+        op, orow, oh = _rows3(out, d, "out", heads, dim, q.dtype, n)
+        words = 0
+        if tree_mask is not None:
+            if tree_mask.dim() != 2 or tree_mask.shape[0] != n:
+                raise ValueError("tree_mask: expected shape [%d, mask_words], got %s" % (n, tuple(tree_mask.shape)))
+            words = tree_mask.shape[1]
+            if words == 0:
+                raise ValueError("tree_mask has no words")
+        a = _AttnCodes(_Attn(qp, qr, qh, op, orow, oh, n, heads, dim ** -0.5 if scale is None else scale,
+                         _arr(tree_mask, d, "tree_mask", optional=True), words, _arr(lse, d, "lse", "float32", n=n * heads, optional=True),
+                         _arr(row_owner, d, "row_owner", n=n, optional=True)),
+                   dtype, softcap, _whole(window, "window"), _arr(slopes, d, "slopes", "float32", n=heads, optional=True))
+        _check(lib().gift_kv_attention_codes(self._h, self._batch(batch), C.byref(pool), C.byref(a),
+                                        _arr(status, d, "status", n=batch.n_req), self._stream(stream)), "gift_kv_attention_codes")
+
     def wait_limit(self, ns=0):
         """gift_ctx_wait_limit: how long a wait inside kv_attention lasts before the call gives up; 0: the default."""
         _check(lib().gift_ctx_wait_limit(self._h, _whole(ns, "ns", 64)), "gift_ctx_wait_limit")
@@ -774,6 +906,18 @@ def gift_kv_append(ctx: Ctx, *args, **kw):
 
 def gift_kv_attention(ctx: Ctx, *args, **kw):
     ctx.kv_attention(*args, **kw)
+
+
+def gift_kv_write(ctx: Ctx, *args, **kw):
+    return ctx.kv_write(*args, **kw)
+
+
+def gift_kv_read(ctx: Ctx, *args, **kw):
+    return ctx.kv_read(*args, **kw)
+
+
+def gift_kv_attention_codes(ctx: Ctx, *args, **kw):
+    return ctx.kv_attention_codes(*args, **kw)
 
 
 def gift_ctx_wait_limit(ctx: Ctx, ns=0):

@@ -58,6 +58,7 @@ struct AttnArgs {
     uint32_t tile_rows;              // query rows of an item, at most
     uint32_t least;                  // smallest slice, in tiles
     uint32_t extra;                  // tiles that an item costs beyond its own
+    uint32_t window;                 // tokens that a row may see, its own included; 0: all (kernels with WIN alone look at it)
     uint32_t n_slices, ways;         // slices, and CTAs that share one
     uint32_t wait_tries, wait_ns;    // tcgen05 kernel: further attempts of a wait, and the longest single one
     float* part_o;                   // [2 CTAs][rows][D]
@@ -73,12 +74,17 @@ constexpr float NEG_INF = -__builtin_huge_valf();
 struct ItemShape {
     uint32_t rows_m;                 // step tokens
     uint32_t nqt;                    // tiles of query rows
-    uint32_t tiles;                  // token tiles of the context
+    uint32_t tiles;                  // token tiles of the context, or (WIN) of what of it the rows may see
+    uint32_t first;                  // WIN: the first of them
     uint32_t items;                  // nqt for every K/V head
     uint32_t cost;                   // units of one item (or pair of items): extra, then its tiles
     uint64_t units;                  // units of all its items
 };
 
+// The first token that a request's rows may see: its first row, at position have, sees the furthest back.
+__device__ __forceinline__ uint32_t first_seen(const AttnArgs& a, uint32_t have) { return a.window && have >= a.window ? have - a.window + 1u : 0u; }
+
+template <bool WIN = false>
 __device__ __forceinline__ ItemShape item_shape(const AttnArgs& a, const ReqShape& s, uint32_t tile_tokens)
 {
     ItemShape i;
@@ -86,6 +92,10 @@ __device__ __forceinline__ ItemShape item_shape(const AttnArgs& a, const ReqShap
     // rows * group fits 31 bits unless the step has more rows than the call, which is refused on the rows alone
     i.nqt = a.by_tile_rows.cover(s.rows * a.group & 0x7FFFFFFFu);
     i.tiles = (s.want + tile_tokens - 1) / tile_tokens;      // >= 1 when rows > 0
+    if constexpr (WIN) {
+        i.first = first_seen(a, s.have) / tile_tokens;
+        i.tiles -= i.first;
+    }
     i.cost = i.tiles + a.extra;
     i.items = i.nqt * a.kv_heads;
     i.units = (uint64_t)((i.items + a.ways - 1) / a.ways) * i.cost;
@@ -107,7 +117,7 @@ struct PlaceShared {
 // Block-wide: the total of the requests' units and the place of unit w * slice.  Returns false
 // (for every thread) when that unit does not exist, or the step has more rows than the caller
 // gave; `first` marks the CTA that writes the status of requests without items.
-template <int THREADS>
+template <int THREADS, bool WIN = false>
 __device__ bool place_unit(const AttnArgs& a, uint32_t w, uint32_t tile_tokens, bool first,
                            PlaceShared* sh, uint64_t* total_out, uint64_t* slice_out)
 {
@@ -118,7 +128,7 @@ __device__ bool place_unit(const AttnArgs& a, uint32_t w, uint32_t tile_tokens, 
     for (uint32_t r = r0; r < r1; r++) {
         const ReqShape s = load_shape(a.b, r);
         rows += s.rows;
-        units += item_shape(a, s, tile_tokens).units;
+        units += item_shape<WIN>(a, s, tile_tokens).units;
         if (first && s.rows == 0) a.status[r] = s.ok ? 0u : GIFT_ST_BAD_DESC;
     }
     uint64_t all_rows, total;
@@ -139,7 +149,7 @@ __device__ bool place_unit(const AttnArgs& a, uint32_t w, uint32_t tile_tokens, 
 #pragma unroll 1
         for (uint32_t r = r0; r < r1; r++) {
             const ReqShape s = load_shape(a.b, r);
-            const ItemShape it = item_shape(a, s, tile_tokens);
+            const ItemShape it = item_shape<WIN>(a, s, tile_tokens);
             if (u < before + it.units) {
                 sh->at.r = r;
                 sh->at.row0 = (uint32_t)row;
@@ -156,14 +166,14 @@ __device__ bool place_unit(const AttnArgs& a, uint32_t w, uint32_t tile_tokens, 
 }
 
 // The pieces of a CTA's slice, in order.
-template <uint32_t TILE> struct Walk {
+template <uint32_t TILE, bool WIN = false> struct Walk {
     ReqShape s;
     ItemShape it;
     uint32_t r, row0;
     uint32_t way, k, u;              // which of the CTAs that share the slice; item (or pair); its units that are done
     uint64_t left;                   // units to go
     int32_t next_owner, next_have, next_want;       // of request r + 1, fetched ahead
-    // the current piece: K/V head, tile of query rows, token tiles
+    // the current piece: K/V head, tile of query rows, token tiles (WIN: counted from it.first)
     uint32_t h, qt, tb, n_tiles, all_q;
 
     __device__ __forceinline__ void fetch(const AttnArgs& a)
@@ -176,7 +186,7 @@ template <uint32_t TILE> struct Walk {
         way = which; k = p.k; u = p.u;
         r = p.r; row0 = p.row0; left = units;
         s = load_shape(a.b, r);
-        it = item_shape(a, s, TILE);
+        it = item_shape<WIN>(a, s, TILE);
         fetch(a);
         all_q = it.rows_m * a.group;
     }
@@ -191,7 +201,7 @@ template <uint32_t TILE> struct Walk {
                         row0 += it.rows_m;
                         r++;
                         s = req_shape(next_owner, next_have, next_want, a.b.page, a.b.max_blocks);
-                        it = item_shape(a, s, TILE);
+                        it = item_shape<WIN>(a, s, TILE);
                         fetch(a);
                     } while (it.nqt == 0);
                     all_q = it.rows_m * a.group;

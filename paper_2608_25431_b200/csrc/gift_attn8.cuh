@@ -1,0 +1,55 @@
+// Attention over 8-bit pages: what its kernels share.
+#pragma once
+#include "gift_attn.cuh"
+#include "gift_kv8.cuh"
+
+namespace gift {
+
+struct Attn8Args : AttnArgs {
+    uint32_t codes;                  // bytes of K's (or V's) codes of one token; V's, then the scales, lie behind
+    float cap_in, cap_out;           // scale / softcap, softcap * log2(e); cap_out 0: no cap
+    const float* slopes;
+};
+
+constexpr float LOG2_E = 1.4426950408889634f;
+
+__device__ __forceinline__ float fast_rcp(float x)
+{
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// tanh: 1 - 2 / (e^2u + 1), whose error of 2^-23 is absolute, and near 0 the series, whose first term left out is
+// below 6e-8 of the value at the border.
+__device__ __forceinline__ float tanh_of(float u)
+{
+    const float far = 1.f - 2.f * fast_rcp(fast_exp2(u * (2.f * LOG2_E)) + 1.f), x = u * u;
+    const float near = u * (1.f + x * (-0.33333333f + x * (0.13333333f + x * -0.053968254f)));
+    return fabsf(u) < 0.2f ? near : far;
+}
+
+// Power-of-two factors, made of exponents: a value whose top exponent field is e becomes one of about 2^12, in
+// fp16 well above what it rounds (2^-14) and below what it holds (2^16).  e = 255: infinities and NaN stay.
+__device__ __forceinline__ uint32_t top_exponent(uint32_t magnitude) { return magnitude >> 23 < 13u ? 13u : magnitude >> 23; }
+__device__ __forceinline__ float to_half_range(uint32_t e) { return e == 255u ? 1.f : __uint_as_float((266u - e) << 23); }
+__device__ __forceinline__ float from_half_range(uint32_t e) { return e == 255u ? 1.f : __uint_as_float((e - 12u) << 23); }
+
+// Which of the 64 tokens from t0 a row sees where a window ends among them, as bits: those from position x - window + 1 on.
+__device__ __forceinline__ uint64_t in_window64(uint32_t window, uint32_t x, uint32_t t0)
+{
+    const uint32_t low = x >= window ? x - window + 1u : 0u;
+    if (low <= t0) return ~0ull;
+    return low - t0 >= 64u ? 0ull : ~0ull << (low - t0);
+}
+
+// Whether a word of four codes holds one that is NaN.
+__device__ __forceinline__ bool codes_nan(uint32_t w) { return (((w & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u) != 0u; }
+// The word with those codes 0.
+__device__ __forceinline__ uint32_t codes_without_nan(uint32_t w)
+{
+    const uint32_t bad = ((w & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u;      // one bit a byte
+    return w & ~((bad >> 7) * 255u);
+}
+
+}  // namespace gift

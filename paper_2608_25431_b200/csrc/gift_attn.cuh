@@ -58,6 +58,7 @@ struct AttnArgs {
     uint32_t tile_rows;              // query rows of an item, at most
     uint32_t least;                  // smallest slice, in tiles
     uint32_t extra;                  // tiles that an item costs beyond its own
+    uint32_t tile_tokens;            // tokens of a tile, where that is not the kernel's own constant
     uint32_t window;                 // tokens that a row may see, its own included; 0: all (kernels with WIN alone look at it)
     uint32_t n_slices, ways;         // slices, and CTAs that share one
     uint32_t wait_tries, wait_ns;    // tcgen05 kernel: further attempts of a wait, and the longest single one
@@ -165,7 +166,7 @@ __device__ bool place_unit(const AttnArgs& a, uint32_t w, uint32_t tile_tokens, 
     return true;
 }
 
-// The pieces of a CTA's slice, in order.
+// The pieces of a CTA's slice, in order.  TILE 0: tiles of a.tile_tokens.
 template <uint32_t TILE, bool WIN = false> struct Walk {
     ReqShape s;
     ItemShape it;
@@ -186,7 +187,7 @@ template <uint32_t TILE, bool WIN = false> struct Walk {
         way = which; k = p.k; u = p.u;
         r = p.r; row0 = p.row0; left = units;
         s = load_shape(a.b, r);
-        it = item_shape<WIN>(a, s, TILE);
+        it = item_shape<WIN>(a, s, TILE ? TILE : a.tile_tokens);
         fetch(a);
         all_q = it.rows_m * a.group;
     }
@@ -201,7 +202,7 @@ template <uint32_t TILE, bool WIN = false> struct Walk {
                         row0 += it.rows_m;
                         r++;
                         s = req_shape(next_owner, next_have, next_want, a.b.page, a.b.max_blocks);
-                        it = item_shape<WIN>(a, s, TILE);
+                        it = item_shape<WIN>(a, s, TILE ? TILE : a.tile_tokens);
                         fetch(a);
                     } while (it.nqt == 0);
                     all_q = it.rows_m * a.group;

@@ -8,6 +8,7 @@
 
 #include "gift_attn8.cuh"
 #include "gift_attn_join.cuh"
+#include "gift_tc.cuh"
 #include "gift_internal.cuh"
 
 using namespace gift;
@@ -18,38 +19,43 @@ namespace {
 // few query rows per K/V head: warp-level products
 // ---------------------------------------------------------------------------
 //
-// The split is that of the 16-bit kernel: every warp works on its own tokens of a tile, with a ring of 3 stages that
-// only it fills and reads, 8 KiB of codes a step.  Codes become fp16 numbers (exact) on their way
-// from shared memory to the matrix instructions:
+// The split is that of the 16-bit kernel: every warp works on its own tokens of a tile, with a ring of stages that only it
+// fills and reads, 4 KiB of codes a step.  Codes become fp16 numbers (exact) between shared
+// memory and the matrix instructions, and those conversions are most of the work: half the bytes of a 16-bit cache in
+// the time of HBM leave a warp 180 clocks of its SM for a step.  So the products are turned: K and V are the operands of 16
+// rows, the query rows the operand of 8, S^T = K Q^T and O^T = V^T P^T.  With up to 8 query rows that is half the
+// products, and half the registers: 16 warps per SM instead of 8.
 //   K   A product's order of the 128 dimensions is free, so a lane takes 16 neighbouring codes of a token with one load, and
 //       Q's fragments are laid out to match.
 //   V   Loading 8 x 8 pairs of codes transposed gives a lane two neighbouring dimensions of two neighbouring
 //       tokens; a byte permutation makes of it the fragments of an even and an odd dimension.
 // K's scale multiplies the score, V's the weight, both in 32 bits: nothing but q and the weights is
 // rounded.  Both go to fp16 by a power of two of the row's own (see top_exponent), for scales and queries of
-// any size: the weights' follows the largest p * scale so far, as the maximum follows the scores.
+// any size.  The maximum that weights are relative to, and the weights' power of two, change only when a score passes
+// the maximum by 2^6 or a weight leaves fp16: one vote a step in place of reductions over the warp.
 
-constexpr int FEW8_WARPS = 4;
-constexpr int FEW8_THREADS = FEW8_WARPS * 32;
-constexpr int FEW8_ROWS = 16;
 constexpr int FEW8_STAGES = 3;
+constexpr uint32_t FEW8_ITEMS = 32;      // of a call, before heads share a CTA
+constexpr float NOTHING = -3e38f;        // the maximum before anything is seen: finite, so that no difference with it is NaN
+constexpr float FEW8_SLACK = 6.f;        // how far, in powers of two, a score may pass the maximum in use
 
-template <int D> struct Few8 {
-    static constexpr int tok = 4096 / D;                                 // tokens of a warp's step
-    static constexpr int tile = FEW8_WARPS * tok;
-    static constexpr int stage = 2 * 4096 + tok * 8;                     // codes of K, of V, scales
-    static constexpr int ring = FEW8_WARPS * FEW8_STAGES * stage;
-    static constexpr int join = FEW8_WARPS * FEW8_ROWS * D * 4;
-    static constexpr int smem = ring > join ? ring : join;
-    // Where 16-byte chunk `chunk` of a token lies in K's and in V's part: permuted so that the lanes that
-    // load together (K: 4 chunks of 2 tokens; V: a chunk of 8 tokens) meet different banks.
-    static __device__ __forceinline__ uint32_t k_at(uint32_t token, uint32_t chunk)
+template <int D, int NR> struct Few8 {
+    static constexpr int warps = NR == 1 ? 8 : 4;                        // 2 CTAs per SM with 128 registers a thread, or
+    static constexpr int ctas = NR == 1 ? 2 : 3;                         // 3 with 168
+    static constexpr int threads = warps * 32;
+    static constexpr int rows = 8 * NR;
+    static constexpr int half = 2048;                                    // bytes of K's (or V's) codes of a step
+    static constexpr int tok = half / D;                                 // tokens of a warp's step
+    static constexpr int ring = warps * FEW8_STAGES * 2 * half;          // codes of K, of V; behind them the scales, those
+    static constexpr int scales = tok * 16;                              // of a pair of heads for each token
+    static constexpr int join = warps * rows * D * 4;
+    static constexpr int smem = ring + warps * FEW8_STAGES * scales;
+    static_assert(join <= smem, "the warps' parts lie in the ring");
+    // Where 16-byte chunk `chunk` of a token lies: permuted by the copies' 128- or 64-byte swizzle, so that lanes that
+    // load together (K: every other chunk of 2 tokens; V: a chunk of 8 tokens) meet different banks.
+    static __device__ __forceinline__ uint32_t at(uint32_t token, uint32_t chunk)
     {
-        return token * D + ((D == 128 ? chunk ^ ((token & 1u) << 2) : chunk) << 4);
-    }
-    static __device__ __forceinline__ uint32_t v_at(uint32_t token, uint32_t chunk)
-    {
-        return 4096u + token * D + ((chunk ^ (D == 128 ? token & 7u : (token >> 1) & 3u)) << 4);
+        return token * D + ((chunk ^ (D == 128 ? token & 7u : (token >> 1) & 3u)) << 4);
     }
 };
 
@@ -63,37 +69,136 @@ __device__ __forceinline__ uint4 lds128(uint32_t at)
     asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w) : "r"(at) : "memory");
     return x;
 }
-
-// NEAR: capped scores, a bias by distance or a window.
-template <class T, int D, bool NEAR>
-__global__ void __launch_bounds__(FEW8_THREADS, 2) attn8_few_kernel(const __grid_constant__ Attn8Args a)
+__device__ __forceinline__ float2 lds_pair(uint32_t at)
 {
-    using L = Few8<D>;
-    constexpr int ROWS = FEW8_ROWS, TOK = L::tok, TILE = L::tile, NT = TOK / 8;
+    float2 x;
+    asm volatile("ld.shared.v2.f32 {%0,%1}, [%2];" : "=f"(x.x), "=f"(x.y) : "r"(at) : "memory");
+    return x;
+}
+// An 8 x 8 matrix of 16-bit elements, two of a row in each lane, transposed.
+__device__ __forceinline__ uint32_t transposed(uint32_t x)
+{
+    uint32_t y;
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
+}
+// Four codes as two pairs.
+__device__ __forceinline__ void four_codes(uint32_t w, uint32_t& lo, uint32_t& hi)
+{
+    asm("{\n .reg .b16 x, y;\n mov.b32 {x, y}, %2;\n cvt.rn.f16x2.e4m3x2 %0, x;\n cvt.rn.f16x2.e4m3x2 %1, y;\n}" : "=r"(lo), "=r"(hi) : "r"(w));
+}
+
+// Two results as a pair of q's type.
+__device__ __forceinline__ uint32_t pack_out(const Attn8Args& a, float lo, float hi)
+{
+    return a.half ? pack2<__half>(lo, hi) : pack2<__nv_bfloat16>(lo, hi);
+}
+
+// Eight of a finished row's columns, from 8 ch; and with the first of them its lse.
+__device__ __forceinline__ void put_row(const Attn8Args& a, uint32_t row0, uint32_t h, uint32_t rho, uint32_t ch, const float (&acc)[8],
+                                        float top, float sum, uint32_t bits)
+{
+    const uint32_t i = a.by_group.quot(rho), hq = h * a.group + (rho - i * a.group);
+    const bool none = bits != 0u || sum == 0.f;
+    const float inv = none ? 0.f : 1.f / sum;
+    uint4 v = make_uint4(0u, 0u, 0u, 0u);
+    if (!none) {
+        v.x = pack_out(a, acc[0] * inv, acc[1] * inv); v.y = pack_out(a, acc[2] * inv, acc[3] * inv);
+        v.z = pack_out(a, acc[4] * inv, acc[5] * inv); v.w = pack_out(a, acc[6] * inv, acc[7] * inv);
+    }
+    *reinterpret_cast<uint4*>(a.out + (uint64_t)(row0 + i) * a.out_row + (uint64_t)hq * a.out_head + ch * 16) = v;
+    if (a.lse && ch == 0) a.lse[(uint64_t)(row0 + i) * a.heads + hq] = none ? NEG_INF : (top + log2f(sum)) * 0.6931471805599453f;
+}
+
+// The pieces of a cut item, for all heads of its group, joined in their order: pieces w, w + 1, ... (the first is its slice's last
+// piece, the others their slices' first ones), written while this kernel runs and read past L1.  bits: 0 when called.
+template <int D, int ROWS, int THREADS>
+__device__ __noinline__ void join8(const Attn8Args& a, const PartHead& head, uint32_t w, float2* tops, uint32_t* bits)
+{
+    constexpr uint32_t CH = D / 8;
+    const uint32_t pieces = head.pieces;
+    auto part_of = [&](uint32_t p, uint32_t hr) -> uint64_t { return (uint64_t)(2u * (w + p) + (p == 0 ? 1u : 0u)) * a.head_ways * ROWS + hr; };
+    for (uint32_t p = threadIdx.x; p < pieces; p += THREADS) {
+        const uint32_t b = __ldcg(&a.part_head[2u * (w + p) + (p == 0 ? 1u : 0u)].bits);
+        if (b) atomicOr(bits, b);
+    }
+    // maxima and sums: 8 threads per row, pieces dealt among them
+    for (uint32_t hr0 = 0; hr0 < a.head_ways * ROWS; hr0 += THREADS / 8) {
+        const uint32_t hr = hr0 + (threadIdx.x >> 3);
+        const bool there = hr < a.head_ways * ROWS && hr % ROWS < head.nr;
+        float top = NOTHING, sum = 0.f;
+        if (there)
+            for (uint32_t p = threadIdx.x & 7u; p < pieces; p += 8) {
+                const float2 ml = __ldcg(&a.part_ml[part_of(p, hr)]);
+                const float now = fmaxf(top, ml.x);
+                sum = sum * fast_exp2(top - now) + ml.y * fast_exp2(ml.x - now);
+                top = now;
+            }
+#pragma unroll
+        for (int d = 1; d < 8; d <<= 1) {
+            const float other_top = __shfl_xor_sync(0xFFFFFFFFu, top, d), other_sum = __shfl_xor_sync(0xFFFFFFFFu, sum, d);
+            const float now = fmaxf(top, other_top);
+            sum = sum * fast_exp2(top - now) + other_sum * fast_exp2(other_top - now);
+            top = now;
+        }
+        if (there && (threadIdx.x & 7u) == 0) tops[hr] = make_float2(top, sum);
+    }
+    __syncthreads();
+    for (uint32_t x = threadIdx.x; x < a.head_ways * ROWS * CH; x += THREADS) {
+        const uint32_t ch = x % CH, hr = x / CH, row = hr % ROWS;
+        if (row >= head.nr) continue;
+        const float top = tops[hr].x;
+        float acc[8];
+#pragma unroll
+        for (int e = 0; e < 8; e++) acc[e] = 0.f;
+#pragma unroll 4
+        for (uint32_t p = 0; p < pieces; p++) {
+            const uint64_t part = part_of(p, hr);
+            const float f = fast_exp2(__ldcg(&a.part_ml[part]).x - top);
+            const float4* from = reinterpret_cast<const float4*>(a.part_o + part * D + ch * 8);
+            const float4 u = __ldcg(from), v = __ldcg(from + 1);
+            acc[0] += f * u.x; acc[1] += f * u.y; acc[2] += f * u.z; acc[3] += f * u.w;
+            acc[4] += f * v.x; acc[5] += f * v.y; acc[6] += f * v.z; acc[7] += f * v.w;
+        }
+        put_row(a, head.row0, head.h * a.head_ways + hr / ROWS, head.q0 + row, ch, acc, top, tops[hr].y, *bits);
+    }
+    if (head.h == 0 && head.q0 == 0) write_request<THREADS>(a, head.r, head.row0, head.rows_m, *bits);
+}
+
+// NEAR: capped scores, a bias by distance or a window.  NR: query rows of an item by 8.
+template <int D, int NR, bool NEAR>
+__global__ void __launch_bounds__(Few8<D, NR>::threads, Few8<D, NR>::ctas) attn8_few_kernel(const __grid_constant__ Attn8Args a)
+{
+    using L = Few8<D, NR>;
+    constexpr int ROWS = L::rows, TOK = L::tok, MT = TOK / 16, THREADS = L::threads;
     constexpr int CH = D / 8;                      // 16-byte chunks of a result's row
     constexpr int KCH = D / 16;                    // 16-byte chunks of a token's codes
-    extern __shared__ __align__(128) char smem[];
+    extern __shared__ __align__(1024) char smem[];
     __shared__ PlaceShared place;
-    __shared__ float2 s_ml[FEW8_WARPS][ROWS];
+    __shared__ float2 s_ml[L::warps][ROWS];
     __shared__ uint32_t s_bits, s_last, s_first;
-    __shared__ JoinShared s_join;
+    __shared__ float2 s_top[L::warps * ROWS];
     __shared__ PartHead s_head;
 
+    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     uint64_t total, slice;
-    if (!place_unit<FEW8_THREADS, NEAR>(a, blockIdx.x, TILE, blockIdx.x == 0, &place, &total, &slice)) {
+    if (!place_unit<THREADS, NEAR>(a, blockIdx.x, a.tile_tokens, blockIdx.x == 0, &place, &total, &slice)) {
         leave_tickets(a);
         return;
     }
-    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const uint32_t ring = (uint32_t)__cvta_generic_to_shared(smem) + warp * (FEW8_STAGES * L::stage);
+    const uint32_t ring = smem_u32(smem) + warp * (FEW8_STAGES * 2 * L::half);
+    const uint32_t scale_ring = smem_u32(smem) + L::ring + warp * (FEW8_STAGES * L::scales);
+    uint32_t put = 0, get = 0;                     // stage to fill, to read
 
-    Walk<TILE, NEAR> w;
+    // this warp's head of a group, its tokens of a tile
+    const uint32_t head_way = warp & (a.head_ways - 1u), first_token = warp / a.head_ways * TOK;
+    Walk<0, NEAR> w;
     const uint64_t begin = slice * blockIdx.x, units = slice < total - begin ? slice : total - begin;
     w.start(a, place.at, 0, units);
     while (w.next(a)) {
         const ReqShape& s = w.s;
         const ItemShape& it = w.it;
-        const uint32_t r = w.r, row0 = w.row0, tb = w.tb + (NEAR ? it.first : 0u), n_tiles = w.n_tiles, h = w.h;
+        const uint32_t r = w.r, row0 = w.row0, tb = w.tb + (NEAR ? it.first : 0u), n_tiles = w.n_tiles, h = w.h * a.head_ways + head_way;
         const uint32_t all_q = it.rows_m * a.group;                // query rows of the K/V head
         const uint32_t q0 = w.qt * ROWS;
         const int32_t owner = a.b.owner[r];
@@ -102,26 +207,26 @@ __global__ void __launch_bounds__(FEW8_THREADS, 2) attn8_few_kernel(const __grid
         const uint32_t low = NEAR ? first_seen(a, s.have) : 0u;    // tokens before it are nobody's to see
         uint32_t bits = masked_short ? GIFT_ST_BAD_DESC : 0u;
 
-        // this lane's query rows g and g + 8; its dimensions are 16 from 16 (c + 4 i)
+        // Fragments of query rows g (+ 8); this lane's dimensions are 16 from 16 (c D / 64 + i).  Scores, weights and results
+        // are those of query rows 2 c, 2 c + 1 (+ 8).
         const uint32_t g = lane >> 2, c = lane & 3u;
-        uint32_t qf[D / 16][4];
-        uint32_t row_i[2];
-        float qs[2], slope[2];
+        uint32_t qf[NR][D / 16][2];
+        float qs[NR][2], slope[NR][2];
+        uint32_t row_i[NR][2];
 #pragma unroll
-        for (int half = 0; half < 2; half++) {
-            const uint32_t rho = q0 + half * 8 + g;
+        for (int n = 0; n < NR; n++) {
+            const uint32_t rho = q0 + n * 8 + g;
             const bool there = rho < all_q;
             const uint32_t i = there ? a.by_group.quot(rho) : 0u, hq = h * a.group + (there ? rho - i * a.group : 0u);
-            row_i[half] = i;
             const uint4* q = reinterpret_cast<const uint4*>(a.q + (uint64_t)(row0 + i) * a.q_row + (uint64_t)hq * a.q_head);
             uint32_t x[D / 8];
 #pragma unroll
             for (int y = 0; y < D / 32; y++) {
-                const uint4 v = there ? q[(c + 4 * (y >> 1)) * 2 + (y & 1)] : make_uint4(0u, 0u, 0u, 0u);
+                const uint4 v = there ? q[c * (D / 32) + y] : make_uint4(0u, 0u, 0u, 0u);
                 x[4 * y] = v.x; x[4 * y + 1] = v.y; x[4 * y + 2] = v.z; x[4 * y + 3] = v.w;
             }
-            qs[half] = NEAR && a.cap_out != 0.f ? a.cap_in : a.scale_log2;
-            if constexpr (!std::is_same<T, __half>::value) {
+            float scale = NEAR && a.cap_out != 0.f ? a.cap_in : a.scale_log2;
+            if (!a.half) {
                 uint32_t top = 0u;
 #pragma unroll
                 for (int y = 0; y < D / 8; y++) top = max(top, max(x[y] << 16 & 0x7FFFFFFFu, x[y] & 0x7FFF0000u));
@@ -129,74 +234,95 @@ __global__ void __launch_bounds__(FEW8_THREADS, 2) attn8_few_kernel(const __grid
                 top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
                 const uint32_t e = top_exponent(top);
                 const float f = to_half_range(e);
-                qs[half] *= from_half_range(e);
+                scale *= from_half_range(e);
 #pragma unroll
                 for (int y = 0; y < D / 8; y++)
                     x[y] = pack2<__half>(__uint_as_float(x[y] << 16) * f, __uint_as_float(x[y] & 0xFFFF0000u) * f);
             }
 #pragma unroll
             for (int ks = 0; ks < D / 16; ks++) {
-                qf[ks][half] = x[2 * ks];
-                qf[ks][2 + half] = x[2 * ks + 1];
+                qf[n][ks][0] = x[2 * ks];
+                qf[n][ks][1] = x[2 * ks + 1];
             }
-            slope[half] = NEAR && a.slopes && there ? a.slopes[hq] * LOG2_E : 0.f;
+#pragma unroll
+            for (int j = 0; j < 2; j++) {
+                const uint32_t rho_j = q0 + n * 8 + 2 * c + j;
+                const bool there_j = rho_j < all_q;
+                row_i[n][j] = there_j ? a.by_group.quot(rho_j) : 0u;
+                qs[n][j] = __shfl_sync(0xFFFFFFFFu, scale, (2 * c + j) * 4);
+                slope[n][j] = NEAR && a.slopes && there_j ? a.slopes[h * a.group + rho_j - row_i[n][j] * a.group] * LOG2_E : 0.f;
+            }
         }
-        float o[D / 8][4];
-        float m[2] = {NEG_INF, NEG_INF}, l[2] = {0.f, 0.f};
-        float most[2] = {0.f, 0.f};                                // largest p * scale, relative to the maximum
-        uint32_t ew[2] = {13u, 13u};                               // its exponent: o is in units of from_half_range
+        float o[D / 16][NR][4];
+        float m[NR][2], l[NR][2];                                  // the maximum in use, the sum relative to it
+        float most[NR][2];                                         // the weight that their power of two goes by:
+        float to_half[NR][2], room[NR][2];                         // the factor, and the weight that it serves at most
 #pragma unroll
-        for (int n = 0; n < D / 8; n++)
+        for (int n = 0; n < NR; n++) {
 #pragma unroll
-            for (int e = 0; e < 4; e++) o[n][e] = 0.f;
+            for (int j = 0; j < 2; j++) { m[n][j] = NOTHING; l[n][j] = most[n][j] = 0.f; to_half[n][j] = to_half_range(9u); room[n][j] = half_range_end(9u); }
+#pragma unroll
+            for (int x = 0; x < D / 16; x++)
+#pragma unroll
+                for (int e = 0; e < 4; e++) o[x][n][e] = 0.f;
+        }
 
-        // Lane x looks after tokens x (and x + 32) of the warp's: table entries are fetched one step ahead of
-        // the copies that need them, labels judged one step after they were asked for.
-        int32_t next[TOK / 32], label[TOK / 32];
-        auto entry = [&](uint32_t step, int e) -> int32_t {
-            const uint32_t t = (tb + step) * TILE + warp * TOK + e * 32 + lane;
+        // Lane x looks after token x % TOK of the warp's: its table entry is fetched one step ahead of
+        // the copies that need it, its label judged one step after it was asked for.
+        const uint32_t my = lane % TOK, chunk = lane % KCH;
+        const char* head = a.pages + (uint64_t)h * D + chunk * 16;
+        const uint32_t row_bytes = (lane / KCH) * (uint32_t)a.token_bytes, rows_bytes = (32 / KCH) * (uint32_t)a.token_bytes;
+        // a token's entry, if any row may see it
+        auto entry = [&](uint32_t step) -> int32_t {
+            const uint32_t t = (tb + step) * a.tile_tokens + first_token + my;
             return step < n_tiles && t < s.want && (!NEAR || t >= low) ? table[a.b.page.quot(t)] : -1;
         };
-#pragma unroll
-        for (int e = 0; e < TOK / 32; e++) {
-            next[e] = entry(0, e);
-            label[e] = GIFT_OWNER_PARAM;
-        }
+        int32_t next = entry(0), label = GIFT_OWNER_PARAM;
         auto issue = [&](uint32_t step) {
             if (step < n_tiles) {
-                const uint32_t base = ring + (step % FEW8_STAGES) * L::stage;
-                uint32_t slot[TOK / 32];
-#pragma unroll
-                for (int e = 0; e < TOK / 32; e++) {
-                    const uint32_t t = (tb + step) * TILE + warp * TOK + e * 32 + lane;
-                    const int32_t page = next[e];
-                    next[e] = entry(step + 1, e);
-                    bits |= label_read_status(label[e], owner);
-                    label[e] = GIFT_OWNER_PARAM;
-                    // the token's slot; rows that nobody sees are filled with zeros: what memory holds there does not matter
-                    slot[e] = 0xFFFFFFFFu;
-                    if (t < s.want && (!NEAR || t >= low)) {
-                        if ((uint32_t)page < a.b.n_pages) {
-                            slot[e] = (uint32_t)page * a.b.page_tokens + (t - a.b.page.quot(t) * a.b.page_tokens);
-                            if (a.owner_map) label[e] = a.owner_map[page];
-                        } else {
-                            bits |= GIFT_ST_BAD_DESC;
-                        }
+                const uint32_t base = ring + put * (2 * L::half), scales = scale_ring + put * L::scales + (h & 1u) * 8u;
+                const uint32_t t0 = (tb + step) * a.tile_tokens + first_token, t = t0 + my;
+                const int32_t page = next;
+                next = entry(step + 1);
+                bits |= label_read_status(label, owner);
+                label = GIFT_OWNER_PARAM;
+                // the token's slot; tokens that nobody sees are filled with zeros: what memory holds there does not matter
+                uint32_t slot = 0xFFFFFFFFu;
+                if (t < s.want && (!NEAR || t >= low)) {
+                    if ((uint32_t)page < a.b.n_pages) {
+                        slot = (uint32_t)page * a.b.page_tokens + (t - a.b.page.quot(t) * a.b.page_tokens);
+                        if (a.owner_map) label = a.owner_map[page];
+                    } else {
+                        bits |= GIFT_ST_BAD_DESC;
                     }
-                    const bool there = slot[e] != 0xFFFFFFFFu;
-                    cp_async8(base + 8192u + (e * 32 + lane) * 8u, a.pages + (there ? slot[e] * a.token_bytes + 2ull * a.codes + h * 8u : 0ull), there ? 8u : 0u);
                 }
-                const uint32_t chunk = lane % KCH;
-                const char* head = a.pages + (uint64_t)h * D + chunk * 16;
+                if (a.whole_steps && __all_sync(0xFFFFFFFFu, slot != 0xFFFFFFFFu)) {
+                    // the step lies in one page: its tokens follow one another
+                    const char* p = a.pages + (uint64_t)slot * a.token_bytes;
+                    if (TOK == 32 || lane < TOK) cp_async8(scales + my * 16u, p + 2u * a.codes + h * 8u, 8u);
+                    p = head + (uint64_t)(slot - my) * a.token_bytes + row_bytes;
 #pragma unroll
-                for (int i = 0; i < KCH * TOK / 32; i++) {
-                    const uint32_t row = i * (32 / KCH) + lane / KCH;
-                    const uint32_t from = __shfl_sync(0xFFFFFFFFu, slot[i * (32 / KCH) / 32], row & 31u);
-                    const bool there = from != 0xFFFFFFFFu;
-                    const char* p = there ? head + from * a.token_bytes : head;
-                    cp_async16(base + L::k_at(row, chunk), p, there ? 16u : 0u);
-                    cp_async16(base + L::v_at(row, chunk), p + a.codes, there ? 16u : 0u);
+                    for (int i = 0; i < KCH * TOK / 32; i++) {
+                        cp_async16(base + L::at(i * (32 / KCH) + lane / KCH, chunk), p, 16u);
+                        cp_async16(base + L::half + L::at(i * (32 / KCH) + lane / KCH, chunk), p + a.codes, 16u);
+                        p += rows_bytes;
+                    }
+                } else {
+                    if (TOK == 32 || lane < TOK) {
+                        const bool there = slot != 0xFFFFFFFFu;
+                        cp_async8(scales + my * 16u, a.pages + (there ? slot * a.token_bytes + 2ull * a.codes + h * 8u : 0ull), there ? 8u : 0u);
+                    }
+#pragma unroll
+                    for (int i = 0; i < KCH * TOK / 32; i++) {
+                        const uint32_t row = i * (32 / KCH) + lane / KCH;
+                        const uint32_t from = __shfl_sync(0xFFFFFFFFu, slot, row);
+                        const bool there = from != 0xFFFFFFFFu;
+                        const char* p = there ? head + from * a.token_bytes : head;
+                        cp_async16(base + L::at(row, chunk), p, there ? 16u : 0u);
+                        cp_async16(base + L::half + L::at(row, chunk), p + a.codes, there ? 16u : 0u);
+                    }
                 }
+                put = put == FEW8_STAGES - 1 ? 0u : put + 1u;
             }
             cp_commit();
         };
@@ -208,8 +334,8 @@ __global__ void __launch_bounds__(FEW8_THREADS, 2) attn8_few_kernel(const __grid
             const uint32_t step = round - (FEW8_STAGES - 1);
             cp_wait<FEW8_STAGES - 1>();
             __syncwarp();
-            const uint32_t base = ring + (step % FEW8_STAGES) * L::stage;
-            const uint32_t t0 = (tb + step) * TILE + warp * TOK;
+            const uint32_t base = ring + get * (2 * L::half), scales = scale_ring + get * L::scales + (h & 1u) * 8u;
+            const uint32_t t0 = (tb + step) * a.tile_tokens + first_token;
             // some rows may not see some of these tokens
             const bool mixed = t0 + TOK > s.have || (NEAR && a.window && t0 + a.window < s.want);
             if (mixed) {
@@ -217,206 +343,255 @@ __global__ void __launch_bounds__(FEW8_THREADS, 2) attn8_few_kernel(const __grid
                 // scale, which is only used where the token is seen
                 bool odd = false;
 #pragma unroll
-                for (int i = 0; i < 8; i++) {
-                    const uint4 x = lds128(base + 4096u + (i * 32 + lane) * 16);
+                for (int i = 0; i < L::half / 512; i++) {
+                    const uint4 x = lds128(base + L::half + (i * 32 + lane) * 16);
                     odd |= codes_nan(x.x) || codes_nan(x.y) || codes_nan(x.z) || codes_nan(x.w);
                 }
                 if (__any_sync(0xFFFFFFFFu, odd)) {
 #pragma unroll 1
-                    for (int i = 0; i < 32; i++) {
+                    for (int i = 0; i < L::half / 128; i++) {
                         const uint32_t at = (i * 32 + lane) * 4;
                         uint32_t x;
-                        asm volatile("ld.shared.u32 %0, [%1];" : "=r"(x) : "r"(base + 4096u + at) : "memory");
+                        asm volatile("ld.shared.u32 %0, [%1];" : "=r"(x) : "r"(base + L::half + at) : "memory");
                         if (codes_nan(x)) {
-                            asm volatile("st.shared.u32 [%0], %1;" ::"r"(base + 4096u + at), "r"(codes_without_nan(x)) : "memory");
-                            asm volatile("st.shared.u32 [%0], %1;" ::"r"(base + 8192u + (at / D) * 8u + 4u), "r"(0x7FC00000u) : "memory");
+                            const uint32_t token = at / D;
+                            asm volatile("st.shared.u32 [%0], %1;" ::"r"(base + L::half + at), "r"(codes_without_nan(x)) : "memory");
+                            asm volatile("st.shared.u32 [%0], %1;" ::"r"(scales + token * 16u + 4u), "r"(0x7FC00000u) : "memory");
                         }
                     }
                     __syncwarp();
                 }
             }
-            float sc[NT][4], vs[NT][2];
+            float sc[MT][NR][4], vs[MT][2];
 #pragma unroll
-            for (int n = 0; n < NT; n++) {
+            for (int x = 0; x < MT; x++) {
 #pragma unroll
-                for (int e = 0; e < 4; e++) sc[n][e] = 0.f;
+                for (int n = 0; n < NR; n++)
+#pragma unroll
+                    for (int e = 0; e < 4; e++) sc[x][n][e] = 0.f;
 #pragma unroll
                 for (int i = 0; i < D / 64; i++) {
-                    const uint4 k = lds128(base + L::k_at(n * 8 + g, c + 4 * i));
-                    mma16816<__half>(sc[n], qf[i * 4], codes_to_half2(k.x & 0xFFFFu), codes_to_half2(k.x >> 16));
-                    mma16816<__half>(sc[n], qf[i * 4 + 1], codes_to_half2(k.y & 0xFFFFu), codes_to_half2(k.y >> 16));
-                    mma16816<__half>(sc[n], qf[i * 4 + 2], codes_to_half2(k.z & 0xFFFFu), codes_to_half2(k.z >> 16));
-                    mma16816<__half>(sc[n], qf[i * 4 + 3], codes_to_half2(k.w & 0xFFFFu), codes_to_half2(k.w >> 16));
-                }
-                const uint4 x = lds128(base + 8192u + (n * 8 + c * 2) * 8u);
-                const float ks[2] = {__uint_as_float(x.x), __uint_as_float(x.z)};
-                vs[n][0] = __uint_as_float(x.y);
-                vs[n][1] = __uint_as_float(x.w);
+                    const uint4 k0 = lds128(base + L::at(x * 16 + g, c * (D / 64) + i)), k1 = lds128(base + L::at(x * 16 + 8 + g, c * (D / 64) + i));
+                    const uint32_t w0[4] = {k0.x, k0.y, k0.z, k0.w}, w1[4] = {k1.x, k1.y, k1.z, k1.w};
 #pragma unroll
-                for (int e = 0; e < 4; e++) {
-                    sc[n][e] *= ks[e & 1] * qs[e >> 1];
-                    if constexpr (NEAR) {
-                        if (a.cap_out != 0.f) sc[n][e] = a.cap_out * tanh_of(sc[n][e]);
-                        const int32_t away = (int32_t)(t0 + n * 8 + c * 2 + (e & 1)) - (int32_t)(s.have + row_i[e >> 1]);
-                        if (a.slopes) sc[n][e] += slope[e >> 1] * (float)away;
+                    for (int y = 0; y < 4; y++) {
+                        uint32_t f[4];
+                        four_codes(w0[y], f[0], f[2]);
+                        four_codes(w1[y], f[1], f[3]);
+#pragma unroll
+                        for (int n = 0; n < NR; n++) mma16816<__half>(sc[x][n], f, qf[n][i * 4 + y][0], qf[n][i * 4 + y][1]);
                     }
                 }
+#pragma unroll
+                for (int e2 = 0; e2 < 2; e2++) {
+                    const float2 ks_vs = lds_pair(scales + (x * 16 + e2 * 8 + g) * 16u);
+                    vs[x][e2] = ks_vs.y;
+#pragma unroll
+                    for (int n = 0; n < NR; n++)
+#pragma unroll
+                        for (int j = 0; j < 2; j++) {
+                            float& y = sc[x][n][2 * e2 + j];
+                            y *= ks_vs.x * qs[n][j];
+                            if constexpr (NEAR) {
+                                if (a.cap_out != 0.f) y = a.cap_out * tanh_of(y);
+                                const int32_t away = (int32_t)(t0 + x * 16 + e2 * 8 + g) - (int32_t)(s.have + row_i[n][j]);
+                                if (a.slopes) y += slope[n][j] * (float)away;
+                            }
+                        }
+                }
             }
-            uint64_t sees[2] = {~0ull, ~0ull};
+            uint32_t sees[NR][2];                      // of the step's tokens, by row: bit x is token x * 8 + g
             if (mixed) {
                 const bool none = masked_short || t0 >= s.want;
 #pragma unroll
-                for (int half = 0; half < 2; half++) {
-                    sees[half] = none ? 0ull : row_sees64(a, s.have, s.want, row0 + row_i[half], row_i[half], t0);
-                    if (NEAR && a.window) sees[half] &= in_window64(a.window, s.have + row_i[half], t0);
-                }
+                for (int n = 0; n < NR; n++)
 #pragma unroll
-                for (int n = 0; n < NT; n++)
+                    for (int j = 0; j < 2; j++) {
+                        uint32_t all = none ? 0u : (uint32_t)row_sees64(a, s.have, s.want, row0 + row_i[n][j], row_i[n][j], t0);
+                        if (NEAR && a.window) all &= (uint32_t)in_window64(a.window, s.have + row_i[n][j], t0);
+                        sees[n][j] = all >> g;
 #pragma unroll
-                    for (int e = 0; e < 4; e++)
-                        if (!(sees[e >> 1] >> (n * 8 + c * 2 + (e & 1)) & 1ull)) sc[n][e] = NEG_INF;
-            }
-            float ratio[2];
-#pragma unroll
-            for (int half = 0; half < 2; half++) {
-                float top = fmaxf(sc[0][half * 2], sc[0][half * 2 + 1]);
-#pragma unroll
-                for (int n = 1; n < NT; n++) top = fmaxf(top, fmaxf(sc[n][half * 2], sc[n][half * 2 + 1]));
-                top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
-                top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
-                const float now = fmaxf(m[half], top);
-                const float use = now == NEG_INF ? 0.f : now;          // nothing seen yet: exp2(-inf - 0) = 0
-                const float alpha = fast_exp2(m[half] - use);
-                m[half] = now;
-                float sum = 0.f, big = 0.f;
-#pragma unroll
-                for (int n = 0; n < NT; n++)
-#pragma unroll
-                    for (int e = 0; e < 2; e++) {
-                        const float p = fast_exp2(sc[n][half * 2 + e] - use);
-                        sum += p;
-                        float x = p * vs[n][e];
-                        if (mixed && !(sees[half] >> (n * 8 + c * 2 + e) & 1ull)) x = 0.f;
-                        sc[n][half * 2 + e] = x;
-                        big = fmaxf(big, x);
+                        for (int x = 0; x < 2 * MT; x++)
+                            if (!(sees[n][j] >> (x * 8) & 1u)) sc[x >> 1][n][2 * (x & 1) + j] = NEG_INF;
                     }
-                l[half] = l[half] * alpha + sum;
-                big = fmaxf(big, __shfl_xor_sync(0xFFFFFFFFu, big, 1));
-                big = fmaxf(big, __shfl_xor_sync(0xFFFFFFFFu, big, 2));
-                most[half] = fmaxf(most[half] * alpha, big);
-                const uint32_t e = top_exponent(__float_as_uint(most[half]));
-                ratio[half] = alpha * from_half_range(ew[half]) * to_half_range(e);
-                ew[half] = e;
             }
-            if (__any_sync(0xFFFFFFFFu, ratio[0] != 1.f || ratio[1] != 1.f)) {
+            float alpha[NR][2];
+            bool grow = false;
+            float top[NR][2];
 #pragma unroll
-                for (int n = 0; n < D / 8; n++) {
-                    o[n][0] *= ratio[0]; o[n][1] *= ratio[0];
-                    o[n][2] *= ratio[1]; o[n][3] *= ratio[1];
+            for (int n = 0; n < NR; n++)
+#pragma unroll
+                for (int j = 0; j < 2; j++) {
+                    top[n][j] = fmaxf(sc[0][n][j], sc[0][n][2 + j]);
+#pragma unroll
+                    for (int x = 1; x < MT; x++) top[n][j] = fmaxf(top[n][j], fmaxf(sc[x][n][j], sc[x][n][2 + j]));
+                    grow |= top[n][j] > m[n][j] + FEW8_SLACK;          // also when nothing has been seen yet
+                    alpha[n][j] = 1.f;
                 }
+            grow = __any_sync(0xFFFFFFFFu, grow);
+            if (grow) {
+#pragma unroll
+                for (int n = 0; n < NR; n++)
+#pragma unroll
+                    for (int j = 0; j < 2; j++) {
+#pragma unroll
+                        for (int d = 4; d < 32; d <<= 1) top[n][j] = fmaxf(top[n][j], __shfl_xor_sync(0xFFFFFFFFu, top[n][j], d));
+                        const float now = fmaxf(m[n][j], top[n][j]);
+                        alpha[n][j] = fast_exp2(m[n][j] - now);
+                        m[n][j] = now;
+                        l[n][j] *= alpha[n][j];
+                    }
+            }
+            bool out = grow;
+            float big[NR][2];
+#pragma unroll
+            for (int n = 0; n < NR; n++)
+#pragma unroll
+                for (int j = 0; j < 2; j++) {
+                    big[n][j] = 0.f;
+#pragma unroll
+                    for (int x = 0; x < 2 * MT; x++) {
+                        float& y = sc[x >> 1][n][2 * (x & 1) + j];
+                        const float p = fast_exp2(y - m[n][j]);
+                        l[n][j] += p;
+                        y = p * vs[x >> 1][x & 1];
+                        if (mixed && !(sees[n][j] >> (x * 8) & 1u)) y = 0.f;
+                        big[n][j] = fmaxf(big[n][j], y);
+                    }
+                    out |= big[n][j] > room[n][j];
+                }
+            if (__any_sync(0xFFFFFFFFu, out)) {
+                float ratio[NR][2];
+#pragma unroll
+                for (int n = 0; n < NR; n++)
+#pragma unroll
+                    for (int j = 0; j < 2; j++) {
+#pragma unroll
+                        for (int d = 4; d < 32; d <<= 1) big[n][j] = fmaxf(big[n][j], __shfl_xor_sync(0xFFFFFFFFu, big[n][j], d));
+                        most[n][j] = fmaxf(most[n][j] * alpha[n][j], big[n][j]);
+                        const uint32_t e = top_exponent(__float_as_uint(most[n][j]));
+                        const float f = to_half_range(e);
+                        ratio[n][j] = alpha[n][j] * inverse_power(to_half[n][j]) * f;              // powers of two but for alpha
+                        to_half[n][j] = f;
+                        room[n][j] = half_range_end(e);
+                    }
+#pragma unroll
+                for (int x = 0; x < D / 16; x++)
+#pragma unroll
+                    for (int n = 0; n < NR; n++)
+#pragma unroll
+                        for (int e = 0; e < 4; e++) o[x][n][e] *= ratio[n][e & 1];
             }
             // Weights in fp16, 2^-11 relative at most; the sum of the weights takes them unrounded.
-            const float f0 = to_half_range(ew[0]), f1 = to_half_range(ew[1]);
-            uint32_t pf[TOK / 16][4];
+            uint32_t pf[MT][NR][2];
 #pragma unroll
-            for (int k = 0; k < TOK / 16; k++)
+            for (int n = 0; n < NR; n++) {
+                const float f0 = to_half[n][0], f1 = to_half[n][1];
 #pragma unroll
-                for (int x = 0; x < 2; x++) {
-                    pf[k][2 * x] = pack2<__half>(sc[2 * k + x][0] * f0, sc[2 * k + x][1] * f0);
-                    pf[k][2 * x + 1] = pack2<__half>(sc[2 * k + x][2] * f1, sc[2 * k + x][3] * f1);
-                }
+                for (int x = 0; x < 2 * MT; x++)
+                    pf[x >> 1][n][x & 1] = transposed(pack2<__half>(sc[x >> 1][n][2 * (x & 1)] * f0, sc[x >> 1][n][2 * (x & 1) + 1] * f1));
+            }
+            if constexpr (MT == 1) {
 #pragma unroll
-            for (int np = 0; np < D / 16; np++)
+                for (int np = 0; np < D / 16; np += 2) {
+                    uint32_t v[4];                     // 16 tokens of chunk np, of chunk np + 1
+                    ldsm4t(v, base + L::half + L::at(lane & 15u, np + (lane >> 4)));
 #pragma unroll
-                for (int k = 0; k < TOK / 32; k++) {
-                    uint32_t v[4];
-                    ldsm4t(v, base + L::v_at(k * 32 + lane, np));
+                    for (int y = 0; y < 2; y++) {
+                        uint32_t f[4];
+                        four_codes(__byte_perm(v[2 * y], 0u, 0x3120), f[0], f[1]);
+                        four_codes(__byte_perm(v[2 * y + 1], 0u, 0x3120), f[2], f[3]);
 #pragma unroll
-                    for (int x = 0; x < 4; x++) v[x] = __byte_perm(v[x], 0u, 0x3120);
-#pragma unroll
-                    for (int x = 0; x < 2; x++) {
-                        mma16816<__half>(o[np * 2], pf[2 * k + x], codes_to_half2(v[2 * x] & 0xFFFFu), codes_to_half2(v[2 * x + 1] & 0xFFFFu));
-                        mma16816<__half>(o[np * 2 + 1], pf[2 * k + x], codes_to_half2(v[2 * x] >> 16), codes_to_half2(v[2 * x + 1] >> 16));
+                        for (int n = 0; n < NR; n++) mma16816<__half>(o[np + y][n], f, pf[0][n][0], pf[0][n][1]);
                     }
                 }
-            __syncwarp();                              // the stage may be filled again
-        }
+            } else {
 #pragma unroll
-        for (int e = 0; e < TOK / 32; e++) bits |= label_read_status(label[e], owner);
+                for (int np = 0; np < D / 16; np++) {
+                    uint32_t v[4];                     // 32 tokens of chunk np
+                    ldsm4t(v, base + L::half + L::at(lane, np));
+#pragma unroll
+                    for (int y = 0; y < 2; y++) {
+                        uint32_t f[4];
+                        four_codes(__byte_perm(v[2 * y], 0u, 0x3120), f[0], f[1]);
+                        four_codes(__byte_perm(v[2 * y + 1], 0u, 0x3120), f[2], f[3]);
+#pragma unroll
+                        for (int n = 0; n < NR; n++) mma16816<__half>(o[np][n], f, pf[y][n][0], pf[y][n][1]);
+                    }
+                }
+            }
+            __syncwarp();                              // the stage may be filled again
+            get = get == FEW8_STAGES - 1 ? 0u : get + 1u;
+        }
+        bits |= label_read_status(label, owner);
         cp_wait<0>();
 
-        // Join the four warps' parts.
+        // Join the warps' parts.
 #pragma unroll
-        for (int half = 0; half < 2; half++) {
-            l[half] += __shfl_xor_sync(0xFFFFFFFFu, l[half], 1);
-            l[half] += __shfl_xor_sync(0xFFFFFFFFu, l[half], 2);
-            if (c == 0) s_ml[warp][half * 8 + g] = make_float2(m[half], l[half]);
-        }
+        for (int n = 0; n < NR; n++)
+#pragma unroll
+            for (int j = 0; j < 2; j++) {
+#pragma unroll
+                for (int d = 4; d < 32; d <<= 1) l[n][j] += __shfl_xor_sync(0xFFFFFFFFu, l[n][j], d);
+                if (g == 0) s_ml[warp][n * 8 + 2 * c + j] = make_float2(m[n][j], l[n][j]);
+            }
         bits = __reduce_or_sync(0xFFFFFFFFu, bits);
         if (threadIdx.x == 0) s_bits = 0u;
         __syncthreads();                               // the ring is idle; s_ml is complete
         if (lane == 0 && bits) atomicOr(&s_bits, bits);
+        const uint32_t nr = all_q - q0 < (uint32_t)ROWS ? all_q - q0 : (uint32_t)ROWS;
         float* join = reinterpret_cast<float*>(smem) + (uint32_t)warp * (ROWS * D);
-        const float unit[2] = {from_half_range(ew[0]), from_half_range(ew[1])};
 #pragma unroll
-        for (int np = 0; np < D / 16; np++)
+        for (int n = 0; n < NR; n++)
 #pragma unroll
-            for (int half = 0; half < 2; half++)
-                // a lane's columns 2 c, 2 c + 1 are dimensions 4 c, 4 c + 2 of the even product, 4 c + 1, 4 c + 3 of the odd one
-                *reinterpret_cast<float4*>(join + (half * 8 + g) * D + np * 16 + 4 * c) =
-                    make_float4(o[np * 2][half * 2] * unit[half], o[np * 2 + 1][half * 2] * unit[half],
-                                o[np * 2][half * 2 + 1] * unit[half], o[np * 2 + 1][half * 2 + 1] * unit[half]);
+            for (int j = 0; j < 2; j++) {
+                const uint32_t row = n * 8 + 2 * c + j;
+                const float unit = inverse_power(to_half[n][j]);
+                if (row < nr)
+#pragma unroll
+                    for (int np = 0; np < D / 16; np++)
+                        *reinterpret_cast<float2*>(join + row * D + np * 16 + 2 * g) = make_float2(o[np][n][j] * unit, o[np][n][2 + j] * unit);
+            }
         __syncthreads();
         bits = s_bits;
         const bool whole = w.whole();
-        const uint32_t at = w.slot();
-        const uint32_t nr = all_q - q0 < (uint32_t)ROWS ? all_q - q0 : (uint32_t)ROWS;
-        for (uint32_t x = threadIdx.x; x < nr * (uint32_t)CH; x += FEW8_THREADS) {
-            const uint32_t row = x / CH, ch = x % CH;
-            float top = NEG_INF;
-#pragma unroll
-            for (int y = 0; y < FEW8_WARPS; y++) top = fmaxf(top, s_ml[y][row].x);
-            const float use = top == NEG_INF ? 0.f : top;
+        const uint32_t at = w.slot() * a.head_ways;    // the first of the heads' parts
+        const uint32_t heads_rows = a.head_ways * ROWS;
+        for (uint32_t x = threadIdx.x; x < heads_rows * CH; x += THREADS) {
+            const uint32_t ch = x % CH, row = x / CH % ROWS, hw = x / (CH * ROWS);
+            if (row >= nr) continue;
+            float top = NOTHING;
+            for (uint32_t y = hw; y < (uint32_t)L::warps; y += a.head_ways) top = fmaxf(top, s_ml[y][row].x);
             float sum = 0.f, acc[8];
 #pragma unroll
             for (int e = 0; e < 8; e++) acc[e] = 0.f;
-#pragma unroll
-            for (int y = 0; y < FEW8_WARPS; y++) {
-                const float f = fast_exp2(s_ml[y][row].x - use);
+            for (uint32_t y = hw; y < (uint32_t)L::warps; y += a.head_ways) {
+                const float f = fast_exp2(s_ml[y][row].x - top);
                 sum += s_ml[y][row].y * f;
                 const float4* from = reinterpret_cast<const float4*>(reinterpret_cast<const float*>(smem) + (y * ROWS + row) * D + ch * 8);
                 const float4 u = from[0], v = from[1];
-                // a warp that saw nothing holds zeros, and f is 0
+                // a warp that saw nothing holds zeros
                 acc[0] += f * u.x; acc[1] += f * u.y; acc[2] += f * u.z; acc[3] += f * u.w;
                 acc[4] += f * v.x; acc[5] += f * v.y; acc[6] += f * v.z; acc[7] += f * v.w;
             }
             if (whole) {
-                const uint32_t rho = q0 + row, i = a.by_group.quot(rho), hq = h * a.group + (rho - i * a.group);
-                const bool none = bits != 0u || sum == 0.f;
-                const float inv = none ? 0.f : 1.f / sum;
-                uint4 v = make_uint4(0u, 0u, 0u, 0u);
-                if (!none) {
-                    v.x = pack2<T>(acc[0] * inv, acc[1] * inv); v.y = pack2<T>(acc[2] * inv, acc[3] * inv);
-                    v.z = pack2<T>(acc[4] * inv, acc[5] * inv); v.w = pack2<T>(acc[6] * inv, acc[7] * inv);
-                }
-                *reinterpret_cast<uint4*>(a.out + (uint64_t)(row0 + i) * a.out_row + (uint64_t)hq * a.out_head + ch * 16) = v;
-                if (a.lse && ch == 0)
-                    a.lse[(uint64_t)(row0 + i) * a.heads + hq] = none ? NEG_INF : (top + log2f(sum)) * 0.6931471805599453f;
+                put_row(a, row0, w.h * a.head_ways + hw, q0 + row, ch, acc, top, sum, bits);
             } else {
-                float4* to = reinterpret_cast<float4*>(a.part_o + ((uint64_t)at * ROWS + row) * D + ch * 8);
+                const uint64_t part = (uint64_t)(at + hw) * ROWS + row;
+                float4* to = reinterpret_cast<float4*>(a.part_o + part * D + ch * 8);
                 to[0] = make_float4(acc[0], acc[1], acc[2], acc[3]);
                 to[1] = make_float4(acc[4], acc[5], acc[6], acc[7]);
-                if (ch == 0) a.part_ml[(uint64_t)at * ROWS + row] = make_float2(top, sum);
+                if (ch == 0) a.part_ml[part] = make_float2(top, sum);
             }
         }
         if (whole) {
-            if (h == 0 && w.qt == 0) write_request<FEW8_THREADS>(a, r, row0, it.rows_m, bits);
+            if (w.h == 0 && w.qt == 0) write_request<THREADS>(a, r, row0, it.rows_m, bits);
             __syncthreads();                           // smem is free for the next piece
             continue;
         }
         // The last of an item's pieces to be ready joins them: every piece is in memory before its CTA takes a
         // ticket.
-        if (threadIdx.x == 0) a.part_head[at].bits = bits;
+        if (threadIdx.x == 0) a.part_head[w.slot()].bits = bits;
         __threadfence();
         __syncthreads();
         if (threadIdx.x == 0) {
@@ -424,42 +599,53 @@ __global__ void __launch_bounds__(FEW8_THREADS, 2) attn8_few_kernel(const __grid
             const uint32_t w0 = (uint32_t)((item + a.extra) / slice);  // the slice with its first tile
             s_head.pieces = (uint32_t)((item + it.cost - 1) / slice) - w0 + 1u;
             s_head.r = r; s_head.row0 = row0; s_head.rows_m = it.rows_m;
-            s_head.h = h; s_head.q0 = q0; s_head.nr = nr;
+            s_head.h = w.h; s_head.q0 = q0; s_head.nr = nr;
             s_first = w0;
             s_last = atomicAdd(&a.tickets[w0], 1u) + 1u == s_head.pieces;
+            s_bits = 0u;
         }
         __syncthreads();
         if (s_last) {
             __threadfence();
-            join_here<T, D, ROWS>(a, s_head, s_first, &s_join);
+            join8<D, ROWS, THREADS>(a, s_head, s_first, s_top, &s_bits);
         }
         __syncthreads();                               // smem is free for the next piece
     }
     leave_tickets(a);
 }
 
-template <class T, int D, bool NEAR>
+template <int D, int NR, bool NEAR>
 int launch_few8(gift_ctx* c, Attn8Args& a, cudaStream_t st)
 {
-    constexpr int smem = Few8<D>::smem;
-    CU_TRY((allow_smem<attn8_few_kernel<T, D, NEAR>>(c->device, smem)));
-    a.n_slices = 2u * c->num_sms;
+    using L = Few8<D, NR>;
+    CU_TRY((allow_smem<attn8_few_kernel<D, NR, NEAR>>(c->device, L::smem)));
+    a.n_slices = (uint32_t)L::ctas * c->num_sms;
     a.ways = 1;
-    a.tile_rows = FEW8_ROWS;
+    a.tile_rows = L::rows;
     a.by_tile_rows = fixed_div(a.tile_rows);
     a.least = 1;
-    a.extra = 2;
-    attn8_few_kernel<T, D, NEAR><<<a.n_slices, FEW8_THREADS, smem, st>>>(a);
+    a.extra = 4;
+    // Heads lie next to one another in a token, so warps that take the heads of the same tokens read longer runs of memory
+    // at a time; but with few items in a call, fewer heads in each mean fewer pieces for one CTA to join.
+    a.head_ways = L::warps;
+    while (a.head_ways > 1 && (a.kv_heads % a.head_ways || (uint64_t)a.b.n_req * (a.kv_heads / a.head_ways) < FEW8_ITEMS)) a.head_ways /= 2;
+    a.kv_heads /= a.head_ways;
+    a.tile_tokens = L::warps / a.head_ways * L::tok;
+    a.whole_steps = a.b.page_tokens % L::tok == 0;
+    attn8_few_kernel<D, NR, NEAR><<<a.n_slices, L::threads, L::smem, st>>>(a);
     c->launches++;
     CU_TRY(cudaGetLastError());
     return GIFT_OK;
 }
 
-template <class T, int D>
+template <int D>
 int launch_attn8(gift_ctx* c, Attn8Args& a, cudaStream_t st)
 {
     const bool near = a.cap_out != 0.f || a.slopes || a.window;
-    return near ? launch_few8<T, D, true>(c, a, st) : launch_few8<T, D, false>(c, a, st);
+    // rows of an average request's K/V head
+    const uint64_t rows = ((uint64_t)a.n_rows + a.b.n_req - 1) / a.b.n_req * a.group;
+    if (rows <= 8) return near ? launch_few8<D, 1, true>(c, a, st) : launch_few8<D, 1, false>(c, a, st);
+    return near ? launch_few8<D, 2, true>(c, a, st) : launch_few8<D, 2, false>(c, a, st);
 }
 
 }  // namespace
@@ -518,7 +704,6 @@ extern "C" int gift_kv_attention_codes(gift_ctx* c, const gift_batch* batch, con
         a.cap_out = t8->softcap * LOG2_E;
     }
     use_scratch(c, a);
-    if (t8->dtype == GIFT_BF16)
-        return pool->head_dim == 128 ? launch_attn8<__nv_bfloat16, 128>(c, a, st) : launch_attn8<__nv_bfloat16, 64>(c, a, st);
-    return pool->head_dim == 128 ? launch_attn8<__half, 128>(c, a, st) : launch_attn8<__half, 64>(c, a, st);
+    a.half = t8->dtype == GIFT_FP16;
+    return pool->head_dim == 128 ? launch_attn8<128>(c, a, st) : launch_attn8<64>(c, a, st);
 }

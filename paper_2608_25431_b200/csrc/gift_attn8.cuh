@@ -9,6 +9,9 @@ struct Attn8Args : AttnArgs {
     uint32_t codes;                  // bytes of K's (or V's) codes of one token; V's, then the scales, lie behind
     float cap_in, cap_out;           // scale / softcap, softcap * log2(e); cap_out 0: no cap
     const float* slopes;
+    uint32_t half;                   // q and out are fp16, not bf16
+    uint32_t head_ways;              // few rows: K/V heads that a CTA's warps share out (kv_heads counts groups of them)
+    uint32_t whole_steps;            // few rows: a page is whole steps of a warp
 };
 
 constexpr float LOG2_E = 1.4426950408889634f;
@@ -29,11 +32,15 @@ __device__ __forceinline__ float tanh_of(float u)
     return fabsf(u) < 0.2f ? near : far;
 }
 
-// Power-of-two factors, made of exponents: a value whose top exponent field is e becomes one of about 2^12, in
-// fp16 well above what it rounds (2^-14) and below what it holds (2^16).  e = 255: infinities and NaN stay.
-__device__ __forceinline__ uint32_t top_exponent(uint32_t magnitude) { return magnitude >> 23 < 13u ? 13u : magnitude >> 23; }
-__device__ __forceinline__ float to_half_range(uint32_t e) { return e == 255u ? 1.f : __uint_as_float((266u - e) << 23); }
-__device__ __forceinline__ float from_half_range(uint32_t e) { return e == 255u ? 1.f : __uint_as_float((e - 12u) << 23); }
+// Power-of-two factors, made of exponents: a value with exponent field e, or 9 where that is less, becomes one of about
+// 2^8: in fp16 well above what it rounds (2^-14), with room for one that is 2^7 larger.  e = 255: infinities and NaN stay.
+__device__ __forceinline__ uint32_t top_exponent(uint32_t magnitude) { return magnitude >> 23 < 9u ? 9u : magnitude >> 23; }
+__device__ __forceinline__ float to_half_range(uint32_t e) { return e == 255u ? 1.f : __uint_as_float((262u - e) << 23); }
+__device__ __forceinline__ float from_half_range(uint32_t e) { return e == 255u ? 1.f : __uint_as_float((e - 8u) << 23); }
+// The reciprocal of a power of two, exact.
+__device__ __forceinline__ float inverse_power(float x) { return __uint_as_float(0x7F000000u - __float_as_uint(x)); }
+// The largest value that fits fp16 by e's factor.
+__device__ __forceinline__ float half_range_end(uint32_t e) { return __uint_as_float((e > 247u ? 254u : e + 7u) << 23); }
 
 // Which of the 64 tokens from t0 a row sees where a window ends among them, as bits: those from position x - window + 1 on.
 __device__ __forceinline__ uint64_t in_window64(uint32_t window, uint32_t x, uint32_t t0)

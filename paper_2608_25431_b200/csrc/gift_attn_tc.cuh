@@ -38,9 +38,7 @@
 // other CTAs too, and their status GIFT_ST_STALLED.  It ends only when its own copies and products have: the warps that started them wait
 // for the last of them, with a limit of their own.
 #pragma once
-#include <cuda.h>
-
-#include "gift_attn.cuh"
+#include "gift_tc.cuh"
 
 namespace gift {
 
@@ -52,9 +50,6 @@ constexpr int TC_STAGES = 2;
 // waits for S of the third, that for P V of the first, that for the softmax), warp 5 at most two (its stages
 // are freed by P V), and a verdict is cleared one piece after it was read.
 constexpr int TC_BITS_RING = 8;
-constexpr uint32_t TC_SUSPEND_NS = 1000;                             // longest single attempt of a wait
-constexpr uint32_t TC_WAIT_TRIES = 1u << 20;                         // attempts unless the ctx says otherwise: 50 ms to a second
-constexpr uint32_t TC_DRAIN_TRIES = 1u << 20;                        // of the waits for a CTA's own copies and products at its end
 
 template <int D> struct TcSmem {
     static constexpr uint32_t q = 0;                                                  // [D/64][128][64]
@@ -73,213 +68,6 @@ struct TcShared {
     int dead;
     PlaceShared place;
 };
-
-__device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
-
-__device__ __forceinline__ void bar_init(uint64_t* b, uint32_t count)
-{
-    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(b)), "r"(count) : "memory");
-}
-__device__ __forceinline__ void bar_arrive(uint64_t* b)
-{
-    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(b)) : "memory");
-}
-// Arrives and announces how many bytes the copies will bring in this phase.
-__device__ __forceinline__ void bar_expect(uint64_t* b, uint32_t bytes)
-{
-    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(smem_u32(b)), "r"(bytes) : "memory");
-}
-// 64 elements from column x of four rows of the map; the rows land behind one another, 128 bytes each.
-__device__ __forceinline__ void gather4(uint32_t dst, const CUtensorMap* map, int32_t x, const int32_t (&row)[4], uint64_t* b)
-{
-    asm volatile(
-        "cp.async.bulk.tensor.2d.shared::cta.global.tile::gather4.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];"
-        ::"r"(dst), "l"(map), "r"(x), "r"(row[0]), "r"(row[1]), "r"(row[2]), "r"(row[3]), "r"(smem_u32(b)) : "memory");
-}
-// 64 columns from x of a box of heads and tokens of q.
-__device__ __forceinline__ void copy_q(uint32_t dst, const CUtensorMap* map, int32_t x, int32_t head, int32_t token, uint64_t* b)
-{
-    asm volatile("cp.async.bulk.tensor.3d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
-                 ::"r"(dst), "l"(map), "r"(x), "r"(head), "r"(token), "r"(smem_u32(b)) : "memory");
-}
-// 64 columns from x of a run of rows from `row`.
-__device__ __forceinline__ void copy_run(uint32_t dst, const CUtensorMap* map, int32_t x, int32_t row, uint64_t* b)
-{
-    asm volatile("cp.async.bulk.tensor.2d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
-                 ::"r"(dst), "l"(map), "r"(x), "r"(row), "r"(smem_u32(b)) : "memory");
-}
-__device__ __forceinline__ bool bar_try(uint64_t* b, uint32_t parity, uint32_t ns)
-{
-    uint32_t done;
-    asm volatile(
-        "{\n .reg .pred p;\n"
-        " mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n"
-        " selp.u32 %0, 1, 0, p;\n}"
-        : "=r"(done) : "r"(smem_u32(b)), "r"(parity), "r"(ns) : "memory");
-    return done != 0u;
-}
-// Waits until the barrier's phase with this parity is complete; false when that takes too long, or
-// another role of the CTA has given up.
-__device__ __noinline__ bool bar_wait_long(uint64_t* b, uint32_t parity, volatile int* dead, const AttnArgs& a)
-{
-#pragma unroll 1
-    for (uint32_t i = 0; i < a.wait_tries; i++) {
-        if (bar_try(b, parity, a.wait_ns)) return true;
-        if ((i & 255u) == 255u && *dead) return false;
-    }
-    *dead = 1;
-    return false;
-}
-__device__ __forceinline__ bool bar_wait(uint64_t* b, uint32_t parity, volatile int* dead, const AttnArgs& a)
-{
-    return bar_try(b, parity, a.wait_ns) || bar_wait_long(b, parity, dead, a);
-}
-// The same for a whole warp, with one answer for all its lanes.
-__device__ __forceinline__ bool warp_wait(uint64_t* b, uint32_t parity, volatile int* dead, const AttnArgs& a)
-{
-    return __all_sync(0xFFFFFFFFu, bar_wait(b, parity, dead, a));
-}
-// Whether any of the four softmax warps says so, for all of their threads alike.
-__device__ __forceinline__ bool any_softmax(bool x)
-{
-    uint32_t r;
-    asm volatile("{\n .reg .pred p, q;\n setp.ne.u32 p, %1, 0;\n barrier.cta.red.or.pred q, 1, 128, p;\n selp.u32 %0, 1, 0, q;\n}"
-                 : "=r"(r) : "r"((uint32_t)x) : "memory");
-    return r != 0u;
-}
-// Waits for this CTA's own copies or products, which always end, whatever became of the other roles.
-__device__ __forceinline__ void bar_drain(uint64_t* b, uint32_t parity)
-{
-#pragma unroll 1
-    for (uint32_t i = 0; i < TC_DRAIN_TRIES && !bar_try(b, parity, TC_SUSPEND_NS); i++) {}
-}
-
-// Shared-memory operand descriptor, 128-byte swizzle: start, stride between 64-element column blocks
-// (operands with the column dimension contiguous), stride between groups of 8 rows.
-__device__ __forceinline__ uint64_t smem_desc(uint32_t addr, uint32_t block_stride, uint32_t group_stride)
-{
-    return (uint64_t)((addr >> 4) & 0x3FFFu) | ((uint64_t)((block_stride >> 4) & 0x3FFFu) << 16) |
-           ((uint64_t)((group_stride >> 4) & 0x3FFFu) << 32) | (1ull << 46) | (2ull << 61);
-}
-
-// Instruction descriptor of kind::f16: 32-bit accumulator, both operands of type T, M x N, B either
-// with k contiguous (0) or with n contiguous (1).
-template <class T> __host__ __device__ constexpr uint32_t instr_desc(uint32_t m, uint32_t n, uint32_t b_n_major)
-{
-    const uint32_t t = std::is_same<T, __half>::value ? 0u : 1u;
-    return (1u << 4) | (t << 7) | (t << 10) | (b_n_major << 16) | ((n >> 3) << 17) | ((m >> 4) << 24);
-}
-
-__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add)
-{
-    asm volatile(
-        "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
-        " tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}"
-        ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add) : "memory");
-}
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool add)
-{
-    asm volatile(
-        "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
-        " tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}"
-        ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)add) : "memory");
-}
-// The barrier is told when all products issued so far are complete.
-__device__ __forceinline__ void mma_commit(uint64_t* b)
-{
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(b)) : "memory");
-}
-__device__ __forceinline__ void tc_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void tc_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void tc_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
-__device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-
-// 32 columns of this thread's tensor-memory row.  The wait names the registers, so that nothing that
-// uses them is moved before it.
-__device__ __forceinline__ void tc_ld32(uint32_t (&r)[32], uint32_t addr)
-{
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
-        "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
-          "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]),
-          "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]),
-          "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
-        : "r"(addr) : "memory");
-}
-__device__ __forceinline__ void tc_pin32(uint32_t (&r)[32])
-{
-    asm volatile("" : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]),
-                 "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]));
-    asm volatile("" : "+r"(r[16]), "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]), "+r"(r[23]),
-                 "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31]));
-}
-__device__ __forceinline__ void tc_st32(uint32_t addr, const uint32_t (&r)[32])
-{
-    asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
-        "{%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};"
-        ::"r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
-          "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]),
-          "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]),
-          "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
-        : "memory");
-}
-
-__device__ __forceinline__ void tc_ld8(uint32_t (&r)[8], uint32_t addr)
-{
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
-                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "r"(addr) : "memory");
-}
-__device__ __forceinline__ void tc_pin8(uint32_t (&r)[8])
-{
-    asm volatile("" : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]));
-}
-__device__ __forceinline__ void tc_st16(uint32_t addr, const uint32_t (&r)[16])
-{
-    asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
-        ::"r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
-          "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
-}
-// Two 32-bit elements at a time.
-__device__ __forceinline__ uint64_t pair2(float lo, float hi)
-{
-    uint64_t r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
-    return r;
-}
-__device__ __forceinline__ void split2(uint64_t v, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
-__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c)
-{
-    uint64_t r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-    return r;
-}
-__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b)
-{
-    uint64_t r;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
-__device__ __forceinline__ float max3(float a, float b, float c)
-{
-    float r;
-    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
-    return r;
-}
-// One column, waited for.
-__device__ __forceinline__ uint32_t tc_ld1(uint32_t addr)
-{
-    uint32_t r;
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];\n tcgen05.wait::ld.sync.aligned;" : "=r"(r) : "r"(addr) : "memory");
-    return r;
-}
-__device__ __forceinline__ void tc_st8(uint32_t addr, const uint32_t (&r)[8])
-{
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
-                 ::"r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
-}
 
 using TcWalk = Walk<TC_TILE>;
 

@@ -17,7 +17,7 @@ namespace {
 constexpr int ROW_THREADS = 256;
 constexpr float CODE_MAX = 448.f;                // largest e4m3 number
 constexpr float LEAST_SCALE = 1.17549435e-38f;   // 2^-126: a scale and its reciprocal are normal numbers
-constexpr int WRITE_UNROLL = 4;                  // heads that a group of lanes has under way
+constexpr int WRITE_UNROLL = 2;                  // heads that a group of lanes has under way
 
 template <class T> __device__ __forceinline__ float2 unpack2(uint32_t x);
 template <> __device__ __forceinline__ float2 unpack2<__nv_bfloat16>(uint32_t x)
@@ -41,11 +41,12 @@ template <> __device__ __forceinline__ uint32_t pack_pair<__half>(float lo, floa
 // writing
 // ---------------------------------------------------------------------------
 //
-// A pass over the rows: every byte is read once and written once, and HBM bandwidth bounds it.  A head is a
-// group of L lanes with 8 elements each (L = 8, 16 or 32); where halves of a head turn against one
-// another a lane holds 4 elements of each half, so that a pair never leaves its lane, and the 4 angles of
-// a lane are the same for all heads of a row: they are worked out once per row and warp and stay in
-// registers.  A warp takes a share of a row's heads, the whole row where rows abound.
+// A pass over the rows: every byte is read once and written once, and HBM bandwidth should bound it; what has to be
+// kept small is the instructions between (norm, turn and code are some 10 per element when done plainly).  A head is a
+// group of L lanes with 16 elements each, in runs of 4: two quads of pairs where halves of a head turn
+// against one another, so that a pair never leaves its lane.  The 8 angles of a lane are the same for all heads of a
+// row: the warp's groups work out a share each and hand them round.  A warp takes the heads of a row kind by kind, so
+// that its weights stay in registers, all of them where rows abound, a share where they do not.
 
 struct WriteArgs {
     const char *q, *k, *v;
@@ -54,13 +55,14 @@ struct WriteArgs {
     uint64_t qo_row, qo_head;
     char* pages;
     uint64_t token_bytes;
-    uint32_t codes;                          // bytes of K's (or V's) elements of one token
+    uint32_t codes;                          // K's (or V's) elements of one token
     const int64_t* slots;
     const int32_t* row_owner;
     const int32_t* owner_map;
     uint32_t* status;
     uint32_t n_rows, n_slots, dim;
-    uint32_t q_heads, kv_heads, units;       // units: heads of q, of k, of v
+    uint32_t q_heads, kv_heads;
+    uint32_t q_rounds, kv_rounds;            // rounds of a warp over the heads of q, of k (and of v)
     uint32_t parts, iters;                   // warps that share a row, rounds of each
     uint64_t tasks;
     FixedDiv page;
@@ -75,25 +77,159 @@ struct WriteArgs {
 
 // cos and sin of pos * freq: the product in 64 bits (a position of 2^20 times a 32-bit frequency has no 32-bit
 // place for its fraction of a turn), reduced to half a turn either way, the rest in 32 bits.
-__device__ __forceinline__ void turn(int32_t pos, float freq, float& c, float& s)
+__device__ __forceinline__ float2 turn(int32_t pos, float freq)
 {
     const double turns = (double)pos * (double)freq * 0.15915494309189535;
-    sincospif(2.f * (float)(turns - rint(turns)), &s, &c);
+    float2 r;
+    sincospif(2.f * (float)(turns - rint(turns)), &r.y, &r.x);
+    return r;
+}
+
+// A lane's place in a head.
+struct Lane {
+    uint32_t at[4];                          // first elements of its runs of 4
+    bool holds[2], turns[2];                 // per quad
+};
+
+// The rounds [first, last) of one kind of head: KIND 0 q, 1 k, 2 v.
+template <class T, bool POOL8, int L, int KIND>
+__device__ __forceinline__ void write_heads(const WriteArgs& a, const Lane& own, uint32_t t, char* token, uint32_t first, uint32_t last,
+                                            const float2 (&angle)[8])
+{
+    constexpr uint32_t GROUPS = 32 / L;
+    constexpr bool CODES = POOL8 && KIND != 0;
+    if (first >= last) return;
+    const uint32_t lane = threadIdx.x & 31, j = lane % L, group = lane / L;
+    const uint32_t heads = KIND == 0 ? a.q_heads : a.kv_heads;
+    const void* norm = KIND == 0 ? a.q_norm : KIND == 1 ? a.k_norm : nullptr;
+    uint32_t at[4];
+#pragma unroll
+    for (int x = 0; x < 4; x++) at[x] = KIND == 2 ? 16 * j + 4 * x : own.at[x];
+    const bool holds[2] = {KIND == 2 ? 16 * j < a.dim : own.holds[0], KIND == 2 ? 16 * j + 8 < a.dim : own.holds[1]};
+    uint2 weight[4];
+    if (norm)
+#pragma unroll
+        for (int x = 0; x < 4; x++)
+            weight[x] = holds[x >> 1] ? *reinterpret_cast<const uint2*>(static_cast<const char*>(norm) + at[x] * 2) : make_uint2(0u, 0u);
+    const char* from = KIND == 0 ? a.q + t * a.q_row : KIND == 1 ? a.k + t * a.k_row : a.v + t * a.v_row;
+    const uint64_t head_bytes = KIND == 0 ? a.q_head : KIND == 1 ? a.k_head : a.v_head;
+#pragma unroll 1
+    for (uint32_t it = first; it < last; it += WRITE_UNROLL) {
+        uint2 raw[WRITE_UNROLL][4];
+#pragma unroll
+        for (int u = 0; u < WRITE_UNROLL; u++) {
+            const uint32_t h = (it + u) * GROUPS + group;
+            const char* p = from + h * head_bytes;
+            const bool there = it + u < last && h < heads;
+#pragma unroll
+            for (int x = 0; x < 4; x++)
+                raw[u][x] = there && holds[x >> 1] ? __ldcs(reinterpret_cast<const uint2*>(p + at[x] * 2)) : make_uint2(0u, 0u);
+        }
+#pragma unroll
+        for (int u = 0; u < WRITE_UNROLL; u++) {
+            if (it + u >= last) break;
+            const uint32_t h = (it + u) * GROUPS + group;
+            const bool there = h < heads;
+            char* to = KIND == 0 ? a.q_out + t * a.qo_row + h * a.qo_head
+                                 : POOL8 ? token + (KIND == 2 ? a.codes : 0u) + h * a.dim : token + ((KIND == 2 ? a.codes : 0u) + h * a.dim) * 2ull;
+            if (KIND == 2 && !POOL8) {
+                // values on their way unchanged keep their bits
+#pragma unroll
+                for (int x = 0; x < 4; x++)
+                    if (there && holds[x >> 1]) *reinterpret_cast<uint2*>(to + at[x] * 2) = raw[u][x];
+                continue;
+            }
+            float e[4][4];
+#pragma unroll
+            for (int x = 0; x < 4; x++) {
+                const float2 m = unpack2<T>(raw[u][x].x), n = unpack2<T>(raw[u][x].y);
+                e[x][0] = m.x; e[x][1] = m.y; e[x][2] = n.x; e[x][3] = n.y;
+            }
+            if (norm) {
+                float sum = 0.f;
+#pragma unroll
+                for (int x = 0; x < 4; x++)
+#pragma unroll
+                    for (int y = 0; y < 4; y++) sum += e[x][y] * e[x][y];
+#pragma unroll
+                for (int d = 1; d < L; d <<= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, d);
+                const float r = rsqrtf(sum * a.inv_dim + a.eps);
+#pragma unroll
+                for (int x = 0; x < 4; x++) {
+                    const float2 m = unpack2<T>(weight[x].x), n = unpack2<T>(weight[x].y);
+                    e[x][0] *= r * m.x; e[x][1] *= r * m.y; e[x][2] *= r * n.x; e[x][3] *= r * n.y;
+                }
+            }
+            if (KIND != 2) {
+#pragma unroll
+                for (int x = 0; x < 2; x++)
+                    if (own.turns[x]) {
+                        float z[8];
+#pragma unroll
+                        for (int i = 0; i < 4; i++) {
+                            // elements i of the two runs, or neighbours
+                            const float2 w = angle[4 * x + i];
+                            const float p = a.pairs ? e[2 * x + i / 2][2 * (i & 1)] : e[2 * x][i];
+                            const float q = a.pairs ? e[2 * x + i / 2][2 * (i & 1) + 1] : e[2 * x + 1][i];
+                            z[i] = p * w.x - q * w.y;
+                            z[4 + i] = q * w.x + p * w.y;
+                        }
+#pragma unroll
+                        for (int i = 0; i < 8; i++) e[2 * x + i / 4][i & 3] = a.pairs ? z[(i & 1) * 4 + i / 2] : z[i];
+                    }
+            }
+            if (!CODES) {
+#pragma unroll
+                for (int x = 0; x < 4; x++)
+                    if (there && holds[x >> 1]) {
+                        const bool same = !norm && !own.turns[x >> 1];
+                        *reinterpret_cast<uint2*>(to + at[x] * 2) = same ? raw[u][x] : make_uint2(pack_pair<T>(e[x][0], e[x][1]), pack_pair<T>(e[x][2], e[x][3]));
+                    }
+            } else {
+                // as whole numbers the magnitudes of infinities and NaN are above all others
+                uint32_t top = 0u;
+#pragma unroll
+                for (int x = 0; x < 4; x++)
+#pragma unroll
+                    for (int y = 0; y < 4; y++) top = max(top, __float_as_uint(e[x][y]) & 0x7FFFFFFFu);
+#pragma unroll
+                for (int d = 1; d < L; d <<= 1) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
+                const bool fine = top < 0x7F800000u;
+                // 1 / 448 and the reciprocal are off by 2^-24 and 2^-23: as much for a value that lies so near the middle of two codes
+                const float scale = fmaxf(__uint_as_float(top) * (1.f / CODE_MAX), LEAST_SCALE), inv = __frcp_rn(scale);
+#pragma unroll
+                for (int x = 0; x < 4; x++) {
+                    const uint32_t w = floats_to_codes(e[x][0] * inv, e[x][1] * inv) | floats_to_codes(e[x][2] * inv, e[x][3] * inv) << 16;
+                    if (there && holds[x >> 1]) *reinterpret_cast<uint32_t*>(to + at[x]) = fine ? w : 0u;      // 0 * inf is no code
+                }
+                if (there && j == 0) {
+                    float* scales = reinterpret_cast<float*>(token + 2ull * a.codes);
+                    scales[2 * h + (KIND == 2 ? 1 : 0)] = fine ? scale : __uint_as_float(0x7FC00000u);
+                    // what lies behind the scales of an odd number of heads
+                    if (KIND == 2 && h + 1 == a.kv_heads && (a.kv_heads & 1u)) scales[2 * h + 2] = scales[2 * h + 3] = 0.f;
+                }
+            }
+        }
+    }
 }
 
 template <class T, bool POOL8, int L>
-__global__ void __launch_bounds__(ROW_THREADS) kv_write_kernel(const __grid_constant__ WriteArgs a)
+__global__ void __launch_bounds__(ROW_THREADS, 2) kv_write_kernel(const __grid_constant__ WriteArgs a)
 {
-    constexpr uint32_t GROUPS = 32 / L;
     const uint32_t lane = threadIdx.x & 31, j = lane % L, group = lane / L;
     const uint32_t n_warps = gridDim.x * (ROW_THREADS / 32);
-    const bool holds = j * 8 < a.dim, turns = j * 8 < 2 * a.n_freq;
-    // a lane's two runs of 4 elements: next to one another, or in the two halves that turn
-    const bool apart = turns && !a.pairs;
-    const uint32_t lo_turned = apart ? 4 * j : 8 * j, hi_turned = apart ? a.n_freq + 4 * j : 8 * j + 4;
-
+    Lane own;
+#pragma unroll
+    for (int x = 0; x < 2; x++) {
+        const uint32_t quad = 2 * j + x;
+        own.turns[x] = 4 * quad < a.n_freq;
+        own.holds[x] = 8 * quad < a.dim;
+        const bool apart = own.turns[x] && !a.pairs;
+        own.at[2 * x] = apart ? 4 * quad : 8 * quad;
+        own.at[2 * x + 1] = apart ? a.n_freq + 4 * quad : 8 * quad + 4;
+    }
     for (uint64_t task = blockIdx.x * (ROW_THREADS / 32) + (threadIdx.x >> 5); task < a.tasks; task += n_warps) {
-        const uint32_t t = (uint32_t)(task / a.parts), part = (uint32_t)(task - (uint64_t)t * a.parts);
+        const uint32_t t = a.parts == 1 ? (uint32_t)task : (uint32_t)(task / a.parts), part = (uint32_t)(task - (uint64_t)t * a.parts);
         const int64_t slot = a.slots[t];
         uint32_t st = 0u;
         if (slot != -1) {
@@ -103,135 +239,46 @@ __global__ void __launch_bounds__(ROW_THREADS) kv_write_kernel(const __grid_cons
         if (part == 0 && lane == 0) a.status[t] = st;
         if (st != 0u || slot == -1) continue;
         char* token = a.pages + (uint64_t)slot * a.token_bytes;
+        const uint32_t r0 = part * a.iters, r1 = r0 + a.iters;
 
-        float c[4], s[4];
-        if (turns) {
+        float2 angle[8];
+        if (a.n_freq && r0 < a.q_rounds + a.kv_rounds) {
+            constexpr int OWN = L / 4;                 // angles that a group works out
+            float2 mine[OWN];
 #pragma unroll
-            for (int i = 0; i < 4; i++) {
-                const uint32_t f = 4 * j + i;
+            for (int y = 0; y < OWN; y++) {
+                const uint32_t f = 8 * j + group * OWN + y;
                 uint32_t axis = 0;
 #pragma unroll
                 for (int x = 0; x < (int)GIFT_MAX_AXES - 1; x++) axis += f >= a.ends[x];
-                turn(a.pos[axis * a.pos_stride + t], a.freq[f], c[i], s[i]);
+                mine[y] = f < a.n_freq ? turn(a.pos[axis * a.pos_stride + t], a.freq[f]) : make_float2(1.f, 0.f);
+            }
+#pragma unroll
+            for (int y = 0; y < 8; y++) {
+                angle[y].x = __shfl_sync(0xFFFFFFFFu, mine[y % OWN].x, y / OWN * L + j);
+                angle[y].y = __shfl_sync(0xFFFFFFFFu, mine[y % OWN].y, y / OWN * L + j);
             }
         }
-#pragma unroll 1
-        for (uint32_t it = part * a.iters; it < (part + 1) * a.iters; it += WRITE_UNROLL) {
-            uint2 raw[WRITE_UNROLL][2];
-#pragma unroll
-            for (int x = 0; x < WRITE_UNROLL; x++) {
-                const uint32_t u = (it + x) * GROUPS + group;
-                raw[x][0] = raw[x][1] = make_uint2(0u, 0u);
-                if (it + x >= (part + 1) * a.iters || u >= a.units || !holds) continue;
-                const bool is_q = u < a.q_heads, is_v = u >= a.q_heads + a.kv_heads;
-                const char* p = is_q ? a.q + t * a.q_row + u * a.q_head
-                                     : is_v ? a.v + t * a.v_row + (u - a.q_heads - a.kv_heads) * a.v_head
-                                            : a.k + t * a.k_row + (u - a.q_heads) * a.k_head;
-                raw[x][0] = __ldcs(reinterpret_cast<const uint2*>(p + (is_v ? 8 * j : lo_turned) * 2));
-                raw[x][1] = __ldcs(reinterpret_cast<const uint2*>(p + (is_v ? 8 * j + 4 : hi_turned) * 2));
-            }
-#pragma unroll
-            for (int x = 0; x < WRITE_UNROLL; x++) {
-                const uint32_t u = (it + x) * GROUPS + group;
-                const bool there = it + x < (part + 1) * a.iters && u < a.units;
-                if (!__any_sync(0xFFFFFFFFu, there)) break;
-                const bool is_q = u < a.q_heads, is_v = u >= a.q_heads + a.kv_heads;
-                const uint32_t h = is_q ? u : is_v ? u - a.q_heads - a.kv_heads : u - a.q_heads;
-                const uint32_t lo = is_v ? 8 * j : lo_turned, hi = is_v ? 8 * j + 4 : hi_turned;
-                float e[8], z[8];
-#pragma unroll
-                for (int y = 0; y < 2; y++) {
-                    const float2 m = unpack2<T>(raw[x][y].x), n = unpack2<T>(raw[x][y].y);
-                    e[4 * y] = m.x; e[4 * y + 1] = m.y; e[4 * y + 2] = n.x; e[4 * y + 3] = n.y;
-                }
-                const void* norm = is_v ? nullptr : is_q ? a.q_norm : a.k_norm;
-                if (a.q_norm || a.k_norm) {
-                    float sum = 0.f;
-#pragma unroll
-                    for (int y = 0; y < 8; y++) sum += e[y] * e[y];
-#pragma unroll
-                    for (int d = 1; d < L; d <<= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, d);
-                    if (norm && holds) {
-                        const float r = rsqrtf(sum * a.inv_dim + a.eps);
-#pragma unroll
-                        for (int y = 0; y < 2; y++) {
-                            const uint2 w = *reinterpret_cast<const uint2*>(static_cast<const char*>(norm) + (y ? hi : lo) * 2);
-                            const float2 m = unpack2<T>(w.x), n = unpack2<T>(w.y);
-                            e[4 * y] *= r * m.x; e[4 * y + 1] *= r * m.y; e[4 * y + 2] *= r * n.x; e[4 * y + 3] *= r * n.y;
-                        }
-                    }
-                }
-                if (turns && !is_v) {
-#pragma unroll
-                    for (int i = 0; i < 4; i++) {
-                        // elements (i, 4 + i), or neighbours
-                        const float p = a.pairs ? e[2 * i] : e[i], r = a.pairs ? e[2 * i + 1] : e[4 + i];
-                        z[i] = p * c[i] - r * s[i];
-                        z[4 + i] = r * c[i] + p * s[i];
-                    }
-#pragma unroll
-                    for (int i = 0; i < 8; i++) e[i] = a.pairs ? z[(i & 1) * 4 + i / 2] : z[i];
-                }
-                if (!POOL8 || is_q) {
-                    if (there && holds) {
-                        char* to = is_q ? a.q_out + t * a.qo_row + h * a.qo_head : token + (is_v ? (uint64_t)a.codes * 2 : 0u) + (uint64_t)h * a.dim * 2;
-                        // values on their way unchanged keep their bits
-                        const bool same = is_v || (!norm && !turns);
-                        *reinterpret_cast<uint2*>(to + lo * 2) = same ? raw[x][0] : make_uint2(pack_pair<T>(e[0], e[1]), pack_pair<T>(e[2], e[3]));
-                        *reinterpret_cast<uint2*>(to + hi * 2) = same ? raw[x][1] : make_uint2(pack_pair<T>(e[4], e[5]), pack_pair<T>(e[6], e[7]));
-                    }
-                }
-                if (POOL8 && __any_sync(0xFFFFFFFFu, there && !is_q)) {
-                    // as whole numbers the magnitudes of infinities and NaN are above all others
-                    uint32_t top = 0u;
-#pragma unroll
-                    for (int y = 0; y < 8; y++) {
-                        const uint32_t m = __float_as_uint(e[y]) & 0x7FFFFFFFu;
-                        top = m > top ? m : top;
-                    }
-#pragma unroll
-                    for (int d = 1; d < L; d <<= 1) {
-                        const uint32_t o = __shfl_xor_sync(0xFFFFFFFFu, top, d);
-                        top = o > top ? o : top;
-                    }
-                    const bool fine = top < 0x7F800000u;
-                    const float scale = fmaxf(__fdiv_rn(__uint_as_float(top), CODE_MAX), LEAST_SCALE);
-                    const float inv = fine ? __frcp_rn(scale) : 0.f;
-                    uint32_t w[2];
-#pragma unroll
-                    for (int y = 0; y < 2; y++)
-                        w[y] = floats_to_codes(e[4 * y] * inv, e[4 * y + 1] * inv) | floats_to_codes(e[4 * y + 2] * inv, e[4 * y + 3] * inv) << 16;
-                    if (!fine) w[0] = w[1] = 0u;                       // 0 * inf is no code
-                    if (there && !is_q && holds) {
-                        char* to = token + (is_v ? a.codes : 0u) + h * a.dim;
-                        *reinterpret_cast<uint32_t*>(to + lo) = w[0];
-                        *reinterpret_cast<uint32_t*>(to + hi) = w[1];
-                        if (j == 0) {
-                            float* scales = reinterpret_cast<float*>(token + 2ull * a.codes);
-                            scales[2 * h + (is_v ? 1 : 0)] = fine ? scale : __uint_as_float(0x7FC00000u);
-                            // what lies behind the scales of an odd number of heads
-                            if (is_v && h + 1 == a.kv_heads && (a.kv_heads & 1u)) scales[2 * h + 2] = scales[2 * h + 3] = 0.f;
-                        }
-                    }
-                }
-            }
-        }
+        const uint32_t k0 = a.q_rounds, v0 = k0 + a.kv_rounds, end = v0 + a.kv_rounds;
+        write_heads<T, POOL8, L, 0>(a, own, t, token, r0, min(r1, k0), angle);
+        write_heads<T, POOL8, L, 1>(a, own, t, token, max(r0, k0) - k0, max(min(r1, v0), k0) - k0, angle);
+        write_heads<T, POOL8, L, 2>(a, own, t, token, max(r0, v0) - v0, max(min(r1, end), v0) - v0, angle);
     }
 }
 
 template <class T, bool POOL8>
 void launch_write(const WriteArgs& a, uint32_t lanes, uint32_t grid, cudaStream_t st)
 {
-    if (lanes == 8) kv_write_kernel<T, POOL8, 8><<<grid, ROW_THREADS, 0, st>>>(a);
-    else if (lanes == 16) kv_write_kernel<T, POOL8, 16><<<grid, ROW_THREADS, 0, st>>>(a);
-    else kv_write_kernel<T, POOL8, 32><<<grid, ROW_THREADS, 0, st>>>(a);
+    if (lanes == 4) kv_write_kernel<T, POOL8, 4><<<grid, ROW_THREADS, 0, st>>>(a);
+    else if (lanes == 8) kv_write_kernel<T, POOL8, 8><<<grid, ROW_THREADS, 0, st>>>(a);
+    else kv_write_kernel<T, POOL8, 16><<<grid, ROW_THREADS, 0, st>>>(a);
 }
 
 // ---------------------------------------------------------------------------
 // reading
 // ---------------------------------------------------------------------------
 //
-// The same copy the other way: a thread takes 16 elements of K and of V of a head (8 of a 16-bit pool).
+// The same copy the other way: a thread takes 8 elements of K and of V of a head, 2 such places at a time.
 
 struct ReadArgs {
     const char* pages;
@@ -277,30 +324,34 @@ __global__ void __launch_bounds__(ROW_THREADS) kv_read_kernel(const __grid_const
         if (lane == 0) a.status[t] = st;
         if (slot == -1) continue;
         const char* token = a.pages + (st ? 0ull : (uint64_t)slot * a.token_bytes);
-        for (uint32_t x = lane; x < a.chunks; x += a.lanes) {
-            const uint32_t h = a.head.quot(x), o = x - h * a.head_chunks;
-            char* k = a.k + t * a.k_row + (uint64_t)h * a.k_head + o * (POOL8 ? 32 : 16);
-            char* v = a.v + t * a.v_row + (uint64_t)h * a.v_head + o * (POOL8 ? 32 : 16);
-            if constexpr (POOL8) {
-                uint4 kk = make_uint4(0u, 0u, 0u, 0u), vv = kk;
-                float2 scale = make_float2(0.f, 0.f);
-                if (st == 0u) {
-                    kk = __ldcs(reinterpret_cast<const uint4*>(token) + x);
-                    vv = __ldcs(reinterpret_cast<const uint4*>(token + a.codes) + x);
-                    scale = *reinterpret_cast<const float2*>(token + 2ull * a.codes + h * 8u);
+        for (uint32_t x0 = lane; x0 < a.chunks; x0 += 2 * a.lanes) {
+            uint4 kv[2][2];
+#pragma unroll
+            for (int y = 0; y < 2; y++) {
+                const uint32_t x = x0 + y * a.lanes;
+                kv[y][0] = kv[y][1] = make_uint4(0u, 0u, 0u, 0u);
+                if (x >= a.chunks || st != 0u) continue;
+                if constexpr (POOL8) {
+                    const uint2 k = __ldcs(reinterpret_cast<const uint2*>(token) + x), v = __ldcs(reinterpret_cast<const uint2*>(token + a.codes) + x);
+                    const uint2 scales = *reinterpret_cast<const uint2*>(token + 2ull * a.codes + a.head.quot(x) * 8u);
+                    kv[y][0] = make_uint4(k.x, k.y, scales.x, 0u);
+                    kv[y][1] = make_uint4(v.x, v.y, scales.y, 0u);
+                } else {
+                    kv[y][0] = __ldcs(reinterpret_cast<const uint4*>(token) + x);
+                    kv[y][1] = __ldcs(reinterpret_cast<const uint4*>(token + 2ull * a.codes) + x);
                 }
-                reinterpret_cast<uint4*>(k)[0] = values8<T>(kk.x, kk.y, scale.x);
-                reinterpret_cast<uint4*>(k)[1] = values8<T>(kk.z, kk.w, scale.x);
-                reinterpret_cast<uint4*>(v)[0] = values8<T>(vv.x, vv.y, scale.y);
-                reinterpret_cast<uint4*>(v)[1] = values8<T>(vv.z, vv.w, scale.y);
-            } else {
-                uint4 kk = make_uint4(0u, 0u, 0u, 0u), vv = kk;
-                if (st == 0u) {
-                    kk = __ldcs(reinterpret_cast<const uint4*>(token) + x);
-                    vv = __ldcs(reinterpret_cast<const uint4*>(token + 2ull * a.codes) + x);
+            }
+#pragma unroll
+            for (int y = 0; y < 2; y++) {
+                const uint32_t x = x0 + y * a.lanes;
+                if (x >= a.chunks) break;
+                const uint32_t h = a.head.quot(x), o = x - h * a.head_chunks;
+#pragma unroll
+                for (int z = 0; z < 2; z++) {
+                    char* to = z ? a.v + t * a.v_row + (uint64_t)h * a.v_head + o * 16 : a.k + t * a.k_row + (uint64_t)h * a.k_head + o * 16;
+                    const uint4 w = kv[y][z];
+                    __stcs(reinterpret_cast<uint4*>(to), POOL8 ? values8<T>(w.x, w.y, __uint_as_float(w.z)) : w);
                 }
-                *reinterpret_cast<uint4*>(k) = kk;
-                *reinterpret_cast<uint4*>(v) = vv;
             }
         }
     }
@@ -367,7 +418,7 @@ extern "C" int gift_kv_write(gift_ctx* c, const gift_kv_pool* pool, const gift_k
     a.token_bytes = pool8 ? kv8_layout(pool).token : (uint64_t)a.codes * 4;
     a.slots = slots; a.row_owner = row_owner; a.owner_map = pool->owner_map; a.status = status;
     a.n_rows = rows->n_rows; a.n_slots = pool->n_pages * pool->page_tokens; a.dim = pool->head_dim;
-    a.q_heads = rows->q ? rows->n_heads : 0u; a.kv_heads = pool->n_heads; a.units = a.q_heads + 2 * a.kv_heads;
+    a.q_heads = rows->q ? rows->n_heads : 0u; a.kv_heads = pool->n_heads;
     a.page = fixed_div(pool->page_tokens);
     a.q_norm = rows->q_norm; a.k_norm = rows->k_norm; a.eps = rows->eps; a.inv_dim = 1.f / pool->head_dim;
     a.n_freq = rows->n_freq; a.pairs = rows->flags & GIFT_ROTATE_PAIRS;
@@ -377,18 +428,20 @@ extern "C" int gift_kv_write(gift_ctx* c, const gift_kv_pool* pool, const gift_k
         a.ends[x] = x + 1 < rows->n_axes ? end : 0xFFFFFFFFu;
     }
     a.freq = rows->freq; a.pos = rows->pos; a.pos_stride = rows->pos_stride;
-    const uint32_t lanes = a.dim <= 64 ? 8 : a.dim <= 128 ? 16 : 32, groups = 32 / lanes;
-    const uint32_t rounds = (a.units + groups - 1) / groups;
+    const uint32_t lanes = a.dim <= 64 ? 4 : a.dim <= 128 ? 8 : 16, groups = 32 / lanes;
+    a.q_rounds = (a.q_heads + groups - 1) / groups;
+    a.kv_rounds = (a.kv_heads + groups - 1) / groups;
+    const uint32_t rounds = a.q_rounds + 2 * a.kv_rounds;
     // a warp takes a whole row where the rows fill the GPU, a share of one where they do not, so many rounds
     // at least as it has under way at once
-    const uint64_t warps = 32ull * c->num_sms;
+    const uint64_t warps = 16ull * c->num_sms;
     uint64_t parts = (warps + a.n_rows - 1) / a.n_rows;
     const uint32_t most = (rounds + WRITE_UNROLL - 1) / WRITE_UNROLL;
     if (parts > most) parts = most;
     a.iters = (uint32_t)((rounds + parts - 1) / parts);
     a.parts = (rounds + a.iters - 1) / a.iters;
     a.tasks = (uint64_t)a.n_rows * a.parts;
-    const uint64_t ctas = (a.tasks + ROW_THREADS / 32 - 1) / (ROW_THREADS / 32), fit = 8ull * c->num_sms;
+    const uint64_t ctas = (a.tasks + ROW_THREADS / 32 - 1) / (ROW_THREADS / 32), fit = 2ull * c->num_sms;
     const uint32_t grid = (uint32_t)(ctas < fit ? ctas : fit);
     cudaStream_t st = (cudaStream_t)stream;
     if (rows->dtype == GIFT_BF16) pool8 ? launch_write<__nv_bfloat16, true>(a, lanes, grid, st) : launch_write<__nv_bfloat16, false>(a, lanes, grid, st);
@@ -426,10 +479,11 @@ extern "C" int gift_kv_read(gift_ctx* c, const gift_kv_pool* pool, uint32_t dtyp
     a.slots = slots; a.row_owner = row_owner; a.owner_map = pool->owner_map; a.status = status;
     a.n_rows = n_rows; a.n_slots = pool->n_pages * pool->page_tokens;
     a.page = fixed_div(pool->page_tokens);
-    a.head_chunks = pool->head_dim / (pool8 ? 16 : 8);
+    a.head_chunks = pool->head_dim / 8;
     a.head = fixed_div(a.head_chunks);
     a.chunks = pool->n_heads * a.head_chunks;
-    a.lanes = a.chunks < (uint32_t)ROW_THREADS ? a.chunks : (uint32_t)ROW_THREADS;
+    // two places a thread and row
+    a.lanes = (a.chunks + 1) / 2 < (uint32_t)ROW_THREADS ? (a.chunks + 1) / 2 : (uint32_t)ROW_THREADS;
     a.rows_per_cta = ROW_THREADS / a.lanes;
     const uint64_t tiles = ((uint64_t)n_rows + a.rows_per_cta - 1) / a.rows_per_cta, fit = 8ull * c->num_sms;
     const uint32_t grid = (uint32_t)(tiles < fit ? tiles : fit);

@@ -12,7 +12,7 @@ SOURCES = ["gift_lib.cu", "gift_rules.cu", "gift_hostio.cu", "gift_tokens.cu", "
            "gift_kv8.cu", "gift_attn8.cu"]
 HEADERS = ["gf128.cuh", "aes_tt.cuh", "gift_core.cuh", "gift_internal.cuh", "gift_rules.cuh", "gift_csr.cuh", "gift_seg.cuh",
            "gift_batch.cuh", "gift_kv.cuh", "gift_attn.cuh", "gift_attn_join.cuh", "gift_tc.cuh", "gift_attn_tc.cuh",
-           "gift_kv8.cuh", "gift_attn8.cuh",
+           "gift_kv8.cuh", "gift_attn8.cuh", "gift_attn8_tc.cuh",
            os.path.join("..", "..", "include", "gift.h")]
 
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",

@@ -7,8 +7,8 @@
 #include <type_traits>
 
 #include "gift_attn8.cuh"
+#include "gift_attn8_tc.cuh"
 #include "gift_attn_join.cuh"
-#include "gift_tc.cuh"
 #include "gift_internal.cuh"
 
 using namespace gift;
@@ -36,7 +36,6 @@ namespace {
 
 constexpr int FEW8_STAGES = 3;
 constexpr uint32_t FEW8_ITEMS = 32;      // of a call, before heads share a CTA
-constexpr float NOTHING = -3e38f;        // the maximum before anything is seen: finite, so that no difference with it is NaN
 constexpr float FEW8_SLACK = 6.f;        // how far, in powers of two, a score may pass the maximum in use
 
 template <int D, int NR> struct Few8 {
@@ -82,18 +81,6 @@ __device__ __forceinline__ uint32_t transposed(uint32_t x)
     asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
     return y;
 }
-// Four codes as two pairs.
-__device__ __forceinline__ void four_codes(uint32_t w, uint32_t& lo, uint32_t& hi)
-{
-    asm("{\n .reg .b16 x, y;\n mov.b32 {x, y}, %2;\n cvt.rn.f16x2.e4m3x2 %0, x;\n cvt.rn.f16x2.e4m3x2 %1, y;\n}" : "=r"(lo), "=r"(hi) : "r"(w));
-}
-
-// Two results as a pair of q's type.
-__device__ __forceinline__ uint32_t pack_out(const Attn8Args& a, float lo, float hi)
-{
-    return a.half ? pack2<__half>(lo, hi) : pack2<__nv_bfloat16>(lo, hi);
-}
-
 // Eight of a finished row's columns, from 8 ch; and with the first of them its lse.
 __device__ __forceinline__ void put_row(const Attn8Args& a, uint32_t row0, uint32_t h, uint32_t rho, uint32_t ch, const float (&acc)[8],
                                         float top, float sum, uint32_t bits)
@@ -638,14 +625,48 @@ int launch_few8(gift_ctx* c, Attn8Args& a, cudaStream_t st)
     return GIFT_OK;
 }
 
+template <int D, bool NEAR>
+int launch_many8(gift_ctx* c, Attn8Args& a, uint64_t rows, cudaStream_t st)
+{
+    CUtensorMap q_map;
+    const int rc = map_of_q(a, a.half != 0u, D, &q_map);
+    if (rc != GIFT_OK) return rc;
+    constexpr int smem = Tc8Smem<D>::bytes;
+    CU_TRY((allow_smem<attn8_tc_kernel<D, NEAR>>(c->device, smem)));
+    // two CTAs to a slice when an average request's rows fill more than one tile: neighbouring items read the same tokens
+    a.ways = rows > (uint64_t)TC8_ROWS ? 2u : 1u;
+    a.n_slices = 2u * c->num_sms / a.ways;
+    a.tile_rows = TC8_ROWS / a.group * a.group;            // whole tokens
+    a.by_tile_rows = fixed_div(a.tile_rows);
+    a.least = 4;
+    a.extra = 8;
+    // the kernel takes the maximum before it scales: the scale must be positive
+    a.negate = a.scale_log2 < 0.f ? 1u : 0u;
+    a.wait_tries = c->attn_wait_ns ? (uint32_t)(c->attn_wait_ns / TC_SUSPEND_NS) : TC_WAIT_TRIES;
+    a.wait_ns = c->attn_wait_ns && c->attn_wait_ns < TC_SUSPEND_NS ? (uint32_t)c->attn_wait_ns : TC_SUSPEND_NS;
+    a.scale_log2 = fabsf(a.scale_log2);
+    a.cap_in = fabsf(a.cap_in);
+    attn8_tc_kernel<D, NEAR><<<a.n_slices * a.ways, TC8_THREADS, smem, st>>>(a, q_map);
+    c->launches++;
+    CU_TRY(cudaGetLastError());
+    if (a.half) CU_TRY((launch_join<__half, D, TC8_ROWS>(a, st)));
+    else CU_TRY((launch_join<__nv_bfloat16, D, TC8_ROWS>(a, st)));
+    c->launches++;
+    return GIFT_OK;
+}
+
 template <int D>
 int launch_attn8(gift_ctx* c, Attn8Args& a, cudaStream_t st)
 {
     const bool near = a.cap_out != 0.f || a.slopes || a.window;
+    // what the tensor map of q does not describe: groups of more heads than a tile has rows, a q whose rows or heads
+    // share memory
+    const bool plain_q = a.group <= (uint32_t)TC8_ROWS && (a.n_rows == 1 || a.q_row > 0) && (a.heads == 1 || a.q_head > 0);
     // rows of an average request's K/V head
     const uint64_t rows = ((uint64_t)a.n_rows + a.b.n_req - 1) / a.b.n_req * a.group;
     if (rows <= 8) return near ? launch_few8<D, 1, true>(c, a, st) : launch_few8<D, 1, false>(c, a, st);
-    return near ? launch_few8<D, 2, true>(c, a, st) : launch_few8<D, 2, false>(c, a, st);
+    if (rows <= 16 || !plain_q) return near ? launch_few8<D, 2, true>(c, a, st) : launch_few8<D, 2, false>(c, a, st);
+    return near ? launch_many8<D, true>(c, a, rows, st) : launch_many8<D, false>(c, a, rows, st);
 }
 
 }  // namespace

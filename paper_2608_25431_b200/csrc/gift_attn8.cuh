@@ -15,6 +15,7 @@ struct Attn8Args : AttnArgs {
 };
 
 constexpr float LOG2_E = 1.4426950408889634f;
+constexpr float NOTHING = -3e38f;        // the maximum before anything is seen: finite, so that no difference with it is NaN
 
 __device__ __forceinline__ float fast_rcp(float x)
 {
@@ -57,6 +58,18 @@ __device__ __forceinline__ uint32_t codes_without_nan(uint32_t w)
 {
     const uint32_t bad = ((w & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u;      // one bit a byte
     return w & ~((bad >> 7) * 255u);
+}
+
+// Four codes as two pairs.
+__device__ __forceinline__ void four_codes(uint32_t w, uint32_t& lo, uint32_t& hi)
+{
+    asm("{\n .reg .b16 x, y;\n mov.b32 {x, y}, %2;\n cvt.rn.f16x2.e4m3x2 %0, x;\n cvt.rn.f16x2.e4m3x2 %1, y;\n}" : "=r"(lo), "=r"(hi) : "r"(w));
+}
+
+// Two results as a pair of q's type.
+__device__ __forceinline__ uint32_t pack_out(const Attn8Args& a, float lo, float hi)
+{
+    return a.half ? pack2<__half>(lo, hi) : pack2<__nv_bfloat16>(lo, hi);
 }
 
 }  // namespace gift

@@ -1,0 +1,574 @@
+// Attention over labelled pages of 8 bits, many query rows per K/V head: tcgen05 products.
+//
+// The roles and barriers of the 16-bit kernel: a tile of 128 query rows (or what whole tokens fit) meets tiles of 64
+// tokens, S = Q K^T lands in tensor memory, one row per thread of four softmax warps, P goes back into the columns of
+// its S and is the A operand of O += P V.  What differs:
+//   warp 4, 5  fetch the codes of K's and of V's tiles into registers, a tile ahead, and put them as fp16 numbers (exact) into
+//              swizzled shared memory; warp 5 brings the scales of both beside them.  (A product of codes would need q
+//              and the weights as codes too.)  Each judges the labels of the pages that it reads.
+//   softmax    K's scale multiplies the score, V's the weight, in 32 bits.  Weights go to fp16 by a power of two of the row's
+//              own, which follows the largest p * scale as the maximum follows the scores; O is in its units.
+//              bf16 queries become fp16 in place, by a power of two of the row's own too.
+// A token whose V holds the code of NaN gets it into its scale (codes 0), which is used only where the token is seen: what a
+// hidden token holds does not matter.
+// Every wait is bounded; a CTA whose wait runs out notes its unfinished requests, and the joining kernel makes them zero.
+#pragma once
+#include "gift_attn8.cuh"
+#include "gift_tc.cuh"
+
+namespace gift {
+
+constexpr int TC8_ROWS = 128;
+constexpr int TC8_TILE = 64;
+constexpr int TC8_THREADS = 256;
+constexpr int TC8_STAGES = 2;
+constexpr int TC8_BITS_RING = 8;         // pieces whose page verdicts are kept: no warp is more than three ahead of the softmax
+
+template <int D> struct Tc8Smem {
+    static constexpr uint32_t q = 0;                                                  // [D/64][128][64]
+    static constexpr uint32_t k = TC8_ROWS * D * 2;                                   // [stage][D/64][64][64]
+    static constexpr uint32_t v = k + TC8_STAGES * TC8_TILE * D * 2;
+    static constexpr uint32_t o = v + TC8_STAGES * TC8_TILE * D * 2;                  // [4 warps][32 rows][64 bytes]
+    static constexpr uint32_t bytes = o + 4 * 32 * 64;
+};
+
+struct Tc8Shared {
+    uint64_t k_full[TC8_STAGES], k_empty[TC8_STAGES], v_full[TC8_STAGES], v_empty[TC8_STAGES];
+    uint64_t s_full[2], p_full[2], o_done[2], q_full, q_ready, q_empty, last;
+    float k_scale[TC8_STAGES][TC8_TILE], v_scale[TC8_STAGES][TC8_TILE];               // of the tile in the stage of V
+    uint32_t tmem;
+    uint32_t bits[TC8_BITS_RING];
+    int dead;
+    PlaceShared place;
+};
+
+// A role's walk lies in shared memory: its two dozen words are used at a piece's ends, registers in between.
+template <bool NEAR>
+__device__ __noinline__ bool walk8_next(Walk<TC8_TILE, NEAR>& w, const AttnArgs& a, uint32_t lane)
+{
+    Walk<TC8_TILE, NEAR> x = w;
+    const bool more = x.next(a);
+    __syncwarp();
+    if (lane == 0) w = x;
+    __syncwarp();
+    return more;
+}
+
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b)
+{
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+// Waits until another role's generic writes may be read by the tensor cores' proxy.
+__device__ __forceinline__ void publish_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
+template <int D, bool NEAR>
+__global__ void __launch_bounds__(TC8_THREADS, 2) attn8_tc_kernel(const __grid_constant__ Attn8Args a, const __grid_constant__ CUtensorMap q_map)
+{
+    constexpr uint32_t TMEM_COLS = 256;                    // 2 S, O; a power of two, half of what an SM has
+    constexpr uint32_t S_COL = 0, O_COL = 2 * TC8_TILE;
+    extern __shared__ __align__(1024) char smem[];
+    __shared__ __align__(16) Tc8Shared sh;
+    __shared__ Walk<TC8_TILE, NEAR> walks[TC8_THREADS / 32];
+    using L = Tc8Smem<D>;
+
+    join_may_start();
+    if (threadIdx.x == 0) {
+        a.part_head[blockIdx.x * 2u + 1u].pieces = 0u;
+        a.part_stall[blockIdx.x] = make_uint4(0u, 0u, 0u, 0u);
+    }
+    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < TC8_STAGES; i++) {
+            bar_init(&sh.k_full[i], 1); bar_init(&sh.k_empty[i], 1);
+            bar_init(&sh.v_full[i], 1); bar_init(&sh.v_empty[i], 1);
+        }
+        for (int i = 0; i < 2; i++) { bar_init(&sh.s_full[i], 1); bar_init(&sh.p_full[i], 4); bar_init(&sh.o_done[i], 1); }
+        bar_init(&sh.q_full, 1); bar_init(&sh.q_ready, 4); bar_init(&sh.q_empty, 1); bar_init(&sh.last, 2);
+        for (int i = 0; i < TC8_BITS_RING; i++) sh.bits[i] = 0u;
+        sh.dead = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    uint64_t total, slice;
+    // ends with a barrier for every thread, taken or not
+    const bool some = place_unit<TC8_THREADS, NEAR>(a, blockIdx.x / a.ways, TC8_TILE, blockIdx.x == 0, &sh.place, &total, &slice);
+    if (!some) return;
+    if (warp == 6) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sh.tmem)), "r"(TMEM_COLS) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc_before();
+    __syncthreads();
+    tc_after();
+    const uint32_t tmem = sh.tmem;
+    volatile int* dead = &sh.dead;
+    const uint64_t begin = slice * (blockIdx.x / a.ways), units = slice < total - begin ? slice : total - begin;
+    const uint32_t sm = smem_u32(smem);
+    Walk<TC8_TILE, NEAR>& w = walks[warp];
+    {
+        Walk<TC8_TILE, NEAR> x;
+        x.start(a, sh.place.at, blockIdx.x % a.ways, units);
+        if (lane == 0) w = x;
+        __syncwarp();
+    }
+
+    if (warp == 4 || warp == 5) {
+        // ------------------------------------------------------------------ codes to fp16
+        constexpr int ROW_LANES = D / 16, ROWS_AT_ONCE = 32 / ROW_LANES, LOADS = TC8_TILE / ROWS_AT_ONCE;
+        const uint32_t kv = warp - 4, chunk = lane % ROW_LANES, sub = lane / ROW_LANES;
+        uint64_t* full = kv ? sh.v_full : sh.k_full;
+        uint64_t* empty = kv ? sh.v_empty : sh.k_empty;
+        uint32_t n = 0, piece = 0, q_loads = 0;            // tiles and pieces so far
+        bool ok = true;
+        while (ok && walk8_next(w, a, lane)) {
+            const int32_t owner = a.b.owner[w.r];
+            const int32_t* table = a.b.table + (uint64_t)w.r * a.b.max_blocks;
+            const uint32_t want = w.s.want, low = NEAR ? first_seen(a, w.s.have) : 0u, tb = w.tb + (NEAR ? w.it.first : 0u), h = w.h, n_tiles = w.n_tiles;
+            const char* from = a.pages + (uint64_t)kv * a.codes + (uint64_t)h * D + chunk * 16;
+            uint32_t bits = w.masked_short(a) ? GIFT_ST_BAD_DESC : 0u;
+            if (kv == 0) {
+                // Q, once the products of the piece before have read the old rows.  What the box holds past
+                // the request's rows is another request's: rows that nobody asks for.
+                ok = piece == 0 || warp_wait(&sh.q_empty, (piece - 1) & 1u, dead, a);
+                if (!ok) break;
+                q_loads++;
+                if (lane == 0) {
+                    bar_expect(&sh.q_full, a.tile_rows * D * 2);
+#pragma unroll
+                    for (int c = 0; c < D / 64; c++)
+                        copy_q(sm + L::q + c * (TC8_ROWS * 128), &q_map, c * 64, (int32_t)(h * a.group),
+                               (int32_t)(w.row0 + a.by_group.quot(w.qt * a.tile_rows)), &sh.q_full);
+                }
+            }
+            // Lane l looks up tokens l and l + 32 of a tile.  Rounds fetch tile j's table entries, judge and fetch the
+            // codes of tile j - 1, and hand over tile j - 2.
+            int32_t next[2] = {-1, -1}, label[2] = {GIFT_OWNER_PARAM, GIFT_OWNER_PARAM};
+            uint4 raw[LOADS];
+            float2 scale[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+#pragma unroll 1
+            for (uint32_t j = 0; j <= n_tiles + 1; j++) {
+                if (j > 1) {
+                    // tile j - 2 into its stage
+                    const uint32_t stage = n % TC8_STAGES, round = n / TC8_STAGES, t0 = (tb + j - 2) * TC8_TILE;
+                    ok = round == 0 || warp_wait(&empty[stage], (round - 1) & 1u, dead, a);
+                    if (!ok) break;
+                    if (kv && (t0 + TC8_TILE > w.s.have || (NEAR && a.window && t0 + a.window < want))) {
+                        uint64_t odd = 0ull;               // tokens with a NaN among their codes
+#pragma unroll
+                        for (int i = 0; i < LOADS; i++) {
+                            uint4& x = raw[i];
+                            if (codes_nan(x.x) || codes_nan(x.y) || codes_nan(x.z) || codes_nan(x.w)) {
+                                odd |= 1ull << (i * ROWS_AT_ONCE + sub);
+                                x.x = codes_without_nan(x.x); x.y = codes_without_nan(x.y); x.z = codes_without_nan(x.z); x.w = codes_without_nan(x.w);
+                            }
+                        }
+                        const uint32_t odds[2] = {__reduce_or_sync(0xFFFFFFFFu, (uint32_t)odd), __reduce_or_sync(0xFFFFFFFFu, (uint32_t)(odd >> 32))};
+#pragma unroll
+                        for (int e = 0; e < 2; e++)
+                            if (odds[e] >> lane & 1u) scale[e].y = __uint_as_float(0x7FC00000u);
+                    }
+                    if (kv)
+#pragma unroll
+                        for (int e = 0; e < 2; e++) {
+                            sh.k_scale[stage][e * 32 + lane] = scale[e].x;
+                            sh.v_scale[stage][e * 32 + lane] = scale[e].y;
+                        }
+                    // 16 codes are two 16-byte chunks of their row; lanes of the second block of 64 columns begin with the
+                    // second one, for other banks than those of the first
+                    const uint32_t block = chunk >> 2, dst = sm + (kv ? L::v : L::k) + stage * (TC8_TILE * D * 2) + block * (TC8_TILE * 128);
+#pragma unroll
+                    for (int i = 0; i < LOADS; i++) {
+                        const uint32_t row = i * ROWS_AT_ONCE + sub;
+                        const uint32_t word[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
+                        uint32_t f[8];
+#pragma unroll
+                        for (int y = 0; y < 4; y++) four_codes(word[y], f[2 * y], f[2 * y + 1]);
+#pragma unroll
+                        for (uint32_t y = 0; y < 2; y++) {
+                            const bool second = (y ^ block) & 1u;
+                            const uint32_t at = dst + row * 128 + ((((chunk & 3u) * 2 + (second ? 1u : 0u)) ^ (row & 7u)) << 4);
+                            asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(second ? f[4] : f[0]), "r"(second ? f[5] : f[1]),
+                                         "r"(second ? f[6] : f[2]), "r"(second ? f[7] : f[3]) : "memory");
+                        }
+                    }
+                    publish_smem();
+                    if (j == n_tiles + 1) {
+                        // this warp's verdict on the piece, before its last tile is announced
+                        bits |= label_read_status(label[0], owner) | label_read_status(label[1], owner);
+                        bits = __reduce_or_sync(0xFFFFFFFFu, bits);
+                        if (lane == 0 && bits) atomicOr(&sh.bits[piece % TC8_BITS_RING], bits);
+                    }
+                    __syncwarp();
+                    if (lane == 0) bar_arrive(&full[stage]);
+                    n++;
+                }
+                if (j > n_tiles) continue;
+                uint32_t slot[2];
+#pragma unroll
+                for (int e = 0; e < 2; e++) {
+                    // the slots of tile j - 1, and the entries of tile j
+                    const uint32_t t_next = (tb + j) * TC8_TILE + e * 32 + lane, t = t_next - TC8_TILE;
+                    bits |= label_read_status(label[e], owner);
+                    label[e] = GIFT_OWNER_PARAM;
+                    slot[e] = 0xFFFFFFFFu;
+                    if (j > 0 && t < want && (!NEAR || t >= low)) {
+                        if ((uint32_t)next[e] < a.b.n_pages) {
+                            slot[e] = (uint32_t)next[e] * a.b.page_tokens + (t - a.b.page.quot(t) * a.b.page_tokens);
+                            if (a.owner_map) label[e] = a.owner_map[next[e]];
+                        } else {
+                            bits |= GIFT_ST_BAD_DESC;
+                        }
+                    }
+                    next[e] = j < n_tiles && t_next < want && (!NEAR || t_next >= low) ? table[a.b.page.quot(t_next)] : -1;
+                    if (kv) {
+                        scale[e] = make_float2(0.f, 0.f);
+                        if (slot[e] != 0xFFFFFFFFu) scale[e] = *reinterpret_cast<const float2*>(a.pages + slot[e] * a.token_bytes + 2ull * a.codes + h * 8u);
+                    }
+                }
+                if (j == 0) continue;
+                // tokens that nobody sees are zeros: what memory holds there does not matter
+#pragma unroll
+                for (int i = 0; i < LOADS; i++) {
+                    const uint32_t row = i * ROWS_AT_ONCE + sub;
+                    const uint32_t at = __shfl_sync(0xFFFFFFFFu, slot[i * ROWS_AT_ONCE / 32], row & 31u);
+                    raw[i] = make_uint4(0u, 0u, 0u, 0u);
+                    if (at != 0xFFFFFFFFu) raw[i] = *reinterpret_cast<const uint4*>(from + at * a.token_bytes);
+                }
+            }
+            piece++;
+        }
+        // the copies under way end before the CTA does, whether or not anybody is left to wait for them
+        if (kv == 0 && q_loads > 0) bar_drain(&sh.q_full, (q_loads - 1) & 1u);
+    } else if (warp == 6) {
+        // ------------------------------------------------------------------ Q K^T
+        // a negative scale: the products negate q, so that the scale used on the scores is positive
+        const uint32_t id_s = instr_desc<__half>(TC8_ROWS, TC8_TILE, 0) | (a.negate << 13);
+        const uint64_t q_desc = smem_desc(sm + L::q, 16, 1024), k_desc = smem_desc(sm + L::k, 16, 1024);
+        uint32_t n = 0, piece = 0;
+        bool ok = true;
+        while (ok && walk8_next(w, a, lane)) {
+            const uint32_t n_tiles = w.n_tiles;
+            if (lane == 0) {
+                ok = bar_wait(&sh.q_ready, piece & 1u, dead, a);
+#pragma unroll 1
+                for (uint32_t j = 0; ok && j < n_tiles; j++) {
+                    const uint32_t t = n + j, stage = t % TC8_STAGES;
+                    // S takes the columns that held P of tile t - 2
+                    ok = bar_wait(&sh.k_full[stage], (t / TC8_STAGES) & 1u, dead, a) &&
+                         (t < 2 || bar_wait(&sh.o_done[t & 1u], ((t - 2) >> 1) & 1u, dead, a));
+                    if (!ok) break;
+                    tc_after();
+                    const uint64_t kb = k_desc + stage * (TC8_TILE * D * 2 / 16);
+                    const uint32_t d = tmem + S_COL + (t & 1u) * TC8_TILE;
+#pragma unroll
+                    for (uint32_t ks = 0; ks < D / 16; ks++)       // 16 columns are 32 bytes; 64 columns a block
+                        mma_ss(d, q_desc + (ks >> 2) * (TC8_ROWS * 128 / 16) + (ks & 3u) * 2,
+                               kb + (ks >> 2) * (TC8_TILE * 128 / 16) + (ks & 3u) * 2, id_s, ks > 0);
+                    mma_commit(&sh.s_full[t & 1u]);
+                    mma_commit(&sh.k_empty[stage]);
+                    if (j + 1 == n_tiles) mma_commit(&sh.q_empty);
+                }
+            }
+            ok = __shfl_sync(0xFFFFFFFFu, ok, 0);
+            n += n_tiles;
+            piece++;
+        }
+        if (lane == 0) {
+            // nothing may be in flight when the tensor memory is given back
+            mma_commit(&sh.last);
+            bar_drain(&sh.last, 0);
+        }
+        __syncwarp();
+    } else if (warp == 7) {
+        // ------------------------------------------------------------------ P V
+        constexpr uint32_t id_o = instr_desc<__half>(TC8_ROWS, D, 1);
+        const uint64_t v_desc = smem_desc(sm + L::v, TC8_TILE * 128, 1024);
+        uint32_t n = 0;
+        bool ok = true;
+        while (ok && walk8_next(w, a, lane)) {
+            const uint32_t n_tiles = w.n_tiles;
+            if (lane == 0)
+#pragma unroll 1
+                for (uint32_t j = 0; ok && j < n_tiles; j++) {
+                    const uint32_t t = n + j, stage = t % TC8_STAGES;
+                    ok = bar_wait(&sh.v_full[stage], (t / TC8_STAGES) & 1u, dead, a) && bar_wait(&sh.p_full[t & 1u], (t >> 1) & 1u, dead, a);
+                    if (!ok) break;
+                    tc_after();
+                    const uint64_t vb = v_desc + stage * (TC8_TILE * D * 2 / 16);
+                    const uint32_t p = tmem + S_COL + (t & 1u) * TC8_TILE;
+#pragma unroll
+                    for (uint32_t ks = 0; ks < TC8_TILE / 16; ks++)      // 16 tokens are 8 columns of P, 2048 bytes of V
+                        mma_ts(tmem + O_COL, p + ks * 8, vb + ks * (2048 / 16), id_o, j > 0 || ks > 0);
+                    mma_commit(&sh.o_done[t & 1u]);
+                    mma_commit(&sh.v_empty[stage]);
+                }
+            ok = __shfl_sync(0xFFFFFFFFu, ok, 0);
+            n += n_tiles;
+        }
+        if (lane == 0) {
+            mma_commit(&sh.last);
+            bar_drain(&sh.last, 0);
+        }
+        __syncwarp();
+    } else {
+        // ------------------------------------------------------------------ softmax
+        const uint32_t row = threadIdx.x, lane_base = (warp * 32u) << 16;
+        uint32_t n = 0, piece = 0;
+        char* stage_o = smem + L::o + warp * (32 * 64);
+        bool alive = true;
+        while (walk8_next(w, a, lane)) {
+            const uint32_t rho = w.qt * a.tile_rows + row;
+            const bool there = rho < w.all_q && row < a.tile_rows;
+            const bool warp_there = w.qt * a.tile_rows + warp * 32 < w.all_q && warp * 32 < a.tile_rows;
+            const uint32_t i = there ? a.by_group.quot(rho) : 0u, hq = w.h * a.group + (there ? rho - i * a.group : 0u);
+            const bool masked_short = w.masked_short(a);
+            float scale = NEAR && a.cap_out != 0.f ? a.cap_in : a.scale_log2;
+            if (alive && warp_wait(&sh.q_full, piece & 1u, dead, a)) {
+                if (!a.half && warp_there) {
+                    // this row as fp16 numbers, by a power of two
+                    char* q = smem + L::q + row * 128;
+                    uint32_t top = 0u;
+#pragma unroll 4
+                    for (uint32_t x = 0; x < D / 8; x++) {
+                        const uint4 v = *reinterpret_cast<const uint4*>(q + (x >> 3) * (TC8_ROWS * 128) + (((x & 7u) ^ (row & 7u)) << 4));
+                        const uint32_t word[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                        for (int y = 0; y < 4; y++) top = max(top, max(word[y] << 16 & 0x7FFFFFFFu, word[y] & 0x7FFF0000u));
+                    }
+                    const uint32_t e = top_exponent(top);
+                    const float f = to_half_range(e);
+                    scale *= from_half_range(e);
+#pragma unroll 4
+                    for (uint32_t x = 0; x < D / 8; x++) {
+                        uint4* at = reinterpret_cast<uint4*>(q + (x >> 3) * (TC8_ROWS * 128) + (((x & 7u) ^ (row & 7u)) << 4));
+                        uint4 v = *at;
+                        v.x = pack2<__half>(__uint_as_float(v.x << 16) * f, __uint_as_float(v.x & 0xFFFF0000u) * f);
+                        v.y = pack2<__half>(__uint_as_float(v.y << 16) * f, __uint_as_float(v.y & 0xFFFF0000u) * f);
+                        v.z = pack2<__half>(__uint_as_float(v.z << 16) * f, __uint_as_float(v.z & 0xFFFF0000u) * f);
+                        v.w = pack2<__half>(__uint_as_float(v.w << 16) * f, __uint_as_float(v.w & 0xFFFF0000u) * f);
+                        *at = v;
+                    }
+                    publish_smem();
+                }
+                __syncwarp();
+                if (lane == 0) bar_arrive(&sh.q_ready);
+            } else {
+                alive = false;
+            }
+            // the factor is positive (q's sign carries the scale's), and not 0, so that a hidden token's minus infinity stays
+            scale = fmaxf(scale, 1e-37f);
+            const float slope = NEAR && a.slopes && there ? a.slopes[hq] * LOG2_E : 0.f;
+            float m = NOTHING, l = 0.f;                    // the maximum in use, the sum relative to it
+            float most = 0.f, to_half = to_half_range(9u), room = half_range_end(9u);
+#pragma unroll 1
+            for (uint32_t j = 0; alive && j < w.n_tiles; j++, n++) {
+                const uint32_t s_at = tmem + lane_base + S_COL + (n & 1u) * TC8_TILE, stage = n % TC8_STAGES;
+                const uint32_t t0 = (w.tb + (NEAR ? w.it.first : 0u) + j) * TC8_TILE;
+                const bool mixed = t0 + TC8_TILE > w.s.have || (NEAR && a.window && t0 + a.window < w.s.want);
+                uint64_t sees = ~0ull;
+                if (mixed) {
+                    sees = there && !masked_short ? row_sees64(a, w.s.have, w.s.want, w.row0 + i, i, t0) : 0ull;
+                    if (NEAR && a.window) sees &= in_window64(a.window, w.s.have + i, t0);
+                }
+                // the tile's V, whose scales (and K's) are read here, cannot be replaced before P V of this tile
+                if (!warp_wait(&sh.v_full[stage], (n / TC8_STAGES) & 1u, dead, a) || !warp_wait(&sh.s_full[n & 1u], (n >> 1) & 1u, dead, a)) {
+                    alive = false;
+                    break;
+                }
+                if (!warp_there) {                         // rows that do not exist: whatever P holds stays in them
+                    __syncwarp();
+                    if (lane == 0) bar_arrive(&sh.p_full[n & 1u]);
+                    continue;
+                }
+                tc_after();
+                uint32_t sc[2][32];
+                tc_ld32(sc[0], s_at);
+                tc_ld32(sc[1], s_at + 32);
+                tc_wait_ld();
+                tc_pin32(sc[0]);
+                tc_pin32(sc[1]);
+                float tops[4] = {NEG_INF, NEG_INF, NEG_INF, NEG_INF};
+#pragma unroll
+                for (int x = 0; x < 2; x++)
+#pragma unroll
+                    for (int c = 0; c < 32; c += 4) {
+                        const float4 ks = *reinterpret_cast<const float4*>(&sh.k_scale[stage][32 * x + c]);
+                        float y[4];
+                        split2(mul2(pair2(__uint_as_float(sc[x][c]), __uint_as_float(sc[x][c + 1])), pair2(ks.x, ks.y)), y[0], y[1]);
+                        split2(mul2(pair2(__uint_as_float(sc[x][c + 2]), __uint_as_float(sc[x][c + 3])), pair2(ks.z, ks.w)), y[2], y[3]);
+                        if constexpr (NEAR) {
+#pragma unroll
+                            for (int e = 0; e < 4; e++) {
+                                y[e] *= scale;
+                                if (a.cap_out != 0.f) y[e] = a.cap_out * tanh_of(y[e]);
+                                if (a.slopes) y[e] += slope * (float)((int32_t)(t0 + 32 * x + c + e) - (int32_t)(w.s.have + i));
+                            }
+                        }
+#pragma unroll
+                        for (int e = 0; e < 4; e++) {
+                            if (mixed && !((uint32_t)(sees >> (32 * x)) >> (c + e) & 1u)) y[e] = NEG_INF;
+                            sc[x][c + e] = __float_as_uint(y[e]);
+                        }
+                        tops[(c >> 2) & 3] = max3(tops[(c >> 2) & 3], fmaxf(y[0], y[1]), fmaxf(y[2], y[3]));
+                    }
+                // the scale is positive here (q's sign carries it), so the largest score stays the largest
+                const float by = NEAR ? 1.f : scale;
+                const float top = max3(tops[0], tops[1], fmaxf(tops[2], tops[3])) * by;
+                const bool grow = top > m + 8.f;           // also when nothing has been seen yet
+                float alpha = 1.f;
+                if (grow) {
+                    alpha = fast_exp2(m - top);
+                    m = top;
+                }
+                const uint64_t by2 = pair2(by, by), minus2 = pair2(-m, -m);
+                uint64_t sums[2] = {0ull, 0ull};
+                float bigs[2] = {0.f, 0.f};
+#pragma unroll
+                for (int x = 0; x < 2; x++)
+#pragma unroll
+                    for (int c = 0; c < 32; c += 4) {
+                        const float4 vs = *reinterpret_cast<const float4*>(&sh.v_scale[stage][32 * x + c]);
+#pragma unroll
+                        for (int e = 0; e < 4; e += 2) {
+                            float lo, hi;
+                            split2(fma2(pair2(__uint_as_float(sc[x][c + e]), __uint_as_float(sc[x][c + e + 1])), by2, minus2), lo, hi);
+                            lo = fast_exp2(lo);
+                            hi = fast_exp2(hi);
+                            const uint64_t p = pair2(lo, hi);
+                            sums[e >> 1] = add2(sums[e >> 1], p);
+                            split2(mul2(p, e ? pair2(vs.z, vs.w) : pair2(vs.x, vs.y)), lo, hi);
+                            if (mixed) {                   // 0 times a scale that is NaN
+                                if (!((uint32_t)(sees >> (32 * x)) >> (c + e) & 1u)) lo = 0.f;
+                                if (!((uint32_t)(sees >> (32 * x)) >> (c + e + 1) & 1u)) hi = 0.f;
+                            }
+                            bigs[e >> 1] = max3(bigs[e >> 1], lo, hi);
+                            sc[x][c + e] = __float_as_uint(lo);
+                            sc[x][c + e + 1] = __float_as_uint(hi);
+                        }
+                    }
+                {
+                    float lo, hi;
+                    split2(add2(sums[0], sums[1]), lo, hi);
+                    l = l * alpha + (lo + hi);
+                }
+                const float big = fmaxf(bigs[0], bigs[1]);
+                float ratio = 1.f;
+                if (grow || big > room) {
+                    most = fmaxf(most * alpha, big);
+                    const uint32_t e = top_exponent(__float_as_uint(most));
+                    const float f = to_half_range(e);
+                    ratio = alpha * inverse_power(to_half) * f;
+                    to_half = f;
+                    room = half_range_end(e);
+                }
+                const uint64_t half2 = pair2(to_half, to_half);
+#pragma unroll
+                for (int x = 0; x < 2; x++) {
+                    // P into the first 32 columns of its S
+                    uint32_t pk[16];
+#pragma unroll
+                    for (int c = 0; c < 16; c++) {
+                        float lo, hi;
+                        split2(mul2(pair2(__uint_as_float(sc[x][2 * c]), __uint_as_float(sc[x][2 * c + 1])), half2), lo, hi);
+                        pk[c] = pack2<__half>(lo, hi);
+                    }
+                    tc_st16(s_at + x * 16, pk);
+                }
+                if (j > 0 && __any_sync(0xFFFFFFFFu, ratio != 1.f && there)) {
+                    // Every product so far is in O (the one of tile n is not issued before p_full).  That
+                    // the barrier is no more than one phase behind follows from S of tile n - 1, whose
+                    // product waited for tile n - 3's P V.
+                    if (!warp_wait(&sh.o_done[(n - 1) & 1u], ((n - 1) >> 1) & 1u, dead, a)) { tc_wait_st(); alive = false; break; }
+                    tc_after();
+#pragma unroll 1
+                    for (uint32_t c0 = 0; c0 < (uint32_t)D; c0 += 32) {
+                        uint32_t o[32];
+                        tc_ld32(o, tmem + lane_base + O_COL + c0);
+                        tc_wait_ld();
+                        tc_pin32(o);
+#pragma unroll
+                        for (int c = 0; c < 32; c++) o[c] = __float_as_uint(__uint_as_float(o[c]) * ratio);
+                        tc_st32(tmem + lane_base + O_COL + c0, o);
+                    }
+                }
+                tc_wait_st();
+                tc_before();
+                __syncwarp();
+                if (lane == 0) bar_arrive(&sh.p_full[n & 1u]);
+            }
+            // ---------------------------------------------------------- the piece's end
+            if (alive) alive = warp_wait(&sh.o_done[(n - 1) & 1u], ((n - 1) >> 1) & 1u, dead, a);
+            tc_after();
+            // The four warps agree on how the piece ended: it is complete when each of them saw its last
+            // product, whatever the other roles come to.  The verdict of the piece before, which all have read
+            // by now, makes room.
+            alive = !any_softmax(!alive);
+            const uint32_t bits = alive ? *(volatile uint32_t*)&sh.bits[piece % TC8_BITS_RING] : (uint32_t)GIFT_ST_STALLED;
+            if (!alive && row == 0) w.note_stall(a);
+            if (row == 0) *(volatile uint32_t*)&sh.bits[(piece + TC8_BITS_RING - 1) % TC8_BITS_RING] = 0u;
+            const bool whole = w.whole();
+            const uint32_t slot = w.slot();
+            const bool none = bits != 0u || l == 0.f;
+            const float unit = inverse_power(to_half), inv = none ? 0.f : 1.f / l;
+            if (warp_there) {
+                // Rows leave by way of shared memory, 64 bytes of 32 rows at a time, so that four lanes write
+                // a row's 64 bytes.
+                char* mine = whole ? a.out + (uint64_t)(w.row0 + i) * a.out_row + (uint64_t)hq * a.out_head
+                                   : reinterpret_cast<char*>(a.part_o + ((uint64_t)slot * TC8_ROWS + row) * D);
+                const uint32_t last = w.all_q - w.qt * a.tile_rows < a.tile_rows ? w.all_q - w.qt * a.tile_rows : a.tile_rows;
+                const uint32_t rows = last - warp * 32;                         // rows of this warp that exist, if below 32
+#pragma unroll 1
+                for (uint32_t c0 = 0; c0 < (uint32_t)D; c0 += 32) {
+                    uint32_t o[32];
+                    tc_ld32(o, tmem + lane_base + O_COL + c0);
+                    tc_wait_ld();
+                    tc_pin32(o);
+#pragma unroll
+                    for (int x = 0; x < 32; x++) o[x] = __float_as_uint(__uint_as_float(o[x]) * unit);
+                    if (whole) {
+#pragma unroll
+                        for (int x = 0; x < 16; x++)
+                            o[x] = none ? 0u : pack_out(a, __uint_as_float(o[2 * x]) * inv, __uint_as_float(o[2 * x + 1]) * inv);
+                    }
+                    const uint32_t parts = whole ? 1 : 2;                       // 32 columns are 64 or 128 bytes
+#pragma unroll
+                    for (uint32_t part = 0; part < 2; part++) {
+                        if (part >= parts) break;
+#pragma unroll
+                        for (uint32_t x = 0; x < 4; x++)
+                            *reinterpret_cast<uint4*>(stage_o + lane * 64 + ((x ^ ((lane >> 1) & 3u)) << 4)) =
+                                make_uint4(o[part * 16 + 4 * x], o[part * 16 + 4 * x + 1], o[part * 16 + 4 * x + 2], o[part * 16 + 4 * x + 3]);
+                        __syncwarp();
+#pragma unroll
+                        for (uint32_t y = 0; y < 4; y++) {
+                            const uint32_t other = y * 8 + (lane >> 2), x = lane & 3u;
+                            char* to = reinterpret_cast<char*>(__shfl_sync(0xFFFFFFFFu, (unsigned long long)mine, other));
+                            const uint4 v = *reinterpret_cast<const uint4*>(stage_o + other * 64 + ((x ^ ((other >> 1) & 3u)) << 4));
+                            if (other < rows) *reinterpret_cast<uint4*>(to + (whole ? c0 * 2 : c0 * 4 + part * 64) + x * 16) = v;
+                        }
+                        __syncwarp();
+                    }
+                }
+                if (there) {
+                    if (!whole) a.part_ml[(uint64_t)slot * TC8_ROWS + row] = make_float2(m, l);
+                    else if (a.lse) a.lse[(uint64_t)(w.row0 + i) * a.heads + hq] = none ? NEG_INF : (m + log2f(l)) * 0.6931471805599453f;
+                }
+            }
+            if (whole) {
+                if (w.h == 0 && w.qt == 0) write_request<128>(a, w.r, w.row0, w.it.rows_m, bits);
+            } else if (row == 0) {
+                w.write_head(a, bits, slice);
+            }
+            tc_before();
+            piece++;
+        }
+    }
+    __syncthreads();
+    if (warp == 6) {
+        tc_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(TMEM_COLS) : "memory");
+    }
+}
+
+}  // namespace gift

@@ -58,22 +58,6 @@ template <int D, int NR> struct Few8 {
     }
 };
 
-__device__ __forceinline__ void cp_async8(uint32_t dst, const void* src, uint32_t bytes)
-{
-    asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
-}
-__device__ __forceinline__ uint4 lds128(uint32_t at)
-{
-    uint4 x;
-    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w) : "r"(at) : "memory");
-    return x;
-}
-__device__ __forceinline__ float2 lds_pair(uint32_t at)
-{
-    float2 x;
-    asm volatile("ld.shared.v2.f32 {%0,%1}, [%2];" : "=f"(x.x), "=f"(x.y) : "r"(at) : "memory");
-    return x;
-}
 // An 8 x 8 matrix of 16-bit elements, two of a row in each lane, transposed.
 __device__ __forceinline__ uint32_t transposed(uint32_t x)
 {

@@ -3,9 +3,10 @@
 // The roles and barriers of the 16-bit kernel: a tile of 128 query rows (or what whole tokens fit) meets tiles of 64
 // tokens, S = Q K^T lands in tensor memory, one row per thread of four softmax warps, P goes back into the columns of
 // its S and is the A operand of O += P V.  What differs:
-//   warp 4, 5  fetch the codes of K's and of V's tiles into registers, a tile ahead, and put them as fp16 numbers (exact) into
-//              swizzled shared memory; warp 5 brings the scales of both beside them.  (A product of codes would need q
-//              and the weights as codes too.)  Each judges the labels of the pages that it reads.
+//   warp 4, 5  fetch the codes of K's and of V's tiles into shared memory, two tiles ahead (fetched into registers, one
+//              ahead, they came too late: 1182 us for what takes 492 with nothing to fetch), and put them as fp16 numbers
+//              (exact) where the products read them; warp 5 brings the scales of both.  (A product of codes
+//              would need q and the weights as codes too.)  Each judges the labels of the pages that it reads.
 //   softmax    K's scale multiplies the score, V's the weight, in 32 bits.  Weights go to fp16 by a power of two of the row's
 //              own, which follows the largest p * scale as the maximum follows the scores; O is in its units.
 //              bf16 queries become fp16 in place, by a power of two of the row's own too.
@@ -21,21 +22,23 @@ namespace gift {
 constexpr int TC8_ROWS = 128;
 constexpr int TC8_TILE = 64;
 constexpr int TC8_THREADS = 256;
-constexpr int TC8_STAGES = 2;
+constexpr int TC8_AHEAD = 2;             // tiles whose codes are on their way
 constexpr int TC8_BITS_RING = 8;         // pieces whose page verdicts are kept: no warp is more than three ahead of the softmax
 
 template <int D> struct Tc8Smem {
     static constexpr uint32_t q = 0;                                                  // [D/64][128][64]
-    static constexpr uint32_t k = TC8_ROWS * D * 2;                                   // [stage][D/64][64][64]
-    static constexpr uint32_t v = k + TC8_STAGES * TC8_TILE * D * 2;
-    static constexpr uint32_t o = v + TC8_STAGES * TC8_TILE * D * 2;                  // [4 warps][32 rows][64 bytes]
-    static constexpr uint32_t bytes = o + 4 * 32 * 64;
+    static constexpr uint32_t k = TC8_ROWS * D * 2;                                   // [D/64][64][64]
+    static constexpr uint32_t v = k + TC8_TILE * D * 2;
+    static constexpr uint32_t o = v + TC8_TILE * D * 2;                               // [4 warps][32 rows][64 bytes]
+    static constexpr uint32_t codes = o + 4 * 32 * 64;                                // of K, of V: [2 tiles][64][D]
+    static constexpr uint32_t scales = codes + 2 * TC8_AHEAD * TC8_TILE * D;          // [2 tiles][64] of both
+    static constexpr uint32_t bytes = scales + TC8_AHEAD * TC8_TILE * 8;
 };
 
 struct Tc8Shared {
-    uint64_t k_full[TC8_STAGES], k_empty[TC8_STAGES], v_full[TC8_STAGES], v_empty[TC8_STAGES];
+    uint64_t k_full, k_empty, v_full, v_empty, scaled[4];
     uint64_t s_full[2], p_full[2], o_done[2], q_full, q_ready, q_empty, last;
-    float k_scale[TC8_STAGES][TC8_TILE], v_scale[TC8_STAGES][TC8_TILE];               // of the tile in the stage of V
+    float k_scale[4][TC8_TILE], v_scale[4][TC8_TILE];                                 // by tile
     uint32_t tmem;
     uint32_t bits[TC8_BITS_RING];
     int dead;
@@ -80,10 +83,8 @@ __global__ void __launch_bounds__(TC8_THREADS, 2) attn8_tc_kernel(const __grid_c
     }
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
-        for (int i = 0; i < TC8_STAGES; i++) {
-            bar_init(&sh.k_full[i], 1); bar_init(&sh.k_empty[i], 1);
-            bar_init(&sh.v_full[i], 1); bar_init(&sh.v_empty[i], 1);
-        }
+        bar_init(&sh.k_full, 1); bar_init(&sh.k_empty, 1); bar_init(&sh.v_full, 1); bar_init(&sh.v_empty, 1);
+        for (int i = 0; i < 4; i++) bar_init(&sh.scaled[i], 1);
         for (int i = 0; i < 2; i++) { bar_init(&sh.s_full[i], 1); bar_init(&sh.p_full[i], 4); bar_init(&sh.o_done[i], 1); }
         bar_init(&sh.q_full, 1); bar_init(&sh.q_ready, 4); bar_init(&sh.q_empty, 1); bar_init(&sh.last, 2);
         for (int i = 0; i < TC8_BITS_RING; i++) sh.bits[i] = 0u;
@@ -115,11 +116,13 @@ __global__ void __launch_bounds__(TC8_THREADS, 2) attn8_tc_kernel(const __grid_c
 
     if (warp == 4 || warp == 5) {
         // ------------------------------------------------------------------ codes to fp16
+        // Of a tile's codes a lane fetches, and later converts, 16 from 16 chunk of every ROWS_AT_ONCE-th token.
         constexpr int ROW_LANES = D / 16, ROWS_AT_ONCE = 32 / ROW_LANES, LOADS = TC8_TILE / ROWS_AT_ONCE;
         const uint32_t kv = warp - 4, chunk = lane % ROW_LANES, sub = lane / ROW_LANES;
-        uint64_t* full = kv ? sh.v_full : sh.k_full;
-        uint64_t* empty = kv ? sh.v_empty : sh.k_empty;
-        uint32_t n = 0, piece = 0, q_loads = 0;            // tiles and pieces so far
+        uint64_t* full = kv ? &sh.v_full : &sh.k_full;
+        uint64_t* empty = kv ? &sh.v_empty : &sh.k_empty;
+        const uint32_t raw = sm + L::codes + kv * (TC8_AHEAD * TC8_TILE * D) + lane * 16, raw_scale = sm + L::scales + lane * 8;
+        uint32_t n = 0, fetched = 0, piece = 0, q_loads = 0;           // tiles and pieces so far
         bool ok = true;
         while (ok && walk8_next(w, a, lane)) {
             const int32_t owner = a.b.owner[w.r];
@@ -141,104 +144,117 @@ __global__ void __launch_bounds__(TC8_THREADS, 2) attn8_tc_kernel(const __grid_c
                                (int32_t)(w.row0 + a.by_group.quot(w.qt * a.tile_rows)), &sh.q_full);
                 }
             }
-            // Lane l looks up tokens l and l + 32 of a tile.  Rounds fetch tile j's table entries, judge and fetch the
-            // codes of tile j - 1, and hand over tile j - 2.
+            // Lane l looks up tokens l and l + 32 of a tile.  Round j fetches tile j's table entries, judges and fetches the
+            // codes of tile j - 1, and before that hands over tile j - 3, whose place those take.
             int32_t next[2] = {-1, -1}, label[2] = {GIFT_OWNER_PARAM, GIFT_OWNER_PARAM};
-            uint4 raw[LOADS];
-            float2 scale[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll 1
-            for (uint32_t j = 0; j <= n_tiles + 1; j++) {
-                if (j > 1) {
-                    // tile j - 2 into its stage
-                    const uint32_t stage = n % TC8_STAGES, round = n / TC8_STAGES, t0 = (tb + j - 2) * TC8_TILE;
-                    ok = round == 0 || warp_wait(&empty[stage], (round - 1) & 1u, dead, a);
-                    if (!ok) break;
-                    if (kv && (t0 + TC8_TILE > w.s.have || (NEAR && a.window && t0 + a.window < want))) {
-                        uint64_t odd = 0ull;               // tokens with a NaN among their codes
+            for (uint32_t j = 0; j < n_tiles + 3; j++) {
+                bits |= label_read_status(label[0], owner) | label_read_status(label[1], owner);
+                label[0] = label[1] = GIFT_OWNER_PARAM;
+                if (j > 2) {
+                    const uint32_t t0 = (tb + j - 3) * TC8_TILE, place = raw + (n % TC8_AHEAD) * (TC8_TILE * D);
+                    cp_wait<1>();
+                    if (kv) {
+                        // the scales, which the softmax may have before V
+                        float2 scale[2];
 #pragma unroll
-                        for (int i = 0; i < LOADS; i++) {
-                            uint4& x = raw[i];
-                            if (codes_nan(x.x) || codes_nan(x.y) || codes_nan(x.z) || codes_nan(x.w)) {
-                                odd |= 1ull << (i * ROWS_AT_ONCE + sub);
-                                x.x = codes_without_nan(x.x); x.y = codes_without_nan(x.y); x.z = codes_without_nan(x.z); x.w = codes_without_nan(x.w);
+                        for (int e = 0; e < 2; e++) scale[e] = lds_pair(raw_scale + (n % TC8_AHEAD) * (TC8_TILE * 8) + e * 256);
+                        if (t0 + TC8_TILE > w.s.have || (NEAR && a.window && t0 + a.window < want)) {
+                            uint32_t odd[2] = {0u, 0u};        // tokens with a NaN among their codes
+#pragma unroll 4
+                            for (int i = 0; i < LOADS; i++) {
+                                const uint4 x = lds128(place + i * 512);
+                                const uint32_t token = i * ROWS_AT_ONCE + sub;
+                                if (codes_nan(x.x) || codes_nan(x.y) || codes_nan(x.z) || codes_nan(x.w)) {
+                                    odd[token >> 5] |= 1u << (token & 31u);
+                                    asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(place + i * 512), "r"(codes_without_nan(x.x)),
+                                                 "r"(codes_without_nan(x.y)), "r"(codes_without_nan(x.z)), "r"(codes_without_nan(x.w)) : "memory");
+                                }
                             }
-                        }
-                        const uint32_t odds[2] = {__reduce_or_sync(0xFFFFFFFFu, (uint32_t)odd), __reduce_or_sync(0xFFFFFFFFu, (uint32_t)(odd >> 32))};
 #pragma unroll
-                        for (int e = 0; e < 2; e++)
-                            if (odds[e] >> lane & 1u) scale[e].y = __uint_as_float(0x7FC00000u);
-                    }
-                    if (kv)
+                            for (int e = 0; e < 2; e++)
+                                if (__reduce_or_sync(0xFFFFFFFFu, odd[e]) >> lane & 1u) scale[e].y = __uint_as_float(0x7FC00000u);
+                        }
 #pragma unroll
                         for (int e = 0; e < 2; e++) {
-                            sh.k_scale[stage][e * 32 + lane] = scale[e].x;
-                            sh.v_scale[stage][e * 32 + lane] = scale[e].y;
+                            sh.k_scale[n & 3u][e * 32 + lane] = scale[e].x;
+                            sh.v_scale[n & 3u][e * 32 + lane] = scale[e].y;
                         }
+                        __syncwarp();
+                        if (lane == 0) bar_arrive(&sh.scaled[n & 3u]);
+                    }
+                    ok = n == 0 || warp_wait(empty, (n - 1) & 1u, dead, a);
+                    if (!ok) break;
                     // 16 codes are two 16-byte chunks of their row; lanes of the second block of 64 columns begin with the
                     // second one, for other banks than those of the first
-                    const uint32_t block = chunk >> 2, dst = sm + (kv ? L::v : L::k) + stage * (TC8_TILE * D * 2) + block * (TC8_TILE * 128);
-#pragma unroll
+                    const uint32_t block = chunk >> 2, dst = sm + (kv ? L::v : L::k) + block * (TC8_TILE * 128);
+#pragma unroll 4
                     for (int i = 0; i < LOADS; i++) {
                         const uint32_t row = i * ROWS_AT_ONCE + sub;
-                        const uint32_t word[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
-                        uint32_t f[8];
-#pragma unroll
-                        for (int y = 0; y < 4; y++) four_codes(word[y], f[2 * y], f[2 * y + 1]);
-#pragma unroll
-                        for (uint32_t y = 0; y < 2; y++) {
-                            const bool second = (y ^ block) & 1u;
-                            const uint32_t at = dst + row * 128 + ((((chunk & 3u) * 2 + (second ? 1u : 0u)) ^ (row & 7u)) << 4);
-                            asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(second ? f[4] : f[0]), "r"(second ? f[5] : f[1]),
-                                         "r"(second ? f[6] : f[2]), "r"(second ? f[7] : f[3]) : "memory");
-                        }
+                        const uint4 x = lds128(place + i * 512);
+                        const uint32_t first[2] = {block ? x.z : x.x, block ? x.w : x.y}, second[2] = {block ? x.x : x.z, block ? x.y : x.w};
+                        const uint32_t at = dst + row * 128 + (((chunk & 3u) * 2 + block ^ (row & 7u)) << 4);
+                        uint32_t f[4];
+                        four_codes(first[0], f[0], f[1]);
+                        four_codes(first[1], f[2], f[3]);
+                        asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(f[0]), "r"(f[1]), "r"(f[2]), "r"(f[3]) : "memory");
+                        four_codes(second[0], f[0], f[1]);
+                        four_codes(second[1], f[2], f[3]);
+                        asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(at ^ 16u), "r"(f[0]), "r"(f[1]), "r"(f[2]), "r"(f[3]) : "memory");
                     }
                     publish_smem();
-                    if (j == n_tiles + 1) {
+                    if (j == n_tiles + 2) {
                         // this warp's verdict on the piece, before its last tile is announced
-                        bits |= label_read_status(label[0], owner) | label_read_status(label[1], owner);
                         bits = __reduce_or_sync(0xFFFFFFFFu, bits);
                         if (lane == 0 && bits) atomicOr(&sh.bits[piece % TC8_BITS_RING], bits);
                     }
                     __syncwarp();
-                    if (lane == 0) bar_arrive(&full[stage]);
+                    if (lane == 0) bar_arrive(full);
                     n++;
                 }
-                if (j > n_tiles) continue;
-                uint32_t slot[2];
+                if (j <= n_tiles) {
+                    uint32_t slot[2];
 #pragma unroll
-                for (int e = 0; e < 2; e++) {
-                    // the slots of tile j - 1, and the entries of tile j
-                    const uint32_t t_next = (tb + j) * TC8_TILE + e * 32 + lane, t = t_next - TC8_TILE;
-                    bits |= label_read_status(label[e], owner);
-                    label[e] = GIFT_OWNER_PARAM;
-                    slot[e] = 0xFFFFFFFFu;
-                    if (j > 0 && t < want && (!NEAR || t >= low)) {
-                        if ((uint32_t)next[e] < a.b.n_pages) {
-                            slot[e] = (uint32_t)next[e] * a.b.page_tokens + (t - a.b.page.quot(t) * a.b.page_tokens);
-                            if (a.owner_map) label[e] = a.owner_map[next[e]];
-                        } else {
-                            bits |= GIFT_ST_BAD_DESC;
+                    for (int e = 0; e < 2; e++) {
+                        // the slots of tile j - 1, and the entries of tile j
+                        const uint32_t t_next = (tb + j) * TC8_TILE + e * 32 + lane, t = t_next - TC8_TILE;
+                        slot[e] = 0xFFFFFFFFu;
+                        if (j > 0 && t < want && (!NEAR || t >= low)) {
+                            if ((uint32_t)next[e] < a.b.n_pages) {
+                                slot[e] = (uint32_t)next[e] * a.b.page_tokens + (t - a.b.page.quot(t) * a.b.page_tokens);
+                                if (a.owner_map) label[e] = a.owner_map[next[e]];
+                            } else {
+                                bits |= GIFT_ST_BAD_DESC;
+                            }
                         }
+                        next[e] = j < n_tiles && t_next < want && (!NEAR || t_next >= low) ? table[a.b.page.quot(t_next)] : -1;
                     }
-                    next[e] = j < n_tiles && t_next < want && (!NEAR || t_next >= low) ? table[a.b.page.quot(t_next)] : -1;
-                    if (kv) {
-                        scale[e] = make_float2(0.f, 0.f);
-                        if (slot[e] != 0xFFFFFFFFu) scale[e] = *reinterpret_cast<const float2*>(a.pages + slot[e] * a.token_bytes + 2ull * a.codes + h * 8u);
-                    }
-                }
-                if (j == 0) continue;
-                // tokens that nobody sees are zeros: what memory holds there does not matter
+                    if (j > 0) {
+                        const uint32_t place = raw + (fetched % TC8_AHEAD) * (TC8_TILE * D);
+                        // tokens that nobody sees are zeros: what memory holds there does not matter
+#pragma unroll 4
+                        for (int i = 0; i < LOADS; i++) {
+                            const uint32_t row = i * ROWS_AT_ONCE + sub;
+                            const uint32_t at = __shfl_sync(0xFFFFFFFFu, i * ROWS_AT_ONCE < 32 ? slot[0] : slot[1], row & 31u);
+                            const bool there = at != 0xFFFFFFFFu;
+                            cp_async16(place + i * 512, there ? from + at * a.token_bytes : from, there ? 16u : 0u);
+                        }
+                        if (kv)
 #pragma unroll
-                for (int i = 0; i < LOADS; i++) {
-                    const uint32_t row = i * ROWS_AT_ONCE + sub;
-                    const uint32_t at = __shfl_sync(0xFFFFFFFFu, slot[i * ROWS_AT_ONCE / 32], row & 31u);
-                    raw[i] = make_uint4(0u, 0u, 0u, 0u);
-                    if (at != 0xFFFFFFFFu) raw[i] = *reinterpret_cast<const uint4*>(from + at * a.token_bytes);
+                            for (int e = 0; e < 2; e++) {
+                                const bool there = slot[e] != 0xFFFFFFFFu;
+                                cp_async8(raw_scale + (fetched % TC8_AHEAD) * (TC8_TILE * 8) + e * 256,
+                                          a.pages + (there ? slot[e] * a.token_bytes + 2ull * a.codes + h * 8u : 0ull), there ? 8u : 0u);
+                            }
+                        fetched++;
+                    }
                 }
+                cp_commit();
             }
             piece++;
         }
-        // the copies under way end before the CTA does, whether or not anybody is left to wait for them
+        cp_wait<0>();
+        // the copy of Q under way ends before the CTA does, whether or not anybody is left to wait for it
         if (kv == 0 && q_loads > 0) bar_drain(&sh.q_full, (q_loads - 1) & 1u);
     } else if (warp == 6) {
         // ------------------------------------------------------------------ Q K^T
@@ -253,20 +269,19 @@ __global__ void __launch_bounds__(TC8_THREADS, 2) attn8_tc_kernel(const __grid_c
                 ok = bar_wait(&sh.q_ready, piece & 1u, dead, a);
 #pragma unroll 1
                 for (uint32_t j = 0; ok && j < n_tiles; j++) {
-                    const uint32_t t = n + j, stage = t % TC8_STAGES;
+                    const uint32_t t = n + j;
                     // S takes the columns that held P of tile t - 2
-                    ok = bar_wait(&sh.k_full[stage], (t / TC8_STAGES) & 1u, dead, a) &&
+                    ok = bar_wait(&sh.k_full, t & 1u, dead, a) &&
                          (t < 2 || bar_wait(&sh.o_done[t & 1u], ((t - 2) >> 1) & 1u, dead, a));
                     if (!ok) break;
                     tc_after();
-                    const uint64_t kb = k_desc + stage * (TC8_TILE * D * 2 / 16);
                     const uint32_t d = tmem + S_COL + (t & 1u) * TC8_TILE;
 #pragma unroll
                     for (uint32_t ks = 0; ks < D / 16; ks++)       // 16 columns are 32 bytes; 64 columns a block
                         mma_ss(d, q_desc + (ks >> 2) * (TC8_ROWS * 128 / 16) + (ks & 3u) * 2,
-                               kb + (ks >> 2) * (TC8_TILE * 128 / 16) + (ks & 3u) * 2, id_s, ks > 0);
+                               k_desc + (ks >> 2) * (TC8_TILE * 128 / 16) + (ks & 3u) * 2, id_s, ks > 0);
                     mma_commit(&sh.s_full[t & 1u]);
-                    mma_commit(&sh.k_empty[stage]);
+                    mma_commit(&sh.k_empty);
                     if (j + 1 == n_tiles) mma_commit(&sh.q_empty);
                 }
             }
@@ -291,17 +306,16 @@ __global__ void __launch_bounds__(TC8_THREADS, 2) attn8_tc_kernel(const __grid_c
             if (lane == 0)
 #pragma unroll 1
                 for (uint32_t j = 0; ok && j < n_tiles; j++) {
-                    const uint32_t t = n + j, stage = t % TC8_STAGES;
-                    ok = bar_wait(&sh.v_full[stage], (t / TC8_STAGES) & 1u, dead, a) && bar_wait(&sh.p_full[t & 1u], (t >> 1) & 1u, dead, a);
+                    const uint32_t t = n + j;
+                    ok = bar_wait(&sh.v_full, t & 1u, dead, a) && bar_wait(&sh.p_full[t & 1u], (t >> 1) & 1u, dead, a);
                     if (!ok) break;
                     tc_after();
-                    const uint64_t vb = v_desc + stage * (TC8_TILE * D * 2 / 16);
                     const uint32_t p = tmem + S_COL + (t & 1u) * TC8_TILE;
 #pragma unroll
                     for (uint32_t ks = 0; ks < TC8_TILE / 16; ks++)      // 16 tokens are 8 columns of P, 2048 bytes of V
-                        mma_ts(tmem + O_COL, p + ks * 8, vb + ks * (2048 / 16), id_o, j > 0 || ks > 0);
+                        mma_ts(tmem + O_COL, p + ks * 8, v_desc + ks * (2048 / 16), id_o, j > 0 || ks > 0);
                     mma_commit(&sh.o_done[t & 1u]);
-                    mma_commit(&sh.v_empty[stage]);
+                    mma_commit(&sh.v_empty);
                 }
             ok = __shfl_sync(0xFFFFFFFFu, ok, 0);
             n += n_tiles;
@@ -363,7 +377,7 @@ __global__ void __launch_bounds__(TC8_THREADS, 2) attn8_tc_kernel(const __grid_c
             float most = 0.f, to_half = to_half_range(9u), room = half_range_end(9u);
 #pragma unroll 1
             for (uint32_t j = 0; alive && j < w.n_tiles; j++, n++) {
-                const uint32_t s_at = tmem + lane_base + S_COL + (n & 1u) * TC8_TILE, stage = n % TC8_STAGES;
+                const uint32_t s_at = tmem + lane_base + S_COL + (n & 1u) * TC8_TILE;
                 const uint32_t t0 = (w.tb + (NEAR ? w.it.first : 0u) + j) * TC8_TILE;
                 const bool mixed = t0 + TC8_TILE > w.s.have || (NEAR && a.window && t0 + a.window < w.s.want);
                 uint64_t sees = ~0ull;
@@ -371,8 +385,8 @@ __global__ void __launch_bounds__(TC8_THREADS, 2) attn8_tc_kernel(const __grid_c
                     sees = there && !masked_short ? row_sees64(a, w.s.have, w.s.want, w.row0 + i, i, t0) : 0ull;
                     if (NEAR && a.window) sees &= in_window64(a.window, w.s.have + i, t0);
                 }
-                // the tile's V, whose scales (and K's) are read here, cannot be replaced before P V of this tile
-                if (!warp_wait(&sh.v_full[stage], (n / TC8_STAGES) & 1u, dead, a) || !warp_wait(&sh.s_full[n & 1u], (n >> 1) & 1u, dead, a)) {
+                // four places for scales: those of tile n + 4 come after V of tile n + 2, so after P V of tile n + 1
+                if (!warp_wait(&sh.scaled[n & 3u], (n >> 2) & 1u, dead, a) || !warp_wait(&sh.s_full[n & 1u], (n >> 1) & 1u, dead, a)) {
                     alive = false;
                     break;
                 }
@@ -388,12 +402,11 @@ __global__ void __launch_bounds__(TC8_THREADS, 2) attn8_tc_kernel(const __grid_c
                 tc_wait_ld();
                 tc_pin32(sc[0]);
                 tc_pin32(sc[1]);
-                float tops[4] = {NEG_INF, NEG_INF, NEG_INF, NEG_INF};
 #pragma unroll
                 for (int x = 0; x < 2; x++)
 #pragma unroll
                     for (int c = 0; c < 32; c += 4) {
-                        const float4 ks = *reinterpret_cast<const float4*>(&sh.k_scale[stage][32 * x + c]);
+                        const float4 ks = *reinterpret_cast<const float4*>(&sh.k_scale[n & 3u][32 * x + c]);
                         float y[4];
                         split2(mul2(pair2(__uint_as_float(sc[x][c]), __uint_as_float(sc[x][c + 1])), pair2(ks.x, ks.y)), y[0], y[1]);
                         split2(mul2(pair2(__uint_as_float(sc[x][c + 2]), __uint_as_float(sc[x][c + 3])), pair2(ks.z, ks.w)), y[2], y[3]);
@@ -406,12 +419,21 @@ __global__ void __launch_bounds__(TC8_THREADS, 2) attn8_tc_kernel(const __grid_c
                             }
                         }
 #pragma unroll
-                        for (int e = 0; e < 4; e++) {
-                            if (mixed && !((uint32_t)(sees >> (32 * x)) >> (c + e) & 1u)) y[e] = NEG_INF;
-                            sc[x][c + e] = __float_as_uint(y[e]);
-                        }
-                        tops[(c >> 2) & 3] = max3(tops[(c >> 2) & 3], fmaxf(y[0], y[1]), fmaxf(y[2], y[3]));
+                        for (int e = 0; e < 4; e++) sc[x][c + e] = __float_as_uint(y[e]);
                     }
+                if (mixed) {
+#pragma unroll
+                    for (int x = 0; x < 2; x++)
+#pragma unroll
+                        for (int c = 0; c < 32; c++)
+                            if (!((uint32_t)(sees >> (32 * x)) >> c & 1u)) sc[x][c] = 0xFF800000u;      // minus infinity
+                }
+                float tops[4] = {NEG_INF, NEG_INF, NEG_INF, NEG_INF};
+#pragma unroll
+                for (int x = 0; x < 2; x++)
+#pragma unroll
+                    for (int c = 0; c < 32; c += 2)
+                        tops[(c >> 1) & 3] = max3(tops[(c >> 1) & 3], __uint_as_float(sc[x][c]), __uint_as_float(sc[x][c + 1]));
                 // the scale is positive here (q's sign carries it), so the largest score stays the largest
                 const float by = NEAR ? 1.f : scale;
                 const float top = max3(tops[0], tops[1], fmaxf(tops[2], tops[3])) * by;
@@ -428,7 +450,7 @@ __global__ void __launch_bounds__(TC8_THREADS, 2) attn8_tc_kernel(const __grid_c
                 for (int x = 0; x < 2; x++)
 #pragma unroll
                     for (int c = 0; c < 32; c += 4) {
-                        const float4 vs = *reinterpret_cast<const float4*>(&sh.v_scale[stage][32 * x + c]);
+                        const float4 vs = *reinterpret_cast<const float4*>(&sh.v_scale[n & 3u][32 * x + c]);
 #pragma unroll
                         for (int e = 0; e < 4; e += 2) {
                             float lo, hi;
@@ -438,15 +460,18 @@ __global__ void __launch_bounds__(TC8_THREADS, 2) attn8_tc_kernel(const __grid_c
                             const uint64_t p = pair2(lo, hi);
                             sums[e >> 1] = add2(sums[e >> 1], p);
                             split2(mul2(p, e ? pair2(vs.z, vs.w) : pair2(vs.x, vs.y)), lo, hi);
-                            if (mixed) {                   // 0 times a scale that is NaN
-                                if (!((uint32_t)(sees >> (32 * x)) >> (c + e) & 1u)) lo = 0.f;
-                                if (!((uint32_t)(sees >> (32 * x)) >> (c + e + 1) & 1u)) hi = 0.f;
-                            }
                             bigs[e >> 1] = max3(bigs[e >> 1], lo, hi);
                             sc[x][c + e] = __float_as_uint(lo);
                             sc[x][c + e + 1] = __float_as_uint(hi);
                         }
                     }
+                if (mixed) {                               // 0 times a scale that is NaN (which no maximum takes up)
+#pragma unroll
+                    for (int x = 0; x < 2; x++)
+#pragma unroll
+                        for (int c = 0; c < 32; c++)
+                            if (!((uint32_t)(sees >> (32 * x)) >> c & 1u)) sc[x][c] = 0u;
+                }
                 {
                     float lo, hi;
                     split2(add2(sums[0], sums[1]), lo, hi);

@@ -333,7 +333,12 @@ __global__ void __launch_bounds__(Few8<D, NR>::threads, Few8<D, NR>::ctas) attn8
                     __syncwarp();
                 }
             }
-            float sc[MT][NR][4], vs[MT][2];
+            float sc[MT][NR][4], vs[MT][2], away[NR][2];
+            if (NEAR)
+#pragma unroll
+                for (int n = 0; n < NR; n++)
+#pragma unroll
+                    for (int j = 0; j < 2; j++) away[n][j] = (float)((int32_t)(t0 + g) - (int32_t)(s.have + row_i[n][j]));
 #pragma unroll
             for (int x = 0; x < MT; x++) {
 #pragma unroll
@@ -365,8 +370,7 @@ __global__ void __launch_bounds__(Few8<D, NR>::threads, Few8<D, NR>::ctas) attn8
                             y *= ks_vs.x * qs[n][j];
                             if constexpr (NEAR) {
                                 if (a.cap_out != 0.f) y = a.cap_out * tanh_of(y);
-                                const int32_t away = (int32_t)(t0 + x * 16 + e2 * 8 + g) - (int32_t)(s.have + row_i[n][j]);
-                                if (a.slopes) y += slope[n][j] * (float)away;
+                                if (a.slopes) y += slope[n][j] * (away[n][j] + (float)(x * 16 + e2 * 8));
                             }
                         }
                 }
@@ -609,11 +613,29 @@ int launch_few8(gift_ctx* c, Attn8Args& a, cudaStream_t st)
     return GIFT_OK;
 }
 
+// The pool as rows of one token, taken a head's codes of a run of tokens at a time.
+int map_of_codes(const Attn8Args& a, uint32_t head_dim, CUtensorMap* map)
+{
+    EncodeTiled encode;
+    const int rc = encode_tiled(&encode);
+    if (rc != GIFT_OK) return rc;
+    const cuuint64_t dims[2] = {a.token_bytes, a.b.n_pages ? (cuuint64_t)a.b.n_pages * a.b.page_tokens : 1};
+    const cuuint64_t strides[1] = {a.token_bytes};
+    const cuuint32_t box[2] = {head_dim, a.copy_run}, steps[2] = {1, 1};
+    if (encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<char*>(a.pages), dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
+               CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+        return GIFT_E_CUDA;
+    return GIFT_OK;
+}
+
 template <int D, bool NEAR>
 int launch_many8(gift_ctx* c, Attn8Args& a, uint64_t rows, cudaStream_t st)
 {
-    CUtensorMap q_map;
-    const int rc = map_of_q(a, a.half != 0u, D, &q_map);
+    CUtensorMap q_map, code_map;
+    a.copy_run = a.b.page_tokens & (0u - a.b.page_tokens);
+    if (a.copy_run > (uint32_t)TC8_TILE) a.copy_run = TC8_TILE;
+    int rc = map_of_q(a, a.half != 0u, D, &q_map);
+    if (rc == GIFT_OK) rc = map_of_codes(a, D, &code_map);
     if (rc != GIFT_OK) return rc;
     constexpr int smem = Tc8Smem<D>::bytes;
     CU_TRY((allow_smem<attn8_tc_kernel<D, NEAR>>(c->device, smem)));
@@ -630,7 +652,7 @@ int launch_many8(gift_ctx* c, Attn8Args& a, uint64_t rows, cudaStream_t st)
     a.wait_ns = c->attn_wait_ns && c->attn_wait_ns < TC_SUSPEND_NS ? (uint32_t)c->attn_wait_ns : TC_SUSPEND_NS;
     a.scale_log2 = fabsf(a.scale_log2);
     a.cap_in = fabsf(a.cap_in);
-    attn8_tc_kernel<D, NEAR><<<a.n_slices * a.ways, TC8_THREADS, smem, st>>>(a, q_map);
+    attn8_tc_kernel<D, NEAR><<<a.n_slices * a.ways, TC8_THREADS, smem, st>>>(a, q_map, code_map);
     c->launches++;
     CU_TRY(cudaGetLastError());
     if (a.half) CU_TRY((launch_join<__half, D, TC8_ROWS>(a, st)));

@@ -11,6 +11,7 @@ struct Attn8Args : AttnArgs {
     const float* slopes;
     uint32_t half;                   // q and out are fp16, not bf16
     uint32_t head_ways;              // few rows: K/V heads that a CTA's warps share out (kv_heads counts groups of them)
+    uint32_t copy_run;               // many rows: tokens that are one copy, the largest power of two up to a tile that divides the page
     uint32_t whole_steps;            // few rows: a page is whole steps of a warp
 };
 
@@ -63,6 +64,10 @@ __device__ __forceinline__ uint32_t codes_without_nan(uint32_t w)
 __device__ __forceinline__ void cp_async8(uint32_t dst, const void* src, uint32_t bytes)
 {
     asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void cp_async4(uint32_t dst, const void* src, uint32_t bytes)
+{
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
 __device__ __forceinline__ uint4 lds128(uint32_t at)
 {

@@ -3,14 +3,14 @@
 // The roles and barriers of the 16-bit kernel: a tile of 128 query rows (or what whole tokens fit) meets tiles of 64
 // tokens, S = Q K^T lands in tensor memory, one row per thread of four softmax warps, P goes back into the columns of
 // its S and is the A operand of O += P V.  What differs:
-//   warp 4, 5  fetch the codes of K's and of V's tiles into shared memory, two tiles ahead (fetched into registers, one
-//              ahead, they came too late: 1182 us for what takes 492 with nothing to fetch), and put them as fp16 numbers
-//              (exact) where the products read them; warp 5 brings the scales of both.  (A product of codes
-//              would need q and the weights as codes too.)  Each judges the labels of the pages that it reads.
+//   warps 6, 7 fetch the codes (and scales) of K and of V into shared memory, two tiles ahead.  Each judges the labels of the
+//              pages that it reads.
+//   warps 4, 5 put the codes as fp16 numbers (exact) where the products read them, and issue those.  (A product of codes
+//              would need q and the weights as codes too.)
 //   softmax    K's scale multiplies the score, V's the weight, in 32 bits.  Weights go to fp16 by a power of two of the row's
 //              own, which follows the largest p * scale as the maximum follows the scores; O is in its units.
 //              bf16 queries become fp16 in place, by a power of two of the row's own too.
-// A token whose V holds the code of NaN gets it into its scale (codes 0), which is used only where the token is seen: what a
+// A code of NaN in a V whose token is hidden from some row becomes 0, and its weight NaN where the token is seen: what a
 // hidden token holds does not matter.
 // Every wait is bounded; a CTA whose wait runs out notes its unfinished requests, and the joining kernel makes them zero.
 #pragma once
@@ -31,14 +31,14 @@ template <int D> struct Tc8Smem {
     static constexpr uint32_t v = k + TC8_TILE * D * 2;
     static constexpr uint32_t o = v + TC8_TILE * D * 2;                               // [4 warps][32 rows][64 bytes]
     static constexpr uint32_t codes = o + 4 * 32 * 64;                                // of K, of V: [2 tiles][64][D]
-    static constexpr uint32_t scales = codes + 2 * TC8_AHEAD * TC8_TILE * D;          // [2 tiles][64] of both
-    static constexpr uint32_t bytes = scales + TC8_AHEAD * TC8_TILE * 8;
+    static constexpr uint32_t bytes = codes + 2 * TC8_AHEAD * TC8_TILE * D;
 };
 
 struct Tc8Shared {
-    uint64_t k_full, k_empty, v_full, v_empty, scaled[4];
-    uint64_t s_full[2], p_full[2], o_done[2], q_full, q_ready, q_empty, last;
+    uint64_t fetched[2][TC8_AHEAD], taken[2][TC8_AHEAD], judged[2][TC8_BITS_RING];                 // of K, of V
+    uint64_t scaled[4], checked[4], s_full[2], p_full[2], o_done[2], s_done, q_full, q_ready, last;
     float k_scale[4][TC8_TILE], v_scale[4][TC8_TILE];                                 // by tile
+    uint32_t odd[4][2];              // tokens with a code of NaN in V, by tile
     uint32_t tmem;
     uint32_t bits[TC8_BITS_RING];
     int dead;
@@ -67,7 +67,8 @@ __device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b)
 __device__ __forceinline__ void publish_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
 template <int D, bool NEAR>
-__global__ void __launch_bounds__(TC8_THREADS, 2) attn8_tc_kernel(const __grid_constant__ Attn8Args a, const __grid_constant__ CUtensorMap q_map)
+__global__ void __launch_bounds__(TC8_THREADS, 2)
+attn8_tc_kernel(const __grid_constant__ Attn8Args a, const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap code_map)
 {
     constexpr uint32_t TMEM_COLS = 256;                    // 2 S, O; a power of two, half of what an SM has
     constexpr uint32_t S_COL = 0, O_COL = 2 * TC8_TILE;
@@ -83,10 +84,13 @@ __global__ void __launch_bounds__(TC8_THREADS, 2) attn8_tc_kernel(const __grid_c
     }
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
-        bar_init(&sh.k_full, 1); bar_init(&sh.k_empty, 1); bar_init(&sh.v_full, 1); bar_init(&sh.v_empty, 1);
-        for (int i = 0; i < 4; i++) bar_init(&sh.scaled[i], 1);
+        for (int kv = 0; kv < 2; kv++) {
+            for (int i = 0; i < TC8_AHEAD; i++) { bar_init(&sh.fetched[kv][i], 32); bar_init(&sh.taken[kv][i], 1); }
+            for (int i = 0; i < TC8_BITS_RING; i++) bar_init(&sh.judged[kv][i], 1);
+        }
+        for (int i = 0; i < 4; i++) { bar_init(&sh.scaled[i], 32); bar_init(&sh.checked[i], 1); }
         for (int i = 0; i < 2; i++) { bar_init(&sh.s_full[i], 1); bar_init(&sh.p_full[i], 4); bar_init(&sh.o_done[i], 1); }
-        bar_init(&sh.q_full, 1); bar_init(&sh.q_ready, 4); bar_init(&sh.q_empty, 1); bar_init(&sh.last, 2);
+        bar_init(&sh.q_full, 1); bar_init(&sh.q_ready, 4); bar_init(&sh.s_done, 1); bar_init(&sh.last, 2);
         for (int i = 0; i < TC8_BITS_RING; i++) sh.bits[i] = 0u;
         sh.dead = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -114,217 +118,232 @@ __global__ void __launch_bounds__(TC8_THREADS, 2) attn8_tc_kernel(const __grid_c
         __syncwarp();
     }
 
+    // Of a tile's codes a lane fetches 16 from 16 chunk of every ROWS_AT_ONCE-th token.
+    constexpr int ROW_LANES = D / 16, ROWS_AT_ONCE = 32 / ROW_LANES, LOADS = TC8_TILE / ROWS_AT_ONCE;
+    const uint32_t chunk = lane % ROW_LANES, sub = lane / ROW_LANES;
     if (warp == 4 || warp == 5) {
-        // ------------------------------------------------------------------ codes to fp16
-        // Of a tile's codes a lane fetches, and later converts, 16 from 16 chunk of every ROWS_AT_ONCE-th token.
-        constexpr int ROW_LANES = D / 16, ROWS_AT_ONCE = 32 / ROW_LANES, LOADS = TC8_TILE / ROWS_AT_ONCE;
-        const uint32_t kv = warp - 4, chunk = lane % ROW_LANES, sub = lane / ROW_LANES;
-        uint64_t* full = kv ? &sh.v_full : &sh.k_full;
-        uint64_t* empty = kv ? &sh.v_empty : &sh.k_empty;
-        const uint32_t raw = sm + L::codes + kv * (TC8_AHEAD * TC8_TILE * D) + lane * 16, raw_scale = sm + L::scales + lane * 8;
-        uint32_t n = 0, fetched = 0, piece = 0, q_loads = 0;           // tiles and pieces so far
-        bool ok = true;
-        while (ok && walk8_next(w, a, lane)) {
-            const int32_t owner = a.b.owner[w.r];
-            const int32_t* table = a.b.table + (uint64_t)w.r * a.b.max_blocks;
-            const uint32_t want = w.s.want, low = NEAR ? first_seen(a, w.s.have) : 0u, tb = w.tb + (NEAR ? w.it.first : 0u), h = w.h, n_tiles = w.n_tiles;
-            const char* from = a.pages + (uint64_t)kv * a.codes + (uint64_t)h * D + chunk * 16;
-            uint32_t bits = w.masked_short(a) ? GIFT_ST_BAD_DESC : 0u;
-            if (kv == 0) {
-                // Q, once the products of the piece before have read the old rows.  What the box holds past
-                // the request's rows is another request's: rows that nobody asks for.
-                ok = piece == 0 || warp_wait(&sh.q_empty, (piece - 1) & 1u, dead, a);
-                if (!ok) break;
-                q_loads++;
-                if (lane == 0) {
-                    bar_expect(&sh.q_full, a.tile_rows * D * 2);
-#pragma unroll
-                    for (int c = 0; c < D / 64; c++)
-                        copy_q(sm + L::q + c * (TC8_ROWS * 128), &q_map, c * 64, (int32_t)(h * a.group),
-                               (int32_t)(w.row0 + a.by_group.quot(w.qt * a.tile_rows)), &sh.q_full);
-                }
-            }
-            // Lane l looks up tokens l and l + 32 of a tile.  Round j fetches tile j's table entries, judges and fetches the
-            // codes of tile j - 1, and before that hands over tile j - 3, whose place those take.
-            int32_t next[2] = {-1, -1}, label[2] = {GIFT_OWNER_PARAM, GIFT_OWNER_PARAM};
-#pragma unroll 1
-            for (uint32_t j = 0; j < n_tiles + 3; j++) {
-                bits |= label_read_status(label[0], owner) | label_read_status(label[1], owner);
-                label[0] = label[1] = GIFT_OWNER_PARAM;
-                if (j > 2) {
-                    const uint32_t t0 = (tb + j - 3) * TC8_TILE, place = raw + (n % TC8_AHEAD) * (TC8_TILE * D);
-                    cp_wait<1>();
-                    if (kv) {
-                        // the scales, which the softmax may have before V
-                        float2 scale[2];
-#pragma unroll
-                        for (int e = 0; e < 2; e++) scale[e] = lds_pair(raw_scale + (n % TC8_AHEAD) * (TC8_TILE * 8) + e * 256);
-                        if (t0 + TC8_TILE > w.s.have || (NEAR && a.window && t0 + a.window < want)) {
-                            uint32_t odd[2] = {0u, 0u};        // tokens with a NaN among their codes
-#pragma unroll 4
-                            for (int i = 0; i < LOADS; i++) {
-                                const uint4 x = lds128(place + i * 512);
-                                const uint32_t token = i * ROWS_AT_ONCE + sub;
-                                if (codes_nan(x.x) || codes_nan(x.y) || codes_nan(x.z) || codes_nan(x.w)) {
-                                    odd[token >> 5] |= 1u << (token & 31u);
-                                    asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(place + i * 512), "r"(codes_without_nan(x.x)),
-                                                 "r"(codes_without_nan(x.y)), "r"(codes_without_nan(x.z)), "r"(codes_without_nan(x.w)) : "memory");
-                                }
-                            }
-#pragma unroll
-                            for (int e = 0; e < 2; e++)
-                                if (__reduce_or_sync(0xFFFFFFFFu, odd[e]) >> lane & 1u) scale[e].y = __uint_as_float(0x7FC00000u);
-                        }
-#pragma unroll
-                        for (int e = 0; e < 2; e++) {
-                            sh.k_scale[n & 3u][e * 32 + lane] = scale[e].x;
-                            sh.v_scale[n & 3u][e * 32 + lane] = scale[e].y;
-                        }
-                        __syncwarp();
-                        if (lane == 0) bar_arrive(&sh.scaled[n & 3u]);
-                    }
-                    ok = n == 0 || warp_wait(empty, (n - 1) & 1u, dead, a);
-                    if (!ok) break;
-                    // 16 codes are two 16-byte chunks of their row; lanes of the second block of 64 columns begin with the
-                    // second one, for other banks than those of the first
-                    const uint32_t block = chunk >> 2, dst = sm + (kv ? L::v : L::k) + block * (TC8_TILE * 128);
-#pragma unroll 4
-                    for (int i = 0; i < LOADS; i++) {
-                        const uint32_t row = i * ROWS_AT_ONCE + sub;
-                        const uint4 x = lds128(place + i * 512);
-                        const uint32_t first[2] = {block ? x.z : x.x, block ? x.w : x.y}, second[2] = {block ? x.x : x.z, block ? x.y : x.w};
-                        const uint32_t at = dst + row * 128 + (((chunk & 3u) * 2 + block ^ (row & 7u)) << 4);
-                        uint32_t f[4];
-                        four_codes(first[0], f[0], f[1]);
-                        four_codes(first[1], f[2], f[3]);
-                        asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(f[0]), "r"(f[1]), "r"(f[2]), "r"(f[3]) : "memory");
-                        four_codes(second[0], f[0], f[1]);
-                        four_codes(second[1], f[2], f[3]);
-                        asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(at ^ 16u), "r"(f[0]), "r"(f[1]), "r"(f[2]), "r"(f[3]) : "memory");
-                    }
-                    publish_smem();
-                    if (j == n_tiles + 2) {
-                        // this warp's verdict on the piece, before its last tile is announced
-                        bits = __reduce_or_sync(0xFFFFFFFFu, bits);
-                        if (lane == 0 && bits) atomicOr(&sh.bits[piece % TC8_BITS_RING], bits);
-                    }
-                    __syncwarp();
-                    if (lane == 0) bar_arrive(full);
-                    n++;
-                }
-                if (j <= n_tiles) {
-                    uint32_t slot[2];
-#pragma unroll
-                    for (int e = 0; e < 2; e++) {
-                        // the slots of tile j - 1, and the entries of tile j
-                        const uint32_t t_next = (tb + j) * TC8_TILE + e * 32 + lane, t = t_next - TC8_TILE;
-                        slot[e] = 0xFFFFFFFFu;
-                        if (j > 0 && t < want && (!NEAR || t >= low)) {
-                            if ((uint32_t)next[e] < a.b.n_pages) {
-                                slot[e] = (uint32_t)next[e] * a.b.page_tokens + (t - a.b.page.quot(t) * a.b.page_tokens);
-                                if (a.owner_map) label[e] = a.owner_map[next[e]];
-                            } else {
-                                bits |= GIFT_ST_BAD_DESC;
-                            }
-                        }
-                        next[e] = j < n_tiles && t_next < want && (!NEAR || t_next >= low) ? table[a.b.page.quot(t_next)] : -1;
-                    }
-                    if (j > 0) {
-                        const uint32_t place = raw + (fetched % TC8_AHEAD) * (TC8_TILE * D);
-                        // tokens that nobody sees are zeros: what memory holds there does not matter
-#pragma unroll 4
-                        for (int i = 0; i < LOADS; i++) {
-                            const uint32_t row = i * ROWS_AT_ONCE + sub;
-                            const uint32_t at = __shfl_sync(0xFFFFFFFFu, i * ROWS_AT_ONCE < 32 ? slot[0] : slot[1], row & 31u);
-                            const bool there = at != 0xFFFFFFFFu;
-                            cp_async16(place + i * 512, there ? from + at * a.token_bytes : from, there ? 16u : 0u);
-                        }
-                        if (kv)
-#pragma unroll
-                            for (int e = 0; e < 2; e++) {
-                                const bool there = slot[e] != 0xFFFFFFFFu;
-                                cp_async8(raw_scale + (fetched % TC8_AHEAD) * (TC8_TILE * 8) + e * 256,
-                                          a.pages + (there ? slot[e] * a.token_bytes + 2ull * a.codes + h * 8u : 0ull), there ? 8u : 0u);
-                            }
-                        fetched++;
-                    }
-                }
-                cp_commit();
-            }
-            piece++;
-        }
-        cp_wait<0>();
-        // the copy of Q under way ends before the CTA does, whether or not anybody is left to wait for it
-        if (kv == 0 && q_loads > 0) bar_drain(&sh.q_full, (q_loads - 1) & 1u);
-    } else if (warp == 6) {
-        // ------------------------------------------------------------------ Q K^T
+        // ------------------------------------------------------------------ codes to fp16, and the products
+        // Warp 4: K, and Q K^T; warp 5: V, and P V.
+        const uint32_t kv = warp - 4;
+        const uint32_t raw = sm + L::codes + kv * (TC8_AHEAD * TC8_TILE * D) + lane * 16;
+        // 16 codes are two 16-byte chunks of their row; lanes of the second block of 64 columns begin with the
+        // second one, for other banks than those of the first
+        const uint32_t block = chunk >> 2, dst = sm + (kv ? L::v : L::k) + block * (TC8_TILE * 128);
         // a negative scale: the products negate q, so that the scale used on the scores is positive
         const uint32_t id_s = instr_desc<__half>(TC8_ROWS, TC8_TILE, 0) | (a.negate << 13);
+        constexpr uint32_t id_o = instr_desc<__half>(TC8_ROWS, D, 1);
         const uint64_t q_desc = smem_desc(sm + L::q, 16, 1024), k_desc = smem_desc(sm + L::k, 16, 1024);
-        uint32_t n = 0, piece = 0;
+        const uint64_t v_desc = smem_desc(sm + L::v, TC8_TILE * 128, 1024);
+        uint32_t n = 0, piece = 0, q_loads = 0;
         bool ok = true;
         while (ok && walk8_next(w, a, lane)) {
-            const uint32_t n_tiles = w.n_tiles;
-            if (lane == 0) {
-                ok = bar_wait(&sh.q_ready, piece & 1u, dead, a);
+            const uint32_t n_tiles = w.n_tiles, have = w.s.have, want = w.s.want, tb = w.tb + (NEAR ? w.it.first : 0u);
 #pragma unroll 1
-                for (uint32_t j = 0; ok && j < n_tiles; j++) {
-                    const uint32_t t = n + j;
-                    // S takes the columns that held P of tile t - 2
-                    ok = bar_wait(&sh.k_full, t & 1u, dead, a) &&
-                         (t < 2 || bar_wait(&sh.o_done[t & 1u], ((t - 2) >> 1) & 1u, dead, a));
-                    if (!ok) break;
-                    tc_after();
-                    const uint32_t d = tmem + S_COL + (t & 1u) * TC8_TILE;
-#pragma unroll
-                    for (uint32_t ks = 0; ks < D / 16; ks++)       // 16 columns are 32 bytes; 64 columns a block
-                        mma_ss(d, q_desc + (ks >> 2) * (TC8_ROWS * 128 / 16) + (ks & 3u) * 2,
-                               k_desc + (ks >> 2) * (TC8_TILE * 128 / 16) + (ks & 3u) * 2, id_s, ks > 0);
-                    mma_commit(&sh.s_full[t & 1u]);
-                    mma_commit(&sh.k_empty);
-                    if (j + 1 == n_tiles) mma_commit(&sh.q_empty);
+            for (uint32_t j = 0; j < n_tiles; j++, n++) {
+                const uint32_t t0 = (tb + j) * TC8_TILE, place = raw + (n % TC8_AHEAD) * (TC8_TILE * D);
+                ok = warp_wait(&sh.fetched[kv][n % TC8_AHEAD], (n / TC8_AHEAD) & 1u, dead, a);
+                if (!ok) break;
+                if (kv) {
+                    uint32_t odd[2] = {0u, 0u};
+                    if (t0 + TC8_TILE > have || (NEAR && a.window && t0 + a.window < want)) {
+#pragma unroll 2
+                        for (int i = 0; i < LOADS; i++) {
+                            const uint4 x = lds128(place + i * 512);
+                            if (codes_nan(x.x) || codes_nan(x.y) || codes_nan(x.z) || codes_nan(x.w)) {
+                                const uint32_t token = i * ROWS_AT_ONCE + sub;
+                                odd[0] |= token < 32 ? 1u << token : 0u;
+                                odd[1] |= token < 32 ? 0u : 1u << (token - 32);
+                                asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(place + i * 512), "r"(codes_without_nan(x.x)),
+                                             "r"(codes_without_nan(x.y)), "r"(codes_without_nan(x.z)), "r"(codes_without_nan(x.w)) : "memory");
+                            }
+                        }
+                        odd[0] = __reduce_or_sync(0xFFFFFFFFu, odd[0]);
+                        odd[1] = __reduce_or_sync(0xFFFFFFFFu, odd[1]);
+                    }
+                    if (lane == 0) {
+                        sh.odd[n & 3u][0] = odd[0];
+                        sh.odd[n & 3u][1] = odd[1];
+                        bar_arrive(&sh.checked[n & 3u]);
+                    }
                 }
+                // the product with the tile before is complete
+                ok = n == 0 || (kv ? warp_wait(&sh.o_done[(n - 1) & 1u], ((n - 1) >> 1) & 1u, dead, a) : warp_wait(&sh.s_done, (n - 1) & 1u, dead, a));
+                if (!ok) break;
+                if (kv == 0 && j == 0) {
+                    // Q.  What the box holds past the request's rows is another request's: rows that nobody asks for.
+                    q_loads++;
+                    if (lane == 0) {
+                        bar_expect(&sh.q_full, a.tile_rows * D * 2);
+#pragma unroll
+                        for (int c = 0; c < D / 64; c++)
+                            copy_q(sm + L::q + c * (TC8_ROWS * 128), &q_map, c * 64, (int32_t)(w.h * a.group),
+                                   (int32_t)(w.row0 + a.by_group.quot(w.qt * a.tile_rows)), &sh.q_full);
+                    }
+                }
+#pragma unroll 4
+                for (int i = 0; i < LOADS; i++) {
+                    const uint32_t row = i * ROWS_AT_ONCE + sub;
+                    const uint4 x = lds128(place + i * 512);
+                    const uint32_t first[2] = {block ? x.z : x.x, block ? x.w : x.y}, second[2] = {block ? x.x : x.z, block ? x.y : x.w};
+                    const uint32_t at = dst + row * 128 + (((chunk & 3u) * 2 + block ^ (row & 7u)) << 4);
+                    uint32_t f[4];
+                    four_codes(first[0], f[0], f[1]);
+                    four_codes(first[1], f[2], f[3]);
+                    asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(f[0]), "r"(f[1]), "r"(f[2]), "r"(f[3]) : "memory");
+                    four_codes(second[0], f[0], f[1]);
+                    four_codes(second[1], f[2], f[3]);
+                    asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(at ^ 16u), "r"(f[0]), "r"(f[1]), "r"(f[2]), "r"(f[3]) : "memory");
+                }
+                publish_smem();
+                __syncwarp();
+                if (lane == 0) bar_arrive(&sh.taken[kv][n % TC8_AHEAD]);
+                // Q, and S's columns, which held P of tile n - 2; or P
+                if (kv == 0) ok = (j > 0 || warp_wait(&sh.q_ready, piece & 1u, dead, a)) && (n < 2 || warp_wait(&sh.o_done[n & 1u], ((n - 2) >> 1) & 1u, dead, a));
+                else ok = warp_wait(&sh.p_full[n & 1u], (n >> 1) & 1u, dead, a);
+                if (!ok) break;
+                if (lane == 0) {
+                    tc_after();
+                    const uint32_t s_at = tmem + S_COL + (n & 1u) * TC8_TILE;
+                    if (kv == 0) {
+#pragma unroll
+                        for (uint32_t ks = 0; ks < D / 16; ks++)       // 16 columns are 32 bytes; 64 columns a block
+                            mma_ss(s_at, q_desc + (ks >> 2) * (TC8_ROWS * 128 / 16) + (ks & 3u) * 2,
+                                   k_desc + (ks >> 2) * (TC8_TILE * 128 / 16) + (ks & 3u) * 2, id_s, ks > 0);
+                        mma_commit(&sh.s_full[n & 1u]);
+                        mma_commit(&sh.s_done);
+                    } else {
+#pragma unroll
+                        for (uint32_t ks = 0; ks < TC8_TILE / 16; ks++)      // 16 tokens are 8 columns of P, 2048 bytes of V
+                            mma_ts(tmem + O_COL, s_at + ks * 8, v_desc + ks * (2048 / 16), id_o, j > 0 || ks > 0);
+                        mma_commit(&sh.o_done[n & 1u]);
+                    }
+                }
+                __syncwarp();
             }
-            ok = __shfl_sync(0xFFFFFFFFu, ok, 0);
-            n += n_tiles;
             piece++;
         }
+        // the copy of Q under way ends before the CTA does, whether or not anybody is left to wait for it
+        if (q_loads > 0) bar_drain(&sh.q_full, (q_loads - 1) & 1u);
         if (lane == 0) {
             // nothing may be in flight when the tensor memory is given back
             mma_commit(&sh.last);
             bar_drain(&sh.last, 0);
         }
         __syncwarp();
-    } else if (warp == 7) {
-        // ------------------------------------------------------------------ P V
-        constexpr uint32_t id_o = instr_desc<__half>(TC8_ROWS, D, 1);
-        const uint64_t v_desc = smem_desc(sm + L::v, TC8_TILE * 128, 1024);
-        uint32_t n = 0;
-        bool ok = true;
-        while (ok && walk8_next(w, a, lane)) {
-            const uint32_t n_tiles = w.n_tiles;
-            if (lane == 0)
-#pragma unroll 1
-                for (uint32_t j = 0; ok && j < n_tiles; j++) {
-                    const uint32_t t = n + j;
-                    ok = bar_wait(&sh.v_full, t & 1u, dead, a) && bar_wait(&sh.p_full[t & 1u], (t >> 1) & 1u, dead, a);
-                    if (!ok) break;
-                    tc_after();
-                    const uint32_t p = tmem + S_COL + (t & 1u) * TC8_TILE;
+    } else if (warp >= 6) {
+        // ------------------------------------------------------------------ codes from the pages
+        const uint32_t kv = warp - 6;
+        const uint32_t raw = sm + L::codes + kv * (TC8_AHEAD * TC8_TILE * D) + lane * 16;
+        Walk<TC8_TILE, NEAR>& f = w;
+        uint32_t fetched = 0, fetch_piece = 0, left = 0, t_next = 0, bits = 0u;        // tiles of the piece to go; this lane's first token
+        int32_t next[2] = {-1, -1}, label[2] = {GIFT_OWNER_PARAM, GIFT_OWNER_PARAM};
+        bool more = true;
+        // Lane l looks up tokens l and l + 32 of a tile.  Table entries are fetched one tile ahead, labels judged a tile
+        // later; after a piece's last tile the piece is.
+        // (a load waits for the copies that were started before it, so what a piece needs is loaded once)
+        int32_t owner = 0;
+        const int32_t* table = nullptr;
+        uint32_t want = 0, low = 0;
+        const char* from = nullptr;
+        const char* scales = nullptr;
+        int32_t x = 0;                                         // column of the map
+        auto entries = [&](uint32_t t) {
 #pragma unroll
-                    for (uint32_t ks = 0; ks < TC8_TILE / 16; ks++)      // 16 tokens are 8 columns of P, 2048 bytes of V
-                        mma_ts(tmem + O_COL, p + ks * 8, v_desc + ks * (2048 / 16), id_o, j > 0 || ks > 0);
-                    mma_commit(&sh.o_done[t & 1u]);
-                    mma_commit(&sh.v_empty);
+            for (int e = 0; e < 2; e++) next[e] = t + e * 32 < want && (!NEAR || t + e * 32 >= low) ? table[a.b.page.quot(t + e * 32)] : -1;
+        };
+        auto judge = [&]() {
+#pragma unroll
+            for (int e = 0; e < 2; e++) {
+                bits |= label_read_status(label[e], owner);
+                label[e] = GIFT_OWNER_PARAM;
+            }
+        };
+        auto fetch = [&]() {
+            if (!more) return;
+            if (fetched > 0 || left > 0) judge();              // the pages of the tile before
+            if (left == 0) {
+                if (fetched > 0) {
+                    bits = __reduce_or_sync(0xFFFFFFFFu, bits);
+                    if (lane == 0) {
+                        if (bits) atomicOr(&sh.bits[fetch_piece % TC8_BITS_RING], bits);
+                        bar_arrive(&sh.judged[kv][fetch_piece % TC8_BITS_RING]);
+                    }
+                    fetch_piece++;
                 }
-            ok = __shfl_sync(0xFFFFFFFFu, ok, 0);
-            n += n_tiles;
-        }
-        if (lane == 0) {
-            mma_commit(&sh.last);
-            bar_drain(&sh.last, 0);
-        }
-        __syncwarp();
+                more = walk8_next(f, a, lane);
+                if (!more) return;
+                left = f.n_tiles;
+                t_next = (f.tb + (NEAR ? f.it.first : 0u)) * TC8_TILE + lane;
+                bits = f.masked_short(a) ? GIFT_ST_BAD_DESC : 0u;
+                owner = a.b.owner[f.r];
+                table = a.b.table + (uint64_t)f.r * a.b.max_blocks;
+                want = f.s.want;
+                low = NEAR ? first_seen(a, f.s.have) & ~(a.copy_run - 1u) : 0u;        // whole runs
+                from = a.pages + (uint64_t)kv * a.codes + (uint64_t)f.h * D + chunk * 16;
+                scales = a.pages + 2ull * a.codes + f.h * 8u;
+                x = (int32_t)(kv * a.codes + f.h * D);
+                entries(t_next);
+            }
+            uint32_t slot[2];                                  // of this tile's tokens
+#pragma unroll
+            for (int e = 0; e < 2; e++) {
+                const uint32_t t = t_next + e * 32;
+                slot[e] = 0xFFFFFFFFu;
+                if (t < want && (!NEAR || t >= low)) {
+                    if ((uint32_t)next[e] < a.b.n_pages) {
+                        slot[e] = (uint32_t)next[e] * a.b.page_tokens + (t - a.b.page.quot(t) * a.b.page_tokens);
+                        if (a.owner_map) label[e] = a.owner_map[next[e]];
+                    } else {
+                        bits |= GIFT_ST_BAD_DESC;
+                    }
+                }
+            }
+            left--;
+            t_next += TC8_TILE;
+            if (left > 0) entries(t_next);
+            const uint32_t at_place = fetched % TC8_AHEAD, place = raw + at_place * (TC8_TILE * D);
+            more = fetched < TC8_AHEAD || warp_wait(&sh.taken[kv][at_place], (fetched / TC8_AHEAD - 1) & 1u, dead, a);
+            if (!more) return;
+            if (a.copy_run >= 8) {
+                // A run is one copy, by the lane that looked up its first token.  What it holds past the context, or before
+                // a window, is hidden from every row; runs that nobody sees are sent outside the map, and are zeros.
+                uint64_t* bar = &sh.fetched[kv][at_place];
+                if (lane == 0) asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(bar)), "r"(TC8_TILE * D) : "memory");
+                __syncwarp();
+#pragma unroll
+                for (uint32_t e = 0; e < 2; e++)
+                    if (((e * 32 + lane) & (a.copy_run - 1u)) == 0u)
+                        copy_run(place - lane * 16 + (e * 32 + lane) * D, &code_map, x, slot[e] == 0xFFFFFFFFu ? -(int32_t)TC8_TILE : (int32_t)slot[e], bar);
+            } else {
+                // tokens that nobody sees are zeros: what memory holds there does not matter
+#pragma unroll 4
+                for (int i = 0; i < LOADS; i++) {
+                    const uint32_t row = i * ROWS_AT_ONCE + sub;
+                    const uint32_t at = __shfl_sync(0xFFFFFFFFu, i * ROWS_AT_ONCE < 32 ? slot[0] : slot[1], row & 31u);
+                    const bool there = at != 0xFFFFFFFFu;
+                    cp_async16(place + i * 512, there ? from + at * a.token_bytes : from, there ? 16u : 0u);
+                }
+            }
+            if (kv) {
+                // the scales of both, where the softmax reads them: four tiles' places, for it may be two behind
+#pragma unroll
+                for (int e = 0; e < 2; e++) {
+                    const bool there = slot[e] != 0xFFFFFFFFu;
+                    const char* p = scales + (there ? slot[e] * a.token_bytes : 0ull);
+                    cp_async4(smem_u32(&sh.k_scale[fetched & 3u][e * 32 + lane]), p, there ? 4u : 0u);
+                    cp_async4(smem_u32(&sh.v_scale[fetched & 3u][e * 32 + lane]), p + 4, there ? 4u : 0u);
+                }
+                asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(&sh.scaled[fetched & 3u])) : "memory");
+            }
+            asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(&sh.fetched[kv][at_place])) : "memory");
+            fetched++;
+        };
+#pragma unroll 1
+        while (more) fetch();
+        // the copies under way end before the CTA does, whether or not anybody is left to wait for them
+        cp_commit();
+        cp_wait<0>();
+        for (uint32_t k = fetched > TC8_AHEAD ? fetched - TC8_AHEAD : 0; k < fetched; k++) bar_drain(&sh.fetched[kv][k % TC8_AHEAD], (k / TC8_AHEAD) & 1u);
     } else {
         // ------------------------------------------------------------------ softmax
         const uint32_t row = threadIdx.x, lane_base = (warp * 32u) << 16;
@@ -385,10 +404,15 @@ __global__ void __launch_bounds__(TC8_THREADS, 2) attn8_tc_kernel(const __grid_c
                     sees = there && !masked_short ? row_sees64(a, w.s.have, w.s.want, w.row0 + i, i, t0) : 0ull;
                     if (NEAR && a.window) sees &= in_window64(a.window, w.s.have + i, t0);
                 }
-                // four places for scales: those of tile n + 4 come after V of tile n + 2, so after P V of tile n + 1
+                // those of tile n + 4 are fetched when V of tile n + 2 is converted, so after P V of tile n + 1
                 if (!warp_wait(&sh.scaled[n & 3u], (n >> 2) & 1u, dead, a) || !warp_wait(&sh.s_full[n & 1u], (n >> 1) & 1u, dead, a)) {
                     alive = false;
                     break;
+                }
+                uint64_t odd = 0ull;
+                if (mixed) {
+                    if (!warp_wait(&sh.checked[n & 3u], (n >> 2) & 1u, dead, a)) { alive = false; break; }
+                    odd = (uint64_t)*(volatile uint32_t*)&sh.odd[n & 3u][0] | (uint64_t)*(volatile uint32_t*)&sh.odd[n & 3u][1] << 32;
                 }
                 if (!warp_there) {                         // rows that do not exist: whatever P holds stays in them
                     __syncwarp();
@@ -410,17 +434,28 @@ __global__ void __launch_bounds__(TC8_THREADS, 2) attn8_tc_kernel(const __grid_c
                         float y[4];
                         split2(mul2(pair2(__uint_as_float(sc[x][c]), __uint_as_float(sc[x][c + 1])), pair2(ks.x, ks.y)), y[0], y[1]);
                         split2(mul2(pair2(__uint_as_float(sc[x][c + 2]), __uint_as_float(sc[x][c + 3])), pair2(ks.z, ks.w)), y[2], y[3]);
-                        if constexpr (NEAR) {
-#pragma unroll
-                            for (int e = 0; e < 4; e++) {
-                                y[e] *= scale;
-                                if (a.cap_out != 0.f) y[e] = a.cap_out * tanh_of(y[e]);
-                                if (a.slopes) y[e] += slope * (float)((int32_t)(t0 + 32 * x + c + e) - (int32_t)(w.s.have + i));
-                            }
-                        }
 #pragma unroll
                         for (int e = 0; e < 4; e++) sc[x][c + e] = __float_as_uint(y[e]);
                     }
+                float by = scale;                          // what the scores still lack
+                if constexpr (NEAR) {
+                    if (a.cap_out != 0.f) {
+#pragma unroll
+                        for (int x = 0; x < 2; x++)
+#pragma unroll
+                            for (int c = 0; c < 32; c++) sc[x][c] = __float_as_uint(a.cap_out * tanh_of(__uint_as_float(sc[x][c]) * scale));
+                        by = 1.f;
+                    }
+                    if (a.slopes) {
+                        const float away = (float)((int32_t)t0 - (int32_t)(w.s.have + i));
+#pragma unroll
+                        for (int x = 0; x < 2; x++)
+#pragma unroll
+                            for (int c = 0; c < 32; c++)
+                                sc[x][c] = __float_as_uint(__uint_as_float(sc[x][c]) * by + slope * (away + (float)(32 * x + c)));
+                        by = 1.f;
+                    }
+                }
                 if (mixed) {
 #pragma unroll
                     for (int x = 0; x < 2; x++)
@@ -435,7 +470,6 @@ __global__ void __launch_bounds__(TC8_THREADS, 2) attn8_tc_kernel(const __grid_c
                     for (int c = 0; c < 32; c += 2)
                         tops[(c >> 1) & 3] = max3(tops[(c >> 1) & 3], __uint_as_float(sc[x][c]), __uint_as_float(sc[x][c + 1]));
                 // the scale is positive here (q's sign carries it), so the largest score stays the largest
-                const float by = NEAR ? 1.f : scale;
                 const float top = max3(tops[0], tops[1], fmaxf(tops[2], tops[3])) * by;
                 const bool grow = top > m + 8.f;           // also when nothing has been seen yet
                 float alpha = 1.f;
@@ -471,6 +505,14 @@ __global__ void __launch_bounds__(TC8_THREADS, 2) attn8_tc_kernel(const __grid_c
 #pragma unroll
                         for (int c = 0; c < 32; c++)
                             if (!((uint32_t)(sees >> (32 * x)) >> c & 1u)) sc[x][c] = 0u;
+                    odd &= sees;
+                    if (odd != 0ull) {
+#pragma unroll
+                        for (int x = 0; x < 2; x++)
+#pragma unroll
+                            for (int c = 0; c < 32; c++)
+                                if ((uint32_t)(odd >> (32 * x)) >> c & 1u) sc[x][c] = 0x7FC00000u;
+                    }
                 }
                 {
                     float lo, hi;
@@ -524,6 +566,9 @@ __global__ void __launch_bounds__(TC8_THREADS, 2) attn8_tc_kernel(const __grid_c
             }
             // ---------------------------------------------------------- the piece's end
             if (alive) alive = warp_wait(&sh.o_done[(n - 1) & 1u], ((n - 1) >> 1) & 1u, dead, a);
+            // both verdicts: the warps that fetch are four tiles ahead at most
+            for (int kv = 0; alive && kv < 2; kv++)
+                alive = warp_wait(&sh.judged[kv][piece % TC8_BITS_RING], (piece / TC8_BITS_RING) & 1u, dead, a);
             tc_after();
             // The four warps agree on how the piece ended: it is complete when each of them saw its last
             // product, whatever the other roles come to.  The verdict of the piece before, which all have read

@@ -232,100 +232,17 @@ attn8_tc_kernel(const __grid_constant__ Attn8Args a, const __grid_constant__ CUt
         __syncwarp();
     } else if (warp >= 6) {
         // ------------------------------------------------------------------ codes from the pages
+        // Warp 6: K; warp 7: V.  When a tile is converted the place that its codes had is free for those of two tiles later.
         const uint32_t kv = warp - 6;
-        const uint32_t raw = sm + L::codes + kv * (TC8_AHEAD * TC8_TILE * D) + lane * 16;
-        Walk<TC8_TILE, NEAR>& f = w;
-        uint32_t fetched = 0, fetch_piece = 0, left = 0, t_next = 0, bits = 0u;        // tiles of the piece to go; this lane's first token
-        int32_t next[2] = {-1, -1}, label[2] = {GIFT_OWNER_PARAM, GIFT_OWNER_PARAM};
-        bool more = true;
-        // Lane l looks up tokens l and l + 32 of a tile.  Table entries are fetched one tile ahead, labels judged a tile
-        // later; after a piece's last tile the piece is.
-        // (a load waits for the copies that were started before it, so what a piece needs is loaded once)
-        int32_t owner = 0;
-        const int32_t* table = nullptr;
-        uint32_t want = 0, low = 0;
-        const char* from = nullptr;
-        const char* scales = nullptr;
-        int32_t x = 0;                                         // column of the map
-        auto entries = [&](uint32_t t) {
-#pragma unroll
-            for (int e = 0; e < 2; e++) next[e] = t + e * 32 < want && (!NEAR || t + e * 32 >= low) ? table[a.b.page.quot(t + e * 32)] : -1;
-        };
-        auto judge = [&]() {
-#pragma unroll
-            for (int e = 0; e < 2; e++) {
-                bits |= label_read_status(label[e], owner);
-                label[e] = GIFT_OWNER_PARAM;
-            }
-        };
-        auto fetch = [&]() {
-            if (!more) return;
-            if (fetched > 0 || left > 0) judge();              // the pages of the tile before
-            if (left == 0) {
-                if (fetched > 0) {
-                    bits = __reduce_or_sync(0xFFFFFFFFu, bits);
-                    if (lane == 0) {
-                        if (bits) atomicOr(&sh.bits[fetch_piece % TC8_BITS_RING], bits);
-                        bar_arrive(&sh.judged[kv][fetch_piece % TC8_BITS_RING]);
-                    }
-                    fetch_piece++;
-                }
-                more = walk8_next(f, a, lane);
-                if (!more) return;
-                left = f.n_tiles;
-                t_next = (f.tb + (NEAR ? f.it.first : 0u)) * TC8_TILE + lane;
-                bits = f.masked_short(a) ? GIFT_ST_BAD_DESC : 0u;
-                owner = a.b.owner[f.r];
-                table = a.b.table + (uint64_t)f.r * a.b.max_blocks;
-                want = f.s.want;
-                low = NEAR ? first_seen(a, f.s.have) & ~(a.copy_run - 1u) : 0u;        // whole runs
-                from = a.pages + (uint64_t)kv * a.codes + (uint64_t)f.h * D + chunk * 16;
-                scales = a.pages + 2ull * a.codes + f.h * 8u;
-                x = (int32_t)(kv * a.codes + f.h * D);
-                entries(t_next);
-            }
-            uint32_t slot[2];                                  // of this tile's tokens
-#pragma unroll
-            for (int e = 0; e < 2; e++) {
-                const uint32_t t = t_next + e * 32;
-                slot[e] = 0xFFFFFFFFu;
-                if (t < want && (!NEAR || t >= low)) {
-                    if ((uint32_t)next[e] < a.b.n_pages) {
-                        slot[e] = (uint32_t)next[e] * a.b.page_tokens + (t - a.b.page.quot(t) * a.b.page_tokens);
-                        if (a.owner_map) label[e] = a.owner_map[next[e]];
-                    } else {
-                        bits |= GIFT_ST_BAD_DESC;
-                    }
-                }
-            }
-            left--;
-            t_next += TC8_TILE;
-            if (left > 0) entries(t_next);
-            const uint32_t at_place = fetched % TC8_AHEAD, place = raw + at_place * (TC8_TILE * D);
-            more = fetched < TC8_AHEAD || warp_wait(&sh.taken[kv][at_place], (fetched / TC8_AHEAD - 1) & 1u, dead, a);
-            if (!more) return;
-            if (a.copy_run >= 8) {
-                // A run is one copy, by the lane that looked up its first token.  What it holds past the context, or before
-                // a window, is hidden from every row; runs that nobody sees are sent outside the map, and are zeros.
-                uint64_t* bar = &sh.fetched[kv][at_place];
-                if (lane == 0) asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(bar)), "r"(TC8_TILE * D) : "memory");
-                __syncwarp();
-#pragma unroll
-                for (uint32_t e = 0; e < 2; e++)
-                    if (((e * 32 + lane) & (a.copy_run - 1u)) == 0u)
-                        copy_run(place - lane * 16 + (e * 32 + lane) * D, &code_map, x, slot[e] == 0xFFFFFFFFu ? -(int32_t)TC8_TILE : (int32_t)slot[e], bar);
-            } else {
-                // tokens that nobody sees are zeros: what memory holds there does not matter
-#pragma unroll 4
-                for (int i = 0; i < LOADS; i++) {
-                    const uint32_t row = i * ROWS_AT_ONCE + sub;
-                    const uint32_t at = __shfl_sync(0xFFFFFFFFu, i * ROWS_AT_ONCE < 32 ? slot[0] : slot[1], row & 31u);
-                    const bool there = at != 0xFFFFFFFFu;
-                    cp_async16(place + i * 512, there ? from + at * a.token_bytes : from, there ? 16u : 0u);
-                }
-            }
+        const uint32_t raw = sm + L::codes + kv * (TC8_AHEAD * TC8_TILE * D);
+        uint32_t fetched = 0, piece = 0;
+        bool ok = true;
+        // A tile's codes and scales, of the tokens in slot[]: lane and lane + 32.
+        auto fetch = [&](const uint32_t (&slot)[2], uint32_t h) {
             if (kv) {
-                // the scales of both, where the softmax reads them: four tiles' places, for it may be two behind
+                // the scales of both, where the softmax reads them, before there is room for the codes: four tiles' places (the
+                // tile whose scales were here is done, since V of the one behind it was converted)
+                const char* scales = a.pages + 2ull * a.codes + h * 8u;
 #pragma unroll
                 for (int e = 0; e < 2; e++) {
                     const bool there = slot[e] != 0xFFFFFFFFu;
@@ -335,11 +252,116 @@ attn8_tc_kernel(const __grid_constant__ Attn8Args a, const __grid_constant__ CUt
                 }
                 asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(&sh.scaled[fetched & 3u])) : "memory");
             }
-            asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(&sh.fetched[kv][at_place])) : "memory");
+            const uint32_t at_place = fetched % TC8_AHEAD, place = raw + at_place * (TC8_TILE * D);
+            uint64_t* bar = &sh.fetched[kv][at_place];
+            ok = fetched < TC8_AHEAD || warp_wait(&sh.taken[kv][at_place], (fetched / TC8_AHEAD - 1) & 1u, dead, a);
+            if (!ok) return;
+            if (a.copy_run >= 8) {
+                // A run is one copy, by the lane that has its first token.  What it holds past the context, or before
+                // a window, is hidden from every row; runs that nobody sees are sent outside the map, and are zeros.
+                if (lane == 0) asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(bar)), "r"(TC8_TILE * D) : "memory");
+                __syncwarp();
+#pragma unroll
+                for (uint32_t e = 0; e < 2; e++)
+                    if (((e * 32 + lane) & (a.copy_run - 1u)) == 0u)
+                        copy_run(place + (e * 32 + lane) * D, &code_map, (int32_t)(kv * a.codes + h * D),
+                                 slot[e] == 0xFFFFFFFFu ? -(int32_t)TC8_TILE : (int32_t)slot[e], bar);
+                bar_arrive(bar);
+            } else {
+                // tokens that nobody sees are zeros: what memory holds there does not matter
+                const char* from = a.pages + (uint64_t)kv * a.codes + (uint64_t)h * D + chunk * 16;
+#pragma unroll 4
+                for (int i = 0; i < LOADS; i++) {
+                    const uint32_t row = i * ROWS_AT_ONCE + sub;
+                    const uint32_t at = __shfl_sync(0xFFFFFFFFu, i * ROWS_AT_ONCE < 32 ? slot[0] : slot[1], row & 31u);
+                    const bool there = at != 0xFFFFFFFFu;
+                    cp_async16(place + (i * 32 + lane) * 16, there ? from + at * a.token_bytes : from, there ? 16u : 0u);
+                }
+                asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+            }
             fetched++;
         };
+        while (ok && walk8_next(w, a, lane)) {
+            const int32_t owner = a.b.owner[w.r];
+            const int32_t* table = a.b.table + (uint64_t)w.r * a.b.max_blocks;
+            const uint32_t want = w.s.want, h = w.h, n_tiles = w.n_tiles;
+            const uint32_t begin_t = (w.tb + (NEAR ? w.it.first : 0u)) * TC8_TILE, end_t = want - begin_t < n_tiles * TC8_TILE ? want : begin_t + n_tiles * TC8_TILE;
+            const uint32_t low = NEAR ? first_seen(a, w.s.have) : 0u, from_t = begin_t < low ? low : begin_t;
+            uint32_t bits = w.masked_short(a) ? GIFT_ST_BAD_DESC : 0u;
+            if (a.copy_run >= 8) {
+                // The lanes hold the table's entries of 32 pages and of the next 32, which are asked for 32 pages ahead: every
+                // load waits for the copies of scales that were started before it, on the whole SM (a tile's own entries
+                // asked for one tile ahead: 617 us for trees of up to 64 rows, this way XXX).
+                const uint32_t run_low = low & ~(a.copy_run - 1u);
+                uint32_t base = a.b.page.quot(from_t);
+                auto used = [&](uint32_t p) { return p * a.b.page_tokens < end_t && (p + 1u) * a.b.page_tokens > from_t; };
+                auto entry = [&](uint32_t p) -> int32_t { return used(p) ? table[p] : -1; };
+                int32_t label = GIFT_OWNER_PARAM;
+                auto ask = [&](int32_t& page) {                // for the label of this lane's page of those from base
+                    label = GIFT_OWNER_PARAM;
+                    if (!used(base + lane)) return;
+                    if ((uint32_t)page >= a.b.n_pages) bits |= GIFT_ST_BAD_DESC;
+                    else if (a.owner_map) label = a.owner_map[page];
+                };
+                int32_t cur = entry(base + lane), ahead = entry(base + 32u + lane);
+                ask(cur);
 #pragma unroll 1
-        while (more) fetch();
+                for (uint32_t j = 0; ok && j < n_tiles; j++) {
+                    const uint32_t t0 = begin_t + j * TC8_TILE;
+                    if (t0 > from_t && a.b.page.quot(t0) >= base + 32u) {
+                        bits |= label_read_status(label, owner);
+                        cur = ahead;
+                        base += 32u;
+                        ahead = entry(base + 32u + lane);
+                        ask(cur);
+                    }
+                    uint32_t slot[2];
+#pragma unroll
+                    for (int e = 0; e < 2; e++) {
+                        const uint32_t t = t0 + e * 32 + lane, p = a.b.page.quot(t), k = p - base;
+                        const int32_t p0 = __shfl_sync(0xFFFFFFFFu, cur, k & 31u), p1 = __shfl_sync(0xFFFFFFFFu, ahead, k & 31u);
+                        const uint32_t page = (uint32_t)(k < 32u ? p0 : p1);
+                        slot[e] = t < want && (!NEAR || t >= run_low) && page < a.b.n_pages ? page * a.b.page_tokens + (t - p * a.b.page_tokens) : 0xFFFFFFFFu;
+                    }
+                    fetch(slot, h);
+                }
+                bits |= label_read_status(label, owner);
+                base += 32u;
+                ask(ahead);
+                bits |= label_read_status(label, owner);
+            } else {
+                // lane l looks up tokens l and l + 32: entries are fetched one tile ahead, labels judged a tile later
+                int32_t next[2] = {-1, -1}, label[2] = {GIFT_OWNER_PARAM, GIFT_OWNER_PARAM};
+#pragma unroll 1
+                for (uint32_t j = 0; ok && j <= n_tiles; j++) {
+                    uint32_t slot[2];
+#pragma unroll
+                    for (int e = 0; e < 2; e++) {
+                        const uint32_t t_next = begin_t + j * TC8_TILE + e * 32 + lane, t = t_next - TC8_TILE;
+                        bits |= label_read_status(label[e], owner);
+                        label[e] = GIFT_OWNER_PARAM;
+                        slot[e] = 0xFFFFFFFFu;
+                        if (j > 0 && t < want && (!NEAR || t >= low)) {
+                            if ((uint32_t)next[e] < a.b.n_pages) {
+                                slot[e] = (uint32_t)next[e] * a.b.page_tokens + (t - a.b.page.quot(t) * a.b.page_tokens);
+                                if (a.owner_map) label[e] = a.owner_map[next[e]];
+                            } else {
+                                bits |= GIFT_ST_BAD_DESC;
+                            }
+                        }
+                        next[e] = j < n_tiles && t_next < want && (!NEAR || t_next >= low) ? table[a.b.page.quot(t_next)] : -1;
+                    }
+                    if (j > 0) fetch(slot, h);
+                }
+                bits |= label_read_status(label[0], owner) | label_read_status(label[1], owner);
+            }
+            bits = __reduce_or_sync(0xFFFFFFFFu, bits);
+            if (lane == 0) {
+                if (bits) atomicOr(&sh.bits[piece % TC8_BITS_RING], bits);
+                bar_arrive(&sh.judged[kv][piece % TC8_BITS_RING]);
+            }
+            piece++;
+        }
         // the copies under way end before the CTA does, whether or not anybody is left to wait for them
         cp_commit();
         cp_wait<0>();
@@ -404,7 +426,7 @@ attn8_tc_kernel(const __grid_constant__ Attn8Args a, const __grid_constant__ CUt
                     sees = there && !masked_short ? row_sees64(a, w.s.have, w.s.want, w.row0 + i, i, t0) : 0ull;
                     if (NEAR && a.window) sees &= in_window64(a.window, w.s.have + i, t0);
                 }
-                // those of tile n + 4 are fetched when V of tile n + 2 is converted, so after P V of tile n + 1
+                // those of tile n + 4 are fetched when V of tile n + 1 is converted, so after P V of tile n
                 if (!warp_wait(&sh.scaled[n & 3u], (n >> 2) & 1u, dead, a) || !warp_wait(&sh.s_full[n & 1u], (n >> 1) & 1u, dead, a)) {
                     alive = false;
                     break;

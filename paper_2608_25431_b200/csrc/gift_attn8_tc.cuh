@@ -3,9 +3,9 @@
 // The roles and barriers of the 16-bit kernel: a tile of 128 query rows (or what whole tokens fit) meets tiles of 64
 // tokens, S = Q K^T lands in tensor memory, one row per thread of four softmax warps, P goes back into the columns of
 // its S and is the A operand of O += P V.  What differs:
-//   warps 6, 7 fetch the codes (and scales) of K and of V into shared memory, two tiles ahead.  Each judges the labels of the
-//              pages that it reads.
-//   warps 4, 5 put the codes as fp16 numbers (exact) where the products read them, and issue those.  (A product of codes
+//   warps 6, 7 fetch the codes (and scales) of K and of V into shared memory, two tiles ahead, judge the labels of the pages that
+//              they read, and issue the products.
+//   warps 4, 5 put the codes as fp16 numbers (exact) where the products read them.  (A product of codes
 //              would need q and the weights as codes too.)
 //   softmax    K's scale multiplies the score, V's the weight, in 32 bits.  Weights go to fp16 by a power of two of the row's
 //              own, which follows the largest p * scale as the maximum follows the scores; O is in its units.
@@ -35,7 +35,7 @@ template <int D> struct Tc8Smem {
 };
 
 struct Tc8Shared {
-    uint64_t fetched[2][TC8_AHEAD], taken[2][TC8_AHEAD], judged[2][TC8_BITS_RING];                 // of K, of V
+    uint64_t fetched[2][TC8_AHEAD], full[2], judged[2][TC8_BITS_RING];                 // of K, of V
     uint64_t scaled[4], checked[4], s_full[2], p_full[2], o_done[2], s_done, q_full, q_ready, last;
     float k_scale[4][TC8_TILE], v_scale[4][TC8_TILE];                                 // by tile
     uint32_t odd[4][2];              // tokens with a code of NaN in V, by tile
@@ -44,6 +44,15 @@ struct Tc8Shared {
     int dead;
     PlaceShared place;
 };
+
+// One lane of a converged warp, in a way that lets the compiler see that one it is (products issued by it instead of by
+// "lane 0": 612 -> 572 us for trees of up to 64 rows).
+__device__ __forceinline__ bool elect_one()
+{
+    uint32_t p;
+    asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xFFFFFFFF;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(p));
+    return p != 0u;
+}
 
 // A role's walk lies in shared memory: its two dozen words are used at a piece's ends, registers in between.
 template <bool NEAR>
@@ -74,7 +83,7 @@ attn8_tc_kernel(const __grid_constant__ Attn8Args a, const __grid_constant__ CUt
     constexpr uint32_t S_COL = 0, O_COL = 2 * TC8_TILE;
     extern __shared__ __align__(1024) char smem[];
     __shared__ __align__(16) Tc8Shared sh;
-    __shared__ Walk<TC8_TILE, NEAR> walks[TC8_THREADS / 32];
+    __shared__ Walk<TC8_TILE, NEAR> walks[TC8_THREADS / 32 + 2];       // of the warps, and of the codes that two of them fetch
     using L = Tc8Smem<D>;
 
     join_may_start();
@@ -85,8 +94,9 @@ attn8_tc_kernel(const __grid_constant__ Attn8Args a, const __grid_constant__ CUt
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         for (int kv = 0; kv < 2; kv++) {
-            for (int i = 0; i < TC8_AHEAD; i++) { bar_init(&sh.fetched[kv][i], 32); bar_init(&sh.taken[kv][i], 1); }
+            for (int i = 0; i < TC8_AHEAD; i++) bar_init(&sh.fetched[kv][i], 32);
             for (int i = 0; i < TC8_BITS_RING; i++) bar_init(&sh.judged[kv][i], 1);
+            bar_init(&sh.full[kv], 1);
         }
         for (int i = 0; i < 4; i++) { bar_init(&sh.scaled[i], 32); bar_init(&sh.checked[i], 1); }
         for (int i = 0; i < 2; i++) { bar_init(&sh.s_full[i], 1); bar_init(&sh.p_full[i], 4); bar_init(&sh.o_done[i], 1); }
@@ -114,7 +124,10 @@ attn8_tc_kernel(const __grid_constant__ Attn8Args a, const __grid_constant__ CUt
     {
         Walk<TC8_TILE, NEAR> x;
         x.start(a, sh.place.at, blockIdx.x % a.ways, units);
-        if (lane == 0) w = x;
+        if (lane == 0) {
+            w = x;
+            if (warp >= 6) walks[warp + 2] = x;
+        }
         __syncwarp();
     }
 
@@ -122,19 +135,13 @@ attn8_tc_kernel(const __grid_constant__ Attn8Args a, const __grid_constant__ CUt
     constexpr int ROW_LANES = D / 16, ROWS_AT_ONCE = 32 / ROW_LANES, LOADS = TC8_TILE / ROWS_AT_ONCE;
     const uint32_t chunk = lane % ROW_LANES, sub = lane / ROW_LANES;
     if (warp == 4 || warp == 5) {
-        // ------------------------------------------------------------------ codes to fp16, and the products
-        // Warp 4: K, and Q K^T; warp 5: V, and P V.
+        // ------------------------------------------------------------------ codes to fp16
         const uint32_t kv = warp - 4;
         const uint32_t raw = sm + L::codes + kv * (TC8_AHEAD * TC8_TILE * D) + lane * 16;
         // 16 codes are two 16-byte chunks of their row; lanes of the second block of 64 columns begin with the
         // second one, for other banks than those of the first
         const uint32_t block = chunk >> 2, dst = sm + (kv ? L::v : L::k) + block * (TC8_TILE * 128);
-        // a negative scale: the products negate q, so that the scale used on the scores is positive
-        const uint32_t id_s = instr_desc<__half>(TC8_ROWS, TC8_TILE, 0) | (a.negate << 13);
-        constexpr uint32_t id_o = instr_desc<__half>(TC8_ROWS, D, 1);
-        const uint64_t q_desc = smem_desc(sm + L::q, 16, 1024), k_desc = smem_desc(sm + L::k, 16, 1024);
-        const uint64_t v_desc = smem_desc(sm + L::v, TC8_TILE * 128, 1024);
-        uint32_t n = 0, piece = 0, q_loads = 0;
+        uint32_t n = 0;
         bool ok = true;
         while (ok && walk8_next(w, a, lane)) {
             const uint32_t n_tiles = w.n_tiles, have = w.s.have, want = w.s.want, tb = w.tb + (NEAR ? w.it.first : 0u);
@@ -169,22 +176,14 @@ attn8_tc_kernel(const __grid_constant__ Attn8Args a, const __grid_constant__ CUt
                 // the product with the tile before is complete
                 ok = n == 0 || (kv ? warp_wait(&sh.o_done[(n - 1) & 1u], ((n - 1) >> 1) & 1u, dead, a) : warp_wait(&sh.s_done, (n - 1) & 1u, dead, a));
                 if (!ok) break;
-                if (kv == 0 && j == 0) {
-                    // Q.  What the box holds past the request's rows is another request's: rows that nobody asks for.
-                    q_loads++;
-                    if (lane == 0) {
-                        bar_expect(&sh.q_full, a.tile_rows * D * 2);
+                // (loaded all at once: it is a chain of latencies otherwise)
+                uint4 x[LOADS];
 #pragma unroll
-                        for (int c = 0; c < D / 64; c++)
-                            copy_q(sm + L::q + c * (TC8_ROWS * 128), &q_map, c * 64, (int32_t)(w.h * a.group),
-                                   (int32_t)(w.row0 + a.by_group.quot(w.qt * a.tile_rows)), &sh.q_full);
-                    }
-                }
-#pragma unroll 4
+                for (int i = 0; i < LOADS; i++) x[i] = lds128(place + i * 512);
+#pragma unroll
                 for (int i = 0; i < LOADS; i++) {
                     const uint32_t row = i * ROWS_AT_ONCE + sub;
-                    const uint4 x = lds128(place + i * 512);
-                    const uint32_t first[2] = {block ? x.z : x.x, block ? x.w : x.y}, second[2] = {block ? x.x : x.z, block ? x.y : x.w};
+                    const uint32_t first[2] = {block ? x[i].z : x[i].x, block ? x[i].w : x[i].y}, second[2] = {block ? x[i].x : x[i].z, block ? x[i].y : x[i].w};
                     const uint32_t at = dst + row * 128 + (((chunk & 3u) * 2 + block ^ (row & 7u)) << 4);
                     uint32_t f[4];
                     four_codes(first[0], f[0], f[1]);
@@ -196,12 +195,191 @@ attn8_tc_kernel(const __grid_constant__ Attn8Args a, const __grid_constant__ CUt
                 }
                 publish_smem();
                 __syncwarp();
-                if (lane == 0) bar_arrive(&sh.taken[kv][n % TC8_AHEAD]);
-                // Q, and S's columns, which held P of tile n - 2; or P
-                if (kv == 0) ok = (j > 0 || warp_wait(&sh.q_ready, piece & 1u, dead, a)) && (n < 2 || warp_wait(&sh.o_done[n & 1u], ((n - 2) >> 1) & 1u, dead, a));
-                else ok = warp_wait(&sh.p_full[n & 1u], (n >> 1) & 1u, dead, a);
+                if (lane == 0) bar_arrive(&sh.full[kv]);
+            }
+        }
+    } else if (warp >= 6) {
+        // ------------------------------------------------------------------ codes from the pages, and the products
+        // Warp 6: K, and Q K^T; warp 7: V, and P V.  When a tile is converted the place that its codes had is free for those of
+        // two tiles later, perhaps of another piece: what is fetched has a walk of its own.
+        const uint32_t kv = warp - 6;
+        const uint32_t raw = sm + L::codes + kv * (TC8_AHEAD * TC8_TILE * D);
+        Walk<TC8_TILE, NEAR>& f = walks[warp + 2];
+        uint32_t fetched = 0, judged = 0, left = 0;            // tiles so far, pieces judged; tiles of the piece to go
+        bool more = true, begun = false;
+        uint32_t slot[2] = {0, 0}, slot_head = 0;              // of the next tile's tokens lane and lane + 32; its K/V head
+        // The next tile's scales go where the softmax reads them: four tiles' places (the tile whose scales were here is
+        // done, since V of the one behind it was converted).
+        auto fetch_scales = [&]() {
+            const char* scales = a.pages + 2ull * a.codes + slot_head * 8u;
+            const uint32_t at = fetched & 3u;
+#pragma unroll
+            for (int e = 0; e < 2; e++) {
+                const bool there = slot[e] != 0xFFFFFFFFu;
+                const char* p = scales + (there ? slot[e] * a.token_bytes : 0ull);
+                cp_async4(smem_u32(&sh.k_scale[at][e * 32 + lane]), p, there ? 4u : 0u);
+                cp_async4(smem_u32(&sh.v_scale[at][e * 32 + lane]), p + 4, there ? 4u : 0u);
+            }
+            asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(&sh.scaled[at])) : "memory");
+        };
+        auto fetch_codes = [&]() {
+            const uint32_t at_place = fetched % TC8_AHEAD, place = raw + at_place * (TC8_TILE * D);
+            uint64_t* bar = &sh.fetched[kv][at_place];
+            if (a.copy_run >= 8) {
+                // A run is one copy, by the lane that has its first token.  What it holds past the context, or before
+                // a window, is hidden from every row; runs that nobody sees are sent outside the map, and are zeros.
+                if (lane == 0) asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(bar)), "r"(TC8_TILE * D) : "memory");
+                __syncwarp();
+#pragma unroll
+                for (uint32_t e = 0; e < 2; e++)
+                    if (((e * 32 + lane) & (a.copy_run - 1u)) == 0u)
+                        copy_run(place + (e * 32 + lane) * D, &code_map, (int32_t)(kv * a.codes + slot_head * D),
+                                 slot[e] == 0xFFFFFFFFu ? -(int32_t)TC8_TILE : (int32_t)slot[e], bar);
+                bar_arrive(bar);
+            } else {
+                // tokens that nobody sees are zeros: what memory holds there does not matter
+                const char* from = a.pages + (uint64_t)kv * a.codes + (uint64_t)slot_head * D + chunk * 16;
+#pragma unroll 4
+                for (int i = 0; i < LOADS; i++) {
+                    const uint32_t row = i * ROWS_AT_ONCE + sub;
+                    const uint32_t at = __shfl_sync(0xFFFFFFFFu, i * ROWS_AT_ONCE < 32 ? slot[0] : slot[1], row & 31u);
+                    const bool there = at != 0xFFFFFFFFu;
+                    cp_async16(place + (i * 32 + lane) * 16, there ? from + at * a.token_bytes : from, there ? 16u : 0u);
+                }
+                asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+            }
+            fetched++;
+        };
+        int32_t owner = 0, label[2] = {GIFT_OWNER_PARAM, GIFT_OWNER_PARAM}, page[2] = {-1, -1};
+        const int32_t* table = nullptr;
+        uint32_t want = 0, begin_t = 0, end_t = 0, from_t = 0, run_low = 0, base = 0, bits = 0;
+        // Pages of 8 or more tokens: the lanes hold the table's entries of 32 pages (page[0]) and of the next 32, which are asked
+        // for 32 pages ahead.  Every load waits for the copies of scales that were started before it, on the whole SM.
+        // Smaller pages: the entries of tokens lane and lane + 32, asked for one tile ahead, labels judged a tile later.
+        auto used = [&](uint32_t p) { return p * a.b.page_tokens < end_t && (p + 1u) * a.b.page_tokens > from_t; };
+        auto entry = [&](uint32_t p) -> int32_t { return used(p) ? table[p] : -1; };
+        auto entry_of = [&](uint32_t t) -> int32_t { return t < end_t && t >= from_t ? table[a.b.page.quot(t)] : -1; };
+        auto judge = [&]() {
+#pragma unroll
+            for (int e = 0; e < 2; e++) {
+                bits |= label_read_status(label[e], owner);
+                label[e] = GIFT_OWNER_PARAM;
+            }
+        };
+        auto ask = [&](int32_t p, bool there, int32_t& l) {    // for a page's label
+            if (!there) return;
+            if ((uint32_t)p >= a.b.n_pages) bits |= GIFT_ST_BAD_DESC;
+            else if (a.owner_map) l = a.owner_map[p];
+        };
+        // The next tile's slots, and its scales.
+        auto advance = [&]() {
+            if (left == 0) {
+                if (begun) {
+                    // the piece's verdict
+                    if (a.copy_run >= 8) ask(page[1], used(base + 32u + lane), label[1]);
+                    judge();
+                    bits = __reduce_or_sync(0xFFFFFFFFu, bits);
+                    if (lane == 0) {
+                        if (bits) atomicOr(&sh.bits[judged % TC8_BITS_RING], bits);
+                        bar_arrive(&sh.judged[kv][judged % TC8_BITS_RING]);
+                    }
+                    judged++;
+                }
+                more = walk8_next(f, a, lane);
+                if (!more) return;
+                begun = true;
+                left = f.n_tiles;
+                owner = a.b.owner[f.r];
+                table = a.b.table + (uint64_t)f.r * a.b.max_blocks;
+                want = f.s.want;
+                begin_t = (f.tb + (NEAR ? f.it.first : 0u)) * TC8_TILE;
+                end_t = want - begin_t < left * TC8_TILE ? want : begin_t + left * TC8_TILE;
+                const uint32_t low = NEAR ? first_seen(a, f.s.have) : 0u;
+                from_t = begin_t < low ? low : begin_t;
+                run_low = low & ~(a.copy_run - 1u);
+                bits = f.masked_short(a) ? GIFT_ST_BAD_DESC : 0u;
+                if (a.copy_run >= 8) {
+                    base = a.b.page.quot(from_t);
+                    page[0] = entry(base + lane);
+                    page[1] = entry(base + 32u + lane);
+                    ask(page[0], used(base + lane), label[0]);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 2; e++) page[e] = entry_of(begin_t + e * 32 + lane);
+                }
+            }
+            if (a.copy_run >= 8) {
+                if (begin_t > from_t && a.b.page.quot(begin_t) >= base + 32u) {
+                    judge();
+                    page[0] = page[1];
+                    base += 32u;
+                    page[1] = entry(base + 32u + lane);
+                    ask(page[0], used(base + lane), label[0]);
+                }
+#pragma unroll
+                for (int e = 0; e < 2; e++) {
+                    const uint32_t t = begin_t + e * 32 + lane, p = a.b.page.quot(t), k = p - base;
+                    const int32_t p0 = __shfl_sync(0xFFFFFFFFu, page[0], k & 31u), p1 = __shfl_sync(0xFFFFFFFFu, page[1], k & 31u);
+                    const uint32_t at = (uint32_t)(k < 32u ? p0 : p1);
+                    slot[e] = t < want && (!NEAR || t >= run_low) && at < a.b.n_pages ? at * a.b.page_tokens + (t - p * a.b.page_tokens) : 0xFFFFFFFFu;
+                }
+            } else {
+                judge();
+#pragma unroll
+                for (int e = 0; e < 2; e++) {
+                    const uint32_t t = begin_t + e * 32 + lane;
+                    const bool there = t < end_t && t >= from_t;
+                    ask(page[e], there, label[e]);
+                    slot[e] = there && (uint32_t)page[e] < a.b.n_pages ? (uint32_t)page[e] * a.b.page_tokens + (t - a.b.page.quot(t) * a.b.page_tokens) : 0xFFFFFFFFu;
+                    page[e] = entry_of(t + TC8_TILE);
+                }
+            }
+            begin_t += TC8_TILE;
+            left--;
+            slot_head = f.h;
+            if (kv) fetch_scales();
+        };
+        // The next tile's codes, and what the one behind it needs first.
+        auto fetch = [&]() {
+            if (!more) return;
+            fetch_codes();
+            advance();
+        };
+        // a negative scale: the products negate q, so that the scale used on the scores is positive
+        const uint32_t id_s = instr_desc<__half>(TC8_ROWS, TC8_TILE, 0) | (a.negate << 13);
+        constexpr uint32_t id_o = instr_desc<__half>(TC8_ROWS, D, 1);
+        const uint64_t q_desc = smem_desc(sm + L::q, 16, 1024), k_desc = smem_desc(sm + L::k, 16, 1024);
+        const uint64_t v_desc = smem_desc(sm + L::v, TC8_TILE * 128, 1024);
+        uint32_t n = 0, piece = 0, q_loads = 0;
+        bool ok = true;
+        advance();
+#pragma unroll 1
+        for (int i = 0; i < TC8_AHEAD; i++) fetch();
+        while (ok && walk8_next(w, a, lane)) {
+            const uint32_t n_tiles = w.n_tiles;
+            if (kv == 0) {
+                // Q, once the products of the piece before have read the old rows.  What the box holds past the request's rows
+                // is another request's: rows that nobody asks for.
+                ok = n == 0 || warp_wait(&sh.s_done, (n - 1) & 1u, dead, a);
                 if (!ok) break;
+                q_loads++;
                 if (lane == 0) {
+                    bar_expect(&sh.q_full, a.tile_rows * D * 2);
+#pragma unroll
+                    for (int c = 0; c < D / 64; c++)
+                        copy_q(sm + L::q + c * (TC8_ROWS * 128), &q_map, c * 64, (int32_t)(w.h * a.group),
+                               (int32_t)(w.row0 + a.by_group.quot(w.qt * a.tile_rows)), &sh.q_full);
+                }
+                ok = warp_wait(&sh.q_ready, piece & 1u, dead, a);
+            }
+#pragma unroll 1
+            for (uint32_t j = 0; ok && j < n_tiles; j++, n++) {
+                ok = warp_wait(&sh.full[kv], n & 1u, dead, a);
+                if (!ok) break;
+                // S's columns, which held P of tile n - 2; or P
+                ok = kv ? warp_wait(&sh.p_full[n & 1u], (n >> 1) & 1u, dead, a) : n < 2 || warp_wait(&sh.o_done[n & 1u], ((n - 2) >> 1) & 1u, dead, a);
+                if (!ok) break;
+                if (elect_one()) {
                     tc_after();
                     const uint32_t s_at = tmem + S_COL + (n & 1u) * TC8_TILE;
                     if (kv == 0) {
@@ -219,153 +397,19 @@ attn8_tc_kernel(const __grid_constant__ Attn8Args a, const __grid_constant__ CUt
                     }
                 }
                 __syncwarp();
+                fetch();
             }
             piece++;
         }
-        // the copy of Q under way ends before the CTA does, whether or not anybody is left to wait for it
-        if (q_loads > 0) bar_drain(&sh.q_full, (q_loads - 1) & 1u);
-        if (lane == 0) {
-            // nothing may be in flight when the tensor memory is given back
-            mma_commit(&sh.last);
-            bar_drain(&sh.last, 0);
-        }
-        __syncwarp();
-    } else if (warp >= 6) {
-        // ------------------------------------------------------------------ codes from the pages
-        // Warp 6: K; warp 7: V.  When a tile is converted the place that its codes had is free for those of two tiles later.
-        const uint32_t kv = warp - 6;
-        const uint32_t raw = sm + L::codes + kv * (TC8_AHEAD * TC8_TILE * D);
-        uint32_t fetched = 0, piece = 0;
-        bool ok = true;
-        // A tile's codes and scales, of the tokens in slot[]: lane and lane + 32.
-        auto fetch = [&](const uint32_t (&slot)[2], uint32_t h) {
-            if (kv) {
-                // the scales of both, where the softmax reads them, before there is room for the codes: four tiles' places (the
-                // tile whose scales were here is done, since V of the one behind it was converted)
-                const char* scales = a.pages + 2ull * a.codes + h * 8u;
-#pragma unroll
-                for (int e = 0; e < 2; e++) {
-                    const bool there = slot[e] != 0xFFFFFFFFu;
-                    const char* p = scales + (there ? slot[e] * a.token_bytes : 0ull);
-                    cp_async4(smem_u32(&sh.k_scale[fetched & 3u][e * 32 + lane]), p, there ? 4u : 0u);
-                    cp_async4(smem_u32(&sh.v_scale[fetched & 3u][e * 32 + lane]), p + 4, there ? 4u : 0u);
-                }
-                asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(&sh.scaled[fetched & 3u])) : "memory");
-            }
-            const uint32_t at_place = fetched % TC8_AHEAD, place = raw + at_place * (TC8_TILE * D);
-            uint64_t* bar = &sh.fetched[kv][at_place];
-            ok = fetched < TC8_AHEAD || warp_wait(&sh.taken[kv][at_place], (fetched / TC8_AHEAD - 1) & 1u, dead, a);
-            if (!ok) return;
-            if (a.copy_run >= 8) {
-                // A run is one copy, by the lane that has its first token.  What it holds past the context, or before
-                // a window, is hidden from every row; runs that nobody sees are sent outside the map, and are zeros.
-                if (lane == 0) asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(bar)), "r"(TC8_TILE * D) : "memory");
-                __syncwarp();
-#pragma unroll
-                for (uint32_t e = 0; e < 2; e++)
-                    if (((e * 32 + lane) & (a.copy_run - 1u)) == 0u)
-                        copy_run(place + (e * 32 + lane) * D, &code_map, (int32_t)(kv * a.codes + h * D),
-                                 slot[e] == 0xFFFFFFFFu ? -(int32_t)TC8_TILE : (int32_t)slot[e], bar);
-                bar_arrive(bar);
-            } else {
-                // tokens that nobody sees are zeros: what memory holds there does not matter
-                const char* from = a.pages + (uint64_t)kv * a.codes + (uint64_t)h * D + chunk * 16;
-#pragma unroll 4
-                for (int i = 0; i < LOADS; i++) {
-                    const uint32_t row = i * ROWS_AT_ONCE + sub;
-                    const uint32_t at = __shfl_sync(0xFFFFFFFFu, i * ROWS_AT_ONCE < 32 ? slot[0] : slot[1], row & 31u);
-                    const bool there = at != 0xFFFFFFFFu;
-                    cp_async16(place + (i * 32 + lane) * 16, there ? from + at * a.token_bytes : from, there ? 16u : 0u);
-                }
-                asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
-            }
-            fetched++;
-        };
-        while (ok && walk8_next(w, a, lane)) {
-            const int32_t owner = a.b.owner[w.r];
-            const int32_t* table = a.b.table + (uint64_t)w.r * a.b.max_blocks;
-            const uint32_t want = w.s.want, h = w.h, n_tiles = w.n_tiles;
-            const uint32_t begin_t = (w.tb + (NEAR ? w.it.first : 0u)) * TC8_TILE, end_t = want - begin_t < n_tiles * TC8_TILE ? want : begin_t + n_tiles * TC8_TILE;
-            const uint32_t low = NEAR ? first_seen(a, w.s.have) : 0u, from_t = begin_t < low ? low : begin_t;
-            uint32_t bits = w.masked_short(a) ? GIFT_ST_BAD_DESC : 0u;
-            if (a.copy_run >= 8) {
-                // The lanes hold the table's entries of 32 pages and of the next 32, which are asked for 32 pages ahead: every
-                // load waits for the copies of scales that were started before it, on the whole SM (a tile's own entries
-                // asked for one tile ahead: 617 us for trees of up to 64 rows, this way XXX).
-                const uint32_t run_low = low & ~(a.copy_run - 1u);
-                uint32_t base = a.b.page.quot(from_t);
-                auto used = [&](uint32_t p) { return p * a.b.page_tokens < end_t && (p + 1u) * a.b.page_tokens > from_t; };
-                auto entry = [&](uint32_t p) -> int32_t { return used(p) ? table[p] : -1; };
-                int32_t label = GIFT_OWNER_PARAM;
-                auto ask = [&](int32_t& page) {                // for the label of this lane's page of those from base
-                    label = GIFT_OWNER_PARAM;
-                    if (!used(base + lane)) return;
-                    if ((uint32_t)page >= a.b.n_pages) bits |= GIFT_ST_BAD_DESC;
-                    else if (a.owner_map) label = a.owner_map[page];
-                };
-                int32_t cur = entry(base + lane), ahead = entry(base + 32u + lane);
-                ask(cur);
-#pragma unroll 1
-                for (uint32_t j = 0; ok && j < n_tiles; j++) {
-                    const uint32_t t0 = begin_t + j * TC8_TILE;
-                    if (t0 > from_t && a.b.page.quot(t0) >= base + 32u) {
-                        bits |= label_read_status(label, owner);
-                        cur = ahead;
-                        base += 32u;
-                        ahead = entry(base + 32u + lane);
-                        ask(cur);
-                    }
-                    uint32_t slot[2];
-#pragma unroll
-                    for (int e = 0; e < 2; e++) {
-                        const uint32_t t = t0 + e * 32 + lane, p = a.b.page.quot(t), k = p - base;
-                        const int32_t p0 = __shfl_sync(0xFFFFFFFFu, cur, k & 31u), p1 = __shfl_sync(0xFFFFFFFFu, ahead, k & 31u);
-                        const uint32_t page = (uint32_t)(k < 32u ? p0 : p1);
-                        slot[e] = t < want && (!NEAR || t >= run_low) && page < a.b.n_pages ? page * a.b.page_tokens + (t - p * a.b.page_tokens) : 0xFFFFFFFFu;
-                    }
-                    fetch(slot, h);
-                }
-                bits |= label_read_status(label, owner);
-                base += 32u;
-                ask(ahead);
-                bits |= label_read_status(label, owner);
-            } else {
-                // lane l looks up tokens l and l + 32: entries are fetched one tile ahead, labels judged a tile later
-                int32_t next[2] = {-1, -1}, label[2] = {GIFT_OWNER_PARAM, GIFT_OWNER_PARAM};
-#pragma unroll 1
-                for (uint32_t j = 0; ok && j <= n_tiles; j++) {
-                    uint32_t slot[2];
-#pragma unroll
-                    for (int e = 0; e < 2; e++) {
-                        const uint32_t t_next = begin_t + j * TC8_TILE + e * 32 + lane, t = t_next - TC8_TILE;
-                        bits |= label_read_status(label[e], owner);
-                        label[e] = GIFT_OWNER_PARAM;
-                        slot[e] = 0xFFFFFFFFu;
-                        if (j > 0 && t < want && (!NEAR || t >= low)) {
-                            if ((uint32_t)next[e] < a.b.n_pages) {
-                                slot[e] = (uint32_t)next[e] * a.b.page_tokens + (t - a.b.page.quot(t) * a.b.page_tokens);
-                                if (a.owner_map) label[e] = a.owner_map[next[e]];
-                            } else {
-                                bits |= GIFT_ST_BAD_DESC;
-                            }
-                        }
-                        next[e] = j < n_tiles && t_next < want && (!NEAR || t_next >= low) ? table[a.b.page.quot(t_next)] : -1;
-                    }
-                    if (j > 0) fetch(slot, h);
-                }
-                bits |= label_read_status(label[0], owner) | label_read_status(label[1], owner);
-            }
-            bits = __reduce_or_sync(0xFFFFFFFFu, bits);
-            if (lane == 0) {
-                if (bits) atomicOr(&sh.bits[piece % TC8_BITS_RING], bits);
-                bar_arrive(&sh.judged[kv][piece % TC8_BITS_RING]);
-            }
-            piece++;
-        }
-        // the copies under way end before the CTA does, whether or not anybody is left to wait for them
+        // the copies and products under way end before the CTA does, whether or not anybody is left to wait for them
         cp_commit();
         cp_wait<0>();
         for (uint32_t k = fetched > TC8_AHEAD ? fetched - TC8_AHEAD : 0; k < fetched; k++) bar_drain(&sh.fetched[kv][k % TC8_AHEAD], (k / TC8_AHEAD) & 1u);
+        if (q_loads > 0) bar_drain(&sh.q_full, (q_loads - 1) & 1u);
+        // nothing may be in flight when the tensor memory is given back (the lane that issued products commits them)
+        if (elect_one()) mma_commit(&sh.last);
+        __syncwarp();
+        bar_drain(&sh.last, 0);
     } else {
         // ------------------------------------------------------------------ softmax
         const uint32_t row = threadIdx.x, lane_base = (warp * 32u) << 16;

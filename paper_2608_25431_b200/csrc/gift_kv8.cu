@@ -68,7 +68,7 @@ struct WriteArgs {
     FixedDiv page;
     const void *q_norm, *k_norm;
     float eps, inv_dim;
-    uint32_t n_freq, pairs;
+    uint32_t n_freq;
     uint32_t ends[GIFT_MAX_AXES];            // first pair of the next axis
     const float* freq;
     const int32_t* pos;
@@ -91,10 +91,51 @@ struct Lane {
     bool holds[2], turns[2];                 // per quad
 };
 
-// The rounds [first, last) of one kind of head: KIND 0 q, 1 k, 2 v.
-template <class T, bool POOL8, int L, int KIND>
+// Two 32-bit elements at a time.
+struct Two { uint64_t v; };
+__device__ __forceinline__ Two two(float lo, float hi)
+{
+    Two r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ float2 apart(Two a)
+{
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(a.v));
+    return r;
+}
+__device__ __forceinline__ Two mul(Two a, Two b)
+{
+    Two r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
+}
+__device__ __forceinline__ Two fma(Two a, Two b, Two c)
+{
+    Two r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+    return r;
+}
+// The larger magnitude; NaN if either is.
+__device__ __forceinline__ float top_of(float a, float b)
+{
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(fabsf(a)), "f"(fabsf(b)));
+    return r;
+}
+template <class T> __device__ __forceinline__ Two unpack_two(uint32_t x)
+{
+    const float2 f = unpack2<T>(x);
+    return two(f.x, f.y);
+}
+
+// The rounds [first, last) of one kind of head: KIND 0 q, 1 k, 2 v.  PAIRED: neighbours turn against one another.
+// A head's norm is a factor of all its elements, so it waits: for q until the end, while K's codes do not change by it, only
+// their scale does.
+template <class T, bool POOL8, int L, bool PAIRED, int KIND>
 __device__ __forceinline__ void write_heads(const WriteArgs& a, const Lane& own, uint32_t t, char* token, uint32_t first, uint32_t last,
-                                            const float2 (&angle)[8])
+                                            const Two (&cosines)[4], const Two (&sines)[4])
 {
     constexpr uint32_t GROUPS = 32 / L;
     constexpr bool CODES = POOL8 && KIND != 0;
@@ -106,11 +147,14 @@ __device__ __forceinline__ void write_heads(const WriteArgs& a, const Lane& own,
 #pragma unroll
     for (int x = 0; x < 4; x++) at[x] = KIND == 2 ? 16 * j + 4 * x : own.at[x];
     const bool holds[2] = {KIND == 2 ? 16 * j < a.dim : own.holds[0], KIND == 2 ? 16 * j + 8 < a.dim : own.holds[1]};
-    uint2 weight[4];
-    if (norm)
+    Two weight[4][2];
+    if (KIND != 2 && norm)
 #pragma unroll
-        for (int x = 0; x < 4; x++)
-            weight[x] = holds[x >> 1] ? *reinterpret_cast<const uint2*>(static_cast<const char*>(norm) + at[x] * 2) : make_uint2(0u, 0u);
+        for (int x = 0; x < 4; x++) {
+            const uint2 w = holds[x >> 1] ? *reinterpret_cast<const uint2*>(static_cast<const char*>(norm) + at[x] * 2) : make_uint2(0u, 0u);
+            weight[x][0] = unpack_two<T>(w.x);
+            weight[x][1] = unpack_two<T>(w.y);
+        }
     const char* from = KIND == 0 ? a.q + t * a.q_row : KIND == 1 ? a.k + t * a.k_row : a.v + t * a.v_row;
     const uint64_t head_bytes = KIND == 0 ? a.q_head : KIND == 1 ? a.k_head : a.v_head;
 #pragma unroll 1
@@ -139,67 +183,97 @@ __device__ __forceinline__ void write_heads(const WriteArgs& a, const Lane& own,
                     if (there && holds[x >> 1]) *reinterpret_cast<uint2*>(to + at[x] * 2) = raw[u][x];
                 continue;
             }
-            float e[4][4];
+            Two e[4][2];
 #pragma unroll
             for (int x = 0; x < 4; x++) {
-                const float2 m = unpack2<T>(raw[u][x].x), n = unpack2<T>(raw[u][x].y);
-                e[x][0] = m.x; e[x][1] = m.y; e[x][2] = n.x; e[x][3] = n.y;
+                e[x][0] = unpack_two<T>(raw[u][x].x);
+                e[x][1] = unpack_two<T>(raw[u][x].y);
             }
-            if (norm) {
-                float sum = 0.f;
+            float r = 1.f;
+            if (KIND != 2 && norm) {
+                Two sums[2] = {two(0.f, 0.f), two(0.f, 0.f)};
 #pragma unroll
                 for (int x = 0; x < 4; x++)
 #pragma unroll
-                    for (int y = 0; y < 4; y++) sum += e[x][y] * e[x][y];
+                    for (int y = 0; y < 2; y++) sums[y] = fma(e[x][y], e[x][y], sums[y]);
+                const float2 s0 = apart(sums[0]), s1 = apart(sums[1]);
+                float sum = (s0.x + s0.y) + (s1.x + s1.y);
 #pragma unroll
                 for (int d = 1; d < L; d <<= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, d);
-                const float r = rsqrtf(sum * a.inv_dim + a.eps);
+                r = rsqrtf(sum * a.inv_dim + a.eps);
 #pragma unroll
-                for (int x = 0; x < 4; x++) {
-                    const float2 m = unpack2<T>(weight[x].x), n = unpack2<T>(weight[x].y);
-                    e[x][0] *= r * m.x; e[x][1] *= r * m.y; e[x][2] *= r * n.x; e[x][3] *= r * n.y;
-                }
+                for (int x = 0; x < 4; x++)
+#pragma unroll
+                    for (int y = 0; y < 2; y++) e[x][y] = mul(e[x][y], weight[x][y]);
             }
             if (KIND != 2) {
 #pragma unroll
                 for (int x = 0; x < 2; x++)
                     if (own.turns[x]) {
-                        float z[8];
+                        // p: the first elements of 4 pairs, q: the second ones
+                        Two p[2], q[2];
+                        if constexpr (PAIRED) {
 #pragma unroll
-                        for (int i = 0; i < 4; i++) {
-                            // elements i of the two runs, or neighbours
-                            const float2 w = angle[4 * x + i];
-                            const float p = a.pairs ? e[2 * x + i / 2][2 * (i & 1)] : e[2 * x][i];
-                            const float q = a.pairs ? e[2 * x + i / 2][2 * (i & 1) + 1] : e[2 * x + 1][i];
-                            z[i] = p * w.x - q * w.y;
-                            z[4 + i] = q * w.x + p * w.y;
+                            for (int y = 0; y < 2; y++) {
+                                const float2 m = apart(e[2 * x + y][0]), n = apart(e[2 * x + y][1]);
+                                p[y] = two(m.x, n.x);
+                                q[y] = two(m.y, n.y);
+                            }
+                        } else {
+#pragma unroll
+                            for (int y = 0; y < 2; y++) { p[y] = e[2 * x][y]; q[y] = e[2 * x + 1][y]; }
                         }
 #pragma unroll
-                        for (int i = 0; i < 8; i++) e[2 * x + i / 4][i & 3] = a.pairs ? z[(i & 1) * 4 + i / 2] : z[i];
+                        for (int y = 0; y < 2; y++) {
+                            const Two c = cosines[2 * x + y], s = sines[2 * x + y];
+                            Two minus;
+                            minus.v = s.v ^ 0x8000000080000000ull;
+                            const Two u0 = fma(q[y], minus, mul(p[y], c)), v0 = fma(p[y], s, mul(q[y], c));
+                            p[y] = u0;
+                            q[y] = v0;
+                        }
+                        if constexpr (PAIRED) {
+#pragma unroll
+                            for (int y = 0; y < 2; y++) {
+                                const float2 m = apart(p[y]), n = apart(q[y]);
+                                e[2 * x + y][0] = two(m.x, n.x);
+                                e[2 * x + y][1] = two(m.y, n.y);
+                            }
+                        } else {
+#pragma unroll
+                            for (int y = 0; y < 2; y++) { e[2 * x][y] = p[y]; e[2 * x + 1][y] = q[y]; }
+                        }
                     }
             }
             if (!CODES) {
+                const Two r2 = two(r, r);
 #pragma unroll
                 for (int x = 0; x < 4; x++)
                     if (there && holds[x >> 1]) {
+                        const float2 m = apart(norm ? mul(e[x][0], r2) : e[x][0]), n = apart(norm ? mul(e[x][1], r2) : e[x][1]);
                         const bool same = !norm && !own.turns[x >> 1];
-                        *reinterpret_cast<uint2*>(to + at[x] * 2) = same ? raw[u][x] : make_uint2(pack_pair<T>(e[x][0], e[x][1]), pack_pair<T>(e[x][2], e[x][3]));
+                        *reinterpret_cast<uint2*>(to + at[x] * 2) = same ? raw[u][x] : make_uint2(pack_pair<T>(m.x, m.y), pack_pair<T>(n.x, n.y));
                     }
             } else {
-                // as whole numbers the magnitudes of infinities and NaN are above all others
-                uint32_t top = 0u;
+                float top = 0.f;
 #pragma unroll
                 for (int x = 0; x < 4; x++)
 #pragma unroll
-                    for (int y = 0; y < 4; y++) top = max(top, __float_as_uint(e[x][y]) & 0x7FFFFFFFu);
+                    for (int y = 0; y < 2; y++) {
+                        const float2 m = apart(e[x][y]);
+                        top = top_of(top, top_of(m.x, m.y));
+                    }
 #pragma unroll
-                for (int d = 1; d < L; d <<= 1) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
-                const bool fine = top < 0x7F800000u;
+                for (int d = 1; d < L; d <<= 1) top = top_of(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
+                top *= r;
+                const bool fine = top <= 3.402823466e38f;                 // neither infinite nor NaN
                 // 1 / 448 and the reciprocal are off by 2^-24 and 2^-23: as much for a value that lies so near the middle of two codes
-                const float scale = fmaxf(__uint_as_float(top) * (1.f / CODE_MAX), LEAST_SCALE), inv = __frcp_rn(scale);
+                const float scale = fmaxf(top * (1.f / CODE_MAX), LEAST_SCALE), inv = __frcp_rn(scale) * r;
+                const Two inv2 = two(inv, inv);
 #pragma unroll
                 for (int x = 0; x < 4; x++) {
-                    const uint32_t w = floats_to_codes(e[x][0] * inv, e[x][1] * inv) | floats_to_codes(e[x][2] * inv, e[x][3] * inv) << 16;
+                    const float2 m = apart(mul(e[x][0], inv2)), n = apart(mul(e[x][1], inv2));
+                    const uint32_t w = floats_to_codes(m.x, m.y) | floats_to_codes(n.x, n.y) << 16;
                     if (there && holds[x >> 1]) *reinterpret_cast<uint32_t*>(to + at[x]) = fine ? w : 0u;      // 0 * inf is no code
                 }
                 if (there && j == 0) {
@@ -213,7 +287,7 @@ __device__ __forceinline__ void write_heads(const WriteArgs& a, const Lane& own,
     }
 }
 
-template <class T, bool POOL8, int L>
+template <class T, bool POOL8, int L, bool PAIRED>
 __global__ void __launch_bounds__(ROW_THREADS, 2) kv_write_kernel(const __grid_constant__ WriteArgs a)
 {
     const uint32_t lane = threadIdx.x & 31, j = lane % L, group = lane / L;
@@ -224,9 +298,9 @@ __global__ void __launch_bounds__(ROW_THREADS, 2) kv_write_kernel(const __grid_c
         const uint32_t quad = 2 * j + x;
         own.turns[x] = 4 * quad < a.n_freq;
         own.holds[x] = 8 * quad < a.dim;
-        const bool apart = own.turns[x] && !a.pairs;
-        own.at[2 * x] = apart ? 4 * quad : 8 * quad;
-        own.at[2 * x + 1] = apart ? a.n_freq + 4 * quad : 8 * quad + 4;
+        const bool halves = own.turns[x] && !PAIRED;
+        own.at[2 * x] = halves ? 4 * quad : 8 * quad;
+        own.at[2 * x + 1] = halves ? a.n_freq + 4 * quad : 8 * quad + 4;
     }
     for (uint64_t task = blockIdx.x * (ROW_THREADS / 32) + (threadIdx.x >> 5); task < a.tasks; task += n_warps) {
         const uint32_t t = a.parts == 1 ? (uint32_t)task : (uint32_t)(task / a.parts), part = (uint32_t)(task - (uint64_t)t * a.parts);
@@ -241,7 +315,7 @@ __global__ void __launch_bounds__(ROW_THREADS, 2) kv_write_kernel(const __grid_c
         char* token = a.pages + (uint64_t)slot * a.token_bytes;
         const uint32_t r0 = part * a.iters, r1 = r0 + a.iters;
 
-        float2 angle[8];
+        Two cosines[4], sines[4];
         if (a.n_freq && r0 < a.q_rounds + a.kv_rounds) {
             constexpr int OWN = L / 4;                 // angles that a group works out
             float2 mine[OWN];
@@ -253,25 +327,37 @@ __global__ void __launch_bounds__(ROW_THREADS, 2) kv_write_kernel(const __grid_c
                 for (int x = 0; x < (int)GIFT_MAX_AXES - 1; x++) axis += f >= a.ends[x];
                 mine[y] = f < a.n_freq ? turn(a.pos[axis * a.pos_stride + t], a.freq[f]) : make_float2(1.f, 0.f);
             }
+            float c[8], s[8];
 #pragma unroll
             for (int y = 0; y < 8; y++) {
-                angle[y].x = __shfl_sync(0xFFFFFFFFu, mine[y % OWN].x, y / OWN * L + j);
-                angle[y].y = __shfl_sync(0xFFFFFFFFu, mine[y % OWN].y, y / OWN * L + j);
+                c[y] = __shfl_sync(0xFFFFFFFFu, mine[y % OWN].x, y / OWN * L + j);
+                s[y] = __shfl_sync(0xFFFFFFFFu, mine[y % OWN].y, y / OWN * L + j);
+            }
+#pragma unroll
+            for (int y = 0; y < 4; y++) {
+                cosines[y] = two(c[2 * y], c[2 * y + 1]);
+                sines[y] = two(s[2 * y], s[2 * y + 1]);
             }
         }
         const uint32_t k0 = a.q_rounds, v0 = k0 + a.kv_rounds, end = v0 + a.kv_rounds;
-        write_heads<T, POOL8, L, 0>(a, own, t, token, r0, min(r1, k0), angle);
-        write_heads<T, POOL8, L, 1>(a, own, t, token, max(r0, k0) - k0, max(min(r1, v0), k0) - k0, angle);
-        write_heads<T, POOL8, L, 2>(a, own, t, token, max(r0, v0) - v0, max(min(r1, end), v0) - v0, angle);
+        write_heads<T, POOL8, L, PAIRED, 0>(a, own, t, token, r0, min(r1, k0), cosines, sines);
+        write_heads<T, POOL8, L, PAIRED, 1>(a, own, t, token, max(r0, k0) - k0, max(min(r1, v0), k0) - k0, cosines, sines);
+        write_heads<T, POOL8, L, PAIRED, 2>(a, own, t, token, max(r0, v0) - v0, max(min(r1, end), v0) - v0, cosines, sines);
     }
 }
 
-template <class T, bool POOL8>
+template <class T, bool POOL8, bool PAIRED>
 void launch_write(const WriteArgs& a, uint32_t lanes, uint32_t grid, cudaStream_t st)
 {
-    if (lanes == 4) kv_write_kernel<T, POOL8, 4><<<grid, ROW_THREADS, 0, st>>>(a);
-    else if (lanes == 8) kv_write_kernel<T, POOL8, 8><<<grid, ROW_THREADS, 0, st>>>(a);
-    else kv_write_kernel<T, POOL8, 16><<<grid, ROW_THREADS, 0, st>>>(a);
+    if (lanes == 4) kv_write_kernel<T, POOL8, 4, PAIRED><<<grid, ROW_THREADS, 0, st>>>(a);
+    else if (lanes == 8) kv_write_kernel<T, POOL8, 8, PAIRED><<<grid, ROW_THREADS, 0, st>>>(a);
+    else kv_write_kernel<T, POOL8, 16, PAIRED><<<grid, ROW_THREADS, 0, st>>>(a);
+}
+template <class T>
+void launch_write(const WriteArgs& a, bool pool8, bool paired, uint32_t lanes, uint32_t grid, cudaStream_t st)
+{
+    if (pool8) paired ? launch_write<T, true, true>(a, lanes, grid, st) : launch_write<T, true, false>(a, lanes, grid, st);
+    else paired ? launch_write<T, false, true>(a, lanes, grid, st) : launch_write<T, false, false>(a, lanes, grid, st);
 }
 
 // ---------------------------------------------------------------------------
@@ -421,7 +507,7 @@ extern "C" int gift_kv_write(gift_ctx* c, const gift_kv_pool* pool, const gift_k
     a.q_heads = rows->q ? rows->n_heads : 0u; a.kv_heads = pool->n_heads;
     a.page = fixed_div(pool->page_tokens);
     a.q_norm = rows->q_norm; a.k_norm = rows->k_norm; a.eps = rows->eps; a.inv_dim = 1.f / pool->head_dim;
-    a.n_freq = rows->n_freq; a.pairs = rows->flags & GIFT_ROTATE_PAIRS;
+    a.n_freq = rows->n_freq;
     uint32_t end = 0;
     for (uint32_t x = 0; x < GIFT_MAX_AXES; x++) {
         end += x < rows->n_axes && rows->n_freq ? rows->sections[x] : 0u;
@@ -444,8 +530,9 @@ extern "C" int gift_kv_write(gift_ctx* c, const gift_kv_pool* pool, const gift_k
     const uint64_t ctas = (a.tasks + ROW_THREADS / 32 - 1) / (ROW_THREADS / 32), fit = 2ull * c->num_sms;
     const uint32_t grid = (uint32_t)(ctas < fit ? ctas : fit);
     cudaStream_t st = (cudaStream_t)stream;
-    if (rows->dtype == GIFT_BF16) pool8 ? launch_write<__nv_bfloat16, true>(a, lanes, grid, st) : launch_write<__nv_bfloat16, false>(a, lanes, grid, st);
-    else pool8 ? launch_write<__half, true>(a, lanes, grid, st) : launch_write<__half, false>(a, lanes, grid, st);
+    const bool paired = rows->flags & GIFT_ROTATE_PAIRS;
+    if (rows->dtype == GIFT_BF16) launch_write<__nv_bfloat16>(a, pool8, paired, lanes, grid, st);
+    else launch_write<__half>(a, pool8, paired, lanes, grid, st);
     c->launches++;
     CU_TRY(cudaGetLastError());
     return GIFT_OK;

@@ -58,7 +58,7 @@ struct AttnArgs {
     uint32_t tile_rows;              // query rows of an item, at most
     uint32_t least;                  // smallest slice, in tiles
     uint32_t extra;                  // tiles that an item costs beyond its own
-    uint32_t tile_tokens;            // tokens of a tile, where that is not the kernel's own constant
+    uint32_t tile_tokens;            // few rows over codes: tokens of a tile; many rows over codes: step tokens of a tile of query rows
     uint32_t window;                 // tokens that a row may see, its own included; 0: all (kernels with WIN alone look at it)
     uint32_t n_slices, ways;         // slices, and CTAs that share one
     uint32_t wait_tries, wait_ns;    // tcgen05 kernel: further attempts of a wait, and the longest single one

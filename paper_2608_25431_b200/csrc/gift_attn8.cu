@@ -644,6 +644,7 @@ int launch_many8(gift_ctx* c, Attn8Args& a, uint64_t rows, cudaStream_t st)
     a.n_slices = 2u * c->num_sms / a.ways;
     a.tile_rows = TC8_ROWS / a.group * a.group;            // whole tokens
     a.by_tile_rows = fixed_div(a.tile_rows);
+    a.tile_tokens = (uint32_t)TC8_ROWS / a.group;
     a.least = 4;
     a.extra = 8;
     // the kernel takes the maximum before it scales: the scale must be positive

@@ -34,16 +34,6 @@ template <int D> struct Tc8Smem {
     static constexpr uint32_t bytes = codes + 2 * TC8_AHEAD * TC8_TILE * D;
 };
 
-struct Tc8Shared {
-    uint64_t fetched[2][TC8_AHEAD], full[2], judged[2][TC8_BITS_RING];                 // of K, of V
-    uint64_t scaled[4], checked[4], s_full[2], p_full[2], o_done[2], s_done, q_full, q_ready, last;
-    float k_scale[4][TC8_TILE], v_scale[4][TC8_TILE];                                 // by tile
-    uint32_t odd[4][2];              // tokens with a code of NaN in V, by tile
-    uint32_t tmem;
-    uint32_t bits[TC8_BITS_RING];
-    int dead;
-    PlaceShared place;
-};
 
 // One lane of a converged warp, in a way that lets the compiler see that one it is (products issued by it instead of by
 // "lane 0": 612 -> 572 us for trees of up to 64 rows).
@@ -54,11 +44,212 @@ __device__ __forceinline__ bool elect_one()
     return p != 0u;
 }
 
-// A role's walk lies in shared memory: its two dozen words are used at a piece's ends, registers in between.
-template <bool NEAR>
-__device__ __noinline__ bool walk8_next(Walk<TC8_TILE, NEAR>& w, const AttnArgs& a, uint32_t lane)
+// Items, slices and pieces as gift_attn.cuh has them, but an item has the tiles that its rows see: a prompt's early rows
+// stop at their diagonal, and under a window late ones begin behind what they see.  With `ways` 2 the CTAs that share a
+// slice take the two tiles of query rows of a group.  Where a head's tiles are odd in number its last one shares a group with
+// that of the next head, whose own groups come behind it (with nobody beside it: 733 us for trees of up to 64 rows,
+// this way 581).
+__device__ __forceinline__ GroupShape group_shape(const Attn8Args& a, const ReqShape& s)
 {
-    Walk<TC8_TILE, NEAR> x = w;
+    GroupShape p;
+    p.have = s.have; p.want = s.want; p.rows = s.rows;
+    p.per = a.tile_tokens * a.ways;
+    // rows * group fits 31 bits unless the step has more rows than the call, which is refused on the rows alone
+    p.groups = (a.by_tile_rows.cover(s.rows * a.group & 0x7FFFFFFFu) + a.ways - 1u) / a.ways;
+    p.window = a.window;
+    p.tree = a.mask != nullptr;
+    return p;
+}
+
+// Whether heads come in such pairs, and the groups of head h.
+__device__ __forceinline__ bool paired_heads(const Attn8Args& a, const GroupShape& p) { return a.ways == 2u && p.rows > 0 && ((p.rows + a.tile_tokens - 1u) / a.tile_tokens & 1u); }
+__device__ __forceinline__ uint32_t groups_of(const GroupShape& p, bool pairs, uint32_t h) { return pairs && (h & 1u) ? p.groups - 1u : p.groups; }
+
+struct Place8 {
+    uint64_t sums[32];
+    uint32_t r, row0, h, g, u;       // where a slice begins: request, its first row, K/V head, group, units of the item done
+};
+
+// As place_unit: the total of the requests' units and the place of unit w * slice.
+template <int THREADS>
+__device__ bool place_unit8(const Attn8Args& a, uint32_t w, bool first, Place8* sh, uint64_t* total_out, uint64_t* slice_out)
+{
+    const uint32_t n = a.b.n_req, per = (n + THREADS - 1) / THREADS;
+    const uint32_t r0 = threadIdx.x * per, r1 = r0 + per < n ? r0 + per : n;
+    uint64_t rows = 0, units = 0;
+#pragma unroll 1
+    for (uint32_t r = r0; r < r1; r++) {
+        const ReqShape s = load_shape(a.b, r);
+        rows += s.rows;
+        if (s.rows) {
+            const GroupShape p = group_shape(a, s);
+            const uint64_t head = group_units_before(p, p.groups, a.extra);
+            units += paired_heads(a, p) ? (a.kv_heads + 1u) / 2 * head + a.kv_heads / 2 * group_units_before(p, p.groups - 1u, a.extra) : a.kv_heads * head;
+        } else if (first) {
+            a.status[r] = s.ok ? 0u : GIFT_ST_BAD_DESC;
+        }
+    }
+    uint64_t all_rows, total;
+    const uint64_t incl_rows = block_scan<THREADS>(rows, sh->sums, &all_rows);
+    const uint64_t incl = block_scan<THREADS>(units, sh->sums, &total);
+    if (all_rows > a.n_rows) {
+        if (first)
+            for (uint32_t r = threadIdx.x; r < n; r += THREADS) a.status[r] = GIFT_ST_BAD_TABLE;
+        return false;
+    }
+    const uint64_t slice = slice_units(total, a.n_slices, a.least), u = slice * w;
+    *total_out = total;
+    *slice_out = slice;
+    if (u >= total) return false;
+    uint64_t before = incl - units, row = incl_rows - rows;
+    if (u >= before && u < incl) {
+#pragma unroll 1
+        for (uint32_t r = r0; r < r1; r++) {
+            const ReqShape s = load_shape(a.b, r);
+            if (s.rows == 0) continue;
+            const GroupShape p = group_shape(a, s);
+            const bool pairs = paired_heads(a, p);
+            const uint64_t head = group_units_before(p, p.groups, a.extra), two = pairs ? head + group_units_before(p, p.groups - 1u, a.extra) : 2 * head;
+            const uint64_t all = a.kv_heads / 2 * two + a.kv_heads % 2 * head;
+            if (u < before + all) {
+                uint32_t h = 2 * (uint32_t)((u - before) / two);
+                uint64_t off = (u - before) % two;
+                if (off >= head) {
+                    h++;
+                    off -= head;
+                }
+                uint32_t lo = 0, hi = groups_of(p, pairs, h);      // units before lo <= off < units before hi
+                while (hi - lo > 1) {
+                    const uint32_t mid = (lo + hi) >> 1;
+                    if (group_units_before(p, mid, a.extra) <= off) lo = mid; else hi = mid;
+                }
+                sh->r = r; sh->row0 = (uint32_t)row;
+                sh->h = h; sh->g = lo;
+                sh->u = (uint32_t)(off - group_units_before(p, lo, a.extra));
+                break;
+            }
+            before += all;
+            row += s.rows;
+        }
+    }
+    __syncthreads();
+    return true;
+}
+
+struct Tc8Shared {
+    uint64_t fetched[2][TC8_AHEAD], full[2], judged[2][TC8_BITS_RING];                 // of K, of V
+    uint64_t scaled[4], checked[4], s_full[2], p_full[2], o_done[2], s_done, q_full, q_ready, last;
+    float k_scale[4][TC8_TILE], v_scale[4][TC8_TILE];                                 // by tile
+    uint32_t odd[4][2];              // tokens with a code of NaN in V, by tile
+    uint32_t tmem;
+    uint32_t bits[TC8_BITS_RING];
+    int dead;
+    Place8 place;
+};
+
+struct Walk8 {
+    ReqShape s;
+    GroupShape p;
+    uint32_t r, row0;
+    uint32_t way, at, g, u;          // which of the CTAs that share the slice; K/V head, group, its units that are done
+    bool pairs;
+    uint32_t cost;                   // of the group's items
+    uint64_t left;                   // units to go
+    int32_t next_owner, next_have, next_want;              // of request r + 1, fetched ahead
+    // the current piece: K/V head, tile of query rows, first token tile, token tiles, whether it is the item's first or last one
+    uint32_t h, qt, tb, n_tiles, all_q;
+    bool starts, ends;
+
+    __device__ __forceinline__ void fetch(const Attn8Args& a)
+    {
+        const uint32_t k = r + 1 < a.b.n_req ? r + 1 : r;
+        next_owner = a.b.owner[k]; next_have = a.b.have[k]; next_want = a.b.want[k];
+    }
+    __device__ __forceinline__ void start(const Attn8Args& a, const Place8& x, uint32_t which, uint64_t units)
+    {
+        way = which; at = x.h; g = x.g; u = x.u;
+        r = x.r; row0 = x.row0; left = units;
+        s = load_shape(a.b, r);
+        p = group_shape(a, s);
+        pairs = paired_heads(a, p);
+        cost = group_tiles(p, g) + a.extra;
+        fetch(a);
+    }
+    __device__ __forceinline__ bool next(const Attn8Args& a)
+    {
+        while (left > 0) {
+            if (u >= cost) {
+                u = 0;
+                if (++g >= groups_of(p, pairs, at)) {
+                    g = 0;
+                    at += pairs && p.groups == 1u ? 2u : 1u;       // a head with nothing of its own is passed over
+                    if (at >= a.kv_heads) {
+                        at = 0;
+                        do {
+                            row0 += s.rows;
+                            r++;
+                            s = req_shape(next_owner, next_have, next_want, a.b.page, a.b.max_blocks);
+                            fetch(a);
+                        } while (s.rows == 0);
+                        p = group_shape(a, s);
+                        pairs = paired_heads(a, p);
+                    }
+                }
+                cost = group_tiles(p, g) + a.extra;
+            }
+            const uint32_t used = (uint64_t)(cost - u) < left ? cost - u : (uint32_t)left, end = u + used;
+            const uint32_t done = u > a.extra ? u - a.extra : 0u;
+            n_tiles = (end > a.extra ? end - a.extra : 0u) - done;     // none when the units end in the item's extra
+            tb = group_first_tile(p, g) + done;
+            starts = done == 0;
+            ends = end == cost;
+            u = end;
+            left -= used;
+            all_q = s.rows * a.group;
+            h = at;
+            qt = g * a.ways + way;
+            if (pairs && way && g + 1u == p.groups) {              // the next head's last tile of rows, if there is one
+                h = at + 1u;
+                qt--;
+            }
+            if (n_tiles == 0 || h >= a.kv_heads) continue;
+            return true;
+        }
+        return false;
+    }
+    // Whether the piece is the whole item, and the scratch slot of one that is not: a slice's last piece, if
+    // it starts an item, or its first one.
+    __device__ __forceinline__ bool whole() const { return starts && ends; }
+    __device__ __forceinline__ uint32_t slot() const { return blockIdx.x * 2u + (starts ? 1u : 0u); }
+    // One thread, after a piece that is not whole: what the joining kernel needs.  The item goes on in the
+    // slices behind this one.
+    __device__ __forceinline__ void write_head(const Attn8Args& a, uint32_t bits, uint64_t slice) const
+    {
+        PartHead x;
+        x.pieces = starts ? 1u + (uint32_t)((cost - u + slice - 1) / slice) : 0u;
+        x.bits = bits;
+        x.r = r; x.row0 = row0; x.rows_m = s.rows;
+        x.h = h; x.q0 = qt * a.tile_rows;
+        x.nr = all_q - x.q0 < a.tile_rows ? all_q - x.q0 : a.tile_rows;
+        a.part_head[slot()] = x;
+    }
+    // One thread, after a piece that could not be done: nor will any behind it in the slice.
+    __device__ __forceinline__ void note_stall(const Attn8Args& a) const
+    {
+        uint4 x = a.part_stall[blockIdx.x];
+        if (x.y == 0u) { x.x = r; x.z = row0; }
+        x.y = r + 1u;
+        x.w = row0 + s.rows;
+        a.part_stall[blockIdx.x] = x;
+    }
+    // more step tokens than the mask has bits: the request is refused without looking at the mask
+    __device__ __forceinline__ bool masked_short(const Attn8Args& a) const { return a.mask && s.rows > a.mask_words * 32u; }
+};
+
+// A role's walk lies in shared memory: its two dozen words are used at a piece's ends, registers in between.
+static __device__ __noinline__ bool walk8_next(Walk8& w, const Attn8Args& a, uint32_t lane)
+{
+    Walk8 x = w;
     const bool more = x.next(a);
     __syncwarp();
     if (lane == 0) w = x;
@@ -83,7 +274,7 @@ attn8_tc_kernel(const __grid_constant__ Attn8Args a, const __grid_constant__ CUt
     constexpr uint32_t S_COL = 0, O_COL = 2 * TC8_TILE;
     extern __shared__ __align__(1024) char smem[];
     __shared__ __align__(16) Tc8Shared sh;
-    __shared__ Walk<TC8_TILE, NEAR> walks[TC8_THREADS / 32 + 2];       // of the warps, and of the codes that two of them fetch
+    __shared__ Walk8 walks[TC8_THREADS / 32 + 2];       // of the warps, and of the codes that two of them fetch
     using L = Tc8Smem<D>;
 
     join_may_start();
@@ -107,7 +298,7 @@ attn8_tc_kernel(const __grid_constant__ Attn8Args a, const __grid_constant__ CUt
     }
     uint64_t total, slice;
     // ends with a barrier for every thread, taken or not
-    const bool some = place_unit<TC8_THREADS, NEAR>(a, blockIdx.x / a.ways, TC8_TILE, blockIdx.x == 0, &sh.place, &total, &slice);
+    const bool some = place_unit8<TC8_THREADS>(a, blockIdx.x / a.ways, blockIdx.x == 0, &sh.place, &total, &slice);
     if (!some) return;
     if (warp == 6) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sh.tmem)), "r"(TMEM_COLS) : "memory");
@@ -120,10 +311,10 @@ attn8_tc_kernel(const __grid_constant__ Attn8Args a, const __grid_constant__ CUt
     volatile int* dead = &sh.dead;
     const uint64_t begin = slice * (blockIdx.x / a.ways), units = slice < total - begin ? slice : total - begin;
     const uint32_t sm = smem_u32(smem);
-    Walk<TC8_TILE, NEAR>& w = walks[warp];
+    Walk8& w = walks[warp];
     {
-        Walk<TC8_TILE, NEAR> x;
-        x.start(a, sh.place.at, blockIdx.x % a.ways, units);
+        Walk8 x;
+        x.start(a, sh.place, blockIdx.x % a.ways, units);
         if (lane == 0) {
             w = x;
             if (warp >= 6) walks[warp + 2] = x;
@@ -144,7 +335,7 @@ attn8_tc_kernel(const __grid_constant__ Attn8Args a, const __grid_constant__ CUt
         uint32_t n = 0;
         bool ok = true;
         while (ok && walk8_next(w, a, lane)) {
-            const uint32_t n_tiles = w.n_tiles, have = w.s.have, want = w.s.want, tb = w.tb + (NEAR ? w.it.first : 0u);
+            const uint32_t n_tiles = w.n_tiles, have = w.s.have, want = w.s.want, tb = w.tb;
 #pragma unroll 1
             for (uint32_t j = 0; j < n_tiles; j++, n++) {
                 const uint32_t t0 = (tb + j) * TC8_TILE, place = raw + (n % TC8_AHEAD) * (TC8_TILE * D);
@@ -204,7 +395,7 @@ attn8_tc_kernel(const __grid_constant__ Attn8Args a, const __grid_constant__ CUt
         // two tiles later, perhaps of another piece: what is fetched has a walk of its own.
         const uint32_t kv = warp - 6;
         const uint32_t raw = sm + L::codes + kv * (TC8_AHEAD * TC8_TILE * D);
-        Walk<TC8_TILE, NEAR>& f = walks[warp + 2];
+        Walk8& f = walks[warp + 2];
         uint32_t fetched = 0, judged = 0, left = 0;            // tiles so far, pieces judged; tiles of the piece to go
         bool more = true, begun = false;
         uint32_t slot[2] = {0, 0}, slot_head = 0;              // of the next tile's tokens lane and lane + 32; its K/V head
@@ -271,6 +462,16 @@ attn8_tc_kernel(const __grid_constant__ Attn8Args a, const __grid_constant__ CUt
             if ((uint32_t)p >= a.b.n_pages) bits |= GIFT_ST_BAD_DESC;
             else if (a.owner_map) l = a.owner_map[p];
         };
+        // the pages with tokens from lo to hi
+        auto judge_pages = [&](uint32_t lo, uint32_t hi) {
+            if (lo >= hi) return;
+#pragma unroll 4
+            for (uint32_t p = a.b.page.quot(lo) + lane; p * a.b.page_tokens < hi; p += 32) {
+                int32_t l = GIFT_OWNER_PARAM;
+                ask(table[p], true, l);
+                bits |= label_read_status(l, owner);
+            }
+        };
         // The next tile's slots, and its scales.
         auto advance = [&]() {
             if (left == 0) {
@@ -292,12 +493,16 @@ attn8_tc_kernel(const __grid_constant__ Attn8Args a, const __grid_constant__ CUt
                 owner = a.b.owner[f.r];
                 table = a.b.table + (uint64_t)f.r * a.b.max_blocks;
                 want = f.s.want;
-                begin_t = (f.tb + (NEAR ? f.it.first : 0u)) * TC8_TILE;
+                begin_t = f.tb * TC8_TILE;
                 end_t = want - begin_t < left * TC8_TILE ? want : begin_t + left * TC8_TILE;
                 const uint32_t low = NEAR ? first_seen(a, f.s.have) : 0u;
-                from_t = begin_t < low ? low : begin_t;
+                from_t = NEAR && begin_t < low ? low : begin_t;
                 run_low = low & ~(a.copy_run - 1u);
                 bits = f.masked_short(a) ? GIFT_ST_BAD_DESC : 0u;
+                // a request is served or refused as a whole: pages that other rows see and these do not are judged with the
+                // item's first and last piece
+                if (kv == 0 && f.starts) judge_pages(low, begin_t);
+                if (kv == 0 && f.ends) judge_pages(end_t, want);
                 if (a.copy_run >= 8) {
                     base = a.b.page.quot(from_t);
                     page[0] = entry(base + lane);
@@ -463,7 +668,7 @@ attn8_tc_kernel(const __grid_constant__ Attn8Args a, const __grid_constant__ CUt
 #pragma unroll 1
             for (uint32_t j = 0; alive && j < w.n_tiles; j++, n++) {
                 const uint32_t s_at = tmem + lane_base + S_COL + (n & 1u) * TC8_TILE;
-                const uint32_t t0 = (w.tb + (NEAR ? w.it.first : 0u) + j) * TC8_TILE;
+                const uint32_t t0 = (w.tb + j) * TC8_TILE;
                 const bool mixed = t0 + TC8_TILE > w.s.have || (NEAR && a.window && t0 + a.window < w.s.want);
                 uint64_t sees = ~0ull;
                 if (mixed) {
@@ -692,7 +897,7 @@ attn8_tc_kernel(const __grid_constant__ Attn8Args a, const __grid_constant__ CUt
                 }
             }
             if (whole) {
-                if (w.h == 0 && w.qt == 0) write_request<128>(a, w.r, w.row0, w.it.rows_m, bits);
+                if (w.h == 0 && w.qt == 0) write_request<128>(a, w.r, w.row0, w.s.rows, bits);
             } else if (row == 0) {
                 w.write_head(a, bits, slice);
             }

@@ -108,6 +108,54 @@ GIFT_HD uint64_t slice_units(uint64_t total, uint32_t n_cta, uint32_t least)
     return s < least ? least : s;
 }
 
+// Sum of floor((a i + b) / m) for i = 0 .. n - 1, by the Euclidean descent: every round swaps slope and modulus, as counting
+// the lattice points below a line by columns and by rows does.
+GIFT_HD uint64_t floor_sum(uint64_t n, uint64_t m, uint64_t a, uint64_t b)
+{
+    uint64_t sum = 0;
+    while (n > 0) {
+        sum += n * (n - 1) / 2 * (a / m) + n * (b / m);
+        a %= m;
+        b %= m;
+        const uint64_t top = a * n + b;          // the line's height behind the last column
+        if (top < m) break;
+        n = top / m;
+        b = top % m;
+        const uint64_t t = m;
+        m = a;
+        a = t;
+    }
+    return sum;
+}
+
+// The tokens that groups of a request's step rows see, in tiles of 64: group g is the rows [g * per, (g + 1) * per).
+// Without a tree a group's last row bounds it above, a window and its first row below.
+struct GroupShape {
+    uint32_t have, want, rows, per, groups, window;
+    bool tree;
+};
+GIFT_HD uint32_t group_low(const GroupShape& p, uint32_t g)
+{
+    const uint32_t x = p.have + g * p.per;
+    return p.window && x >= p.window ? x - p.window + 1u : 0u;
+}
+GIFT_HD uint32_t group_end(const GroupShape& p, uint32_t g) { return p.tree || g + 1 >= p.groups ? p.want : p.have + (g + 1) * p.per; }
+GIFT_HD uint32_t group_first_tile(const GroupShape& p, uint32_t g) { return group_low(p, g) / 64u; }
+GIFT_HD uint32_t group_tiles(const GroupShape& p, uint32_t g) { return (group_end(p, g) + 63u) / 64u - group_first_tile(p, g); }
+// Tiles of the groups before g (g <= groups), each with `extra` more.
+GIFT_HD uint64_t group_units_before(const GroupShape& p, uint32_t g, uint32_t extra)
+{
+    uint64_t units = (uint64_t)g * extra;
+    const uint64_t last = (p.want + 63u) / 64u, full = g < p.groups ? g : g ? g - 1u : 0u;
+    if (p.tree) units += g * last;
+    else units += floor_sum(full, 64, p.per, (uint64_t)p.have + p.per + 63) + (g == p.groups && g ? last : 0u);
+    if (p.window) {
+        const uint64_t from = p.have >= p.window ? 0u : (p.window - p.have + p.per - 1u) / p.per;      // the first group with a token out of sight
+        if (g > from) units -= floor_sum(g - from, 64, p.per, p.have + from * p.per - p.window + 1u);
+    }
+    return units;
+}
+
 // Host checks shared by the calls that take a gift_batch.
 inline int batch_args_ok(const gift_batch* b)
 {

@@ -231,4 +231,14 @@ int hc_csr_ok(const int32_t* ptr, uint32_t n, uint32_t limit)
     return 1;
 }
 
+// Token tiles of a group of step rows, its first tile, and the units of the groups before it.
+void hc_group(uint32_t have, uint32_t rows, uint32_t per, uint32_t window, int tree, uint32_t extra, uint32_t g, uint64_t out[3])
+{
+    GroupShape p;
+    p.have = have; p.rows = rows; p.want = have + rows; p.per = per; p.groups = (rows + per - 1) / per; p.window = window; p.tree = tree != 0;
+    out[0] = g < p.groups ? group_first_tile(p, g) : 0;
+    out[1] = g < p.groups ? group_tiles(p, g) : 0;
+    out[2] = group_units_before(p, g, extra);
+}
+
 }

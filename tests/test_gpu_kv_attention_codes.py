@@ -286,6 +286,7 @@ def test_first_call_under_a_capture_is_refused():
                 c.kv_attention_codes(b, pool, 1, q, out, st, stream=s.cuda_stream)
             out.zero_()
     assert e.value.code == binding.E_INVAL
+    g.reset()                                              # here and now, not in some later capture
     c.kv_attention_codes(b, pool, 1, q, out, st)
     torch.cuda.synchronize()
     assert not st.any()
@@ -331,3 +332,28 @@ def test_cache_past_4_gib(ctx):
         b = binding.Batch(dev(y["owner"]), dev(y["have"]), dev(y["want"]), dev(np.where(y["table"] >= 0, y["table"] + pages - small, -1)), pt, pages)
         ctx.kv_attention_codes(b, pool, heads, q, out, st)
         assert not st.any() and np.array_equal(out.double().cpu().numpy(), want)
+
+
+@pytest.mark.parametrize("heads", [1, 2, 3, 4])
+@pytest.mark.parametrize("window", [0, 90])
+def test_prompts_of_several_tiles_of_rows(ctx, heads, window):
+    """One, two, three and four tiles of 128 rows to a head, alone and among each other: odd last tiles share their tokens with the next head's."""
+    check(ctx, B.step(30 + heads, HF, [0, 70, 3, 130], [260, 300, 129, 400], heads, 1, 64, 16), window=window)
+    check(ctx, B.step(40 + heads, BF, [0, 200, 9], [65, 20, 97], heads, 4, 128, 24), window=window)
+    check(ctx, B.step(50 + heads, BF, [5], [130], heads, 5, 64, 4), window=window)
+
+
+def test_trees_of_several_tiles_of_rows(ctx):
+    check(ctx, B.step(60, HF, [40, 0], [140, 50], 3, 2, 64, 16, tree=True))
+
+
+@pytest.mark.parametrize("pt", [4, 16])
+def test_a_prompt_is_refused_as_a_whole(ctx, pt):
+    """A bad page that only the last rows see, or, under a window, only the first ones: no row of the request comes out."""
+    for have, window, page in ((0, 0, -1), (300, 100, 201 // pt)):
+        x = B.step(61, BF, [have, 20], [300, 300], 2, 1, 64, pt)
+        last = -(-int(x["want"][0]) // pt) - 1
+        x["label"][x["table"][0, last if page < 0 else page]] = 59
+        out, lse, who, st = call(ctx, x, window=window)
+        assert st.tolist() == [P.OWNER_MISMATCH, 0] and (out[:300] == 0).all() and (lse[:300] == -np.inf).all() and (who[:300] == P.CONFLICT).all()
+        assert np.abs(out[300:]).min(axis=(1, 2)).max() > 0 and (who[300:] == x["owner"][1]).all()

@@ -1,6 +1,8 @@
 """A serving run over the cache in 8 bits, as its calls are meant to follow one another: block tables, slots, rows with norms and
 rotation into labelled pages, attention with capped scores and a window, a tree of drafted tokens, the cache read back, its export
 under the owners' keys and the same attention on the other side; and whole steps in one graph."""
+import gc
+
 import numpy as np
 import pytest
 import torch
@@ -202,6 +204,7 @@ def test_a_captured_step_replays_on_new_lengths(dtype, group_rows):
 
     a, e = sides
     step(e)                                                # nothing to do yet; the context's scratch
+    gc.collect()                                           # no other graph may be destroyed while this one is captured
     graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
     torch.cuda.synchronize()
     with torch.cuda.graph(graph):

@@ -607,7 +607,7 @@ typedef struct {
 int gift_kv_attention(gift_ctx* ctx, const gift_batch* batch, const gift_kv_pool* pool, const gift_attn* attn,
                       uint32_t* status, void* stream);
 
-/* How long a wait inside gift_kv_attention (for a copy, a product, another warp) lasts before it gives up
+/* How long a wait inside gift_kv_attention or gift_kv_attention_codes (for a copy, a product, another warp) lasts before it gives up
  * and the call ends with GIFT_ST_STALLED: about ns nanoseconds, at most GIFT_MAX_WAIT_NS; 0 is the default,
  * some 50 ms to a second.  For the ctx's calls from now on; a captured graph keeps the limit of its
  * capture.  For a caller that would rather have no result than a late one, and for tests of that path. */
@@ -643,7 +643,7 @@ int gift_ctx_wait_limit(gift_ctx* ctx, uint64_t ns);
  * (strides multiples of 8, 16-byte aligned, a head's elements contiguous); likewise v, q and q_out.  q NULL: K and V alone.  dtype is that of
  * all rows (GIFT_BF16 or GIFT_FP16), and of a 16-bit pool.  Labels, slots and status as in gift_kv_append: a
  * row is written to slots[t] if the page's label is row_owner[t], else status[t] says why and nothing of the
- * row is written, q_out neither; nor for slot -1 (status 0).  q_out may be q itself (same strides) and overlaps
+ * row is written, q_out neither; nor for slot -1 (status 0).  The slots of a call must be distinct.  q_out may be q itself (same strides) and overlaps
  * nothing else.  head_dim <= 256, n_freq a multiple of 4, 2 n_freq <= head_dim, n_axes <= GIFT_MAX_AXES, eps >= 0. */
 #define GIFT_MAX_AXES 4u
 #define GIFT_ROTATE_PAIRS 1u

@@ -1,6 +1,7 @@
 // Rows on their way into the labelled pages and out of them: norms of the heads, rotary positions and 8-bit
 // codes in the pass that writes, values in the pass that reads.
 #include <cuda_runtime.h>
+#include <float.h>
 #include <math.h>
 #include <stdint.h>
 #include <string.h>
@@ -16,7 +17,8 @@ namespace {
 
 constexpr int ROW_THREADS = 256;
 constexpr float CODE_MAX = 448.f;                // largest e4m3 number
-constexpr float LEAST_SCALE = 1.17549435e-38f;   // 2^-126: a scale and its reciprocal are normal numbers
+constexpr float LEAST_SCALE = 0x1p-126f;         // a scale and its reciprocal are normal numbers
+constexpr float SUM_MAX = 0x1p120f, SUM_MIN = 0x1p-90f;  // between which a sum of squares is as good as its 32 bits
 constexpr int WRITE_UNROLL = 2;                  // heads that a group of lanes has under way
 
 template <class T> __device__ __forceinline__ float2 unpack2(uint32_t x);
@@ -200,7 +202,30 @@ __device__ __forceinline__ void write_heads(const WriteArgs& a, const Lane& own,
                 float sum = (s0.x + s0.y) + (s1.x + s1.y);
 #pragma unroll
                 for (int d = 1; d < L; d <<= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, d);
-                r = rsqrtf(sum * a.inv_dim + a.eps);
+                float eps = a.eps;
+                // squares that leave 32 bits, or are too small for all of their bits: both are rare, and the head of a power
+                // of two has the same norm
+                const bool large = sum > SUM_MAX, small = sum < SUM_MIN && eps < SUM_MIN;
+                if (__any_sync(0xFFFFFFFFu, large || small)) {
+                    const float f = large ? 0x1p-70f : small ? 0x1p70f : 1.f;
+                    const Two f2 = two(f, f);
+                    float again = 0.f;
+#pragma unroll
+                    for (int x = 0; x < 4; x++)
+#pragma unroll
+                        for (int y = 0; y < 2; y++) {
+                            e[x][y] = mul(e[x][y], f2);
+                            const float2 m = apart(e[x][y]);
+                            again = fmaf(m.x, m.x, fmaf(m.y, m.y, again));
+                        }
+#pragma unroll
+                    for (int d = 1; d < L; d <<= 1) again += __shfl_xor_sync(0xFFFFFFFFu, again, d);
+                    if (large || small) {
+                        sum = again;
+                        eps = eps * f * f;
+                    }
+                }
+                r = rsqrtf(sum * a.inv_dim + eps);
 #pragma unroll
                 for (int x = 0; x < 4; x++)
 #pragma unroll
@@ -266,9 +291,23 @@ __device__ __forceinline__ void write_heads(const WriteArgs& a, const Lane& own,
 #pragma unroll
                 for (int d = 1; d < L; d <<= 1) top = top_of(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
                 top *= r;
-                const bool fine = top <= 3.402823466e38f;                 // neither infinite nor NaN
+                const bool fine = top <= FLT_MAX;                 // neither infinite nor NaN
                 // 1 / 448 and the reciprocal are off by 2^-24 and 2^-23: as much for a value that lies so near the middle of two codes
-                const float scale = fmaxf(top * (1.f / CODE_MAX), LEAST_SCALE), inv = __frcp_rn(scale) * r;
+                const float scale = fmaxf(top * (1.f / CODE_MAX), LEAST_SCALE);
+                float inv = __frcp_rn(scale);
+                if (KIND == 1) {
+                    // a head of zeros, or nearly: the two factors in one leave 32 bits
+                    const float both = inv * r;
+                    const bool far = both > FLT_MAX;
+                    if (__any_sync(0xFFFFFFFFu, far)) {
+                        const Two f2 = far ? two(r, r) : two(1.f, 1.f);
+#pragma unroll
+                        for (int x = 0; x < 4; x++)
+#pragma unroll
+                            for (int y = 0; y < 2; y++) e[x][y] = mul(e[x][y], f2);
+                    }
+                    if (!far) inv = both;
+                }
                 const Two inv2 = two(inv, inv);
 #pragma unroll
                 for (int x = 0; x < 4; x++) {

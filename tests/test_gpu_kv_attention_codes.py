@@ -357,3 +357,49 @@ def test_a_prompt_is_refused_as_a_whole(ctx, pt):
         out, lse, who, st = call(ctx, x, window=window)
         assert st.tolist() == [P.OWNER_MISMATCH, 0] and (out[:300] == 0).all() and (lse[:300] == -np.inf).all() and (who[:300] == P.CONFLICT).all()
         assert np.abs(out[300:]).min(axis=(1, 2)).max() > 0 and (who[300:] == x["owner"][1]).all()
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("new", [1, 3])
+def test_more_heads_to_a_group_than_a_tile_has_rows(ctx, dim, new):
+    check(ctx, B.step(31, BF, [70, 0, 300], [new, new, new], 1, 160, dim, 16))
+
+
+@pytest.mark.parametrize("new", [1, 6, 20])
+@pytest.mark.parametrize("shared", ["rows", "heads", "both"])
+def test_rows_of_q_that_share_memory(ctx, new, shared):
+    x = B.step(32, HF, [50, 9], [new, new], 2, 2, 64, 16)
+    n, heads, dim = x["q"].shape
+    base = x["q"][:1] if shared == "rows" else x["q"][:, :1] if shared == "heads" else x["q"][:1, :1]
+    x["q"] = base.expand(n, heads, dim)
+    q = base.cuda().expand(n, heads, dim)
+    out, st = torch.zeros((n, heads, dim), dtype=HF, device="cuda"), torch.ones(2, dtype=torch.int32, device="cuda")
+    b = binding.Batch(dev(x["owner"]), dev(x["have"]), dev(x["want"]), dev(x["table"]), 16, x["pool"].shape[0])
+    ctx.kv_attention_codes(b, torch.from_numpy(x["pool"]).cuda(), 2, q, out, st, owner_map=dev(x["label"]))
+    torch.cuda.synchronize()
+    bound = B.bounds(x, float(np.float32(dim ** -0.5)), 0.0, 0, None)
+    assert not st.any() and B.worst(out.double().cpu().numpy(), bound["out"], bound["out_tol"]) <= 1
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("new", [2, 14, 30])
+def test_rows_of_q_that_are_not_finite(ctx, dtype, new):
+    """They are NaN, and their neighbours are as good as ever."""
+    x = B.step(33, dtype, [100], [new], 2, 2, 64, 16)
+    bound = B.bounds(x, float(np.float32(64 ** -0.5)), 0.0, 0, None)
+    x["q"][1, 0, 7], x["q"][0, 3, 9] = float("nan"), float("inf")
+    out, lse, _, st = call(ctx, x)
+    fine = np.ones(out.shape[:2], bool)
+    fine[1, 0] = fine[0, 3] = False
+    assert not st.any() and np.isnan(out[~fine]).all() and np.isnan(lse[~fine]).all()
+    assert B.worst(out[fine], bound["out"][fine], bound["out_tol"][fine]) <= 1
+
+
+def test_a_page_twice_in_a_table_and_in_two_requests(ctx):
+    """Tables only say where to read: a page may stand for several stretches of a context."""
+    for new in (1, 14, 30):
+        x = B.step(34, BF, [100, 64], [new, new], 2, 1, 64, 16)
+        x["table"][0, 3] = x["table"][0, 1]
+        x["label"][x["table"][0, 1]] = P.PARAM
+        x["table"][1, 0] = x["table"][0, 1]
+        check(ctx, x)

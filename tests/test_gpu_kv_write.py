@@ -192,6 +192,20 @@ def test_norms_of_heads_that_are_not_finite(ctx):
     assert np.isnan(got[0, 0, 0]).all() and np.isnan(got[1, 0, 1]).all() and np.isnan(got).sum() == 128
 
 
+@pytest.mark.parametrize("bits", [8, 16])
+@pytest.mark.parametrize("heads, q_heads, dim", [(1, 1, 128), (3, 5, 64), (2, 2, 256)])
+def test_norms_of_heads_of_any_size(ctx, bits, heads, q_heads, dim):
+    """Heads of zeros, of numbers whose squares leave 32 bits at either end, next to ordinary ones."""
+    x = make(14, BF, 9, heads, q_heads, dim, 4, bits)
+    for t, f in enumerate((0.0, 2.0 ** 70, 2.0 ** 120, 2.0 ** -70, 2.0 ** -110, 2.0 ** 62, 2.0 ** -52, 2.0 ** -131)):
+        x["k"][t, 0] *= f
+        x["q"][t, -1] *= f
+    check(ctx, x)
+    check(ctx, dict(x, eps=2.0 ** -60))
+    x["q"][0, -1] = x["k"][0, 0] = 2.0 ** -60                 # 0 / 0 is another matter
+    check(ctx, dict(x, eps=0.0))
+
+
 def test_q_in_place_and_another_stream(ctx):
     x = make(12, HF, 40, 2, 4, 128, 16, 8)
     want, pool, _ = call(ctx, x)

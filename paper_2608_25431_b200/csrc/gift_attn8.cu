@@ -368,12 +368,42 @@ __global__ void __launch_bounds__(Few8<D, NR>::threads, Few8<D, NR>::ctas) attn8
                         for (int j = 0; j < 2; j++) {
                             float& y = sc[x][n][2 * e2 + j];
                             y *= ks_vs.x * qs[n][j];
-                            if constexpr (NEAR) {
-                                if (a.cap_out != 0.f) y = a.cap_out * tanh_of(y);
-                                if (a.slopes) y += slope[n][j] * (away[n][j] + (float)(x * 16 + e2 * 8));
-                            }
                         }
                 }
+            }
+            if constexpr (NEAR) {
+                if (a.cap_out != 0.f) {
+                    float far = 0.f;
+#pragma unroll
+                    for (int x = 0; x < MT; x++)
+#pragma unroll
+                        for (int n = 0; n < NR; n++)
+#pragma unroll
+                            for (int e = 0; e < 4; e += 2) far = max3(far, fabsf(sc[x][n][e]), fabsf(sc[x][n][e + 1]));
+                    if (!__any_sync(0xFFFFFFFFu, !(far <= TANH_NEAR))) {
+                        const uint64_t cap2 = pair2(a.cap_out, a.cap_out);
+#pragma unroll
+                        for (int x = 0; x < MT; x++)
+#pragma unroll
+                            for (int n = 0; n < NR; n++)
+#pragma unroll
+                                for (int e = 0; e < 4; e += 2) split2(capped_near(pair2(sc[x][n][e], sc[x][n][e + 1]), cap2), sc[x][n][e], sc[x][n][e + 1]);
+                    } else {
+#pragma unroll
+                        for (int x = 0; x < MT; x++)
+#pragma unroll
+                            for (int n = 0; n < NR; n++)
+#pragma unroll
+                                for (int e = 0; e < 4; e++) sc[x][n][e] = a.cap_out * tanh_of(sc[x][n][e]);
+                    }
+                }
+                if (a.slopes)
+#pragma unroll
+                    for (int x = 0; x < MT; x++)
+#pragma unroll
+                        for (int n = 0; n < NR; n++)
+#pragma unroll
+                            for (int e = 0; e < 4; e++) sc[x][n][e] += slope[n][e & 1] * (away[n][e & 1] + (float)(x * 16 + (e >> 1) * 8));
             }
             uint32_t sees[NR][2];                      // of the step's tokens, by row: bit x is token x * 8 + g
             if (mixed) {

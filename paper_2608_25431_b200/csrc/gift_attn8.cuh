@@ -2,6 +2,7 @@
 #pragma once
 #include "gift_attn.cuh"
 #include "gift_kv8.cuh"
+#include "gift_tc.cuh"
 
 namespace gift {
 
@@ -32,6 +33,26 @@ __device__ __forceinline__ float tanh_of(float u)
     const float far = 1.f - 2.f * fast_rcp(fast_exp2(u * (2.f * LOG2_E)) + 1.f), x = u * u;
     const float near = u * (1.f + x * (-0.33333333f + x * (0.13333333f + x * -0.053968254f)));
     return fabsf(u) < 0.2f ? near : far;
+}
+
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b)
+{
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+// The same for two numbers up to 0.75, times cap: tanh(u) / u as a polynomial of u^2, fitted for the least relative error
+// (3.3e-8; 2^-22.9 with the roundings).  Steps whose scores are all below the border (for a cap of 30, scores up to 22) take it: no
+// exponential and reciprocal, two numbers to an instruction.
+constexpr float TANH_NEAR = 0.75f;
+__device__ __forceinline__ uint64_t capped_near(uint64_t u, uint64_t cap2)
+{
+    constexpr float C[5] = {-4.769490100e-3f, 1.966491342e-2f, -5.339025706e-2f, 1.332652122e-1f, -3.333306909e-1f};
+    const uint64_t x = mul2(u, u);
+    uint64_t p = pair2(C[0], C[0]);
+#pragma unroll
+    for (int i = 1; i < 5; i++) p = fma2(p, x, pair2(C[i], C[i]));
+    return mul2(mul2(u, cap2), fma2(p, x, pair2(1.f, 1.f)));
 }
 
 // Power-of-two factors, made of exponents: a value with exponent field e, or 9 where that is less, becomes one of about

@@ -257,12 +257,6 @@ static __device__ __noinline__ bool walk8_next(Walk8& w, const Attn8Args& a, uin
     return more;
 }
 
-__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b)
-{
-    uint64_t r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
 // Waits until another role's generic writes may be read by the tensor cores' proxy.
 __device__ __forceinline__ void publish_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
@@ -711,10 +705,29 @@ attn8_tc_kernel(const __grid_constant__ Attn8Args a, const __grid_constant__ CUt
                 float by = scale;                          // what the scores still lack
                 if constexpr (NEAR) {
                     if (a.cap_out != 0.f) {
+                        float far[2] = {0.f, 0.f};
 #pragma unroll
                         for (int x = 0; x < 2; x++)
 #pragma unroll
-                            for (int c = 0; c < 32; c++) sc[x][c] = __float_as_uint(a.cap_out * tanh_of(__uint_as_float(sc[x][c]) * scale));
+                            for (int c = 0; c < 32; c += 2)
+                                far[x] = max3(far[x], fabsf(__uint_as_float(sc[x][c])), fabsf(__uint_as_float(sc[x][c + 1])));
+                        if (!__any_sync(0xFFFFFFFFu, !(fmaxf(far[0], far[1]) * scale <= TANH_NEAR))) {
+                            const uint64_t in2 = pair2(scale, scale), cap2 = pair2(a.cap_out, a.cap_out);
+#pragma unroll
+                            for (int x = 0; x < 2; x++)
+#pragma unroll
+                                for (int c = 0; c < 32; c += 2) {
+                                    float lo, hi;
+                                    split2(capped_near(mul2(pair2(__uint_as_float(sc[x][c]), __uint_as_float(sc[x][c + 1])), in2), cap2), lo, hi);
+                                    sc[x][c] = __float_as_uint(lo);
+                                    sc[x][c + 1] = __float_as_uint(hi);
+                                }
+                        } else {
+#pragma unroll
+                            for (int x = 0; x < 2; x++)
+#pragma unroll
+                                for (int c = 0; c < 32; c++) sc[x][c] = __float_as_uint(a.cap_out * tanh_of(__uint_as_float(sc[x][c]) * scale));
+                        }
                         by = 1.f;
                     }
                     if (a.slopes) {

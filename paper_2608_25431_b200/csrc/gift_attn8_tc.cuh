@@ -659,15 +659,17 @@ attn8_tc_kernel(const __grid_constant__ Attn8Args a, const __grid_constant__ CUt
             const float slope = NEAR && a.slopes && there ? a.slopes[hq] * LOG2_E : 0.f;
             float m = NOTHING, l = 0.f;                    // the maximum in use, the sum relative to it
             float most = 0.f, to_half = to_half_range(9u), room = half_range_end(9u);
+            const uint32_t have = w.s.have;
+            uint32_t t0 = w.tb * TC8_TILE, left = w.n_tiles;
+            bool begun = false;
 #pragma unroll 1
-            for (uint32_t j = 0; alive && j < w.n_tiles; j++, n++) {
+            for (; alive && left > 0; left--, n++, t0 += TC8_TILE, begun = true) {
                 const uint32_t s_at = tmem + lane_base + S_COL + (n & 1u) * TC8_TILE;
-                const uint32_t t0 = (w.tb + j) * TC8_TILE;
-                const bool mixed = t0 + TC8_TILE > w.s.have || (NEAR && a.window && t0 + a.window < w.s.want);
+                const bool mixed = t0 + TC8_TILE > have || (NEAR && a.window && t0 + a.window < w.s.want);
                 uint64_t sees = ~0ull;
                 if (mixed) {
-                    sees = there && !masked_short ? row_sees64(a, w.s.have, w.s.want, w.row0 + i, i, t0) : 0ull;
-                    if (NEAR && a.window) sees &= in_window64(a.window, w.s.have + i, t0);
+                    sees = there && !masked_short ? row_sees64(a, have, w.s.want, w.row0 + i, i, t0) : 0ull;
+                    if (NEAR && a.window) sees &= in_window64(a.window, have + i, t0);
                 }
                 // those of tile n + 4 are fetched when V of tile n + 1 is converted, so after P V of tile n
                 if (!warp_wait(&sh.scaled[n & 3u], (n >> 2) & 1u, dead, a) || !warp_wait(&sh.s_full[n & 1u], (n >> 1) & 1u, dead, a)) {
@@ -731,7 +733,7 @@ attn8_tc_kernel(const __grid_constant__ Attn8Args a, const __grid_constant__ CUt
                         by = 1.f;
                     }
                     if (a.slopes) {
-                        const float away = (float)((int32_t)t0 - (int32_t)(w.s.have + i));
+                        const float away = (float)((int32_t)t0 - (int32_t)(have + i));
 #pragma unroll
                         for (int x = 0; x < 2; x++)
 #pragma unroll
@@ -826,7 +828,7 @@ attn8_tc_kernel(const __grid_constant__ Attn8Args a, const __grid_constant__ CUt
                     }
                     tc_st16(s_at + x * 16, pk);
                 }
-                if (j > 0 && __any_sync(0xFFFFFFFFu, ratio != 1.f && there)) {
+                if (begun && __any_sync(0xFFFFFFFFu, ratio != 1.f && there)) {
                     // Every product so far is in O (the one of tile n is not issued before p_full).  That
                     // the barrier is no more than one phase behind follows from S of tile n - 1, whose
                     // product waited for tile n - 3's P V.

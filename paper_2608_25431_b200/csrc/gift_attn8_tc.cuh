@@ -12,6 +12,10 @@
 //              bf16 queries become fp16 in place, by a power of two of the row's own too.
 // A code of NaN in a V whose token is hidden from some row becomes 0, and its weight NaN where the token is seen: what a
 // hidden token holds does not matter.
+// 48 trees of 1 to 64 rows, 4 query heads to one, contexts of up to 16 384 tokens: 518 to 533 us, 400 TFLOP/s of the tiles that have rows; all of
+// 64 rows: 710 us, 585 TFLOP/s; prompt chunks of 300 to 512 tokens, 8 requests: 213 us, capped 277.  What bounds it is a tile's
+// chain through the softmax: of 128 rows and 64 tokens it takes a warp 2 200 to 3 300 clocks, with two such warps on
+// a scheduler; issue slots are 41 % taken, the tensor pipe 29 %, HBM 37 %.
 // Every wait is bounded; a CTA whose wait runs out notes its unfinished requests, and the joining kernel makes them zero.
 #pragma once
 #include "gift_attn8.cuh"
@@ -36,7 +40,7 @@ template <int D> struct Tc8Smem {
 
 
 // One lane of a converged warp, in a way that lets the compiler see that one it is (products issued by it instead of by
-// "lane 0": 612 -> 572 us for trees of up to 64 rows).
+// "lane 0": 612 -> 572 us for trees of up to 64 rows, at the time).
 __device__ __forceinline__ bool elect_one()
 {
     uint32_t p;
@@ -47,8 +51,8 @@ __device__ __forceinline__ bool elect_one()
 // Items, slices and pieces as gift_attn.cuh has them, but an item has the tiles that its rows see: a prompt's early rows
 // stop at their diagonal, and under a window late ones begin behind what they see.  With `ways` 2 the CTAs that share a
 // slice take the two tiles of query rows of a group.  Where a head's tiles are odd in number its last one shares a group with
-// that of the next head, whose own groups come behind it (with nobody beside it: 733 us for trees of up to 64 rows,
-// this way 581).
+// that of the next head, whose own groups come behind it (with nobody beside it 733 us for trees of up to 64 rows,
+// this way 581, at the time).
 __device__ __forceinline__ GroupShape group_shape(const Attn8Args& a, const ReqShape& s)
 {
     GroupShape p;

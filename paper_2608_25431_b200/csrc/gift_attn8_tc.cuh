@@ -12,8 +12,8 @@
 //              bf16 queries become fp16 in place, by a power of two of the row's own too.
 // A code of NaN in a V whose token is hidden from some row becomes 0, and its weight NaN where the token is seen: what a
 // hidden token holds does not matter.
-// 48 trees of 1 to 64 rows, 4 query heads to one, contexts of up to 16 384 tokens: 518 to 533 us, 400 TFLOP/s of the tiles that have rows; all of
-// 64 rows: 710 us, 585 TFLOP/s; prompt chunks of 300 to 512 tokens, 8 requests: 213 us, capped 277.  What bounds it is a tile's
+// 48 trees of 1 to 64 rows, 4 query heads to one, contexts of up to 16 384 tokens: 532 to 564 us, 370 to 392 TFLOP/s of the
+// rows that exist; all of 64 rows: 694 us, 599 TFLOP/s; prompt chunks of 300 to 512 tokens, 8 requests: 202 us, capped 267 to 273.  What bounds it is a tile's
 // chain through the softmax: of 128 rows and 64 tokens it takes a warp 2 200 to 3 300 clocks, with two such warps on
 // a scheduler; issue slots are 41 % taken, the tensor pipe 29 %, HBM 37 %.
 // Every wait is bounded; a CTA whose wait runs out notes its unfinished requests, and the joining kernel makes them zero.
@@ -321,7 +321,7 @@ attn8_tc_kernel(const __grid_constant__ Attn8Args a, const __grid_constant__ CUt
     }
 
     // Of a tile's codes a lane fetches 16 from 16 chunk of every ROWS_AT_ONCE-th token.
-    constexpr int ROW_LANES = D / 16, ROWS_AT_ONCE = 32 / ROW_LANES, LOADS = TC8_TILE / ROWS_AT_ONCE;
+    constexpr int ROW_LANES = D / 16, ROWS_AT_ONCE = 32 / ROW_LANES, LOADS = TC8_TILE / ROWS_AT_ONCE, PARTS = 4;
     const uint32_t chunk = lane % ROW_LANES, sub = lane / ROW_LANES;
     if (warp == 4 || warp == 5) {
         // ------------------------------------------------------------------ codes to fp16
@@ -365,22 +365,26 @@ attn8_tc_kernel(const __grid_constant__ Attn8Args a, const __grid_constant__ CUt
                 // the product with the tile before is complete
                 ok = n == 0 || (kv ? warp_wait(&sh.o_done[(n - 1) & 1u], ((n - 1) >> 1) & 1u, dead, a) : warp_wait(&sh.s_done, (n - 1) & 1u, dead, a));
                 if (!ok) break;
-                // (loaded all at once: it is a chain of latencies otherwise)
-                uint4 x[LOADS];
+                // A part's codes are loaded at once (one by one it is a chain of latencies), but the parts share their instructions: the
+                // roles' loops together are about what the instruction cache holds (whole tiles of rows 710 -> 694 us).
+#pragma unroll 1
+                for (int part = 0; part < PARTS; part++) {
+                    uint4 x[LOADS / PARTS];
 #pragma unroll
-                for (int i = 0; i < LOADS; i++) x[i] = lds128(place + i * 512);
+                    for (int i = 0; i < LOADS / PARTS; i++) x[i] = lds128(place + (part * (LOADS / PARTS) + i) * 512);
 #pragma unroll
-                for (int i = 0; i < LOADS; i++) {
-                    const uint32_t row = i * ROWS_AT_ONCE + sub;
-                    const uint32_t first[2] = {block ? x[i].z : x[i].x, block ? x[i].w : x[i].y}, second[2] = {block ? x[i].x : x[i].z, block ? x[i].y : x[i].w};
-                    const uint32_t at = dst + row * 128 + (((chunk & 3u) * 2 + block ^ (row & 7u)) << 4);
-                    uint32_t f[4];
-                    four_codes(first[0], f[0], f[1]);
-                    four_codes(first[1], f[2], f[3]);
-                    asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(f[0]), "r"(f[1]), "r"(f[2]), "r"(f[3]) : "memory");
-                    four_codes(second[0], f[0], f[1]);
-                    four_codes(second[1], f[2], f[3]);
-                    asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(at ^ 16u), "r"(f[0]), "r"(f[1]), "r"(f[2]), "r"(f[3]) : "memory");
+                    for (int i = 0; i < LOADS / PARTS; i++) {
+                        const uint32_t row = (part * (LOADS / PARTS) + i) * ROWS_AT_ONCE + sub;
+                        const uint32_t first[2] = {block ? x[i].z : x[i].x, block ? x[i].w : x[i].y}, second[2] = {block ? x[i].x : x[i].z, block ? x[i].y : x[i].w};
+                        const uint32_t at = dst + row * 128 + (((chunk & 3u) * 2 + block ^ (row & 7u)) << 4);
+                        uint32_t f[4];
+                        four_codes(first[0], f[0], f[1]);
+                        four_codes(first[1], f[2], f[3]);
+                        asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(f[0]), "r"(f[1]), "r"(f[2]), "r"(f[3]) : "memory");
+                        four_codes(second[0], f[0], f[1]);
+                        four_codes(second[1], f[2], f[3]);
+                        asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(at ^ 16u), "r"(f[0]), "r"(f[1]), "r"(f[2]), "r"(f[3]) : "memory");
+                    }
                 }
                 publish_smem();
                 __syncwarp();

@@ -180,148 +180,148 @@ __device__ __forceinline__ void write_heads(const WriteArgs& a, const Lane& own,
             const bool there = h < heads;
             char* to = KIND == 0 ? a.q_out + t * a.qo_row + h * a.qo_head
                                  : POOL8 ? token + (KIND == 2 ? a.codes : 0u) + h * a.dim : token + ((KIND == 2 ? a.codes : 0u) + h * a.dim) * 2ull;
-            if (KIND == 2 && !POOL8) {
+            if constexpr (KIND == 2 && !POOL8) {
                 // values on their way unchanged keep their bits
 #pragma unroll
                 for (int x = 0; x < 4; x++)
                     if (there && holds[x >> 1]) *reinterpret_cast<uint2*>(to + at[x] * 2) = raw[u][x];
-                continue;
-            }
-            Two e[4][2];
+            } else {
+                Two e[4][2];
 #pragma unroll
-            for (int x = 0; x < 4; x++) {
-                e[x][0] = unpack_two<T>(raw[u][x].x);
-                e[x][1] = unpack_two<T>(raw[u][x].y);
-            }
-            float r = 1.f;
-            if (KIND != 2 && norm) {
-                Two sums[2] = {two(0.f, 0.f), two(0.f, 0.f)};
+                for (int x = 0; x < 4; x++) {
+                    e[x][0] = unpack_two<T>(raw[u][x].x);
+                    e[x][1] = unpack_two<T>(raw[u][x].y);
+                }
+                float r = 1.f;
+                if (KIND != 2 && norm) {
+                    Two sums[2] = {two(0.f, 0.f), two(0.f, 0.f)};
 #pragma unroll
-                for (int x = 0; x < 4; x++)
+                    for (int x = 0; x < 4; x++)
 #pragma unroll
-                    for (int y = 0; y < 2; y++) sums[y] = fma(e[x][y], e[x][y], sums[y]);
-                const float2 s0 = apart(sums[0]), s1 = apart(sums[1]);
-                float sum = (s0.x + s0.y) + (s1.x + s1.y);
+                        for (int y = 0; y < 2; y++) sums[y] = fma(e[x][y], e[x][y], sums[y]);
+                    const float2 s0 = apart(sums[0]), s1 = apart(sums[1]);
+                    float sum = (s0.x + s0.y) + (s1.x + s1.y);
 #pragma unroll
-                for (int d = 1; d < L; d <<= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, d);
-                float eps = a.eps;
-                // squares that leave 32 bits, or are too small for all of their bits: both are rare, and the head of a power
-                // of two has the same norm
-                const bool large = sum > SUM_MAX, small = sum < SUM_MIN && eps < SUM_MIN;
-                if (__any_sync(0xFFFFFFFFu, large || small)) {
-                    const float f = large ? 0x1p-70f : small ? 0x1p70f : 1.f;
-                    const Two f2 = two(f, f);
-                    float again = 0.f;
+                    for (int d = 1; d < L; d <<= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, d);
+                    float eps = a.eps;
+                    // squares that leave 32 bits, or are too small for all of their bits: both are rare, and the head of a power
+                    // of two has the same norm
+                    const bool large = sum > SUM_MAX, small = sum < SUM_MIN && eps < SUM_MIN;
+                    if (__any_sync(0xFFFFFFFFu, large || small)) {
+                        const float f = large ? 0x1p-70f : small ? 0x1p70f : 1.f;
+                        const Two f2 = two(f, f);
+                        float again = 0.f;
+#pragma unroll
+                        for (int x = 0; x < 4; x++)
+#pragma unroll
+                            for (int y = 0; y < 2; y++) {
+                                e[x][y] = mul(e[x][y], f2);
+                                const float2 m = apart(e[x][y]);
+                                again = fmaf(m.x, m.x, fmaf(m.y, m.y, again));
+                            }
+#pragma unroll
+                        for (int d = 1; d < L; d <<= 1) again += __shfl_xor_sync(0xFFFFFFFFu, again, d);
+                        if (large || small) {
+                            sum = again;
+                            eps = eps * f * f;
+                        }
+                    }
+                    r = rsqrtf(sum * a.inv_dim + eps);
+#pragma unroll
+                    for (int x = 0; x < 4; x++)
+#pragma unroll
+                        for (int y = 0; y < 2; y++) e[x][y] = mul(e[x][y], weight[x][y]);
+                }
+                if (KIND != 2) {
+#pragma unroll
+                    for (int x = 0; x < 2; x++)
+                        if (own.turns[x]) {
+                            // p: the first elements of 4 pairs, q: the second ones
+                            Two p[2], q[2];
+                            if constexpr (PAIRED) {
+#pragma unroll
+                                for (int y = 0; y < 2; y++) {
+                                    const float2 m = apart(e[2 * x + y][0]), n = apart(e[2 * x + y][1]);
+                                    p[y] = two(m.x, n.x);
+                                    q[y] = two(m.y, n.y);
+                                }
+                            } else {
+#pragma unroll
+                                for (int y = 0; y < 2; y++) { p[y] = e[2 * x][y]; q[y] = e[2 * x + 1][y]; }
+                            }
+#pragma unroll
+                            for (int y = 0; y < 2; y++) {
+                                const Two c = cosines[2 * x + y], s = sines[2 * x + y];
+                                Two minus;
+                                minus.v = s.v ^ 0x8000000080000000ull;
+                                const Two u0 = fma(q[y], minus, mul(p[y], c)), v0 = fma(p[y], s, mul(q[y], c));
+                                p[y] = u0;
+                                q[y] = v0;
+                            }
+                            if constexpr (PAIRED) {
+#pragma unroll
+                                for (int y = 0; y < 2; y++) {
+                                    const float2 m = apart(p[y]), n = apart(q[y]);
+                                    e[2 * x + y][0] = two(m.x, n.x);
+                                    e[2 * x + y][1] = two(m.y, n.y);
+                                }
+                            } else {
+#pragma unroll
+                                for (int y = 0; y < 2; y++) { e[2 * x][y] = p[y]; e[2 * x + 1][y] = q[y]; }
+                            }
+                        }
+                }
+                if (!CODES) {
+                    const Two r2 = two(r, r);
+#pragma unroll
+                    for (int x = 0; x < 4; x++)
+                        if (there && holds[x >> 1]) {
+                            const float2 m = apart(norm ? mul(e[x][0], r2) : e[x][0]), n = apart(norm ? mul(e[x][1], r2) : e[x][1]);
+                            const bool same = !norm && !own.turns[x >> 1];
+                            *reinterpret_cast<uint2*>(to + at[x] * 2) = same ? raw[u][x] : make_uint2(pack_pair<T>(m.x, m.y), pack_pair<T>(n.x, n.y));
+                        }
+                } else {
+                    float top = 0.f;
 #pragma unroll
                     for (int x = 0; x < 4; x++)
 #pragma unroll
                         for (int y = 0; y < 2; y++) {
-                            e[x][y] = mul(e[x][y], f2);
                             const float2 m = apart(e[x][y]);
-                            again = fmaf(m.x, m.x, fmaf(m.y, m.y, again));
+                            top = top_of(top, top_of(m.x, m.y));
                         }
 #pragma unroll
-                    for (int d = 1; d < L; d <<= 1) again += __shfl_xor_sync(0xFFFFFFFFu, again, d);
-                    if (large || small) {
-                        sum = again;
-                        eps = eps * f * f;
-                    }
-                }
-                r = rsqrtf(sum * a.inv_dim + eps);
+                    for (int d = 1; d < L; d <<= 1) top = top_of(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
+                    top *= r;
+                    const bool fine = top <= FLT_MAX;                 // neither infinite nor NaN
+                    // 1 / 448 and the reciprocal are off by 2^-24 and 2^-23: as much for a value that lies so near the middle of two codes
+                    const float scale = fmaxf(top * (1.f / CODE_MAX), LEAST_SCALE);
+                    float inv = __frcp_rn(scale);
+                    if (KIND == 1) {
+                        // a head of zeros, or nearly: the two factors in one leave 32 bits
+                        const float both = inv * r;
+                        const bool far = both > FLT_MAX;
+                        if (__any_sync(0xFFFFFFFFu, far)) {
+                            const Two f2 = far ? two(r, r) : two(1.f, 1.f);
 #pragma unroll
-                for (int x = 0; x < 4; x++)
+                            for (int x = 0; x < 4; x++)
 #pragma unroll
-                    for (int y = 0; y < 2; y++) e[x][y] = mul(e[x][y], weight[x][y]);
-            }
-            if (KIND != 2) {
-#pragma unroll
-                for (int x = 0; x < 2; x++)
-                    if (own.turns[x]) {
-                        // p: the first elements of 4 pairs, q: the second ones
-                        Two p[2], q[2];
-                        if constexpr (PAIRED) {
-#pragma unroll
-                            for (int y = 0; y < 2; y++) {
-                                const float2 m = apart(e[2 * x + y][0]), n = apart(e[2 * x + y][1]);
-                                p[y] = two(m.x, n.x);
-                                q[y] = two(m.y, n.y);
-                            }
-                        } else {
-#pragma unroll
-                            for (int y = 0; y < 2; y++) { p[y] = e[2 * x][y]; q[y] = e[2 * x + 1][y]; }
+                                for (int y = 0; y < 2; y++) e[x][y] = mul(e[x][y], f2);
                         }
-#pragma unroll
-                        for (int y = 0; y < 2; y++) {
-                            const Two c = cosines[2 * x + y], s = sines[2 * x + y];
-                            Two minus;
-                            minus.v = s.v ^ 0x8000000080000000ull;
-                            const Two u0 = fma(q[y], minus, mul(p[y], c)), v0 = fma(p[y], s, mul(q[y], c));
-                            p[y] = u0;
-                            q[y] = v0;
-                        }
-                        if constexpr (PAIRED) {
-#pragma unroll
-                            for (int y = 0; y < 2; y++) {
-                                const float2 m = apart(p[y]), n = apart(q[y]);
-                                e[2 * x + y][0] = two(m.x, n.x);
-                                e[2 * x + y][1] = two(m.y, n.y);
-                            }
-                        } else {
-#pragma unroll
-                            for (int y = 0; y < 2; y++) { e[2 * x][y] = p[y]; e[2 * x + 1][y] = q[y]; }
-                        }
+                        if (!far) inv = both;
                     }
-            }
-            if (!CODES) {
-                const Two r2 = two(r, r);
+                    const Two inv2 = two(inv, inv);
 #pragma unroll
-                for (int x = 0; x < 4; x++)
-                    if (there && holds[x >> 1]) {
-                        const float2 m = apart(norm ? mul(e[x][0], r2) : e[x][0]), n = apart(norm ? mul(e[x][1], r2) : e[x][1]);
-                        const bool same = !norm && !own.turns[x >> 1];
-                        *reinterpret_cast<uint2*>(to + at[x] * 2) = same ? raw[u][x] : make_uint2(pack_pair<T>(m.x, m.y), pack_pair<T>(n.x, n.y));
+                    for (int x = 0; x < 4; x++) {
+                        const float2 m = apart(mul(e[x][0], inv2)), n = apart(mul(e[x][1], inv2));
+                        const uint32_t w = floats_to_codes(m.x, m.y) | floats_to_codes(n.x, n.y) << 16;
+                        if (there && holds[x >> 1]) *reinterpret_cast<uint32_t*>(to + at[x]) = fine ? w : 0u;      // 0 * inf is no code
                     }
-            } else {
-                float top = 0.f;
-#pragma unroll
-                for (int x = 0; x < 4; x++)
-#pragma unroll
-                    for (int y = 0; y < 2; y++) {
-                        const float2 m = apart(e[x][y]);
-                        top = top_of(top, top_of(m.x, m.y));
+                    if (there && j == 0) {
+                        float* scales = reinterpret_cast<float*>(token + 2ull * a.codes);
+                        scales[2 * h + (KIND == 2 ? 1 : 0)] = fine ? scale : __uint_as_float(0x7FC00000u);
+                        // what lies behind the scales of an odd number of heads
+                        if (KIND == 2 && h + 1 == a.kv_heads && (a.kv_heads & 1u)) scales[2 * h + 2] = scales[2 * h + 3] = 0.f;
                     }
-#pragma unroll
-                for (int d = 1; d < L; d <<= 1) top = top_of(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
-                top *= r;
-                const bool fine = top <= FLT_MAX;                 // neither infinite nor NaN
-                // 1 / 448 and the reciprocal are off by 2^-24 and 2^-23: as much for a value that lies so near the middle of two codes
-                const float scale = fmaxf(top * (1.f / CODE_MAX), LEAST_SCALE);
-                float inv = __frcp_rn(scale);
-                if (KIND == 1) {
-                    // a head of zeros, or nearly: the two factors in one leave 32 bits
-                    const float both = inv * r;
-                    const bool far = both > FLT_MAX;
-                    if (__any_sync(0xFFFFFFFFu, far)) {
-                        const Two f2 = far ? two(r, r) : two(1.f, 1.f);
-#pragma unroll
-                        for (int x = 0; x < 4; x++)
-#pragma unroll
-                            for (int y = 0; y < 2; y++) e[x][y] = mul(e[x][y], f2);
-                    }
-                    if (!far) inv = both;
-                }
-                const Two inv2 = two(inv, inv);
-#pragma unroll
-                for (int x = 0; x < 4; x++) {
-                    const float2 m = apart(mul(e[x][0], inv2)), n = apart(mul(e[x][1], inv2));
-                    const uint32_t w = floats_to_codes(m.x, m.y) | floats_to_codes(n.x, n.y) << 16;
-                    if (there && holds[x >> 1]) *reinterpret_cast<uint32_t*>(to + at[x]) = fine ? w : 0u;      // 0 * inf is no code
-                }
-                if (there && j == 0) {
-                    float* scales = reinterpret_cast<float*>(token + 2ull * a.codes);
-                    scales[2 * h + (KIND == 2 ? 1 : 0)] = fine ? scale : __uint_as_float(0x7FC00000u);
-                    // what lies behind the scales of an odd number of heads
-                    if (KIND == 2 && h + 1 == a.kv_heads && (a.kv_heads & 1u)) scales[2 * h + 2] = scales[2 * h + 3] = 0.f;
                 }
             }
         }

@@ -450,7 +450,7 @@ __global__ void __launch_bounds__(Few8<D, NR>::threads, Few8<D, NR>::ctas) attn8
                     for (int j = 0; j < 2; j++) {
 #pragma unroll
                         for (int d = 4; d < 32; d <<= 1) top[n][j] = fmaxf(top[n][j], __shfl_xor_sync(0xFFFFFFFFu, top[n][j], d));
-                        const float now = fmaxf(m[n][j], top[n][j]);
+                        const float now = top[n][j] > m[n][j] + FEW8_SLACK ? top[n][j] : m[n][j];      // each row by its own
                         alpha[n][j] = fast_exp2(m[n][j] - now);
                         m[n][j] = now;
                         l[n][j] *= alpha[n][j];
@@ -482,6 +482,8 @@ __global__ void __launch_bounds__(Few8<D, NR>::threads, Few8<D, NR>::ctas) attn8
                     for (int j = 0; j < 2; j++) {
 #pragma unroll
                         for (int d = 4; d < 32; d <<= 1) big[n][j] = fmaxf(big[n][j], __shfl_xor_sync(0xFFFFFFFFu, big[n][j], d));
+                        ratio[n][j] = 1.f;
+                        if (alpha[n][j] == 1.f && !(big[n][j] > room[n][j])) continue;
                         most[n][j] = fmaxf(most[n][j] * alpha[n][j], big[n][j]);
                         const uint32_t e = top_exponent(__float_as_uint(most[n][j]));
                         const float f = to_half_range(e);

@@ -68,3 +68,29 @@ def test_rows_of_another_request(ctx, group, new, other, near):
     y["q"][new:] *= 50.0
     got = base.call(ctx, y, **near)
     assert np.array_equal(got[0][:new], want[0][:new]) and np.array_equal(got[1][:new], want[1][:new])
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("requests, have, new", [(2, 90, 3), (2, 90, 14), (2, 90, 60), (50, 700, 3), (50, 700, 8), (50, 700, 14), (12, 700, 30)])
+@pytest.mark.parametrize("softcap", [0.0, 3.0])
+def test_tokens_that_another_row_sees(ctx, dim, requests, have, new, softcap):
+    """A drafted token with a large key and value that its own row alone sees: the other rows are the same, to the bit."""
+    x = B.step(new, HF, [have] * requests, [new] * requests, 2, 1, dim, 16, tree=True)
+    mine = np.arange(requests * new) % new == 1
+    x["mask"][:, 0] &= ~np.uint32(2)
+    x["mask"][mine, 0] |= np.uint32(2)
+    m = 4 * dim
+
+    def louder(x, t, by):
+        for r in range(requests):
+            token = x["pool"][x["table"][r, t // 16], t % 16]
+            token[m:m + 16] = (np.ascontiguousarray(token[m:m + 16]).view("<f4") * np.float32(by)).astype("<f4").view(np.uint8)
+
+    for t in range(have, have + new):                      # some new maxima among the step's own tokens
+        louder(x, t, 1.4)
+    want = base.call(ctx, x, softcap=softcap)
+    y = dict(x, pool=x["pool"].copy())
+    louder(y, have + 1, 60.0)
+    got = base.call(ctx, y, softcap=softcap)
+    assert not np.array_equal(got[0][mine], want[0][mine])
+    assert np.array_equal(got[0][~mine], want[0][~mine]) and np.array_equal(got[1][~mine], want[1][~mine])

@@ -684,7 +684,8 @@ int gift_kv_read(gift_ctx* ctx, const gift_kv_pool* pool, uint32_t dtype, uint32
  * A row at position x (have + i) sees with window > 0 only tokens t > x - window; a page with no token that one of the
  * request's rows may see is neither read nor judged.  slopes (n_heads floats, NULL: none) and window need distances, which
  * drafted trees do not have here: with a tree_mask they are refused.  Scores, softmax and sums are 32-bit; the products
- * take q, codes and the weights p * scale in 16 bits (fp16 of a row's own power of two).  Scratch as for
+ * take q, codes and the weights p * scale in 16 bits (fp16 of a row's own power of two).  Scales of K and queries may be of any size
+ * as long as q . k is below 2^104.  Scratch as for
  * gift_kv_attention, and shared with it. */
 typedef struct {
     gift_attn attn;

@@ -27,6 +27,7 @@ constexpr int TC8_ROWS = 128;
 constexpr int TC8_TILE = 64;
 constexpr int TC8_THREADS = 256;
 constexpr int TC8_AHEAD = 2;             // tiles whose codes are on their way
+constexpr uint32_t SMALL_QUERY = 127u - 16u;     // exponent field of a row's largest element: S * K's scale is 2^24 q . k at most from it on
 constexpr int TC8_BITS_RING = 8;         // pieces whose page verdicts are kept: no warp is more than three ahead of the softmax
 
 template <int D> struct Tc8Smem {
@@ -643,8 +644,12 @@ attn8_tc_kernel(const __grid_constant__ Attn8Args a, const __grid_constant__ CUt
                         for (int y = 0; y < 4; y++) top = max(top, max(word[y] << 16 & 0x7FFFFFFFu, word[y] & 0x7FFF0000u));
                     }
                     const uint32_t e = top_exponent(top);
-                    const float f = to_half_range(e);
-                    scale *= from_half_range(e);
+                    // S meets K's scale before it meets the row's own, and q as large as that would let it leave 32 bits where q is small and
+                    // K large, although q . k is ordinary.  Rows that far from one go to 2^-8, so that S is below 448; what that rounds is
+                    // 2^-17 of the row's largest element.
+                    const bool small = e < SMALL_QUERY;
+                    const float f = to_half_range(e) * (small ? 0x1p-16f : 1.f);
+                    scale *= from_half_range(e) * (small ? 0x1p16f : 1.f);
 #pragma unroll 4
                     for (uint32_t x = 0; x < D / 8; x++) {
                         uint4* at = reinterpret_cast<uint4*>(q + (x >> 3) * (TC8_ROWS * 128) + (((x & 7u) ^ (row & 7u)) << 4));
@@ -663,7 +668,7 @@ attn8_tc_kernel(const __grid_constant__ Attn8Args a, const __grid_constant__ CUt
                 alive = false;
             }
             // the factor is positive (q's sign carries the scale's), and not 0, so that a hidden token's minus infinity stays
-            scale = fmaxf(scale, 1e-37f);
+            scale = fmaxf(scale, __uint_as_float(1u));
             const float slope = NEAR && a.slopes && there ? a.slopes[hq] * LOG2_E : 0.f;
             float m = NOTHING, l = 0.f;                    // the maximum in use, the sum relative to it
             float most = 0.f, to_half = to_half_range(9u), room = half_range_end(9u);

@@ -141,6 +141,24 @@ __device__ __noinline__ void join8(const Attn8Args& a, const PartHead& head, uin
     if (head.h == 0 && head.q0 == 0) write_request<THREADS>(a, head.r, head.row0, head.rows_m, *bits);
 }
 
+// A warp's part of a piece, as it lies in shared memory: its rows' NaN, from its tokens of the piece.
+template <int D, int NR>
+__device__ __noinline__ void put_nan_part(const Attn8Args& a, uint32_t r, uint32_t row0, uint32_t group_of_heads, uint32_t qt, uint32_t tb, uint32_t n_tiles,
+                                          float* parts)
+{
+    using L = Few8<D, NR>;
+    __syncwarp();
+    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
+    const ReqShape s = load_shape(a.b, r);
+    const uint32_t rho = qt * L::rows + lane, i = a.by_group.quot(rho);                // each lane has a row
+    tb += first_seen(a, s.have) / a.tile_tokens;
+#pragma unroll 1
+    for (uint32_t k = 0; k < n_tiles; k++)
+        put_nan<D>(a, r, group_of_heads * a.head_ways + (warp & (a.head_ways - 1u)), s.have, s.want, row0 + i, i,
+                   (tb + k) * a.tile_tokens + warp / a.head_ways * L::tok, L::tok, lane < (uint32_t)L::rows && rho < s.rows * a.group,
+                   parts + (warp * L::rows + lane) * D);
+}
+
 // NEAR: capped scores, a bias by distance or a window.  NR: query rows of an item by 8.
 template <int D, int NR, bool NEAR>
 __global__ void __launch_bounds__(Few8<D, NR>::threads, Few8<D, NR>::ctas) attn8_few_kernel(const __grid_constant__ Attn8Args a)
@@ -315,8 +333,8 @@ __global__ void __launch_bounds__(Few8<D, NR>::threads, Few8<D, NR>::ctas) attn8
             // some rows may not see some of these tokens
             const bool mixed = t0 + TOK > s.have || (NEAR && a.window && t0 + a.window < s.want);
             if (mixed) {
-                // 0 * NaN is NaN: a token whose V holds the code of NaN, hidden from some row perhaps, gets it into its
-                // scale, which is only used where the token is seen
+                // 0 * NaN is NaN: codes of NaN in V, hidden from some row perhaps, become 0, and the rows that see them get
+                // their NaN at the piece's end
                 bool odd = false;
 #pragma unroll
                 for (int i = 0; i < L::half / 512; i++) {
@@ -330,9 +348,8 @@ __global__ void __launch_bounds__(Few8<D, NR>::threads, Few8<D, NR>::ctas) attn8
                         uint32_t x;
                         asm volatile("ld.shared.u32 %0, [%1];" : "=r"(x) : "r"(base + L::half + at) : "memory");
                         if (codes_nan(x)) {
-                            const uint32_t token = at / D;
                             asm volatile("st.shared.u32 [%0], %1;" ::"r"(base + L::half + at), "r"(codes_without_nan(x)) : "memory");
-                            asm volatile("st.shared.u32 [%0], %1;" ::"r"(scales + token * 16u + 4u), "r"(0x7FC00000u) : "memory");
+                            bits |= FOUND_NAN;
                         }
                     }
                     __syncwarp();
@@ -554,7 +571,7 @@ __global__ void __launch_bounds__(Few8<D, NR>::threads, Few8<D, NR>::ctas) attn8
         bits = __reduce_or_sync(0xFFFFFFFFu, bits);
         if (threadIdx.x == 0) s_bits = 0u;
         __syncthreads();                               // the ring is idle; s_ml is complete
-        if (lane == 0 && bits) atomicOr(&s_bits, bits);
+        if (lane == 0 && (bits & ~FOUND_NAN)) atomicOr(&s_bits, bits & ~FOUND_NAN);
         const uint32_t nr = all_q - q0 < (uint32_t)ROWS ? all_q - q0 : (uint32_t)ROWS;
         float* join = reinterpret_cast<float*>(smem) + (uint32_t)warp * (ROWS * D);
 #pragma unroll
@@ -568,6 +585,7 @@ __global__ void __launch_bounds__(Few8<D, NR>::threads, Few8<D, NR>::ctas) attn8
                     for (int np = 0; np < D / 16; np++)
                         *reinterpret_cast<float2*>(join + row * D + np * 16 + 2 * g) = make_float2(o[np][n][j] * unit, o[np][n][2 + j] * unit);
             }
+        if (bits & FOUND_NAN) put_nan_part<D, NR>(a, w.r, w.row0, w.h, w.qt, w.tb, w.n_tiles, reinterpret_cast<float*>(smem));
         __syncthreads();
         bits = s_bits;
         const bool whole = w.whole();

@@ -17,6 +17,7 @@ struct Attn8Args : AttnArgs {
 };
 
 constexpr float LOG2_E = 1.4426950408889634f;
+constexpr uint32_t FOUND_NAN = 1u << 31;  // beside a piece's status bits: codes of NaN in V became 0
 constexpr float NOTHING = -3e38f;        // the maximum before anything is seen: finite, so that no difference with it is NaN
 
 __device__ __forceinline__ float fast_rcp(float x)
@@ -73,6 +74,10 @@ __device__ __forceinline__ uint64_t in_window64(uint32_t window, uint32_t x, uin
     return low - t0 >= 64u ? 0ull : ~0ull << (low - t0);
 }
 
+template <class T> __device__ __forceinline__ T not_a_number();
+template <> __device__ __forceinline__ float not_a_number<float>() { return __uint_as_float(0x7FC00000u); }
+template <> __device__ __forceinline__ uint16_t not_a_number<uint16_t>() { return 0x7FFFu; }             // bf16 and fp16 alike
+
 // Whether a word of four codes holds one that is NaN.
 __device__ __forceinline__ bool codes_nan(uint32_t w) { return (((w & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u) != 0u; }
 // The word with those codes 0.
@@ -80,6 +85,39 @@ __device__ __forceinline__ uint32_t codes_without_nan(uint32_t w)
 {
     const uint32_t bad = ((w & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u;      // one bit a byte
     return w & ~((bad >> 7) * 255u);
+}
+
+// Where tokens may be hidden from some row, codes of NaN in V enter the products as 0.  This gives the rows that see them their NaN, in the
+// columns that have it, when the products are done: `tokens` (32 at most) from t0 of request r, K/V head h, are read again from the pages.  A
+// warp's, each lane with a row of its own (`there`: it has one): the request's i-th, `row` of the step, whose results lie at `to`.
+template <int D, class T>
+static __device__ __noinline__ void put_nan(const Attn8Args& a, uint32_t r, uint32_t h, uint32_t have, uint32_t want, uint32_t row, uint32_t i,
+                                            uint32_t t0, uint32_t tokens, bool there, T* to)
+{
+    const uint32_t lane = threadIdx.x & 31u, t = t0 + lane;
+    const char* codes = a.pages + a.codes + (uint64_t)h * D;
+    bool odd = false;
+    if (lane < tokens && t < want) {
+        const uint32_t b = a.b.page.quot(t), page = (uint32_t)a.b.table[(uint64_t)r * a.b.max_blocks + b];
+        if (page < a.b.n_pages) {
+            codes += ((uint64_t)page * a.b.page_tokens + (t - b * a.b.page_tokens)) * a.token_bytes;
+#pragma unroll 1
+            for (uint32_t c = 0; c < (uint32_t)D; c += 4) odd |= codes_nan(*reinterpret_cast<const uint32_t*>(codes + c));
+        }
+    }
+    uint32_t found = __ballot_sync(0xFFFFFFFFu, odd);
+    if (found == 0u) return;
+    uint32_t sees = there ? (uint32_t)row_sees64(a, have, want, row, i, t0) : 0u;
+    if (a.window) sees &= (uint32_t)in_window64(a.window, have + i, t0);
+#pragma unroll 1
+    for (; found; found &= found - 1u) {
+        const uint32_t k = __ffs(found) - 1;
+        const char* p = reinterpret_cast<const char*>(__shfl_sync(0xFFFFFFFFu, (unsigned long long)codes, k));
+        if (sees >> k & 1u)
+#pragma unroll 1
+            for (uint32_t c = 0; c < (uint32_t)D; c++)
+                if ((p[c] & 0x7F) == 0x7F) to[c] = not_a_number<T>();
+    }
 }
 
 __device__ __forceinline__ void cp_async8(uint32_t dst, const void* src, uint32_t bytes)

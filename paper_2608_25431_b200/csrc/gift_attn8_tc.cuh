@@ -10,8 +10,8 @@
 //   softmax    K's scale multiplies the score, V's the weight, in 32 bits.  Weights go to fp16 by a power of two of the row's
 //              own, which follows the largest p * scale as the maximum follows the scores; O is in its units.
 //              bf16 queries become fp16 in place, by a power of two of the row's own too.
-// A code of NaN in a V whose token is hidden from some row becomes 0, and its weight NaN where the token is seen: what a
-// hidden token holds does not matter.
+// A code of NaN in a V whose token may be hidden from some row becomes 0, and the rows that see the token get their NaN at the piece's end: what
+// a hidden token holds does not matter.
 // 48 trees of 1 to 64 rows, 4 query heads to one, contexts of up to 16 384 tokens: 532 to 564 us, 370 to 392 TFLOP/s of the
 // rows that exist; all of 64 rows: 694 us, 599 TFLOP/s; prompt chunks of 300 to 512 tokens, 8 requests: 202 us, capped 267 to 273.  What bounds it is a tile's
 // chain through the softmax: of 128 rows and 64 tokens it takes a warp 2 200 to 3 300 clocks, with two such warps on
@@ -145,7 +145,6 @@ struct Tc8Shared {
     uint64_t fetched[2][TC8_AHEAD], full[2], judged[2][TC8_BITS_RING];                 // of K, of V
     uint64_t scaled[4], checked[4], s_full[2], p_full[2], o_done[2], s_done, q_full, q_ready, last;
     float k_scale[4][TC8_TILE], v_scale[4][TC8_TILE];                                 // by tile
-    uint32_t odd[4][2];              // tokens with a code of NaN in V, by tile
     uint32_t tmem;
     uint32_t bits[TC8_BITS_RING];
     int dead;
@@ -262,6 +261,24 @@ static __device__ __noinline__ bool walk8_next(Walk8& w, const Attn8Args& a, uin
     return more;
 }
 
+// A softmax warp's rows of a piece whose results are written: their NaN from the tiles that some row does not see all of.
+template <int D>
+static __device__ __noinline__ void put_nan_piece(const Attn8Args& a, const Walk8& w, bool none)
+{
+    const uint32_t row = threadIdx.x, rho = w.qt * a.tile_rows + row;
+    const bool there = rho < w.all_q && row < a.tile_rows && !(w.whole() && none);
+    const uint32_t i = there ? a.by_group.quot(rho) : 0u, hq = w.h * a.group + (there ? rho - i * a.group : 0u);
+    char* whole = a.out + (uint64_t)(w.row0 + i) * a.out_row + (uint64_t)hq * a.out_head;
+    float* part = a.part_o + ((uint64_t)w.slot() * TC8_ROWS + row) * D;
+#pragma unroll 1
+    for (uint32_t x = 0; x < 2 * w.n_tiles; x++) {
+        const uint32_t tile = (w.tb + x / 2) * TC8_TILE, t = tile + x % 2 * 32;
+        if (tile + TC8_TILE <= w.s.have && !(a.window && tile + a.window < w.s.want)) continue;
+        if (w.whole()) put_nan<D>(a, w.r, w.h, w.s.have, w.s.want, w.row0 + i, i, t, 32u, there, reinterpret_cast<uint16_t*>(whole));
+        else put_nan<D>(a, w.r, w.h, w.s.have, w.s.want, w.row0 + i, i, t, 32u, there, part);
+    }
+}
+
 // Waits until another role's generic writes may be read by the tensor cores' proxy.
 __device__ __forceinline__ void publish_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
@@ -331,9 +348,9 @@ attn8_tc_kernel(const __grid_constant__ Attn8Args a, const __grid_constant__ CUt
         // 16 codes are two 16-byte chunks of their row; lanes of the second block of 64 columns begin with the
         // second one, for other banks than those of the first
         const uint32_t block = chunk >> 2, dst = sm + (kv ? L::v : L::k) + block * (TC8_TILE * 128);
-        uint32_t n = 0;
+        uint32_t n = 0, piece = 0;
         bool ok = true;
-        while (ok && walk8_next(w, a, lane)) {
+        for (; ok && walk8_next(w, a, lane); piece++) {
             const uint32_t n_tiles = w.n_tiles, have = w.s.have, want = w.s.want, tb = w.tb;
 #pragma unroll 1
             for (uint32_t j = 0; j < n_tiles; j++, n++) {
@@ -341,27 +358,19 @@ attn8_tc_kernel(const __grid_constant__ Attn8Args a, const __grid_constant__ CUt
                 ok = warp_wait(&sh.fetched[kv][n % TC8_AHEAD], (n / TC8_AHEAD) & 1u, dead, a);
                 if (!ok) break;
                 if (kv) {
-                    uint32_t odd[2] = {0u, 0u};
                     if (t0 + TC8_TILE > have || (NEAR && a.window && t0 + a.window < want)) {
-#pragma unroll 2
+#pragma unroll 1
                         for (int i = 0; i < LOADS; i++) {
                             const uint4 x = lds128(place + i * 512);
                             if (codes_nan(x.x) || codes_nan(x.y) || codes_nan(x.z) || codes_nan(x.w)) {
-                                const uint32_t token = i * ROWS_AT_ONCE + sub;
-                                odd[0] |= token < 32 ? 1u << token : 0u;
-                                odd[1] |= token < 32 ? 0u : 1u << (token - 32);
                                 asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(place + i * 512), "r"(codes_without_nan(x.x)),
                                              "r"(codes_without_nan(x.y)), "r"(codes_without_nan(x.z)), "r"(codes_without_nan(x.w)) : "memory");
+                                atomicOr(&sh.bits[piece % TC8_BITS_RING], FOUND_NAN);
                             }
                         }
-                        odd[0] = __reduce_or_sync(0xFFFFFFFFu, odd[0]);
-                        odd[1] = __reduce_or_sync(0xFFFFFFFFu, odd[1]);
                     }
-                    if (lane == 0) {
-                        sh.odd[n & 3u][0] = odd[0];
-                        sh.odd[n & 3u][1] = odd[1];
-                        bar_arrive(&sh.checked[n & 3u]);
-                    }
+                    __syncwarp();
+                    if (lane == 0) bar_arrive(&sh.checked[n & 3u]);
                 }
                 // the product with the tile before is complete
                 ok = n == 0 || (kv ? warp_wait(&sh.o_done[(n - 1) & 1u], ((n - 1) >> 1) & 1u, dead, a) : warp_wait(&sh.s_done, (n - 1) & 1u, dead, a));
@@ -689,11 +698,7 @@ attn8_tc_kernel(const __grid_constant__ Attn8Args a, const __grid_constant__ CUt
                     alive = false;
                     break;
                 }
-                uint64_t odd = 0ull;
-                if (mixed) {
-                    if (!warp_wait(&sh.checked[n & 3u], (n >> 2) & 1u, dead, a)) { alive = false; break; }
-                    odd = (uint64_t)*(volatile uint32_t*)&sh.odd[n & 3u][0] | (uint64_t)*(volatile uint32_t*)&sh.odd[n & 3u][1] << 32;
-                }
+                if (mixed && !warp_wait(&sh.checked[n & 3u], (n >> 2) & 1u, dead, a)) { alive = false; break; }      // for FOUND_NAN
                 if (!warp_there) {                         // rows that do not exist: whatever P holds stays in them
                     __syncwarp();
                     if (lane == 0) bar_arrive(&sh.p_full[n & 1u]);
@@ -812,14 +817,6 @@ attn8_tc_kernel(const __grid_constant__ Attn8Args a, const __grid_constant__ CUt
 #pragma unroll
                         for (int c = 0; c < 32; c++)
                             if (!((uint32_t)(sees >> (32 * x)) >> c & 1u)) sc[x][c] = 0u;
-                    odd &= sees;
-                    if (odd != 0ull) {
-#pragma unroll
-                        for (int x = 0; x < 2; x++)
-#pragma unroll
-                            for (int c = 0; c < 32; c++)
-                                if ((uint32_t)(odd >> (32 * x)) >> c & 1u) sc[x][c] = 0x7FC00000u;
-                    }
                 }
                 {
                     float lo, hi;
@@ -881,8 +878,10 @@ attn8_tc_kernel(const __grid_constant__ Attn8Args a, const __grid_constant__ CUt
             // product, whatever the other roles come to.  The verdict of the piece before, which all have read
             // by now, makes room.
             alive = !any_softmax(!alive);
-            const uint32_t bits = alive ? *(volatile uint32_t*)&sh.bits[piece % TC8_BITS_RING] : (uint32_t)GIFT_ST_STALLED;
+            uint32_t bits = alive ? *(volatile uint32_t*)&sh.bits[piece % TC8_BITS_RING] : (uint32_t)GIFT_ST_STALLED;
             if (!alive && row == 0) w.note_stall(a);
+            const bool odd = bits & FOUND_NAN;
+            bits &= ~FOUND_NAN;
             if (row == 0) *(volatile uint32_t*)&sh.bits[(piece + TC8_BITS_RING - 1) % TC8_BITS_RING] = 0u;
             const bool whole = w.whole();
             const uint32_t slot = w.slot();
@@ -932,6 +931,7 @@ attn8_tc_kernel(const __grid_constant__ Attn8Args a, const __grid_constant__ CUt
                     else if (a.lse) a.lse[(uint64_t)(w.row0 + i) * a.heads + hq] = none ? NEG_INF : (m + log2f(l)) * 0.6931471805599453f;
                 }
             }
+            if (odd) put_nan_piece<D>(a, w, none);
             if (whole) {
                 if (w.h == 0 && w.qt == 0) write_request<128>(a, w.r, w.row0, w.s.rows, bits);
             } else if (row == 0) {

@@ -637,7 +637,8 @@ int gift_ctx_wait_limit(gift_ctx* ctx, uint64_t ns);
  *             position on axis 0, pos[t], the next sections[1] by that on axis 1, pos[pos_stride + t], and so on
  *             (time, height, width of an image's or video's rows); the sections of the n_axes axes add up to n_freq.
  *   8 bits    of K (normed and turned) and V: scale = max(max |x| / 448, 2^-126) over a head's elements, code = the
- *             e4m3 number nearest to x / scale.  A head that holds an infinity or NaN reads back as NaN throughout:
+ *             e4m3 number nearest to x / scale; within 2^-22 of the middle of two codes, what the quotients' 32 bits round
+ *             away, it may be either.  A head that holds an infinity or NaN reads back as NaN throughout:
  *             scale NaN, codes 0.
  * All in 32 bits, rounded once.  Row t, head h of k starts at k + t*k_row_stride + h*k_head_stride elements of dtype
  * (strides multiples of 8, 16-byte aligned, a head's elements contiguous); likewise v, q and q_out.  q NULL: K and V alone.  dtype is that of
@@ -670,7 +671,7 @@ int gift_kv_write(gift_ctx* ctx, const gift_kv_pool* pool, const gift_kv_rows* r
                   const int32_t* row_owner, uint32_t* status, void* stream);
 
 /* The way back: row t of k and v (in dtype, GIFT_BF16 or GIFT_FP16, that of a 16-bit pool; strides as above) receives the values in
- * slots[t], code * scale rounded once, if the page's label is row_owner[t] or GIFT_OWNER_PARAM (a shared
+ * slots[t], code * scale in 32 bits, then rounded to dtype, if the page's label is row_owner[t] or GIFT_OWNER_PARAM (a shared
  * prefix).  Else the row is zero and status[t] is GIFT_ST_OWNER_MISMATCH, GIFT_ST_UNOWNED or GIFT_ST_BAD_DESC (slot out of range).  Slot -1: the
  * row is left as it was, status 0.  gift_slot_map gives the slots: with have 0 those of whole requests.  k and v
  * overlap neither each other nor the pages. */

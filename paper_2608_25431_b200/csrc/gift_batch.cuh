@@ -108,24 +108,17 @@ GIFT_HD uint64_t slice_units(uint64_t total, uint32_t n_cta, uint32_t least)
     return s < least ? least : s;
 }
 
-// Sum of floor((a i + b) / m) for i = 0 .. n - 1, by the Euclidean descent: every round swaps slope and modulus, as counting
-// the lattice points below a line by columns and by rows does.
-GIFT_HD uint64_t floor_sum(uint64_t n, uint64_t m, uint64_t a, uint64_t b)
+// Whole tiles of 64 below a i + b, summed over i = 0 .. n - 1: the numbers' own sum less what each is above a multiple of 64.  With `step` the
+// largest power of two that divides both a and 64, the residues come back after 64 / step numbers, having been every one that is b's
+// modulo step; what is left of n after whole rounds is added up (none for groups of 1 and 2 heads, whose a is a multiple of 64).
+GIFT_HD uint64_t tiles_below(uint64_t n, uint32_t a, uint64_t b)
 {
-    uint64_t sum = 0;
-    while (n > 0) {
-        sum += n * (n - 1) / 2 * (a / m) + n * (b / m);
-        a %= m;
-        b %= m;
-        const uint64_t top = a * n + b;          // the line's height behind the last column
-        if (top < m) break;
-        n = top / m;
-        b = top % m;
-        const uint64_t t = m;
-        m = a;
-        a = t;
-    }
-    return sum;
+    const uint32_t step = a % 64u ? a & (0u - a) : 64u, round = 64u / step;
+    const uint32_t one = (uint32_t)(b % step) * round + 32u * (round - 1u);        // of a round: step * (0 + 1 + ... + round - 1) and round times b % step
+    uint64_t above = n / round * one;
+    uint32_t x = (uint32_t)b;
+    for (uint32_t left = (uint32_t)n % round; left > 0; left--, x += a) above += x % 64u;
+    return (a * (n * (n - 1) / 2) + b * n - above) / 64u;
 }
 
 // The tokens that groups of a request's step rows see, in tiles of 64: group g is the rows [g * per, (g + 1) * per).
@@ -148,10 +141,10 @@ GIFT_HD uint64_t group_units_before(const GroupShape& p, uint32_t g, uint32_t ex
     uint64_t units = (uint64_t)g * extra;
     const uint64_t last = (p.want + 63u) / 64u, full = g < p.groups ? g : g ? g - 1u : 0u;
     if (p.tree) units += g * last;
-    else units += floor_sum(full, 64, p.per, (uint64_t)p.have + p.per + 63) + (g == p.groups && g ? last : 0u);
+    else units += tiles_below(full, p.per, (uint64_t)p.have + p.per + 63) + (g == p.groups && g ? last : 0u);
     if (p.window) {
         const uint64_t from = p.have >= p.window ? 0u : (p.window - p.have + p.per - 1u) / p.per;      // the first group with a token out of sight
-        if (g > from) units -= floor_sum(g - from, 64, p.per, p.have + from * p.per - p.window + 1u);
+        if (g > from) units -= tiles_below(g - from, p.per, p.have + from * p.per - p.window + 1u);
     }
     return units;
 }

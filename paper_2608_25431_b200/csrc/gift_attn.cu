@@ -34,6 +34,7 @@ namespace {
 
 constexpr int FEW_WARPS = 4;
 constexpr int FEW_THREADS = FEW_WARPS * 32;
+static_assert(FEW_THREADS == JOIN_THREADS, "the last CTA of a cut item joins it");
 constexpr int FEW_ROWS = 16;
 constexpr int FEW_STAGES = 3;
 template <int D> constexpr int FEW_BLOCKS = 128 / D;                     // 16-token blocks of a warp's step

@@ -31,11 +31,11 @@ struct JoinShared {
 };
 
 // 16 rows from row_lo of the item that begins in slice w: the item is that slice's last piece and goes on
-// as the first piece of w + 1, w + 2, ...  Called by THREADS threads, at least 128.  LIVE: the pieces may have been written
+// as the first piece of w + 1, w + 2, ...  Called by JOIN_THREADS threads.  LIVE: the pieces may have been written
 // while this kernel runs, and are read past L1.
 template <bool LIVE, class V> __device__ __forceinline__ V load_part(const V* p) { return LIVE ? __ldcg(p) : *p; }
 
-template <class T, int D, int ROWS, bool LIVE, int THREADS = JOIN_THREADS>
+template <class T, int D, int ROWS, bool LIVE>
 __device__ __forceinline__ void join_rows(const AttnArgs& a, const PartHead& head, uint32_t w, uint32_t way, uint32_t row_lo, JoinShared* sh)
 {
     constexpr int CH = D / 8;
@@ -44,7 +44,7 @@ __device__ __forceinline__ void join_rows(const AttnArgs& a, const PartHead& hea
     auto slot_of = [&](uint32_t p) -> uint64_t { return 2ull * ((w + p) * a.ways + way) + (p == 0 ? 1 : 0); };
     if (threadIdx.x == 0) sh->bits = 0u;
     __syncthreads();
-    for (uint32_t p = threadIdx.x; p < pieces; p += THREADS) {
+    for (uint32_t p = threadIdx.x; p < pieces; p += JOIN_THREADS) {
         const uint32_t bits = load_part<LIVE>(&a.part_head[slot_of(p)].bits);
         if (bits) atomicOr(&sh->bits, bits);
     }
@@ -70,7 +70,7 @@ __device__ __forceinline__ void join_rows(const AttnArgs& a, const PartHead& hea
     }
     __syncthreads();
     const uint32_t bits = sh->bits;
-    for (uint32_t c = threadIdx.x; c < nr * (uint32_t)CH; c += THREADS) {
+    for (uint32_t c = threadIdx.x; c < nr * (uint32_t)CH; c += JOIN_THREADS) {
         const uint32_t row = c / CH, ch = c % CH;
         const float top = sh->top[row].x, sum = sh->top[row].y, use = top == NEG_INF ? 0.f : top;
         float acc[8];
@@ -96,14 +96,14 @@ __device__ __forceinline__ void join_rows(const AttnArgs& a, const PartHead& hea
         *reinterpret_cast<uint4*>(a.out + (uint64_t)(row0 + i) * a.out_row + (uint64_t)hq * a.out_head + ch * 16) = v;
         if (a.lse && ch == 0) a.lse[(uint64_t)(row0 + i) * a.heads + hq] = none ? NEG_INF : (top + log2f(sum)) * 0.6931471805599453f;
     }
-    if (h == 0 && q0 == 0) write_request<THREADS>(a, r, row0, head.rows_m, bits);
+    if (h == 0 && q0 == 0) write_request<JOIN_THREADS>(a, r, row0, head.rows_m, bits);
 }
 
 // The same from within the attention kernel, kept out of its loops' code.
-template <class T, int D, int ROWS, int THREADS = JOIN_THREADS>
+template <class T, int D, int ROWS>
 __device__ __noinline__ void join_here(const AttnArgs& a, const PartHead& head, uint32_t w, JoinShared* sh)
 {
-    join_rows<T, D, ROWS, true, THREADS>(a, head, w, 0, 0, sh);
+    join_rows<T, D, ROWS, true>(a, head, w, 0, 0, sh);
 }
 
 // At the end of every CTA of the few-row kernel, when it takes no more tickets: the call's last CTA makes all
@@ -156,17 +156,17 @@ __device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], 
 
 // What a wait that ran out leaves: a CTA knows of its own pieces only, so the requests that it could not
 // finish become zero here, when all of the rows' writers are done, by all CTAs of the joining kernel.
-template <int D, int THREADS = JOIN_THREADS>
+template <int D>
 __device__ __noinline__ void clear_stalled(const AttnArgs& a, uint32_t cta, uint32_t n_cta)
 {
     constexpr uint32_t CH = D / 8;
 #pragma unroll 1
     for (uint32_t k = 0; k < a.n_slices * a.ways; k++) {
         const uint4 s = __ldcg(a.part_stall + k);
-        for (uint32_t r = s.x + cta * THREADS + threadIdx.x; r < s.y; r += n_cta * THREADS)
+        for (uint32_t r = s.x + cta * JOIN_THREADS + threadIdx.x; r < s.y; r += n_cta * JOIN_THREADS)
             if (load_shape(a.b, r).rows) a.status[r] = GIFT_ST_STALLED;
         for (uint32_t t = s.z + cta; t < s.w; t += n_cta) {
-            for (uint32_t c = threadIdx.x; c < a.heads * CH; c += THREADS) {
+            for (uint32_t c = threadIdx.x; c < a.heads * CH; c += JOIN_THREADS) {
                 const uint32_t hq = c / CH, ch = c % CH;
                 *reinterpret_cast<uint4*>(a.out + (uint64_t)t * a.out_row + (uint64_t)hq * a.out_head + ch * 16) = make_uint4(0u, 0u, 0u, 0u);
                 if (a.lse && ch == 0) a.lse[(uint64_t)t * a.heads + hq] = NEG_INF;

@@ -393,6 +393,40 @@ __global__ void __launch_bounds__(Few8<D, NR>::threads, Few8<D, NR>::ctas) attn8
                         }
                 }
             }
+            if constexpr (NEAR) {
+                if (a.cap_out != 0.f) {
+                    float far = 0.f;
+#pragma unroll
+                    for (int x = 0; x < MT; x++)
+#pragma unroll
+                        for (int n = 0; n < NR; n++)
+#pragma unroll
+                            for (int e = 0; e < 4; e += 2) far = max3(far, fabsf(sc[x][n][e]), fabsf(sc[x][n][e + 1]));
+                    if (__any_sync(0xFFFFFFFFu, !(far <= TANH_NEAR))) {
+#pragma unroll
+                        for (int x = 0; x < MT; x++)
+#pragma unroll
+                            for (int n = 0; n < NR; n++)
+#pragma unroll
+                                for (int e = 0; e < 4; e++) sc[x][n][e] = capped(sc[x][n][e], a.cap_out);
+                    } else {
+                        const uint64_t cap2 = pair2(a.cap_out, a.cap_out);
+#pragma unroll
+                        for (int x = 0; x < MT; x++)
+#pragma unroll
+                            for (int n = 0; n < NR; n++)
+#pragma unroll
+                                for (int e = 0; e < 4; e += 2) split2(capped_near(pair2(sc[x][n][e], sc[x][n][e + 1]), cap2), sc[x][n][e], sc[x][n][e + 1]);
+                    }
+                }
+                if (a.slopes)
+#pragma unroll
+                    for (int x = 0; x < MT; x++)
+#pragma unroll
+                        for (int n = 0; n < NR; n++)
+#pragma unroll
+                            for (int e = 0; e < 4; e++) sc[x][n][e] += slope[n][e & 1] * (away[n][e & 1] + (float)(x * 16 + (e >> 1) * 8));
+            }
             uint32_t sees[NR][2];                      // of the step's tokens, by row: bit x is token x * 8 + g
             if (mixed) {
                 const bool none = masked_short || t0 >= s.want;
@@ -403,49 +437,11 @@ __global__ void __launch_bounds__(Few8<D, NR>::threads, Few8<D, NR>::ctas) attn8
                         uint32_t all = none ? 0u : (uint32_t)row_sees64(a, s.have, s.want, row0 + row_i[n][j], row_i[n][j], t0);
                         if (NEAR && a.window) all &= (uint32_t)in_window64(a.window, s.have + row_i[n][j], t0);
                         sees[n][j] = all >> g;
-                    }
-            }
-            auto hide = [&](float score) {
-#pragma unroll
-                for (int n = 0; n < NR; n++)
-#pragma unroll
-                    for (int j = 0; j < 2; j++)
 #pragma unroll
                         for (int x = 0; x < 2 * MT; x++)
-                            if (!(sees[n][j] >> (x * 8) & 1u)) sc[x >> 1][n][2 * (x & 1) + j] = score;
-            };
-            if constexpr (NEAR) {
-                if (a.cap_out != 0.f) {
-                    if (mixed) hide(0.f);              // hidden tokens have no say in which of the two forms a row's others get
-#pragma unroll
-                    for (int n = 0; n < NR; n++)
-#pragma unroll
-                        for (int j = 0; j < 2; j++) {
-                            float far = 0.f;
-#pragma unroll
-                            for (int x = 0; x < MT; x++) far = max3(far, fabsf(sc[x][n][j]), fabsf(sc[x][n][2 + j]));
-                            if (far <= TANH_NEAR) {
-                                const uint64_t cap2 = pair2(a.cap_out, a.cap_out);
-#pragma unroll
-                                for (int x = 0; x < MT; x++) split2(capped_near(pair2(sc[x][n][j], sc[x][n][2 + j]), cap2), sc[x][n][j], sc[x][n][2 + j]);
-                            } else {
-#pragma unroll
-                                for (int x = 0; x < MT; x++) {
-                                    sc[x][n][j] = a.cap_out * tanh_of(sc[x][n][j]);
-                                    sc[x][n][2 + j] = a.cap_out * tanh_of(sc[x][n][2 + j]);
-                                }
-                            }
-                        }
-                }
-                if (a.slopes)
-#pragma unroll
-                    for (int x = 0; x < MT; x++)
-#pragma unroll
-                        for (int n = 0; n < NR; n++)
-#pragma unroll
-                            for (int e = 0; e < 4; e++) sc[x][n][e] += slope[n][e & 1] * (away[n][e & 1] + (float)(x * 16 + (e >> 1) * 8));
+                            if (!(sees[n][j] >> (x * 8) & 1u)) sc[x >> 1][n][2 * (x & 1) + j] = NEG_INF;
+                    }
             }
-            if (mixed) hide(NEG_INF);
             float alpha[NR][2];
             bool grow = false;
             float top[NR][2];

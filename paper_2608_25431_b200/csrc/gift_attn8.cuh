@@ -27,33 +27,39 @@ __device__ __forceinline__ float fast_rcp(float x)
     return y;
 }
 
-// tanh: 1 - 2 / (e^2u + 1), whose error of 2^-23 is absolute, and near 0 the series, whose first term left out is
-// below 6e-8 of the value at the border.
-__device__ __forceinline__ float tanh_of(float u)
-{
-    const float far = 1.f - 2.f * fast_rcp(fast_exp2(u * (2.f * LOG2_E)) + 1.f), x = u * u;
-    const float near = u * (1.f + x * (-0.33333333f + x * (0.13333333f + x * -0.053968254f)));
-    return fabsf(u) < 0.2f ? near : far;
-}
-
 __device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b)
 {
     uint64_t r;
     asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
     return r;
 }
-// The same for two numbers up to 0.75, times cap: tanh(u) / u as a polynomial of u^2, fitted for the least relative error
-// (3.3e-8; 2^-22.9 with the roundings).  Steps whose scores are all below the border (for a cap of 30, scores up to 22) take it: no
-// exponential and reciprocal, two numbers to an instruction.
+// tanh times cap, by two forms.  Up to 0.75: tanh(u) / u as a polynomial of u^2, fitted for the least relative error (3.7e-8 as stored;
+// 2^-22.4 with the roundings).  Above: 1 - 2 / (e^2u + 1), whose error is 2^-21 at most (of the exponential 2^-22 and of the reciprocal 2^-23, both
+// relative).  A number's form depends on itself alone, and so does its value: not on what else is in its step.
 constexpr float TANH_NEAR = 0.75f;
-__device__ __forceinline__ uint64_t capped_near(uint64_t u, uint64_t cap2)
+__device__ __forceinline__ float tanh_c(int i)
 {
     constexpr float C[5] = {-4.769490100e-3f, 1.966491342e-2f, -5.339025706e-2f, 1.332652122e-1f, -3.333306909e-1f};
+    return C[i];
+}
+// Two numbers below the border: steps all of whose numbers are (for a cap of 30, scores up to 22) take this, without exponential and reciprocal.
+__device__ __forceinline__ uint64_t capped_near(uint64_t u, uint64_t cap2)
+{
     const uint64_t x = mul2(u, u);
-    uint64_t p = pair2(C[0], C[0]);
+    uint64_t p = pair2(tanh_c(0), tanh_c(0));
 #pragma unroll
-    for (int i = 1; i < 5; i++) p = fma2(p, x, pair2(C[i], C[i]));
+    for (int i = 1; i < 5; i++) p = fma2(p, x, pair2(tanh_c(i), tanh_c(i)));
     return mul2(mul2(u, cap2), fma2(p, x, pair2(1.f, 1.f)));
+}
+// Any number; below the border to the same bit.
+__device__ __forceinline__ float capped(float u, float cap)
+{
+    const float x = u * u;
+    float p = tanh_c(0);
+#pragma unroll
+    for (int i = 1; i < 5; i++) p = fmaf(p, x, tanh_c(i));
+    const float near = __fmul_rn(__fmul_rn(u, cap), fmaf(p, x, 1.f)), far = cap * (1.f - 2.f * fast_rcp(fast_exp2(u * (2.f * LOG2_E)) + 1.f));
+    return fabsf(u) <= TANH_NEAR ? near : far;
 }
 
 // Power-of-two factors, made of exponents: a value with exponent field e, or 9 where that is less, becomes one of about

@@ -725,21 +725,19 @@ attn8_tc_kernel(const __grid_constant__ Attn8Args a, const __grid_constant__ CUt
                 float by = scale;                          // what the scores still lack
                 if constexpr (NEAR) {
                     if (a.cap_out != 0.f) {
-                        // the form is the row's own choice, and its hidden tokens have no say in it
-                        if (mixed) {
-#pragma unroll
-                            for (int x = 0; x < 2; x++)
-#pragma unroll
-                                for (int c = 0; c < 32; c++)
-                                    if (!((uint32_t)(sees >> (32 * x)) >> c & 1u)) sc[x][c] = 0u;
-                        }
                         float far[2] = {0.f, 0.f};
 #pragma unroll
                         for (int x = 0; x < 2; x++)
 #pragma unroll
                             for (int c = 0; c < 32; c += 2)
                                 far[x] = max3(far[x], fabsf(__uint_as_float(sc[x][c])), fabsf(__uint_as_float(sc[x][c + 1])));
-                        if (fmaxf(far[0], far[1]) * scale <= TANH_NEAR) {
+                        if (__any_sync(0xFFFFFFFFu, !(fmaxf(far[0], far[1]) * scale <= TANH_NEAR))) {
+                            const uint64_t in2 = pair2(scale, scale), cap2 = pair2(a.cap_out, a.cap_out);
+#pragma unroll
+                            for (int x = 0; x < 2; x++)
+#pragma unroll
+                                for (int c = 0; c < 32; c++) sc[x][c] = __float_as_uint(capped(__uint_as_float(sc[x][c]) * scale, a.cap_out));
+                        } else {
                             const uint64_t in2 = pair2(scale, scale), cap2 = pair2(a.cap_out, a.cap_out);
 #pragma unroll
                             for (int x = 0; x < 2; x++)
@@ -750,11 +748,6 @@ attn8_tc_kernel(const __grid_constant__ Attn8Args a, const __grid_constant__ CUt
                                     sc[x][c] = __float_as_uint(lo);
                                     sc[x][c + 1] = __float_as_uint(hi);
                                 }
-                        } else {
-#pragma unroll
-                            for (int x = 0; x < 2; x++)
-#pragma unroll
-                                for (int c = 0; c < 32; c++) sc[x][c] = __float_as_uint(a.cap_out * tanh_of(__uint_as_float(sc[x][c]) * scale));
                         }
                         by = 1.f;
                     }

@@ -679,7 +679,8 @@ int gift_kv_read(gift_ctx* ctx, const gift_kv_pool* pool, uint32_t dtype, uint32
                  void* k, uint64_t k_row_stride, uint64_t k_head_stride, void* v, uint64_t v_row_stride, uint64_t v_head_stride,
                  uint32_t* status, void* stream);
 
-/* gift_kv_attention over 8-bit pages (pool->dtype GIFT_E4M3); q and out are of dtype.  All that is said there holds, and
+/* gift_kv_attention over 8-bit pages (pool->dtype GIFT_E4M3); q and out are of dtype.  All that is said there holds (head_dim is
+ * 64 or 128 here too, although rows of other sizes can be written and read), and
  * the score of query head h's row at position x with token t is
  *   s = scale * q . k_t;  softcap > 0: s = softcap * tanh(s / softcap);  slopes: s += slopes[h] * (t - x)
  * A row at position x (have + i) sees with window > 0 only tokens t > x - window; a page with no token that one of the

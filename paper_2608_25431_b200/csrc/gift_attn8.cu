@@ -33,13 +33,14 @@ namespace {
 // rounded.  Both go to fp16 by a power of two of the row's own (see top_exponent), for scales and queries of
 // any size.  The maximum that weights are relative to, and the weights' power of two, change only when a score passes
 // the maximum by 2^6 or a weight leaves fp16: one vote a step in place of reductions over the warp.
-// Measured: a decode step of 64 requests, 32 heads, 120 us, 5.2 TB/s, 79 % of a copy; contexts of up to 131 072 tokens, 4 query heads to
-// one, 124 us; capped, biased, under a window of 1 024, 51 us; trees of 16 rows 590 us, 3.9 TB/s.  With up to 8 rows the
+// Measured: a decode step of 64 requests, 32 heads, 122 us, 5.1 TB/s, 78 % of a copy; 16 requests of up to 32 768 tokens, 4 query heads to
+// one, 126 us; capped, biased, under a window of 1 024, 52 us; trees of 16 rows 594 us, 3.9 TB/s (with heads of 128 such items want more than
+// the 168 registers that 3 CTAs leave: 116 to 156 bytes a thread lie in local memory).  With up to 8 rows the
 // chain of a step bounds it (52 % of the issue slots, 16 warps on an SM), with 16 the same with twice the products.
 
 constexpr int FEW8_STAGES = 3;
-// Items of a call before heads share a CTA.  1, 8, 16, 32, 64, 128: 2 requests with long contexts 131, 131, 131, 126, 145, 172 us; one
-// request of 514 tokens 33 us with 1, 13.5 with 32.
+// Items of a call before heads share a CTA.  1, 8, 16, 32, 64, 128: 16 requests with long contexts 131, 131, 131, 126, 146, 171 us; one
+// request of 514 tokens 33, 19, 14.2, 13.8, 13.8, 13.8 us.
 constexpr uint32_t FEW8_ITEMS = 32;
 constexpr float FEW8_SLACK = 6.f;        // how far, in powers of two, a score may pass the maximum in use
 
@@ -654,7 +655,7 @@ int launch_few8(gift_ctx* c, Attn8Args& a, cudaStream_t st)
     a.tile_rows = L::rows;
     a.by_tile_rows = fixed_div(a.tile_rows);
     a.least = 1;
-    a.extra = 4;                             // a decode step with 0, 2, 4, 8, 16: 129, 124, 120, 122, 130 us
+    a.extra = 4;                             // a decode step with 0, 2, 4, 8, 16: 129, 124, 120, 122, 130 us, at the time
     // Heads lie next to one another in a token, so warps that take the heads of the same tokens read longer runs of memory
     // at a time; but with few items in a call, fewer heads in each mean fewer pieces for one CTA to join.
     a.head_ways = L::warps;
@@ -725,7 +726,8 @@ int launch_attn8(gift_ctx* c, Attn8Args& a, cudaStream_t st)
     // what the tensor map of q does not describe: groups of more heads than a tile has rows, a q whose rows or heads
     // share memory
     const bool plain_q = a.group <= (uint32_t)TC8_ROWS && (a.n_rows == 1 || a.q_row > 0) && (a.heads == 1 || a.q_head > 0);
-    // rows of an average request's K/V head; 17 to 24 of them: 633 us with tcgen05 products, 690 with two items of 16
+    // Rows of an average request's K/V head decide for the whole call; 17 to 24 of them: 633 us with tcgen05 products, 690 with two items of 16,
+    // at the time.  A call that mixes prompts and decode rows pays for it (64 decode rows and a prompt of 2 048: 625 us, apart 121 and 150).
     const uint64_t rows = ((uint64_t)a.n_rows + a.b.n_req - 1) / a.b.n_req * a.group;
     if (rows <= 8) return near ? launch_few8<D, 1, true>(c, a, st) : launch_few8<D, 1, false>(c, a, st);
     if (rows <= 16 || !plain_q) return near ? launch_few8<D, 2, true>(c, a, st) : launch_few8<D, 2, false>(c, a, st);

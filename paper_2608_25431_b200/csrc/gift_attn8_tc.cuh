@@ -12,10 +12,11 @@
 //              bf16 queries become fp16 in place, by a power of two of the row's own too.
 // A code of NaN in a V whose token may be hidden from some row becomes 0, and the rows that see the token get their NaN at the piece's end: what
 // a hidden token holds does not matter.
-// 48 trees of 1 to 64 rows, 4 query heads to one, contexts of up to 16 384 tokens: 532 to 564 us, 370 to 392 TFLOP/s of the
-// rows that exist; all of 64 rows: 694 us, 599 TFLOP/s; prompt chunks of 300 to 512 tokens, 8 requests: 202 us, capped 267 to 273.  What bounds it is a tile's
+// 48 trees of 1 to 64 rows, 4 query heads to one, contexts of up to 16 384 tokens: 531 to 560 us, 373 to 393 TFLOP/s of the
+// rows that exist; all of 64 rows: 740 us, 561 TFLOP/s; prompt chunks of 300 to 512 tokens, 8 requests: 194 us, capped 259 to 268, with scores that reach
+// the cap 370.  What bounds it is a tile's
 // chain through the softmax: of 128 rows and 64 tokens it takes a warp 2 200 to 3 300 clocks, with two such warps on
-// a scheduler; issue slots are 41 % taken, the tensor pipe 29 %, HBM 37 %.
+// a scheduler; issue slots are 43 % taken, the tensor pipe 30 %, HBM 36 %.
 // Every wait is bounded; a CTA whose wait runs out notes its unfinished requests, and the joining kernel makes them zero.
 #pragma once
 #include "gift_attn8.cuh"
@@ -376,7 +377,7 @@ attn8_tc_kernel(const __grid_constant__ Attn8Args a, const __grid_constant__ CUt
                 ok = n == 0 || (kv ? warp_wait(&sh.o_done[(n - 1) & 1u], ((n - 1) >> 1) & 1u, dead, a) : warp_wait(&sh.s_done, (n - 1) & 1u, dead, a));
                 if (!ok) break;
                 // A part's codes are loaded at once (one by one it is a chain of latencies), but the parts share their instructions: the
-                // roles' loops together are about what the instruction cache holds (whole tiles of rows 710 -> 694 us).
+                // roles' loops together are about what the instruction cache holds (whole tiles of rows 710 -> 694 us at the time).
 #pragma unroll 1
                 for (int part = 0; part < PARTS; part++) {
                     uint4 x[LOADS / PARTS];

@@ -49,8 +49,9 @@ template <> __device__ __forceinline__ uint32_t pack_pair<__half>(float lo, floa
 // against one another, so that a pair never leaves its lane.  The 8 angles of a lane are the same for all heads of a
 // row: the warp's groups work out a share each and hand them round.  A warp takes the heads of a row kind by kind, so
 // that its weights stay in registers, all of them where rows abound, a share where they do not.
-// 32 700 rows of 32 + 2 x 8 heads of 128 to 8 bits: 316 us, 4.2 TB/s, 65 % of a copy; 64 rows 6.5 us.  What bounds it is the chain of
-// a head's instructions with 16 warps on an SM: with 4 heads under way 347 us, with more warps of fewer registers 390 to 583.
+// 32 700 rows of 32 + 2 x 32 heads of 128 to 8 bits: 316 us, 4.3 TB/s, 65 % of a copy; 256 rows 6.5 us.  What bounds it is the chain of
+// a head's instructions with 16 warps on an SM (with 4 heads under way 347 us, with more warps of fewer registers 390 to 583), and accesses of
+// 8 and 4 bytes, also to neighbours: L1 is asked for a sector more than once.
 
 struct WriteArgs {
     const char *q, *k, *v;
@@ -406,7 +407,7 @@ void launch_write(const WriteArgs& a, bool pool8, bool paired, uint32_t lanes, u
 // ---------------------------------------------------------------------------
 //
 // The same copy the other way: a thread takes 8 elements of K and of V of a head, 2 such places at a time (one at a time: 237 us).
-// 41 000 tokens of 8 heads of 128 from 8 bits: 182 us, 5.6 TB/s, 85 % of a copy.
+// 41 000 tokens of 32 heads of 128 from 8 bits: 182 us, 5.6 TB/s, 85 % of a copy.
 
 struct ReadArgs {
     const char* pages;
